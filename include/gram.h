@@ -299,6 +299,59 @@ gram_status gram_window_reset(gram_ctx* ctx, gram_stream stream);
  * [ceil(n_items/32)], cache fp32 [n_items, d] (converted).  NULL skips one. */
 gram_status gram_get_window(gram_ctx* ctx, float* h_table, uint32_t* h_touched, float* h_cache);
 
+/* --- answers over a pool, and learning from them -----------------------------
+ * Where the task module of Section 3.1 scores a few candidates, a deployed model answers over the whole pool (Table 3:
+ * 2.6k to 104k items) or the encoder's vocabulary, and a smaller encoder is trained on a larger one's answers.  A row of
+ * logits z[v], v < V, is scaled first, x = scale * z (scale finite and > 0: one over the temperature).  A place at -inf is
+ * masked out: it has no probability, is never an alternative, and a gradient there is 0.  In a row with nothing left
+ * log probabilities are -inf, the entropy is 0, there are no alternatives, and all gradients are 0.  A row that holds NaN or
+ * +inf has NaN statistics, log probabilities, entropy, loss and gradients (alternatives: the largest of its other entries
+ * and +inf, with log probability NaN).
+ * Logits are [N, V] of `dtype` (GRAM_F32 or GRAM_BF16), `ld` elements between rows (ld >= V), at any address and stride that
+ * the type allows; 1 <= V, 0 <= N < 2^31.  All other arrays are contiguous.  Sums and statistics are held in fp32.
+ * The work's order is fixed by the sizes and addresses' alignment: repeated calls give bit-identical results.
+ * Token IDs are int32 in [0, V), or -1 for "none"; another value records GRAM_ERR_ID_RANGE and counts as -1.
+ * No call needs a module in the context, and none allocates. */
+enum { GRAM_TOP_MAX = 128 };             /* most given tokens (C), alternatives and teacher entries (k) of a row */
+
+/* Per row n, each part only where its array is given:
+ *   d_logp    [N, C]  log probability of d_targets[n, c]; 0 for "none"             (both arrays for C > 0)
+ *   d_stats   [N, 2]  the largest logit m (not scaled), and log sum_v exp(scale (z[v] - m)); what the gradient needs
+ *   d_entropy [N]     -sum_v p_v log p_v
+ *   d_top_ids [N, k], d_top_logp [N, k]  the k largest logits, largest first, equal ones by ascending place, and their log
+ *                     probabilities; ID -1 and -inf where fewer are left          (both arrays for k > 0)
+ * One pass over the logits. */
+gram_status gram_logprobs(gram_ctx* ctx, const void* d_logits, int dtype, int64_t ld, int64_t N, int32_t V, float scale,
+                          const int32_t* d_targets, int32_t C, float* d_logp, float* d_stats, float* d_entropy,
+                          float* d_top_logp, int32_t* d_top_ids, int32_t k, gram_stream stream);
+/* The gradient of sum_nc dlogp[n, c] logp[n, c] + sum_n dentropy[n] H_n with respect to the logits:
+ *   d_dlogits[n, v] = scale (sum of dlogp[n, c] over d_targets[n, c] = v - p_v (sum_c dlogp[n, c] + dentropy[n] (log p_v + H_n)))
+ * with d_stats and d_entropy (needed with d_dentropy) as gram_logprobs wrote them.  d_dlogp [N, C] may be NULL for C = 0,
+ * d_dentropy [N] may be NULL.  A given token at a masked place takes no part.  d_dlogits has the logits' type and rows
+ * ld_out elements apart; it may be d_logits itself with the same ld, else the two must not overlap. */
+gram_status gram_logprobs_backward(gram_ctx* ctx, const void* d_logits, int dtype, int64_t ld, int64_t N, int32_t V, float scale,
+                                   const int32_t* d_targets, int32_t C, const float* d_stats, const float* d_entropy,
+                                   const float* d_dlogp, const float* d_dentropy, void* d_dlogits, int64_t ld_out,
+                                   gram_stream stream);
+/* Distillation from a teacher's top logits: d_teacher_ids, d_teacher_logits [N, k] are a row's best entries by the teacher
+ * (logits or log probabilities: gram_logprobs' alternatives as they stand).  An entry takes no part if its ID is -1, its own
+ * logit is -inf, or the student's logit there is masked out.  With q the softmax of scale * teacher logits over the entries
+ * left (entries of one place add up) and p the student's softmax over the whole row,
+ *   d_loss[n] = sum_j q_j (log q_j - log p(id_j)),     0 where no entry is left
+ *   d_dlogits[n, v] = weight[n] scale (p_v - sum of q_j over id_j = v),  the gradient of sum_n weight[n] loss[n]
+ * d_weight [N] may be NULL (all 1); a row of weight 0 has a gradient of 0 whatever its logits.  d_dlogits may be NULL (loss
+ * only); else as in gram_logprobs_backward. */
+gram_status gram_distill(gram_ctx* ctx, const void* d_logits, int dtype, int64_t ld, int64_t N, int32_t V, float scale,
+                         const int32_t* d_teacher_ids, const float* d_teacher_logits, int32_t k, float* d_loss,
+                         const float* d_weight, void* d_dlogits, int64_t ld_out, gram_stream stream);
+/* gram_logprobs of z[n, v] = users[n, :] . items[v, :] + bias[v] without the logits ever being written: d_users bf16 [N, d]
+ * and d_items bf16 [V, d] with rows ld_users and ld_items elements apart (multiples of 8, addresses 16-byte aligned: else
+ * GRAM_ERR_UNSUPPORTED), d_bias fp32 [V] or NULL (-inf takes an item out), products summed in fp32. */
+gram_status gram_score_logprobs(gram_ctx* ctx, const void* d_users, int64_t ld_users, const void* d_items, int64_t ld_items,
+                                const float* d_bias, int64_t N, int32_t V, int32_t d, float scale, const int32_t* d_targets,
+                                int32_t C, float* d_logp, float* d_stats, float* d_entropy, float* d_top_logp,
+                                int32_t* d_top_ids, int32_t k, gram_stream stream);
+
 /* --- checkpoint / resume (the paper keeps the checkpoint of the best validation epoch, Appendix D) ------------------
  * Everything a context holds besides what the caller gave it: parameters (gram_get_params / gram_set_params), the
  * optimiser's state, and for K > 1 the open window.  Exported by one context and imported into another context of the

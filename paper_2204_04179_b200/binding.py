@@ -22,6 +22,7 @@ GRAM_TASK_NONE, GRAM_TASK_KT, GRAM_TASK_NR = 0, 1, 2
 GRAM_MODULE_CE, GRAM_MODULE_TASK = 0, 1
 GRAM_OPT_SGD, GRAM_OPT_ADAM = 0, 1
 GRAM_MULTI_TABLE, GRAM_MULTI_PSEUDO_TARGET = 0, 1
+GRAM_TOP_MAX = 128
 STATUS = {0: "GRAM_OK", 1: "GRAM_ERR_ARG", 2: "GRAM_ERR_ID_RANGE", 3: "GRAM_ERR_WORKSPACE", 4: "GRAM_ERR_UNSUPPORTED",
           5: "GRAM_ERR_CUDA", 6: "GRAM_ERR_TIMEOUT"}
 
@@ -35,7 +36,7 @@ SYMBOLS = ["gram_create", "gram_destroy", "gram_sync", "gram_last_error", "gram_
            "gram_launch_count", "gram_profile_dump", "gram_accumulate_static", "gram_optimizer_step",
            "gram_optimizer_reset", "gram_noam_rate", "gram_adam_update", "gram_state_export", "gram_state_import",
            "gram_optimizer_export", "gram_optimizer_import", "gram_selftest_bounded_wait", "gram_selftest_ring_rows", "gram_selftest_cluster_blocks", "gram_selftest_column_sums", "gram_grads_device",
-           "gram_gemm_bf16_epilogue"]
+           "gram_gemm_bf16_epilogue", "gram_logprobs", "gram_logprobs_backward", "gram_distill", "gram_score_logprobs"]
 
 KINDS = ["gemm", "attention", "layernorm", "colsum", "embed_pool", "dedup", "gather", "accumulate", "task_head", "other",
          "optimizer"]
@@ -125,6 +126,25 @@ def _ptr(t) -> C.c_void_p:
         return C.c_void_p(t.ctypes.data)
     assert t.is_contiguous()
     return C.c_void_p(t.data_ptr())
+
+
+def _rows(t):
+    """(address, dtype, elements between rows) of a matrix whose rows are contiguous but may lie further apart."""
+    import torch
+    assert t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1), "rows must be contiguous"
+    assert t.dtype in (torch.float32, torch.bfloat16)
+    ld = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return C.c_void_p(t.data_ptr()), GRAM_F32 if t.dtype == torch.float32 else GRAM_BF16, C.c_int64(ld)
+
+
+def _width(t) -> int:
+    return 0 if t is None else t.shape[1]
+
+
+def _check(t, dtype, *shape):
+    """An array that a call takes as contiguous, of this type and shape; None passes."""
+    if t is not None:
+        assert t.dtype == dtype and tuple(t.shape) == shape, (t.dtype, tuple(t.shape), dtype, shape)
 
 
 def _stream(stream) -> C.c_void_p:
@@ -262,6 +282,59 @@ class Gram:
 
     def task(self, E, labels, B, dE, loss, stream=None):
         self._ck(lib().gram_task(self._h, _ptr(E), _ptr(labels), C.c_int32(B), _ptr(dE), _ptr(loss), _stream(stream)))
+
+    # answers over a pool, and learning from them: logits [N, V] fp32 or bf16, rows may lie further apart
+    def _answers(self, N, targets, logp, stats, entropy, top_logp, top_ids):
+        import torch
+        _check(targets, torch.int32, N, _width(targets)); _check(logp, torch.float32, N, _width(targets))
+        _check(stats, torch.float32, N, 2); _check(entropy, torch.float32, N)
+        _check(top_ids, torch.int32, N, _width(top_ids)); _check(top_logp, torch.float32, N, _width(top_ids))
+        return (_ptr(targets), C.c_int32(_width(targets)), _ptr(logp), _ptr(stats), _ptr(entropy), _ptr(top_logp), _ptr(top_ids),
+                C.c_int32(_width(top_ids)))
+
+    def logprobs(self, logits, scale=1.0, targets=None, logp=None, stats=None, entropy=None, top_logp=None, top_ids=None, stream=None):
+        p, dtype, ld = _rows(logits)
+        N, V = logits.shape
+        self._ck(lib().gram_logprobs(self._h, p, C.c_int(dtype), ld, C.c_int64(N), C.c_int32(V), C.c_float(scale),
+                                     *self._answers(N, targets, logp, stats, entropy, top_logp, top_ids), _stream(stream)))
+
+    def logprobs_backward(self, logits, stats, dlogits, scale=1.0, targets=None, dlogp=None, entropy=None, dentropy=None, stream=None):
+        import torch
+        p, dtype, ld = _rows(logits)
+        q, dtype_out, ld_out = _rows(dlogits)
+        N, V = logits.shape
+        assert dlogits.shape == logits.shape and dtype_out == dtype
+        _check(targets, torch.int32, N, _width(targets)); _check(dlogp, torch.float32, N, _width(targets))
+        _check(stats, torch.float32, N, 2); _check(entropy, torch.float32, N); _check(dentropy, torch.float32, N)
+        self._ck(lib().gram_logprobs_backward(self._h, p, C.c_int(dtype), ld, C.c_int64(N), C.c_int32(V), C.c_float(scale), _ptr(targets),
+                                              C.c_int32(_width(targets)), _ptr(stats), _ptr(entropy), _ptr(dlogp), _ptr(dentropy), q, ld_out,
+                                              _stream(stream)))
+
+    def distill(self, logits, teacher_ids, teacher_logits, loss, scale=1.0, weight=None, dlogits=None, stream=None):
+        import torch
+        p, dtype, ld = _rows(logits)
+        N, V = logits.shape
+        q, ld_out = C.c_void_p(0), C.c_int64(0)
+        if dlogits is not None:
+            q, dtype_out, ld_out = _rows(dlogits)
+            assert dlogits.shape == logits.shape and dtype_out == dtype
+        k = teacher_ids.shape[1]
+        _check(teacher_ids, torch.int32, N, k); _check(teacher_logits, torch.float32, N, k)
+        _check(loss, torch.float32, N); _check(weight, torch.float32, N)
+        self._ck(lib().gram_distill(self._h, p, C.c_int(dtype), ld, C.c_int64(N), C.c_int32(V), C.c_float(scale), _ptr(teacher_ids),
+                                    _ptr(teacher_logits), C.c_int32(k), _ptr(loss), _ptr(weight), q, ld_out, _stream(stream)))
+
+    def score_logprobs(self, users, items, bias=None, scale=1.0, targets=None, logp=None, stats=None, entropy=None, top_logp=None,
+                       top_ids=None, stream=None):
+        import torch
+        p, dtype, ld = _rows(users)
+        q, dtype_items, ld_items = _rows(items)
+        assert dtype == GRAM_BF16 and dtype_items == GRAM_BF16 and users.shape[1] == items.shape[1]
+        (N, d), V = users.shape, items.shape[0]
+        _check(bias, torch.float32, V)
+        self._ck(lib().gram_score_logprobs(self._h, p, ld, q, ld_items, _ptr(bias), C.c_int64(N), C.c_int32(V), C.c_int32(d),
+                                           C.c_float(scale), *self._answers(N, targets, logp, stats, entropy, top_logp, top_ids),
+                                           _stream(stream)))
 
     def encoder_backward(self, G, items, U, stream=None):
         self._ck(lib().gram_encoder_backward(self._h, _ptr(G), _ptr(items), C.c_int32(U), _stream(stream)))

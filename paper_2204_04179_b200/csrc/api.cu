@@ -1,4 +1,5 @@
 // The C ABI of libgram: context life cycle, argument checks, and the calls of include/gram.h.
+#include <math.h>
 #include <stdarg.h>
 
 #include <new>
@@ -7,6 +8,7 @@
 #include "gram_internal.h"
 #include "model.h"
 #include "layers.h"
+#include "logits.h"
 
 constexpr int kProfSlots = 16384;
 struct ProfRec {
@@ -457,6 +459,103 @@ gram_status gram_gemm_bf16_epilogue(gram_ctx* ctx, const void* d_A, int a_kmajor
   }
   return gemm_launch(ctx, &ctx->gws, GRAM_BF16, d_A, a_kmajor, a_kmajor ? K : M, d_B, b_kmajor, b_kmajor ? K : N, d_C,
                      c_f32, N, M, N, K, e, 0, S(stream));
+}
+
+// ---- answers over a pool -------------------------------------------------------------------
+#define ROWS_ARG(cond, what) \
+  if (!(cond)) return gram_set_error(ctx, "%s: %s", name, what), GRAM_ERR_ARG;
+
+static gram_status check_rows(gram_ctx* ctx, const char* name, int64_t N, int32_t V, float scale) {
+  ROWS_ARG(N >= 0 && N <= INT32_MAX, "N must be in [0, 2^31)");
+  ROWS_ARG(V >= 1, "V must be positive");
+  ROWS_ARG(isfinite(scale) && scale > 0.f, "scale must be finite and positive");
+  return GRAM_OK;
+}
+static gram_status check_logits(gram_ctx* ctx, const char* name, const void* p, int dtype, int64_t ld, int64_t N, int32_t V) {
+  ROWS_ARG(dtype == GRAM_F32 || dtype == GRAM_BF16, "unknown dtype");
+  ROWS_ARG(p || N == 0, "null logits or gradient");
+  ROWS_ARG(ld >= V && ld <= INT64_MAX / 8 / (N > 0 ? N : 1), "rows must be at least V elements apart");
+  ROWS_ARG(reinterpret_cast<uintptr_t>(p) % (dtype == GRAM_F32 ? 4 : 2) == 0, "an address that the type does not allow");
+  return GRAM_OK;
+}
+static gram_status check_answers(gram_ctx* ctx, const char* name, const RowAnswers& ask, int64_t N) {
+  ROWS_ARG(ask.C >= 0 && ask.C <= GRAM_TOP_MAX, "C must be in [0, 128]");
+  ROWS_ARG(ask.k >= 0 && ask.k <= GRAM_TOP_MAX, "k must be in [0, 128]");
+  ROWS_ARG(N == 0 || ask.C == 0 || (ask.targets && ask.logp), "given tokens need both arrays");
+  ROWS_ARG(N == 0 || ask.k == 0 || (ask.top_ids && ask.top_logp), "alternatives need both arrays");
+  return GRAM_OK;
+}
+// a gradient may take the logits' own place, row on row; another overlap would be overwritten before it is read
+static gram_status check_overlap(gram_ctx* ctx, const char* name, const void* z, int64_t ld, const void* dz, int64_t ld_out, int dtype,
+                                 int64_t N, int32_t V) {
+  const int64_t size = dtype == GRAM_F32 ? 4 : 2;
+  const uintptr_t a = reinterpret_cast<uintptr_t>(z), b = reinterpret_cast<uintptr_t>(dz);
+  const uintptr_t a_end = a + (uintptr_t)(((N - 1) * ld + V) * size), b_end = b + (uintptr_t)(((N - 1) * ld_out + V) * size);
+  ROWS_ARG(N == 0 || (a == b && (ld == ld_out || N == 1)) || a_end <= b || b_end <= a, "the gradient overlaps the logits");
+  return GRAM_OK;
+}
+
+gram_status gram_logprobs(gram_ctx* ctx, const void* d_logits, int dtype, int64_t ld, int64_t N, int32_t V, float scale,
+                          const int32_t* d_targets, int32_t C, float* d_logp, float* d_stats, float* d_entropy,
+                          float* d_top_logp, int32_t* d_top_ids, int32_t k, gram_stream stream) {
+  if (!ctx) return GRAM_ERR_ARG;
+  const char* name = "gram_logprobs";
+  const RowAnswers ask{d_targets, d_logp, d_stats, d_entropy, d_top_logp, d_top_ids, C, k};
+  GRAM_TRY(check_rows(ctx, name, N, V, scale));
+  GRAM_TRY(check_logits(ctx, name, d_logits, dtype, ld, N, V));
+  GRAM_TRY(check_answers(ctx, name, ask, N));
+  return logprobs_launch(ctx, d_logits, dtype, ld, N, V, scale, ask, S(stream));
+}
+gram_status gram_logprobs_backward(gram_ctx* ctx, const void* d_logits, int dtype, int64_t ld, int64_t N, int32_t V, float scale,
+                                   const int32_t* d_targets, int32_t C, const float* d_stats, const float* d_entropy,
+                                   const float* d_dlogp, const float* d_dentropy, void* d_dlogits, int64_t ld_out,
+                                   gram_stream stream) {
+  if (!ctx) return GRAM_ERR_ARG;
+  const char* name = "gram_logprobs_backward";
+  GRAM_TRY(check_rows(ctx, name, N, V, scale));
+  GRAM_TRY(check_logits(ctx, name, d_logits, dtype, ld, N, V));
+  GRAM_TRY(check_logits(ctx, name, d_dlogits, dtype, ld_out, N, V));
+  GRAM_TRY(check_overlap(ctx, name, d_logits, ld, d_dlogits, ld_out, dtype, N, V));
+  ROWS_ARG(C >= 0 && C <= GRAM_TOP_MAX, "C must be in [0, 128]");
+  ROWS_ARG(N == 0 || C == 0 || (d_targets && d_dlogp), "given tokens need both arrays");
+  ROWS_ARG(N == 0 || d_stats, "null d_stats");
+  ROWS_ARG(N == 0 || !d_dentropy || d_entropy, "the entropy's gradient needs the entropy");
+  return logprobs_backward_launch(ctx, d_logits, dtype, ld, N, V, scale, d_targets, C, d_stats, d_entropy, d_dlogp, d_dentropy,
+                                  d_dlogits, ld_out, S(stream));
+}
+gram_status gram_distill(gram_ctx* ctx, const void* d_logits, int dtype, int64_t ld, int64_t N, int32_t V, float scale,
+                         const int32_t* d_teacher_ids, const float* d_teacher_logits, int32_t k, float* d_loss,
+                         const float* d_weight, void* d_dlogits, int64_t ld_out, gram_stream stream) {
+  if (!ctx) return GRAM_ERR_ARG;
+  const char* name = "gram_distill";
+  GRAM_TRY(check_rows(ctx, name, N, V, scale));
+  GRAM_TRY(check_logits(ctx, name, d_logits, dtype, ld, N, V));
+  if (d_dlogits) {
+    GRAM_TRY(check_logits(ctx, name, d_dlogits, dtype, ld_out, N, V));
+    GRAM_TRY(check_overlap(ctx, name, d_logits, ld, d_dlogits, ld_out, dtype, N, V));
+  }
+  ROWS_ARG(k >= 1 && k <= GRAM_TOP_MAX, "k must be in [1, 128]");
+  ROWS_ARG(N == 0 || (d_teacher_ids && d_teacher_logits && d_loss), "null buffer");
+  return distill_launch(ctx, d_logits, dtype, ld, N, V, scale, d_teacher_ids, d_teacher_logits, k, d_loss, d_weight, d_dlogits,
+                        ld_out, S(stream));
+}
+gram_status gram_score_logprobs(gram_ctx* ctx, const void* d_users, int64_t ld_users, const void* d_items, int64_t ld_items,
+                                const float* d_bias, int64_t N, int32_t V, int32_t d, float scale, const int32_t* d_targets,
+                                int32_t C, float* d_logp, float* d_stats, float* d_entropy, float* d_top_logp,
+                                int32_t* d_top_ids, int32_t k, gram_stream stream) {
+  if (!ctx) return GRAM_ERR_ARG;
+  const char* name = "gram_score_logprobs";
+  const RowAnswers ask{d_targets, d_logp, d_stats, d_entropy, d_top_logp, d_top_ids, C, k};
+  GRAM_TRY(check_rows(ctx, name, N, V, scale));
+  GRAM_TRY(check_answers(ctx, name, ask, N));
+  ROWS_ARG(d >= 1 && ld_users >= d && ld_items >= d, "rows must be at least d elements apart, d positive");
+  ROWS_ARG(ld_items <= INT64_MAX / 8 / V && ld_users <= INT64_MAX / 8 / (N > 0 ? N : 1), "rows too far apart");
+  ROWS_ARG(N == 0 || (d_users && d_items), "null vectors");
+  if (ld_users % 8 || ld_items % 8 || reinterpret_cast<uintptr_t>(d_users) % 16 || reinterpret_cast<uintptr_t>(d_items) % 16)
+    return gram_set_error(ctx, "%s: vectors must be 16-byte aligned, rows a multiple of 8 elements apart", name), GRAM_ERR_UNSUPPORTED;
+  if (N == 0) return GRAM_OK;
+  return score_logprobs_launch(ctx, d_users, ld_users, d_items, ld_items, d_bias, N, V, d, scale, ask, ctx->gws.splitk,
+                               ctx->gws.splitk_bytes, S(stream));
 }
 
 }  // extern "C"
