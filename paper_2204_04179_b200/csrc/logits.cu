@@ -1,4 +1,12 @@
 // Answers read from rows of logits, and their gradients (gram_logprobs, gram_logprobs_backward, gram_distill).
+//
+// All three are bound by the bytes of the logits: each is read once, and a gradient is written once.  A row belongs to a
+// group of threads, a warp for short rows (eight rows a block) or a block of 256, and where a row is long or rows are few,
+// to a cluster of up to 16 blocks with a contiguous slice each, whose statistics meet in distributed shared memory.  Rows
+// begin anywhere (a stride of 30 522 bf16 leaves them on 4-byte boundaries): the places up to the first 16-byte boundary
+// and after the last are single elements of the slice's first threads, all others move 16 bytes at a time.
+#include <float.h>
+
 #include "logits.h"
 #include "row_softmax.cuh"
 
@@ -6,59 +14,446 @@ namespace {
 
 constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32;
 
-// the block's statistics, in every thread
-__device__ __forceinline__ RowStat join_block(RowStat r, float c, RowStat* part) {
-  r = row_join_warp(r, c);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = r;
-  __syncthreads();
-  r = part[0];
-  for (int w = 1; w < LP_WARPS; ++w) r = row_join(r, part[w], c);
-  return r;
-}
-template <typename T> __device__ __forceinline__ RowStat row_statistics(const T* z, int V, float c, RowStat* part) {
-  RowStat r = row_empty();
-  for (int v = threadIdx.x; v < V; v += LP_THREADS) row_add(r, row_load(z + v), c);
-  return join_block(r, c, part);
+// ------------------------------ groups of threads that own a row ------------------------------------------------------
+// TPR threads a row: a warp, or the block.  All threads of a group call these together.
+template <int TPR> struct Group {
+  static constexpr int ROWS = LP_THREADS / TPR;
+  static_assert(TPR == 32 || TPR == LP_THREADS, "a warp or the block");
+  static __device__ __forceinline__ int tid() { return threadIdx.x % TPR; }
+  static __device__ __forceinline__ int row() { return threadIdx.x / TPR; }
+  static __device__ __forceinline__ void sync() {
+    if constexpr (TPR == 32) __syncwarp();
+    else __syncthreads();
+  }
+  static __device__ __forceinline__ int count(bool p) {        // also a barrier
+    if constexpr (TPR == 32) return __popc(__ballot_sync(0xffffffffu, p));
+    else return __syncthreads_count(p);
+  }
+  static __device__ __forceinline__ int sum(int v, int* part) {
+    v = __reduce_add_sync(0xffffffffu, v);
+    if constexpr (TPR > 32) {
+      __syncthreads();
+      if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+      __syncthreads();
+      v = 0;
+#pragma unroll
+      for (int w = 0; w < LP_WARPS; ++w) v += part[w];
+    }
+    return v;
+  }
+  // the group's statistics in all its threads, joined in the same order everywhere
+  static __device__ __forceinline__ RowStat join(RowStat r, float c, RowStat* part) {
+    r = row_join_lanes<32>(r, c);
+    if constexpr (TPR > 32) {
+      __syncthreads();
+      if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = r;
+      __syncthreads();
+      r = row_join_lanes<LP_WARPS>(part[threadIdx.x & (LP_WARPS - 1)], c);
+    }
+    return r;
+  }
+  // two at once
+  static __device__ __forceinline__ void join(RowStat& r, RowStat& q, float c, RowStat (*part)[2]) {
+    r = row_join_lanes<32>(r, c);
+    q = row_join_lanes<32>(q, c);
+    if constexpr (TPR > 32) {
+      __syncthreads();
+      if ((threadIdx.x & 31) == 0) { part[threadIdx.x >> 5][0] = r; part[threadIdx.x >> 5][1] = q; }
+      __syncthreads();
+      r = row_join_lanes<LP_WARPS>(part[threadIdx.x & (LP_WARPS - 1)][0], c);
+      q = row_join_lanes<LP_WARPS>(part[threadIdx.x & (LP_WARPS - 1)][1], c);
+    }
+  }
+  static __device__ __forceinline__ float sum(float v, float* part) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if constexpr (TPR > 32) {
+      __syncthreads();
+      if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+      __syncthreads();
+      v = 0.f;
+#pragma unroll
+      for (int w = 0; w < LP_WARPS; ++w) v += part[w];
+    }
+    return v;
+  }
+};
+
+// ------------------------------ a slice of a row ----------------------------------------------------------------------
+// Places [0, head) and [tail, V) are single elements, of the first and the last slice; the vectors between them are split
+// evenly: a slice holds vectors [v0, v1), vector v the places head + v N ..
+template <typename T> struct Slice {
+  static constexpr int N = RowVec<T>::N;
+  const T* z;                    // the row
+  int head, tail, V, v0, v1;
+  bool first, last;
+  __device__ __forceinline__ Slice(const T* row, int V_, int rank, int slices) : z(row), V(V_), first(rank == 0), last(rank == slices - 1) {
+    const int past = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+    head = min(past ? N - past : 0, V);
+    const int nv = (V - head) / N;
+    tail = head + nv * N;
+    const int per = (nv + slices - 1) / slices;
+    v0 = min(rank * per, nv);
+    v1 = min(v0 + per, nv);
+  }
+  // A thread's single element: threads 0 .. 7 those at the row's start, 8 .. 15 those at its end.  -1: none
+  __device__ __forceinline__ int edge(int tid) const {
+    if (tid < 8) return first && tid < head ? tid : -1;
+    return last && tid < 16 && tail + tid - 8 < V ? tail + tid - 8 : -1;
+  }
+  __device__ __forceinline__ int place(int v) const { return head + v * N; }
+  __device__ __forceinline__ uint4 load(int v) const { return __ldcs(reinterpret_cast<const uint4*>(z + head) + v); }
+  __device__ __forceinline__ bool has(int p) const {
+    if (p < head) return first;
+    if (p >= tail) return last;
+    return p >= place(v0) && p < place(v1);
+  }
+  template <int TPR, int NV> __device__ __forceinline__ int chunks() const { return max(1, (v1 - v0 + TPR * NV - 1) / (TPR * NV)); }
+  template <int TPR, int NV> __device__ __forceinline__ void load_chunk(int ch, int tid, uint4 (&q)[NV]) const {
+    const int v = v0 + ch * (TPR * NV) + tid;
+    if (v - tid + TPR * NV <= v1) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) q[i] = load(v + i * TPR);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        constexpr uint32_t none = RowVec<T>::NONE;
+        q[i] = make_uint4(none, none, none, none);
+        if (v + i * TPR < v1) q[i] = load(v + i * TPR);
+      }
+    }
+  }
+};
+template <typename T, int NV> __device__ __forceinline__ float chunk_top(const uint4 (&q)[NV]) {
+  float top = ROW_NEG_INF;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) top = fmaxf(top, RowVec<T>::top(q[i]));
+  return top;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(const T* logits, int64_t ld, int32_t V, float scale, RowAnswers ask,
-                                                              int32_t* status) {
+// the same address in another block of the cluster
+__device__ __forceinline__ uint32_t in_block(const void* p, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void put_stat(RowStat* p, uint32_t rank, const RowStat& r) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0+4], %2;\n\tst.shared::cluster.f32 [%0+8], %3;" ::"r"(in_block(p, rank)),
+               "f"(r.m), "f"(r.s), "f"(r.t)
+               : "memory");
+}
+__device__ __forceinline__ void put_key(uint64_t* p, uint32_t rank, uint64_t key) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(in_block(p, rank)), "l"(key) : "memory");
+}
+constexpr int MAX_SLICES = 16;
+// the slices' statistics, joined in the same order everywhere
+__device__ __forceinline__ RowStat join_slices(const RowStat* of, int slices, float c) {
+  const int i = threadIdx.x & (MAX_SLICES - 1);
+  return row_join_lanes<MAX_SLICES>(i < slices ? of[i] : row_empty(), c);
+}
+
+// ------------------------------ the best k places of a slice ----------------------------------------------------------
+// Candidates are kept as keys (row_key: larger logit first, then lower place) in shared memory, in no order.  The first
+// chunk sets a bar: the k-th largest of the threads' maxima, or a little below; k entries at least reach it.  An entry below
+// the bar is not among the best k, and once k entries have reached it neither is a later one that equals it, since slices
+// are read in ascending order.  So of a chunk only a few entries are looked at twice.  Where more than half the list fills,
+// it is cut to its best k, the last of which sets the new bar; a chunk that would overflow the list (equal logits, ascending
+// rows) gives its own best k, found by bisection over the keys.
+template <int TPR> struct TopList {
+  static constexpr int CAP = TPR == 32 ? 384 : 1024;
+  static_assert(CAP >= 4 * GRAM_TOP_MAX || TPR == 32 && CAP >= 3 * GRAM_TOP_MAX, "a list past its half holds more than k");
+  uint64_t keys[CAP];
+  int added[3];                  // entries of a chunk; three in turn, so that one is cleared while none looks at it
+  int slow;
+  int part[LP_WARPS];
+  uint32_t lowest[LP_WARPS], highest[LP_WARPS];
+};
+
+template <typename T, int TPR, int NV> struct TopChunk {
+  const uint4 (&q)[NV];
+  int place0;                    // of this thread's first vector
+  float edge;                    // this thread's single element, -inf without one
+  int edge_place;
+  // f(logit, place) of each entry of this thread's part of the chunk
+  template <typename F> __device__ __forceinline__ void each(F f) const {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < RowVec<T>::N / 2; ++j) {
+        const float2 x = x2_unpack(RowVec<T>::pair(q[i], j));
+        const int p = place0 + i * (TPR * RowVec<T>::N) + 2 * j;
+        f(x.x, p);
+        f(x.y, p + 1);
+      }
+    f(edge, edge_place);
+  }
+};
+
+// the largest t such that at least k keys are >= t; there are k at least, at_least(t) counts them
+template <typename F> __device__ __forceinline__ uint64_t kth_key(int k, F at_least) {
+  uint64_t lo = 1, hi = ~0ull;
+  while (lo < hi) {
+    const uint64_t mid = hi - (hi - lo) / 2;
+    const int n = at_least(mid);
+    if (n == k) return mid;
+    if (n > k) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+// the first `have` keys of the list (k at least) cut to the best k; returns a bar that only better logits than theirs reach
+template <int TPR> __device__ __noinline__ float top_cut(TopList<TPR>& l, int have, int k) {
+  using G = Group<TPR>;
+  constexpr int PER = TopList<TPR>::CAP / TPR;
+  const int tid = G::tid();
+  uint64_t key[PER], last = ~0ull;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) key[i] = tid + i * TPR < have ? l.keys[tid + i * TPR] : 0;
+  const uint64_t kth = kth_key(k, [&](uint64_t t) {
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) c += key[i] >= t;
+    return G::sum(c, l.part);
+  });
+  if (tid == 0) l.slow = 0;
+  G::sync();
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (key[i] >= kth) {
+      l.keys[atomicAdd(&l.slow, 1)] = key[i];
+      last = min(last, key[i]);
+    }
+  uint32_t low = __reduce_min_sync(0xffffffffu, (uint32_t)(last >> 32));
+  if constexpr (TPR > 32) {
+    if ((threadIdx.x & 31) == 0) l.lowest[threadIdx.x >> 5] = low;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < LP_WARPS; ++w) low = min(low, l.lowest[w]);
+  }
+  G::sync();
+  return row_order_logit(low + 1u);
+}
+// the best k of a chunk's entries of at least `bar` (more than k) behind the list's first `have`
+template <typename T, int TPR, int NV>
+__device__ __noinline__ void top_take_best(TopList<TPR>& l, const TopChunk<T, TPR, NV>& ch, int have, int k, float bar) {
+  using G = Group<TPR>;
+  const uint64_t kth = kth_key(k, [&](uint64_t t) {
+    int c = 0;
+    ch.each([&](float x, int p) { c += x >= bar && row_key(x, p) >= t; });
+    return G::sum(c, l.part);
+  });
+  if (G::tid() == 0) l.slow = have;
+  G::sync();
+  ch.each([&](float x, int p) {
+    if (x >= bar && row_key(x, p) >= kth) l.keys[atomicAdd(&l.slow, 1)] = row_key(x, p);
+  });
+  G::sync();
+}
+
+// the first chunk's bar, from the threads' largest entries
+template <int TPR> __device__ __forceinline__ float top_first_bar(TopList<TPR>& l, float top, int k) {
+  using G = Group<TPR>;
+  const bool some = top > ROW_NEG_INF;
+  const uint32_t o = row_order(top);
+  uint32_t lo = __reduce_min_sync(0xffffffffu, some ? o : 0xffffffffu), hi = __reduce_max_sync(0xffffffffu, some ? o : 0u);
+  if constexpr (TPR > 32) {
+    if ((threadIdx.x & 31) == 0) { l.lowest[threadIdx.x >> 5] = lo; l.highest[threadIdx.x >> 5] = hi; }
+  }
+  if (G::count(some) < k) return -FLT_MAX;              // a barrier, for the two arrays too
+  if constexpr (TPR > 32) {
+#pragma unroll
+    for (int w = 0; w < LP_WARPS; ++w) { lo = min(lo, l.lowest[w]); hi = max(hi, l.highest[w]); }
+  }
+  for (int step = 0; lo < hi && step < 12; ++step) {
+    const uint32_t mid = hi - (hi - lo) / 2;
+    const int n = G::count(some && o >= mid);
+    if (n < k) hi = mid - 1;
+    else {
+      lo = mid;
+      if (n <= k + k / 8) break;
+    }
+  }
+  return row_order_logit(lo);
+}
+
+struct TopState {
+  int have;                      // keys in the list
+  float bar;
+  bool reached;                  // k entries have reached the bar: later ones must pass it
+};
+// one chunk's entries into the list; top: the thread's largest
+template <typename T, int TPR, int NV>
+__device__ __forceinline__ void top_chunk(TopList<TPR>& l, TopState& st, const TopChunk<T, TPR, NV>& ch, float top, int k, int number, bool last) {
+  using G = Group<TPR>;
+  constexpr int CAP = TopList<TPR>::CAP;
+  if (number == 0) st.bar = top_first_bar(l, top, k);
+  int* added = &l.added[number % 3];
+  if (top >= st.bar)
+    ch.each([&](float x, int p) {
+      if (x >= st.bar) {
+        const int at = st.have + atomicAdd(added, 1);
+        if (at < CAP) l.keys[at] = row_key(x, p);
+      }
+    });
+  if (G::tid() == 0) l.added[(number + 1) % 3] = 0;
+  G::sync();
+  const int n = *added;
+  if (st.have + n > CAP) {
+    if (st.have > k) (void)top_cut(l, st.have, k);
+    st.have = min(st.have, k);
+    if (n > k) top_take_best(l, ch, st.have, k, st.bar);
+    else top_take_best(l, ch, st.have, n, st.bar);
+    st.have += min(n, k);
+    if (st.have >= k) { st.bar = top_cut(l, st.have, k); st.have = k; st.reached = true; }
+    return;
+  }
+  st.have += n;
+  if (st.have >= k && !st.reached) {
+    st.bar = row_order_logit(row_order(st.bar) + 1u);
+    st.reached = true;
+  }
+  if (st.have > CAP / 2 && !last) {
+    st.bar = top_cut(l, st.have, k);
+    st.have = k;
+    st.reached = true;
+  }
+}
+
+// ------------------------------ log probabilities ---------------------------------------------------------------------
+template <typename T, int TPR, bool TOP>
+__global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const T* logits, int64_t ld, int64_t N, int32_t V, float scale, int32_t slices,
+                                                                 RowAnswers ask, int32_t* status) {
+  using G = Group<TPR>;
+  constexpr int NV = 4;
   if (!chain_begin()) return;
-  __shared__ RowStat part[LP_WARPS];
-  __shared__ uint64_t best[LP_WARPS];
-  const int64_t n = blockIdx.x;
-  const T* z = logits + n * ld;
-  const RowStat r = row_statistics(z, V, scale * kLog2e, part);
+  __shared__ RowStat part[LP_WARPS], of_slice[MAX_SLICES];
+  __shared__ TopList<TPR> lists[TOP ? G::ROWS : 1];
+  extern __shared__ uint64_t merged[];                  // [slices, k], sorted, in the first block of a cluster
+  const int tid = G::tid(), rank = TPR == 32 ? 0 : blockIdx.x % slices;
+  const int64_t n = TPR == 32 ? (int64_t)blockIdx.x * G::ROWS + G::row() : blockIdx.x / slices;
+  if (TPR > 32 && slices > 1) gram_cluster_sync();      // every block of the cluster runs before another writes to it
+  if (n >= N) return;                                   // whole warps, in the form that has no barrier over the block
+  TopList<TPR>& list = lists[TOP ? G::row() : 0];
+  const float c = scale * kLog2e;
+  const Slice<T> s(logits + n * ld, V, rank, slices);
+  const int chunks = s.template chunks<TPR, NV>();
+  const int edge_place = s.edge(tid);
+  const float edge = edge_place >= 0 ? row_load(s.z + edge_place) : ROW_NEG_INF;
+  RowStat r = row_empty();
+  TopState st{0, 0.f, false};
+  if constexpr (TOP) {
+    if (tid == 0) list.added[0] = 0;
+    G::sync();
+  }
+  for (int ch = 0; ch < chunks; ++ch) {
+    uint4 q[NV];
+    s.template load_chunk<TPR, NV>(ch, tid, q);
+    float top = chunk_top<T, NV>(q);
+    row_add_vectors<T, NV>(r, q, top, c);
+    const bool on_edge = edge_place >= 0 && (tid < 8 ? ch == 0 : ch == chunks - 1);
+    if (on_edge) {
+      row_add(r, edge, c);
+      top = fmaxf(top, edge);
+    }
+    if constexpr (TOP)
+      top_chunk(list, st, TopChunk<T, TPR, NV>{q, s.place(s.v0 + ch * (TPR * NV) + tid), on_edge ? edge : ROW_NEG_INF, edge_place}, top, ask.k, ch,
+                ch == chunks - 1);
+  }
+  r = G::join(r, c, part);
+  if constexpr (TOP) {
+    if (st.have > 256 && st.have > ask.k) {
+      (void)top_cut(list, st.have, ask.k);
+      st.have = ask.k;
+    }
+  }
+  if (TPR > 32 && slices > 1) {
+    if (tid == 0) put_stat(&of_slice[rank], 0, r);
+    if constexpr (TOP) {                                // this slice's best, sorted, to the first block
+      for (int i = tid; i < st.have; i += TPR) {
+        const uint64_t key = list.keys[i];
+        int above = 0;
+        for (int j = 0; j < st.have; ++j) above += list.keys[j] > key;
+        if (above < ask.k) put_key(&merged[rank * ask.k + above], 0, key);
+      }
+      for (int i = st.have + tid; i < ask.k; i += TPR) put_key(&merged[rank * ask.k + i], 0, 0);
+    }
+    gram_cluster_sync();
+    if (rank != 0) return;
+    r = join_slices(of_slice, slices, c);
+  }
   const float log_s = row_log_sum(r);
-  if (threadIdx.x == 0) {
+  if (tid == 0) {
     if (ask.stats) { ask.stats[2 * n] = r.m; ask.stats[2 * n + 1] = log_s; }
     if (ask.entropy) ask.entropy[n] = row_entropy(r);
   }
-  for (int i = threadIdx.x; i < ask.C; i += LP_THREADS) {
+  for (int i = tid; i < ask.C; i += TPR) {
     const int32_t t = ask.targets[n * ask.C + i];
     if (t < -1 || t >= V) gram_device_fail(status, GRAM_ERR_ID_RANGE);
-    ask.logp[n * ask.C + i] = t >= 0 && t < V ? row_logp(row_load(z + t), r.m, log_s, scale) : 0.f;
+    ask.logp[n * ask.C + i] = t >= 0 && t < V ? row_logp(row_load(s.z + t), r.m, log_s, scale) : 0.f;
   }
-  uint64_t last = ~0ull;
-  for (int j = 0; j < ask.k; ++j) {                 // the largest key below the last one
-    uint64_t b = 0;
-    for (int v = threadIdx.x; v < V; v += LP_THREADS) {
-      const float x = row_load(z + v);
-      const uint64_t key = row_key(x, v);
-      if (x > ROW_NEG_INF && key < last && key > b) b = key;
+  if constexpr (TOP) {
+    const int64_t o = n * ask.k;
+    auto answer = [&](int at, uint64_t key) {
+      ask.top_ids[o + at] = key ? row_key_place(key) : -1;
+      ask.top_logp[o + at] = key ? row_logp(row_key_logit(key), r.m, log_s, scale) : ROW_NEG_INF;
+    };
+    if (TPR == 32 || slices == 1) {
+      for (int i = tid; i < st.have; i += TPR) {
+        const uint64_t key = list.keys[i];
+        int above = 0;
+        for (int j = 0; j < st.have; ++j) above += list.keys[j] > key;
+        if (above < ask.k) answer(above, key);
+      }
+      for (int i = st.have + tid; i < ask.k; i += TPR) answer(i, 0);
+      return;
     }
-    for (int o = 16; o > 0; o >>= 1) b = max(b, __shfl_xor_sync(0xffffffffu, b, o));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) best[threadIdx.x >> 5] = b;
-    __syncthreads();
-    for (int w = 0; w < LP_WARPS; ++w) b = max(b, best[w]);
-    if (threadIdx.x == 0) {
-      ask.top_ids[n * ask.k + j] = b ? row_key_place(b) : -1;
-      ask.top_logp[n * ask.k + j] = b ? row_logp(row_key_logit(b), r.m, log_s, scale) : ROW_NEG_INF;
+    int found = 0;
+    for (int i = tid; i < slices * ask.k; i += TPR) {
+      const uint64_t key = merged[i];
+      if (!key) continue;
+      ++found;
+      int at = 0;
+      for (int b = 0; b < slices; ++b) {                // keys of list b above this one: the lists descend, zeros last
+        int lo = 0, hi = ask.k;
+        while (lo < hi) {
+          const int mid = (lo + hi) / 2;
+          if (merged[b * ask.k + mid] > key) lo = mid + 1;
+          else hi = mid;
+        }
+        at += lo;
+      }
+      if (at < ask.k) answer(at, key);
     }
-    last = b;
+    found = G::sum(found, list.part);
+    for (int i = found + tid; i < ask.k; i += TPR) answer(i, 0);
+  }
+}
+
+// ------------------------------ gradients -----------------------------------------------------------------------------
+template <typename T> __device__ __forceinline__ bool same_alignment(const T* a, const T* b) {
+  return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15) == 0;
+}
+template <typename T> __device__ __forceinline__ void store_vector(T* dz, int place, const uint4& q, bool vec) {
+  if (vec) {
+    __stcs(reinterpret_cast<uint4*>(dz + place), q);
+  } else {
+    const T* e = reinterpret_cast<const T*>(&q);
+#pragma unroll
+    for (int j = 0; j < RowVec<T>::N; ++j) dz[place + j] = e[j];
+  }
+}
+// f(pair of logits) -> pair of results, over a chunk that is in registers
+template <typename T, int TPR, int NV, typename F>
+__device__ __forceinline__ void store_chunk(const Slice<T>& s, int ch, int tid, const uint4 (&q)[NV], T* dz, bool vec, F f) {
+  const int v = s.v0 + ch * (TPR * NV) + tid;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    if (v + i * TPR < s.v1) {
+      uint4 o;
+#pragma unroll
+      for (int j = 0; j < RowVec<T>::N / 2; ++j) RowVec<T>::put(o, j, f(RowVec<T>::pair(q[i], j)));
+      store_vector(dz, s.place(v + i * TPR), o, vec);
+    }
   }
 }
 
@@ -68,52 +463,73 @@ struct BackwardArgs {
   const float* entropy;
   const float* dlogp;
   const float* dentropy;
-  int64_t ld, ld_out;
-  int32_t V, C;
+  int64_t ld, ld_out, N;
+  int32_t V, C, slices;
   float scale;
   int32_t* status;
 };
 
-// dz = scale (sum of g at the given places - p (sum of all g + h (log p + H))), 0 at masked places
-template <typename T>
-__global__ void __launch_bounds__(LP_THREADS) logprobs_backward_kernel(const T* logits, T* dlogits, BackwardArgs a) {
+// dz = scale (sum of g at the given places - p (sum of all g + h (log p + H))), 0 at masked places.  With l = log2 p the
+// dense part is 2^l (A + B l), A = -scale (G + h H), B = -scale h ln 2; l is held at -200 as in row_softmax.cuh.
+template <typename T, int TPR>
+__global__ void __launch_bounds__(LP_THREADS, 4) logprobs_backward_kernel(const T* logits, T* dlogits, BackwardArgs a) {
+  using G = Group<TPR>;
+  constexpr int NV = 4;
   if (!chain_begin()) return;
-  __shared__ float g_at[GRAM_TOP_MAX];               // of each given token that takes part: its gradient, place and logit
-  __shared__ int32_t place[GRAM_TOP_MAX];
-  __shared__ float z_at[GRAM_TOP_MAX];
-  const int64_t n = blockIdx.x;
-  const T* z = logits + n * a.ld;
+  __shared__ struct { float g[GRAM_TOP_MAX], z[GRAM_TOP_MAX]; int32_t place[GRAM_TOP_MAX]; } given[G::ROWS];   // the given tokens that take part
+  const int tid = G::tid(), rank = TPR == 32 ? 0 : blockIdx.x % a.slices;
+  const int64_t n = TPR == 32 ? (int64_t)blockIdx.x * G::ROWS + G::row() : blockIdx.x / a.slices;
+  if (n >= a.N) return;
+  auto& mine = given[G::row()];
+  const Slice<T> s(logits + n * a.ld, a.V, rank, a.slices);
   T* dz = dlogits + n * a.ld_out;
-  for (int i = threadIdx.x; i < a.C; i += LP_THREADS) {
+  const bool vec = same_alignment(s.z, dz);
+  uint4 q[NV];
+  s.template load_chunk<TPR, NV>(0, tid, q);
+  const int edge_place = s.edge(tid);
+  const float edge = edge_place >= 0 ? row_load(s.z + edge_place) : ROW_NEG_INF;
+  for (int i = tid; i < a.C; i += TPR) {
     int32_t t = a.targets[n * a.C + i];
     if (t < -1 || t >= a.V) { gram_device_fail(a.status, GRAM_ERR_ID_RANGE); t = -1; }
-    const float x = t >= 0 ? row_load(z + t) : ROW_NEG_INF;
-    place[i] = x == ROW_NEG_INF ? -1 : t;
-    z_at[i] = x;
-    g_at[i] = x == ROW_NEG_INF ? 0.f : a.dlogp[n * a.C + i];
+    const float x = t >= 0 ? row_load(s.z + t) : ROW_NEG_INF;
+    mine.place[i] = x == ROW_NEG_INF ? -1 : t;
+    mine.z[i] = x;
+    mine.g[i] = x == ROW_NEG_INF ? 0.f : a.dlogp[n * a.C + i];
   }
-  __syncthreads();
-  float G = 0.f;
-  for (int i = 0; i < a.C; ++i) G += g_at[i];
-  const float m = row_base(a.stats[2 * n]), log_s = a.stats[2 * n + 1], h = a.dentropy ? a.dentropy[n] : 0.f, H = a.dentropy ? a.entropy[n] : 0.f;
-  const bool none = G == 0.f && h == 0.f;
-  auto dense = [&](float x) {
-    if (none || x == ROW_NEG_INF) return 0.f;
-    const float lp = (x - m) * a.scale - log_s;
-    return -a.scale * (row_ex2(lp * kLog2e) * (G + h * row_hold(lp + H)));
+  // in place, no slice may be overwritten before all have read the given tokens' logits
+  if (TPR > 32 && a.slices > 1 && a.C > 0) gram_cluster_sync();
+  else G::sync();
+  float sum = 0.f;
+  for (int i = 0; i < a.C; ++i) sum += mine.g[i];
+  const float m = row_base(a.stats[2 * n]), ls2 = a.stats[2 * n + 1] * kLog2e, h = a.dentropy ? a.dentropy[n] : 0.f;
+  const float c = a.scale * kLog2e, A = -a.scale * (sum + (a.dentropy ? h * a.entropy[n] : 0.f)), B = -a.scale * h * kLn2;
+  const bool none = (sum == 0.f && h == 0.f) || ls2 == ROW_NEG_INF;      // nothing asked, or nothing left in the row
+  const f32x2 mb = x2_pack(-m, -m), cc = x2_pack(c, c), lb = x2_pack(-ls2, -ls2), AA = x2_pack(A, A), BB = x2_pack(B, B);
+  auto dense2 = [&](f32x2 x) {
+    const float2 y = x2_unpack(x2_fma(x2_add(x, mb), cc, lb));
+    const float l0 = row_hold(y.x), l1 = row_hold(y.y);
+    return x2_unpack(x2_mul(x2_pack(row_ex2(l0), row_ex2(l1)), x2_fma(x2_pack(l0, l1), BB, AA)));
   };
-  for (int v = threadIdx.x; v < a.V; v += LP_THREADS) dz[v] = row_round<T>(dense(row_load(z + v)));
-  __syncthreads();
-  for (int i = threadIdx.x; i < a.C; i += LP_THREADS) {
-    if (place[i] < 0) continue;
+  auto dense = [&](float x) { return none || x == ROW_NEG_INF ? 0.f : dense2(x2_pack(x, x)).x; };
+  const int chunks = s.template chunks<TPR, NV>();
+  for (int ch = 0; ch < chunks; ++ch) {
+    if (ch > 0 && !none) s.template load_chunk<TPR, NV>(ch, tid, q);
+    if (none) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, [](f32x2) { return make_float2(0.f, 0.f); });
+    else store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, dense2);
+  }
+  if (edge_place >= 0) dz[edge_place] = row_round<T>(dense(edge));
+  G::sync();                                             // the given places are written again, by one thread each
+  for (int i = tid; i < a.C; i += TPR) {
+    const int p = mine.place[i];
+    if (p < 0 || !s.has(p)) continue;
     float g = 0.f;
     bool first = true;
     for (int j = 0; j < a.C; ++j)
-      if (place[j] == place[i]) {
+      if (mine.place[j] == p) {
         first = first && j >= i;
-        g += g_at[j];
+        g += mine.g[j];
       }
-    if (first) dz[place[i]] = row_round<T>(dense(z_at[i]) + a.scale * g);
+    if (first) dz[p] = row_round<T>(dense(mine.z[i]) + a.scale * g);
   }
 }
 
@@ -122,64 +538,166 @@ struct DistillArgs {
   const float* teacher;
   float* loss;
   const float* weight;
-  int64_t ld, ld_out;
-  int32_t V, k;
+  int64_t ld, ld_out, N;
+  int32_t V, k, slices;
   float scale;
   int32_t* status;
 };
 
-template <typename T>
-__global__ void __launch_bounds__(LP_THREADS) distill_kernel(const T* logits, T* dlogits, DistillArgs a) {
+// A block's slice stays in registers between the statistics and the gradient where it fits (8 vectors a thread), so the
+// logits are read once; of a longer one the last chunk does, and the others are read again, the latest first.
+template <typename T, int TPR>
+__global__ void __launch_bounds__(LP_THREADS, 4) distill_kernel(const T* logits, T* dlogits, DistillArgs a) {
+  using G = Group<TPR>;
+  constexpr int NV = 8;
   if (!chain_begin()) return;
-  __shared__ RowStat part[LP_WARPS];
-  __shared__ float q_at[GRAM_TOP_MAX], z_at[GRAM_TOP_MAX];
-  __shared__ int32_t place[GRAM_TOP_MAX];
-  const int64_t n = blockIdx.x;
-  const T* z = logits + n * a.ld;
-  for (int i = threadIdx.x; i < a.k; i += LP_THREADS) {
-    int32_t t = a.ids[n * a.k + i];
-    if (t < -1 || t >= a.V) { gram_device_fail(a.status, GRAM_ERR_ID_RANGE); t = -1; }
-    const float x = t >= 0 ? row_load(z + t) : ROW_NEG_INF, b = a.teacher[n * a.k + i];
-    place[i] = x == ROW_NEG_INF || b == ROW_NEG_INF ? -1 : t;
-    z_at[i] = x;
-    q_at[i] = b;
+  __shared__ RowStat part[LP_WARPS][2], of_slice[MAX_SLICES];
+  __shared__ float fpart[LP_WARPS];
+  __shared__ struct { float q[GRAM_TOP_MAX], z[GRAM_TOP_MAX]; int32_t place[GRAM_TOP_MAX]; } entries[G::ROWS];
+  const int tid = G::tid(), rank = TPR == 32 ? 0 : blockIdx.x % a.slices;
+  const int64_t n = TPR == 32 ? (int64_t)blockIdx.x * G::ROWS + G::row() : blockIdx.x / a.slices;
+  if (n >= a.N) return;
+  auto& mine = entries[G::row()];
+  const float c = a.scale * kLog2e;
+  const Slice<T> s(logits + n * a.ld, a.V, rank, a.slices);
+  const int chunks = s.template chunks<TPR, NV>();
+  uint4 q[NV];
+  s.template load_chunk<TPR, NV>(0, tid, q);
+  const int edge_place = s.edge(tid);
+  const float edge = edge_place >= 0 ? row_load(s.z + edge_place) : ROW_NEG_INF;
+  RowStat r = row_empty(), t = row_empty();
+  for (int i = tid; i < a.k; i += TPR) {
+    int32_t id = a.ids[n * a.k + i];
+    if (id < -1 || id >= a.V) { gram_device_fail(a.status, GRAM_ERR_ID_RANGE); id = -1; }
+    const float x = id >= 0 ? row_load(s.z + id) : ROW_NEG_INF, b = a.teacher[n * a.k + i];
+    const bool use = x != ROW_NEG_INF && b != ROW_NEG_INF;
+    mine.place[i] = use ? id : -1;
+    mine.z[i] = x;
+    mine.q[i] = b;
+    if (use) row_add(t, b, c);
   }
-  const RowStat r = row_statistics(z, a.V, a.scale * kLog2e, part);
-  const float log_s = row_log_sum(r), m = row_base(r.m);
-  RowStat q = row_empty();
-  for (int i = 0; i < a.k; ++i)
-    if (place[i] >= 0) row_add(q, q_at[i], a.scale * kLog2e);
-  const bool some = q.s != 0.f;
-  const float log_q = row_log_sum(q);
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    float sum = 0.f;
-    for (int i = 0; i < a.k; ++i) {
-      if (place[i] < 0) continue;
-      const float lq = (q_at[i] - q.m) * a.scale - log_q, e = expf(lq);
-      if (!(e == 0.f)) sum += e * (lq - row_logp(z_at[i], r.m, log_s, a.scale));
+  if (TPR > 32 && a.slices > 1) gram_cluster_sync();     // every block of the cluster runs before another writes to it
+  for (int ch = 0; ch < chunks; ++ch) {
+    if (ch > 0) s.template load_chunk<TPR, NV>(ch, tid, q);
+    row_add_vectors<T, NV>(r, q, chunk_top<T, NV>(q), c);
+  }
+  if (edge_place >= 0) row_add(r, edge, c);
+  G::join(r, t, c, part);
+  if (TPR > 32 && a.slices > 1) {
+    if (tid < a.slices) put_stat(&of_slice[rank], tid, r);
+    gram_cluster_sync();                                 // all have read the teacher's places by now, too
+    r = join_slices(of_slice, a.slices, c);
+  }
+  const float log_s = row_log_sum(r), m = row_base(r.m), log_t = row_log_sum(t);
+  float loss = 0.f;
+  for (int i = tid; i < a.k; i += TPR) {
+    float qi = 0.f;
+    if (mine.place[i] >= 0) {
+      const float lq = (mine.q[i] - t.m) * a.scale - log_t;
+      qi = expf(lq);
+      if (!(qi == 0.f)) loss += qi * (lq - row_logp(mine.z[i], r.m, log_s, a.scale));
     }
-    a.loss[n] = sum;
+    mine.q[i] = qi;
+  }
+  if (rank == 0) {
+    loss = G::sum(loss, fpart);
+    if (tid == 0) a.loss[n] = loss;
   }
   if (!dlogits) return;
   const float w = (a.weight ? a.weight[n] : 1.f) * a.scale;
-  const bool none = w == 0.f || !some;
+  const bool none = w == 0.f || t.s == 0.f;
   T* dz = dlogits + n * a.ld_out;
-  auto p = [&](float x) { return none ? 0.f : w * row_ex2(row_hold((x - m) * a.scale * kLog2e - log_s * kLog2e)); };
-  for (int v = threadIdx.x; v < a.V; v += LP_THREADS) dz[v] = row_round<T>(p(row_load(z + v)));
-  __syncthreads();
+  const bool vec = same_alignment(s.z, dz);
+  const float ls2 = log_s * kLog2e;
+  const f32x2 mb = x2_pack(-m, -m), cc = x2_pack(c, c), lb = x2_pack(-ls2, -ls2), ww = x2_pack(w, w);
+  auto dense2 = [&](f32x2 x) {
+    const float2 y = x2_unpack(x2_fma(x2_add(x, mb), cc, lb));
+    return x2_unpack(x2_mul(x2_pack(row_ex2(y.x), row_ex2(y.y)), ww));
+  };
+  for (int ch = chunks - 1; ch >= 0; --ch) {
+    if (ch < chunks - 1 && !none) s.template load_chunk<TPR, NV>(ch, tid, q);
+    if (none) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, [](f32x2) { return make_float2(0.f, 0.f); });
+    else store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, dense2);
+  }
+  if (edge_place >= 0) dz[edge_place] = row_round<T>(none ? 0.f : dense2(x2_pack(edge, edge)).x);
+  G::sync();                                             // the teacher's places are written again, by one thread each
   if (none) return;
-  for (int i = threadIdx.x; i < a.k; i += LP_THREADS) {
-    if (place[i] < 0) continue;
+  for (int i = tid; i < a.k; i += TPR) {
+    const int p = mine.place[i];
+    if (p < 0 || !s.has(p)) continue;
     float sum = 0.f;
     bool first = true;
     for (int j = 0; j < a.k; ++j)
-      if (place[j] == place[i]) {
+      if (mine.place[j] == p) {
         first = first && j >= i;
-        sum += expf((q_at[j] - q.m) * a.scale - log_q);
+        sum += mine.q[j];
       }
-    if (first) dz[place[i]] = row_round<T>(p(z_at[i]) - w * sum);
+    if (first) dz[p] = row_round<T>(dense2(x2_pack(mine.z[i], mine.z[i])).x - w * sum);
   }
+}
+
+// ------------------------------ host side -----------------------------------------------------------------------------
+// Rows of up to 4 KB go to warps where there are enough of them to fill the blocks' places; other rows to a block, or to a
+// cluster: as many blocks as hold the row (hold: vectors that a block keeps; 0: it keeps none), and more while the GPU has
+// room for them and each still has a vector a thread.
+struct RowPlan {
+  bool warps;
+  int slices;
+};
+RowPlan row_plan(gram_ctx* ctx, int64_t N, int64_t row_bytes, int64_t hold) {
+  RowPlan p{row_bytes <= 4096 && N >= 4 * kNumSMs, 1};
+  if (p.warps) return p;
+  const int64_t vectors = row_bytes / 16;
+  const int most = gram_cluster_blocks(ctx) < MAX_SLICES ? gram_cluster_blocks(ctx) : MAX_SLICES;
+  while (hold && p.slices < most && ceil_div64(vectors, p.slices) > hold) p.slices *= 2;
+  while (p.slices < most && N * p.slices * 2 <= 4 * kNumSMs && vectors / (2 * p.slices) >= LP_THREADS) p.slices *= 2;
+  return p;
+}
+template <typename... P, typename... A>
+gram_status launch_rows(gram_ctx* ctx, void (*kern)(P...), const RowPlan& plan, int64_t N, size_t smem, cudaStream_t st, A... args) {
+  const int64_t blocks = plan.warps ? ceil_div64(N, LP_WARPS) : N * plan.slices;
+  if (blocks > INT32_MAX) return gram_set_error(ctx, "%lld rows of %d slices", (long long)N, plan.slices), GRAM_ERR_UNSUPPORTED;
+  if (plan.slices > 8) GRAM_CUDA(ctx, cudaFuncSetAttribute(reinterpret_cast<const void*>(kern), cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.blockDim = dim3(LP_THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0] = chain_attribute();
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)plan.slices;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = plan.slices > 1 ? 2 : 1;
+  GRAM_CUDA(ctx, cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...));
+  return GRAM_OK;
+}
+
+template <typename T>
+gram_status logprobs_typed(gram_ctx* ctx, const T* z, int64_t ld, int64_t N, int32_t V, float scale, const RowAnswers& ask, cudaStream_t st) {
+  const RowPlan plan = row_plan(ctx, N, (int64_t)V * sizeof(T), 0);
+  ProfScope prof(ctx, GRAM_K_OTHER, (double)N * V * sizeof(T), 1, st, "logprobs");
+  int32_t* status = gram_status_word(ctx);
+  const size_t smem = plan.slices > 1 ? sizeof(uint64_t) * plan.slices * ask.k : 0;
+  auto run = [&](auto kern) { return launch_rows(ctx, kern, plan, N, smem, st, z, ld, N, V, scale, plan.slices, ask, status); };
+  if (plan.warps) return ask.k ? run(logprobs_kernel<T, 32, true>) : run(logprobs_kernel<T, 32, false>);
+  return ask.k ? run(logprobs_kernel<T, LP_THREADS, true>) : run(logprobs_kernel<T, LP_THREADS, false>);
+}
+template <typename T> gram_status backward_typed(gram_ctx* ctx, const T* z, T* dz, BackwardArgs a, cudaStream_t st) {
+  const RowPlan plan = row_plan(ctx, a.N, (int64_t)a.V * sizeof(T), 0);
+  ProfScope prof(ctx, GRAM_K_OTHER, 2.0 * a.N * a.V * sizeof(T), 1, st, "logprobs_backward");
+  a.slices = plan.slices;
+  if (plan.warps) return launch_rows(ctx, logprobs_backward_kernel<T, 32>, plan, a.N, 0, st, z, dz, a);
+  return launch_rows(ctx, logprobs_backward_kernel<T, LP_THREADS>, plan, a.N, 0, st, z, dz, a);
+}
+template <typename T> gram_status distill_typed(gram_ctx* ctx, const T* z, T* dz, DistillArgs a, cudaStream_t st) {
+  const RowPlan plan = row_plan(ctx, a.N, (int64_t)a.V * sizeof(T), LP_THREADS * 8);
+  ProfScope prof(ctx, GRAM_K_OTHER, (dz ? 2.0 : 1.0) * a.N * a.V * sizeof(T), 1, st, "distill");
+  a.slices = plan.slices;
+  if (plan.warps) return launch_rows(ctx, distill_kernel<T, 32>, plan, a.N, 0, st, z, dz, a);
+  return launch_rows(ctx, distill_kernel<T, LP_THREADS>, plan, a.N, 0, st, z, dz, a);
 }
 
 }  // namespace
@@ -187,40 +705,24 @@ __global__ void __launch_bounds__(LP_THREADS) distill_kernel(const T* logits, T*
 gram_status logprobs_launch(gram_ctx* ctx, const void* logits, int dtype, int64_t ld, int64_t N, int32_t V, float scale,
                             const RowAnswers& ask, cudaStream_t st) {
   if (N == 0) return GRAM_OK;
-  ProfScope prof(ctx, GRAM_K_OTHER, (double)N * V * (dtype == GRAM_F32 ? 4 : 2), 1, st, "logprobs");
-  int32_t* status = gram_status_word(ctx);
-  if (dtype == GRAM_F32)
-    launch_chain(logprobs_kernel<float>, dim3((unsigned)N), LP_THREADS, 0, st, (const float*)logits, ld, V, scale, ask, status);
-  else
-    launch_chain(logprobs_kernel<bf16>, dim3((unsigned)N), LP_THREADS, 0, st, (const bf16*)logits, ld, V, scale, ask, status);
-  GRAM_LAUNCH_CHECK(ctx);
-  return GRAM_OK;
+  if (dtype == GRAM_F32) return logprobs_typed(ctx, (const float*)logits, ld, N, V, scale, ask, st);
+  return logprobs_typed(ctx, (const bf16*)logits, ld, N, V, scale, ask, st);
 }
 
 gram_status logprobs_backward_launch(gram_ctx* ctx, const void* logits, int dtype, int64_t ld, int64_t N, int32_t V, float scale,
                                      const int32_t* targets, int32_t C, const float* stats, const float* entropy, const float* dlogp,
                                      const float* dentropy, void* dlogits, int64_t ld_out, cudaStream_t st) {
   if (N == 0) return GRAM_OK;
-  ProfScope prof(ctx, GRAM_K_OTHER, 2.0 * N * V * (dtype == GRAM_F32 ? 4 : 2), 1, st, "logprobs_backward");
-  const BackwardArgs a{targets, stats, entropy, dlogp, dentropy, ld, ld_out, V, C, scale, gram_status_word(ctx)};
-  if (dtype == GRAM_F32)
-    launch_chain(logprobs_backward_kernel<float>, dim3((unsigned)N), LP_THREADS, 0, st, (const float*)logits, (float*)dlogits, a);
-  else
-    launch_chain(logprobs_backward_kernel<bf16>, dim3((unsigned)N), LP_THREADS, 0, st, (const bf16*)logits, (bf16*)dlogits, a);
-  GRAM_LAUNCH_CHECK(ctx);
-  return GRAM_OK;
+  const BackwardArgs a{targets, stats, entropy, dlogp, dentropy, ld, ld_out, N, V, C, 1, scale, gram_status_word(ctx)};
+  if (dtype == GRAM_F32) return backward_typed(ctx, (const float*)logits, (float*)dlogits, a, st);
+  return backward_typed(ctx, (const bf16*)logits, (bf16*)dlogits, a, st);
 }
 
 gram_status distill_launch(gram_ctx* ctx, const void* logits, int dtype, int64_t ld, int64_t N, int32_t V, float scale,
                            const int32_t* teacher_ids, const float* teacher_logits, int32_t k, float* loss, const float* weight,
                            void* dlogits, int64_t ld_out, cudaStream_t st) {
   if (N == 0) return GRAM_OK;
-  ProfScope prof(ctx, GRAM_K_OTHER, (dlogits ? 2.0 : 1.0) * N * V * (dtype == GRAM_F32 ? 4 : 2), 1, st, "distill");
-  const DistillArgs a{teacher_ids, teacher_logits, loss, weight, ld, ld_out, V, k, scale, gram_status_word(ctx)};
-  if (dtype == GRAM_F32)
-    launch_chain(distill_kernel<float>, dim3((unsigned)N), LP_THREADS, 0, st, (const float*)logits, (float*)dlogits, a);
-  else
-    launch_chain(distill_kernel<bf16>, dim3((unsigned)N), LP_THREADS, 0, st, (const bf16*)logits, (bf16*)dlogits, a);
-  GRAM_LAUNCH_CHECK(ctx);
-  return GRAM_OK;
+  const DistillArgs a{teacher_ids, teacher_logits, loss, weight, ld, ld_out, N, V, k, 1, scale, gram_status_word(ctx)};
+  if (dtype == GRAM_F32) return distill_typed(ctx, (const float*)logits, (float*)dlogits, a, st);
+  return distill_typed(ctx, (const bf16*)logits, (bf16*)dlogits, a, st);
 }

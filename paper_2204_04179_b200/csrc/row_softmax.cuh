@@ -37,25 +37,27 @@ __device__ __forceinline__ RowStat row_join(const RowStat& a, const RowStat& b, 
   r.t = fa * (a.t + a.s * da) + fb * (b.t + b.s * db);
   return r;
 }
+// r's statistics as they are with a larger m
+__device__ __forceinline__ void row_raise(RowStat& r, float m, float c) {
+  const float d = row_hold((r.m - m) * c), f = row_ex2(d);
+  r.t = f * (r.t + r.s * d);
+  r.s *= f;
+  r.m = m;
+}
 __device__ __forceinline__ void row_add(RowStat& r, float z, float c) {
-  if (z > r.m) {
-    const float d = row_hold((r.m - z) * c), f = row_ex2(d);
-    r.t = f * (r.t + r.s * d);
-    r.s *= f;
-    r.m = z;
-  }
+  if (z > r.m) row_raise(r, z, c);
   const float y = row_hold((z - row_base(r.m)) * c), e = row_ex2(y);
   r.s += e;
   r.t += e * y;
 }
-__device__ __forceinline__ RowStat row_join_warp(RowStat r, float c) {
+// the statistics of L neighbouring lanes, in all of them; the lower lane's come first on both sides, so that all get the same bits
+template <int L> __device__ __forceinline__ RowStat row_join_lanes(RowStat r, float c) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
+  for (int o = L / 2; o > 0; o >>= 1) {
     RowStat x;
     x.m = __shfl_xor_sync(0xffffffffu, r.m, o);
     x.s = __shfl_xor_sync(0xffffffffu, r.s, o);
     x.t = __shfl_xor_sync(0xffffffffu, r.t, o);
-    // the lower lane's statistics come first on both sides, so that both get the same bits
     r = (threadIdx.x & o) ? row_join(x, r, c) : row_join(r, x, c);
   }
   return r;
@@ -80,9 +82,99 @@ __device__ __forceinline__ float row_key_logit(uint64_t key) {
 }
 __device__ __forceinline__ int32_t row_key_place(uint64_t key) { return (int32_t)~(uint32_t)key; }
 
+__device__ __forceinline__ uint32_t row_order(float z) { return (uint32_t)(row_key(z, 0) >> 32); }
+__device__ __forceinline__ float row_order_logit(uint32_t o) { return __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xffffffffu)); }
+
 template <typename T> __device__ __forceinline__ float row_load(const T* p);
 template <> __device__ __forceinline__ float row_load<float>(const float* p) { return *p; }
 template <> __device__ __forceinline__ float row_load<bf16>(const bf16* p) { return __bfloat162float(*p); }
 template <typename T> __device__ __forceinline__ T row_round(float v);
 template <> __device__ __forceinline__ float row_round<float>(float v) { return v; }
 template <> __device__ __forceinline__ bf16 row_round<bf16>(float v) { return __float2bfloat16_rn(v); }
+
+// ---------------------------------------------------------------------------
+// Sixteen bytes of a row, and pairs of fp32 values in one register pair (one instruction for the two).
+// ---------------------------------------------------------------------------
+typedef uint64_t f32x2;
+__device__ __forceinline__ f32x2 x2_pack(float a, float b) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 x2_unpack(f32x2 v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ f32x2 x2_add(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 x2_mul(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 x2_fma(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
+template <typename T> struct RowVec;                 // 16 bytes of logits
+template <> struct RowVec<float> {
+  static constexpr int N = 4;
+  static constexpr uint32_t NONE = 0xff800000u;      // a word of masked places
+  static __device__ __forceinline__ float top(const uint4& q) {
+    return fmaxf(fmaxf(__uint_as_float(q.x), __uint_as_float(q.y)), fmaxf(__uint_as_float(q.z), __uint_as_float(q.w)));
+  }
+  static __device__ __forceinline__ f32x2 pair(const uint4& q, int i) {
+    return i == 0 ? x2_pack(__uint_as_float(q.x), __uint_as_float(q.y)) : x2_pack(__uint_as_float(q.z), __uint_as_float(q.w));
+  }
+  static __device__ __forceinline__ void put(uint4& q, int i, float2 v) {
+    if (i == 0) { q.x = __float_as_uint(v.x); q.y = __float_as_uint(v.y); }
+    else { q.z = __float_as_uint(v.x); q.w = __float_as_uint(v.y); }
+  }
+};
+template <> struct RowVec<bf16> {
+  static constexpr int N = 8;
+  static constexpr uint32_t NONE = 0xff80ff80u;
+  static __device__ __forceinline__ float top(const uint4& q) {
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&q);
+    const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    return fmaxf(__low2float(m), __high2float(m));
+  }
+  static __device__ __forceinline__ f32x2 pair(const uint4& q, int i) {
+    const uint32_t w = i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w;
+    return x2_pack(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  }
+  static __device__ __forceinline__ void put(uint4& q, int i, float2 v) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(&h);
+    if (i == 0) q.x = w; else if (i == 1) q.y = w; else if (i == 2) q.z = w; else q.w = w;
+  }
+};
+
+// The statistics of NV vectors' worth of logits added to r, whose m is at least their maximum afterwards.
+template <typename T, int NV>
+__device__ __forceinline__ void row_add_vectors(RowStat& r, const uint4 (&q)[NV], float top, float c) {
+  if (top > r.m) row_raise(r, top, c);
+  const float base = row_base(r.m);
+  const f32x2 mb = x2_pack(-base, -base), cc = x2_pack(c, c);
+  f32x2 s = x2_pack(0.f, 0.f), t = s;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+#pragma unroll
+    for (int j = 0; j < RowVec<T>::N / 2; ++j) {
+      const float2 y = x2_unpack(x2_mul(x2_add(RowVec<T>::pair(q[i], j), mb), cc));
+      const float y0 = row_hold(y.x), y1 = row_hold(y.y);
+      const f32x2 e = x2_pack(row_ex2(y0), row_ex2(y1));
+      s = x2_add(s, e);
+      t = x2_fma(e, x2_pack(y0, y1), t);
+    }
+  }
+  const float2 s2 = x2_unpack(s), t2 = x2_unpack(t);
+  r.s += s2.x + s2.y;
+  r.t += t2.x + t2.y;
+}
