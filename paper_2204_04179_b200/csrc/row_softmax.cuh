@@ -92,6 +92,72 @@ template <typename T> __device__ __forceinline__ T row_round(float v);
 template <> __device__ __forceinline__ float row_round<float>(float v) { return v; }
 template <> __device__ __forceinline__ bf16 row_round<bf16>(float v) { return __float2bfloat16_rn(v); }
 
+constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32;
+
+// TPR threads a row: a warp, or the block.  All threads of a group call these together.
+template <int TPR> struct Group {
+  static constexpr int ROWS = LP_THREADS / TPR;
+  static_assert(TPR == 32 || TPR == LP_THREADS, "a warp or the block");
+  static __device__ __forceinline__ int tid() { return threadIdx.x % TPR; }
+  static __device__ __forceinline__ int row() { return threadIdx.x / TPR; }
+  static __device__ __forceinline__ void sync() {
+    if constexpr (TPR == 32) __syncwarp();
+    else __syncthreads();
+  }
+  static __device__ __forceinline__ int count(bool p) {        // also a barrier
+    if constexpr (TPR == 32) return __popc(__ballot_sync(0xffffffffu, p));
+    else return __syncthreads_count(p);
+  }
+  static __device__ __forceinline__ int sum(int v, int* part) {
+    v = __reduce_add_sync(0xffffffffu, v);
+    if constexpr (TPR > 32) {
+      __syncthreads();
+      if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+      __syncthreads();
+      v = 0;
+#pragma unroll
+      for (int w = 0; w < LP_WARPS; ++w) v += part[w];
+    }
+    return v;
+  }
+  // the group's statistics in all its threads, joined in the same order everywhere
+  static __device__ __forceinline__ RowStat join(RowStat r, float c, RowStat* part) {
+    r = row_join_lanes<32>(r, c);
+    if constexpr (TPR > 32) {
+      __syncthreads();
+      if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = r;
+      __syncthreads();
+      r = row_join_lanes<LP_WARPS>(part[threadIdx.x & (LP_WARPS - 1)], c);
+    }
+    return r;
+  }
+  // two at once
+  static __device__ __forceinline__ void join(RowStat& r, RowStat& q, float c, RowStat (*part)[2]) {
+    r = row_join_lanes<32>(r, c);
+    q = row_join_lanes<32>(q, c);
+    if constexpr (TPR > 32) {
+      __syncthreads();
+      if ((threadIdx.x & 31) == 0) { part[threadIdx.x >> 5][0] = r; part[threadIdx.x >> 5][1] = q; }
+      __syncthreads();
+      r = row_join_lanes<LP_WARPS>(part[threadIdx.x & (LP_WARPS - 1)][0], c);
+      q = row_join_lanes<LP_WARPS>(part[threadIdx.x & (LP_WARPS - 1)][1], c);
+    }
+  }
+  static __device__ __forceinline__ float sum(float v, float* part) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if constexpr (TPR > 32) {
+      __syncthreads();
+      if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+      __syncthreads();
+      v = 0.f;
+#pragma unroll
+      for (int w = 0; w < LP_WARPS; ++w) v += part[w];
+    }
+    return v;
+  }
+};
+
 // ---------------------------------------------------------------------------
 // Sixteen bytes of a row, and pairs of fp32 values in one register pair (one instruction for the two).
 // ---------------------------------------------------------------------------

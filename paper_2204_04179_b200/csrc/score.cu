@@ -1,27 +1,518 @@
 // Answers over an item table from the vectors themselves (gram_score_logprobs).
+//
+// The product users x items^T runs on pairs of SMs (tcgen05 cta_group::2) as in gemm.cu: a cluster of two blocks owns a tile
+// of 256 users x 256 items, each stages its own 128 users and its own half of the items by TMA, the leader issues the MMAs,
+// and each block's tensor memory receives 128 users' logits, two tiles in turn.  The logits never leave it: an epilogue
+// thread owns one user (a lane of tensor memory) and half of a tile's columns, keeps the softmax statistics of what it has
+// seen in registers, and puts entries that reach its bar on a list of its own in global memory.
+//
+// Work is cut evenly: the units of 128 items of all row tiles, one row tile after another, are divided into contiguous
+// runs, one for each pair.  A run touches at most two row tiles, so a user's statistics and lists lie with a few pairs;
+// score_join_kernel, one block a user, joins them.
 #include "logits.h"
+#include "row_softmax.cuh"
+#include "row_top.cuh"
+#include "tc_common.cuh"
 
 namespace {
+using namespace tc;
 
-constexpr int SC_TILE = 32, SC_K = 32;
+constexpr int SM_ROWS = 128, SC_ROWS = 2 * SM_ROWS;     // users of a block and of a pair
+constexpr int SC_BK = 64, SC_UNIT = 128, SC_COLS = 256; // k of a stage, items of a unit and of the widest tile
+constexpr int SC_A_BYTES = SM_ROWS * SC_BK * 2, SC_B_BYTES = SC_COLS / 2 * SC_BK * 2, SC_STAGE = SC_A_BYTES + SC_B_BYTES;
+constexpr int SC_STAGES = 6, SC_EPI_WARPS = 8, SC_THREADS = 64 + 32 * SC_EPI_WARPS;
+constexpr int SC_BIAS_BYTES = SC_EPI_WARPS * 128 * 4;   // a warp's 128 columns
+constexpr int SC_SMEM = SC_STAGES * SC_STAGE + SC_BIAS_BYTES + 1024 + 256;
+constexpr int SC_LIST_MAX = 256;                        // most entries of a thread's list
+constexpr int SC_PAIR_THREADS = 2 * SC_ROWS;            // epilogue threads of a pair, one for each user and half
 
-// z[n, v] = users[n] . items[v] + bias[v], a 32 x 32 tile per block
-__global__ void __launch_bounds__(SC_TILE * SC_TILE) score_tile_kernel(const bf16* users, int64_t ld_u, const bf16* items, int64_t ld_i,
-                                                                      const float* bias, int64_t N, int32_t V, int32_t d, float* z) {
-  if (!chain_begin()) return;
-  __shared__ float u[SC_TILE][SC_K + 1], w[SC_TILE][SC_K + 1];
-  const int tx = threadIdx.x % SC_TILE, ty = threadIdx.x / SC_TILE;
-  const int64_t n0 = (int64_t)blockIdx.y * SC_TILE, v0 = (int64_t)blockIdx.x * SC_TILE;
-  float acc = 0.f;
-  for (int k0 = 0; k0 < d; k0 += SC_K) {
-    const bool in = k0 + tx < d;
-    u[ty][tx] = in && n0 + ty < N ? __bfloat162float(users[(n0 + ty) * ld_u + k0 + tx]) : 0.f;
-    w[ty][tx] = in && v0 + ty < V ? __bfloat162float(items[(v0 + ty) * ld_i + k0 + tx]) : 0.f;
-    __syncthreads();
-    for (int k = 0; k < SC_K; ++k) acc = fmaf(u[ty][k], w[tx][k], acc);
+struct ScoreArgs {
+  const float* bias;
+  int64_t N;
+  int32_t V, num_kb, k, cap;     // cap: entries that a list holds
+  int32_t units, total, per_run; // units of a row tile, of all, of a pair's run
+  float c;
+  uint64_t* lists;               // [pair, half, row of the tile, cap]
+  uint64_t* early;               // [pair, half, row, k]: the best of the row tile that a run leaves before its last
+  float4* stats;                 // [pair, row tile of the run (0, 1), half, row]: m, s, t, entries of the list
+  int32_t* status;
+};
+
+// The tiles of a run, as all roles walk over them.
+struct ScoreRun {
+  int32_t units, begin, at, end;
+  int32_t tm, unit, width;       // row tile, first unit and width in units of the current tile
+  bool first, last;              // of the run's part of this row tile
+  __device__ __forceinline__ ScoreRun(const ScoreArgs& a, int pair)
+      : units(a.units), begin(pair * a.per_run), at(begin), end(min(begin + a.per_run, a.total)), tm(0), unit(0), width(0), first(false), last(false) {}
+  __device__ __forceinline__ bool next() {
+    at += width;
+    if (at >= end) return false;
+    tm = at / units;
+    unit = at - tm * units;
+    const int left = min(units - unit, end - at);
+    width = min(left, SC_COLS / SC_UNIT);
+    first = at == begin || unit == 0;
+    last = left == width;
+    return true;
+  }
+  __device__ __forceinline__ int part() const { return tm - begin / units; }             // 0, or 1 for the second row tile
+  __device__ __forceinline__ bool leaves() const { return (end - 1) / units != tm; }     // the run goes on with another row tile
+};
+
+// The list of lane `of` of this warp cut to its best k by the whole warp; returns (in every lane) the bar that better logits reach.
+__device__ __noinline__ float score_cut(uint64_t* list, int have, int k) {
+  constexpr int PER = SC_LIST_MAX / 32;
+  const int lane = threadIdx.x & 31;
+  uint64_t key[PER];
+  uint32_t low = 0xffffffffu, high = 0u;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    key[i] = i * 32 + lane < have ? list[i * 32 + lane] : 0;
+    if (key[i]) { low = min(low, (uint32_t)(key[i] >> 32)); high = max(high, (uint32_t)(key[i] >> 32)); }
+  }
+  low = __reduce_min_sync(0xffffffffu, low);
+  high = __reduce_max_sync(0xffffffffu, high);
+  const uint64_t kth = kth_key(k, [&](uint64_t t) {
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) c += key[i] >= t;
+    return (int)__reduce_add_sync(0xffffffffu, c);
+  }, (uint64_t)low << 32, (uint64_t)high << 32 | 0xffffffffu);
+  int at = 0;
+  low = 0xffffffffu;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const bool keep = key[i] >= kth && key[i] != 0;
+    const uint32_t who = __ballot_sync(0xffffffffu, keep);
+    if (keep) {
+      list[at + __popc(who & ((1u << lane) - 1u))] = key[i];
+      low = min(low, (uint32_t)(key[i] >> 32));
+    }
+    at += __popc(who);
+  }
+  __syncwarp();
+  return row_order_logit(__reduce_min_sync(0xffffffffu, low) + 1u);
+}
+
+// x[32]: a block of 32 columns of this thread's row, with the bias (b: the warp's 32 values in shared memory; null: none)
+__device__ __forceinline__ void score_block(uint32_t taddr, const float* b, float (&x)[32]) {
+  uint32_t v[32];
+  tc_ld32_issue(taddr, v);
+  tc_ld32_wait(v);
+#pragma unroll
+  for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(v[j]);
+  if (b) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float4 f = reinterpret_cast<const float4*>(b)[j];
+      x[4 * j] += f.x; x[4 * j + 1] += f.y; x[4 * j + 2] += f.z; x[4 * j + 3] += f.w;
+    }
+  }
+}
+__device__ __forceinline__ float score_top(const float (&x)[32]) {
+  float t[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) t[j] = fmaxf(fmaxf(x[j], x[j + 8]), fmaxf(x[j + 16], x[j + 24]));
+  return fmaxf(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])), fmaxf(fmaxf(t[4], t[5]), fmaxf(t[6], t[7])));
+}
+__device__ __forceinline__ void score_add(RowStat& r, const float (&x)[32], float top, float c) {
+  if (top > r.m) row_raise(r, top, c);
+  const float base = row_base(r.m);
+  const f32x2 mb = x2_pack(-base, -base), cc = x2_pack(c, c);
+  f32x2 s = x2_pack(0.f, 0.f), t = s;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    const float2 y = x2_unpack(x2_mul(x2_add(x2_pack(x[2 * j], x[2 * j + 1]), mb), cc));
+    const float y0 = row_hold(y.x), y1 = row_hold(y.y);
+    const f32x2 e = x2_pack(row_ex2(y0), row_ex2(y1));
+    s = x2_add(s, e);
+    t = x2_fma(e, x2_pack(y0, y1), t);
+  }
+  const float2 s2 = x2_unpack(s), t2 = x2_unpack(t);
+  r.s += s2.x + s2.y;
+  r.t += t2.x + t2.y;
+}
+// A first bar for each lane's row from its columns of the first tile: a value that k of them reach, and few more.
+__device__ __forceinline__ float score_first_bar(uint32_t taddr, const float* b, int blocks, int k) {
+  float x[4][32];
+  uint32_t lo = 0xffffffffu, hi = 0u;
+  int some = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (i < blocks) {
+      score_block(taddr + i * 32, b ? b + i * 32 : nullptr, x[i]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) x[i][j] = ROW_NEG_INF;
+    }
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      if (x[i][j] > ROW_NEG_INF) {
+        const uint32_t o = row_order(x[i][j]);
+        lo = min(lo, o);
+        hi = max(hi, o);
+        ++some;
+      }
+  }
+  const bool enough = some >= k;
+  bool done = !enough || lo >= hi;
+  for (int step = 0; step < 16 && __any_sync(0xffffffffu, !done); ++step) {
+    const uint32_t mid = hi - (hi - lo) / 2;
+    const float f = row_order_logit(mid);
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 32; ++j) n += x[i][j] >= f;
+    if (!done) {
+      if (n < k) hi = mid - 1;
+      else lo = mid;
+      done = lo >= hi || (n >= k && n <= k + k / 8);
+    }
+  }
+  return enough ? row_order_logit(lo) : -FLT_MAX;
+}
+
+template <bool TOP>
+__global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_constant__ CUtensorMap users, const __grid_constant__ CUtensorMap items,
+                                                              const __grid_constant__ ScoreArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t tiles = (raw + 1023u) & ~1023u;        // the same offset in both blocks of the pair
+  float* bias_s = reinterpret_cast<float*>(smem_raw + (tiles - raw) + SC_STAGES * SC_STAGE);
+  const uint32_t bar0 = tiles + SC_STAGES * SC_STAGE + SC_BIAS_BYTES;
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };                            // used in the leader
+  auto empty_bar = [&](int s) { return bar0 + 8u * (SC_STAGES + s); };             // one per block
+  auto tfull_bar = [&](int b) { return bar0 + 8u * (2 * SC_STAGES + b); };         // one per block
+  auto tempty_bar = [&](int b) { return bar0 + 8u * (2 * SC_STAGES + 2 + b); };    // used in the leader
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_raw + (bar0 - raw) + 8 * (2 * SC_STAGES + 4));
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < SC_STAGES; ++s) {
+      mbar_init(full_bar(s), 2);                        // the two blocks' copies, each with its byte count
+      mbar_init(empty_bar(s), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(tfull_bar(b), 1);
+      mbar_init(tempty_bar(b), 2 * SC_EPI_WARPS);
+    }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  gram_cluster_sync();                                  // both blocks' barriers exist before anyone signals them
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const bool go = chain_begin();
+  const int pair = blockIdx.x >> 1;
+  bool failed = false;
+  ScoreRun run(a, pair);
+
+  if (warp == 0 && go) {
+    // ------------------------------ copies (both blocks) ------------------------------
+    int s = 0;
+    uint32_t ph = 0;
+    const uint32_t lead_bar0 = map_to_cta(bar0, 0);
+    while (!failed && run.next()) {
+      const int m0 = run.tm * SC_ROWS + (int)rank * SM_ROWS;
+      const int n0 = run.unit * SC_UNIT + (int)rank * (run.width * SC_UNIT / 2);     // this block's half of the items: boxes of 64
+      const uint32_t bytes = SC_A_BYTES + (uint32_t)run.width * (SC_UNIT / 2 * SC_BK * 2);
+      for (int kb = 0; kb < a.num_kb; ++kb) {
+        if (!mbar_wait_warp(empty_bar(s), ph ^ 1u, abort_flag)) { failed = true; break; }
+        const uint32_t lead_full = lead_bar0 + 8u * s;
+        const uint32_t sa = tiles + s * SC_STAGE, sb = sa + SC_A_BYTES;
+        if (elect_one()) {
+          mbar_arrive_expect_tx_remote(lead_full, bytes);
+          tma_load_2d_pair(sa, &users, kb * SC_BK, m0, lead_full);
+          tma_load_2d_pair(sb, &items, kb * SC_BK, n0, lead_full);
+          if (run.width == 2) tma_load_2d_pair(sb + 8192, &items, kb * SC_BK, n0 + 64, lead_full);
+        }
+        __syncwarp();
+        if (++s == SC_STAGES) { s = 0; ph ^= 1u; }
+      }
+    }
+  } else if (warp == 1 && go) {
+    // ------------------------------ products (leader) ------------------------------
+    if (rank == 0) {
+      constexpr uint32_t idesc0 = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(SC_ROWS >> 4) << 24);
+      int s = 0;
+      uint32_t ph = 0, it = 0;
+      const uint64_t da0 = make_desc(tiles, 16, 1024), db0 = make_desc(tiles + SC_A_BYTES, 16, 1024);
+      while (!failed && run.next()) {
+        const uint32_t idesc = idesc0 | ((uint32_t)(run.width * SC_UNIT >> 3) << 17);
+        const int buf = (int)(it & 1);
+        if (!mbar_wait_warp(tempty_bar(buf), ((it >> 1) & 1) ^ 1u, abort_flag)) { failed = true; break; }
+        tc_fence_after();
+        const uint32_t tmem_d = tmem_base + (uint32_t)(buf * SC_COLS);
+        for (int kb = 0; kb < a.num_kb; ++kb) {
+          if (!mbar_wait_warp(full_bar(s), ph, abort_flag)) { failed = true; break; }
+          tc_fence_after();
+          const uint32_t soff = (uint32_t)(s * (SC_STAGE >> 4));
+          if (elect_one()) {
+#pragma unroll
+            for (int k = 0; k < SC_BK / 16; ++k)
+              tc_mma_pair(tmem_d, da0 + soff + (uint64_t)(k * 2), db0 + soff + (uint64_t)(k * 2), idesc, (kb > 0 || k > 0) ? 1u : 0u);
+            tc_commit_pair(empty_bar(s));
+            if (kb == a.num_kb - 1) tc_commit_pair(tfull_bar(buf));
+          }
+          __syncwarp();
+          if (++s == SC_STAGES) { s = 0; ph ^= 1u; }
+        }
+        ++it;
+      }
+    }
+  } else if (go) {
+    // ------------------------------ statistics and lists (both blocks) ------------------------------
+    const int q = warp & 3, half = (warp - 2) >> 2;
+    const int row = (int)rank * SM_ROWS + q * 32 + lane;          // of the pair's tile
+    float* bias_w = bias_s + (warp - 2) * 128;
+    uint64_t* warp_lists = a.lists + ((int64_t)(pair * 2 + half) * SC_ROWS + (row - lane)) * a.cap;
+    uint64_t* list = warp_lists + (int64_t)lane * a.cap;
+    const uint32_t lane_addr = tmem_base + ((uint32_t)(q * 32) << 16);
+    RowStat r = row_empty();
+    int have = 0;
+    float bar = 0.f;
+    bool reached = false;
+    uint32_t it = 0;
+    const uint32_t lead_tempty = map_to_cta(tempty_bar(0), 0);
+    for (; !failed && run.next(); ++it) {
+      const int buf = (int)(it & 1), blocks = run.width * (SC_UNIT / 64);      // blocks of 32 columns
+      const int col0 = run.unit * SC_UNIT + half * blocks * 32;
+      const int64_t n = (int64_t)run.tm * SC_ROWS + row;
+      const bool active = n - lane < a.N;                         // of the warp
+      // columns past the table count as masked out
+      const float* bias = nullptr;
+      if (active && (a.bias || col0 + blocks * 32 > a.V)) {
+        for (int b = 0; b < blocks; ++b) {
+          const int v = col0 + b * 32 + lane;
+          bias_w[b * 32 + lane] = v >= a.V ? ROW_NEG_INF : a.bias ? __ldg(a.bias + v) : 0.f;
+        }
+        __syncwarp();
+        bias = bias_w;
+      }
+      if (!mbar_wait_warp(tfull_bar(buf), (it >> 1) & 1, abort_flag)) { failed = true; break; }
+      tc_fence_after();
+      if (active) {
+        const uint32_t taddr = lane_addr + (uint32_t)(buf * SC_COLS + half * blocks * 32);
+        if (run.first) {
+          r = row_empty();
+          have = 0;
+          reached = false;
+          if (TOP) {
+            bar = score_first_bar(taddr, bias, blocks, a.k);
+            if (n >= a.N) bar = __int_as_float(0x7f800000);
+          }
+        }
+        for (int b = 0; b < blocks; ++b) {
+          float x[32];
+          score_block(taddr + b * 32, bias ? bias + b * 32 : nullptr, x);
+          const float top = score_top(x);
+          score_add(r, x, top, a.c);
+          if constexpr (TOP) {
+            if (__any_sync(0xffffffffu, top >= bar)) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                if (x[j] >= bar) list[have++] = row_key(x[j], (uint32_t)(col0 + b * 32 + j));
+              if (!reached && have >= a.k) {                      // later entries must pass the bar
+                bar = row_order_logit(row_order(bar) + 1u);
+                reached = true;
+              }
+              uint32_t full = __ballot_sync(0xffffffffu, have > a.cap - 32);
+              __syncwarp();
+              while (full) {
+                const int of = __ffs(full) - 1;
+                full &= full - 1;
+                const float up = score_cut(warp_lists + (int64_t)of * a.cap, __shfl_sync(0xffffffffu, have, of), a.k);
+                if (lane == of) { have = a.k; bar = up; reached = true; }
+              }
+            }
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_remote(lead_tempty + 8u * buf);
+      if (active && run.last) {
+        if constexpr (TOP) {
+          if (run.leaves()) {                                     // the lists are needed again: the best go elsewhere
+            uint64_t* to = a.early + ((int64_t)(pair * 2 + half) * SC_ROWS + (row - lane)) * a.k;
+            __syncwarp();
+            for (int of = 0; of < 32; ++of) {
+              uint64_t* from = warp_lists + (int64_t)of * a.cap;
+              const int n_of = __shfl_sync(0xffffffffu, have, of);
+              if (n_of > a.k) (void)score_cut(from, n_of, a.k);
+              for (int i = lane; i < min(n_of, a.k); i += 32) to[(int64_t)of * a.k + i] = from[i];
+            }
+            have = min(have, a.k);
+            __syncwarp();
+          }
+        }
+        a.stats[((int64_t)(pair * 2 + run.part()) * 2 + half) * SC_ROWS + row] = make_float4(r.m, r.s, r.t, __int_as_float(have));
+      }
+    }
+  }
+  if (failed && lane == 0) {
+    *abort_flag = 1;
+    gram_device_fail(a.status, GRAM_ERR_TIMEOUT);
+  }
+  // ------------------------------ teardown ------------------------------
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) {
+    if (warp == 1 && lane == 0) {                       // let copies and MMAs already issued drain (bounded)
+      const uint64_t t0 = clock64();
+      while (clock64() - t0 < WAIT_LIMIT_CYCLES / 64) {}
+    }
     __syncthreads();
   }
-  if (n0 + ty < N && v0 + tx < V) z[(n0 + ty) * V + v0 + tx] = acc + (bias ? bias[v0 + tx] : 0.f);
+  gram_cluster_sync();                                  // the peer no longer reads this block's memory or signals its barriers
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+  }
+}
+
+// users[n] . items[v], by a warp
+__device__ __forceinline__ float score_dot(const bf16* u, const bf16* w, int d) {
+  const int lane = threadIdx.x & 31;
+  float sum = 0.f;
+  for (int i = lane; i < d / 8; i += 32) {
+    const uint4 a = __ldg(reinterpret_cast<const uint4*>(u) + i), b = __ldg(reinterpret_cast<const uint4*>(w) + i);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 x = x2_unpack(RowVec<bf16>::pair(a, j)), y = x2_unpack(RowVec<bf16>::pair(b, j));
+      sum = fmaf(x.x, y.x, sum);
+      sum = fmaf(x.y, y.y, sum);
+    }
+  }
+  if (lane < d % 8) sum = fmaf(__bfloat162float(u[d / 8 * 8 + lane]), __bfloat162float(w[d / 8 * 8 + lane]), sum);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  return sum;
+}
+
+// One block a user: joins the statistics of the runs that crossed its row tile, and their lists.
+__global__ void __launch_bounds__(LP_THREADS) score_join_kernel(const ScoreArgs a, const bf16* users, int64_t ld_u, const bf16* items, int64_t ld_i,
+                                                                int32_t d, float scale, RowAnswers ask) {
+  using G = Group<LP_THREADS>;
+  if (!chain_begin()) return;
+  __shared__ TopList<LP_THREADS> list;
+  __shared__ RowStat part[LP_WARPS];
+  __shared__ int have_of[LP_THREADS];
+  const int64_t n = blockIdx.x;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tm = (int)(n / SC_ROWS), row = (int)(n % SC_ROWS);
+  const int p0 = tm * a.units / a.per_run, p1 = ((tm + 1) * a.units - 1) / a.per_run, parts = (p1 - p0 + 1) * 2;     // at most 150
+  // of part i: pair p0 + i / 2, half i % 2
+  auto is_early = [&](int p) { return (min((p + 1) * a.per_run, a.total) - 1) / a.units != tm; };
+  RowStat r = row_empty();
+  int have = 0;
+  if (tid < parts) {
+    const int p = p0 + tid / 2;
+    const float4 f = a.stats[((int64_t)(p * 2 + tm - p * a.per_run / a.units) * 2 + (tid & 1)) * SC_ROWS + row];
+    r = RowStat{f.x, f.y, f.z};
+    have = __float_as_int(f.w);
+    have_of[tid] = have;
+  }
+  r = G::join(r, a.c, part);
+  const float log_s = row_log_sum(r);
+  if (tid == 0) {
+    if (ask.stats) { ask.stats[2 * n] = r.m; ask.stats[2 * n + 1] = log_s; }
+    if (ask.entropy) ask.entropy[n] = row_entropy(r);
+  }
+  for (int i = warp; i < ask.C; i += LP_WARPS) {
+    const int32_t t = ask.targets[n * ask.C + i];
+    float lp = 0.f;
+    if (t >= 0 && t < a.V) {
+      float z = score_dot(users + n * ld_u, items + (int64_t)t * ld_i, d);
+      if (a.bias) z += a.bias[t];
+      lp = row_logp(z, r.m, log_s, scale);
+    } else if (t != -1) {
+      gram_device_fail(a.status, GRAM_ERR_ID_RANGE);
+    }
+    if (lane == 0) ask.logp[n * ask.C + i] = lp;
+  }
+  if (ask.k == 0) return;
+  const int k = ask.k;
+  // f(key) for each key of this thread's share: a warp takes a list at a time
+  auto each = [&](auto f) {
+    for (int i = warp; i < parts; i += LP_WARPS) {
+      const int p = p0 + i / 2;
+      const int64_t at = (int64_t)(p * 2 + (i & 1)) * SC_ROWS + row;
+      const uint64_t* l = is_early(p) ? a.early + at * k : a.lists + at * a.cap;
+      for (int j = lane; j < have_of[i]; j += 32) f(l[j]);
+    }
+  };
+  const int all = G::sum(have, list.part);              // also the barrier behind have_of
+  uint64_t least = 1;
+  if (all > TopList<LP_THREADS>::CAP) {
+    uint64_t best = 0;
+    each([&](uint64_t key) { best = max(best, key); });
+    if (G::count(best != 0) >= k) least = kth_key(k, [&](uint64_t t) { return G::count(best >= t); });
+    int c = 0;
+    each([&](uint64_t key) { c += key >= least; });
+    if (G::sum(c, list.part) > TopList<LP_THREADS>::CAP)          // many equal or clustered logits: the k-th key itself
+      least = kth_key(k, [&](uint64_t t) {
+        int m = 0;
+        each([&](uint64_t key) { m += key >= t; });
+        return G::sum(m, list.part);
+      }, least);
+  }
+  if (tid == 0) list.slow = 0;
+  G::sync();
+  each([&](uint64_t key) {
+    if (key >= least) list.keys[atomicAdd(&list.slow, 1)] = key;
+  });
+  G::sync();
+  have = list.slow;
+  G::sync();
+  if (have > 256 && have > k) {
+    (void)top_cut(list, have, k);
+    have = k;
+  }
+  const int64_t o = n * k;
+  for (int i = tid; i < have; i += LP_THREADS) {
+    const uint64_t key = list.keys[i];
+    int above = 0;
+    for (int j = 0; j < have; ++j) above += list.keys[j] > key;
+    if (above < k) {
+      ask.top_ids[o + above] = row_key_place(key);
+      ask.top_logp[o + above] = row_logp(row_key_logit(key), r.m, log_s, scale);
+    }
+  }
+  for (int i = have + tid; i < k; i += LP_THREADS) {
+    ask.top_ids[o + i] = -1;
+    ask.top_logp[o + i] = ROW_NEG_INF;
+  }
+}
+
+template <bool TOP> cudaError_t launch_score(const CUtensorMap& users, const CUtensorMap& items, const ScoreArgs& a, int pairs, cudaStream_t st) {
+  auto kern = score_kernel<TOP>;
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SC_SMEM);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(2 * pairs));
+  cfg.blockDim = dim3(SC_THREADS);
+  cfg.dynamicSmemBytes = SC_SMEM;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1] = chain_attribute();
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kern, users, items, a);
 }
 
 }  // namespace
@@ -29,19 +520,58 @@ __global__ void __launch_bounds__(SC_TILE * SC_TILE) score_tile_kernel(const bf1
 gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_users, const void* items, int64_t ld_items,
                                   const float* bias, int64_t N, int32_t V, int32_t d, float scale, const RowAnswers& ask, void* ws,
                                   size_t ws_bytes, cudaStream_t st) {
-  const int64_t rows = (int64_t)(ws_bytes / sizeof(float)) / V;
-  if (rows < 1) return gram_set_error(ctx, "gram_score_logprobs: %d items", V), GRAM_ERR_UNSUPPORTED;
-  for (int64_t n = 0; n < N; n += rows) {
-    const int64_t now = N - n < rows ? N - n : rows;
-    launch_chain(score_tile_kernel, dim3((unsigned)ceil_div(V, SC_TILE), (unsigned)ceil_div64(now, SC_TILE)), SC_TILE * SC_TILE, 0, st,
-                 (const bf16*)users + n * ld_users, ld_users, (const bf16*)items, ld_items, bias, now, V, d, (float*)ws);
-    GRAM_LAUNCH_CHECK(ctx);
+  // Lists as long as the workspace allows for all pairs (up to 256 entries a thread; a longer one is cut less often); where
+  // that leaves less than 40 over k (small workspace, large k), lists of k + 64 and as many pairs as have room.
+  const size_t fixed = 2 * SC_PAIR_THREADS * sizeof(float4);
+  int pairs = kNumSMs / 2;
+  int64_t cap = 0;
+  if (ask.k) {
+    const int64_t room = (int64_t)(ws_bytes / pairs - fixed) / (SC_PAIR_THREADS * 8) - ask.k;
+    cap = room < SC_LIST_MAX ? room : SC_LIST_MAX;
+    if (cap < ask.k + 40) {
+      cap = ask.k + 64;
+      pairs = (int)(ws_bytes / (fixed + (size_t)(cap + ask.k) * SC_PAIR_THREADS * 8));
+      if (pairs > kNumSMs / 2) pairs = kNumSMs / 2;
+    }
+  }
+  const int32_t units = ceil_div(V, SC_UNIT);
+  int64_t most = pairs;                                 // row tiles of a launch: a run then touches two at most
+  if (most * units > (1 << 30)) most = (1 << 30) / units;
+  if (pairs < 1 || most < 1) return gram_set_error(ctx, "gram_score_logprobs: %d items, %d alternatives", V, ask.k), GRAM_ERR_UNSUPPORTED;
+  const int64_t tiles = ceil_div64(N, SC_ROWS), launches = ceil_div64(tiles, most), per_launch = ceil_div64(tiles, launches) * SC_ROWS;
+  CUtensorMap map_u, map_i;
+  if (!make_map(&map_i, items, (uint64_t)d, (uint64_t)V, (uint64_t)ld_items, SC_BK, 64))
+    return gram_set_error(ctx, "gram_score_logprobs: cannot describe the items"), GRAM_ERR_UNSUPPORTED;
+  ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * N * V * d, 2 * (int)launches, st, "score");
+  for (int64_t n = 0; n < N; n += per_launch) {
+    const int64_t now = N - n < per_launch ? N - n : per_launch;
+    const bf16* u = (const bf16*)users + n * ld_users;
+    if (!make_map(&map_u, u, (uint64_t)d, (uint64_t)now, (uint64_t)ld_users, SC_BK, SM_ROWS))
+      return gram_set_error(ctx, "gram_score_logprobs: cannot describe the users"), GRAM_ERR_UNSUPPORTED;
+    ScoreArgs a = {};
+    a.bias = bias;
+    a.N = now;
+    a.V = V;
+    a.num_kb = ceil_div(d, SC_BK);
+    a.k = ask.k;
+    a.cap = (int32_t)cap;
+    a.units = units;
+    a.total = (int32_t)(ceil_div64(now, SC_ROWS) * units);
+    a.per_run = ceil_div(a.total, pairs);
+    a.c = scale * 1.4426950408889634f;
+    a.stats = (float4*)ws;
+    a.lists = (uint64_t*)((uint8_t*)ws + fixed * pairs);
+    a.early = a.lists + (int64_t)pairs * SC_PAIR_THREADS * cap;
+    a.status = gram_status_word(ctx);
     RowAnswers part = ask;
     if (ask.C) { part.targets += n * ask.C; part.logp += n * ask.C; }
     if (ask.stats) part.stats += 2 * n;
     if (ask.entropy) part.entropy += n;
     if (ask.k) { part.top_logp += n * ask.k; part.top_ids += n * ask.k; }
-    GRAM_TRY(logprobs_launch(ctx, ws, GRAM_F32, V, now, V, scale, part, st));
+    const int used = ceil_div(a.total, a.per_run);
+    GRAM_CUDA(ctx, ask.k ? launch_score<true>(map_u, map_i, a, used, st) : launch_score<false>(map_u, map_i, a, used, st));
+    launch_chain(score_join_kernel, dim3((unsigned)now), LP_THREADS, 0, st, a, u, ld_users, (const bf16*)items, ld_items, d, scale, part);
+    GRAM_LAUNCH_CHECK(ctx);
   }
   return GRAM_OK;
 }
