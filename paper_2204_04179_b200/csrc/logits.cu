@@ -84,6 +84,29 @@ __device__ __forceinline__ RowStat join_slices(const RowStat* of, int slices, fl
   return row_join_lanes<MAX_SLICES>(i < slices ? of[i] : row_empty(), c);
 }
 
+// The statistics of a row whose largest logit m is huge (row_is_huge), by one group: relative to m itself, R = c m is not used.
+template <typename T, int TPR> __device__ __noinline__ float2 huge_sums(const T* z, int V, float m, float c, float* part) {
+  using G = Group<TPR>;
+  float s = 0.f, t = 0.f;
+  for (int v = G::tid(); v < V; v += TPR) {
+    const float y = (row_load(z + v) - m) * c, e = row_ex2(y);
+    s += e;
+    t = fmaf(e, fmaxf(y, -200.f), t);
+  }
+  s = G::sum(s, part);
+  t = G::sum(t, part);
+  return make_float2(s, t);
+}
+// of a row: ln of the sum of exp(scale (z - m)), the entropy
+struct RowLogs { float log_s, entropy; };
+template <typename T, int TPR> __device__ __forceinline__ RowLogs row_logs(const RowStat& r, const T* z, int V, float c, float* part) {
+  if (row_is_huge(r.m, c)) {
+    const float2 h = huge_sums<T, TPR>(z, V, r.m, c, part);
+    return RowLogs{logf(h.x), logf(h.x) - kLn2 * (h.y / h.x)};
+  }
+  return RowLogs{row_log_sum(r, c), row_entropy(r)};
+}
+
 // ------------------------------ log probabilities ---------------------------------------------------------------------
 template <typename T, int TPR, bool TOP>
 __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const T* logits, int64_t ld, int64_t N, int32_t V, float scale, int32_t slices,
@@ -92,6 +115,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const T* logits
   constexpr int NV = 4;
   if (!chain_begin()) return;
   __shared__ RowStat part[LP_WARPS], of_slice[MAX_SLICES];
+  __shared__ float fpart[LP_WARPS];
   __shared__ TopList<TPR> lists[TOP ? G::ROWS : 1];
   extern __shared__ uint64_t merged[];                  // [slices, k], sorted, in the first block of a cluster
   const int tid = G::tid(), rank = TPR == 32 ? 0 : blockIdx.x % slices;
@@ -146,10 +170,11 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const T* logits
     if (rank != 0) return;
     r = join_slices(of_slice, slices, c);
   }
-  const float log_s = row_log_sum(r);
+  const RowLogs logs = row_logs<T, TPR>(r, s.z, V, c, fpart);
+  const float log_s = logs.log_s;
   if (tid == 0) {
     if (ask.stats) { ask.stats[2 * n] = r.m; ask.stats[2 * n + 1] = log_s; }
-    if (ask.entropy) ask.entropy[n] = row_entropy(r);
+    if (ask.entropy) ask.entropy[n] = logs.entropy;
   }
   for (int i = tid; i < ask.C; i += TPR) {
     const int32_t t = ask.targets[n * ask.C + i];
@@ -207,7 +232,7 @@ template <typename T> __device__ __forceinline__ void store_vector(T* dz, int pl
     for (int j = 0; j < RowVec<T>::N; ++j) dz[place + j] = e[j];
   }
 }
-// f(pair of logits) -> pair of results, over a chunk that is in registers
+// f(logit) -> result, over a chunk that is in registers
 template <typename T, int TPR, int NV, typename F>
 __device__ __forceinline__ void store_chunk(const Slice<T>& s, int ch, int tid, const uint4 (&q)[NV], T* dz, bool vec, F f) {
   const int v = s.v0 + ch * (TPR * NV) + tid;
@@ -216,11 +241,25 @@ __device__ __forceinline__ void store_chunk(const Slice<T>& s, int ch, int tid, 
     if (v + i * TPR < s.v1) {
       uint4 o;
 #pragma unroll
-      for (int j = 0; j < RowVec<T>::N / 2; ++j) RowVec<T>::put(o, j, f(RowVec<T>::pair(q[i], j)));
+      for (int j = 0; j < RowVec<T>::N / 2; ++j) {
+        const float2 x = RowVec<T>::pair(q[i], j);
+        RowVec<T>::put(o, j, make_float2(f(x.x), f(x.y)));
+      }
       store_vector(dz, s.place(v + i * TPR), o, vec);
     }
   }
 }
+
+// p of a logit x, given its row's statistics: 2^y / s, y = c x - R(m) as in row_softmax.cuh, or c (x - m) in a row of huge logits.
+struct RowPower {
+  float m, c, ref, log2_s;           // log2_s: of the sum that belongs to y
+  bool is_huge;
+  __device__ __forceinline__ RowPower(float m_, float log_s, float c_) : m(m_), c(c_), ref(row_ref(m_, c_)), is_huge(row_is_huge(m_, c_)) {
+    log2_s = log_s * kLog2e + (is_huge ? 0.f : fmaf(m, c, -ref));
+  }
+  __device__ __forceinline__ float plain(float x) const { return fmaf(x, c, -ref); }
+  __device__ __forceinline__ float huge(float x) const { return (x - m) * c; }
+};
 
 struct BackwardArgs {
   const int32_t* targets;
@@ -235,7 +274,8 @@ struct BackwardArgs {
 };
 
 // dz = scale (sum of g at the given places - p (sum of all g + h (log p + H))), 0 at masked places.  With l = log2 p the
-// dense part is 2^l (A + B l), A = -scale (G + h H), B = -scale h ln 2; l is held at -200 as in row_softmax.cuh.
+// dense part is 2^l (A + B l), A = -scale (G + h H), B = -scale h ln 2, or in y = l + log2 s, which takes one rounding less per
+// element, 2^y (A - B log2 s + B y) / s; y is held at -200 as in row_softmax.cuh.
 template <typename T, int TPR>
 __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_backward_kernel(const T* logits, T* dlogits, BackwardArgs a) {
   using G = Group<TPR>;
@@ -266,23 +306,23 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_backward_kernel(const 
   else G::sync();
   float sum = 0.f;
   for (int i = 0; i < a.C; ++i) sum += mine.g[i];
-  const float m = row_base(a.stats[2 * n]), ls2 = a.stats[2 * n + 1] * kLog2e, h = a.dentropy ? a.dentropy[n] : 0.f;
+  const float m = a.stats[2 * n], log_s = a.stats[2 * n + 1], h = a.dentropy ? a.dentropy[n] : 0.f;
   const float c = a.scale * kLog2e, A = -a.scale * (sum + (a.dentropy ? h * a.entropy[n] : 0.f)), B = -a.scale * h * kLn2;
-  const bool none = (sum == 0.f && h == 0.f) || ls2 == ROW_NEG_INF;      // nothing asked, or nothing left in the row
-  const f32x2 mb = x2_pack(-m, -m), cc = x2_pack(c, c), lb = x2_pack(-ls2, -ls2), AA = x2_pack(A, A), BB = x2_pack(B, B);
-  auto dense2 = [&](f32x2 x) {
-    const float2 y = x2_unpack(x2_fma(x2_add(x, mb), cc, lb));
-    const float l0 = row_hold(y.x), l1 = row_hold(y.y);
-    return x2_unpack(x2_mul(x2_pack(row_ex2(l0), row_ex2(l1)), x2_fma(x2_pack(l0, l1), BB, AA)));
-  };
-  auto dense = [&](float x) { return none || x == ROW_NEG_INF ? 0.f : dense2(x2_pack(x, x)).x; };
+  const bool none = (sum == 0.f && h == 0.f) || log_s == ROW_NEG_INF;    // nothing asked, or nothing left in the row
+  const RowPower l(m, log_s, c);
+  const float inv = exp2f(-l.log2_s), Ay = inv * fmaf(-B, l.log2_s, A), By = inv * B;
+  auto value = [&](float y) { return row_ex2(y) * fmaf(fmaxf(y, -200.f), By, Ay); };
+  auto dense = [&](float x) { return value(l.plain(x)); };
+  auto dense_huge = [&](float x) { return value(l.huge(x)); };
+  auto one = [&](float x) { return none || x == ROW_NEG_INF ? 0.f : l.is_huge ? dense_huge(x) : dense(x); };
   const int chunks = s.template chunks<TPR, NV>();
   for (int ch = 0; ch < chunks; ++ch) {
     if (ch > 0 && !none) s.template load_chunk<TPR, NV>(ch, tid, q);
-    if (none) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, [](f32x2) { return make_float2(0.f, 0.f); });
-    else store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, dense2);
+    if (none) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, [](float) { return 0.f; });
+    else if (l.is_huge) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, dense_huge);
+    else store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, dense);
   }
-  if (edge_place >= 0) dz[edge_place] = row_round<T>(dense(edge));
+  if (edge_place >= 0) dz[edge_place] = row_round<T>(one(edge));
   G::sync();                                             // the given places are written again, by one thread each
   for (int i = tid; i < a.C; i += TPR) {
     const int p = mine.place[i];
@@ -294,7 +334,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_backward_kernel(const 
         first = first && j >= i;
         g += mine.g[j];
       }
-    if (first) dz[p] = row_round<T>(dense(mine.z[i]) + a.scale * g);
+    if (first) dz[p] = row_round<T>(one(mine.z[i]) + a.scale * g);
   }
 }
 
@@ -353,7 +393,16 @@ __global__ void __launch_bounds__(LP_THREADS, 4) distill_kernel(const T* logits,
     gram_cluster_sync();                                 // all have read the teacher's places by now, too
     r = join_slices(of_slice, a.slices, c);
   }
-  const float log_s = row_log_sum(r), m = row_base(r.m), log_t = row_log_sum(t);
+  const float log_s = row_logs<T, TPR>(r, s.z, a.V, c, fpart).log_s;
+  float log_t = row_log_sum(t, c);
+  if (row_is_huge(t.m, c)) {
+    float sum = 0.f;
+    for (int i = tid; i < a.k; i += TPR)
+      if (mine.place[i] >= 0) sum += row_ex2((mine.q[i] - t.m) * c);
+    log_t = logf(G::sum(sum, fpart));
+  }
+  // such a row was read again as a whole: in place, no slice may be overwritten before all have done so
+  if (TPR > 32 && a.slices > 1 && row_is_huge(r.m, c)) gram_cluster_sync();
   float loss = 0.f;
   for (int i = tid; i < a.k; i += TPR) {
     float qi = 0.f;
@@ -373,18 +422,18 @@ __global__ void __launch_bounds__(LP_THREADS, 4) distill_kernel(const T* logits,
   const bool none = w == 0.f || t.s == 0.f;
   T* dz = dlogits + n * a.ld_out;
   const bool vec = same_alignment(s.z, dz);
-  const float ls2 = log_s * kLog2e;
-  const f32x2 mb = x2_pack(-m, -m), cc = x2_pack(c, c), lb = x2_pack(-ls2, -ls2), ww = x2_pack(w, w);
-  auto dense2 = [&](f32x2 x) {
-    const float2 y = x2_unpack(x2_fma(x2_add(x, mb), cc, lb));
-    return x2_unpack(x2_mul(x2_pack(row_ex2(y.x), row_ex2(y.y)), ww));
-  };
+  const RowPower l(r.m, log_s, c);
+  const float w_s = w * exp2f(-l.log2_s);
+  auto dense = [&](float x) { return w_s * row_ex2(l.plain(x)); };
+  auto dense_huge = [&](float x) { return w_s * row_ex2(l.huge(x)); };
+  auto one = [&](float x) { return l.is_huge ? dense_huge(x) : dense(x); };
   for (int ch = chunks - 1; ch >= 0; --ch) {
     if (ch < chunks - 1 && !none) s.template load_chunk<TPR, NV>(ch, tid, q);
-    if (none) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, [](f32x2) { return make_float2(0.f, 0.f); });
-    else store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, dense2);
+    if (none) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, [](float) { return 0.f; });
+    else if (l.is_huge) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, dense_huge);
+    else store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, dense);
   }
-  if (edge_place >= 0) dz[edge_place] = row_round<T>(none ? 0.f : dense2(x2_pack(edge, edge)).x);
+  if (edge_place >= 0) dz[edge_place] = row_round<T>(none ? 0.f : one(edge));
   G::sync();                                             // the teacher's places are written again, by one thread each
   if (none) return;
   for (int i = tid; i < a.k; i += TPR) {
@@ -397,7 +446,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) distill_kernel(const T* logits,
         first = first && j >= i;
         sum += mine.q[j];
       }
-    if (first) dz[p] = row_round<T>(dense2(x2_pack(mine.z[i], mine.z[i])).x - w * sum);
+    if (first) dz[p] = row_round<T>(one(mine.z[i]) - w * sum);
   }
 }
 

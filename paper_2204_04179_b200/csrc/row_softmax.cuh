@@ -1,11 +1,16 @@
 // Softmax statistics of a row that is read once, and the order of its entries, shared by the kernels on logits.
 //
-// A row's statistics are (m, s, t): m the largest logit, s = sum of e, t = sum of e y over e = 2^y, y = c (z - m),
-// c = scale log2(e).  The difference z - m is taken before the product, so that logits of the type's lowest value stay what
-// they are: scale z alone could overflow.  Then log p(z) = scale (z - m) - ln s and the entropy is ln 2 (log2 s - t / s).
-// A masked place (-inf) has y = -inf; y is held at -200, where 2^y is 0 in 32 bits, so that e y is 0 there and not NaN.  The
-// hold passes a NaN on, so a NaN (or +inf, whose z - m is one) reaches s and everything computed from it.
+// A row's statistics are (m, s, t): m the largest logit, s = sum of e, t = sum of e y over e = 2^y, y = c z - R(m),
+// c = scale log2(e).  R(m) is c m rounded to a whole number: c z - R is one fused multiply-add with a single rounding, and
+// statistics of different m differ by exact powers of two.  Then ln sum exp(scale (z - m)) = ln s + ln 2 (R - c m), and the
+// entropy is ln 2 (log2 s - t / s).
+// A masked place (-inf) has e = 0; in t its y is held at -200, so that e y is 0 and not NaN.  A NaN (or +inf, whose c z - R is
+// one) reaches s and everything computed from it.
+// Logits so large that c m has no place left for a fraction (all places of a row at the type's lowest value) are the exception,
+// row_is_huge: their rows are summed again with the difference z - m taken first.
 #pragma once
+#include <float.h>
+
 #include "gram_internal.h"
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -19,50 +24,39 @@ __device__ __forceinline__ float row_ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ float row_hold(float y) {   // at least -200; NaN stays NaN
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(y), "f"(-200.f));
-  return r;
-}
-// what differences are taken to: a row with nothing in it has m = -inf
-__device__ __forceinline__ float row_base(float m) { return m == ROW_NEG_INF ? 0.f : m; }
+// R(m), held at -2^23: a thread that has seen nothing, or only logits of the type's lowest value, keeps sums of 0
+__device__ __forceinline__ float row_ref(float m, float c) { return fmaxf(rintf(m * c), -8388608.f); }
+__device__ __forceinline__ bool row_is_huge(float m, float c) { return fabsf(m) <= FLT_MAX && !(fabsf(m * c) <= 4194304.f); }
 __device__ __forceinline__ RowStat row_empty() { return RowStat{ROW_NEG_INF, 0.f, 0.f}; }
-__device__ __forceinline__ RowStat row_join(const RowStat& a, const RowStat& b, float c) {
-  RowStat r;
-  r.m = fmaxf(a.m, b.m);
-  const float base = row_base(r.m);
-  const float da = row_hold((a.m - base) * c), db = row_hold((b.m - base) * c);
-  const float fa = row_ex2(da), fb = row_ex2(db);
-  r.s = a.s * fa + b.s * fb;
-  r.t = fa * (a.t + a.s * da) + fb * (b.t + b.s * db);
-  return r;
-}
 // r's statistics as they are with a larger m
 __device__ __forceinline__ void row_raise(RowStat& r, float m, float c) {
-  const float d = row_hold((r.m - m) * c), f = row_ex2(d);
-  r.t = f * (r.t + r.s * d);
+  const float d = fmaxf(row_ref(r.m, c) - row_ref(m, c), -200.f), f = row_ex2(d);
+  r.t = f * fmaf(r.s, d, r.t);
   r.s *= f;
   r.m = m;
 }
 __device__ __forceinline__ void row_add(RowStat& r, float z, float c) {
   if (z > r.m) row_raise(r, z, c);
-  const float y = row_hold((z - row_base(r.m)) * c), e = row_ex2(y);
+  const float y = fmaf(z, c, -row_ref(r.m, c)), e = row_ex2(y);
   r.s += e;
-  r.t += e * y;
+  r.t = fmaf(e, fmaxf(y, -200.f), r.t);
 }
-// the statistics of L neighbouring lanes, in all of them; the lower lane's come first on both sides, so that all get the same bits
+// the statistics of L neighbouring lanes, in all of them
 template <int L> __device__ __forceinline__ RowStat row_join_lanes(RowStat r, float c) {
+  float m = r.m;
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (m > r.m) row_raise(r, m, c);
 #pragma unroll
   for (int o = L / 2; o > 0; o >>= 1) {
-    RowStat x;
-    x.m = __shfl_xor_sync(0xffffffffu, r.m, o);
-    x.s = __shfl_xor_sync(0xffffffffu, r.s, o);
-    x.t = __shfl_xor_sync(0xffffffffu, r.t, o);
-    r = (threadIdx.x & o) ? row_join(x, r, c) : row_join(r, x, c);
+    r.s += __shfl_xor_sync(0xffffffffu, r.s, o);
+    r.t += __shfl_xor_sync(0xffffffffu, r.t, o);
   }
   return r;
 }
-__device__ __forceinline__ float row_log_sum(const RowStat& r) { return logf(r.s); }
+__device__ __forceinline__ float row_log_sum(const RowStat& r, float c) {
+  return r.m == ROW_NEG_INF ? logf(r.s) : fmaf(fmaf(-r.m, c, row_ref(r.m, c)), kLn2, logf(r.s));
+}
 __device__ __forceinline__ float row_entropy(const RowStat& r) { return r.s == 0.f ? 0.f : logf(r.s) - kLn2 * (r.t / r.s); }
 __device__ __forceinline__ float row_logp(float z, float m, float log_s, float scale) {
   if (z == ROW_NEG_INF) return log_s != log_s ? log_s : z;
@@ -158,36 +152,6 @@ template <int TPR> struct Group {
   }
 };
 
-// ---------------------------------------------------------------------------
-// Sixteen bytes of a row, and pairs of fp32 values in one register pair (one instruction for the two).
-// ---------------------------------------------------------------------------
-typedef uint64_t f32x2;
-__device__ __forceinline__ f32x2 x2_pack(float a, float b) {
-  f32x2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ float2 x2_unpack(f32x2 v) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-  return r;
-}
-__device__ __forceinline__ f32x2 x2_add(f32x2 a, f32x2 b) {
-  f32x2 r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ f32x2 x2_mul(f32x2 a, f32x2 b) {
-  f32x2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ f32x2 x2_fma(f32x2 a, f32x2 b, f32x2 c) {
-  f32x2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-
 template <typename T> struct RowVec;                 // 16 bytes of logits
 template <> struct RowVec<float> {
   static constexpr int N = 4;
@@ -195,8 +159,8 @@ template <> struct RowVec<float> {
   static __device__ __forceinline__ float top(const uint4& q) {
     return fmaxf(fmaxf(__uint_as_float(q.x), __uint_as_float(q.y)), fmaxf(__uint_as_float(q.z), __uint_as_float(q.w)));
   }
-  static __device__ __forceinline__ f32x2 pair(const uint4& q, int i) {
-    return i == 0 ? x2_pack(__uint_as_float(q.x), __uint_as_float(q.y)) : x2_pack(__uint_as_float(q.z), __uint_as_float(q.w));
+  static __device__ __forceinline__ float2 pair(const uint4& q, int i) {
+    return i == 0 ? make_float2(__uint_as_float(q.x), __uint_as_float(q.y)) : make_float2(__uint_as_float(q.z), __uint_as_float(q.w));
   }
   static __device__ __forceinline__ void put(uint4& q, int i, float2 v) {
     if (i == 0) { q.x = __float_as_uint(v.x); q.y = __float_as_uint(v.y); }
@@ -211,9 +175,9 @@ template <> struct RowVec<bf16> {
     const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
     return fmaxf(__low2float(m), __high2float(m));
   }
-  static __device__ __forceinline__ f32x2 pair(const uint4& q, int i) {
+  static __device__ __forceinline__ float2 pair(const uint4& q, int i) {
     const uint32_t w = i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w;
-    return x2_pack(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
   }
   static __device__ __forceinline__ void put(uint4& q, int i, float2 v) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
@@ -226,21 +190,20 @@ template <> struct RowVec<bf16> {
 template <typename T, int NV>
 __device__ __forceinline__ void row_add_vectors(RowStat& r, const uint4 (&q)[NV], float top, float c) {
   if (top > r.m) row_raise(r, top, c);
-  const float base = row_base(r.m);
-  const f32x2 mb = x2_pack(-base, -base), cc = x2_pack(c, c);
-  f32x2 s = x2_pack(0.f, 0.f), t = s;
+  const float ref = -row_ref(r.m, c);
+  float s[2] = {}, t[2] = {};
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
 #pragma unroll
     for (int j = 0; j < RowVec<T>::N / 2; ++j) {
-      const float2 y = x2_unpack(x2_mul(x2_add(RowVec<T>::pair(q[i], j), mb), cc));
-      const float y0 = row_hold(y.x), y1 = row_hold(y.y);
-      const f32x2 e = x2_pack(row_ex2(y0), row_ex2(y1));
-      s = x2_add(s, e);
-      t = x2_fma(e, x2_pack(y0, y1), t);
+      const float2 x = RowVec<T>::pair(q[i], j);
+      const float y0 = fmaf(x.x, c, ref), y1 = fmaf(x.y, c, ref), e0 = row_ex2(y0), e1 = row_ex2(y1);
+      s[0] += e0;
+      s[1] += e1;
+      t[0] = fmaf(e0, fmaxf(y0, -200.f), t[0]);
+      t[1] = fmaf(e1, fmaxf(y1, -200.f), t[1]);
     }
   }
-  const float2 s2 = x2_unpack(s), t2 = x2_unpack(t);
-  r.s += s2.x + s2.y;
-  r.t += t2.x + t2.y;
+  r.s += s[0] + s[1];
+  r.t += t[0] + t[1];
 }

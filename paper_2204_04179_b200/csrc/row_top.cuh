@@ -7,8 +7,6 @@
 // it is cut to its best k, the last of which sets the new bar; a chunk that would overflow the list (equal logits, ascending
 // rows) gives its own best k, found by bisection over the keys.
 #pragma once
-#include <float.h>
-
 #include "row_softmax.cuh"
 
 template <int TPR> struct TopList {
@@ -32,7 +30,7 @@ template <typename T, int TPR, int NV> struct TopChunk {
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int j = 0; j < RowVec<T>::N / 2; ++j) {
-        const float2 x = x2_unpack(RowVec<T>::pair(q[i], j));
+        const float2 x = RowVec<T>::pair(q[i], j);
         const int p = place0 + i * (TPR * RowVec<T>::N) + 2 * j;
         f(x.x, p);
         f(x.y, p + 1);

@@ -118,20 +118,16 @@ __device__ __forceinline__ float score_top(const float (&x)[32]) {
 }
 __device__ __forceinline__ void score_add(RowStat& r, const float (&x)[32], float top, float c) {
   if (top > r.m) row_raise(r, top, c);
-  const float base = row_base(r.m);
-  const f32x2 mb = x2_pack(-base, -base), cc = x2_pack(c, c);
-  f32x2 s = x2_pack(0.f, 0.f), t = s;
+  const float ref = -row_ref(r.m, c);
+  float s[2] = {}, t[2] = {};
 #pragma unroll
-  for (int j = 0; j < 16; ++j) {
-    const float2 y = x2_unpack(x2_mul(x2_add(x2_pack(x[2 * j], x[2 * j + 1]), mb), cc));
-    const float y0 = row_hold(y.x), y1 = row_hold(y.y);
-    const f32x2 e = x2_pack(row_ex2(y0), row_ex2(y1));
-    s = x2_add(s, e);
-    t = x2_fma(e, x2_pack(y0, y1), t);
+  for (int j = 0; j < 32; ++j) {
+    const float y = fmaf(x[j], c, ref), e = row_ex2(y);
+    s[j & 1] += e;
+    t[j & 1] = fmaf(e, fmaxf(y, -200.f), t[j & 1]);
   }
-  const float2 s2 = x2_unpack(s), t2 = x2_unpack(t);
-  r.s += s2.x + s2.y;
-  r.t += t2.x + t2.y;
+  r.s += s[0] + s[1];
+  r.t += t[0] + t[1];
 }
 // A first bar for each lane's row from its columns of the first tile: a value that k of them reach, and few more.
 __device__ __forceinline__ float score_first_bar(uint32_t taddr, const float* b, int blocks, int k) {
@@ -389,7 +385,7 @@ __device__ __forceinline__ float score_dot(const bf16* u, const bf16* w, int d) 
     const uint4 a = __ldg(reinterpret_cast<const uint4*>(u) + i), b = __ldg(reinterpret_cast<const uint4*>(w) + i);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float2 x = x2_unpack(RowVec<bf16>::pair(a, j)), y = x2_unpack(RowVec<bf16>::pair(b, j));
+      const float2 x = RowVec<bf16>::pair(a, j), y = RowVec<bf16>::pair(b, j);
       sum = fmaf(x.x, y.x, sum);
       sum = fmaf(x.y, y.y, sum);
     }
@@ -407,6 +403,7 @@ __global__ void __launch_bounds__(LP_THREADS) score_join_kernel(const ScoreArgs 
   if (!chain_begin()) return;
   __shared__ TopList<LP_THREADS> list;
   __shared__ RowStat part[LP_WARPS];
+  __shared__ float fpart[LP_WARPS];
   __shared__ int have_of[LP_THREADS];
   const int64_t n = blockIdx.x;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -424,10 +421,23 @@ __global__ void __launch_bounds__(LP_THREADS) score_join_kernel(const ScoreArgs 
     have_of[tid] = have;
   }
   r = G::join(r, a.c, part);
-  const float log_s = row_log_sum(r);
+  float log_s = row_log_sum(r, a.c), entropy = row_entropy(r);
+  if (row_is_huge(r.m, a.c)) {                          // summed again, relative to m itself
+    float s = 0.f, t = 0.f;
+    for (int v = warp; v < a.V; v += LP_WARPS) {
+      const float z = score_dot(users + n * ld_u, items + (int64_t)v * ld_i, d) + (a.bias ? a.bias[v] : 0.f);
+      const float y = (z - r.m) * a.c, e = row_ex2(y);
+      s += e;
+      t = fmaf(e, fmaxf(y, -200.f), t);
+    }
+    s = G::sum(lane == 0 ? s : 0.f, fpart);
+    t = G::sum(lane == 0 ? t : 0.f, fpart);
+    log_s = logf(s);
+    entropy = log_s - kLn2 * (t / s);
+  }
   if (tid == 0) {
     if (ask.stats) { ask.stats[2 * n] = r.m; ask.stats[2 * n + 1] = log_s; }
-    if (ask.entropy) ask.entropy[n] = row_entropy(r);
+    if (ask.entropy) ask.entropy[n] = entropy;
   }
   for (int i = warp; i < ask.C; i += LP_WARPS) {
     const int32_t t = ask.targets[n * ask.C + i];
