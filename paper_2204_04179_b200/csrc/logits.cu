@@ -1,15 +1,18 @@
 // Answers read from rows of logits, and their gradients (gram_logprobs, gram_logprobs_backward, gram_distill).
 //
-// All three are bound by the bytes of the logits: each is read once, and a gradient is written once.  A row belongs to a
-// group of threads, a warp for short rows (eight rows a block) or a block of 256, and where a row is long or rows are few,
-// to a cluster of up to 16 blocks with a contiguous slice each, whose statistics meet in distributed shared memory.  Rows
-// begin anywhere (a stride of 30 522 bf16 leaves them on 4-byte boundaries): the places up to the first 16-byte boundary
-// and after the last are single elements of the slice's first threads, all others move 16 bytes at a time.
+// All three are bound by the bytes of the logits: each is read from HBM once, and a gradient is written once.  A row belongs
+// to a group of threads, a warp for short rows (four rows a block) or a block of 128, and where a row is long or rows are
+// few, to a cluster of up to 16 blocks with a contiguous slice each, whose statistics meet in distributed shared memory.
+// Rows begin anywhere (a stride of 30 522 bf16 leaves them on 4-byte boundaries): the places up to the first 16-byte
+// boundary and after the last are single elements of the slice's first threads, all others move 16 bytes at a time, four
+// vectors a thread and chunk, the next chunk's on their way while one is added up.
 #include "logits.h"
 #include "row_softmax.cuh"
 #include "row_top.cuh"
 
 namespace {
+
+constexpr int LP_THREADS = 128, LP_WARPS = LP_THREADS / 32;      // of a block
 
 // ------------------------------ a slice of a row ----------------------------------------------------------------------
 // Places [0, head) and [tail, V) are single elements, of the first and the last slice; the vectors between them are split
@@ -19,12 +22,12 @@ template <typename T> struct Slice {
   const T* z;                    // the row
   int head, tail, V, v0, v1;
   bool first, last;
-  __device__ __forceinline__ Slice(const T* row, int V_, int rank, int slices) : z(row), V(V_), first(rank == 0), last(rank == slices - 1) {
+  __device__ __forceinline__ Slice(const T* row, int V_, int rank, int shift) : z(row), V(V_), first(rank == 0), last(rank == (1 << shift) - 1) {
     const int past = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
     head = min(past ? N - past : 0, V);
     const int nv = (V - head) / N;
     tail = head + nv * N;
-    const int per = (nv + slices - 1) / slices;
+    const int per = (nv + (1 << shift) - 1) >> shift;     // 2^shift slices
     v0 = min(rank * per, nv);
     v1 = min(v0 + per, nv);
   }
@@ -34,32 +37,36 @@ template <typename T> struct Slice {
     return last && tid < 16 && tail + tid - 8 < V ? tail + tid - 8 : -1;
   }
   __device__ __forceinline__ int place(int v) const { return head + v * N; }
-  __device__ __forceinline__ uint4 load(int v) const { return __ldcs(reinterpret_cast<const uint4*>(z + head) + v); }
+  template <bool LAST> __device__ __forceinline__ uint4 load(int v) const {        // LAST: nobody reads it again
+    const uint4* p = reinterpret_cast<const uint4*>(z + head) + v;
+    return LAST ? __ldcs(p) : *p;
+  }
   __device__ __forceinline__ bool has(int p) const {
     if (p < head) return first;
     if (p >= tail) return last;
     return p >= place(v0) && p < place(v1);
   }
   template <int TPR, int NV> __device__ __forceinline__ int chunks() const { return max(1, (v1 - v0 + TPR * NV - 1) / (TPR * NV)); }
-  template <int TPR, int NV> __device__ __forceinline__ void load_chunk(int ch, int tid, uint4 (&q)[NV]) const {
+  template <int TPR, int NV, bool LAST> __device__ __forceinline__ void load_chunk(int ch, int tid, uint4 (&q)[NV]) const {
     const int v = v0 + ch * (TPR * NV) + tid;
     if (v - tid + TPR * NV <= v1) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) q[i] = load(v + i * TPR);
+      for (int i = 0; i < NV; ++i) q[i] = load<LAST>(v + i * TPR);
     } else {
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         constexpr uint32_t none = RowVec<T>::NONE;
         q[i] = make_uint4(none, none, none, none);
-        if (v + i * TPR < v1) q[i] = load(v + i * TPR);
+        if (v + i * TPR < v1) q[i] = load<LAST>(v + i * TPR);
       }
     }
   }
 };
-template <typename T, int NV> __device__ __forceinline__ float chunk_top(const uint4 (&q)[NV]) {
-  float top = ROW_NEG_INF;
+// the largest of the vectors [A, B)
+template <typename T, int A, int B, int NV> __device__ __forceinline__ float chunk_top(const uint4 (&q)[NV]) {
+  float top = RowVec<T>::top(q[A]);
 #pragma unroll
-  for (int i = 0; i < NV; ++i) top = fmaxf(top, RowVec<T>::top(q[i]));
+  for (int i = A + 1; i < B; ++i) top = fmaxf(top, RowVec<T>::top(q[i]));
   return top;
 }
 
@@ -109,22 +116,22 @@ template <typename T, int TPR> __device__ __forceinline__ RowLogs row_logs(const
 
 // ------------------------------ log probabilities ---------------------------------------------------------------------
 template <typename T, int TPR, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const T* logits, int64_t ld, int64_t N, int32_t V, float scale, int32_t slices,
+__global__ void __launch_bounds__(LP_THREADS, 7) logprobs_kernel(const T* logits, int64_t ld, int64_t N, int32_t V, float scale, int32_t shift,
                                                                  RowAnswers ask, int32_t* status) {
   using G = Group<TPR>;
   constexpr int NV = 4;
   if (!chain_begin()) return;
   __shared__ RowStat part[LP_WARPS], of_slice[MAX_SLICES];
   __shared__ float fpart[LP_WARPS];
-  __shared__ TopList<TPR> lists[TOP ? G::ROWS : 1];
+  __shared__ TopList<TPR> lists[TOP ? (LP_THREADS / TPR) : 1];
   extern __shared__ uint64_t merged[];                  // [slices, k], sorted, in the first block of a cluster
-  const int tid = G::tid(), rank = TPR == 32 ? 0 : blockIdx.x % slices;
-  const int64_t n = TPR == 32 ? (int64_t)blockIdx.x * G::ROWS + G::row() : blockIdx.x / slices;
+  const int slices = TPR == 32 ? 1 : 1 << shift, tid = G::tid(), rank = blockIdx.x & (slices - 1);
+  const int64_t n = TPR == 32 ? (int64_t)blockIdx.x * LP_WARPS + G::row() : blockIdx.x >> shift;
   if (TPR > 32 && slices > 1) gram_cluster_sync();      // every block of the cluster runs before another writes to it
   if (n >= N) return;                                   // whole warps, in the form that has no barrier over the block
   TopList<TPR>& list = lists[TOP ? G::row() : 0];
   const float c = scale * kLog2e;
-  const Slice<T> s(logits + n * ld, V, rank, slices);
+  const Slice<T> s(logits + n * ld, V, rank, shift);
   const int chunks = s.template chunks<TPR, NV>();
   const int edge_place = s.edge(tid);
   const float edge = edge_place >= 0 ? row_load(s.z + edge_place) : ROW_NEG_INF;
@@ -134,23 +141,28 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(const T* logits
     if (tid == 0) list.added[0] = 0;
     G::sync();
   }
+  uint4 q[NV], next[NV];
+  s.template load_chunk<TPR, NV, true>(0, tid, q);
   for (int ch = 0; ch < chunks; ++ch) {
-    uint4 q[NV];
-    s.template load_chunk<TPR, NV>(ch, tid, q);
-    float top = chunk_top<T, NV>(q);
-    row_add_vectors<T, NV>(r, q, top, c);
+    if (ch + 1 < chunks) s.template load_chunk<TPR, NV, true>(ch + 1, tid, next);
+    float a = chunk_top<T, 0, NV / 2>(q), b = chunk_top<T, NV / 2, NV>(q);
+    row_add_vectors<T, NV>(r, q, fmaxf(a, b), c);
     const bool on_edge = edge_place >= 0 && (tid < 8 ? ch == 0 : ch == chunks - 1);
     if (on_edge) {
       row_add(r, edge, c);
-      top = fmaxf(top, edge);
+      a = fmaxf(a, edge);
     }
     if constexpr (TOP)
-      top_chunk(list, st, TopChunk<T, TPR, NV>{q, s.place(s.v0 + ch * (TPR * NV) + tid), on_edge ? edge : ROW_NEG_INF, edge_place}, top, ask.k, ch,
+      top_chunk(list, st, TopChunk<T, TPR, NV>{q, s.place(s.v0 + ch * (TPR * NV) + tid), on_edge ? edge : ROW_NEG_INF, edge_place}, a, b, ask.k, ch,
                 ch == chunks - 1);
+    if (ch + 1 < chunks) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) q[i] = next[i];
+    }
   }
   r = G::join(r, c, part);
   if constexpr (TOP) {
-    if (st.have > 256 && st.have > ask.k) {
+    if (st.have > ask.k + ask.k / 4 + 16) {
       (void)top_cut(list, st.have, ask.k);
       st.have = ask.k;
     }
@@ -268,7 +280,7 @@ struct BackwardArgs {
   const float* dlogp;
   const float* dentropy;
   int64_t ld, ld_out, N;
-  int32_t V, C, slices;
+  int32_t V, C, shift;
   float scale;
   int32_t* status;
 };
@@ -277,20 +289,20 @@ struct BackwardArgs {
 // dense part is 2^l (A + B l), A = -scale (G + h H), B = -scale h ln 2, or in y = l + log2 s, which takes one rounding less per
 // element, 2^y (A - B log2 s + B y) / s; y is held at -200 as in row_softmax.cuh.
 template <typename T, int TPR>
-__global__ void __launch_bounds__(LP_THREADS, 4) logprobs_backward_kernel(const T* logits, T* dlogits, BackwardArgs a) {
+__global__ void __launch_bounds__(LP_THREADS, 7) logprobs_backward_kernel(const T* logits, T* dlogits, BackwardArgs a) {
   using G = Group<TPR>;
   constexpr int NV = 4;
   if (!chain_begin()) return;
-  __shared__ struct { float g[GRAM_TOP_MAX], z[GRAM_TOP_MAX]; int32_t place[GRAM_TOP_MAX]; } given[G::ROWS];   // the given tokens that take part
-  const int tid = G::tid(), rank = TPR == 32 ? 0 : blockIdx.x % a.slices;
-  const int64_t n = TPR == 32 ? (int64_t)blockIdx.x * G::ROWS + G::row() : blockIdx.x / a.slices;
+  __shared__ struct { float g[GRAM_TOP_MAX], z[GRAM_TOP_MAX]; int32_t place[GRAM_TOP_MAX]; } given[(LP_THREADS / TPR)];   // the given tokens that take part
+  const int slices = TPR == 32 ? 1 : 1 << a.shift, tid = G::tid(), rank = blockIdx.x & (slices - 1);
+  const int64_t n = TPR == 32 ? (int64_t)blockIdx.x * LP_WARPS + G::row() : blockIdx.x >> a.shift;
   if (n >= a.N) return;
   auto& mine = given[G::row()];
-  const Slice<T> s(logits + n * a.ld, a.V, rank, a.slices);
+  const Slice<T> s(logits + n * a.ld, a.V, rank, a.shift);
   T* dz = dlogits + n * a.ld_out;
   const bool vec = same_alignment(s.z, dz);
-  uint4 q[NV];
-  s.template load_chunk<TPR, NV>(0, tid, q);
+  uint4 q[NV], next[NV];
+  s.template load_chunk<TPR, NV, true>(0, tid, q);
   const int edge_place = s.edge(tid);
   const float edge = edge_place >= 0 ? row_load(s.z + edge_place) : ROW_NEG_INF;
   for (int i = tid; i < a.C; i += TPR) {
@@ -302,7 +314,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_backward_kernel(const 
     mine.g[i] = x == ROW_NEG_INF ? 0.f : a.dlogp[n * a.C + i];
   }
   // in place, no slice may be overwritten before all have read the given tokens' logits
-  if (TPR > 32 && a.slices > 1 && a.C > 0) gram_cluster_sync();
+  if (TPR > 32 && slices > 1 && a.C > 0) gram_cluster_sync();
   else G::sync();
   float sum = 0.f;
   for (int i = 0; i < a.C; ++i) sum += mine.g[i];
@@ -317,10 +329,12 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_backward_kernel(const 
   auto one = [&](float x) { return none || x == ROW_NEG_INF ? 0.f : l.is_huge ? dense_huge(x) : dense(x); };
   const int chunks = s.template chunks<TPR, NV>();
   for (int ch = 0; ch < chunks; ++ch) {
-    if (ch > 0 && !none) s.template load_chunk<TPR, NV>(ch, tid, q);
+    if (ch + 1 < chunks && !none) s.template load_chunk<TPR, NV, true>(ch + 1, tid, next);
     if (none) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, [](float) { return 0.f; });
     else if (l.is_huge) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, dense_huge);
     else store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, dense);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) q[i] = next[i];
   }
   if (edge_place >= 0) dz[edge_place] = row_round<T>(one(edge));
   G::sync();                                             // the given places are written again, by one thread each
@@ -344,30 +358,30 @@ struct DistillArgs {
   float* loss;
   const float* weight;
   int64_t ld, ld_out, N;
-  int32_t V, k, slices;
+  int32_t V, k, shift;
   float scale;
   int32_t* status;
 };
 
-// A block's slice stays in registers between the statistics and the gradient where it fits (8 vectors a thread), so the
-// logits are read once; of a longer one the last chunk does, and the others are read again, the latest first.
+// A slice is walked over twice: forwards for the statistics, backwards for the gradient, whose reads find it in L2 (the last
+// chunk is still in registers).  The plan keeps the slices of the blocks that run together well below L2's size.
 template <typename T, int TPR>
-__global__ void __launch_bounds__(LP_THREADS, 4) distill_kernel(const T* logits, T* dlogits, DistillArgs a) {
+__global__ void __launch_bounds__(LP_THREADS, 7) distill_kernel(const T* logits, T* dlogits, DistillArgs a) {
   using G = Group<TPR>;
-  constexpr int NV = 8;
+  constexpr int NV = 4;
   if (!chain_begin()) return;
   __shared__ RowStat part[LP_WARPS][2], of_slice[MAX_SLICES];
   __shared__ float fpart[LP_WARPS];
-  __shared__ struct { float q[GRAM_TOP_MAX], z[GRAM_TOP_MAX]; int32_t place[GRAM_TOP_MAX]; } entries[G::ROWS];
-  const int tid = G::tid(), rank = TPR == 32 ? 0 : blockIdx.x % a.slices;
-  const int64_t n = TPR == 32 ? (int64_t)blockIdx.x * G::ROWS + G::row() : blockIdx.x / a.slices;
+  __shared__ struct { float q[GRAM_TOP_MAX], z[GRAM_TOP_MAX]; int32_t place[GRAM_TOP_MAX]; } entries[(LP_THREADS / TPR)];
+  const int slices = TPR == 32 ? 1 : 1 << a.shift, tid = G::tid(), rank = blockIdx.x & (slices - 1);
+  const int64_t n = TPR == 32 ? (int64_t)blockIdx.x * LP_WARPS + G::row() : blockIdx.x >> a.shift;
   if (n >= a.N) return;
   auto& mine = entries[G::row()];
   const float c = a.scale * kLog2e;
-  const Slice<T> s(logits + n * a.ld, a.V, rank, a.slices);
+  const Slice<T> s(logits + n * a.ld, a.V, rank, a.shift);
   const int chunks = s.template chunks<TPR, NV>();
-  uint4 q[NV];
-  s.template load_chunk<TPR, NV>(0, tid, q);
+  uint4 q[NV], next[NV];
+  s.template load_chunk<TPR, NV, false>(0, tid, q);
   const int edge_place = s.edge(tid);
   const float edge = edge_place >= 0 ? row_load(s.z + edge_place) : ROW_NEG_INF;
   RowStat r = row_empty(), t = row_empty();
@@ -381,17 +395,22 @@ __global__ void __launch_bounds__(LP_THREADS, 4) distill_kernel(const T* logits,
     mine.q[i] = b;
     if (use) row_add(t, b, c);
   }
-  if (TPR > 32 && a.slices > 1) gram_cluster_sync();     // every block of the cluster runs before another writes to it
+  if (TPR > 32 && slices > 1) gram_cluster_sync();       // every block of the cluster runs before another writes to it
   for (int ch = 0; ch < chunks; ++ch) {
-    if (ch > 0) s.template load_chunk<TPR, NV>(ch, tid, q);
-    row_add_vectors<T, NV>(r, q, chunk_top<T, NV>(q), c);
+    if (ch + 1 < chunks) s.template load_chunk<TPR, NV, false>(ch + 1, tid, next);
+    row_add_vectors<T, NV>(r, q, chunk_top<T, 0, NV>(q), c);
+    if (ch + 1 < chunks) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) q[i] = next[i];
+    }
   }
+  if (dlogits && chunks > 1) s.template load_chunk<TPR, NV, true>(chunks - 2, tid, next);
   if (edge_place >= 0) row_add(r, edge, c);
   G::join(r, t, c, part);
-  if (TPR > 32 && a.slices > 1) {
-    if (tid < a.slices) put_stat(&of_slice[rank], tid, r);
+  if (TPR > 32 && slices > 1) {
+    if (tid < slices) put_stat(&of_slice[rank], tid, r);
     gram_cluster_sync();                                 // all have read the teacher's places by now, too
-    r = join_slices(of_slice, a.slices, c);
+    r = join_slices(of_slice, slices, c);
   }
   const float log_s = row_logs<T, TPR>(r, s.z, a.V, c, fpart).log_s;
   float log_t = row_log_sum(t, c);
@@ -402,7 +421,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) distill_kernel(const T* logits,
     log_t = logf(G::sum(sum, fpart));
   }
   // such a row was read again as a whole: in place, no slice may be overwritten before all have done so
-  if (TPR > 32 && a.slices > 1 && row_is_huge(r.m, c)) gram_cluster_sync();
+  if (TPR > 32 && slices > 1 && row_is_huge(r.m, c)) gram_cluster_sync();
   float loss = 0.f;
   for (int i = tid; i < a.k; i += TPR) {
     float qi = 0.f;
@@ -428,10 +447,12 @@ __global__ void __launch_bounds__(LP_THREADS, 4) distill_kernel(const T* logits,
   auto dense_huge = [&](float x) { return w_s * row_ex2(l.huge(x)); };
   auto one = [&](float x) { return l.is_huge ? dense_huge(x) : dense(x); };
   for (int ch = chunks - 1; ch >= 0; --ch) {
-    if (ch < chunks - 1 && !none) s.template load_chunk<TPR, NV>(ch, tid, q);
     if (none) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, [](float) { return 0.f; });
     else if (l.is_huge) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, dense_huge);
     else store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, dense);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) q[i] = next[i];
+    if (ch > 1 && !none) s.template load_chunk<TPR, NV, true>(ch - 2, tid, next);
   }
   if (edge_place >= 0) dz[edge_place] = row_round<T>(none ? 0.f : one(edge));
   G::sync();                                             // the teacher's places are written again, by one thread each
@@ -452,26 +473,27 @@ __global__ void __launch_bounds__(LP_THREADS, 4) distill_kernel(const T* logits,
 
 // ------------------------------ host side -----------------------------------------------------------------------------
 // Rows of up to 4 KB go to warps where there are enough of them to fill the blocks' places; other rows to a block, or to a
-// cluster: as many blocks as hold the row (hold: vectors that a block keeps; 0: it keeps none), and more while the GPU has
-// room for them and each still has a vector a thread.
+// cluster: slices of at most `most_bytes`, and more of them while the GPU has room for their blocks and each thread still has
+// a vector.
 struct RowPlan {
   bool warps;
-  int slices;
+  int shift;                     // 2^shift slices
 };
-RowPlan row_plan(gram_ctx* ctx, int64_t N, int64_t row_bytes, int64_t hold) {
-  RowPlan p{row_bytes <= 4096 && N >= 4 * kNumSMs, 1};
+constexpr int LP_PER_SM = 7;     // blocks of these kernels that an SM holds
+RowPlan row_plan(gram_ctx* ctx, int64_t N, int64_t row_bytes, int64_t most_bytes) {
+  RowPlan p{row_bytes <= 4096 && N >= 4 * kNumSMs, 0};
   if (p.warps) return p;
   const int64_t vectors = row_bytes / 16;
   const int most = gram_cluster_blocks(ctx) < MAX_SLICES ? gram_cluster_blocks(ctx) : MAX_SLICES;
-  while (hold && p.slices < most && ceil_div64(vectors, p.slices) > hold) p.slices *= 2;
-  while (p.slices < most && N * p.slices * 2 <= 4 * kNumSMs && vectors / (2 * p.slices) >= LP_THREADS) p.slices *= 2;
+  while ((1 << p.shift) < most && (row_bytes >> p.shift) > most_bytes) ++p.shift;
+  while ((1 << p.shift) < most && (N << (p.shift + 1)) <= LP_PER_SM * kNumSMs && (vectors >> (p.shift + 1)) >= LP_THREADS) ++p.shift;
   return p;
 }
 template <typename... P, typename... A>
 gram_status launch_rows(gram_ctx* ctx, void (*kern)(P...), const RowPlan& plan, int64_t N, size_t smem, cudaStream_t st, A... args) {
-  const int64_t blocks = plan.warps ? ceil_div64(N, LP_WARPS) : N * plan.slices;
-  if (blocks > INT32_MAX) return gram_set_error(ctx, "%lld rows of %d slices", (long long)N, plan.slices), GRAM_ERR_UNSUPPORTED;
-  if (plan.slices > 8) GRAM_CUDA(ctx, cudaFuncSetAttribute(reinterpret_cast<const void*>(kern), cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+  const int64_t blocks = plan.warps ? ceil_div64(N, LP_WARPS) : N << plan.shift;
+  if (blocks > INT32_MAX) return gram_set_error(ctx, "%lld rows of %d slices", (long long)N, 1 << plan.shift), GRAM_ERR_UNSUPPORTED;
+  if (plan.shift > 3) GRAM_CUDA(ctx, cudaFuncSetAttribute(reinterpret_cast<const void*>(kern), cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks);
   cfg.blockDim = dim3(LP_THREADS);
@@ -480,36 +502,36 @@ gram_status launch_rows(gram_ctx* ctx, void (*kern)(P...), const RowPlan& plan, 
   cudaLaunchAttribute attr[2];
   attr[0] = chain_attribute();
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)plan.slices;
+  attr[1].val.clusterDim.x = 1u << plan.shift;
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = plan.slices > 1 ? 2 : 1;
+  cfg.numAttrs = plan.shift > 0 ? 2 : 1;
   GRAM_CUDA(ctx, cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...));
   return GRAM_OK;
 }
 
 template <typename T>
 gram_status logprobs_typed(gram_ctx* ctx, const T* z, int64_t ld, int64_t N, int32_t V, float scale, const RowAnswers& ask, cudaStream_t st) {
-  const RowPlan plan = row_plan(ctx, N, (int64_t)V * sizeof(T), 0);
+  const RowPlan plan = row_plan(ctx, N, (int64_t)V * sizeof(T), INT64_MAX);
   ProfScope prof(ctx, GRAM_K_OTHER, (double)N * V * sizeof(T), 1, st, "logprobs");
   int32_t* status = gram_status_word(ctx);
-  const size_t smem = plan.slices > 1 ? sizeof(uint64_t) * plan.slices * ask.k : 0;
-  auto run = [&](auto kern) { return launch_rows(ctx, kern, plan, N, smem, st, z, ld, N, V, scale, plan.slices, ask, status); };
+  const size_t smem = plan.shift > 0 ? (sizeof(uint64_t) * ask.k) << plan.shift : 0;
+  auto run = [&](auto kern) { return launch_rows(ctx, kern, plan, N, smem, st, z, ld, N, V, scale, plan.shift, ask, status); };
   if (plan.warps) return ask.k ? run(logprobs_kernel<T, 32, true>) : run(logprobs_kernel<T, 32, false>);
   return ask.k ? run(logprobs_kernel<T, LP_THREADS, true>) : run(logprobs_kernel<T, LP_THREADS, false>);
 }
 template <typename T> gram_status backward_typed(gram_ctx* ctx, const T* z, T* dz, BackwardArgs a, cudaStream_t st) {
-  const RowPlan plan = row_plan(ctx, a.N, (int64_t)a.V * sizeof(T), 0);
+  const RowPlan plan = row_plan(ctx, a.N, (int64_t)a.V * sizeof(T), INT64_MAX);
   ProfScope prof(ctx, GRAM_K_OTHER, 2.0 * a.N * a.V * sizeof(T), 1, st, "logprobs_backward");
-  a.slices = plan.slices;
+  a.shift = plan.shift;
   if (plan.warps) return launch_rows(ctx, logprobs_backward_kernel<T, 32>, plan, a.N, 0, st, z, dz, a);
   return launch_rows(ctx, logprobs_backward_kernel<T, LP_THREADS>, plan, a.N, 0, st, z, dz, a);
 }
 template <typename T> gram_status distill_typed(gram_ctx* ctx, const T* z, T* dz, DistillArgs a, cudaStream_t st) {
-  const RowPlan plan = row_plan(ctx, a.N, (int64_t)a.V * sizeof(T), LP_THREADS * 8);
+  const RowPlan plan = row_plan(ctx, a.N, (int64_t)a.V * sizeof(T), 64 << 10);
   ProfScope prof(ctx, GRAM_K_OTHER, (dz ? 2.0 : 1.0) * a.N * a.V * sizeof(T), 1, st, "distill");
-  a.slices = plan.slices;
+  a.shift = plan.shift;
   if (plan.warps) return launch_rows(ctx, distill_kernel<T, 32>, plan, a.N, 0, st, z, dz, a);
   return launch_rows(ctx, distill_kernel<T, LP_THREADS>, plan, a.N, 0, st, z, dz, a);
 }
@@ -527,7 +549,7 @@ gram_status logprobs_backward_launch(gram_ctx* ctx, const void* logits, int dtyp
                                      const int32_t* targets, int32_t C, const float* stats, const float* entropy, const float* dlogp,
                                      const float* dentropy, void* dlogits, int64_t ld_out, cudaStream_t st) {
   if (N == 0) return GRAM_OK;
-  const BackwardArgs a{targets, stats, entropy, dlogp, dentropy, ld, ld_out, N, V, C, 1, scale, gram_status_word(ctx)};
+  const BackwardArgs a{targets, stats, entropy, dlogp, dentropy, ld, ld_out, N, V, C, 0, scale, gram_status_word(ctx)};
   if (dtype == GRAM_F32) return backward_typed(ctx, (const float*)logits, (float*)dlogits, a, st);
   return backward_typed(ctx, (const bf16*)logits, (bf16*)dlogits, a, st);
 }
@@ -536,7 +558,7 @@ gram_status distill_launch(gram_ctx* ctx, const void* logits, int dtype, int64_t
                            const int32_t* teacher_ids, const float* teacher_logits, int32_t k, float* loss, const float* weight,
                            void* dlogits, int64_t ld_out, cudaStream_t st) {
   if (N == 0) return GRAM_OK;
-  const DistillArgs a{teacher_ids, teacher_logits, loss, weight, ld, ld_out, N, V, k, 1, scale, gram_status_word(ctx)};
+  const DistillArgs a{teacher_ids, teacher_logits, loss, weight, ld, ld_out, N, V, k, 0, scale, gram_status_word(ctx)};
   if (dtype == GRAM_F32) return distill_typed(ctx, (const float*)logits, (float*)dlogits, a, st);
   return distill_typed(ctx, (const bf16*)logits, (bf16*)dlogits, a, st);
 }

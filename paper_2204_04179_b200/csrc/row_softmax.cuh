@@ -86,19 +86,16 @@ template <typename T> __device__ __forceinline__ T row_round(float v);
 template <> __device__ __forceinline__ float row_round<float>(float v) { return v; }
 template <> __device__ __forceinline__ bf16 row_round<bf16>(float v) { return __float2bfloat16_rn(v); }
 
-constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32;
-
-// TPR threads a row: a warp, or the block.  All threads of a group call these together.
+// A row belongs to TPR threads: a warp, or a block of that many.  All threads of a group call these together.
 template <int TPR> struct Group {
-  static constexpr int ROWS = LP_THREADS / TPR;
-  static_assert(TPR == 32 || TPR == LP_THREADS, "a warp or the block");
+  static constexpr int WARPS = TPR / 32;
   static __device__ __forceinline__ int tid() { return threadIdx.x % TPR; }
   static __device__ __forceinline__ int row() { return threadIdx.x / TPR; }
   static __device__ __forceinline__ void sync() {
     if constexpr (TPR == 32) __syncwarp();
     else __syncthreads();
   }
-  static __device__ __forceinline__ int count(bool p) {        // also a barrier
+  static __device__ __forceinline__ int count(bool p) {        // of a block: also a barrier
     if constexpr (TPR == 32) return __popc(__ballot_sync(0xffffffffu, p));
     else return __syncthreads_count(p);
   }
@@ -110,7 +107,20 @@ template <int TPR> struct Group {
       __syncthreads();
       v = 0;
 #pragma unroll
-      for (int w = 0; w < LP_WARPS; ++w) v += part[w];
+      for (int w = 0; w < WARPS; ++w) v += part[w];
+    }
+    return v;
+  }
+  static __device__ __forceinline__ float sum(float v, float* part) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if constexpr (TPR > 32) {
+      __syncthreads();
+      if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+      __syncthreads();
+      v = 0.f;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) v += part[w];
     }
     return v;
   }
@@ -121,7 +131,7 @@ template <int TPR> struct Group {
       __syncthreads();
       if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = r;
       __syncthreads();
-      r = row_join_lanes<LP_WARPS>(part[threadIdx.x & (LP_WARPS - 1)], c);
+      r = row_join_lanes<WARPS>(part[threadIdx.x & (WARPS - 1)], c);
     }
     return r;
   }
@@ -133,22 +143,9 @@ template <int TPR> struct Group {
       __syncthreads();
       if ((threadIdx.x & 31) == 0) { part[threadIdx.x >> 5][0] = r; part[threadIdx.x >> 5][1] = q; }
       __syncthreads();
-      r = row_join_lanes<LP_WARPS>(part[threadIdx.x & (LP_WARPS - 1)][0], c);
-      q = row_join_lanes<LP_WARPS>(part[threadIdx.x & (LP_WARPS - 1)][1], c);
+      r = row_join_lanes<WARPS>(part[threadIdx.x & (WARPS - 1)][0], c);
+      q = row_join_lanes<WARPS>(part[threadIdx.x & (WARPS - 1)][1], c);
     }
-  }
-  static __device__ __forceinline__ float sum(float v, float* part) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if constexpr (TPR > 32) {
-      __syncthreads();
-      if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-      __syncthreads();
-      v = 0.f;
-#pragma unroll
-      for (int w = 0; w < LP_WARPS; ++w) v += part[w];
-    }
-    return v;
   }
 };
 

@@ -1,22 +1,23 @@
 // The best k places of a row or a slice of one.
 //
 // Candidates are kept as keys (row_key: larger logit first, then lower place) in shared memory, in no order.  The first
-// chunk sets a bar: the k-th largest of the threads' maxima, or a little below; k entries at least reach it.  An entry below
-// the bar is not among the best k, and once k entries have reached it neither is a later one that equals it, since slices
-// are read in ascending order.  So of a chunk only a few entries are looked at twice.  Where more than half the list fills,
-// it is cut to its best k, the last of which sets the new bar; a chunk that would overflow the list (equal logits, ascending
-// rows) gives its own best k, found by bisection over the keys.
+// chunk sets a bar that at least k of its entries reach: in each warp the value that k / warps of its lanes' maxima (two a
+// lane) reach, or a little less, and the smallest of the warps'.  An entry below the bar is not among the best k, and once k
+// entries have reached it neither is a later one that equals it, since slices are read in ascending order.  So of a chunk
+// only a few entries are looked at twice.  Where more than half the list fills, it is cut to its best k, the last of which
+// sets the new bar; a chunk that would overflow the list (equal logits, ascending rows) gives its own best k, found by
+// bisection over the keys.
 #pragma once
 #include "row_softmax.cuh"
 
 template <int TPR> struct TopList {
   static constexpr int CAP = TPR == 32 ? 384 : 1024;
-  static_assert(CAP >= 4 * GRAM_TOP_MAX || TPR == 32 && CAP >= 3 * GRAM_TOP_MAX, "a list past its half holds more than k");
+  static_assert(CAP >= 3 * GRAM_TOP_MAX, "half a list holds k, and a cut one k more");
   uint64_t keys[CAP];
   int added[3];                  // entries of a chunk; three in turn, so that one is cleared while none looks at it
   int slow;
-  int part[LP_WARPS];
-  uint32_t lowest[LP_WARPS], highest[LP_WARPS];
+  int part[Group<TPR>::WARPS];
+  uint32_t low[Group<TPR>::WARPS];
 };
 
 template <typename T, int TPR, int NV> struct TopChunk {
@@ -50,39 +51,52 @@ template <typename F> __device__ __forceinline__ uint64_t kth_key(int k, F at_le
   }
   return lo;
 }
-// the first `have` keys of the list (k at least) cut to the best k; returns a bar that only better logits than theirs reach
-template <int TPR> __device__ __noinline__ float top_cut(TopList<TPR>& l, int have, int k) {
-  using G = Group<TPR>;
-  constexpr int PER = TopList<TPR>::CAP / TPR;
-  const int tid = G::tid();
-  uint64_t key[PER], last = ~0ull;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) key[i] = tid + i * TPR < have ? l.keys[tid + i * TPR] : 0;
+// `have` keys (k at least) cut to the best k by a warp; returns a bar that only better logits than theirs reach.  The keys are read
+// again in each step of the bisection (shared memory, or L1): no array of them lives in registers.
+__device__ __forceinline__ float warp_cut(uint64_t* keys, int have, int k) {
+  const int lane = threadIdx.x & 31;
+  uint32_t low = 0xffffffffu, high = 0u;
+  for (int i = lane; i < have; i += 32) {
+    const uint32_t o = (uint32_t)(keys[i] >> 32);
+    low = min(low, o);
+    high = max(high, o);
+  }
+  low = __reduce_min_sync(0xffffffffu, low);
+  high = __reduce_max_sync(0xffffffffu, high);
   const uint64_t kth = kth_key(k, [&](uint64_t t) {
     int c = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) c += key[i] >= t;
-    return G::sum(c, l.part);
-  });
-  if (tid == 0) l.slow = 0;
-  G::sync();
-#pragma unroll
-  for (int i = 0; i < PER; ++i)
-    if (key[i] >= kth) {
-      l.keys[atomicAdd(&l.slow, 1)] = key[i];
-      last = min(last, key[i]);
+#pragma unroll 4
+    for (int i = lane; i < have; i += 32) c += keys[i] >= t;
+    return (int)__reduce_add_sync(0xffffffffu, c);
+  }, (uint64_t)low << 32, (uint64_t)high << 32 | 0xffffffffu);
+  int at = 0;
+  low = 0xffffffffu;
+  for (int i = 0; i < have; i += 32) {                   // what is kept moves down, behind what has been read
+    const uint64_t key = i + lane < have ? keys[i + lane] : 0;
+    const bool keep = key >= kth;                        // kth > 0
+    const uint32_t who = __ballot_sync(0xffffffffu, keep);
+    if (keep) {
+      keys[at + __popc(who & ((1u << lane) - 1u))] = key;
+      low = min(low, (uint32_t)(key >> 32));
     }
-  uint32_t low = __reduce_min_sync(0xffffffffu, (uint32_t)(last >> 32));
-  if constexpr (TPR > 32) {
-    if ((threadIdx.x & 31) == 0) l.lowest[threadIdx.x >> 5] = low;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < LP_WARPS; ++w) low = min(low, l.lowest[w]);
+    at += __popc(who);
+    __syncwarp();
+  }
+  return row_order_logit(__reduce_min_sync(0xffffffffu, low) + 1u);
+}
+// the same of a group's list, by its first warp; the list is complete behind a barrier, and so is what this leaves
+template <int TPR> __device__ __noinline__ float top_cut(TopList<TPR>& l, int have, int k) {
+  using G = Group<TPR>;
+  if (G::tid() < 32) {
+    const float bar = warp_cut(l.keys, have, k);
+    if (G::tid() == 0) l.low[0] = __float_as_uint(bar);
   }
   G::sync();
-  return row_order_logit(low + 1u);
+  const float bar = __uint_as_float(l.low[0]);
+  G::sync();
+  return bar;
 }
-// the best k of a chunk's entries of at least `bar` (more than k) behind the list's first `have`
+// the best k of a chunk's entries of at least `bar` (k at least) behind the list's first `have`
 template <typename T, int TPR, int NV>
 __device__ __noinline__ void top_take_best(TopList<TPR>& l, const TopChunk<T, TPR, NV>& ch, int have, int k, float bar) {
   using G = Group<TPR>;
@@ -99,30 +113,32 @@ __device__ __noinline__ void top_take_best(TopList<TPR>& l, const TopChunk<T, TP
   G::sync();
 }
 
-// the first chunk's bar, from the threads' largest entries
-template <int TPR> __device__ __forceinline__ float top_first_bar(TopList<TPR>& l, float top, int k) {
+// the first chunk's bar, from two of each thread's entries, the largest of either half
+template <int TPR> __device__ __forceinline__ float top_first_bar(TopList<TPR>& l, float a, float b, int k) {
   using G = Group<TPR>;
-  const bool some = top > ROW_NEG_INF;
-  const uint32_t o = row_order(top);
-  uint32_t lo = __reduce_min_sync(0xffffffffu, some ? o : 0xffffffffu), hi = __reduce_max_sync(0xffffffffu, some ? o : 0u);
-  if constexpr (TPR > 32) {
-    if ((threadIdx.x & 31) == 0) { l.lowest[threadIdx.x >> 5] = lo; l.highest[threadIdx.x >> 5] = hi; }
-  }
-  if (G::count(some) < k) return -FLT_MAX;              // a barrier, for the two arrays too
-  if constexpr (TPR > 32) {
-#pragma unroll
-    for (int w = 0; w < LP_WARPS; ++w) { lo = min(lo, l.lowest[w]); hi = max(hi, l.highest[w]); }
-  }
-  for (int step = 0; lo < hi && step < 12; ++step) {
-    const uint32_t mid = hi - (hi - lo) / 2;
-    const int n = G::count(some && o >= mid);
-    if (n < k) hi = mid - 1;
-    else {
-      lo = mid;
-      if (n <= k + k / 8) break;
+  const int want = (k + G::WARPS - 1) / G::WARPS;        // of each warp's 64
+  const uint32_t oa = a > ROW_NEG_INF ? row_order(a) : 0u, ob = b > ROW_NEG_INF ? row_order(b) : 0u;
+  uint32_t lo = 0u;
+  if (__popc(__ballot_sync(0xffffffffu, oa != 0u)) + __popc(__ballot_sync(0xffffffffu, ob != 0u)) >= want) {
+    lo = __reduce_min_sync(0xffffffffu, min(oa ? oa : ~0u, ob ? ob : ~0u));
+    uint32_t hi = __reduce_max_sync(0xffffffffu, max(oa, ob));
+    for (int step = 0; lo < hi && step < 12; ++step) {
+      const uint32_t mid = hi - (hi - lo) / 2;
+      const int n = __popc(__ballot_sync(0xffffffffu, oa >= mid)) + __popc(__ballot_sync(0xffffffffu, ob >= mid));
+      if (n < want) hi = mid - 1;
+      else {
+        lo = mid;
+        if (n <= want + want / 8) break;
+      }
     }
   }
-  return row_order_logit(lo);
+  if constexpr (TPR > 32) {
+    if ((threadIdx.x & 31) == 0) l.low[threadIdx.x >> 5] = lo;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < G::WARPS; ++w) lo = min(lo, l.low[w]);
+  }
+  return lo ? row_order_logit(lo) : -FLT_MAX;
 }
 
 struct TopState {
@@ -130,14 +146,14 @@ struct TopState {
   float bar;
   bool reached;                  // k entries have reached the bar: later ones must pass it
 };
-// one chunk's entries into the list; top: the thread's largest
+// one chunk's entries into the list; a, b: the largest of either half of the thread's
 template <typename T, int TPR, int NV>
-__device__ __forceinline__ void top_chunk(TopList<TPR>& l, TopState& st, const TopChunk<T, TPR, NV>& ch, float top, int k, int number, bool last) {
+__device__ __forceinline__ void top_chunk(TopList<TPR>& l, TopState& st, const TopChunk<T, TPR, NV>& ch, float a, float b, int k, int number, bool last) {
   using G = Group<TPR>;
   constexpr int CAP = TopList<TPR>::CAP;
-  if (number == 0) st.bar = top_first_bar(l, top, k);
+  if (number == 0) st.bar = top_first_bar(l, a, b, k);
   int* added = &l.added[number % 3];
-  if (top >= st.bar)
+  if (fmaxf(a, b) >= st.bar)
     ch.each([&](float x, int p) {
       if (x >= st.bar) {
         const int at = st.have + atomicAdd(added, 1);
@@ -150,10 +166,13 @@ __device__ __forceinline__ void top_chunk(TopList<TPR>& l, TopState& st, const T
   if (st.have + n > CAP) {
     if (st.have > k) (void)top_cut(l, st.have, k);
     st.have = min(st.have, k);
-    if (n > k) top_take_best(l, ch, st.have, k, st.bar);
-    else top_take_best(l, ch, st.have, n, st.bar);
+    top_take_best(l, ch, st.have, min(n, k), st.bar);
     st.have += min(n, k);
-    if (st.have >= k) { st.bar = top_cut(l, st.have, k); st.have = k; st.reached = true; }
+    if (st.have >= k) {
+      st.bar = top_cut(l, st.have, k);
+      st.have = k;
+      st.reached = true;
+    }
     return;
   }
   st.have += n;

@@ -24,6 +24,7 @@ constexpr int SC_STAGES = 6, SC_EPI_WARPS = 8, SC_THREADS = 64 + 32 * SC_EPI_WAR
 constexpr int SC_BIAS_BYTES = SC_EPI_WARPS * 128 * 4;   // a warp's 128 columns
 constexpr int SC_SMEM = SC_STAGES * SC_STAGE + SC_BIAS_BYTES + 1024 + 256;
 constexpr int SC_LIST_MAX = 256;                        // most entries of a thread's list
+constexpr int SJ_THREADS = 256, SJ_WARPS = SJ_THREADS / 32;
 constexpr int SC_PAIR_THREADS = 2 * SC_ROWS;            // epilogue threads of a pair, one for each user and half
 
 struct ScoreArgs {
@@ -60,40 +61,7 @@ struct ScoreRun {
   __device__ __forceinline__ bool leaves() const { return (end - 1) / units != tm; }     // the run goes on with another row tile
 };
 
-// The list of lane `of` of this warp cut to its best k by the whole warp; returns (in every lane) the bar that better logits reach.
-__device__ __noinline__ float score_cut(uint64_t* list, int have, int k) {
-  constexpr int PER = SC_LIST_MAX / 32;
-  const int lane = threadIdx.x & 31;
-  uint64_t key[PER];
-  uint32_t low = 0xffffffffu, high = 0u;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    key[i] = i * 32 + lane < have ? list[i * 32 + lane] : 0;
-    if (key[i]) { low = min(low, (uint32_t)(key[i] >> 32)); high = max(high, (uint32_t)(key[i] >> 32)); }
-  }
-  low = __reduce_min_sync(0xffffffffu, low);
-  high = __reduce_max_sync(0xffffffffu, high);
-  const uint64_t kth = kth_key(k, [&](uint64_t t) {
-    int c = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) c += key[i] >= t;
-    return (int)__reduce_add_sync(0xffffffffu, c);
-  }, (uint64_t)low << 32, (uint64_t)high << 32 | 0xffffffffu);
-  int at = 0;
-  low = 0xffffffffu;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const bool keep = key[i] >= kth && key[i] != 0;
-    const uint32_t who = __ballot_sync(0xffffffffu, keep);
-    if (keep) {
-      list[at + __popc(who & ((1u << lane) - 1u))] = key[i];
-      low = min(low, (uint32_t)(key[i] >> 32));
-    }
-    at += __popc(who);
-  }
-  __syncwarp();
-  return row_order_logit(__reduce_min_sync(0xffffffffu, low) + 1u);
-}
+__device__ __noinline__ float score_cut(uint64_t* list, int have, int k) { return warp_cut(list, have, k); }
 
 // x[32]: a block of 32 columns of this thread's row, with the bias (b: the warp's 32 values in shared memory; null: none)
 __device__ __forceinline__ void score_block(uint32_t taddr, const float* b, float (&x)[32]) {
@@ -397,14 +365,14 @@ __device__ __forceinline__ float score_dot(const bf16* u, const bf16* w, int d) 
 }
 
 // One block a user: joins the statistics of the runs that crossed its row tile, and their lists.
-__global__ void __launch_bounds__(LP_THREADS) score_join_kernel(const ScoreArgs a, const bf16* users, int64_t ld_u, const bf16* items, int64_t ld_i,
+__global__ void __launch_bounds__(SJ_THREADS) score_join_kernel(const ScoreArgs a, const bf16* users, int64_t ld_u, const bf16* items, int64_t ld_i,
                                                                 int32_t d, float scale, RowAnswers ask) {
-  using G = Group<LP_THREADS>;
+  using G = Group<SJ_THREADS>;
   if (!chain_begin()) return;
-  __shared__ TopList<LP_THREADS> list;
-  __shared__ RowStat part[LP_WARPS];
-  __shared__ float fpart[LP_WARPS];
-  __shared__ int have_of[LP_THREADS];
+  __shared__ TopList<SJ_THREADS> list;
+  __shared__ RowStat part[SJ_WARPS];
+  __shared__ float fpart[SJ_WARPS];
+  __shared__ int have_of[SJ_THREADS];
   const int64_t n = blockIdx.x;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int tm = (int)(n / SC_ROWS), row = (int)(n % SC_ROWS);
@@ -424,7 +392,7 @@ __global__ void __launch_bounds__(LP_THREADS) score_join_kernel(const ScoreArgs 
   float log_s = row_log_sum(r, a.c), entropy = row_entropy(r);
   if (row_is_huge(r.m, a.c)) {                          // summed again, relative to m itself
     float s = 0.f, t = 0.f;
-    for (int v = warp; v < a.V; v += LP_WARPS) {
+    for (int v = warp; v < a.V; v += SJ_WARPS) {
       const float z = score_dot(users + n * ld_u, items + (int64_t)v * ld_i, d) + (a.bias ? a.bias[v] : 0.f);
       const float y = (z - r.m) * a.c, e = row_ex2(y);
       s += e;
@@ -439,7 +407,7 @@ __global__ void __launch_bounds__(LP_THREADS) score_join_kernel(const ScoreArgs 
     if (ask.stats) { ask.stats[2 * n] = r.m; ask.stats[2 * n + 1] = log_s; }
     if (ask.entropy) ask.entropy[n] = entropy;
   }
-  for (int i = warp; i < ask.C; i += LP_WARPS) {
+  for (int i = warp; i < ask.C; i += SJ_WARPS) {
     const int32_t t = ask.targets[n * ask.C + i];
     float lp = 0.f;
     if (t >= 0 && t < a.V) {
@@ -455,7 +423,7 @@ __global__ void __launch_bounds__(LP_THREADS) score_join_kernel(const ScoreArgs 
   const int k = ask.k;
   // f(key) for each key of this thread's share: a warp takes a list at a time
   auto each = [&](auto f) {
-    for (int i = warp; i < parts; i += LP_WARPS) {
+    for (int i = warp; i < parts; i += SJ_WARPS) {
       const int p = p0 + i / 2;
       const int64_t at = (int64_t)(p * 2 + (i & 1)) * SC_ROWS + row;
       const uint64_t* l = is_early(p) ? a.early + at * k : a.lists + at * a.cap;
@@ -464,13 +432,13 @@ __global__ void __launch_bounds__(LP_THREADS) score_join_kernel(const ScoreArgs 
   };
   const int all = G::sum(have, list.part);              // also the barrier behind have_of
   uint64_t least = 1;
-  if (all > TopList<LP_THREADS>::CAP) {
+  if (all > TopList<SJ_THREADS>::CAP) {
     uint64_t best = 0;
     each([&](uint64_t key) { best = max(best, key); });
     if (G::count(best != 0) >= k) least = kth_key(k, [&](uint64_t t) { return G::count(best >= t); });
     int c = 0;
     each([&](uint64_t key) { c += key >= least; });
-    if (G::sum(c, list.part) > TopList<LP_THREADS>::CAP)          // many equal or clustered logits: the k-th key itself
+    if (G::sum(c, list.part) > TopList<SJ_THREADS>::CAP)          // many equal or clustered logits: the k-th key itself
       least = kth_key(k, [&](uint64_t t) {
         int m = 0;
         each([&](uint64_t key) { m += key >= t; });
@@ -490,7 +458,7 @@ __global__ void __launch_bounds__(LP_THREADS) score_join_kernel(const ScoreArgs 
     have = k;
   }
   const int64_t o = n * k;
-  for (int i = tid; i < have; i += LP_THREADS) {
+  for (int i = tid; i < have; i += SJ_THREADS) {
     const uint64_t key = list.keys[i];
     int above = 0;
     for (int j = 0; j < have; ++j) above += list.keys[j] > key;
@@ -499,7 +467,7 @@ __global__ void __launch_bounds__(LP_THREADS) score_join_kernel(const ScoreArgs 
       ask.top_logp[o + above] = row_logp(row_key_logit(key), r.m, log_s, scale);
     }
   }
-  for (int i = have + tid; i < k; i += LP_THREADS) {
+  for (int i = have + tid; i < k; i += SJ_THREADS) {
     ask.top_ids[o + i] = -1;
     ask.top_logp[o + i] = ROW_NEG_INF;
   }
@@ -580,7 +548,7 @@ gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_u
     if (ask.k) { part.top_logp += n * ask.k; part.top_ids += n * ask.k; }
     const int used = ceil_div(a.total, a.per_run);
     GRAM_CUDA(ctx, ask.k ? launch_score<true>(map_u, map_i, a, used, st) : launch_score<false>(map_u, map_i, a, used, st));
-    launch_chain(score_join_kernel, dim3((unsigned)now), LP_THREADS, 0, st, a, u, ld_users, (const bf16*)items, ld_items, d, scale, part);
+    launch_chain(score_join_kernel, dim3((unsigned)now), SJ_THREADS, 0, st, a, u, ld_users, (const bf16*)items, ld_items, d, scale, part);
     GRAM_LAUNCH_CHECK(ctx);
   }
   return GRAM_OK;
