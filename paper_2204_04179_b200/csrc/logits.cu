@@ -37,9 +37,9 @@ template <typename T> struct Slice {
     return last && tid < 16 && tail + tid - 8 < V ? tail + tid - 8 : -1;
   }
   __device__ __forceinline__ int place(int v) const { return head + v * N; }
+  __device__ __forceinline__ const uint4* vectors() const { return reinterpret_cast<const uint4*>(z + head); }
   template <bool LAST> __device__ __forceinline__ uint4 load(int v) const {        // LAST: nobody reads it again
-    const uint4* p = reinterpret_cast<const uint4*>(z + head) + v;
-    return LAST ? __ldcs(p) : *p;
+    return LAST ? __ldcs(vectors() + v) : vectors()[v];
   }
   __device__ __forceinline__ bool has(int p) const {
     if (p < head) return first;
@@ -116,67 +116,64 @@ template <typename T, int TPR> __device__ __forceinline__ RowLogs row_logs(const
 
 // ------------------------------ log probabilities ---------------------------------------------------------------------
 template <typename T, int TPR, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS, 7) logprobs_kernel(const T* logits, int64_t ld, int64_t N, int32_t V, float scale, int32_t shift,
+__global__ void __launch_bounds__(LP_THREADS, TOP ? 6 : 7) logprobs_kernel(const T* logits, int64_t ld, int64_t N, int32_t V, float scale, int32_t shift,
                                                                  RowAnswers ask, int32_t* status) {
   using G = Group<TPR>;
   constexpr int NV = 4;
   if (!chain_begin()) return;
   __shared__ RowStat part[LP_WARPS], of_slice[MAX_SLICES];
   __shared__ float fpart[LP_WARPS];
-  __shared__ TopList<TPR> lists[TOP ? (LP_THREADS / TPR) : 1];
+  __shared__ uint64_t lists[TOP ? LP_WARPS * TOP_CAP : 1];
+  __shared__ uint32_t low[LP_WARPS][2];
+  __shared__ int counts[LP_WARPS];
   extern __shared__ uint64_t merged[];                  // [slices, k], sorted, in the first block of a cluster
   const int slices = TPR == 32 ? 1 : 1 << shift, tid = G::tid(), rank = blockIdx.x & (slices - 1);
   const int64_t n = TPR == 32 ? (int64_t)blockIdx.x * LP_WARPS + G::row() : blockIdx.x >> shift;
   if (TPR > 32 && slices > 1) gram_cluster_sync();      // every block of the cluster runs before another writes to it
   if (n >= N) return;                                   // whole warps, in the form that has no barrier over the block
-  TopList<TPR>& list = lists[TOP ? G::row() : 0];
+  uint64_t* warp_list = lists + (TOP ? (threadIdx.x >> 5) * TOP_CAP : 0);
+  uint64_t* list = TPR == 32 ? warp_list : lists;      // of the row
   const float c = scale * kLog2e;
   const Slice<T> s(logits + n * ld, V, rank, shift);
   const int chunks = s.template chunks<TPR, NV>();
   const int edge_place = s.edge(tid);
   const float edge = edge_place >= 0 ? row_load(s.z + edge_place) : ROW_NEG_INF;
-  RowStat r = row_empty();
-  TopState st{0, 0.f, false};
-  if constexpr (TOP) {
-    if (tid == 0) list.added[0] = 0;
-    G::sync();
-  }
+  RowSums sums;
+  TopState st{0, 0.f};
   uint4 q[NV], next[NV];
   s.template load_chunk<TPR, NV, true>(0, tid, q);
+#pragma unroll(TOP ? 1 : 2)
   for (int ch = 0; ch < chunks; ++ch) {
     if (ch + 1 < chunks) s.template load_chunk<TPR, NV, true>(ch + 1, tid, next);
     float a = chunk_top<T, 0, NV / 2>(q), b = chunk_top<T, NV / 2, NV>(q);
-    row_add_vectors<T, NV>(r, q, fmaxf(a, b), c);
+    row_add_vectors<T, NV>(sums, q, fmaxf(a, b), c);
     const bool on_edge = edge_place >= 0 && (tid < 8 ? ch == 0 : ch == chunks - 1);
     if (on_edge) {
-      row_add(r, edge, c);
+      sums.add(edge, c);
       a = fmaxf(a, edge);
     }
-    if constexpr (TOP)
-      top_chunk(list, st, TopChunk<T, TPR, NV>{q, s.place(s.v0 + ch * (TPR * NV) + tid), on_edge ? edge : ROW_NEG_INF, edge_place}, a, b, ask.k, ch,
-                ch == chunks - 1);
-    if (ch + 1 < chunks) {
+    if constexpr (TOP) {
+      if (ch == 0) st.bar = top_first_bar<TPR>(a, b, ask.k, low);
+      const int v = s.v0 + ch * (TPR * NV) + tid;
+      top_chunk<T, NV>(warp_list, st, TopChunk<T>{s.z, s.vectors() + v, s.place(v), s.v1 - v, TPR, NV, edge_place}, q, fmaxf(a, b), on_edge, ask.k);
+      if (ch == 0 && st.bar > -FLT_MAX) st.bar = row_order_logit(row_order(st.bar) + 1u);
+    }
 #pragma unroll
-      for (int i = 0; i < NV; ++i) q[i] = next[i];
-    }
+    for (int i = 0; i < NV; ++i) q[i] = next[i];
   }
-  r = G::join(r, c, part);
-  if constexpr (TOP) {
-    if (st.have > ask.k + ask.k / 4 + 16) {
-      (void)top_cut(list, st.have, ask.k);
-      st.have = ask.k;
-    }
-  }
+  RowStat r = G::join(sums.stat(c), c, part);
+  int have = 0;
+  if constexpr (TOP) have = top_gather<T, TPR>(s.z, list, counts, st.have, ask.k);
   if (TPR > 32 && slices > 1) {
     if (tid == 0) put_stat(&of_slice[rank], 0, r);
     if constexpr (TOP) {                                // this slice's best, sorted, to the first block
-      for (int i = tid; i < st.have; i += TPR) {
-        const uint64_t key = list.keys[i];
+      for (int i = tid; i < have; i += TPR) {
+        const uint64_t key = list[i];
         int above = 0;
-        for (int j = 0; j < st.have; ++j) above += list.keys[j] > key;
+        for (int j = 0; j < have; ++j) above += list[j] > key;
         if (above < ask.k) put_key(&merged[rank * ask.k + above], 0, key);
       }
-      for (int i = st.have + tid; i < ask.k; i += TPR) put_key(&merged[rank * ask.k + i], 0, 0);
+      for (int i = have + tid; i < ask.k; i += TPR) put_key(&merged[rank * ask.k + i], 0, 0);
     }
     gram_cluster_sync();
     if (rank != 0) return;
@@ -200,13 +197,13 @@ __global__ void __launch_bounds__(LP_THREADS, 7) logprobs_kernel(const T* logits
       ask.top_logp[o + at] = key ? row_logp(row_key_logit(key), r.m, log_s, scale) : ROW_NEG_INF;
     };
     if (TPR == 32 || slices == 1) {
-      for (int i = tid; i < st.have; i += TPR) {
-        const uint64_t key = list.keys[i];
+      for (int i = tid; i < have; i += TPR) {
+        const uint64_t key = list[i];
         int above = 0;
-        for (int j = 0; j < st.have; ++j) above += list.keys[j] > key;
+        for (int j = 0; j < have; ++j) above += list[j] > key;
         if (above < ask.k) answer(above, key);
       }
-      for (int i = st.have + tid; i < ask.k; i += TPR) answer(i, 0);
+      for (int i = have + tid; i < ask.k; i += TPR) answer(i, 0);
       return;
     }
     int found = 0;
@@ -226,7 +223,7 @@ __global__ void __launch_bounds__(LP_THREADS, 7) logprobs_kernel(const T* logits
       }
       if (at < ask.k) answer(at, key);
     }
-    found = G::sum(found, list.part);
+    found = G::sum(found, counts);
     for (int i = found + tid; i < ask.k; i += TPR) answer(i, 0);
   }
 }
@@ -384,7 +381,7 @@ __global__ void __launch_bounds__(LP_THREADS, 7) distill_kernel(const T* logits,
   s.template load_chunk<TPR, NV, false>(0, tid, q);
   const int edge_place = s.edge(tid);
   const float edge = edge_place >= 0 ? row_load(s.z + edge_place) : ROW_NEG_INF;
-  RowStat r = row_empty(), t = row_empty();
+  RowSums sums, teacher;
   for (int i = tid; i < a.k; i += TPR) {
     int32_t id = a.ids[n * a.k + i];
     if (id < -1 || id >= a.V) { gram_device_fail(a.status, GRAM_ERR_ID_RANGE); id = -1; }
@@ -393,19 +390,20 @@ __global__ void __launch_bounds__(LP_THREADS, 7) distill_kernel(const T* logits,
     mine.place[i] = use ? id : -1;
     mine.z[i] = x;
     mine.q[i] = b;
-    if (use) row_add(t, b, c);
+    if (use) teacher.add(b, c);
   }
   if (TPR > 32 && slices > 1) gram_cluster_sync();       // every block of the cluster runs before another writes to it
   for (int ch = 0; ch < chunks; ++ch) {
     if (ch + 1 < chunks) s.template load_chunk<TPR, NV, false>(ch + 1, tid, next);
-    row_add_vectors<T, NV>(r, q, chunk_top<T, 0, NV>(q), c);
+    row_add_vectors<T, NV>(sums, q, chunk_top<T, 0, NV>(q), c);
     if (ch + 1 < chunks) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) q[i] = next[i];
     }
   }
   if (dlogits && chunks > 1) s.template load_chunk<TPR, NV, true>(chunks - 2, tid, next);
-  if (edge_place >= 0) row_add(r, edge, c);
+  if (edge_place >= 0) sums.add(edge, c);
+  RowStat r = sums.stat(c), t = teacher.stat(c);
   G::join(r, t, c, part);
   if (TPR > 32 && slices > 1) {
     if (tid < slices) put_stat(&of_slice[rank], tid, r);

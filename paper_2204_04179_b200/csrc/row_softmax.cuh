@@ -14,7 +14,7 @@
 #include "gram_internal.h"
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-#define ROW_NEG_INF __int_as_float(0xff800000)
+#define ROW_NEG_INF (-__builtin_inff())
 
 struct RowStat {
   float m, s, t;
@@ -35,12 +35,31 @@ __device__ __forceinline__ void row_raise(RowStat& r, float m, float c) {
   r.s *= f;
   r.m = m;
 }
-__device__ __forceinline__ void row_add(RowStat& r, float z, float c) {
-  if (z > r.m) row_raise(r, z, c);
-  const float y = fmaf(z, c, -row_ref(r.m, c)), e = row_ex2(y);
-  r.s += e;
-  r.t = fmaf(e, fmaxf(y, -200.f), r.t);
-}
+// A thread's own sums while it reads.  Their reference lags behind m: it is raised when an entry lies 2^24 above it, so that
+// most chunks leave it alone.
+struct RowSums {
+  float m, ref, s, t;
+  __device__ __forceinline__ RowSums() : m(ROW_NEG_INF), ref(-8388608.f), s(0.f), t(0.f) {}
+  __device__ __forceinline__ void see(float top, float c) {            // before entries of at most `top` are added
+    m = fmaxf(m, top);
+    if (fmaf(top, c, -ref) > 24.f) {
+      const float up = row_ref(top, c), d = fmaxf(ref - up, -200.f), f = row_ex2(d);
+      t = f * fmaf(s, d, t);
+      s *= f;
+      ref = up;
+    }
+  }
+  __device__ __forceinline__ void add(float z, float c) {
+    see(z, c);
+    const float y = fmaf(z, c, -ref), e = row_ex2(y);
+    s += e;
+    t = fmaf(e, fmaxf(y, -200.f), t);
+  }
+  __device__ __forceinline__ RowStat stat(float c) const {
+    const float d = fmaxf(ref - row_ref(m, c), -200.f), f = row_ex2(d);
+    return RowStat{m, s * f, f * fmaf(s, d, t)};
+  }
+};
 // the statistics of L neighbouring lanes, in all of them
 template <int L> __device__ __forceinline__ RowStat row_join_lanes(RowStat r, float c) {
   float m = r.m;
@@ -183,24 +202,23 @@ template <> struct RowVec<bf16> {
   }
 };
 
-// The statistics of NV vectors' worth of logits added to r, whose m is at least their maximum afterwards.
+// NV vectors' worth of logits, of at most `top`
 template <typename T, int NV>
-__device__ __forceinline__ void row_add_vectors(RowStat& r, const uint4 (&q)[NV], float top, float c) {
-  if (top > r.m) row_raise(r, top, c);
-  const float ref = -row_ref(r.m, c);
-  float s[2] = {}, t[2] = {};
+__device__ __forceinline__ void row_add_vectors(RowSums& r, const uint4 (&q)[NV], float top, float c) {
+  r.see(top, c);
+  float s1 = 0.f, t1 = 0.f;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
 #pragma unroll
     for (int j = 0; j < RowVec<T>::N / 2; ++j) {
       const float2 x = RowVec<T>::pair(q[i], j);
-      const float y0 = fmaf(x.x, c, ref), y1 = fmaf(x.y, c, ref), e0 = row_ex2(y0), e1 = row_ex2(y1);
-      s[0] += e0;
-      s[1] += e1;
-      t[0] = fmaf(e0, fmaxf(y0, -200.f), t[0]);
-      t[1] = fmaf(e1, fmaxf(y1, -200.f), t[1]);
+      const float y0 = fmaf(x.x, c, -r.ref), y1 = fmaf(x.y, c, -r.ref), e0 = row_ex2(y0), e1 = row_ex2(y1);
+      r.s += e0;
+      s1 += e1;
+      r.t = fmaf(e0, fmaxf(y0, -200.f), r.t);
+      t1 = fmaf(e1, fmaxf(y1, -200.f), t1);
     }
   }
-  r.s += s[0] + s[1];
-  r.t += t[0] + t[1];
+  r.s += s1;
+  r.t += t1;
 }

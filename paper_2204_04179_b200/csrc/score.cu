@@ -24,7 +24,7 @@ constexpr int SC_STAGES = 6, SC_EPI_WARPS = 8, SC_THREADS = 64 + 32 * SC_EPI_WAR
 constexpr int SC_BIAS_BYTES = SC_EPI_WARPS * 128 * 4;   // a warp's 128 columns
 constexpr int SC_SMEM = SC_STAGES * SC_STAGE + SC_BIAS_BYTES + 1024 + 256;
 constexpr int SC_LIST_MAX = 256;                        // most entries of a thread's list
-constexpr int SJ_THREADS = 256, SJ_WARPS = SJ_THREADS / 32;
+constexpr int SJ_LIST = 1024, SJ_THREADS = 256, SJ_WARPS = SJ_THREADS / 32;
 constexpr int SC_PAIR_THREADS = 2 * SC_ROWS;            // epilogue threads of a pair, one for each user and half
 
 struct ScoreArgs {
@@ -84,18 +84,19 @@ __device__ __forceinline__ float score_top(const float (&x)[32]) {
   for (int j = 0; j < 8; ++j) t[j] = fmaxf(fmaxf(x[j], x[j + 8]), fmaxf(x[j + 16], x[j + 24]));
   return fmaxf(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])), fmaxf(fmaxf(t[4], t[5]), fmaxf(t[6], t[7])));
 }
-__device__ __forceinline__ void score_add(RowStat& r, const float (&x)[32], float top, float c) {
-  if (top > r.m) row_raise(r, top, c);
-  const float ref = -row_ref(r.m, c);
-  float s[2] = {}, t[2] = {};
+__device__ __forceinline__ void score_add(RowSums& r, const float (&x)[32], float top, float c) {
+  r.see(top, c);
+  float s1 = 0.f, t1 = 0.f;
 #pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    const float y = fmaf(x[j], c, ref), e = row_ex2(y);
-    s[j & 1] += e;
-    t[j & 1] = fmaf(e, fmaxf(y, -200.f), t[j & 1]);
+  for (int j = 0; j < 32; j += 2) {
+    const float y0 = fmaf(x[j], c, -r.ref), y1 = fmaf(x[j + 1], c, -r.ref), e0 = row_ex2(y0), e1 = row_ex2(y1);
+    r.s += e0;
+    s1 += e1;
+    r.t = fmaf(e0, fmaxf(y0, -200.f), r.t);
+    t1 = fmaf(e1, fmaxf(y1, -200.f), t1);
   }
-  r.s += s[0] + s[1];
-  r.t += t[0] + t[1];
+  r.s += s1;
+  r.t += t1;
 }
 // A first bar for each lane's row from its columns of the first tile: a value that k of them reach, and few more.
 __device__ __forceinline__ float score_first_bar(uint32_t taddr, const float* b, int blocks, int k) {
@@ -241,7 +242,7 @@ __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_const
     uint64_t* warp_lists = a.lists + ((int64_t)(pair * 2 + half) * SC_ROWS + (row - lane)) * a.cap;
     uint64_t* list = warp_lists + (int64_t)lane * a.cap;
     const uint32_t lane_addr = tmem_base + ((uint32_t)(q * 32) << 16);
-    RowStat r = row_empty();
+    RowSums sums;
     int have = 0;
     float bar = 0.f;
     bool reached = false;
@@ -267,7 +268,7 @@ __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_const
       if (active) {
         const uint32_t taddr = lane_addr + (uint32_t)(buf * SC_COLS + half * blocks * 32);
         if (run.first) {
-          r = row_empty();
+          sums = RowSums();
           have = 0;
           reached = false;
           if (TOP) {
@@ -279,7 +280,7 @@ __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_const
           float x[32];
           score_block(taddr + b * 32, bias ? bias + b * 32 : nullptr, x);
           const float top = score_top(x);
-          score_add(r, x, top, a.c);
+          score_add(sums, x, top, a.c);
           if constexpr (TOP) {
             if (__any_sync(0xffffffffu, top >= bar)) {
 #pragma unroll
@@ -305,6 +306,7 @@ __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_const
       __syncwarp();
       if (lane == 0) mbar_arrive_remote(lead_tempty + 8u * buf);
       if (active && run.last) {
+        const RowStat r = sums.stat(a.c);
         if constexpr (TOP) {
           if (run.leaves()) {                                     // the lists are needed again: the best go elsewhere
             uint64_t* to = a.early + ((int64_t)(pair * 2 + half) * SC_ROWS + (row - lane)) * a.k;
@@ -369,7 +371,8 @@ __global__ void __launch_bounds__(SJ_THREADS) score_join_kernel(const ScoreArgs 
                                                                 int32_t d, float scale, RowAnswers ask) {
   using G = Group<SJ_THREADS>;
   if (!chain_begin()) return;
-  __shared__ TopList<SJ_THREADS> list;
+  __shared__ uint64_t keys[SJ_LIST];
+  __shared__ int ipart[SJ_WARPS], listed;
   __shared__ RowStat part[SJ_WARPS];
   __shared__ float fpart[SJ_WARPS];
   __shared__ int have_of[SJ_THREADS];
@@ -430,38 +433,39 @@ __global__ void __launch_bounds__(SJ_THREADS) score_join_kernel(const ScoreArgs 
       for (int j = lane; j < have_of[i]; j += 32) f(l[j]);
     }
   };
-  const int all = G::sum(have, list.part);              // also the barrier behind have_of
+  const int all = G::sum(have, ipart);              // also the barrier behind have_of
   uint64_t least = 1;
-  if (all > TopList<SJ_THREADS>::CAP) {
+  if (all > SJ_LIST) {
     uint64_t best = 0;
     each([&](uint64_t key) { best = max(best, key); });
     if (G::count(best != 0) >= k) least = kth_key(k, [&](uint64_t t) { return G::count(best >= t); });
     int c = 0;
     each([&](uint64_t key) { c += key >= least; });
-    if (G::sum(c, list.part) > TopList<SJ_THREADS>::CAP)          // many equal or clustered logits: the k-th key itself
+    if (G::sum(c, ipart) > SJ_LIST)          // many equal or clustered logits: the k-th key itself
       least = kth_key(k, [&](uint64_t t) {
         int m = 0;
         each([&](uint64_t key) { m += key >= t; });
-        return G::sum(m, list.part);
+        return G::sum(m, ipart);
       }, least);
   }
-  if (tid == 0) list.slow = 0;
+  if (tid == 0) listed = 0;
   G::sync();
   each([&](uint64_t key) {
-    if (key >= least) list.keys[atomicAdd(&list.slow, 1)] = key;
+    if (key >= least) keys[atomicAdd(&listed, 1)] = key;
   });
   G::sync();
-  have = list.slow;
+  have = listed;
   G::sync();
-  if (have > 256 && have > k) {
-    (void)top_cut(list, have, k);
+  if (have > 128 && have > k + k / 4) {
+    if (warp == 0) (void)warp_cut(keys, have, k);
     have = k;
+    G::sync();
   }
   const int64_t o = n * k;
   for (int i = tid; i < have; i += SJ_THREADS) {
-    const uint64_t key = list.keys[i];
+    const uint64_t key = keys[i];
     int above = 0;
-    for (int j = 0; j < have; ++j) above += list.keys[j] > key;
+    for (int j = 0; j < have; ++j) above += keys[j] > key;
     if (above < k) {
       ask.top_ids[o + above] = row_key_place(key);
       ask.top_logp[o + above] = row_logp(row_key_logit(key), r.m, log_s, scale);
