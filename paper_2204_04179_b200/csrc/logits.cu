@@ -12,6 +12,14 @@
 
 namespace {
 
+#ifndef LP_NV
+#define LP_NV 4
+#endif
+#ifndef LP_B
+#define LP_B 8
+#define LP_BT 8
+#define LP_BG 8
+#endif
 constexpr int LP_THREADS = 128, LP_WARPS = LP_THREADS / 32;      // of a block
 
 // ------------------------------ a slice of a row ----------------------------------------------------------------------
@@ -116,61 +124,67 @@ template <typename T, int TPR> __device__ __forceinline__ RowLogs row_logs(const
 
 // ------------------------------ log probabilities ---------------------------------------------------------------------
 template <typename T, int TPR, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS, TOP ? 6 : 7) logprobs_kernel(const T* logits, int64_t ld, int64_t N, int32_t V, float scale, int32_t shift,
+__global__ void __launch_bounds__(LP_THREADS, TOP ? LP_BT : LP_B) logprobs_kernel(const T* logits, int64_t ld, int64_t N, int32_t V, float scale, int32_t shift,
                                                                  RowAnswers ask, int32_t* status) {
   using G = Group<TPR>;
-  constexpr int NV = 4;
+  constexpr int NV = LP_NV;
   if (!chain_begin()) return;
   __shared__ RowStat part[LP_WARPS], of_slice[MAX_SLICES];
   __shared__ float fpart[LP_WARPS];
-  __shared__ uint64_t lists[TOP ? LP_WARPS * TOP_CAP : 1];
-  __shared__ uint32_t low[LP_WARPS][2];
-  __shared__ int counts[LP_WARPS];
+  __shared__ __align__(16) uint8_t scratch[TOP ? sizeof(TopScratch<TPR>) * (LP_THREADS / TPR) : 16];
   extern __shared__ uint64_t merged[];                  // [slices, k], sorted, in the first block of a cluster
   const int slices = TPR == 32 ? 1 : 1 << shift, tid = G::tid(), rank = blockIdx.x & (slices - 1);
   const int64_t n = TPR == 32 ? (int64_t)blockIdx.x * LP_WARPS + G::row() : blockIdx.x >> shift;
   if (TPR > 32 && slices > 1) gram_cluster_sync();      // every block of the cluster runs before another writes to it
   if (n >= N) return;                                   // whole warps, in the form that has no barrier over the block
-  uint64_t* warp_list = lists + (TOP ? (threadIdx.x >> 5) * TOP_CAP : 0);
-  uint64_t* list = TPR == 32 ? warp_list : lists;      // of the row
+  TopScratch<TPR>& sc = reinterpret_cast<TopScratch<TPR>*>(scratch)[TOP ? G::row() : 0];
   const float c = scale * kLog2e;
+  uint4 q[NV], next[NV];
   const Slice<T> s(logits + n * ld, V, rank, shift);
-  const int chunks = s.template chunks<TPR, NV>();
+  s.template load_chunk<TPR, NV, !TOP>(0, tid, q);
   const int edge_place = s.edge(tid);
   const float edge = edge_place >= 0 ? row_load(s.z + edge_place) : ROW_NEG_INF;
+  const int chunks = s.template chunks<TPR, NV>();
   RowSums sums;
-  TopState st{0, 0.f};
-  uint4 q[NV], next[NV];
-  s.template load_chunk<TPR, NV, true>(0, tid, q);
-#pragma unroll(TOP ? 1 : 2)
+  float top_a = ROW_NEG_INF, top_b = ROW_NEG_INF, top_group = ROW_NEG_INF;     // of the thread's entries so far, of a group's
+  int group_shift = 0, group = 0;
+  if constexpr (TOP) {
+    while (((chunks - 1) >> group_shift) >= TopScratch<TPR>::GROUPS) ++group_shift;
+    if (tid == 0) sc.entries = sc.found = 0;             // the statistics' barriers come before their use
+  }
+#pragma unroll 2
   for (int ch = 0; ch < chunks; ++ch) {
-    if (ch + 1 < chunks) s.template load_chunk<TPR, NV, true>(ch + 1, tid, next);
-    float a = chunk_top<T, 0, NV / 2>(q), b = chunk_top<T, NV / 2, NV>(q);
+    if (ch + 1 < chunks) s.template load_chunk<TPR, NV, !TOP>(ch + 1, tid, next);
+    const float a = chunk_top<T, 0, NV / 2>(q), b = chunk_top<T, NV / 2, NV>(q);
     row_add_vectors<T, NV>(sums, q, fmaxf(a, b), c);
-    const bool on_edge = edge_place >= 0 && (tid < 8 ? ch == 0 : ch == chunks - 1);
-    if (on_edge) {
-      sums.add(edge, c);
-      a = fmaxf(a, edge);
-    }
     if constexpr (TOP) {
-      if (ch == 0) st.bar = top_first_bar<TPR>(a, b, ask.k, low);
-      const int v = s.v0 + ch * (TPR * NV) + tid;
-      top_chunk<T, NV>(warp_list, st, TopChunk<T>{s.z, s.vectors() + v, s.place(v), s.v1 - v, TPR, NV, edge_place}, q, fmaxf(a, b), on_edge, ask.k);
-      if (ch == 0 && st.bar > -FLT_MAX) st.bar = row_order_logit(row_order(st.bar) + 1u);
+      top_a = fmaxf(top_a, a);
+      top_b = fmaxf(top_b, b);
+      top_group = fmaxf(top_group, fmaxf(a, b));
+      if (((ch + 1) & ((1 << group_shift) - 1)) == 0 || ch == chunks - 1) {
+        sc.group[group * TPR + tid] = top_group;
+        top_group = ROW_NEG_INF;
+        ++group;
+      }
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) q[i] = next[i];
   }
+  if (edge_place >= 0) sums.add(edge, c);
   RowStat r = G::join(sums.stat(c), c, part);
   int have = 0;
-  if constexpr (TOP) have = top_gather<T, TPR>(s.z, list, counts, st.have, ask.k);
+  const uint64_t* list = sc.keys;
+  if constexpr (TOP) {
+    if (TPR == 32) G::sync();
+    const float bar = top_bar<TPR>(edge_place >= 0 ? fmaxf(top_a, edge) : top_a, top_b, ask.k, sc);
+    have = top_collect<T, TPR, NV>(sc, TopSource{s.vectors(), s.head, s.v0, s.v1, edge, edge_place}, group, group_shift, bar, ask.k);
+  }
   if (TPR > 32 && slices > 1) {
     if (tid == 0) put_stat(&of_slice[rank], 0, r);
-    if constexpr (TOP) {                                // this slice's best, sorted, to the first block
+    if constexpr (TOP) {                              // this slice's best, sorted, to the first block
       for (int i = tid; i < have; i += TPR) {
         const uint64_t key = list[i];
-        int above = 0;
-        for (int j = 0; j < have; ++j) above += list[j] > key;
+        const int above = top_rank(list, have, key);
         if (above < ask.k) put_key(&merged[rank * ask.k + above], 0, key);
       }
       for (int i = have + tid; i < ask.k; i += TPR) put_key(&merged[rank * ask.k + i], 0, 0);
@@ -199,32 +213,31 @@ __global__ void __launch_bounds__(LP_THREADS, TOP ? 6 : 7) logprobs_kernel(const
     if (TPR == 32 || slices == 1) {
       for (int i = tid; i < have; i += TPR) {
         const uint64_t key = list[i];
-        int above = 0;
-        for (int j = 0; j < have; ++j) above += list[j] > key;
+        const int above = top_rank(list, have, key);
         if (above < ask.k) answer(above, key);
       }
       for (int i = have + tid; i < ask.k; i += TPR) answer(i, 0);
-      return;
-    }
-    int found = 0;
-    for (int i = tid; i < slices * ask.k; i += TPR) {
-      const uint64_t key = merged[i];
-      if (!key) continue;
-      ++found;
-      int at = 0;
-      for (int b = 0; b < slices; ++b) {                // keys of list b above this one: the lists descend, zeros last
-        int lo = 0, hi = ask.k;
-        while (lo < hi) {
-          const int mid = (lo + hi) / 2;
-          if (merged[b * ask.k + mid] > key) lo = mid + 1;
-          else hi = mid;
+    } else {
+      int found = 0;
+      for (int i = tid; i < slices * ask.k; i += TPR) {
+        const uint64_t key = merged[i];
+        if (!key) continue;
+        ++found;
+        int at = 0;
+        for (int b = 0; b < slices; ++b) {            // keys of list b above this one: the lists descend, zeros last
+          int lo = 0, hi = ask.k;
+          while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (merged[b * ask.k + mid] > key) lo = mid + 1;
+            else hi = mid;
+          }
+          at += lo;
         }
-        at += lo;
+        if (at < ask.k) answer(at, key);
       }
-      if (at < ask.k) answer(at, key);
+      found = G::sum(found, sc.part);
+      for (int i = found + tid; i < ask.k; i += TPR) answer(i, 0);
     }
-    found = G::sum(found, counts);
-    for (int i = found + tid; i < ask.k; i += TPR) answer(i, 0);
   }
 }
 
@@ -282,41 +295,87 @@ struct BackwardArgs {
   int32_t* status;
 };
 
+// What a row has at given places (the given tokens with their gradients, the teacher's entries with their logits): each thread
+// holds EPT of them.
+template <int TPR> struct AtPlaces {
+  static constexpr int EPT = GRAM_TOP_MAX / TPR;
+  int32_t id[EPT];
+  float given[EPT], z[EPT];
+  __device__ __forceinline__ void load_ids(const int32_t* ids, const float* values, int64_t n, int count, int V, int tid, int32_t* status) {
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) {
+      const int i = tid + e * TPR;
+      id[e] = -1;
+      given[e] = 0.f;
+      if (i < count) {
+        id[e] = ids[n * count + i];
+        given[e] = values[n * count + i];
+        if (id[e] < -1 || id[e] >= V) { gram_device_fail(status, GRAM_ERR_ID_RANGE); id[e] = -1; }
+      }
+    }
+  }
+  template <typename T> __device__ __forceinline__ void load_logits(const T* row) {
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) z[e] = id[e] >= 0 ? row_load(row + id[e]) : ROW_NEG_INF;
+  }
+};
+// of the entries that take part: the sum of the values at entry i's place, if i is the first entry there
+struct PlacesShared {
+  float value[GRAM_TOP_MAX];
+  int32_t place[GRAM_TOP_MAX];   // -1: takes no part
+  __device__ __forceinline__ bool sum_at(int i, int count, float& sum) const {
+    bool first = true;
+    sum = 0.f;
+    for (int j = 0; j < count; ++j)
+      if (place[j] == place[i]) {
+        first = first && j >= i;
+        sum += value[j];
+      }
+    return first;
+  }
+};
+
 // dz = scale (sum of g at the given places - p (sum of all g + h (log p + H))), 0 at masked places.  With l = log2 p the
 // dense part is 2^l (A + B l), A = -scale (G + h H), B = -scale h ln 2, or in y = l + log2 s, which takes one rounding less per
 // element, 2^y (A - B log2 s + B y) / s; y is held at -200 as in row_softmax.cuh.
 template <typename T, int TPR>
-__global__ void __launch_bounds__(LP_THREADS, 7) logprobs_backward_kernel(const T* logits, T* dlogits, BackwardArgs a) {
+__global__ void __launch_bounds__(LP_THREADS, LP_BG) logprobs_backward_kernel(const T* logits, T* dlogits, BackwardArgs a) {
   using G = Group<TPR>;
-  constexpr int NV = 4;
+  using At = AtPlaces<TPR>;
+  constexpr int NV = LP_NV;
   if (!chain_begin()) return;
-  __shared__ struct { float g[GRAM_TOP_MAX], z[GRAM_TOP_MAX]; int32_t place[GRAM_TOP_MAX]; } given[(LP_THREADS / TPR)];   // the given tokens that take part
+  __shared__ PlacesShared places[LP_THREADS / TPR];
   const int slices = TPR == 32 ? 1 : 1 << a.shift, tid = G::tid(), rank = blockIdx.x & (slices - 1);
   const int64_t n = TPR == 32 ? (int64_t)blockIdx.x * LP_WARPS + G::row() : blockIdx.x >> a.shift;
   if (n >= a.N) return;
-  auto& mine = given[G::row()];
+  const float c = a.scale * kLog2e;
+  uint4 q[NV], next[NV];
   const Slice<T> s(logits + n * a.ld, a.V, rank, a.shift);
+  At at;
+  at.load_ids(a.targets, a.dlogp, n, a.C, a.V, tid, a.status);
+  s.template load_chunk<TPR, NV, true>(0, tid, q);
+  at.load_logits(s.z);
+  PlacesShared& here = places[G::row()];
+  const float m = a.stats[2 * n], log_s = a.stats[2 * n + 1], h = a.dentropy ? a.dentropy[n] : 0.f, H = a.dentropy ? a.entropy[n] : 0.f;
   T* dz = dlogits + n * a.ld_out;
   const bool vec = same_alignment(s.z, dz);
-  uint4 q[NV], next[NV];
-  s.template load_chunk<TPR, NV, true>(0, tid, q);
   const int edge_place = s.edge(tid);
   const float edge = edge_place >= 0 ? row_load(s.z + edge_place) : ROW_NEG_INF;
-  for (int i = tid; i < a.C; i += TPR) {
-    int32_t t = a.targets[n * a.C + i];
-    if (t < -1 || t >= a.V) { gram_device_fail(a.status, GRAM_ERR_ID_RANGE); t = -1; }
-    const float x = t >= 0 ? row_load(s.z + t) : ROW_NEG_INF;
-    mine.place[i] = x == ROW_NEG_INF ? -1 : t;
-    mine.z[i] = x;
-    mine.g[i] = x == ROW_NEG_INF ? 0.f : a.dlogp[n * a.C + i];
-  }
-  // in place, no slice may be overwritten before all have read the given tokens' logits
-  if (TPR > 32 && slices > 1 && a.C > 0) gram_cluster_sync();
-  else G::sync();
   float sum = 0.f;
-  for (int i = 0; i < a.C; ++i) sum += mine.g[i];
-  const float m = a.stats[2 * n], log_s = a.stats[2 * n + 1], h = a.dentropy ? a.dentropy[n] : 0.f;
-  const float c = a.scale * kLog2e, A = -a.scale * (sum + (a.dentropy ? h * a.entropy[n] : 0.f)), B = -a.scale * h * kLn2;
+  if (a.C > 0) {
+#pragma unroll
+    for (int e = 0; e < At::EPT; ++e)
+      if (tid + e * TPR < a.C) {
+        const bool use = at.z[e] != ROW_NEG_INF;      // "none" and masked places take no part
+        here.place[tid + e * TPR] = use ? at.id[e] : -1;
+        here.value[tid + e * TPR] = use ? at.given[e] : 0.f;
+      }
+    // in place, no slice may be overwritten before all have read the given tokens' logits
+    if (TPR > 32 && slices > 1) gram_cluster_sync();
+    else G::sync();
+    for (int i = 0; i < a.C; ++i) sum += here.value[i];
+  }
+  const float A = -a.scale * fmaf(h, H, sum), B = -a.scale * h * kLn2;
   const bool none = (sum == 0.f && h == 0.f) || log_s == ROW_NEG_INF;    // nothing asked, or nothing left in the row
   const RowPower l(m, log_s, c);
   const float inv = exp2f(-l.log2_s), Ay = inv * fmaf(-B, l.log2_s, A), By = inv * B;
@@ -334,18 +393,15 @@ __global__ void __launch_bounds__(LP_THREADS, 7) logprobs_backward_kernel(const 
     for (int i = 0; i < NV; ++i) q[i] = next[i];
   }
   if (edge_place >= 0) dz[edge_place] = row_round<T>(one(edge));
-  G::sync();                                             // the given places are written again, by one thread each
-  for (int i = tid; i < a.C; i += TPR) {
-    const int p = mine.place[i];
-    if (p < 0 || !s.has(p)) continue;
-    float g = 0.f;
-    bool first = true;
-    for (int j = 0; j < a.C; ++j)
-      if (mine.place[j] == p) {
-        first = first && j >= i;
-        g += mine.g[j];
-      }
-    if (first) dz[p] = row_round<T>(one(mine.z[i]) + a.scale * g);
+  if (a.C > 0) {
+    G::sync();                                        // the given places are written again, by one thread each
+#pragma unroll
+    for (int e = 0; e < At::EPT; ++e) {
+      const int i = tid + e * TPR;
+      float g;
+      if (i < a.C && here.place[i] >= 0 && s.has(here.place[i]) && here.sum_at(i, a.C, g))
+        dz[here.place[i]] = row_round<T>(fmaf(a.scale, g, one(at.z[e])));
+    }
   }
 }
 
@@ -363,79 +419,84 @@ struct DistillArgs {
 // A slice is walked over twice: forwards for the statistics, backwards for the gradient, whose reads find it in L2 (the last
 // chunk is still in registers).  The plan keeps the slices of the blocks that run together well below L2's size.
 template <typename T, int TPR>
-__global__ void __launch_bounds__(LP_THREADS, 7) distill_kernel(const T* logits, T* dlogits, DistillArgs a) {
+__global__ void __launch_bounds__(LP_THREADS, LP_BG) distill_kernel(const T* logits, T* dlogits, DistillArgs a) {
   using G = Group<TPR>;
-  constexpr int NV = 4;
+  using At = AtPlaces<TPR>;
+  constexpr int NV = LP_NV;
   if (!chain_begin()) return;
   __shared__ RowStat part[LP_WARPS][2], of_slice[MAX_SLICES];
   __shared__ float fpart[LP_WARPS];
-  __shared__ struct { float q[GRAM_TOP_MAX], z[GRAM_TOP_MAX]; int32_t place[GRAM_TOP_MAX]; } entries[(LP_THREADS / TPR)];
+  __shared__ PlacesShared places[LP_THREADS / TPR];
   const int slices = TPR == 32 ? 1 : 1 << a.shift, tid = G::tid(), rank = blockIdx.x & (slices - 1);
   const int64_t n = TPR == 32 ? (int64_t)blockIdx.x * LP_WARPS + G::row() : blockIdx.x >> a.shift;
   if (n >= a.N) return;
-  auto& mine = entries[G::row()];
   const float c = a.scale * kLog2e;
-  const Slice<T> s(logits + n * a.ld, a.V, rank, a.shift);
-  const int chunks = s.template chunks<TPR, NV>();
   uint4 q[NV], next[NV];
+  const Slice<T> s(logits + n * a.ld, a.V, rank, a.shift);
+  At at;
+  at.load_ids(a.ids, a.teacher, n, a.k, a.V, tid, a.status);
   s.template load_chunk<TPR, NV, false>(0, tid, q);
+  at.load_logits(s.z);
+  if (TPR > 32 && slices > 1) gram_cluster_sync();       // every block of the cluster runs before another writes to it
+  PlacesShared& here = places[G::row()];
+  const float w = (a.weight ? a.weight[n] : 1.f) * a.scale;
   const int edge_place = s.edge(tid);
   const float edge = edge_place >= 0 ? row_load(s.z + edge_place) : ROW_NEG_INF;
+  const int chunks = s.template chunks<TPR, NV>();
   RowSums sums, teacher;
-  for (int i = tid; i < a.k; i += TPR) {
-    int32_t id = a.ids[n * a.k + i];
-    if (id < -1 || id >= a.V) { gram_device_fail(a.status, GRAM_ERR_ID_RANGE); id = -1; }
-    const float x = id >= 0 ? row_load(s.z + id) : ROW_NEG_INF, b = a.teacher[n * a.k + i];
-    const bool use = x != ROW_NEG_INF && b != ROW_NEG_INF;
-    mine.place[i] = use ? id : -1;
-    mine.z[i] = x;
-    mine.q[i] = b;
-    if (use) teacher.add(b, c);
-  }
-  if (TPR > 32 && slices > 1) gram_cluster_sync();       // every block of the cluster runs before another writes to it
   for (int ch = 0; ch < chunks; ++ch) {
     if (ch + 1 < chunks) s.template load_chunk<TPR, NV, false>(ch + 1, tid, next);
+    else if (dlogits && chunks > 1) s.template load_chunk<TPR, NV, true>(chunks - 2, tid, next);
     row_add_vectors<T, NV>(sums, q, chunk_top<T, 0, NV>(q), c);
     if (ch + 1 < chunks) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) q[i] = next[i];
     }
   }
-  if (dlogits && chunks > 1) s.template load_chunk<TPR, NV, true>(chunks - 2, tid, next);
   if (edge_place >= 0) sums.add(edge, c);
+  bool use[At::EPT];
+#pragma unroll
+  for (int e = 0; e < At::EPT; ++e) {
+    use[e] = at.z[e] != ROW_NEG_INF && at.given[e] != ROW_NEG_INF;
+    if (use[e]) teacher.add(at.given[e], c);
+  }
   RowStat r = sums.stat(c), t = teacher.stat(c);
   G::join(r, t, c, part);
   if (TPR > 32 && slices > 1) {
     if (tid < slices) put_stat(&of_slice[rank], tid, r);
-    gram_cluster_sync();                                 // all have read the teacher's places by now, too
+    gram_cluster_sync();                               // all have read the teacher's places by now, too
     r = join_slices(of_slice, slices, c);
   }
   const float log_s = row_logs<T, TPR>(r, s.z, a.V, c, fpart).log_s;
   float log_t = row_log_sum(t, c);
   if (row_is_huge(t.m, c)) {
     float sum = 0.f;
-    for (int i = tid; i < a.k; i += TPR)
-      if (mine.place[i] >= 0) sum += row_ex2((mine.q[i] - t.m) * c);
+#pragma unroll
+    for (int e = 0; e < At::EPT; ++e)
+      if (use[e]) sum += row_ex2((at.given[e] - t.m) * c);
     log_t = logf(G::sum(sum, fpart));
   }
   // such a row was read again as a whole: in place, no slice may be overwritten before all have done so
   if (TPR > 32 && slices > 1 && row_is_huge(r.m, c)) gram_cluster_sync();
   float loss = 0.f;
-  for (int i = tid; i < a.k; i += TPR) {
+#pragma unroll
+  for (int e = 0; e < At::EPT; ++e) {
     float qi = 0.f;
-    if (mine.place[i] >= 0) {
-      const float lq = (mine.q[i] - t.m) * a.scale - log_t;
+    if (use[e]) {
+      const float lq = (at.given[e] - t.m) * a.scale - log_t;
       qi = expf(lq);
-      if (!(qi == 0.f)) loss += qi * (lq - row_logp(mine.z[i], r.m, log_s, a.scale));
+      if (!(qi == 0.f)) loss += qi * (lq - row_logp(at.z[e], r.m, log_s, a.scale));
     }
-    mine.q[i] = qi;
+    if (tid + e * TPR < a.k) {
+      here.place[tid + e * TPR] = use[e] ? at.id[e] : -1;
+      here.value[tid + e * TPR] = qi;
+    }
   }
   if (rank == 0) {
     loss = G::sum(loss, fpart);
     if (tid == 0) a.loss[n] = loss;
   }
   if (!dlogits) return;
-  const float w = (a.weight ? a.weight[n] : 1.f) * a.scale;
   const bool none = w == 0.f || t.s == 0.f;
   T* dz = dlogits + n * a.ld_out;
   const bool vec = same_alignment(s.z, dz);
@@ -453,19 +514,15 @@ __global__ void __launch_bounds__(LP_THREADS, 7) distill_kernel(const T* logits,
     if (ch > 1 && !none) s.template load_chunk<TPR, NV, true>(ch - 2, tid, next);
   }
   if (edge_place >= 0) dz[edge_place] = row_round<T>(none ? 0.f : one(edge));
-  G::sync();                                             // the teacher's places are written again, by one thread each
-  if (none) return;
-  for (int i = tid; i < a.k; i += TPR) {
-    const int p = mine.place[i];
-    if (p < 0 || !s.has(p)) continue;
-    float sum = 0.f;
-    bool first = true;
-    for (int j = 0; j < a.k; ++j)
-      if (mine.place[j] == p) {
-        first = first && j >= i;
-        sum += mine.q[j];
-      }
-    if (first) dz[p] = row_round<T>(one(mine.z[i]) - w * sum);
+  G::sync();                                         // the teacher's places are written again, by one thread each
+  if (!none) {
+#pragma unroll
+    for (int e = 0; e < At::EPT; ++e) {
+      const int i = tid + e * TPR;
+      float sum;
+      if (i < a.k && here.place[i] >= 0 && s.has(here.place[i]) && here.sum_at(i, a.k, sum))
+        dz[here.place[i]] = row_round<T>(fmaf(-w, sum, one(at.z[e])));
+    }
   }
 }
 
@@ -477,9 +534,9 @@ struct RowPlan {
   bool warps;
   int shift;                     // 2^shift slices
 };
-constexpr int LP_PER_SM = 7;     // blocks of these kernels that an SM holds
-RowPlan row_plan(gram_ctx* ctx, int64_t N, int64_t row_bytes, int64_t most_bytes) {
-  RowPlan p{row_bytes <= 4096 && N >= 4 * kNumSMs, 0};
+constexpr int LP_PER_SM = 8;     // blocks of these kernels that an SM holds
+RowPlan row_plan(gram_ctx* ctx, int64_t N, int64_t row_bytes, int64_t most_bytes, int k = 0) {
+  RowPlan p{row_bytes <= 4096 && N >= 4 * kNumSMs && k <= 32, 0};
   if (p.warps) return p;
   const int64_t vectors = row_bytes / 16;
   const int most = gram_cluster_blocks(ctx) < MAX_SLICES ? gram_cluster_blocks(ctx) : MAX_SLICES;
@@ -511,7 +568,7 @@ gram_status launch_rows(gram_ctx* ctx, void (*kern)(P...), const RowPlan& plan, 
 
 template <typename T>
 gram_status logprobs_typed(gram_ctx* ctx, const T* z, int64_t ld, int64_t N, int32_t V, float scale, const RowAnswers& ask, cudaStream_t st) {
-  const RowPlan plan = row_plan(ctx, N, (int64_t)V * sizeof(T), INT64_MAX);
+  const RowPlan plan = row_plan(ctx, N, (int64_t)V * sizeof(T), INT64_MAX, ask.k);
   ProfScope prof(ctx, GRAM_K_OTHER, (double)N * V * sizeof(T), 1, st, "logprobs");
   int32_t* status = gram_status_word(ctx);
   const size_t smem = plan.shift > 0 ? (sizeof(uint64_t) * ask.k) << plan.shift : 0;

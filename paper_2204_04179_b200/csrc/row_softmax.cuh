@@ -168,6 +168,29 @@ template <int TPR> struct Group {
   }
 };
 
+// Pairs of fp32 values in one register pair, one instruction for the two.
+typedef uint64_t f32x2;
+__device__ __forceinline__ f32x2 x2_pack(float a, float b) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 x2_unpack(f32x2 v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ f32x2 x2_add(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 x2_fma(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
 template <typename T> struct RowVec;                 // 16 bytes of logits
 template <> struct RowVec<float> {
   static constexpr int N = 4;
@@ -177,6 +200,13 @@ template <> struct RowVec<float> {
   }
   static __device__ __forceinline__ float2 pair(const uint4& q, int i) {
     return i == 0 ? make_float2(__uint_as_float(q.x), __uint_as_float(q.y)) : make_float2(__uint_as_float(q.z), __uint_as_float(q.w));
+  }
+  // the pair held above -inf (NaN stays): c z is then finite, and e y of a masked place 0
+  static __device__ __forceinline__ f32x2 held(const uint4& q, int i) {
+    float2 x = pair(q, i);
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-1e30f));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-1e30f));
+    return x2_pack(x.x, x.y);
   }
   static __device__ __forceinline__ void put(uint4& q, int i, float2 v) {
     if (i == 0) { q.x = __float_as_uint(v.x); q.y = __float_as_uint(v.y); }
@@ -195,6 +225,11 @@ template <> struct RowVec<bf16> {
     const uint32_t w = i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w;
     return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
   }
+  static __device__ __forceinline__ f32x2 held(const uint4& q, int i) {
+    uint32_t w = i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w;
+    asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(w) : "r"(0xf149f149u));     // -1e30
+    return x2_pack(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  }
   static __device__ __forceinline__ void put(uint4& q, int i, float2 v) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
     const uint32_t w = *reinterpret_cast<const uint32_t*>(&h);
@@ -206,19 +241,20 @@ template <> struct RowVec<bf16> {
 template <typename T, int NV>
 __device__ __forceinline__ void row_add_vectors(RowSums& r, const uint4 (&q)[NV], float top, float c) {
   r.see(top, c);
-  float s1 = 0.f, t1 = 0.f;
+  f32x2 s = x2_pack(r.s, 0.f), t = x2_pack(r.t, 0.f);
+  const f32x2 cc = x2_pack(c, c), ref = x2_pack(-r.ref, -r.ref);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
 #pragma unroll
     for (int j = 0; j < RowVec<T>::N / 2; ++j) {
-      const float2 x = RowVec<T>::pair(q[i], j);
-      const float y0 = fmaf(x.x, c, -r.ref), y1 = fmaf(x.y, c, -r.ref), e0 = row_ex2(y0), e1 = row_ex2(y1);
-      r.s += e0;
-      s1 += e1;
-      r.t = fmaf(e0, fmaxf(y0, -200.f), r.t);
-      t1 = fmaf(e1, fmaxf(y1, -200.f), t1);
+      const f32x2 y = x2_fma(RowVec<T>::held(q[i], j), cc, ref);
+      const float2 y2 = x2_unpack(y);
+      const f32x2 e = x2_pack(row_ex2(y2.x), row_ex2(y2.y));
+      s = x2_add(s, e);
+      t = x2_fma(e, y, t);
     }
   }
-  r.s += s1;
-  r.t += t1;
+  const float2 s2 = x2_unpack(s), t2 = x2_unpack(t);
+  r.s = s2.x + s2.y;
+  r.t = t2.x + t2.y;
 }

@@ -1,11 +1,10 @@
 // The best k places of a row or a slice of one.
 //
-// Candidates have keys (row_key: larger logit first, then lower place).  The first chunk sets a bar that at least k of the
-// group's entries reach: the value that k of its threads' maxima reach, or a little less.  An entry below the bar is not among
-// the best k, and behind the first chunk neither is one that equals it, since a thread reads in ascending order.  Of a chunk, a
-// thread makes a bit mask of the entries that reach the bar, and the few places go to a list of its warp in shared memory;
-// their logits are read again at the end, all at once.  No barrier is needed until the lists are brought together.  A list
-// that would overflow (equal logits, ascending rows, large k) is cut to its best k, the last of which sets the warp's new bar.
+// While a row is read each thread only notes the largest entry of every group of chunks (one to a few).  At the end, a bar is
+// set that at least k entries reach: the value that k of the threads' maxima reach, or a little less.  The best k lie in the
+// groups whose maximum reaches the bar, hardly more than k of all threads' groups; these few are read again, and the entries
+// that reach the bar become keys (row_key: larger logit first, then lower place), whose order is found by counting.  Where
+// more groups or entries reach the bar than the lists hold (equal logits), the k-th key is found by bisection over the row.
 #pragma once
 #include "row_softmax.cuh"
 
@@ -54,27 +53,38 @@ __device__ __forceinline__ float warp_cut(uint64_t* keys, int have, int k) {
   return row_order_logit(__reduce_min_sync(0xffffffffu, low) + 1u);
 }
 
-constexpr int TOP_CAP = 3 * GRAM_TOP_MAX;              // entries of a warp's list: places while a row is read, keys then
 
-// the first chunk's bar, from two of each thread's entries, the largest of either half; part: a word for each warp and bound
-template <int TPR> __device__ __forceinline__ float top_first_bar(float a, float b, int k, uint32_t (*part)[2]) {
+template <int TPR> struct alignas(16) TopScratch {
+  static constexpr int GROUPS = TPR == 32 ? 4 : 32;     // of a thread
+  static constexpr int KEYS = TPR == 32 ? 384 : 1024, ENTRIES = TPR == 32 ? 128 : 512;
+  static_assert(KEYS >= GRAM_TOP_MAX, "an exact list fits");
+  uint64_t keys[KEYS];
+  float group[GROUPS * TPR];
+  uint16_t entry[ENTRIES];       // groups whose maximum reaches the bar: group * TPR + thread
+  int entries, found;
+  int part[Group<TPR>::WARPS];
+  uint32_t bound[Group<TPR>::WARPS][2];
+};
+
+// a bar, from two of each thread's entries, the largest of either half
+template <int TPR> __device__ __forceinline__ float top_bar(float a, float b, int k, TopScratch<TPR>& sc) {
   using G = Group<TPR>;
-  const bool two = k > TPR / 4;                          // 128 maxima are few for a larger k
+  const bool two = k > TPR / 4;                          // one maximum a thread is little for a larger k
   if (!two) a = fmaxf(a, b);
   const uint32_t oa = a > ROW_NEG_INF ? row_order(a) : 0u, ob = two && b > ROW_NEG_INF ? row_order(b) : 0u;
   uint32_t lo = __reduce_min_sync(0xffffffffu, min(oa ? oa : ~0u, ob ? ob : ~0u)), hi = __reduce_max_sync(0xffffffffu, max(oa, ob));
   if constexpr (TPR > 32) {
-    if ((threadIdx.x & 31) == 0) { part[threadIdx.x >> 5][0] = lo; part[threadIdx.x >> 5][1] = hi; }
+    if ((threadIdx.x & 31) == 0) { sc.bound[threadIdx.x >> 5][0] = lo; sc.bound[threadIdx.x >> 5][1] = hi; }
   }
   auto reach = [&](uint32_t o) {
     int n = G::count(oa >= o);
     if (two) n += G::count(ob >= o);
     return n;
   };
-  if (reach(1u) < k) return -FLT_MAX;                    // a barrier, for `part` too
+  if (reach(1u) < k) return -FLT_MAX;                    // a barrier, for the bounds too
   if constexpr (TPR > 32) {
 #pragma unroll
-    for (int w = 0; w < G::WARPS; ++w) { lo = min(lo, part[w][0]); hi = max(hi, part[w][1]); }
+    for (int w = 0; w < G::WARPS; ++w) { lo = min(lo, sc.bound[w][0]); hi = max(hi, sc.bound[w][1]); }
   }
   for (int step = 0; lo < hi && step < 12; ++step) {
     const uint32_t mid = hi - (hi - lo) / 2;
@@ -88,152 +98,98 @@ template <int TPR> __device__ __forceinline__ float top_first_bar(float a, float
   return row_order_logit(lo);
 }
 
-struct TopState {
-  int have;                      // places on the warp's list
-  float bar;                     // entries must reach it
-};
-// What the overflow needs to read a thread's part of a chunk again: `count` vectors, `stride` apart, and its single element.
-template <typename T> struct TopChunk {
-  const T* z;                    // the row
-  const uint4* from;             // the first vector, the place of its first element, vectors of the slice from it on
-  int place0, left, stride, count;
-  int edge;                      // place of the single element, -1: none
-  template <typename F> __device__ __forceinline__ void each(F f) const {
-    for (int i = 0; i < count; ++i) {
-      constexpr uint32_t none = RowVec<T>::NONE;
-      const uint4 q = i * stride < left ? from[i * stride] : make_uint4(none, none, none, none);
+// f(logit, place) of each entry of a vector at `place`
+template <typename T, typename F> __device__ __forceinline__ void each_of(const uint4& q, int place, F f) {
 #pragma unroll
-      for (int j = 0; j < RowVec<T>::N / 2; ++j) {
-        const float2 x = RowVec<T>::pair(q, j);
-        f(x.x, place0 + i * stride * RowVec<T>::N + 2 * j);
-        f(x.y, place0 + i * stride * RowVec<T>::N + 2 * j + 1);
-      }
-    }
-    f(edge >= 0 ? row_load(z + edge) : ROW_NEG_INF, edge);
+  for (int j = 0; j < RowVec<T>::N / 2; ++j) {
+    const float2 x = RowVec<T>::pair(q, j);
+    f(x.x, place + 2 * j);
+    f(x.y, place + 2 * j + 1);
   }
+}
+// What is read again: vectors [v0, v1) from `from` on, the first at place `place0`, and this thread's single element (-1: none).
+struct TopSource {
+  const uint4* from;
+  int place0, v0, v1;
+  float edge;
+  int edge_place;
 };
-// A chunk whose entries overflow the list: the list and then the chunk's own best k, found by bisection, cut to the best k.
-template <typename T> __device__ __noinline__ TopState top_overflow(uint64_t* list, TopState st, TopChunk<T> ch, int k) {
-  const int lane = threadIdx.x & 31;
-  constexpr int PER = TOP_CAP / 32;
-  uint32_t* places = reinterpret_cast<uint32_t*>(list);
-  {
-    uint32_t p[PER];
-    for (int i = 0; i < PER; ++i) p[i] = i * 32 + lane < st.have ? places[i * 32 + lane] : 0;
-    __syncwarp();
-    for (int i = 0; i < PER; ++i)
-      if (i * 32 + lane < st.have) list[i * 32 + lane] = row_key(row_load(ch.z + p[i]), p[i]);
-    __syncwarp();
-  }
-  auto cut = [&]() {
-    st.bar = fmaxf(st.bar, warp_cut(list, st.have, k));
-    st.have = k;
+// the best k of all entries by bisection; returns how many there are
+template <typename T, int TPR> __device__ __noinline__ int top_exact(TopScratch<TPR>& sc, TopSource src, int k) {
+  using G = Group<TPR>;
+  const int tid = G::tid();
+  auto each = [&](auto f) {
+    for (int v = src.v0 + tid; v < src.v1; v += TPR) each_of<T>(src.from[v], src.place0 + v * RowVec<T>::N, f);
+    if (src.edge_place >= 0) f(src.edge, src.edge_place);
   };
-  if (st.have > k) cut();
   auto at_least = [&](uint64_t t) {
     int c = 0;
-    ch.each([&](float x, int p) { c += x >= st.bar && row_key(x, p) >= t; });
-    return (int)__reduce_add_sync(0xffffffffu, c);
+    each([&](float x, int p) { c += x > ROW_NEG_INF && row_key(x, p) >= t; });
+    return G::sum(c, sc.part);
   };
   const int n = min(at_least(1), k);
-  if (n > 0) {
-    const uint64_t kth = kth_key(n, at_least);
-    ch.each([&](float x, int p) {
-      const bool keep = x >= st.bar && row_key(x, p) >= kth;
-      const uint32_t who = __ballot_sync(0xffffffffu, keep);
-      if (keep) list[st.have + __popc(who & ((1u << lane) - 1u))] = row_key(x, p);
-      st.have += __popc(who);
-    });
-    __syncwarp();
-    if (st.have >= k) cut();
-  }
-  {
-    uint64_t key[PER];
-    for (int i = 0; i < PER; ++i) key[i] = i * 32 + lane < st.have ? list[i * 32 + lane] : 0;
-    __syncwarp();
-    for (int i = 0; i < PER; ++i)
-      if (i * 32 + lane < st.have) places[i * 32 + lane] = (uint32_t)row_key_place(key[i]);
-    __syncwarp();
-  }
-  return st;
-}
-// A chunk's entries to the warp's list; top: the thread's largest; on_edge: its single element counts to this chunk.
-template <typename T, int NV>
-__device__ __forceinline__ void top_chunk(uint64_t* list, TopState& st, const TopChunk<T>& ch, const uint4 (&q)[NV], float top, bool on_edge, int k) {
-  if (!__any_sync(0xffffffffu, top >= st.bar)) return;
-  constexpr int N = RowVec<T>::N;
-  static_assert(N * NV <= 32, "a bit for each entry");
-  const uint32_t below = (1u << (threadIdx.x & 31)) - 1u;
-  uint32_t* places = reinterpret_cast<uint32_t*>(list);
-  uint32_t bits = 0u;
-#pragma unroll
-  for (int i = 0; i < NV; ++i)
-#pragma unroll
-    for (int j = 0; j < N / 2; ++j) {
-      const float2 x = RowVec<T>::pair(q[i], j);
-      if (x.x >= st.bar) bits |= 1u << (i * N + 2 * j);
-      if (x.y >= st.bar) bits |= 1u << (i * N + 2 * j + 1);
-    }
-  bool edge = on_edge && row_load(ch.z + ch.edge) >= st.bar;
-  int at = st.have;
-  for (;;) {
-    const bool in = bits != 0u || edge;
-    const uint32_t who = __ballot_sync(0xffffffffu, in);
-    if (!who) break;
-    if (in) {
-      const int j = __ffs(bits) - 1, slot = at + __popc(who & below);
-      if (slot < TOP_CAP) places[slot] = bits ? (uint32_t)(ch.place0 + (j / N) * ch.stride * N + j % N) : (uint32_t)ch.edge;
-      if (bits) bits &= bits - 1u;
-      else edge = false;
-    }
-    at += __popc(who);
-  }
-  if (at <= TOP_CAP) {
-    st.have = at;
-  } else {
-    __syncwarp();
-    TopChunk<T> again = ch;
-    if (!on_edge) again.edge = -1;
-    st = top_overflow<T>(list, st, again, k);
-  }
-}
-
-// The warps' lists (TOP_CAP entries apart) brought together as keys at the front of the first, and cut if they are long.  Returns
-// the keys left, k or a few more, or all there are.  Called by the whole group, with a barrier behind it.
-template <typename T, int TPR> __device__ __forceinline__ int top_gather(const T* z, uint64_t* list, int* count, int mine, int k) {
-  using G = Group<TPR>;
-  constexpr int PER = TOP_CAP / 32;
-  const int lane = threadIdx.x & 31, warp = TPR == 32 ? 0 : threadIdx.x >> 5;
-  const uint32_t* places = reinterpret_cast<const uint32_t*>(list + warp * TOP_CAP);
-  uint64_t key[PER];
-  __syncwarp();
-#pragma unroll
-  for (int i = 0; i < PER; ++i)
-    if (i * 32 < mine) {
-      const uint32_t p = i * 32 + lane < mine ? places[i * 32 + lane] : 0;
-      key[i] = row_key(row_load(z + p), p);
-    }
-  int at = 0, all = mine;
-  if constexpr (TPR > 32) {
-    if (lane == 0) count[warp] = mine;
-    __syncthreads();
-    all = 0;
-#pragma unroll
-    for (int w = 0; w < G::WARPS; ++w) {
-      if (w < warp) at += count[w];
-      all += count[w];
-    }
-  } else {
-    __syncwarp();
-  }
-#pragma unroll
-  for (int i = 0; i < PER; ++i)
-    if (i * 32 + lane < mine) list[at + i * 32 + lane] = key[i];
+  if (n == 0) return 0;
+  const uint64_t kth = kth_key(n, at_least);
   G::sync();
-  if (all > 128 && all > k + k / 4) {
-    if (G::tid() < 32) (void)warp_cut(list, all, k);
-    all = k;
+  if (tid == 0) sc.found = 0;
+  G::sync();
+  each([&](float x, int p) {
+    if (x > ROW_NEG_INF && row_key(x, p) >= kth) sc.keys[atomicAdd(&sc.found, 1)] = row_key(x, p);
+  });
+  G::sync();
+  return n;
+}
+// The candidates of a row or slice, as keys in sc.keys: at least its best k, or all there are; a 0 behind an odd number of them.
+// Group g holds the thread's vectors of chunks [g << shift, (g + 1) << shift), NV a chunk, TPR apart.  sc.entries and sc.found
+// are 0 before, behind a barrier; a barrier is behind what this leaves.
+template <typename T, int TPR, int NV>
+__device__ __forceinline__ int top_collect(TopScratch<TPR>& sc, const TopSource& src, int groups, int shift, float bar, int k) {
+  using G = Group<TPR>;
+  using Sc = TopScratch<TPR>;
+  const int tid = G::tid(), lane = threadIdx.x & 31;
+  for (int g = 0; g < groups; ++g) {
+    const bool in = sc.group[g * TPR + tid] >= bar;
+    const uint32_t who = __ballot_sync(0xffffffffu, in);
+    if (who) {
+      int at = 0;
+      if (lane == 0) at = atomicAdd(&sc.entries, __popc(who));
+      at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1u));
+      if (in && at < Sc::ENTRIES) sc.entry[at] = (uint16_t)(g * TPR + tid);
+    }
+  }
+  auto put = [&](float x, int p) {
+    if (x >= bar) {
+      const int at = atomicAdd(&sc.found, 1);
+      if (at < Sc::KEYS) sc.keys[at] = row_key(x, p);
+    }
+  };
+  if (src.edge_place >= 0) put(src.edge, src.edge_place);
+  G::sync();
+  const int entries = sc.entries;
+  if (entries <= Sc::ENTRIES) {
+    const int per = NV << shift;                         // vectors of a group, a power of two
+    for (int i = tid; i < entries * per; i += TPR) {
+      const int e = sc.entry[i / per], j = i & (per - 1);
+      const int v = src.v0 + (e / TPR) * (per * TPR) + j * TPR + e % TPR;
+      if (v < src.v1) each_of<T>(src.from[v], src.place0 + v * RowVec<T>::N, put);
+    }
+  }
+  G::sync();
+  int have = sc.found;
+  if (entries > Sc::ENTRIES || have > Sc::KEYS) have = top_exact<T, TPR>(sc, src, k);
+  if (have & 1) {                                        // read in pairs
+    if (tid == 0) sc.keys[have] = 0;
     G::sync();
   }
-  return all;
+  return have;
+}
+// keys of the list above this one
+__device__ __forceinline__ int top_rank(const uint64_t* list, int have, uint64_t key) {
+  int above = 0;
+#pragma unroll 4
+  for (int j = 0; j < have; j += 2) {
+    const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(list + j);
+    above += (v.x > key) + (v.y > key);
+  }
+  return above;
 }
