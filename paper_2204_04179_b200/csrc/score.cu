@@ -3,8 +3,12 @@
 // The product users x items^T runs on pairs of SMs (tcgen05 cta_group::2) as in gemm.cu: a cluster of two blocks owns a tile
 // of 256 users x 256 items, each stages its own 128 users and its own half of the items by TMA, the leader issues the MMAs,
 // and each block's tensor memory receives 128 users' logits, two tiles in turn.  The logits never leave it: an epilogue
-// thread owns one user (a lane of tensor memory) and half of a tile's columns, keeps the softmax statistics of what it has
-// seen in registers, and puts entries that reach its bar on a list of its own in global memory.
+// thread owns one user (a lane of tensor memory) and half of a tile's columns and keeps the softmax statistics of what it has
+// seen in registers.
+//
+// Alternatives take a first pass over a part of the items (score_kernel<SAMPLE>), which writes the maxima of groups of 8 or
+// 32 columns; score_bar_kernel takes from them a bar that at least k entries of a user reach, and in the main pass a thread puts
+// entries that reach its user's bar on a list of its own.  With a sample of S items about k V / S entries of a user do.
 //
 // Work is cut evenly: the units of 128 items of all row tiles, one row tile after another, are divided into contiguous
 // runs, one for each pair.  A run touches at most two row tiles, so a user's statistics and lists lie with a few pairs;
@@ -24,18 +28,26 @@ constexpr int SC_STAGES = 6, SC_EPI_WARPS = 8, SC_THREADS = 64 + 32 * SC_EPI_WAR
 constexpr int SC_BIAS_BYTES = SC_EPI_WARPS * 128 * 4;   // a warp's 128 columns
 constexpr int SC_SMEM = SC_STAGES * SC_STAGE + SC_BIAS_BYTES + 1024 + 256;
 constexpr int SC_LIST_MAX = 256;                        // most entries of a thread's list
-constexpr int SJ_LIST = 1024, SJ_THREADS = 256, SJ_WARPS = SJ_THREADS / 32;
 constexpr int SC_PAIR_THREADS = 2 * SC_ROWS;            // epilogue threads of a pair, one for each user and half
+constexpr int SJ_LIST = 1024, SJ_THREADS = 256, SJ_WARPS = SJ_THREADS / 32;
+constexpr int SB_ROWS = 8, SB_GROUPS = 1024;            // score_bar_kernel: rows of a block, most groups of a row
+
+enum ScoreMode { STATISTICS = 0, LISTS = 1, SAMPLE = 2 };   // LISTS: statistics too
 
 struct ScoreArgs {
   const float* bias;
   int64_t N;
-  int32_t V, num_kb, k, cap;     // cap: entries that a list holds
+  int32_t V, num_kb, k, cap;     // V: items of this pass; cap: entries that a list holds
   int32_t units, total, per_run; // units of a row tile, of all, of a pair's run
   float c;
+  const float* bars;             // [N]
   uint64_t* lists;               // [pair, half, row of the tile, cap]
-  uint64_t* early;               // [pair, half, row, k]: the best of the row tile that a run leaves before its last
+  uint64_t* early;               // [row tile, half, row, early_cap]: of the run that goes on with the next row tile
+  int32_t early_cap;
   float4* stats;                 // [pair, row tile of the run (0, 1), half, row]: m, s, t, entries of the list
+  float* sample;                 // maxima: [block of 32 columns, row] float4 of groups of 8, or one float
+  int64_t sample_rows;
+  int32_t fine;                  // groups of 8
   int32_t* status;
 };
 
@@ -61,6 +73,7 @@ struct ScoreRun {
   __device__ __forceinline__ bool leaves() const { return (end - 1) / units != tm; }     // the run goes on with another row tile
 };
 
+// a list cut to its best k by the whole warp; returns (in every lane) the bar that better logits reach
 __device__ __noinline__ float score_cut(uint64_t* list, int have, int k) { return warp_cut(list, have, k); }
 
 // x[32]: a block of 32 columns of this thread's row, with the bias (b: the warp's 32 values in shared memory; null: none)
@@ -78,11 +91,15 @@ __device__ __forceinline__ void score_block(uint32_t taddr, const float* b, floa
     }
   }
 }
-__device__ __forceinline__ float score_top(const float (&x)[32]) {
-  float t[8];
+// the maxima of its four groups of 8 columns
+__device__ __forceinline__ float4 score_tops(const float (&x)[32]) {
+  float t[4];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) t[j] = fmaxf(fmaxf(x[j], x[j + 8]), fmaxf(x[j + 16], x[j + 24]));
-  return fmaxf(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])), fmaxf(fmaxf(t[4], t[5]), fmaxf(t[6], t[7])));
+  for (int g = 0; g < 4; ++g) {
+    const float* y = x + 8 * g;
+    t[g] = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
+  }
+  return make_float4(t[0], t[1], t[2], t[3]);
 }
 __device__ __forceinline__ void score_add(RowSums& r, const float (&x)[32], float top, float c) {
   r.see(top, c);
@@ -98,48 +115,7 @@ __device__ __forceinline__ void score_add(RowSums& r, const float (&x)[32], floa
   r.s += s1;
   r.t += t1;
 }
-// A first bar for each lane's row from its columns of the first tile: a value that k of them reach, and few more.
-__device__ __forceinline__ float score_first_bar(uint32_t taddr, const float* b, int blocks, int k) {
-  float x[4][32];
-  uint32_t lo = 0xffffffffu, hi = 0u;
-  int some = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (i < blocks) {
-      score_block(taddr + i * 32, b ? b + i * 32 : nullptr, x[i]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 32; ++j) x[i][j] = ROW_NEG_INF;
-    }
-#pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (x[i][j] > ROW_NEG_INF) {
-        const uint32_t o = row_order(x[i][j]);
-        lo = min(lo, o);
-        hi = max(hi, o);
-        ++some;
-      }
-  }
-  const bool enough = some >= k;
-  bool done = !enough || lo >= hi;
-  for (int step = 0; step < 16 && __any_sync(0xffffffffu, !done); ++step) {
-    const uint32_t mid = hi - (hi - lo) / 2;
-    const float f = row_order_logit(mid);
-    int n = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 32; ++j) n += x[i][j] >= f;
-    if (!done) {
-      if (n < k) hi = mid - 1;
-      else lo = mid;
-      done = lo >= hi || (n >= k && n <= k + k / 8);
-    }
-  }
-  return enough ? row_order_logit(lo) : -FLT_MAX;
-}
-
-template <bool TOP>
+template <int MODE>
 __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_constant__ CUtensorMap users, const __grid_constant__ CUtensorMap items,
                                                               const __grid_constant__ ScoreArgs a) {
   extern __shared__ uint8_t smem_raw[];
@@ -245,7 +221,6 @@ __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_const
     RowSums sums;
     int have = 0;
     float bar = 0.f;
-    bool reached = false;
     uint32_t it = 0;
     const uint32_t lead_tempty = map_to_cta(tempty_bar(0), 0);
     for (; !failed && run.next(); ++it) {
@@ -267,36 +242,42 @@ __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_const
       tc_fence_after();
       if (active) {
         const uint32_t taddr = lane_addr + (uint32_t)(buf * SC_COLS + half * blocks * 32);
-        if (run.first) {
+        if (MODE != SAMPLE && run.first) {
           sums = RowSums();
           have = 0;
-          reached = false;
-          if (TOP) {
-            bar = score_first_bar(taddr, bias, blocks, a.k);
-            if (n >= a.N) bar = __int_as_float(0x7f800000);
-          }
+          if (MODE == LISTS) bar = n < a.N ? a.bars[n] : -ROW_NEG_INF;
         }
         for (int b = 0; b < blocks; ++b) {
           float x[32];
           score_block(taddr + b * 32, bias ? bias + b * 32 : nullptr, x);
-          const float top = score_top(x);
+          const float4 tops = score_tops(x);
+          const float top = fmaxf(fmaxf(tops.x, tops.y), fmaxf(tops.z, tops.w));
+          if constexpr (MODE == SAMPLE) {
+            const int64_t at = (int64_t)((col0 + b * 32) / 32) * a.sample_rows + n;
+            if (a.fine) reinterpret_cast<float4*>(a.sample)[at] = tops;
+            else a.sample[at] = top;
+            continue;
+          }
           score_add(sums, x, top, a.c);
-          if constexpr (TOP) {
+          if constexpr (MODE == LISTS) {
             if (__any_sync(0xffffffffu, top >= bar)) {
+              const float t[4] = {tops.x, tops.y, tops.z, tops.w};
 #pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (x[j] >= bar) list[have++] = row_key(x[j], (uint32_t)(col0 + b * 32 + j));
-              if (!reached && have >= a.k) {                      // later entries must pass the bar
-                bar = row_order_logit(row_order(bar) + 1u);
-                reached = true;
+              for (int g = 0; g < 4; ++g) {
+                if (!__any_sync(0xffffffffu, t[g] >= bar)) continue;
+#pragma unroll
+                for (int j = 8 * g; j < 8 * g + 8; ++j) {
+                  if (!__any_sync(0xffffffffu, x[j] >= bar)) continue;
+                  if (x[j] >= bar) list[have++] = row_key(x[j], (uint32_t)(col0 + b * 32 + j));
+                }
               }
               uint32_t full = __ballot_sync(0xffffffffu, have > a.cap - 32);
               __syncwarp();
-              while (full) {
+              while (full) {                                      // more entries reach the bar than a list holds: its best k stay
                 const int of = __ffs(full) - 1;
                 full &= full - 1;
                 const float up = score_cut(warp_lists + (int64_t)of * a.cap, __shfl_sync(0xffffffffu, have, of), a.k);
-                if (lane == of) { have = a.k; bar = up; reached = true; }
+                if (lane == of) { have = a.k; bar = up; }
               }
             }
           }
@@ -305,19 +286,22 @@ __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_const
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_remote(lead_tempty + 8u * buf);
-      if (active && run.last) {
+      if (MODE != SAMPLE && active && run.last) {
         const RowStat r = sums.stat(a.c);
-        if constexpr (TOP) {
-          if (run.leaves()) {                                     // the lists are needed again: the best go elsewhere
-            uint64_t* to = a.early + ((int64_t)(pair * 2 + half) * SC_ROWS + (row - lane)) * a.k;
+        if constexpr (MODE == LISTS) {
+          if (run.leaves()) {                                     // the lists are needed again: these go elsewhere
+            uint64_t* to = a.early + ((int64_t)(run.tm * 2 + half) * SC_ROWS + (row - lane)) * a.early_cap;
             __syncwarp();
             for (int of = 0; of < 32; ++of) {
               uint64_t* from = warp_lists + (int64_t)of * a.cap;
-              const int n_of = __shfl_sync(0xffffffffu, have, of);
-              if (n_of > a.k) (void)score_cut(from, n_of, a.k);
-              for (int i = lane; i < min(n_of, a.k); i += 32) to[(int64_t)of * a.k + i] = from[i];
+              int n_of = __shfl_sync(0xffffffffu, have, of);
+              if (n_of > a.early_cap) {
+                (void)score_cut(from, n_of, a.k);
+                n_of = a.k;
+                if (lane == of) have = n_of;
+              }
+              for (int i = lane; i < n_of; i += 32) to[(int64_t)of * a.early_cap + i] = from[i];
             }
-            have = min(have, a.k);
             __syncwarp();
           }
         }
@@ -347,6 +331,54 @@ __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_const
   }
 }
 
+// The bar of each user: a value that k of its groups' maxima reach, or a little less; the lowest finite value if they are fewer.
+// A block takes 8 rows, a warp each.
+__global__ void __launch_bounds__(32 * SB_ROWS) score_bar_kernel(const float* sample, int64_t rows, int32_t blocks, int32_t fine, int64_t N, int32_t k,
+                                                                 float* bars) {
+  if (!chain_begin()) return;
+  __shared__ __align__(16) float value[SB_ROWS][SB_GROUPS + 4];
+  const int64_t n0 = (int64_t)blockIdx.x * SB_ROWS;
+  const int groups = fine ? 4 * blocks : blocks;
+  for (int i = threadIdx.x; i < blocks * SB_ROWS; i += 32 * SB_ROWS) {
+    const int r = i % SB_ROWS, b = i / SB_ROWS;
+    const int64_t at = (int64_t)b * rows + n0 + r;      // the rows are padded to whole tiles
+    if (fine) *reinterpret_cast<float4*>(&value[r][4 * b]) = reinterpret_cast<const float4*>(sample)[at];
+    else value[r][b] = sample[at];
+  }
+  __syncthreads();
+  const int lane = threadIdx.x & 31, r = threadIdx.x >> 5;
+  if (n0 + r >= N) return;
+  uint32_t lo = ~0u, hi = 0u;
+  int some = 0;
+  for (int i = lane; i < groups; i += 32)
+    if (value[r][i] > ROW_NEG_INF) {
+      const uint32_t o = row_order(value[r][i]);
+      lo = min(lo, o);
+      hi = max(hi, o);
+      ++some;
+    }
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  float bar = -FLT_MAX;
+  if ((int)__reduce_add_sync(0xffffffffu, some) >= k) {
+    for (int step = 0; lo < hi && step < 16; ++step) {
+      const uint32_t mid = hi - (hi - lo) / 2;
+      const float f = row_order_logit(mid);
+      int n = 0;
+#pragma unroll 4
+      for (int i = lane; i < groups; i += 32) n += value[r][i] >= f;
+      n = __reduce_add_sync(0xffffffffu, n);
+      if (n < k) hi = mid - 1;
+      else {
+        lo = mid;
+        if (n <= k + k / 8) break;
+      }
+    }
+    bar = row_order_logit(lo);
+  }
+  if (lane == 0) bars[n0 + r] = bar;
+}
+
 // users[n] . items[v], by a warp
 __device__ __forceinline__ float score_dot(const bf16* u, const bf16* w, int d) {
   const int lane = threadIdx.x & 31;
@@ -372,7 +404,7 @@ __global__ void __launch_bounds__(SJ_THREADS) score_join_kernel(const ScoreArgs 
   using G = Group<SJ_THREADS>;
   if (!chain_begin()) return;
   __shared__ uint64_t keys[SJ_LIST];
-  __shared__ int ipart[SJ_WARPS], listed;
+  __shared__ int ipart[SJ_WARPS], wpart[SJ_WARPS], listed;
   __shared__ RowStat part[SJ_WARPS];
   __shared__ float fpart[SJ_WARPS];
   __shared__ int have_of[SJ_THREADS];
@@ -424,16 +456,36 @@ __global__ void __launch_bounds__(SJ_THREADS) score_join_kernel(const ScoreArgs 
   }
   if (ask.k == 0) return;
   const int k = ask.k;
-  // f(key) for each key of this thread's share: a warp takes a list at a time
+  // f(key) for each key of this thread's share: the lists as rows of a table as wide as the longest, eight loads at once
+  const int wide = (int)__reduce_max_sync(0xffffffffu, have);
+  if (lane == 0) wpart[warp] = wide;
+  __syncthreads();                                      // of have_of, too
+  int width = 0;
+#pragma unroll
+  for (int w = 0; w < SJ_WARPS; ++w) width = max(width, wpart[w]);
   auto each = [&](auto f) {
-    for (int i = warp; i < parts; i += SJ_WARPS) {
-      const int p = p0 + i / 2;
-      const int64_t at = (int64_t)(p * 2 + (i & 1)) * SC_ROWS + row;
-      const uint64_t* l = is_early(p) ? a.early + at * k : a.lists + at * a.cap;
-      for (int j = lane; j < have_of[i]; j += 32) f(l[j]);
+    const int cells = parts * width;
+    for (int c0 = tid; c0 < cells; c0 += 8 * SJ_THREADS) {
+      uint64_t key[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int cell = c0 + u * SJ_THREADS;
+        key[u] = 0;
+        if (cell < cells) {
+          const int i = cell / width, j = cell - i * width, p = p0 + i / 2;
+          if (j < have_of[i]) {
+            const uint64_t* l = is_early(p) ? a.early + ((int64_t)(tm * 2 + (i & 1)) * SC_ROWS + row) * a.early_cap
+                                            : a.lists + ((int64_t)(p * 2 + (i & 1)) * SC_ROWS + row) * a.cap;
+            key[u] = l[j];
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (key[u]) f(key[u]);
     }
   };
-  const int all = G::sum(have, ipart);              // also the barrier behind have_of
+  const int all = G::sum(have, ipart);
   uint64_t least = 1;
   if (all > SJ_LIST) {
     uint64_t best = 0;
@@ -477,8 +529,8 @@ __global__ void __launch_bounds__(SJ_THREADS) score_join_kernel(const ScoreArgs 
   }
 }
 
-template <bool TOP> cudaError_t launch_score(const CUtensorMap& users, const CUtensorMap& items, const ScoreArgs& a, int pairs, cudaStream_t st) {
-  auto kern = score_kernel<TOP>;
+template <int MODE> cudaError_t launch_score(const CUtensorMap& users, const CUtensorMap& items, const ScoreArgs& a, int pairs, cudaStream_t st) {
+  auto kern = score_kernel<MODE>;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SC_SMEM);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -502,56 +554,93 @@ template <bool TOP> cudaError_t launch_score(const CUtensorMap& users, const CUt
 gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_users, const void* items, int64_t ld_items,
                                   const float* bias, int64_t N, int32_t V, int32_t d, float scale, const RowAnswers& ask, void* ws,
                                   size_t ws_bytes, cudaStream_t st) {
-  // Lists as long as the workspace allows for all pairs (up to 256 entries a thread; a longer one is cut less often); where
-  // that leaves less than 40 over k (small workspace, large k), lists of k + 64 and as many pairs as have room.
-  const size_t fixed = 2 * SC_PAIR_THREADS * sizeof(float4);
-  int pairs = kNumSMs / 2;
-  int64_t cap = 0;
+  const int32_t all_units = ceil_div(V, SC_UNIT);
+  if (all_units > (1 << 30) / (kNumSMs / 2)) return gram_set_error(ctx, "gram_score_logprobs: %d items", V), GRAM_ERR_UNSUPPORTED;
+  // The sample: so many items that about 256 entries of a user reach the bar, but 4096 at least and a quarter of the table at
+  // most; its maxima by groups of 8 columns, by 32 where that is more than score_bar_kernel holds.
+  int32_t sample = 0, fine = 1;
   if (ask.k) {
-    const int64_t room = (int64_t)(ws_bytes / pairs - fixed) / (SC_PAIR_THREADS * 8) - ask.k;
-    cap = room < SC_LIST_MAX ? room : SC_LIST_MAX;
-    if (cap < ask.k + 40) {
-      cap = ask.k + 64;
-      pairs = (int)(ws_bytes / (fixed + (size_t)(cap + ask.k) * SC_PAIR_THREADS * 8));
-      if (pairs > kNumSMs / 2) pairs = kNumSMs / 2;
-    }
+    int64_t want = (int64_t)ask.k * V / 256;
+    if (want > V / 4) want = V / 4;
+    if (want < 4096) want = 4096;
+    if (want > SB_GROUPS * 32) want = SB_GROUPS * 32;
+    sample = (int32_t)(want < V ? ceil_div64(want, SC_UNIT) * SC_UNIT : V);
+    if (sample > V) sample = V;
+    fine = sample <= SB_GROUPS * 8;
   }
-  const int32_t units = ceil_div(V, SC_UNIT);
-  int64_t most = pairs;                                 // row tiles of a launch: a run then touches two at most
-  if (most * units > (1 << 30)) most = (1 << 30) / units;
-  if (pairs < 1 || most < 1) return gram_set_error(ctx, "gram_score_logprobs: %d items, %d alternatives", V, ask.k), GRAM_ERR_UNSUPPORTED;
-  const int64_t tiles = ceil_div64(N, SC_ROWS), launches = ceil_div64(tiles, most), per_launch = ceil_div64(tiles, launches) * SC_ROWS;
+  const int32_t sample_units = ceil_div(sample, SC_UNIT);
+  // Row tiles of a launch: half the pairs at most, so that a run touches two row tiles at most and several threads share a
+  // user's list; and no more than the sample's maxima have room for.
+  const int64_t tiles = ceil_div64(N, SC_ROWS);
+  int64_t most = kNumSMs / 4;
+  const size_t sample_tile = (size_t)sample_units * (SC_UNIT / 32) * SC_ROWS * (fine ? 16 : 4);
+  const size_t stats_bytes = (size_t)(kNumSMs / 2) * 2 * SC_PAIR_THREADS * sizeof(float4), bars_tile = SC_ROWS * sizeof(float);
+  if (ask.k && most > (int64_t)((ws_bytes - stats_bytes) / (sample_tile + bars_tile))) most = (int64_t)((ws_bytes - stats_bytes) / (sample_tile + bars_tile));
+  // Lists share the sample's place, 32 entries more than k in each.  Where the workspace is too small for those of all pairs and the
+  // early ones of all row tiles, a launch takes fewer row tiles, and fewer pairs run.
+  const int early_cap = ask.k > 64 ? ask.k : 64;
+  int64_t per_launch, cap;
+  int pairs;
+  for (;; most /= 2) {
+    per_launch = ceil_div64(tiles, ceil_div64(tiles, most));
+    pairs = kNumSMs / 2;
+    cap = 0;
+    if (!ask.k) break;
+    const int64_t room = ((int64_t)ws_bytes - (int64_t)stats_bytes - per_launch * (int64_t)bars_tile) / (SC_PAIR_THREADS * 8) - per_launch * early_cap;
+    cap = room / pairs < SC_LIST_MAX ? room / pairs : SC_LIST_MAX;
+    if (cap >= ask.k + 32) break;
+    cap = ask.k + 32;
+    pairs = (int)(room / cap);
+    if (pairs >= 2 * per_launch) break;
+    if (most == 1) return gram_set_error(ctx, "gram_score_logprobs: the workspace is too small for %d alternatives", ask.k), GRAM_ERR_WORKSPACE;
+  }
+  const size_t early_bytes = ask.k ? (size_t)per_launch * SC_PAIR_THREADS * early_cap * 8 : 0;
   CUtensorMap map_u, map_i;
   if (!make_map(&map_i, items, (uint64_t)d, (uint64_t)V, (uint64_t)ld_items, SC_BK, 64))
     return gram_set_error(ctx, "gram_score_logprobs: cannot describe the items"), GRAM_ERR_UNSUPPORTED;
-  ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * N * V * d, 2 * (int)launches, st, "score");
-  for (int64_t n = 0; n < N; n += per_launch) {
-    const int64_t now = N - n < per_launch ? N - n : per_launch;
+  ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * N * V * d, (ask.k ? 4 : 2) * (int)ceil_div64(tiles, per_launch), st, "score");
+  for (int64_t n = 0; n < N; n += per_launch * SC_ROWS) {
+    const int64_t now = N - n < per_launch * SC_ROWS ? N - n : per_launch * SC_ROWS, now_tiles = ceil_div64(now, SC_ROWS);
     const bf16* u = (const bf16*)users + n * ld_users;
     if (!make_map(&map_u, u, (uint64_t)d, (uint64_t)now, (uint64_t)ld_users, SC_BK, SM_ROWS))
       return gram_set_error(ctx, "gram_score_logprobs: cannot describe the users"), GRAM_ERR_UNSUPPORTED;
     ScoreArgs a = {};
     a.bias = bias;
     a.N = now;
-    a.V = V;
     a.num_kb = ceil_div(d, SC_BK);
     a.k = ask.k;
     a.cap = (int32_t)cap;
-    a.units = units;
-    a.total = (int32_t)(ceil_div64(now, SC_ROWS) * units);
-    a.per_run = ceil_div(a.total, pairs);
-    a.c = scale * 1.4426950408889634f;
+    a.early_cap = early_cap;
+    a.c = scale * kLog2e;
     a.stats = (float4*)ws;
-    a.lists = (uint64_t*)((uint8_t*)ws + fixed * pairs);
-    a.early = a.lists + (int64_t)pairs * SC_PAIR_THREADS * cap;
+    float* bars = (float*)((uint8_t*)ws + stats_bytes);
+    a.bars = bars;
+    a.early = (uint64_t*)((uint8_t*)bars + per_launch * bars_tile);
+    a.lists = a.early + early_bytes / 8;
+    a.sample = (float*)a.early;
+    a.sample_rows = now_tiles * SC_ROWS;
+    a.fine = fine;
     a.status = gram_status_word(ctx);
+    auto cut = [&](int32_t items_now, int over) {       // the units of a pass in runs; returns their number
+      a.V = items_now;
+      a.units = ceil_div(items_now, SC_UNIT);
+      a.total = (int32_t)(now_tiles * a.units);
+      a.per_run = ceil_div(a.total, over);
+      return ceil_div(a.total, a.per_run);
+    };
+    if (ask.k) {
+      const int used = cut(sample, kNumSMs / 2);
+      GRAM_CUDA(ctx, launch_score<SAMPLE>(map_u, map_i, a, used, st));
+      launch_chain(score_bar_kernel, dim3((unsigned)ceil_div64(now, SB_ROWS)), 32 * SB_ROWS, 0, st, a.sample, a.sample_rows,
+                   a.units * (SC_UNIT / 32), fine, now, ask.k, bars);
+    }
     RowAnswers part = ask;
     if (ask.C) { part.targets += n * ask.C; part.logp += n * ask.C; }
     if (ask.stats) part.stats += 2 * n;
     if (ask.entropy) part.entropy += n;
     if (ask.k) { part.top_logp += n * ask.k; part.top_ids += n * ask.k; }
-    const int used = ceil_div(a.total, a.per_run);
-    GRAM_CUDA(ctx, ask.k ? launch_score<true>(map_u, map_i, a, used, st) : launch_score<false>(map_u, map_i, a, used, st));
+    const int used = cut(V, pairs);
+    GRAM_CUDA(ctx, ask.k ? launch_score<LISTS>(map_u, map_i, a, used, st) : launch_score<STATISTICS>(map_u, map_i, a, used, st));
     launch_chain(score_join_kernel, dim3((unsigned)now), SJ_THREADS, 0, st, a, u, ld_users, (const bf16*)items, ld_items, d, scale, part);
     GRAM_LAUNCH_CHECK(ctx);
   }
