@@ -38,6 +38,12 @@ SYMBOLS = ["gram_create", "gram_destroy", "gram_sync", "gram_last_error", "gram_
            "gram_optimizer_export", "gram_optimizer_import", "gram_selftest_bounded_wait", "gram_selftest_ring_rows", "gram_selftest_cluster_blocks", "gram_selftest_column_sums", "gram_grads_device",
            "gram_gemm_bf16_epilogue", "gram_logprobs", "gram_logprobs_backward", "gram_distill", "gram_score_logprobs"]
 
+# argument types of the calls on rows of logits, which a serving loop makes for single rows: declared once, so that a call passes
+# plain numbers and addresses (p: address, i: int32, l: int64, f: float)
+_TYPES = {"p": C.c_void_p, "i": C.c_int32, "l": C.c_int64, "f": C.c_float}
+_ROW_CALLS = {"gram_logprobs": "ppillifpipppppip", "gram_logprobs_backward": "ppillifpippppplp", "gram_distill": "ppillifppippplp",
+              "gram_score_logprobs": "pplplpliifpipppppip"}
+
 KINDS = ["gemm", "attention", "layernorm", "colsum", "embed_pool", "dedup", "gather", "accumulate", "task_head", "other",
          "optimizer"]
 
@@ -88,6 +94,8 @@ def lib():
         for s in SYMBOLS:
             getattr(L, s).restype = C.c_int
         L.gram_last_error.restype = C.c_char_p
+        for s, types in _ROW_CALLS.items():
+            getattr(L, s).argtypes = [_TYPES[t] for t in types]
         _lib = L
     return _lib
 
@@ -130,21 +138,40 @@ def _ptr(t) -> C.c_void_p:
 
 def _rows(t):
     """(address, dtype, elements between rows) of a matrix whose rows are contiguous but may lie further apart."""
-    import torch
-    assert t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1), "rows must be contiguous"
-    assert t.dtype in (torch.float32, torch.bfloat16)
-    ld = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
-    return C.c_void_p(t.data_ptr()), GRAM_F32 if t.dtype == torch.float32 else GRAM_BF16, C.c_int64(ld)
+    N, V = t.shape
+    ld, step = t.stride()
+    assert step == 1 or V <= 1, "rows must be contiguous"
+    return t.data_ptr(), _row_types()[t.dtype], ld if N > 1 else max(ld, V)
+
+
+_ROW_TYPES = {}
+
+
+def _row_types():
+    if not _ROW_TYPES:
+        import torch
+        _ROW_TYPES.update({torch.float32: GRAM_F32, torch.bfloat16: GRAM_BF16, "f": torch.float32, "i": torch.int32})
+    return _ROW_TYPES
 
 
 def _width(t) -> int:
     return 0 if t is None else t.shape[1]
 
 
-def _check(t, dtype, *shape):
-    """An array that a call takes as contiguous, of this type and shape; None passes."""
-    if t is not None:
-        assert t.dtype == dtype and tuple(t.shape) == shape, (t.dtype, tuple(t.shape), dtype, shape)
+def _array(t, kind: str, count: int):
+    """Address of a contiguous array of this type ("f" or "i") and number of elements; None -> NULL."""
+    if t is None:
+        return None
+    assert t.dtype is _ROW_TYPES[kind] and t.numel() == count and t.is_contiguous(), (t.dtype, t.shape, kind, count)
+    return t.data_ptr()
+
+
+def _raw_stream(stream) -> int:
+    """The stream's handle for a call with declared argument types."""
+    if stream is None:
+        import torch
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
 def _stream(stream) -> C.c_void_p:
@@ -284,57 +311,41 @@ class Gram:
         self._ck(lib().gram_task(self._h, _ptr(E), _ptr(labels), C.c_int32(B), _ptr(dE), _ptr(loss), _stream(stream)))
 
     # answers over a pool, and learning from them: logits [N, V] fp32 or bf16, rows may lie further apart
-    def _answers(self, N, targets, logp, stats, entropy, top_logp, top_ids):
-        import torch
-        _check(targets, torch.int32, N, _width(targets)); _check(logp, torch.float32, N, _width(targets))
-        _check(stats, torch.float32, N, 2); _check(entropy, torch.float32, N)
-        _check(top_ids, torch.int32, N, _width(top_ids)); _check(top_logp, torch.float32, N, _width(top_ids))
-        return (_ptr(targets), C.c_int32(_width(targets)), _ptr(logp), _ptr(stats), _ptr(entropy), _ptr(top_logp), _ptr(top_ids),
-                C.c_int32(_width(top_ids)))
-
     def logprobs(self, logits, scale=1.0, targets=None, logp=None, stats=None, entropy=None, top_logp=None, top_ids=None, stream=None):
         p, dtype, ld = _rows(logits)
-        N, V = logits.shape
-        self._ck(lib().gram_logprobs(self._h, p, C.c_int(dtype), ld, C.c_int64(N), C.c_int32(V), C.c_float(scale),
-                                     *self._answers(N, targets, logp, stats, entropy, top_logp, top_ids), _stream(stream)))
+        (N, V), nc, k = logits.shape, _width(targets), _width(top_ids)
+        self._ck(lib().gram_logprobs(self._h, p, dtype, ld, N, V, scale, _array(targets, "i", N * nc), nc, _array(logp, "f", N * nc),
+                                     _array(stats, "f", N * 2), _array(entropy, "f", N), _array(top_logp, "f", N * k),
+                                     _array(top_ids, "i", N * k), k, _raw_stream(stream)))
 
     def logprobs_backward(self, logits, stats, dlogits, scale=1.0, targets=None, dlogp=None, entropy=None, dentropy=None, stream=None):
-        import torch
         p, dtype, ld = _rows(logits)
         q, dtype_out, ld_out = _rows(dlogits)
-        N, V = logits.shape
+        (N, V), nc = logits.shape, _width(targets)
         assert dlogits.shape == logits.shape and dtype_out == dtype
-        _check(targets, torch.int32, N, _width(targets)); _check(dlogp, torch.float32, N, _width(targets))
-        _check(stats, torch.float32, N, 2); _check(entropy, torch.float32, N); _check(dentropy, torch.float32, N)
-        self._ck(lib().gram_logprobs_backward(self._h, p, C.c_int(dtype), ld, C.c_int64(N), C.c_int32(V), C.c_float(scale), _ptr(targets),
-                                              C.c_int32(_width(targets)), _ptr(stats), _ptr(entropy), _ptr(dlogp), _ptr(dentropy), q, ld_out,
-                                              _stream(stream)))
+        self._ck(lib().gram_logprobs_backward(self._h, p, dtype, ld, N, V, scale, _array(targets, "i", N * nc), nc, _array(stats, "f", N * 2),
+                                              _array(entropy, "f", N), _array(dlogp, "f", N * nc), _array(dentropy, "f", N), q, ld_out,
+                                              _raw_stream(stream)))
 
     def distill(self, logits, teacher_ids, teacher_logits, loss, scale=1.0, weight=None, dlogits=None, stream=None):
-        import torch
         p, dtype, ld = _rows(logits)
-        N, V = logits.shape
-        q, ld_out = C.c_void_p(0), C.c_int64(0)
+        (N, V), k = logits.shape, teacher_ids.shape[1]
+        q, ld_out = None, 0
         if dlogits is not None:
             q, dtype_out, ld_out = _rows(dlogits)
             assert dlogits.shape == logits.shape and dtype_out == dtype
-        k = teacher_ids.shape[1]
-        _check(teacher_ids, torch.int32, N, k); _check(teacher_logits, torch.float32, N, k)
-        _check(loss, torch.float32, N); _check(weight, torch.float32, N)
-        self._ck(lib().gram_distill(self._h, p, C.c_int(dtype), ld, C.c_int64(N), C.c_int32(V), C.c_float(scale), _ptr(teacher_ids),
-                                    _ptr(teacher_logits), C.c_int32(k), _ptr(loss), _ptr(weight), q, ld_out, _stream(stream)))
+        self._ck(lib().gram_distill(self._h, p, dtype, ld, N, V, scale, _array(teacher_ids, "i", N * k), _array(teacher_logits, "f", N * k), k,
+                                    _array(loss, "f", N), _array(weight, "f", N), q, ld_out, _raw_stream(stream)))
 
     def score_logprobs(self, users, items, bias=None, scale=1.0, targets=None, logp=None, stats=None, entropy=None, top_logp=None,
                        top_ids=None, stream=None):
-        import torch
         p, dtype, ld = _rows(users)
         q, dtype_items, ld_items = _rows(items)
         assert dtype == GRAM_BF16 and dtype_items == GRAM_BF16 and users.shape[1] == items.shape[1]
-        (N, d), V = users.shape, items.shape[0]
-        _check(bias, torch.float32, V)
-        self._ck(lib().gram_score_logprobs(self._h, p, ld, q, ld_items, _ptr(bias), C.c_int64(N), C.c_int32(V), C.c_int32(d),
-                                           C.c_float(scale), *self._answers(N, targets, logp, stats, entropy, top_logp, top_ids),
-                                           _stream(stream)))
+        (N, d), V, nc, k = users.shape, items.shape[0], _width(targets), _width(top_ids)
+        self._ck(lib().gram_score_logprobs(self._h, p, ld, q, ld_items, _array(bias, "f", V), N, V, d, scale, _array(targets, "i", N * nc), nc,
+                                           _array(logp, "f", N * nc), _array(stats, "f", N * 2), _array(entropy, "f", N),
+                                           _array(top_logp, "f", N * k), _array(top_ids, "i", N * k), k, _raw_stream(stream)))
 
     def encoder_backward(self, G, items, U, stream=None):
         self._ck(lib().gram_encoder_backward(self._h, _ptr(G), _ptr(items), C.c_int32(U), _stream(stream)))

@@ -551,6 +551,8 @@ gram_status gram_score_logprobs(gram_ctx* ctx, const void* d_users, int64_t ld_u
   ROWS_ARG(d >= 1 && ld_users >= d && ld_items >= d, "rows must be at least d elements apart, d positive");
   ROWS_ARG(ld_items <= INT64_MAX / 8 / V && ld_users <= INT64_MAX / 8 / (N > 0 ? N : 1), "rows too far apart");
   ROWS_ARG(N == 0 || (d_users && d_items), "null vectors");
+  if (N == 1) ld_users = (ld_users + 7) / 8 * 8;        // of a single row the distance means nothing
+  if (V == 1) ld_items = (ld_items + 7) / 8 * 8;
   if (ld_users % 8 || ld_items % 8 || reinterpret_cast<uintptr_t>(d_users) % 16 || reinterpret_cast<uintptr_t>(d_items) % 16)
     return gram_set_error(ctx, "%s: vectors must be 16-byte aligned, rows a multiple of 8 elements apart", name), GRAM_ERR_UNSUPPORTED;
   if (N == 0) return GRAM_OK;

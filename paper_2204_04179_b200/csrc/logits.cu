@@ -2,7 +2,7 @@
 //
 // All three are bound by the bytes of the logits: each is read from HBM once, and a gradient is written once.  A row belongs
 // to a group of threads, a warp for short rows (four rows a block) or a block of 128, and where a row is long or rows are
-// few, to a cluster of up to 16 blocks with a contiguous slice each, whose statistics meet in distributed shared memory.
+// few, to a cluster of up to 8 blocks with a contiguous slice each, whose statistics meet in distributed shared memory.
 // Rows begin anywhere (a stride of 30 522 bf16 leaves them on 4-byte boundaries): the places up to the first 16-byte
 // boundary and after the last are single elements of the slice's first threads, all others move 16 bytes at a time, four
 // vectors a thread and chunk, the next chunk's on their way while one is added up.
@@ -12,14 +12,7 @@
 
 namespace {
 
-#ifndef LP_NV
-#define LP_NV 4
-#endif
-#ifndef LP_B
-#define LP_B 8
-#define LP_BT 8
-#define LP_BG 8
-#endif
+constexpr int LP_NV = 4, LP_PER_SM = 8;                           // vectors of a thread's chunk; blocks that an SM holds
 constexpr int LP_THREADS = 128, LP_WARPS = LP_THREADS / 32;      // of a block
 
 // ------------------------------ a slice of a row ----------------------------------------------------------------------
@@ -92,7 +85,7 @@ __device__ __forceinline__ void put_stat(RowStat* p, uint32_t rank, const RowSta
 __device__ __forceinline__ void put_key(uint64_t* p, uint32_t rank, uint64_t key) {
   asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(in_block(p, rank)), "l"(key) : "memory");
 }
-constexpr int MAX_SLICES = 16;
+constexpr int MAX_SLICES = 8;
 // the slices' statistics, joined in the same order everywhere
 __device__ __forceinline__ RowStat join_slices(const RowStat* of, int slices, float c) {
   const int i = threadIdx.x & (MAX_SLICES - 1);
@@ -124,7 +117,7 @@ template <typename T, int TPR> __device__ __forceinline__ RowLogs row_logs(const
 
 // ------------------------------ log probabilities ---------------------------------------------------------------------
 template <typename T, int TPR, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS, TOP ? LP_BT : LP_B) logprobs_kernel(const T* logits, int64_t ld, int64_t N, int32_t V, float scale, int32_t shift,
+__global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) logprobs_kernel(const T* logits, int64_t ld, int64_t N, int32_t V, float scale, int32_t shift,
                                                                  RowAnswers ask, int32_t* status) {
   using G = Group<TPR>;
   constexpr int NV = LP_NV;
@@ -339,7 +332,7 @@ struct PlacesShared {
 // dense part is 2^l (A + B l), A = -scale (G + h H), B = -scale h ln 2, or in y = l + log2 s, which takes one rounding less per
 // element, 2^y (A - B log2 s + B y) / s; y is held at -200 as in row_softmax.cuh.
 template <typename T, int TPR>
-__global__ void __launch_bounds__(LP_THREADS, LP_BG) logprobs_backward_kernel(const T* logits, T* dlogits, BackwardArgs a) {
+__global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) logprobs_backward_kernel(const T* logits, T* dlogits, BackwardArgs a) {
   using G = Group<TPR>;
   using At = AtPlaces<TPR>;
   constexpr int NV = LP_NV;
@@ -419,7 +412,7 @@ struct DistillArgs {
 // A slice is walked over twice: forwards for the statistics, backwards for the gradient, whose reads find it in L2 (the last
 // chunk is still in registers).  The plan keeps the slices of the blocks that run together well below L2's size.
 template <typename T, int TPR>
-__global__ void __launch_bounds__(LP_THREADS, LP_BG) distill_kernel(const T* logits, T* dlogits, DistillArgs a) {
+__global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) distill_kernel(const T* logits, T* dlogits, DistillArgs a) {
   using G = Group<TPR>;
   using At = AtPlaces<TPR>;
   constexpr int NV = LP_NV;
@@ -534,7 +527,6 @@ struct RowPlan {
   bool warps;
   int shift;                     // 2^shift slices
 };
-constexpr int LP_PER_SM = 8;     // blocks of these kernels that an SM holds
 RowPlan row_plan(gram_ctx* ctx, int64_t N, int64_t row_bytes, int64_t most_bytes, int k = 0) {
   RowPlan p{row_bytes <= 4096 && N >= 4 * kNumSMs && k <= 32, 0};
   if (p.warps) return p;
@@ -548,7 +540,6 @@ template <typename... P, typename... A>
 gram_status launch_rows(gram_ctx* ctx, void (*kern)(P...), const RowPlan& plan, int64_t N, size_t smem, cudaStream_t st, A... args) {
   const int64_t blocks = plan.warps ? ceil_div64(N, LP_WARPS) : N << plan.shift;
   if (blocks > INT32_MAX) return gram_set_error(ctx, "%lld rows of %d slices", (long long)N, 1 << plan.shift), GRAM_ERR_UNSUPPORTED;
-  if (plan.shift > 3) GRAM_CUDA(ctx, cudaFuncSetAttribute(reinterpret_cast<const void*>(kern), cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks);
   cfg.blockDim = dim3(LP_THREADS);

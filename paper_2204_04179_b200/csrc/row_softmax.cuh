@@ -35,14 +35,14 @@ __device__ __forceinline__ void row_raise(RowStat& r, float m, float c) {
   r.s *= f;
   r.m = m;
 }
-// A thread's own sums while it reads.  Their reference lags behind m: it is raised when an entry lies 2^24 above it, so that
-// most chunks leave it alone.
+// A thread's own sums while it reads.  Their reference lags behind m: it is raised when an entry lies 2^4 above it, so that
+// most chunks leave it alone (further behind, the entropy's two parts would grow large against their difference).
 struct RowSums {
   float m, ref, s, t;
   __device__ __forceinline__ RowSums() : m(ROW_NEG_INF), ref(-8388608.f), s(0.f), t(0.f) {}
   __device__ __forceinline__ void see(float top, float c) {            // before entries of at most `top` are added
     m = fmaxf(m, top);
-    if (fmaf(top, c, -ref) > 24.f) {
+    if (fmaf(top, c, -ref) > 4.f) {
       const float up = row_ref(top, c), d = fmaxf(ref - up, -200.f), f = row_ex2(d);
       t = f * fmaf(s, d, t);
       s *= f;
@@ -191,6 +191,13 @@ __device__ __forceinline__ f32x2 x2_fma(f32x2 a, f32x2 b, f32x2 c) {
   return r;
 }
 
+// a pair held above -inf (NaN stays): c z is then finite, and e y of a masked place 0
+__device__ __forceinline__ f32x2 row_held(float a, float b) {
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(-1e30f));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(b) : "f"(-1e30f));
+  return x2_pack(a, b);
+}
+
 template <typename T> struct RowVec;                 // 16 bytes of logits
 template <> struct RowVec<float> {
   static constexpr int N = 4;
@@ -201,12 +208,9 @@ template <> struct RowVec<float> {
   static __device__ __forceinline__ float2 pair(const uint4& q, int i) {
     return i == 0 ? make_float2(__uint_as_float(q.x), __uint_as_float(q.y)) : make_float2(__uint_as_float(q.z), __uint_as_float(q.w));
   }
-  // the pair held above -inf (NaN stays): c z is then finite, and e y of a masked place 0
   static __device__ __forceinline__ f32x2 held(const uint4& q, int i) {
-    float2 x = pair(q, i);
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-1e30f));
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-1e30f));
-    return x2_pack(x.x, x.y);
+    const float2 x = pair(q, i);
+    return row_held(x.x, x.y);
   }
   static __device__ __forceinline__ void put(uint4& q, int i, float2 v) {
     if (i == 0) { q.x = __float_as_uint(v.x); q.y = __float_as_uint(v.y); }
@@ -241,7 +245,7 @@ template <> struct RowVec<bf16> {
 template <typename T, int NV>
 __device__ __forceinline__ void row_add_vectors(RowSums& r, const uint4 (&q)[NV], float top, float c) {
   r.see(top, c);
-  f32x2 s = x2_pack(r.s, 0.f), t = x2_pack(r.t, 0.f);
+  f32x2 s = x2_pack(0.f, 0.f), t = s;                    // sums of their own: small terms would be lost in the row's so far
   const f32x2 cc = x2_pack(c, c), ref = x2_pack(-r.ref, -r.ref);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -255,6 +259,6 @@ __device__ __forceinline__ void row_add_vectors(RowSums& r, const uint4 (&q)[NV]
     }
   }
   const float2 s2 = x2_unpack(s), t2 = x2_unpack(t);
-  r.s = s2.x + s2.y;
-  r.t = t2.x + t2.y;
+  r.s += s2.x + s2.y;
+  r.t += t2.x + t2.y;
 }

@@ -54,6 +54,50 @@ __device__ __forceinline__ float warp_cut(uint64_t* keys, int have, int k) {
 }
 
 
+// of up to 512 keys (k at least) a warp keeps the best k or a few more, in no order; returns how many
+__device__ __forceinline__ int warp_keep(uint64_t* keys, int have, int k) {
+  const int lane = threadIdx.x & 31;
+  uint64_t key[16];
+  uint32_t lo = ~0u, hi = 0u;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    key[i] = 0;
+    if (i * 32 < have && i * 32 + lane < have) {
+      key[i] = keys[i * 32 + lane];
+      lo = min(lo, (uint32_t)(key[i] >> 32));
+      hi = max(hi, (uint32_t)(key[i] >> 32));
+    }
+  }
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  uint64_t a = (uint64_t)lo << 32, b = (uint64_t)hi << 32 | 0xffffffffu;
+  int left = have;
+  while (a < b && left > k + 16) {
+    const uint64_t mid = b - (b - a) / 2;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (i * 32 < have) n += key[i] >= mid;
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (n < k) b = mid - 1;
+    else {
+      a = mid;
+      left = n;
+    }
+  }
+  int at = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (i * 32 < have) {
+      const bool keep = key[i] >= a && key[i] != 0;
+      const uint32_t who = __ballot_sync(0xffffffffu, keep);
+      if (keep) keys[at + __popc(who & ((1u << lane) - 1u))] = key[i];
+      at += __popc(who);
+    }
+  __syncwarp();
+  return at;
+}
+
 template <int TPR> struct alignas(16) TopScratch {
   static constexpr int GROUPS = TPR == 32 ? 4 : 32;     // of a thread
   static constexpr int KEYS = TPR == 32 ? 384 : 1024, ENTRIES = TPR == 32 ? 128 : 512;

@@ -29,7 +29,7 @@ constexpr int SC_BIAS_BYTES = SC_EPI_WARPS * 128 * 4;   // a warp's 128 columns
 constexpr int SC_SMEM = SC_STAGES * SC_STAGE + SC_BIAS_BYTES + 1024 + 256;
 constexpr int SC_LIST_MAX = 256;                        // most entries of a thread's list
 constexpr int SC_PAIR_THREADS = 2 * SC_ROWS;            // epilogue threads of a pair, one for each user and half
-constexpr int SJ_LIST = 1024, SJ_THREADS = 256, SJ_WARPS = SJ_THREADS / 32;
+constexpr int SJ_THREADS = 256, SJ_WARPS = SJ_THREADS / 32;
 constexpr int SB_ROWS = 8, SB_GROUPS = 1024;            // score_bar_kernel: rows of a block, most groups of a row
 
 enum ScoreMode { STATISTICS = 0, LISTS = 1, SAMPLE = 2 };   // LISTS: statistics too
@@ -39,6 +39,7 @@ struct ScoreArgs {
   int64_t N;
   int32_t V, num_kb, k, cap;     // V: items of this pass; cap: entries that a list holds
   int32_t units, total, per_run; // units of a row tile, of all, of a pair's run
+  int32_t box_rows;              // users of a copy
   float c;
   const float* bars;             // [N]
   uint64_t* lists;               // [pair, half, row of the tile, cap]
@@ -76,45 +77,65 @@ struct ScoreRun {
 // a list cut to its best k by the whole warp; returns (in every lane) the bar that better logits reach
 __device__ __noinline__ float score_cut(uint64_t* list, int have, int k) { return warp_cut(list, have, k); }
 
-// x[32]: a block of 32 columns of this thread's row, with the bias (b: the warp's 32 values in shared memory; null: none)
-__device__ __forceinline__ void score_block(uint32_t taddr, const float* b, float (&x)[32]) {
-  uint32_t v[32];
-  tc_ld32_issue(taddr, v);
-  tc_ld32_wait(v);
+// a block of 32 columns of this thread's row as it left tensor memory, plus the bias (the warp's 32 values in shared memory)
+__device__ __forceinline__ void score_bias(uint32_t (&v)[32], const float* b) {
 #pragma unroll
-  for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(v[j]);
-  if (b) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float4 f = reinterpret_cast<const float4*>(b)[j];
-      x[4 * j] += f.x; x[4 * j + 1] += f.y; x[4 * j + 2] += f.z; x[4 * j + 3] += f.w;
-    }
+  for (int j = 0; j < 8; ++j) {
+    const float4 f = reinterpret_cast<const float4*>(b)[j];
+    v[4 * j] = __float_as_uint(__uint_as_float(v[4 * j]) + f.x);
+    v[4 * j + 1] = __float_as_uint(__uint_as_float(v[4 * j + 1]) + f.y);
+    v[4 * j + 2] = __float_as_uint(__uint_as_float(v[4 * j + 2]) + f.z);
+    v[4 * j + 3] = __float_as_uint(__uint_as_float(v[4 * j + 3]) + f.w);
   }
 }
 // the maxima of its four groups of 8 columns
-__device__ __forceinline__ float4 score_tops(const float (&x)[32]) {
-  float t[4];
+__device__ __forceinline__ void score_tops(const uint32_t (&v)[32], float (&t)[4]) {
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
-    const float* y = x + 8 * g;
-    t[g] = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
+    float x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(v[8 * g + j]);
+    t[g] = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
   }
-  return make_float4(t[0], t[1], t[2], t[3]);
 }
-__device__ __forceinline__ void score_add(RowSums& r, const float (&x)[32], float top, float c) {
+__device__ __forceinline__ void score_add(RowSums& r, const uint32_t (&v)[32], float top, float c) {
   r.see(top, c);
-  float s1 = 0.f, t1 = 0.f;
+  f32x2 s = x2_pack(0.f, 0.f), t = s;                    // sums of their own: small terms would be lost in the row's so far
+  const f32x2 cc = x2_pack(c, c), ref = x2_pack(-r.ref, -r.ref);
 #pragma unroll
   for (int j = 0; j < 32; j += 2) {
-    const float y0 = fmaf(x[j], c, -r.ref), y1 = fmaf(x[j + 1], c, -r.ref), e0 = row_ex2(y0), e1 = row_ex2(y1);
-    r.s += e0;
-    s1 += e1;
-    r.t = fmaf(e0, fmaxf(y0, -200.f), r.t);
-    t1 = fmaf(e1, fmaxf(y1, -200.f), t1);
+    const f32x2 y = x2_fma(row_held(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), cc, ref);
+    const float2 y2 = x2_unpack(y);
+    const f32x2 e = x2_pack(row_ex2(y2.x), row_ex2(y2.y));
+    s = x2_add(s, e);
+    t = x2_fma(e, y, t);
   }
-  r.s += s1;
-  r.t += t1;
+  const float2 s2 = x2_unpack(s), t2 = x2_unpack(t);
+  r.s += s2.x + s2.y;
+  r.t += t2.x + t2.y;
 }
+// The entries of a block that reach the bar, to the thread's list: a bit for each of a group of 8, then one entry of each lane at a time.
+__device__ __forceinline__ void score_list(const uint32_t (&v)[32], const float (&t)[4], float bar, uint32_t col, uint64_t* list, int& have) {
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    if (!__any_sync(0xffffffffu, t[g] >= bar)) continue;
+    uint32_t bits = 0u;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (__uint_as_float(v[8 * g + j]) >= bar) bits |= 1u << j;
+    while (__any_sync(0xffffffffu, bits != 0u)) {
+      if (bits) {
+        const int j = __ffs(bits) - 1;
+        bits &= bits - 1u;
+        const uint32_t a = j & 1 ? v[8 * g + 1] : v[8 * g], b = j & 1 ? v[8 * g + 3] : v[8 * g + 2];
+        const uint32_t c = j & 1 ? v[8 * g + 5] : v[8 * g + 4], d = j & 1 ? v[8 * g + 7] : v[8 * g + 6];
+        const uint32_t ab = j & 2 ? b : a, cd = j & 2 ? d : c;
+        list[have++] = row_key(__uint_as_float(j & 4 ? cd : ab), col + 8 * g + j);
+      }
+    }
+  }
+}
+
 template <int MODE>
 __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_constant__ CUtensorMap users, const __grid_constant__ CUtensorMap items,
                                                               const __grid_constant__ ScoreArgs a) {
@@ -165,14 +186,16 @@ __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_const
     while (!failed && run.next()) {
       const int m0 = run.tm * SC_ROWS + (int)rank * SM_ROWS;
       const int n0 = run.unit * SC_UNIT + (int)rank * (run.width * SC_UNIT / 2);     // this block's half of the items: boxes of 64
-      const uint32_t bytes = SC_A_BYTES + (uint32_t)run.width * (SC_UNIT / 2 * SC_BK * 2);
+      // a block whose users are all past the last fetches none; what its rows of the product hold is not looked at
+      const bool some = m0 < a.N;
+      const uint32_t bytes = (some ? (uint32_t)a.box_rows * (SC_BK * 2) : 0u) + (uint32_t)run.width * (SC_UNIT / 2 * SC_BK * 2);
       for (int kb = 0; kb < a.num_kb; ++kb) {
         if (!mbar_wait_warp(empty_bar(s), ph ^ 1u, abort_flag)) { failed = true; break; }
         const uint32_t lead_full = lead_bar0 + 8u * s;
         const uint32_t sa = tiles + s * SC_STAGE, sb = sa + SC_A_BYTES;
         if (elect_one()) {
           mbar_arrive_expect_tx_remote(lead_full, bytes);
-          tma_load_2d_pair(sa, &users, kb * SC_BK, m0, lead_full);
+          if (some) tma_load_2d_pair(sa, &users, kb * SC_BK, m0, lead_full);
           tma_load_2d_pair(sb, &items, kb * SC_BK, n0, lead_full);
           if (run.width == 2) tma_load_2d_pair(sb + 8192, &items, kb * SC_BK, n0 + 64, lead_full);
         }
@@ -245,32 +268,23 @@ __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_const
         if (MODE != SAMPLE && run.first) {
           sums = RowSums();
           have = 0;
-          if (MODE == LISTS) bar = n < a.N ? a.bars[n] : -ROW_NEG_INF;
+          if (MODE == LISTS) bar = n < a.N ? a.bars[n] : __int_as_float(0x7fffffff);     // nothing reaches a NaN
         }
-        for (int b = 0; b < blocks; ++b) {
-          float x[32];
-          score_block(taddr + b * 32, bias ? bias + b * 32 : nullptr, x);
-          const float4 tops = score_tops(x);
-          const float top = fmaxf(fmaxf(tops.x, tops.y), fmaxf(tops.z, tops.w));
+        auto block = [&](uint32_t (&v)[32], int b) {
+          if (bias) score_bias(v, bias + b * 32);
+          float t[4];
+          score_tops(v, t);
+          const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
           if constexpr (MODE == SAMPLE) {
             const int64_t at = (int64_t)((col0 + b * 32) / 32) * a.sample_rows + n;
-            if (a.fine) reinterpret_cast<float4*>(a.sample)[at] = tops;
+            if (a.fine) reinterpret_cast<float4*>(a.sample)[at] = make_float4(t[0], t[1], t[2], t[3]);
             else a.sample[at] = top;
-            continue;
+          } else {
+            score_add(sums, v, top, a.c);
           }
-          score_add(sums, x, top, a.c);
           if constexpr (MODE == LISTS) {
             if (__any_sync(0xffffffffu, top >= bar)) {
-              const float t[4] = {tops.x, tops.y, tops.z, tops.w};
-#pragma unroll
-              for (int g = 0; g < 4; ++g) {
-                if (!__any_sync(0xffffffffu, t[g] >= bar)) continue;
-#pragma unroll
-                for (int j = 8 * g; j < 8 * g + 8; ++j) {
-                  if (!__any_sync(0xffffffffu, x[j] >= bar)) continue;
-                  if (x[j] >= bar) list[have++] = row_key(x[j], (uint32_t)(col0 + b * 32 + j));
-                }
-              }
+              score_list(v, t, bar, (uint32_t)(col0 + b * 32), list, have);
               uint32_t full = __ballot_sync(0xffffffffu, have > a.cap - 32);
               __syncwarp();
               while (full) {                                      // more entries reach the bar than a list holds: its best k stay
@@ -281,6 +295,15 @@ __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_const
               }
             }
           }
+        };
+        for (int b = 0; b < blocks; b += 2) {                     // 2 or 4 blocks
+          uint32_t v0[32], v1[32];
+          tc_ld32_issue(taddr + b * 32, v0);
+          tc_ld32_issue(taddr + (b + 1) * 32, v1);
+          tc_ld32_wait(v0);
+          tc_ld32_wait(v1);
+          block(v0, b);
+          block(v1, b + 1);
         }
       }
       tc_fence_before();
@@ -348,25 +371,28 @@ __global__ void __launch_bounds__(32 * SB_ROWS) score_bar_kernel(const float* sa
   __syncthreads();
   const int lane = threadIdx.x & 31, r = threadIdx.x >> 5;
   if (n0 + r >= N) return;
-  uint32_t lo = ~0u, hi = 0u;
+  uint32_t o[SB_GROUPS / 32], lo = ~0u, hi = 0u;
   int some = 0;
-  for (int i = lane; i < groups; i += 32)
-    if (value[r][i] > ROW_NEG_INF) {
-      const uint32_t o = row_order(value[r][i]);
-      lo = min(lo, o);
-      hi = max(hi, o);
-      ++some;
-    }
+#pragma unroll
+  for (int i = 0; i < SB_GROUPS / 32; ++i) {
+    const float x = i * 32 + lane < groups ? value[r][i * 32 + lane] : ROW_NEG_INF;
+    o[i] = x > ROW_NEG_INF ? row_order(x) : 0u;
+    if (o[i]) lo = min(lo, o[i]);
+    hi = max(hi, o[i]);
+    some += o[i] != 0u;
+  }
+  // k of 32 lanes' maxima are above the least of them
+  const uint32_t lane_hi = hi;
   lo = __reduce_min_sync(0xffffffffu, lo);
+  if (k <= 32) lo = max(lo, __reduce_min_sync(0xffffffffu, lane_hi));
   hi = __reduce_max_sync(0xffffffffu, hi);
   float bar = -FLT_MAX;
   if ((int)__reduce_add_sync(0xffffffffu, some) >= k) {
     for (int step = 0; lo < hi && step < 16; ++step) {
       const uint32_t mid = hi - (hi - lo) / 2;
-      const float f = row_order_logit(mid);
       int n = 0;
-#pragma unroll 4
-      for (int i = lane; i < groups; i += 32) n += value[r][i] >= f;
+#pragma unroll
+      for (int i = 0; i < SB_GROUPS / 32; ++i) n += o[i] >= mid;
       n = __reduce_add_sync(0xffffffffu, n);
       if (n < k) hi = mid - 1;
       else {
@@ -398,51 +424,81 @@ __device__ __forceinline__ float score_dot(const bf16* u, const bf16* w, int d) 
   return sum;
 }
 
-// One block a user: joins the statistics of the runs that crossed its row tile, and their lists.
+// Joins the statistics of the runs that crossed a user's row tile, and their lists.  A warp takes a user, eight users a block; where
+// users are few a block takes one (ALONE): its warps share the given tokens and the reading of the lists.
+constexpr int SJ_PARTS = kNumSMs + 2, SJ_KEYS = 512;    // parts of a user at most; keys that are sorted out in shared memory
+template <bool ALONE>
 __global__ void __launch_bounds__(SJ_THREADS) score_join_kernel(const ScoreArgs a, const bf16* users, int64_t ld_u, const bf16* items, int64_t ld_i,
                                                                 int32_t d, float scale, RowAnswers ask) {
-  using G = Group<SJ_THREADS>;
   if (!chain_begin()) return;
-  __shared__ uint64_t keys[SJ_LIST];
-  __shared__ int ipart[SJ_WARPS], wpart[SJ_WARPS], listed;
-  __shared__ RowStat part[SJ_WARPS];
-  __shared__ float fpart[SJ_WARPS];
-  __shared__ int have_of[SJ_THREADS];
-  const int64_t n = blockIdx.x;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  __shared__ __align__(16) uint64_t keys_of[ALONE ? 1 : SJ_WARPS][SJ_KEYS];
+  __shared__ int starts_of[ALONE ? 1 : SJ_WARPS][SJ_PARTS + 1];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t n = ALONE ? blockIdx.x : (int64_t)blockIdx.x * SJ_WARPS + warp;
+  if (n >= a.N) return;                                 // whole warps; the block's barriers are in the other form only
+  uint64_t* keys = keys_of[ALONE ? 0 : warp];
+  int* starts = starts_of[ALONE ? 0 : warp];            // of each part's list among all of the user's keys
   const int tm = (int)(n / SC_ROWS), row = (int)(n % SC_ROWS);
-  const int p0 = tm * a.units / a.per_run, p1 = ((tm + 1) * a.units - 1) / a.per_run, parts = (p1 - p0 + 1) * 2;     // at most 150
-  // of part i: pair p0 + i / 2, half i % 2
-  auto is_early = [&](int p) { return (min((p + 1) * a.per_run, a.total) - 1) / a.units != tm; };
+  const int p0 = tm * a.units / a.per_run, p1 = ((tm + 1) * a.units - 1) / a.per_run, parts = (p1 - p0 + 1) * 2;
   RowStat r = row_empty();
-  int have = 0;
-  if (tid < parts) {
-    const int p = p0 + tid / 2;
-    const float4 f = a.stats[((int64_t)(p * 2 + tm - p * a.per_run / a.units) * 2 + (tid & 1)) * SC_ROWS + row];
-    r = RowStat{f.x, f.y, f.z};
-    have = __float_as_int(f.w);
-    have_of[tid] = have;
+  int all = 0;
+  for (int i0 = 0; i0 < parts; i0 += 32) {              // part i: pair p0 + i / 2, half i % 2; every warp of a block does the same
+    const int i = i0 + lane, p = p0 + i / 2;
+    int have = 0;
+    if (i < parts) {
+      const float4 f = a.stats[((int64_t)(p * 2 + tm - p * a.per_run / a.units) * 2 + (i & 1)) * SC_ROWS + row];
+      have = __float_as_int(f.w);
+      RowStat x{f.x, f.y, f.z};
+      const float m = fmaxf(r.m, x.m);
+      if (m > r.m) row_raise(r, m, a.c);
+      if (m > x.m) row_raise(x, m, a.c);
+      r.s += x.s;
+      r.t += x.t;
+    }
+    int before = have;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, before, o);
+      if (lane >= o) before += x;
+    }
+    if (i < parts) starts[i] = all + before - have;
+    all += __shfl_sync(0xffffffffu, before, 31);
   }
-  r = G::join(r, a.c, part);
+  if (lane == 0) starts[parts] = all;
+  r = row_join_lanes<32>(r, a.c);
+  if (ALONE) __syncthreads();                           // (the warps have written the same starts)
+  else __syncwarp();
+  const int k = ask.k;
+  auto key_at = [&](int idx) {
+    int lo = 0, hi = parts - 1;                         // the last part that starts at or before idx
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (starts[mid] <= idx) lo = mid;
+      else hi = mid - 1;
+    }
+    const int p = p0 + lo / 2;
+    const bool early = (min((p + 1) * a.per_run, a.total) - 1) / a.units != tm;
+    const uint64_t* l = early ? a.early + ((int64_t)(tm * 2 + (lo & 1)) * SC_ROWS + row) * a.early_cap
+                              : a.lists + ((int64_t)(p * 2 + (lo & 1)) * SC_ROWS + row) * a.cap;
+    return l[idx - starts[lo]];
+  };
+  if (k > 0 && all <= SJ_KEYS) {
+#pragma unroll 4
+    for (int i = ALONE ? (int)threadIdx.x : lane; i < all; i += ALONE ? SJ_THREADS : 32) keys[i] = key_at(i);
+  }
   float log_s = row_log_sum(r, a.c), entropy = row_entropy(r);
   if (row_is_huge(r.m, a.c)) {                          // summed again, relative to m itself
     float s = 0.f, t = 0.f;
-    for (int v = warp; v < a.V; v += SJ_WARPS) {
+    for (int v = 0; v < a.V; ++v) {
       const float z = score_dot(users + n * ld_u, items + (int64_t)v * ld_i, d) + (a.bias ? a.bias[v] : 0.f);
       const float y = (z - r.m) * a.c, e = row_ex2(y);
       s += e;
       t = fmaf(e, fmaxf(y, -200.f), t);
     }
-    s = G::sum(lane == 0 ? s : 0.f, fpart);
-    t = G::sum(lane == 0 ? t : 0.f, fpart);
     log_s = logf(s);
     entropy = log_s - kLn2 * (t / s);
   }
-  if (tid == 0) {
-    if (ask.stats) { ask.stats[2 * n] = r.m; ask.stats[2 * n + 1] = log_s; }
-    if (ask.entropy) ask.entropy[n] = entropy;
-  }
-  for (int i = warp; i < ask.C; i += SJ_WARPS) {
+  for (int i = ALONE ? warp : 0; i < ask.C; i += ALONE ? SJ_WARPS : 1) {
     const int32_t t = ask.targets[n * ask.C + i];
     float lp = 0.f;
     if (t >= 0 && t < a.V) {
@@ -454,76 +510,46 @@ __global__ void __launch_bounds__(SJ_THREADS) score_join_kernel(const ScoreArgs 
     }
     if (lane == 0) ask.logp[n * ask.C + i] = lp;
   }
-  if (ask.k == 0) return;
-  const int k = ask.k;
-  // f(key) for each key of this thread's share: the lists as rows of a table as wide as the longest, eight loads at once
-  const int wide = (int)__reduce_max_sync(0xffffffffu, have);
-  if (lane == 0) wpart[warp] = wide;
-  __syncthreads();                                      // of have_of, too
-  int width = 0;
-#pragma unroll
-  for (int w = 0; w < SJ_WARPS; ++w) width = max(width, wpart[w]);
-  auto each = [&](auto f) {
-    const int cells = parts * width;
-    for (int c0 = tid; c0 < cells; c0 += 8 * SJ_THREADS) {
-      uint64_t key[8];
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int cell = c0 + u * SJ_THREADS;
-        key[u] = 0;
-        if (cell < cells) {
-          const int i = cell / width, j = cell - i * width, p = p0 + i / 2;
-          if (j < have_of[i]) {
-            const uint64_t* l = is_early(p) ? a.early + ((int64_t)(tm * 2 + (i & 1)) * SC_ROWS + row) * a.early_cap
-                                            : a.lists + ((int64_t)(p * 2 + (i & 1)) * SC_ROWS + row) * a.cap;
-            key[u] = l[j];
-          }
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < 8; ++u)
-        if (key[u]) f(key[u]);
-    }
-  };
-  const int all = G::sum(have, ipart);
-  uint64_t least = 1;
-  if (all > SJ_LIST) {
-    uint64_t best = 0;
-    each([&](uint64_t key) { best = max(best, key); });
-    if (G::count(best != 0) >= k) least = kth_key(k, [&](uint64_t t) { return G::count(best >= t); });
-    int c = 0;
-    each([&](uint64_t key) { c += key >= least; });
-    if (G::sum(c, ipart) > SJ_LIST)          // many equal or clustered logits: the k-th key itself
-      least = kth_key(k, [&](uint64_t t) {
-        int m = 0;
-        each([&](uint64_t key) { m += key >= t; });
-        return G::sum(m, ipart);
-      }, least);
+  if (ALONE) __syncthreads();
+  else __syncwarp();
+  if (ALONE && warp != 0) return;
+  if (lane == 0) {
+    if (ask.stats) { ask.stats[2 * n] = r.m; ask.stats[2 * n + 1] = log_s; }
+    if (ask.entropy) ask.entropy[n] = entropy;
   }
-  if (tid == 0) listed = 0;
-  G::sync();
-  each([&](uint64_t key) {
-    if (key >= least) keys[atomicAdd(&listed, 1)] = key;
-  });
-  G::sync();
-  have = listed;
-  G::sync();
-  if (have > 128 && have > k + k / 4) {
-    if (warp == 0) (void)warp_cut(keys, have, k);
-    have = k;
-    G::sync();
+  if (k == 0) return;
+  int have = all;
+  if (all <= SJ_KEYS) {
+    if (have > k + 16) have = warp_keep(keys, have, k);
+  } else {                                              // many equal or clustered logits: the k-th key by bisection over the lists
+    const uint64_t kth = kth_key(k, [&](uint64_t t) {
+      int c = 0;
+      for (int i = lane; i < all; i += 32) c += key_at(i) >= t;
+      return (int)__reduce_add_sync(0xffffffffu, c);
+    });
+    have = 0;
+    for (int i0 = 0; i0 < all; i0 += 32) {
+      const uint64_t key = i0 + lane < all ? key_at(i0 + lane) : 0;
+      const uint32_t who = __ballot_sync(0xffffffffu, key >= kth);
+      if (key >= kth) keys[have + __popc(who & ((1u << lane) - 1u))] = key;
+      have += __popc(who);
+    }
+    __syncwarp();
+  }
+  if (have & 1) {
+    if (lane == 0) keys[have] = 0;                      // read in pairs
+    __syncwarp();
   }
   const int64_t o = n * k;
-  for (int i = tid; i < have; i += SJ_THREADS) {
+  for (int i = lane; i < have; i += 32) {
     const uint64_t key = keys[i];
-    int above = 0;
-    for (int j = 0; j < have; ++j) above += keys[j] > key;
+    const int above = top_rank(keys, have, key);
     if (above < k) {
       ask.top_ids[o + above] = row_key_place(key);
       ask.top_logp[o + above] = row_logp(row_key_logit(key), r.m, log_s, scale);
     }
   }
-  for (int i = have + tid; i < k; i += SJ_THREADS) {
+  for (int i = have + lane; i < k; i += 32) {
     ask.top_ids[o + i] = -1;
     ask.top_logp[o + i] = ROW_NEG_INF;
   }
@@ -556,12 +582,12 @@ gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_u
                                   size_t ws_bytes, cudaStream_t st) {
   const int32_t all_units = ceil_div(V, SC_UNIT);
   if (all_units > (1 << 30) / (kNumSMs / 2)) return gram_set_error(ctx, "gram_score_logprobs: %d items", V), GRAM_ERR_UNSUPPORTED;
-  // The sample: so many items that about 256 entries of a user reach the bar, but 4096 at least and a quarter of the table at
+  // The sample: so many items that about 256 entries of a user reach the bar, but 4096 at least and a third of the table at
   // most; its maxima by groups of 8 columns, by 32 where that is more than score_bar_kernel holds.
   int32_t sample = 0, fine = 1;
   if (ask.k) {
     int64_t want = (int64_t)ask.k * V / 256;
-    if (want > V / 4) want = V / 4;
+    if (want > V / 3) want = V / 3;
     if (want < 4096) want = 4096;
     if (want > SB_GROUPS * 32) want = SB_GROUPS * 32;
     sample = (int32_t)(want < V ? ceil_div64(want, SC_UNIT) * SC_UNIT : V);
@@ -595,6 +621,10 @@ gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_u
     if (most == 1) return gram_set_error(ctx, "gram_score_logprobs: the workspace is too small for %d alternatives", ask.k), GRAM_ERR_WORKSPACE;
   }
   const size_t early_bytes = ask.k ? (size_t)per_launch * SC_PAIR_THREADS * early_cap * 8 : 0;
+  // few users: the copies' boxes are no larger (rows past the last are filled with zeros, which takes time: one user against
+  // 100 000 items of 768 46 us with boxes of 128 rows)
+  int box_rows = SM_ROWS;
+  while (box_rows > 8 && box_rows / 2 >= N) box_rows /= 2;
   CUtensorMap map_u, map_i;
   if (!make_map(&map_i, items, (uint64_t)d, (uint64_t)V, (uint64_t)ld_items, SC_BK, 64))
     return gram_set_error(ctx, "gram_score_logprobs: cannot describe the items"), GRAM_ERR_UNSUPPORTED;
@@ -602,9 +632,10 @@ gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_u
   for (int64_t n = 0; n < N; n += per_launch * SC_ROWS) {
     const int64_t now = N - n < per_launch * SC_ROWS ? N - n : per_launch * SC_ROWS, now_tiles = ceil_div64(now, SC_ROWS);
     const bf16* u = (const bf16*)users + n * ld_users;
-    if (!make_map(&map_u, u, (uint64_t)d, (uint64_t)now, (uint64_t)ld_users, SC_BK, SM_ROWS))
+    if (!make_map(&map_u, u, (uint64_t)d, (uint64_t)now, (uint64_t)ld_users, SC_BK, (uint32_t)box_rows))
       return gram_set_error(ctx, "gram_score_logprobs: cannot describe the users"), GRAM_ERR_UNSUPPORTED;
     ScoreArgs a = {};
+    a.box_rows = box_rows;
     a.bias = bias;
     a.N = now;
     a.num_kb = ceil_div(d, SC_BK);
@@ -641,7 +672,11 @@ gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_u
     if (ask.k) { part.top_logp += n * ask.k; part.top_ids += n * ask.k; }
     const int used = cut(V, pairs);
     GRAM_CUDA(ctx, ask.k ? launch_score<LISTS>(map_u, map_i, a, used, st) : launch_score<STATISTICS>(map_u, map_i, a, used, st));
-    launch_chain(score_join_kernel, dim3((unsigned)now), SJ_THREADS, 0, st, a, u, ld_users, (const bf16*)items, ld_items, d, scale, part);
+    if (now >= 4 * kNumSMs)
+      launch_chain(score_join_kernel<false>, dim3((unsigned)ceil_div64(now, SJ_WARPS)), SJ_THREADS, 0, st, a, u, ld_users, (const bf16*)items, ld_items,
+                   d, scale, part);
+    else
+      launch_chain(score_join_kernel<true>, dim3((unsigned)now), SJ_THREADS, 0, st, a, u, ld_users, (const bf16*)items, ld_items, d, scale, part);
     GRAM_LAUNCH_CHECK(ctx);
   }
   return GRAM_OK;
