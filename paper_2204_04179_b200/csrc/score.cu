@@ -29,7 +29,6 @@ constexpr int SC_BIAS_BYTES = SC_EPI_WARPS * 128 * 4;   // a warp's 128 columns
 constexpr int SC_SMEM = SC_STAGES * SC_STAGE + SC_BIAS_BYTES + 1024 + 256;
 constexpr int SC_LIST_MAX = 256;                        // most entries of a thread's list
 constexpr int SC_PAIR_THREADS = 2 * SC_ROWS;            // epilogue threads of a pair, one for each user and half
-constexpr int SJ_THREADS = 256, SJ_WARPS = SJ_THREADS / 32;
 constexpr int SB_ROWS = 8, SB_GROUPS = 1024;            // score_bar_kernel: rows of a block, most groups of a row
 
 enum ScoreMode { STATISTICS = 0, LISTS = 1, SAMPLE = 2 };   // LISTS: statistics too
@@ -424,11 +423,13 @@ __device__ __forceinline__ float score_dot(const bf16* u, const bf16* w, int d) 
   return sum;
 }
 
-// Joins the statistics of the runs that crossed a user's row tile, and their lists.  A warp takes a user, eight users a block; where
-// users are few a block takes one (ALONE): its warps share the given tokens and the reading of the lists.
-constexpr int SJ_PARTS = kNumSMs + 2, SJ_KEYS = 512;    // parts of a user at most; keys that are sorted out in shared memory
+// Joins the statistics of the runs that crossed a user's row tile, and their lists.  A warp takes a user, four users a block; where
+// users are few a block takes one (ALONE): its eight warps share the given tokens and the reading of the lists.
+// About 256 keys come in; that so many as 512 do, one user in 200 with 10 alternatives, is met by warp_cut.
+constexpr int SJ_PARTS = kNumSMs + 2, SJ_KEYS = 1024;   // parts of a user at most; keys that are sorted out in shared memory
+constexpr int SJ_WARPS = 4, SJ_ALONE_WARPS = 8;
 template <bool ALONE>
-__global__ void __launch_bounds__(SJ_THREADS) score_join_kernel(const ScoreArgs a, const bf16* users, int64_t ld_u, const bf16* items, int64_t ld_i,
+__global__ void __launch_bounds__(32 * (ALONE ? SJ_ALONE_WARPS : SJ_WARPS)) score_join_kernel(const ScoreArgs a, const bf16* users, int64_t ld_u, const bf16* items, int64_t ld_i,
                                                                 int32_t d, float scale, RowAnswers ask) {
   if (!chain_begin()) return;
   __shared__ __align__(16) uint64_t keys_of[ALONE ? 1 : SJ_WARPS][SJ_KEYS];
@@ -484,7 +485,7 @@ __global__ void __launch_bounds__(SJ_THREADS) score_join_kernel(const ScoreArgs 
   };
   if (k > 0 && all <= SJ_KEYS) {
 #pragma unroll 4
-    for (int i = ALONE ? (int)threadIdx.x : lane; i < all; i += ALONE ? SJ_THREADS : 32) keys[i] = key_at(i);
+    for (int i = ALONE ? (int)threadIdx.x : lane; i < all; i += ALONE ? 32 * SJ_ALONE_WARPS : 32) keys[i] = key_at(i);
   }
   float log_s = row_log_sum(r, a.c), entropy = row_entropy(r);
   if (row_is_huge(r.m, a.c)) {                          // summed again, relative to m itself
@@ -498,7 +499,7 @@ __global__ void __launch_bounds__(SJ_THREADS) score_join_kernel(const ScoreArgs 
     log_s = logf(s);
     entropy = log_s - kLn2 * (t / s);
   }
-  for (int i = ALONE ? warp : 0; i < ask.C; i += ALONE ? SJ_WARPS : 1) {
+  for (int i = ALONE ? warp : 0; i < ask.C; i += ALONE ? SJ_ALONE_WARPS : 1) {
     const int32_t t = ask.targets[n * ask.C + i];
     float lp = 0.f;
     if (t >= 0 && t < a.V) {
@@ -520,7 +521,12 @@ __global__ void __launch_bounds__(SJ_THREADS) score_join_kernel(const ScoreArgs 
   if (k == 0) return;
   int have = all;
   if (all <= SJ_KEYS) {
-    if (have > k + 16) have = warp_keep(keys, have, k);
+    if (have > 512) {
+      (void)warp_cut(keys, have, k);
+      have = k;
+    } else if (have > k + 16) {
+      have = warp_keep(keys, have, k);
+    }
   } else {                                              // many equal or clustered logits: the k-th key by bisection over the lists
     const uint64_t kth = kth_key(k, [&](uint64_t t) {
       int c = 0;
@@ -673,10 +679,10 @@ gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_u
     const int used = cut(V, pairs);
     GRAM_CUDA(ctx, ask.k ? launch_score<LISTS>(map_u, map_i, a, used, st) : launch_score<STATISTICS>(map_u, map_i, a, used, st));
     if (now >= 4 * kNumSMs)
-      launch_chain(score_join_kernel<false>, dim3((unsigned)ceil_div64(now, SJ_WARPS)), SJ_THREADS, 0, st, a, u, ld_users, (const bf16*)items, ld_items,
+      launch_chain(score_join_kernel<false>, dim3((unsigned)ceil_div64(now, SJ_WARPS)), 32 * SJ_WARPS, 0, st, a, u, ld_users, (const bf16*)items, ld_items,
                    d, scale, part);
     else
-      launch_chain(score_join_kernel<true>, dim3((unsigned)now), SJ_THREADS, 0, st, a, u, ld_users, (const bf16*)items, ld_items, d, scale, part);
+      launch_chain(score_join_kernel<true>, dim3((unsigned)now), 32 * SJ_ALONE_WARPS, 0, st, a, u, ld_users, (const bf16*)items, ld_items, d, scale, part);
     GRAM_LAUNCH_CHECK(ctx);
   }
   return GRAM_OK;
