@@ -235,32 +235,41 @@ __global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) logprobs_kernel(const T
 }
 
 // ------------------------------ gradients -----------------------------------------------------------------------------
-template <typename T> __device__ __forceinline__ bool same_alignment(const T* a, const T* b) {
-  return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15) == 0;
+// Rows of the gradient may begin elsewhere within 16 bytes than the logits': a vector is then stored in pieces of the size that
+// its address allows (bytes: 16, 8, 4 or, for bf16, 2; the same for all vectors of a row).
+template <typename T> __device__ __forceinline__ int store_bytes(const T* first) {
+  const uint32_t a = (uint32_t)reinterpret_cast<uintptr_t>(first);
+  return a % 16 == 0 ? 16 : a % 8 == 0 ? 8 : a % 4 == 0 ? 4 : 2;
 }
-template <typename T> __device__ __forceinline__ void store_vector(T* dz, int place, const uint4& q, bool vec) {
-  if (vec) {
-    __stcs(reinterpret_cast<uint4*>(dz + place), q);
+template <typename T> __device__ __forceinline__ void store_vector(T* at, const uint4& q, int bytes) {
+  if (bytes == 16) {
+    __stcs(reinterpret_cast<uint4*>(at), q);
+  } else if (bytes == 8) {
+    __stcs(reinterpret_cast<uint2*>(at), make_uint2(q.x, q.y));
+    __stcs(reinterpret_cast<uint2*>(at) + 1, make_uint2(q.z, q.w));
+  } else if (bytes == 4) {
+    __stcs(reinterpret_cast<uint32_t*>(at), q.x);
+    __stcs(reinterpret_cast<uint32_t*>(at) + 1, q.y);
+    __stcs(reinterpret_cast<uint32_t*>(at) + 2, q.z);
+    __stcs(reinterpret_cast<uint32_t*>(at) + 3, q.w);
   } else {
-    const T* e = reinterpret_cast<const T*>(&q);
+    const uint16_t* e = reinterpret_cast<const uint16_t*>(&q);
 #pragma unroll
-    for (int j = 0; j < RowVec<T>::N; ++j) dz[place + j] = e[j];
+    for (int j = 0; j < 8; ++j) reinterpret_cast<uint16_t*>(at)[j] = e[j];
   }
 }
-// f(logit) -> result, over a chunk that is in registers
+// f(pair of logits) -> pair of results, over a chunk that is in registers
 template <typename T, int TPR, int NV, typename F>
-__device__ __forceinline__ void store_chunk(const Slice<T>& s, int ch, int tid, const uint4 (&q)[NV], T* dz, bool vec, F f) {
+__device__ __forceinline__ void store_chunk(const Slice<T>& s, int ch, int tid, const uint4 (&q)[NV], T* dz, int bytes, F f) {
   const int v = s.v0 + ch * (TPR * NV) + tid;
+  T* at = dz + s.place(v);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     if (v + i * TPR < s.v1) {
       uint4 o;
 #pragma unroll
-      for (int j = 0; j < RowVec<T>::N / 2; ++j) {
-        const float2 x = RowVec<T>::pair(q[i], j);
-        RowVec<T>::put(o, j, make_float2(f(x.x), f(x.y)));
-      }
-      store_vector(dz, s.place(v + i * TPR), o, vec);
+      for (int j = 0; j < RowVec<T>::N / 2; ++j) RowVec<T>::put(o, j, f(RowVec<T>::pair(q[i], j)));
+      store_vector(at + i * (TPR * RowVec<T>::N), o, bytes);
     }
   }
 }
@@ -272,8 +281,8 @@ struct RowPower {
   __device__ __forceinline__ RowPower(float m_, float log_s, float c_) : m(m_), c(c_), ref(row_ref(m_, c_)), is_huge(row_is_huge(m_, c_)) {
     log2_s = log_s * kLog2e + (is_huge ? 0.f : fmaf(m, c, -ref));
   }
-  __device__ __forceinline__ float plain(float x) const { return fmaf(x, c, -ref); }
-  __device__ __forceinline__ float huge(float x) const { return (x - m) * c; }
+  __device__ __forceinline__ float2 plain(float2 x) const { return x2_unpack(x2_fma(x2_pack(x.x, x.y), x2_pack(c, c), x2_pack(-ref, -ref))); }
+  __device__ __forceinline__ float2 huge(float2 x) const { return make_float2((x.x - m) * c, (x.y - m) * c); }
 };
 
 struct BackwardArgs {
@@ -312,19 +321,29 @@ template <int TPR> struct AtPlaces {
     for (int e = 0; e < EPT; ++e) z[e] = id[e] >= 0 ? row_load(row + id[e]) : ROW_NEG_INF;
   }
 };
-// of the entries that take part: the sum of the values at entry i's place, if i is the first entry there
-struct PlacesShared {
-  float value[GRAM_TOP_MAX];
+// The entries that take part, as all threads see them.
+struct alignas(16) PlacesShared {
   int32_t place[GRAM_TOP_MAX];   // -1: takes no part
+  float value[GRAM_TOP_MAX];
+  // whether entry i is the first at its place, and the sum of all values there
   __device__ __forceinline__ bool sum_at(int i, int count, float& sum) const {
-    bool first = true;
+    const int p = place[i];
+    int same = 0, before = 0;
+#pragma unroll 4
+    for (int j = 0; j < count; j += 4) {               // what lies behind `count` is -1
+      const int4 q = *reinterpret_cast<const int4*>(place + j);
+      const int n = (q.x == p) + (q.y == p) + (q.z == p) + (q.w == p);
+      same += n;
+      if (j + 3 < i) before += n;
+    }
+    sum = value[i];
+    if (same == 1) return true;                         // as good as always
+    for (int j = i & ~3; j < i; ++j) before += place[j] == p;
+    if (before > 0) return false;
     sum = 0.f;
-    for (int j = 0; j < count; ++j)
-      if (place[j] == place[i]) {
-        first = first && j >= i;
-        sum += value[j];
-      }
-    return first;
+    for (int j = i; j < count; ++j)
+      if (place[j] == p) sum += value[j];
+    return true;
   }
 };
 
@@ -345,20 +364,20 @@ __global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) logprobs_backward_kerne
   uint4 q[NV], next[NV];
   const Slice<T> s(logits + n * a.ld, a.V, rank, a.shift);
   At at;
-  at.load_ids(a.targets, a.dlogp, n, a.C, a.V, tid, a.status);
   s.template load_chunk<TPR, NV, true>(0, tid, q);
+  at.load_ids(a.targets, a.dlogp, n, a.C, a.V, tid, a.status);
   at.load_logits(s.z);
   PlacesShared& here = places[G::row()];
   const float m = a.stats[2 * n], log_s = a.stats[2 * n + 1], h = a.dentropy ? a.dentropy[n] : 0.f, H = a.dentropy ? a.entropy[n] : 0.f;
   T* dz = dlogits + n * a.ld_out;
-  const bool vec = same_alignment(s.z, dz);
+  const int bytes = store_bytes(dz + s.head);
   const int edge_place = s.edge(tid);
   const float edge = edge_place >= 0 ? row_load(s.z + edge_place) : ROW_NEG_INF;
   float sum = 0.f;
   if (a.C > 0) {
 #pragma unroll
     for (int e = 0; e < At::EPT; ++e)
-      if (tid + e * TPR < a.C) {
+      if (tid + e * TPR < ((a.C + 3) & ~3)) {
         const bool use = at.z[e] != ROW_NEG_INF;      // "none" and masked places take no part
         here.place[tid + e * TPR] = use ? at.id[e] : -1;
         here.value[tid + e * TPR] = use ? at.given[e] : 0.f;
@@ -373,15 +392,24 @@ __global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) logprobs_backward_kerne
   const RowPower l(m, log_s, c);
   const float inv = exp2f(-l.log2_s), Ay = inv * fmaf(-B, l.log2_s, A), By = inv * B;
   auto value = [&](float y) { return row_ex2(y) * fmaf(fmaxf(y, -200.f), By, Ay); };
-  auto dense = [&](float x) { return value(l.plain(x)); };
-  auto dense_huge = [&](float x) { return value(l.huge(x)); };
-  auto one = [&](float x) { return none || x == ROW_NEG_INF ? 0.f : l.is_huge ? dense_huge(x) : dense(x); };
+  auto dense = [&](float2 x) {
+    const float2 y = l.plain(x);
+    return make_float2(value(y.x), value(y.y));
+  };
+  auto dense_huge = [&](float2 x) {
+    const float2 y = l.huge(x);
+    return make_float2(value(y.x), value(y.y));
+  };
+  auto one = [&](float x) {
+    const float2 xx = make_float2(x, x);
+    return none || x == ROW_NEG_INF ? 0.f : l.is_huge ? dense_huge(xx).x : dense(xx).x;
+  };
   const int chunks = s.template chunks<TPR, NV>();
   for (int ch = 0; ch < chunks; ++ch) {
     if (ch + 1 < chunks && !none) s.template load_chunk<TPR, NV, true>(ch + 1, tid, next);
-    if (none) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, [](float) { return 0.f; });
-    else if (l.is_huge) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, dense_huge);
-    else store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, dense);
+    if (none) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, bytes, [](float2) { return make_float2(0.f, 0.f); });
+    else if (l.is_huge) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, bytes, dense_huge);
+    else store_chunk<T, TPR, NV>(s, ch, tid, q, dz, bytes, dense);
 #pragma unroll
     for (int i = 0; i < NV; ++i) q[i] = next[i];
   }
@@ -427,8 +455,8 @@ __global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) distill_kernel(const T*
   uint4 q[NV], next[NV];
   const Slice<T> s(logits + n * a.ld, a.V, rank, a.shift);
   At at;
-  at.load_ids(a.ids, a.teacher, n, a.k, a.V, tid, a.status);
   s.template load_chunk<TPR, NV, false>(0, tid, q);
+  at.load_ids(a.ids, a.teacher, n, a.k, a.V, tid, a.status);
   at.load_logits(s.z);
   if (TPR > 32 && slices > 1) gram_cluster_sync();       // every block of the cluster runs before another writes to it
   PlacesShared& here = places[G::row()];
@@ -480,7 +508,7 @@ __global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) distill_kernel(const T*
       qi = expf(lq);
       if (!(qi == 0.f)) loss += qi * (lq - row_logp(at.z[e], r.m, log_s, a.scale));
     }
-    if (tid + e * TPR < a.k) {
+    if (tid + e * TPR < ((a.k + 3) & ~3)) {
       here.place[tid + e * TPR] = use[e] ? at.id[e] : -1;
       here.value[tid + e * TPR] = qi;
     }
@@ -492,16 +520,22 @@ __global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) distill_kernel(const T*
   if (!dlogits) return;
   const bool none = w == 0.f || t.s == 0.f;
   T* dz = dlogits + n * a.ld_out;
-  const bool vec = same_alignment(s.z, dz);
+  const int bytes = store_bytes(dz + s.head);
   const RowPower l(r.m, log_s, c);
   const float w_s = w * exp2f(-l.log2_s);
-  auto dense = [&](float x) { return w_s * row_ex2(l.plain(x)); };
-  auto dense_huge = [&](float x) { return w_s * row_ex2(l.huge(x)); };
-  auto one = [&](float x) { return l.is_huge ? dense_huge(x) : dense(x); };
+  auto dense = [&](float2 x) {
+    const float2 y = l.plain(x);
+    return make_float2(w_s * row_ex2(y.x), w_s * row_ex2(y.y));
+  };
+  auto dense_huge = [&](float2 x) {
+    const float2 y = l.huge(x);
+    return make_float2(w_s * row_ex2(y.x), w_s * row_ex2(y.y));
+  };
+  auto one = [&](float x) { return l.is_huge ? dense_huge(make_float2(x, x)).x : dense(make_float2(x, x)).x; };
   for (int ch = chunks - 1; ch >= 0; --ch) {
-    if (none) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, [](float) { return 0.f; });
-    else if (l.is_huge) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, dense_huge);
-    else store_chunk<T, TPR, NV>(s, ch, tid, q, dz, vec, dense);
+    if (none) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, bytes, [](float2) { return make_float2(0.f, 0.f); });
+    else if (l.is_huge) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, bytes, dense_huge);
+    else store_chunk<T, TPR, NV>(s, ch, tid, q, dz, bytes, dense);
 #pragma unroll
     for (int i = 0; i < NV; ++i) q[i] = next[i];
     if (ch > 1 && !none) s.template load_chunk<TPR, NV, true>(ch - 2, tid, next);
