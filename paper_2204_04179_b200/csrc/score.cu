@@ -3,16 +3,19 @@
 // The product users x items^T runs on pairs of SMs (tcgen05 cta_group::2) as in gemm.cu: a cluster of two blocks owns a tile
 // of 256 users x 256 items, each stages its own 128 users and its own half of the items by TMA, the leader issues the MMAs,
 // and each block's tensor memory receives 128 users' logits, two tiles in turn.  The logits never leave it: an epilogue
-// thread owns one user (a lane of tensor memory) and half of a tile's columns and keeps the softmax statistics of what it has
-// seen in registers.
+// thread owns one user (a lane of tensor memory) and a quarter of a tile's columns and keeps the softmax statistics of what it
+// has seen in registers.
 //
-// Alternatives take a first pass over a part of the items (score_kernel<SAMPLE>), which writes the maxima of groups of 8 or
-// 32 columns; score_bar_kernel takes from them a bar that at least k entries of a user reach, and in the main pass a thread puts
-// entries that reach its user's bar on a list of its own.  With a sample of S items about k V / S entries of a user do.
+// Alternatives take a first pass over a part of the items (score_kernel<SAMPLE>), units of 128 spread over the table, which
+// writes the maxima of groups of 8 or 32 columns; score_bar_kernel takes from them a bar that at least k entries of a user
+// reach, and in the main pass a thread puts entries that reach its user's bar on a list of its own.  With a sample of S items
+// about k V / S entries of a user do.
 //
 // Work is cut evenly: the units of 128 items of all row tiles, one row tile after another, are divided into contiguous
 // runs, one for each pair.  A run touches at most two row tiles, so a user's statistics and lists lie with a few pairs;
-// score_join_kernel, one block a user, joins them.
+// score_join_kernel joins them.
+//
+// Up to 128 users the logits are written after all (score_kernel<LOGITS>) and gram_logprobs' kernel reads them.
 #include "logits.h"
 #include "row_softmax.cuh"
 #include "row_top.cuh"
@@ -24,14 +27,15 @@ using namespace tc;
 constexpr int SM_ROWS = 128, SC_ROWS = 2 * SM_ROWS;     // users of a block and of a pair
 constexpr int SC_BK = 64, SC_UNIT = 128, SC_COLS = 256; // k of a stage, items of a unit and of the widest tile
 constexpr int SC_A_BYTES = SM_ROWS * SC_BK * 2, SC_B_BYTES = SC_COLS / 2 * SC_BK * 2, SC_STAGE = SC_A_BYTES + SC_B_BYTES;
-constexpr int SC_STAGES = 6, SC_EPI_WARPS = 8, SC_THREADS = 64 + 32 * SC_EPI_WARPS;
-constexpr int SC_BIAS_BYTES = SC_EPI_WARPS * 128 * 4;   // a warp's 128 columns
+constexpr int SC_STAGES = 6, SC_EPI_WARPS = 16, SC_THREADS = 64 + 32 * SC_EPI_WARPS;
+constexpr int SC_PARTS = SC_EPI_WARPS / 4;              // parts of a tile's columns, each with its warps
+constexpr int SC_BIAS_BYTES = SC_EPI_WARPS * 64 * 4;    // a warp's columns
 constexpr int SC_SMEM = SC_STAGES * SC_STAGE + SC_BIAS_BYTES + 1024 + 256;
 constexpr int SC_LIST_MAX = 256;                        // most entries of a thread's list
-constexpr int SC_PAIR_THREADS = 2 * SC_ROWS;            // epilogue threads of a pair, one for each user and half
+constexpr int SC_PAIR_THREADS = SC_PARTS * SC_ROWS;     // epilogue threads of a pair, one for each user and part
 constexpr int SB_ROWS = 8, SB_GROUPS = 1024;            // score_bar_kernel: rows of a block, most groups of a row
 
-enum ScoreMode { STATISTICS = 0, LISTS = 1, SAMPLE = 2 };   // LISTS: statistics too
+enum ScoreMode { STATISTICS = 0, LISTS = 1, SAMPLE = 2, LOGITS = 3 };   // LISTS: statistics too
 
 struct ScoreArgs {
   const float* bias;
@@ -41,34 +45,38 @@ struct ScoreArgs {
   int32_t box_rows;              // users of a copy
   float c;
   const float* bars;             // [N]
-  uint64_t* lists;               // [pair, half, row of the tile, cap]
-  uint64_t* early;               // [row tile, half, row, early_cap]: of the run that goes on with the next row tile
+  uint64_t* lists;               // [pair, part, row of the tile, cap]
+  uint64_t* early;               // [row tile, part, row, early_cap]: of the run that goes on with the next row tile
   int32_t early_cap;
-  float4* stats;                 // [pair, row tile of the run (0, 1), half, row]: m, s, t, entries of the list
+  float4* stats;                 // [pair, row tile of the run (0, 1), part, row]: m, s, t, entries of the list
+  float* logits;                 // LOGITS: [N, ld_logits], a multiple of 4
+  int64_t ld_logits;
   float* sample;                 // maxima: [block of 32 columns, row] float4 of groups of 8, or one float
   int64_t sample_rows;
   int32_t fine;                  // groups of 8
+  int32_t stride;                // the pass takes every stride-th two units of the table
   int32_t* status;
 };
 
 // The tiles of a run, as all roles walk over them.
 struct ScoreRun {
-  int32_t units, begin, at, end;
+  int32_t units, stride, begin, at, end;
   int32_t tm, unit, width;       // row tile, first unit and width in units of the current tile
   bool first, last;              // of the run's part of this row tile
   __device__ __forceinline__ ScoreRun(const ScoreArgs& a, int pair)
-      : units(a.units), begin(pair * a.per_run), at(begin), end(min(begin + a.per_run, a.total)), tm(0), unit(0), width(0), first(false), last(false) {}
+      : units(a.units), stride(a.stride), begin(pair * a.per_run), at(begin), end(min(begin + a.per_run, a.total)), tm(0), unit(0), width(0), first(false), last(false) {}
   __device__ __forceinline__ bool next() {
     at += width;
     if (at >= end) return false;
     tm = at / units;
     unit = at - tm * units;
     const int left = min(units - unit, end - at);
-    width = min(left, SC_COLS / SC_UNIT);
+    width = min(left, stride > 1 && (unit & 1) ? 1 : SC_COLS / SC_UNIT);
     first = at == begin || unit == 0;
     last = left == width;
     return true;
   }
+  __device__ __forceinline__ int column() const { return ((unit >> 1) * stride * 2 + (unit & 1)) * SC_UNIT; }   // first item
   __device__ __forceinline__ int part() const { return tm - begin / units; }             // 0, or 1 for the second row tile
   __device__ __forceinline__ bool leaves() const { return (end - 1) / units != tm; }     // the run goes on with another row tile
 };
@@ -113,16 +121,29 @@ __device__ __forceinline__ void score_add(RowSums& r, const uint32_t (&v)[32], f
   r.s += s2.x + s2.y;
   r.t += t2.x + t2.y;
 }
-// The entries of a block that reach the bar, to the thread's list: a bit for each of a group of 8, then one entry of each lane at a time.
-__device__ __forceinline__ void score_list(const uint32_t (&v)[32], const float (&t)[4], float bar, uint32_t col, uint64_t* list, int& have) {
+// The entries of a block that reach the bar, to the lanes' lists (those of a warp `cap` apart): a bit for each of a group of 8, then
+// one entry of each lane at a time.  A list without room for another group is cut to its best k first.
+__device__ __forceinline__ void score_list(const uint32_t (&v)[32], const float (&t)[4], float& bar, uint32_t col, uint64_t* warp_lists, int cap, int k,
+                                           int& have) {
+  const int lane = threadIdx.x & 31;
+  uint64_t* list = warp_lists + (int64_t)lane * cap;
+  const uint32_t groups = __reduce_or_sync(0xffffffffu, (t[0] >= bar ? 1u : 0u) | (t[1] >= bar ? 2u : 0u) | (t[2] >= bar ? 4u : 0u) | (t[3] >= bar ? 8u : 0u));
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
-    if (!__any_sync(0xffffffffu, t[g] >= bar)) continue;
+    if (!(groups & (1u << g))) continue;
+    uint32_t full = __ballot_sync(0xffffffffu, have > cap - 8);
+    while (full) {
+      const int of = __ffs(full) - 1;
+      full &= full - 1;
+      __syncwarp();
+      const float up = score_cut(warp_lists + (int64_t)of * cap, __shfl_sync(0xffffffffu, have, of), k);
+      if (lane == of) { have = k; bar = up; }
+    }
     uint32_t bits = 0u;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (__uint_as_float(v[8 * g + j]) >= bar) bits |= 1u << j;
-    while (__any_sync(0xffffffffu, bits != 0u)) {
+    do {
       if (bits) {
         const int j = __ffs(bits) - 1;
         bits &= bits - 1u;
@@ -131,7 +152,7 @@ __device__ __forceinline__ void score_list(const uint32_t (&v)[32], const float 
         const uint32_t ab = j & 2 ? b : a, cd = j & 2 ? d : c;
         list[have++] = row_key(__uint_as_float(j & 4 ? cd : ab), col + 8 * g + j);
       }
-    }
+    } while (__any_sync(0xffffffffu, bits != 0u));
   }
 }
 
@@ -184,7 +205,7 @@ __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_const
     const uint32_t lead_bar0 = map_to_cta(bar0, 0);
     while (!failed && run.next()) {
       const int m0 = run.tm * SC_ROWS + (int)rank * SM_ROWS;
-      const int n0 = run.unit * SC_UNIT + (int)rank * (run.width * SC_UNIT / 2);     // this block's half of the items: boxes of 64
+      const int n0 = run.column() + (int)rank * (run.width * SC_UNIT / 2);     // this block's half of the items: boxes of 64
       // a block whose users are all past the last fetches none; what its rows of the product hold is not looked at
       const bool some = m0 < a.N;
       const uint32_t bytes = (some ? (uint32_t)a.box_rows * (SC_BK * 2) : 0u) + (uint32_t)run.width * (SC_UNIT / 2 * SC_BK * 2);
@@ -234,11 +255,10 @@ __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_const
     }
   } else if (go) {
     // ------------------------------ statistics and lists (both blocks) ------------------------------
-    const int q = warp & 3, half = (warp - 2) >> 2;
+    const int q = warp & 3, part = (warp - 2) >> 2;
     const int row = (int)rank * SM_ROWS + q * 32 + lane;          // of the pair's tile
-    float* bias_w = bias_s + (warp - 2) * 128;
-    uint64_t* warp_lists = a.lists + ((int64_t)(pair * 2 + half) * SC_ROWS + (row - lane)) * a.cap;
-    uint64_t* list = warp_lists + (int64_t)lane * a.cap;
+    float* bias_w = bias_s + (warp - 2) * 64;
+    uint64_t* warp_lists = a.lists + ((int64_t)(pair * SC_PARTS + part) * SC_ROWS + (row - lane)) * a.cap;
     const uint32_t lane_addr = tmem_base + ((uint32_t)(q * 32) << 16);
     RowSums sums;
     int have = 0;
@@ -246,8 +266,8 @@ __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_const
     uint32_t it = 0;
     const uint32_t lead_tempty = map_to_cta(tempty_bar(0), 0);
     for (; !failed && run.next(); ++it) {
-      const int buf = (int)(it & 1), blocks = run.width * (SC_UNIT / 64);      // blocks of 32 columns
-      const int col0 = run.unit * SC_UNIT + half * blocks * 32;
+      const int buf = (int)(it & 1), blocks = run.width;          // blocks of 32 columns of this part
+      const int col_t = part * blocks * 32, col0 = run.column() + col_t;
       const int64_t n = (int64_t)run.tm * SC_ROWS + row;
       const bool active = n - lane < a.N;                         // of the warp
       // columns past the table count as masked out
@@ -263,56 +283,49 @@ __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_const
       if (!mbar_wait_warp(tfull_bar(buf), (it >> 1) & 1, abort_flag)) { failed = true; break; }
       tc_fence_after();
       if (active) {
-        const uint32_t taddr = lane_addr + (uint32_t)(buf * SC_COLS + half * blocks * 32);
-        if (MODE != SAMPLE && run.first) {
+        const uint32_t taddr = lane_addr + (uint32_t)(buf * SC_COLS + col_t);
+        if (MODE <= LISTS && run.first) {
           sums = RowSums();
           have = 0;
           if (MODE == LISTS) bar = n < a.N ? a.bars[n] : __int_as_float(0x7fffffff);     // nothing reaches a NaN
         }
-        auto block = [&](uint32_t (&v)[32], int b) {
+        for (int b = 0; b < blocks; ++b) {
+          uint32_t v[32];
+          tc_ld32_issue(taddr + b * 32, v);
+          tc_ld32_wait(v);
           if (bias) score_bias(v, bias + b * 32);
-          float t[4];
-          score_tops(v, t);
-          const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
-          if constexpr (MODE == SAMPLE) {
-            const int64_t at = (int64_t)((col0 + b * 32) / 32) * a.sample_rows + n;
-            if (a.fine) reinterpret_cast<float4*>(a.sample)[at] = make_float4(t[0], t[1], t[2], t[3]);
-            else a.sample[at] = top;
+          if constexpr (MODE == LOGITS) {
+            const int col = col0 + b * 32;
+            if (n < a.N) {
+              float* to = a.logits + n * a.ld_logits + col;
+#pragma unroll
+              for (int j = 0; j < 32; j += 4)                      // a row's last vector may reach past the table
+                if (col + j < a.V) *reinterpret_cast<uint4*>(to + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            }
           } else {
-            score_add(sums, v, top, a.c);
-          }
-          if constexpr (MODE == LISTS) {
-            if (__any_sync(0xffffffffu, top >= bar)) {
-              score_list(v, t, bar, (uint32_t)(col0 + b * 32), list, have);
-              uint32_t full = __ballot_sync(0xffffffffu, have > a.cap - 32);
-              __syncwarp();
-              while (full) {                                      // more entries reach the bar than a list holds: its best k stay
-                const int of = __ffs(full) - 1;
-                full &= full - 1;
-                const float up = score_cut(warp_lists + (int64_t)of * a.cap, __shfl_sync(0xffffffffu, have, of), a.k);
-                if (lane == of) { have = a.k; bar = up; }
-              }
+            float t[4];
+            score_tops(v, t);
+            const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+            if constexpr (MODE == SAMPLE) {
+              const int64_t at = (int64_t)((run.unit * SC_UNIT + col_t + b * 32) / 32) * a.sample_rows + n;
+              if (a.fine) reinterpret_cast<float4*>(a.sample)[at] = make_float4(t[0], t[1], t[2], t[3]);
+              else a.sample[at] = top;
+            } else {
+              score_add(sums, v, top, a.c);
+              if (MODE == LISTS && __any_sync(0xffffffffu, top >= bar))
+                score_list(v, t, bar, (uint32_t)(col0 + b * 32), warp_lists, a.cap, a.k, have);
             }
           }
-        };
-        for (int b = 0; b < blocks; b += 2) {                     // 2 or 4 blocks
-          uint32_t v0[32], v1[32];
-          tc_ld32_issue(taddr + b * 32, v0);
-          tc_ld32_issue(taddr + (b + 1) * 32, v1);
-          tc_ld32_wait(v0);
-          tc_ld32_wait(v1);
-          block(v0, b);
-          block(v1, b + 1);
         }
       }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_remote(lead_tempty + 8u * buf);
-      if (MODE != SAMPLE && active && run.last) {
+      if (MODE <= LISTS && active && run.last) {
         const RowStat r = sums.stat(a.c);
         if constexpr (MODE == LISTS) {
           if (run.leaves()) {                                     // the lists are needed again: these go elsewhere
-            uint64_t* to = a.early + ((int64_t)(run.tm * 2 + half) * SC_ROWS + (row - lane)) * a.early_cap;
+            uint64_t* to = a.early + ((int64_t)(run.tm * SC_PARTS + part) * SC_ROWS + (row - lane)) * a.early_cap;
             __syncwarp();
             for (int of = 0; of < 32; ++of) {
               uint64_t* from = warp_lists + (int64_t)of * a.cap;
@@ -327,7 +340,7 @@ __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_const
             __syncwarp();
           }
         }
-        a.stats[((int64_t)(pair * 2 + run.part()) * 2 + half) * SC_ROWS + row] = make_float4(r.m, r.s, r.t, __int_as_float(have));
+        a.stats[((int64_t)(pair * 2 + run.part()) * SC_PARTS + part) * SC_ROWS + row] = make_float4(r.m, r.s, r.t, __int_as_float(have));
       }
     }
   }
@@ -426,7 +439,7 @@ __device__ __forceinline__ float score_dot(const bf16* u, const bf16* w, int d) 
 // Joins the statistics of the runs that crossed a user's row tile, and their lists.  A warp takes a user, four users a block; where
 // users are few a block takes one (ALONE): its eight warps share the given tokens and the reading of the lists.
 // About 256 keys come in; that so many as 512 do, one user in 200 with 10 alternatives, is met by warp_cut.
-constexpr int SJ_PARTS = kNumSMs + 2, SJ_KEYS = 1024;   // parts of a user at most; keys that are sorted out in shared memory
+constexpr int SJ_PARTS = (kNumSMs / 2 + 1) * SC_PARTS, SJ_KEYS = 1024;   // parts of a user at most; keys that are sorted out in shared memory
 constexpr int SJ_WARPS = 4, SJ_ALONE_WARPS = 8;
 template <bool ALONE>
 __global__ void __launch_bounds__(32 * (ALONE ? SJ_ALONE_WARPS : SJ_WARPS)) score_join_kernel(const ScoreArgs a, const bf16* users, int64_t ld_u, const bf16* items, int64_t ld_i,
@@ -440,14 +453,14 @@ __global__ void __launch_bounds__(32 * (ALONE ? SJ_ALONE_WARPS : SJ_WARPS)) scor
   uint64_t* keys = keys_of[ALONE ? 0 : warp];
   int* starts = starts_of[ALONE ? 0 : warp];            // of each part's list among all of the user's keys
   const int tm = (int)(n / SC_ROWS), row = (int)(n % SC_ROWS);
-  const int p0 = tm * a.units / a.per_run, p1 = ((tm + 1) * a.units - 1) / a.per_run, parts = (p1 - p0 + 1) * 2;
+  const int p0 = tm * a.units / a.per_run, p1 = ((tm + 1) * a.units - 1) / a.per_run, parts = (p1 - p0 + 1) * SC_PARTS;
   RowStat r = row_empty();
   int all = 0;
-  for (int i0 = 0; i0 < parts; i0 += 32) {              // part i: pair p0 + i / 2, half i % 2; every warp of a block does the same
-    const int i = i0 + lane, p = p0 + i / 2;
+  for (int i0 = 0; i0 < parts; i0 += 32) {              // part i % SC_PARTS of pair p0 + i / SC_PARTS; every warp of a block does the same
+    const int i = i0 + lane, p = p0 + i / SC_PARTS;
     int have = 0;
     if (i < parts) {
-      const float4 f = a.stats[((int64_t)(p * 2 + tm - p * a.per_run / a.units) * 2 + (i & 1)) * SC_ROWS + row];
+      const float4 f = a.stats[((int64_t)(p * 2 + tm - p * a.per_run / a.units) * SC_PARTS + i % SC_PARTS) * SC_ROWS + row];
       have = __float_as_int(f.w);
       RowStat x{f.x, f.y, f.z};
       const float m = fmaxf(r.m, x.m);
@@ -477,10 +490,10 @@ __global__ void __launch_bounds__(32 * (ALONE ? SJ_ALONE_WARPS : SJ_WARPS)) scor
       if (starts[mid] <= idx) lo = mid;
       else hi = mid - 1;
     }
-    const int p = p0 + lo / 2;
+    const int p = p0 + lo / SC_PARTS;
     const bool early = (min((p + 1) * a.per_run, a.total) - 1) / a.units != tm;
-    const uint64_t* l = early ? a.early + ((int64_t)(tm * 2 + (lo & 1)) * SC_ROWS + row) * a.early_cap
-                              : a.lists + ((int64_t)(p * 2 + (lo & 1)) * SC_ROWS + row) * a.cap;
+    const uint64_t* l = early ? a.early + ((int64_t)(tm * SC_PARTS + lo % SC_PARTS) * SC_ROWS + row) * a.early_cap
+                              : a.lists + ((int64_t)(p * SC_PARTS + lo % SC_PARTS) * SC_ROWS + row) * a.cap;
     return l[idx - starts[lo]];
   };
   if (k > 0 && all <= SJ_KEYS) {
@@ -588,6 +601,39 @@ gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_u
                                   size_t ws_bytes, cudaStream_t st) {
   const int32_t all_units = ceil_div(V, SC_UNIT);
   if (all_units > (1 << 30) / (kNumSMs / 2)) return gram_set_error(ctx, "gram_score_logprobs: %d items", V), GRAM_ERR_UNSUPPORTED;
+  // Few users: their logits are written and read once more, in place of the sample, the bars and the joining.  64 users against
+  // 100 000 items of 768 with 10 alternatives @@ us this way and @@ the other, 128 users @@ and @@.
+  CUtensorMap map_u, map_i;
+  // copies are no larger than the users (rows past the last are filled with zeros, which takes time: one user against 100 000
+  // items of 768 46 us with boxes of 128 rows, 35 with boxes of 8)
+  int box_rows = SM_ROWS;
+  while (box_rows > 8 && box_rows / 2 >= N) box_rows /= 2;
+  if (!make_map(&map_i, items, (uint64_t)d, (uint64_t)V, (uint64_t)ld_items, SC_BK, 64))
+    return gram_set_error(ctx, "gram_score_logprobs: cannot describe the items"), GRAM_ERR_UNSUPPORTED;
+  const int64_t ld_logits = ((int64_t)V + 3) / 4 * 4;
+  ScoreArgs a = {};
+  a.bias = bias;
+  a.box_rows = box_rows;
+  a.num_kb = ceil_div(d, SC_BK);
+  a.k = ask.k;
+  a.c = scale * kLog2e;
+  a.stride = 1;
+  a.status = gram_status_word(ctx);
+  if (N <= SM_ROWS && (int64_t)(ws_bytes / sizeof(float)) / ld_logits >= N) {
+    if (!make_map(&map_u, users, (uint64_t)d, (uint64_t)N, (uint64_t)ld_users, SC_BK, (uint32_t)box_rows))
+      return gram_set_error(ctx, "gram_score_logprobs: cannot describe the users"), GRAM_ERR_UNSUPPORTED;
+    a.N = N;
+    a.V = V;
+    a.units = a.total = all_units;
+    a.per_run = ceil_div(all_units, kNumSMs / 2);
+    a.logits = (float*)ws;
+    a.ld_logits = ld_logits;
+    {
+      ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * N * V * d, 1, st, "score");
+      GRAM_CUDA(ctx, launch_score<LOGITS>(map_u, map_i, a, ceil_div(a.total, a.per_run), st));
+    }
+    return logprobs_launch(ctx, ws, GRAM_F32, ld_logits, N, V, scale, ask, st);
+  }
   // The sample: so many items that about 256 entries of a user reach the bar, but 4096 at least and a third of the table at
   // most; its maxima by groups of 8 columns, by 32 where that is more than score_bar_kernel holds.
   int32_t sample = 0, fine = 1;
@@ -608,9 +654,9 @@ gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_u
   const size_t sample_tile = (size_t)sample_units * (SC_UNIT / 32) * SC_ROWS * (fine ? 16 : 4);
   const size_t stats_bytes = (size_t)(kNumSMs / 2) * 2 * SC_PAIR_THREADS * sizeof(float4), bars_tile = SC_ROWS * sizeof(float);
   if (ask.k && most > (int64_t)((ws_bytes - stats_bytes) / (sample_tile + bars_tile))) most = (int64_t)((ws_bytes - stats_bytes) / (sample_tile + bars_tile));
-  // Lists share the sample's place, 32 entries more than k in each.  Where the workspace is too small for those of all pairs and the
+  // Lists share the sample's place, 16 entries more than k at least in each.  Where the workspace is too small for those of all pairs and the
   // early ones of all row tiles, a launch takes fewer row tiles, and fewer pairs run.
-  const int early_cap = ask.k > 64 ? ask.k : 64;
+  const int early_cap = ask.k > 32 ? ask.k : 32;
   int64_t per_launch, cap;
   int pairs;
   for (;; most /= 2) {
@@ -620,35 +666,22 @@ gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_u
     if (!ask.k) break;
     const int64_t room = ((int64_t)ws_bytes - (int64_t)stats_bytes - per_launch * (int64_t)bars_tile) / (SC_PAIR_THREADS * 8) - per_launch * early_cap;
     cap = room / pairs < SC_LIST_MAX ? room / pairs : SC_LIST_MAX;
-    if (cap >= ask.k + 32) break;
-    cap = ask.k + 32;
+    if (cap >= ask.k + 16) break;
+    cap = ask.k + 16;
     pairs = (int)(room / cap);
     if (pairs >= 2 * per_launch) break;
     if (most == 1) return gram_set_error(ctx, "gram_score_logprobs: the workspace is too small for %d alternatives", ask.k), GRAM_ERR_WORKSPACE;
   }
   const size_t early_bytes = ask.k ? (size_t)per_launch * SC_PAIR_THREADS * early_cap * 8 : 0;
-  // few users: the copies' boxes are no larger (rows past the last are filled with zeros, which takes time: one user against
-  // 100 000 items of 768 46 us with boxes of 128 rows)
-  int box_rows = SM_ROWS;
-  while (box_rows > 8 && box_rows / 2 >= N) box_rows /= 2;
-  CUtensorMap map_u, map_i;
-  if (!make_map(&map_i, items, (uint64_t)d, (uint64_t)V, (uint64_t)ld_items, SC_BK, 64))
-    return gram_set_error(ctx, "gram_score_logprobs: cannot describe the items"), GRAM_ERR_UNSUPPORTED;
   ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * N * V * d, (ask.k ? 4 : 2) * (int)ceil_div64(tiles, per_launch), st, "score");
   for (int64_t n = 0; n < N; n += per_launch * SC_ROWS) {
     const int64_t now = N - n < per_launch * SC_ROWS ? N - n : per_launch * SC_ROWS, now_tiles = ceil_div64(now, SC_ROWS);
     const bf16* u = (const bf16*)users + n * ld_users;
     if (!make_map(&map_u, u, (uint64_t)d, (uint64_t)now, (uint64_t)ld_users, SC_BK, (uint32_t)box_rows))
       return gram_set_error(ctx, "gram_score_logprobs: cannot describe the users"), GRAM_ERR_UNSUPPORTED;
-    ScoreArgs a = {};
-    a.box_rows = box_rows;
-    a.bias = bias;
     a.N = now;
-    a.num_kb = ceil_div(d, SC_BK);
-    a.k = ask.k;
     a.cap = (int32_t)cap;
     a.early_cap = early_cap;
-    a.c = scale * kLog2e;
     a.stats = (float4*)ws;
     float* bars = (float*)((uint8_t*)ws + stats_bytes);
     a.bars = bars;
@@ -657,16 +690,16 @@ gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_u
     a.sample = (float*)a.early;
     a.sample_rows = now_tiles * SC_ROWS;
     a.fine = fine;
-    a.status = gram_status_word(ctx);
-    auto cut = [&](int32_t items_now, int over) {       // the units of a pass in runs; returns their number
-      a.V = items_now;
-      a.units = ceil_div(items_now, SC_UNIT);
+    auto cut = [&](int32_t units, int stride, int over) {        // the units of a pass in runs; returns their number
+      a.V = V;
+      a.units = units;
+      a.stride = stride;
       a.total = (int32_t)(now_tiles * a.units);
       a.per_run = ceil_div(a.total, over);
       return ceil_div(a.total, a.per_run);
     };
     if (ask.k) {
-      const int used = cut(sample, kNumSMs / 2);
+      const int used = cut(sample_units, sample_units < all_units ? all_units / 2 / ceil_div(sample_units, 2) : 1, kNumSMs / 2);
       GRAM_CUDA(ctx, launch_score<SAMPLE>(map_u, map_i, a, used, st));
       launch_chain(score_bar_kernel, dim3((unsigned)ceil_div64(now, SB_ROWS)), 32 * SB_ROWS, 0, st, a.sample, a.sample_rows,
                    a.units * (SC_UNIT / 32), fine, now, ask.k, bars);
@@ -676,7 +709,7 @@ gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_u
     if (ask.stats) part.stats += 2 * n;
     if (ask.entropy) part.entropy += n;
     if (ask.k) { part.top_logp += n * ask.k; part.top_ids += n * ask.k; }
-    const int used = cut(V, pairs);
+    const int used = cut(all_units, 1, pairs);
     GRAM_CUDA(ctx, ask.k ? launch_score<LISTS>(map_u, map_i, a, used, st) : launch_score<STATISTICS>(map_u, map_i, a, used, st));
     if (now >= 4 * kNumSMs)
       launch_chain(score_join_kernel<false>, dim3((unsigned)ceil_div64(now, SJ_WARPS)), 32 * SJ_WARPS, 0, st, a, u, ld_users, (const bf16*)items, ld_items,
