@@ -49,7 +49,7 @@ struct ScoreArgs {
   uint64_t* early;               // [row tile, part, row, early_cap]: of the run that goes on with the next row tile
   int32_t early_cap;
   float4* stats;                 // [pair, row tile of the run (0, 1), part, row]: m, s, t, entries of the list
-  float* logits;                 // LOGITS: [N, ld_logits], a multiple of 4
+  float* logits;                 // LOGITS: [N, ld_logits], a multiple of 8
   int64_t ld_logits;
   float* sample;                 // maxima: [block of 32 columns, row] float4 of groups of 8, or one float
   int64_t sample_rows;
@@ -299,8 +299,11 @@ __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_const
             if (n < a.N) {
               float* to = a.logits + n * a.ld_logits + col;
 #pragma unroll
-              for (int j = 0; j < 32; j += 4)                      // a row's last vector may reach past the table
-                if (col + j < a.V) *reinterpret_cast<uint4*>(to + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+              for (int j = 0; j < 32; j += 8)                      // whole 32-byte sectors; a row's last may reach past the table
+                if (col + j < a.V)
+                  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + j), "r"(v[j]), "r"(v[j + 1]), "r"(v[j + 2]),
+                               "r"(v[j + 3]), "r"(v[j + 4]), "r"(v[j + 5]), "r"(v[j + 6]), "r"(v[j + 7])
+                               : "memory");
             }
           } else {
             float t[4];
@@ -387,11 +390,16 @@ __global__ void __launch_bounds__(32 * SB_ROWS) score_bar_kernel(const float* sa
   int some = 0;
 #pragma unroll
   for (int i = 0; i < SB_GROUPS / 32; ++i) {
-    const float x = i * 32 + lane < groups ? value[r][i * 32 + lane] : ROW_NEG_INF;
-    o[i] = x > ROW_NEG_INF ? row_order(x) : 0u;
-    if (o[i]) lo = min(lo, o[i]);
-    hi = max(hi, o[i]);
-    some += o[i] != 0u;
+    o[i] = 0u;
+    if (i * 32 < groups) {
+      const float x = i * 32 + lane < groups ? value[r][i * 32 + lane] : ROW_NEG_INF;
+      if (x > ROW_NEG_INF) {
+        o[i] = row_order(x);
+        lo = min(lo, o[i]);
+        hi = max(hi, o[i]);
+        ++some;
+      }
+    }
   }
   // k of 32 lanes' maxima are above the least of them
   const uint32_t lane_hi = hi;
@@ -404,7 +412,8 @@ __global__ void __launch_bounds__(32 * SB_ROWS) score_bar_kernel(const float* sa
       const uint32_t mid = hi - (hi - lo) / 2;
       int n = 0;
 #pragma unroll
-      for (int i = 0; i < SB_GROUPS / 32; ++i) n += o[i] >= mid;
+      for (int i = 0; i < SB_GROUPS / 32; ++i)
+        if (i * 32 < groups) n += o[i] >= mid;
       n = __reduce_add_sync(0xffffffffu, n);
       if (n < k) hi = mid - 1;
       else {
@@ -438,29 +447,35 @@ __device__ __forceinline__ float score_dot(const bf16* u, const bf16* w, int d) 
 
 // Joins the statistics of the runs that crossed a user's row tile, and their lists.  A warp takes a user, four users a block; where
 // users are few a block takes one (ALONE): its eight warps share the given tokens and the reading of the lists.
-// About 256 keys come in; that so many as 512 do, one user in 200 with 10 alternatives, is met by warp_cut.
-constexpr int SJ_PARTS = (kNumSMs / 2 + 1) * SC_PARTS, SJ_KEYS = 1024;   // parts of a user at most; keys that are sorted out in shared memory
+// About 256 keys come in; more than fit are taken in turns, the best k of each going into the next.
+constexpr int SJ_PARTS = (kNumSMs / 2 + 1) * SC_PARTS, SJ_KEYS = 512;          // parts of a user at most; keys of a turn
 constexpr int SJ_WARPS = 4, SJ_ALONE_WARPS = 8;
 template <bool ALONE>
 __global__ void __launch_bounds__(32 * (ALONE ? SJ_ALONE_WARPS : SJ_WARPS)) score_join_kernel(const ScoreArgs a, const bf16* users, int64_t ld_u, const bf16* items, int64_t ld_i,
                                                                 int32_t d, float scale, RowAnswers ask) {
   if (!chain_begin()) return;
-  __shared__ __align__(16) uint64_t keys_of[ALONE ? 1 : SJ_WARPS][SJ_KEYS];
-  __shared__ int starts_of[ALONE ? 1 : SJ_WARPS][SJ_PARTS + 1];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int ROWS = ALONE ? 1 : SJ_WARPS;
+  __shared__ __align__(16) uint64_t keys_of[ROWS][SJ_KEYS];
+  __shared__ const uint64_t* lists_of[ROWS][SJ_PARTS];
+  __shared__ int starts_of[ROWS][SJ_PARTS + 1], kept;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, slot = ALONE ? 0 : warp;
   const int64_t n = ALONE ? blockIdx.x : (int64_t)blockIdx.x * SJ_WARPS + warp;
   if (n >= a.N) return;                                 // whole warps; the block's barriers are in the other form only
-  uint64_t* keys = keys_of[ALONE ? 0 : warp];
-  int* starts = starts_of[ALONE ? 0 : warp];            // of each part's list among all of the user's keys
+  auto sync = [&]() {
+    if (ALONE) __syncthreads();
+    else __syncwarp();
+  };
+  uint64_t* keys = keys_of[slot];
+  int* starts = starts_of[slot];                        // of each part's list among all of the user's keys
   const int tm = (int)(n / SC_ROWS), row = (int)(n % SC_ROWS);
   const int p0 = tm * a.units / a.per_run, p1 = ((tm + 1) * a.units - 1) / a.per_run, parts = (p1 - p0 + 1) * SC_PARTS;
   RowStat r = row_empty();
   int all = 0;
   for (int i0 = 0; i0 < parts; i0 += 32) {              // part i % SC_PARTS of pair p0 + i / SC_PARTS; every warp of a block does the same
-    const int i = i0 + lane, p = p0 + i / SC_PARTS;
+    const int i = i0 + lane, p = p0 + i / SC_PARTS, part = i % SC_PARTS;
     int have = 0;
     if (i < parts) {
-      const float4 f = a.stats[((int64_t)(p * 2 + tm - p * a.per_run / a.units) * SC_PARTS + i % SC_PARTS) * SC_ROWS + row];
+      const float4 f = a.stats[((int64_t)(p * 2 + (p == p0 && p * a.per_run < tm * a.units ? 1 : 0)) * SC_PARTS + part) * SC_ROWS + row];
       have = __float_as_int(f.w);
       RowStat x{f.x, f.y, f.z};
       const float m = fmaxf(r.m, x.m);
@@ -468,6 +483,9 @@ __global__ void __launch_bounds__(32 * (ALONE ? SJ_ALONE_WARPS : SJ_WARPS)) scor
       if (m > x.m) row_raise(x, m, a.c);
       r.s += x.s;
       r.t += x.t;
+      const bool early = p == p1 && min((p + 1) * a.per_run, a.total) > (tm + 1) * a.units;      // the run goes on with the next row tile
+      lists_of[slot][i] = early ? a.early + ((int64_t)(tm * SC_PARTS + part) * SC_ROWS + row) * a.early_cap
+                                : a.lists + ((int64_t)(p * SC_PARTS + part) * SC_ROWS + row) * a.cap;
     }
     int before = have;
 #pragma unroll
@@ -480,25 +498,25 @@ __global__ void __launch_bounds__(32 * (ALONE ? SJ_ALONE_WARPS : SJ_WARPS)) scor
   }
   if (lane == 0) starts[parts] = all;
   r = row_join_lanes<32>(r, a.c);
-  if (ALONE) __syncthreads();                           // (the warps have written the same starts)
-  else __syncwarp();
+  sync();                                               // (the warps of a block have written the same)
   const int k = ask.k;
-  auto key_at = [&](int idx) {
-    int lo = 0, hi = parts - 1;                         // the last part that starts at or before idx
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) / 2;
-      if (starts[mid] <= idx) lo = mid;
-      else hi = mid - 1;
-    }
-    const int p = p0 + lo / SC_PARTS;
-    const bool early = (min((p + 1) * a.per_run, a.total) - 1) / a.units != tm;
-    const uint64_t* l = early ? a.early + ((int64_t)(tm * SC_PARTS + lo % SC_PARTS) * SC_ROWS + row) * a.early_cap
-                              : a.lists + ((int64_t)(p * SC_PARTS + lo % SC_PARTS) * SC_ROWS + row) * a.cap;
-    return l[idx - starts[lo]];
-  };
-  if (k > 0 && all <= SJ_KEYS) {
+  // keys [from, from + count) of all lists to keys[at ..)
+  auto take = [&](int from, int count, int at) {
 #pragma unroll 4
-    for (int i = ALONE ? (int)threadIdx.x : lane; i < all; i += ALONE ? 32 * SJ_ALONE_WARPS : 32) keys[i] = key_at(i);
+    for (int i = ALONE ? (int)threadIdx.x : lane; i < count; i += ALONE ? 32 * SJ_ALONE_WARPS : 32) {
+      int lo = 0, hi = parts - 1;                       // the last part that starts at or before this key
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (starts[mid] <= from + i) lo = mid;
+        else hi = mid - 1;
+      }
+      keys[at + i] = lists_of[slot][lo][from + i - starts[lo]];
+    }
+  };
+  int have = 0;
+  if (k > 0) {
+    have = min(all, SJ_KEYS);
+    take(0, have, 0);
   }
   float log_s = row_log_sum(r, a.c), entropy = row_entropy(r);
   if (row_is_huge(r.m, a.c)) {                          // summed again, relative to m itself
@@ -524,37 +542,26 @@ __global__ void __launch_bounds__(32 * (ALONE ? SJ_ALONE_WARPS : SJ_WARPS)) scor
     }
     if (lane == 0) ask.logp[n * ask.C + i] = lp;
   }
-  if (ALONE) __syncthreads();
-  else __syncwarp();
-  if (ALONE && warp != 0) return;
-  if (lane == 0) {
+  if (lane == 0 && (!ALONE || warp == 0)) {
     if (ask.stats) { ask.stats[2 * n] = r.m; ask.stats[2 * n + 1] = log_s; }
     if (ask.entropy) ask.entropy[n] = entropy;
   }
   if (k == 0) return;
-  int have = all;
-  if (all <= SJ_KEYS) {
-    if (have > 512) {
-      (void)warp_cut(keys, have, k);
-      have = k;
-    } else if (have > k + 16) {
-      have = warp_keep(keys, have, k);
+  for (int from = have;;) {
+    sync();
+    if (!ALONE || warp == 0) {
+      if (have > k + 16) have = warp_keep(keys, have, k);
+      if (ALONE && lane == 0) kept = have;
     }
-  } else {                                              // many equal or clustered logits: the k-th key by bisection over the lists
-    const uint64_t kth = kth_key(k, [&](uint64_t t) {
-      int c = 0;
-      for (int i = lane; i < all; i += 32) c += key_at(i) >= t;
-      return (int)__reduce_add_sync(0xffffffffu, c);
-    });
-    have = 0;
-    for (int i0 = 0; i0 < all; i0 += 32) {
-      const uint64_t key = i0 + lane < all ? key_at(i0 + lane) : 0;
-      const uint32_t who = __ballot_sync(0xffffffffu, key >= kth);
-      if (key >= kth) keys[have + __popc(who & ((1u << lane) - 1u))] = key;
-      have += __popc(who);
-    }
-    __syncwarp();
+    sync();
+    if (ALONE) have = kept;
+    if (from == all) break;
+    const int count = min(all - from, SJ_KEYS - have);
+    take(from, count, have);
+    from += count;
+    have += count;
   }
+  if (ALONE && warp != 0) return;
   if (have & 1) {
     if (lane == 0) keys[have] = 0;                      // read in pairs
     __syncwarp();
@@ -610,7 +617,7 @@ gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_u
   while (box_rows > 8 && box_rows / 2 >= N) box_rows /= 2;
   if (!make_map(&map_i, items, (uint64_t)d, (uint64_t)V, (uint64_t)ld_items, SC_BK, 64))
     return gram_set_error(ctx, "gram_score_logprobs: cannot describe the items"), GRAM_ERR_UNSUPPORTED;
-  const int64_t ld_logits = ((int64_t)V + 3) / 4 * 4;
+  const int64_t ld_logits = ((int64_t)V + 7) / 8 * 8;
   ScoreArgs a = {};
   a.bias = bias;
   a.box_rows = box_rows;
@@ -619,7 +626,7 @@ gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_u
   a.c = scale * kLog2e;
   a.stride = 1;
   a.status = gram_status_word(ctx);
-  if (N <= SM_ROWS && (int64_t)(ws_bytes / sizeof(float)) / ld_logits >= N) {
+  if (ask.k > 0 && N <= SM_ROWS && (int64_t)(ws_bytes / sizeof(float)) / ld_logits >= N) {
     if (!make_map(&map_u, users, (uint64_t)d, (uint64_t)N, (uint64_t)ld_users, SC_BK, (uint32_t)box_rows))
       return gram_set_error(ctx, "gram_score_logprobs: cannot describe the users"), GRAM_ERR_UNSUPPORTED;
     a.N = N;
