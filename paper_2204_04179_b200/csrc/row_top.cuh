@@ -107,6 +107,7 @@ template <int TPR> struct alignas(16) TopScratch {
   uint16_t entry[ENTRIES];       // groups whose maximum reaches the bar: group * TPR + thread
   int entries, found;
   int part[Group<TPR>::WARPS];
+  int count[2][Group<TPR>::WARPS];
   uint32_t bound[Group<TPR>::WARPS][2];
 };
 
@@ -183,6 +184,56 @@ template <typename T, int TPR> __device__ __noinline__ int top_exact(TopScratch<
   G::sync();
   return n;
 }
+// of many keys a group keeps the best k or a few more; returns how many, with a barrier behind it
+template <int TPR> __device__ __noinline__ int top_keep(TopScratch<TPR>& sc, int have, int k) {
+  using G = Group<TPR>;
+  if constexpr (TPR == 32) return warp_keep(sc.keys, have, k);
+  constexpr int PER = TopScratch<TPR>::KEYS / TPR;
+  const int tid = G::tid(), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint64_t key[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) key[i] = i * TPR + tid < have ? sc.keys[i * TPR + tid] : 0;
+  int turn = 0;
+  auto at_least = [&](uint64_t t) {                      // one barrier: the counts of two calls lie apart
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (i * TPR < have) c += key[i] >= t;
+    c = __reduce_add_sync(0xffffffffu, c);
+    if (lane == 0) sc.count[turn][warp] = c;
+    __syncthreads();
+    int n = 0;
+#pragma unroll
+    for (int w = 0; w < G::WARPS; ++w) n += sc.count[turn][w];
+    turn ^= 1;
+    return n;
+  };
+  uint64_t lo = 1, hi = ~0ull;
+  int left = have;
+  while (lo < hi && left > k + 16) {
+    const uint64_t mid = hi - (hi - lo) / 2;
+    const int n = at_least(mid);
+    if (n < k) hi = mid - 1;
+    else {
+      lo = mid;
+      left = n;
+    }
+  }
+  left = at_least(lo);
+  int at = 0;
+#pragma unroll
+  for (int w = 0; w < G::WARPS; ++w) at += w < warp ? sc.count[turn ^ 1][w] : 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (i * TPR < have) {
+      const bool in = key[i] >= lo;
+      const uint32_t who = __ballot_sync(0xffffffffu, in);
+      if (in) sc.keys[at + __popc(who & ((1u << lane) - 1u))] = key[i];
+      at += __popc(who);
+    }
+  __syncthreads();
+  return left;
+}
 // The candidates of a row or slice, as keys in sc.keys: at least its best k, or all there are; a 0 behind an odd number of them.
 // Group g holds the thread's vectors of chunks [g << shift, (g + 1) << shift), NV a chunk, TPR apart.  sc.entries and sc.found
 // are 0 before, behind a barrier; a barrier is behind what this leaves.
@@ -211,16 +262,18 @@ __device__ __forceinline__ int top_collect(TopScratch<TPR>& sc, const TopSource&
   G::sync();
   const int entries = sc.entries;
   if (entries <= Sc::ENTRIES) {
-    const int per = NV << shift;                         // vectors of a group, a power of two
-    for (int i = tid; i < entries * per; i += TPR) {
-      const int e = sc.entry[i / per], j = i & (per - 1);
-      const int v = src.v0 + (e / TPR) * (per * TPR) + j * TPR + e % TPR;
+    static_assert(NV == 4, "the vectors of a group are a power of two");
+    const int per = 2 + shift;                           // 2^per of them
+    for (int i = tid; i < entries << per; i += TPR) {
+      const int e = sc.entry[i >> per], j = i & ((1 << per) - 1);
+      const int v = src.v0 + (((e / TPR) << per) + j) * TPR + e % TPR;
       if (v < src.v1) each_of<T>(src.from[v], src.place0 + v * RowVec<T>::N, put);
     }
   }
   G::sync();
   int have = sc.found;
   if (entries > Sc::ENTRIES || have > Sc::KEYS) have = top_exact<T, TPR>(sc, src, k);
+  else if (have > 2 * k + 96) have = top_keep<TPR>(sc, have, k);     // counting takes have^2 comparisons
   if (have & 1) {                                        // read in pairs
     if (tid == 0) sc.keys[have] = 0;
     G::sync();
