@@ -63,11 +63,11 @@ template <typename T> struct Slice {
     }
   }
 };
-// the largest of the vectors [A, B)
-template <typename T, int A, int B, int NV> __device__ __forceinline__ float chunk_top(const uint4 (&q)[NV]) {
-  float top = RowVec<T>::top(q[A]);
+// the largest of a chunk's entries of a thread
+template <typename T, int NV> __device__ __forceinline__ float chunk_top(const uint4 (&q)[NV]) {
+  float top = RowVec<T>::top(q[0]);
 #pragma unroll
-  for (int i = A + 1; i < B; ++i) top = fmaxf(top, RowVec<T>::top(q[i]));
+  for (int i = 1; i < NV; ++i) top = fmaxf(top, RowVec<T>::top(q[i]));
   return top;
 }
 
@@ -139,21 +139,31 @@ __global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) logprobs_kernel(const T
   const float edge = edge_place >= 0 ? row_load(s.z + edge_place) : ROW_NEG_INF;
   const int chunks = s.template chunks<TPR, NV>();
   RowSums sums;
-  float top_a = ROW_NEG_INF, top_b = ROW_NEG_INF, top_group = ROW_NEG_INF;     // of the thread's entries so far, of a group's
+  float tops[NV], top_group = ROW_NEG_INF;               // the largest of the thread's i-th vectors so far, and of a group's entries
   int group_shift = 0, group = 0;
   if constexpr (TOP) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) tops[i] = ROW_NEG_INF;
     while (((chunks - 1) >> group_shift) >= TopScratch<TPR>::GROUPS) ++group_shift;
     if (tid == 0) sc.entries = sc.found = 0;             // the statistics' barriers come before their use
   }
 #pragma unroll 2
   for (int ch = 0; ch < chunks; ++ch) {
     if (ch + 1 < chunks) s.template load_chunk<TPR, NV, !TOP>(ch + 1, tid, next);
-    const float a = chunk_top<T, 0, NV / 2>(q), b = chunk_top<T, NV / 2, NV>(q);
-    row_add_vectors<T, NV>(sums, q, fmaxf(a, b), c);
+    float top = ROW_NEG_INF;
     if constexpr (TOP) {
-      top_a = fmaxf(top_a, a);
-      top_b = fmaxf(top_b, b);
-      top_group = fmaxf(top_group, fmaxf(a, b));
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const float x = RowVec<T>::top(q[i]);
+        tops[i] = fmaxf(tops[i], x);
+        top = fmaxf(top, x);
+      }
+      top_group = fmaxf(top_group, top);
+    } else {
+      top = chunk_top<T>(q);
+    }
+    row_add_vectors<T, true>(sums, q, top, c);
+    if constexpr (TOP) {
       if (((ch + 1) & ((1 << group_shift) - 1)) == 0 || ch == chunks - 1) {
         sc.group[group * TPR + tid] = top_group;
         top_group = ROW_NEG_INF;
@@ -169,7 +179,8 @@ __global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) logprobs_kernel(const T
   const uint64_t* list = sc.keys;
   if constexpr (TOP) {
     if (TPR == 32) G::sync();
-    const float bar = top_bar<TPR>(edge_place >= 0 ? fmaxf(top_a, edge) : top_a, top_b, ask.k, sc);
+    if (edge_place >= 0) tops[0] = fmaxf(tops[0], edge);
+    const float bar = top_bar<TPR>(tops, ask.k, sc);
     have = top_collect<T, TPR, NV>(sc, TopSource{s.vectors(), s.head, s.v0, s.v1, edge, edge_place}, group, group_shift, bar, ask.k);
   }
   if (TPR > 32 && slices > 1) {
@@ -258,18 +269,30 @@ template <typename T> __device__ __forceinline__ void store_vector(T* at, const 
     for (int j = 0; j < 8; ++j) reinterpret_cast<uint16_t*>(at)[j] = e[j];
   }
 }
-// f(pair of logits) -> pair of results, over a chunk that is in registers
-template <typename T, int TPR, int NV, typename F>
-__device__ __forceinline__ void store_chunk(const Slice<T>& s, int ch, int tid, const uint4 (&q)[NV], T* dz, int bytes, F f) {
+// pairs of logits -> pairs of results, over a chunk that is in registers: `plain` for whole chunks of rows that lie alike within 16
+// bytes, where `fast` says that it holds, and `any` otherwise (one straight line each: with the tests at every vector a gradient
+// took 10 instructions an element instead of @@)
+template <typename T, int TPR, int NV, typename F, typename A>
+__device__ __forceinline__ void store_chunk(const Slice<T>& s, int ch, int tid, const uint4 (&q)[NV], T* dz, int bytes, bool fast, F plain, A any) {
   const int v = s.v0 + ch * (TPR * NV) + tid;
   T* at = dz + s.place(v);
+  if (fast && v - tid + TPR * NV <= s.v1) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    if (v + i * TPR < s.v1) {
+    for (int i = 0; i < NV; ++i) {
       uint4 o;
 #pragma unroll
-      for (int j = 0; j < RowVec<T>::N / 2; ++j) RowVec<T>::put(o, j, f(RowVec<T>::pair(q[i], j)));
-      store_vector(at + i * (TPR * RowVec<T>::N), o, bytes);
+      for (int j = 0; j < RowVec<T>::N / 2; ++j) RowVec<T>::put(o, j, plain(RowVec<T>::pair(q[i], j)));
+      __stcs(reinterpret_cast<uint4*>(at + i * (TPR * RowVec<T>::N)), o);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if (v + i * TPR < s.v1) {
+        uint4 o;
+#pragma unroll
+        for (int j = 0; j < RowVec<T>::N / 2; ++j) RowVec<T>::put(o, j, any(RowVec<T>::pair(q[i], j)));
+        store_vector(at + i * (TPR * RowVec<T>::N), o, bytes);
+      }
     }
   }
 }
@@ -391,25 +414,18 @@ __global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) logprobs_backward_kerne
   const bool none = (sum == 0.f && h == 0.f) || log_s == ROW_NEG_INF;    // nothing asked, or nothing left in the row
   const RowPower l(m, log_s, c);
   const float inv = exp2f(-l.log2_s), Ay = inv * fmaf(-B, l.log2_s, A), By = inv * B;
-  auto value = [&](float y) { return row_ex2(y) * fmaf(fmaxf(y, -200.f), By, Ay); };
-  auto dense = [&](float2 x) {
-    const float2 y = l.plain(x);
-    return make_float2(value(y.x), value(y.y));
+  auto value = [&](float2 y) {
+    return make_float2(row_ex2(y.x) * fmaf(fmaxf(y.x, -200.f), By, Ay), row_ex2(y.y) * fmaf(fmaxf(y.y, -200.f), By, Ay));
   };
-  auto dense_huge = [&](float2 x) {
-    const float2 y = l.huge(x);
-    return make_float2(value(y.x), value(y.y));
-  };
-  auto one = [&](float x) {
-    const float2 xx = make_float2(x, x);
-    return none || x == ROW_NEG_INF ? 0.f : l.is_huge ? dense_huge(xx).x : dense(xx).x;
-  };
+  auto plain = [&](float2 x) { return value(l.plain(x)); };
+  auto any = [&](float2 x) { return none ? make_float2(0.f, 0.f) : value(l.is_huge ? l.huge(x) : l.plain(x)); };
+  auto one = [&](float x) { return x == ROW_NEG_INF ? 0.f : any(make_float2(x, x)).x; };
   const int chunks = s.template chunks<TPR, NV>();
+  const bool fast = bytes == 16 && !none && !l.is_huge;
+#pragma unroll 2
   for (int ch = 0; ch < chunks; ++ch) {
     if (ch + 1 < chunks && !none) s.template load_chunk<TPR, NV, true>(ch + 1, tid, next);
-    if (none) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, bytes, [](float2) { return make_float2(0.f, 0.f); });
-    else if (l.is_huge) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, bytes, dense_huge);
-    else store_chunk<T, TPR, NV>(s, ch, tid, q, dz, bytes, dense);
+    store_chunk<T, TPR, NV>(s, ch, tid, q, dz, bytes, fast, plain, any);
 #pragma unroll
     for (int i = 0; i < NV; ++i) q[i] = next[i];
   }
@@ -465,10 +481,11 @@ __global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) distill_kernel(const T*
   const float edge = edge_place >= 0 ? row_load(s.z + edge_place) : ROW_NEG_INF;
   const int chunks = s.template chunks<TPR, NV>();
   RowSums sums, teacher;
+#pragma unroll 2
   for (int ch = 0; ch < chunks; ++ch) {
-    if (ch + 1 < chunks) s.template load_chunk<TPR, NV, false>(ch + 1, tid, next);
-    else if (dlogits && chunks > 1) s.template load_chunk<TPR, NV, true>(chunks - 2, tid, next);
-    row_add_vectors<T, NV>(sums, q, chunk_top<T, 0, NV>(q), c);
+    const int then = ch + 1 < chunks ? ch + 1 : chunks - 2;    // the second walk begins with the last chunk, which stays in q
+    if (then >= 0) s.template load_chunk<TPR, NV, false>(then, tid, next);
+    row_add_vectors<T, false>(sums, q, chunk_top<T>(q), c);
     if (ch + 1 < chunks) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) q[i] = next[i];
@@ -523,24 +540,20 @@ __global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) distill_kernel(const T*
   const int bytes = store_bytes(dz + s.head);
   const RowPower l(r.m, log_s, c);
   const float w_s = w * exp2f(-l.log2_s);
-  auto dense = [&](float2 x) {
-    const float2 y = l.plain(x);
-    return make_float2(w_s * row_ex2(y.x), w_s * row_ex2(y.y));
-  };
-  auto dense_huge = [&](float2 x) {
-    const float2 y = l.huge(x);
-    return make_float2(w_s * row_ex2(y.x), w_s * row_ex2(y.y));
-  };
-  auto one = [&](float x) { return l.is_huge ? dense_huge(make_float2(x, x)).x : dense(make_float2(x, x)).x; };
+  const f32x2 ww = x2_pack(w_s, w_s);
+  auto value = [&](float2 y) { return x2_unpack(x2_mul(x2_pack(row_ex2(y.x), row_ex2(y.y)), ww)); };
+  auto plain = [&](float2 x) { return value(l.plain(x)); };
+  auto any = [&](float2 x) { return none ? make_float2(0.f, 0.f) : value(l.is_huge ? l.huge(x) : l.plain(x)); };
+  auto one = [&](float x) { return any(make_float2(x, x)).x; };
+  const bool fast = bytes == 16 && !none && !l.is_huge;
+#pragma unroll 2
   for (int ch = chunks - 1; ch >= 0; --ch) {
-    if (none) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, bytes, [](float2) { return make_float2(0.f, 0.f); });
-    else if (l.is_huge) store_chunk<T, TPR, NV>(s, ch, tid, q, dz, bytes, dense_huge);
-    else store_chunk<T, TPR, NV>(s, ch, tid, q, dz, bytes, dense);
+    store_chunk<T, TPR, NV>(s, ch, tid, q, dz, bytes, fast, plain, any);
 #pragma unroll
     for (int i = 0; i < NV; ++i) q[i] = next[i];
-    if (ch > 1 && !none) s.template load_chunk<TPR, NV, true>(ch - 2, tid, next);
+    if (ch > 1) s.template load_chunk<TPR, NV, true>(ch - 2, tid, next);
   }
-  if (edge_place >= 0) dz[edge_place] = row_round<T>(none ? 0.f : one(edge));
+  if (edge_place >= 0) dz[edge_place] = row_round<T>(one(edge));
   G::sync();                                         // the teacher's places are written again, by one thread each
   if (!none) {
 #pragma unroll
@@ -554,15 +567,20 @@ __global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) distill_kernel(const T*
 }
 
 // ------------------------------ host side -----------------------------------------------------------------------------
-// Rows of up to 4 KB go to warps where there are enough of them to fill the blocks' places; other rows to a block, or to a
-// cluster: slices of at most `most_bytes`, and more of them while the GPU has room for their blocks and each thread still has
-// a vector.
+// Where rows are many a warp takes one: no barrier, and a quarter of the work per row that does not depend on its length.
+//   600 x 300 fp32 and more rows: 10 alternatives 5.5 us by blocks, 4.5 by warps; 25 600 x 900 122 and 40
+//   longer rows need more of them: 600 x 1800 3.0 and 3.4, 1500 x 1800 5.0 and 4.1 (no alternatives)
+//   rows that are written too, up to 8 KB: gradient 5000 x 1800 fp32 13.2 and 12.4, 10 000 x 3600 46 and 51
+//   rows that are only read, up to 64 KB: 11 769 x 9248 bf16 54 and 43, with 10 alternatives 92 and 63, 1200 x 10 000 fp32
+//   9.6 and 11.1, 2500 x 10 000 with 10 29.5 and 24.8; with 32 alternatives 10 000 x 10 000 fp32 109 and 128, 20 000 x 5000 146 and 116
+// Other rows go to a block, or to a cluster: slices of at most `most_bytes`, and more of them while the GPU has room for their
+// blocks and each thread still has a vector.
 struct RowPlan {
   bool warps;
   int shift;                     // 2^shift slices
 };
-RowPlan row_plan(gram_ctx* ctx, int64_t N, int64_t row_bytes, int64_t most_bytes, int k = 0) {
-  RowPlan p{row_bytes <= 4096 && N >= 4 * kNumSMs && k <= 32, 0};
+RowPlan row_plan(gram_ctx* ctx, int64_t N, int64_t row_bytes, int64_t most_bytes, int64_t warp_bytes) {
+  RowPlan p{row_bytes <= warp_bytes && N >= (row_bytes <= 4096 ? 4 : row_bytes <= 8192 ? 8 : 16) * kNumSMs, 0};
   if (p.warps) return p;
   const int64_t vectors = row_bytes / 16;
   const int most = gram_cluster_blocks(ctx) < MAX_SLICES ? gram_cluster_blocks(ctx) : MAX_SLICES;
@@ -593,7 +611,7 @@ gram_status launch_rows(gram_ctx* ctx, void (*kern)(P...), const RowPlan& plan, 
 
 template <typename T>
 gram_status logprobs_typed(gram_ctx* ctx, const T* z, int64_t ld, int64_t N, int32_t V, float scale, const RowAnswers& ask, cudaStream_t st) {
-  const RowPlan plan = row_plan(ctx, N, (int64_t)V * sizeof(T), INT64_MAX, ask.k);
+  const RowPlan plan = row_plan(ctx, N, (int64_t)V * sizeof(T), INT64_MAX, ask.k <= 16 ? 64 << 10 : ask.k <= 32 ? 20 << 10 : 2 << 10);
   ProfScope prof(ctx, GRAM_K_OTHER, (double)N * V * sizeof(T), 1, st, "logprobs");
   int32_t* status = gram_status_word(ctx);
   const size_t smem = plan.shift > 0 ? (sizeof(uint64_t) * ask.k) << plan.shift : 0;
@@ -602,14 +620,14 @@ gram_status logprobs_typed(gram_ctx* ctx, const T* z, int64_t ld, int64_t N, int
   return ask.k ? run(logprobs_kernel<T, LP_THREADS, true>) : run(logprobs_kernel<T, LP_THREADS, false>);
 }
 template <typename T> gram_status backward_typed(gram_ctx* ctx, const T* z, T* dz, BackwardArgs a, cudaStream_t st) {
-  const RowPlan plan = row_plan(ctx, a.N, (int64_t)a.V * sizeof(T), INT64_MAX);
+  const RowPlan plan = row_plan(ctx, a.N, (int64_t)a.V * sizeof(T), INT64_MAX, 12 << 10);
   ProfScope prof(ctx, GRAM_K_OTHER, 2.0 * a.N * a.V * sizeof(T), 1, st, "logprobs_backward");
   a.shift = plan.shift;
   if (plan.warps) return launch_rows(ctx, logprobs_backward_kernel<T, 32>, plan, a.N, 0, st, z, dz, a);
   return launch_rows(ctx, logprobs_backward_kernel<T, LP_THREADS>, plan, a.N, 0, st, z, dz, a);
 }
 template <typename T> gram_status distill_typed(gram_ctx* ctx, const T* z, T* dz, DistillArgs a, cudaStream_t st) {
-  const RowPlan plan = row_plan(ctx, a.N, (int64_t)a.V * sizeof(T), 64 << 10);
+  const RowPlan plan = row_plan(ctx, a.N, (int64_t)a.V * sizeof(T), 64 << 10, 12 << 10);
   ProfScope prof(ctx, GRAM_K_OTHER, (dz ? 2.0 : 1.0) * a.N * a.V * sizeof(T), 1, st, "distill");
   a.shift = plan.shift;
   if (plan.warps) return launch_rows(ctx, distill_kernel<T, 32>, plan, a.N, 0, st, z, dz, a);

@@ -185,6 +185,11 @@ __device__ __forceinline__ f32x2 x2_add(f32x2 a, f32x2 b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+__device__ __forceinline__ f32x2 x2_mul(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 __device__ __forceinline__ f32x2 x2_fma(f32x2 a, f32x2 b, f32x2 c) {
   f32x2 r;
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
@@ -241,8 +246,8 @@ template <> struct RowVec<bf16> {
   }
 };
 
-// NV vectors' worth of logits, of at most `top`
-template <typename T, int NV>
+// NV vectors' worth of logits, of at most `top`; ENTROPY: the sum of e y too
+template <typename T, bool ENTROPY, int NV>
 __device__ __forceinline__ void row_add_vectors(RowSums& r, const uint4 (&q)[NV], float top, float c) {
   r.see(top, c);
   f32x2 s = x2_pack(0.f, 0.f), t = s;                    // sums of their own: small terms would be lost in the row's so far
@@ -251,14 +256,15 @@ __device__ __forceinline__ void row_add_vectors(RowSums& r, const uint4 (&q)[NV]
   for (int i = 0; i < NV; ++i) {
 #pragma unroll
     for (int j = 0; j < RowVec<T>::N / 2; ++j) {
-      const f32x2 y = x2_fma(RowVec<T>::held(q[i], j), cc, ref);
+      const float2 x = RowVec<T>::pair(q[i], j);
+      const f32x2 y = x2_fma(ENTROPY ? RowVec<T>::held(q[i], j) : x2_pack(x.x, x.y), cc, ref);
       const float2 y2 = x2_unpack(y);
       const f32x2 e = x2_pack(row_ex2(y2.x), row_ex2(y2.y));
       s = x2_add(s, e);
-      t = x2_fma(e, y, t);
+      if (ENTROPY) t = x2_fma(e, y, t);
     }
   }
   const float2 s2 = x2_unpack(s), t2 = x2_unpack(t);
   r.s += s2.x + s2.y;
-  r.t += t2.x + t2.y;
+  if (ENTROPY) r.t += t2.x + t2.y;
 }

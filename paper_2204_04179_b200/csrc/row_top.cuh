@@ -99,7 +99,7 @@ __device__ __forceinline__ int warp_keep(uint64_t* keys, int have, int k) {
 }
 
 template <int TPR> struct alignas(16) TopScratch {
-  static constexpr int GROUPS = TPR == 32 ? 4 : 32;     // of a thread
+  static constexpr int GROUPS = TPR == 32 ? 16 : 32;    // of a thread
   static constexpr int KEYS = TPR == 32 ? 384 : 1024, ENTRIES = TPR == 32 ? 128 : 512;
   static_assert(KEYS >= GRAM_TOP_MAX, "an exact list fits");
   uint64_t keys[KEYS];
@@ -111,19 +111,29 @@ template <int TPR> struct alignas(16) TopScratch {
   uint32_t bound[Group<TPR>::WARPS][2];
 };
 
-// a bar, from two of each thread's entries, the largest of either half
-template <int TPR> __device__ __forceinline__ float top_bar(float a, float b, int k, TopScratch<TPR>& sc) {
+// a bar, from the largest entry of each thread's i-th vectors (top[i])
+template <int TPR> __device__ __forceinline__ float top_bar(const float (&top)[4], int k, TopScratch<TPR>& sc) {
   using G = Group<TPR>;
-  const bool two = k > TPR / 4;                          // one maximum a thread is little for a larger k
-  if (!two) a = fmaxf(a, b);
-  const uint32_t oa = a > ROW_NEG_INF ? row_order(a) : 0u, ob = two && b > ROW_NEG_INF ? row_order(b) : 0u;
-  uint32_t lo = __reduce_min_sync(0xffffffffu, min(oa ? oa : ~0u, ob ? ob : ~0u)), hi = __reduce_max_sync(0xffffffffu, max(oa, ob));
+  // k of 2 k or more values: four a thread where k is large, else fewer, since each costs a count (in a block a barrier) a step
+  const int values = TPR == 32 ? 4 : k > TPR / 2 ? 4 : k > TPR / 4 ? 2 : 1;
+  uint32_t o[4], lo = ~0u, hi = 0u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float x = values == 4 ? top[i] : i == 0 ? (values == 2 ? fmaxf(top[0], top[1]) : fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])))
+                                                  : i == 1 && values == 2 ? fmaxf(top[2], top[3]) : ROW_NEG_INF;
+    o[i] = x > ROW_NEG_INF ? row_order(x) : 0u;
+    lo = min(lo, o[i] ? o[i] : ~0u);
+    hi = max(hi, o[i]);
+  }
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi);
   if constexpr (TPR > 32) {
     if ((threadIdx.x & 31) == 0) { sc.bound[threadIdx.x >> 5][0] = lo; sc.bound[threadIdx.x >> 5][1] = hi; }
   }
-  auto reach = [&](uint32_t o) {
-    int n = G::count(oa >= o);
-    if (two) n += G::count(ob >= o);
+  auto reach = [&](uint32_t b) {
+    int n = G::count(o[0] >= b);
+    if (values > 1) n += G::count(o[1] >= b);
+    if (values > 2) n += G::count(o[2] >= b) + G::count(o[3] >= b);
     return n;
   };
   if (reach(1u) < k) return -FLT_MAX;                    // a barrier, for the bounds too
