@@ -271,7 +271,7 @@ template <typename T> __device__ __forceinline__ void store_vector(T* at, const 
 }
 // pairs of logits -> pairs of results, over a chunk that is in registers: `plain` for whole chunks of rows that lie alike within 16
 // bytes, where `fast` says that it holds, and `any` otherwise (one straight line each: with the tests at every vector a gradient
-// took 10 instructions an element instead of @@)
+// took 10 instructions an element instead of 8)
 template <typename T, int TPR, int NV, typename F, typename A>
 __device__ __forceinline__ void store_chunk(const Slice<T>& s, int ch, int tid, const uint4 (&q)[NV], T* dz, int bytes, bool fast, F plain, A any) {
   const int v = s.v0 + ch * (TPR * NV) + tid;
@@ -456,7 +456,7 @@ struct DistillArgs {
 // A slice is walked over twice: forwards for the statistics, backwards for the gradient, whose reads find it in L2 (the last
 // chunk is still in registers).  The plan keeps the slices of the blocks that run together well below L2's size.
 template <typename T, int TPR>
-__global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) distill_kernel(const T* logits, T* dlogits, DistillArgs a) {
+__global__ void __launch_bounds__(LP_THREADS, TPR == 32 ? 6 : LP_PER_SM) distill_kernel(const T* logits, T* dlogits, DistillArgs a) {
   using G = Group<TPR>;
   using At = AtPlaces<TPR>;
   constexpr int NV = LP_NV;
@@ -570,7 +570,8 @@ __global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) distill_kernel(const T*
 // Where rows are many a warp takes one: no barrier, and a quarter of the work per row that does not depend on its length.
 //   600 x 300 fp32 and more rows: 10 alternatives 5.5 us by blocks, 4.5 by warps; 25 600 x 900 122 and 40
 //   longer rows need more of them: 600 x 1800 3.0 and 3.4, 1500 x 1800 5.0 and 4.1 (no alternatives)
-//   rows that are written too, up to 8 KB: gradient 5000 x 1800 fp32 13.2 and 12.4, 10 000 x 3600 46 and 51
+//   rows that are written too, up to 12 KB: gradient 8192 x 2500 fp32 31.9 and 27.9, 10 000 x 3600 46 and 51; distillation
+//   8192 x 2500 fp32 55 and 40, 10 000 x 6000 bf16 77 and 59
 //   rows that are only read, up to 64 KB: 11 769 x 9248 bf16 54 and 43, with 10 alternatives 92 and 63, 1200 x 10 000 fp32
 //   9.6 and 11.1, 2500 x 10 000 with 10 29.5 and 24.8; with 32 alternatives 10 000 x 10 000 fp32 109 and 128, 20 000 x 5000 146 and 116
 // Other rows go to a block, or to a cluster: slices of at most `most_bytes`, and more of them while the GPU has room for their

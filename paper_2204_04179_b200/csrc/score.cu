@@ -608,8 +608,11 @@ gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_u
                                   size_t ws_bytes, cudaStream_t st) {
   const int32_t all_units = ceil_div(V, SC_UNIT);
   if (all_units > (1 << 30) / (kNumSMs / 2)) return gram_set_error(ctx, "gram_score_logprobs: %d items", V), GRAM_ERR_UNSUPPORTED;
-  // Few users: their logits are written and read once more, in place of the sample, the bars and the joining.  64 users against
-  // 100 000 items of 768 with 10 alternatives @@ us this way and @@ the other, 128 users @@ and @@.
+  // Few users: their logits are written and read once more, in place of the sample, the bars and the joining.  Against 100 000
+  // items of 768, this way and the other: 10 alternatives, 1 user 39.9 and 52.4 us, 64 users 48.1 and 58.4; 128 users against
+  // 30 522 items 27.9 and 36.8.  100 alternatives of 64 users 72.9 and 88.6, but of 128 users against 30 522 items 60.9 and 50.3.
+  // Without alternatives the other way has no sample to take: 1 user 35.2 and 37.9, 64 users 42.5 and 39.0, but 17.4 and 21.0
+  // against 30 522 items.
   CUtensorMap map_u, map_i;
   // copies are no larger than the users (rows past the last are filled with zeros, which takes time: one user against 100 000
   // items of 768 46 us with boxes of 128 rows, 35 with boxes of 8)
@@ -626,7 +629,7 @@ gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_u
   a.c = scale * kLog2e;
   a.stride = 1;
   a.status = gram_status_word(ctx);
-  if (ask.k > 0 && N <= SM_ROWS && (int64_t)(ws_bytes / sizeof(float)) / ld_logits >= N) {
+  if (N <= SM_ROWS && (ask.k > 0 ? N * ask.k <= 64 * SM_ROWS : N * V <= (2 << 20)) && (int64_t)(ws_bytes / sizeof(float)) / ld_logits >= N) {
     if (!make_map(&map_u, users, (uint64_t)d, (uint64_t)N, (uint64_t)ld_users, SC_BK, (uint32_t)box_rows))
       return gram_set_error(ctx, "gram_score_logprobs: cannot describe the users"), GRAM_ERR_UNSUPPORTED;
     a.N = N;

@@ -113,6 +113,29 @@ def test_a_row_with_nan_or_infinity_keeps_to_itself(V):
     g.close()
 
 
+def _backward_reference(r, targets, dlogp, dH, dtype):
+    """(gradient by the formula, its bound) in 64 bits."""
+    N, V, C = len(r.z), r.V, 0 if targets is None else targets.shape[1]
+    gsum, at, mag = np.zeros(N), np.zeros((N, V)), np.zeros((N, V))
+    for c in range(C):
+        live = (targets[:, c] >= 0) & ~np.isneginf(r.at(r.z, targets[:, c:c + 1], -INF)[:, 0])
+        gl = np.where(live, dlogp[:, c].astype(float), 0.0)
+        np.add.at(at, (np.arange(N), np.maximum(targets[:, c], 0)), gl)
+        np.add.at(mag, (np.arange(N), np.maximum(targets[:, c], 0)), np.abs(gl))
+        gsum += gl
+    lp = np.where(r.p > 0, r.logp, 0.0)
+    h = np.zeros(N) if dH is None else dH.astype(float)
+    inner = gsum[:, None] + h[:, None] * (lp + r.H[:, None])
+    want = r.scale * np.where(np.isneginf(r.z), 0.0, at - r.p * inner)
+    # log p from rounded statistics: 2 u |log s| more; the factor's own roundings: d_logp |h| + 8 u of its parts
+    size = np.abs(gsum)[:, None] + np.abs(h)[:, None] * (np.abs(lp) + r.H[:, None])
+    d_lp = r.d_logp + 2 * U * np.abs(np.where(r.empty, 0, r.log_s))[:, None]
+    bound = r.scale * (r.d_p * size + r.p * (np.abs(h)[:, None] * d_lp + (16 + C) * U * size + C * U * mag.sum(1, keepdims=True)) + (8 + C) * U * mag) + 1e-37
+    if dtype == "bf16":
+        bound = bound * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(want)
+    return want, bound
+
+
 @pytest.mark.parametrize("what", ["both", "tokens", "entropy"])
 @pytest.mark.parametrize("N,V,dtype,pad,offset", SIZES)
 def test_logprobs_backward(N, V, dtype, pad, offset, what):
@@ -132,24 +155,7 @@ def test_logprobs_backward(N, V, dtype, pad, offset, what):
     if N > 4 and C:
         targets[3] = -1                                  # a row with nothing given
     up = lambda a: None if a is None else torch.from_numpy(a).to(DEV)  # noqa: E731
-    # by the formula
-    gsum, at, mag = np.zeros(N), np.zeros((N, V)), np.zeros((N, V))
-    for c in range(C):
-        live = (targets[:, c] >= 0) & ~np.isneginf(r.at(z, targets[:, c:c + 1], -INF)[:, 0])
-        gl = np.where(live, dlogp[:, c].astype(float), 0.0)
-        np.add.at(at, (np.arange(N), np.maximum(targets[:, c], 0)), gl)
-        np.add.at(mag, (np.arange(N), np.maximum(targets[:, c], 0)), np.abs(gl))
-        gsum += gl
-    lp = np.where(r.p > 0, r.logp, 0.0)
-    h = np.zeros(N) if dH is None else dH.astype(float)
-    inner = gsum[:, None] + h[:, None] * (lp + r.H[:, None])
-    want = scale * np.where(np.isneginf(z), 0.0, at - r.p * inner)
-    # log p from rounded statistics: 2 u |log s| more; the factor's own roundings: d_logp |h| + 8 u of its parts
-    size = np.abs(gsum)[:, None] + np.abs(h)[:, None] * (np.abs(lp) + r.H[:, None])
-    d_lp = r.d_logp + 2 * U * np.abs(np.where(r.empty, 0, r.log_s))[:, None]
-    bound = scale * (r.d_p * size + r.p * (np.abs(h)[:, None] * d_lp + (16 + C) * U * size + C * U * mag.sum(1, keepdims=True)) + (8 + C) * U * mag) + 1e-37
-    if dtype == "bf16":
-        bound = bound * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(want)
+    want, bound = _backward_reference(r, targets, dlogp, dH, dtype)
     g = context()
     for same in (False, True):
         if same:
@@ -317,6 +323,164 @@ def test_distill_against_differences():
     g.distill(view, up(ids), up(a), loss, scale=scale, dlogits=dz)
     near(dz, want, 2.0 ** -8 / 6 + 2.0 ** -15, "differences")
     g.sync()
+    g.close()
+
+
+# V, type, elements between rows, elements ahead, k: as many rows as give each one a warp (the few are repeated)
+MANY = [(1, "f32", 0, 0, 1), (7, "bf16", 1, 1, 5), (300, "f32", 0, 0, 128), (1000, "bf16", 0, 3, 128), (1029, "f32", 3, 1, 10), (2500, "f32", 0, 0, 32),
+        (3001, "bf16", 2, 5, 16), (5000, "f32", 0, 0, 31), (10_001, "bf16", 0, 0, 20), (16_384, "f32", 0, 0, 16), (16_381, "f32", 2, 3, 10),
+        (32_760, "bf16", 1, 7, 3), (20_000, "bf16", 0, 0, 0)]
+
+
+def _tiled(few, N, dtype, pad, offset):
+    base, z = place(few, dtype)
+    flat, view = buffer(N, few.shape[1], dtype, pad, offset)
+    view.copy_(base.repeat(-(-N // len(few)), 1)[:N])
+    return flat, view, z
+
+
+def _same(a, n, what, bound=None):
+    """Each group of n rows holds, to the bit, what the first n hold; within twice `bound` of it where one is given (repeated rows
+    of another alignment, whose sums take another order)."""
+    a = torch.nan_to_num(a.double(), nan=1.25e40, posinf=1.5e40, neginf=-1.5e40)
+    wide = lambda x: x.repeat(-(-len(a) // n), *[1] * (x.dim() - 1))[:len(a)]  # noqa: E731
+    if bound is None:
+        assert torch.equal(a, wide(a[:n])), what
+    else:
+        bound = torch.from_numpy(np.broadcast_to(np.where(np.isfinite(bound), bound, 0.0), a[:n].shape).copy()).to(a.device)
+        assert ((a - wide(a[:n])).abs() <= 2 * wide(bound)).all(), what
+
+
+@pytest.mark.parametrize("V,dtype,pad,offset,k", MANY)
+def test_logprobs_of_many_rows(V, dtype, pad, offset, k):
+    N = 2400
+    few = np.concatenate([_special(V, float(torch.finfo(DT[dtype]).min)), _draw(6, V, V)[1]])
+    n = len(few)
+    flat, view, z = _tiled(few, N, dtype, pad, offset)
+    targets = _targets(np.random.default_rng(V), n, V, 3)
+    g = context()
+    out = answers(N, 3, k)
+    g.logprobs(view, scale=0.5, targets=torch.from_numpy(np.tile(targets, (N // n + 1, 1))[:N].copy()).to(DEV), **out)
+    g.sync()
+    r = Rows(z, 0.5)
+    check_answers({x: None if out[x] is None else out[x][:n] for x in out}, r, targets, k)
+    aligned = (V + pad) * view.element_size() % 16 == 0
+    bounds = dict(stats=np.stack([np.zeros(n), r.d_log_s], 1), entropy=r.d_H, logp=r.at(r.d_logp, targets, 0.0))
+    if k:
+        bounds["top_logp"] = r.at(r.d_logp, r.top(k), 0.0)
+    for x in out:
+        if out[x] is not None:
+            _same(out[x], n, x, None if aligned else bounds.get(x))
+    view[5] = float("nan")                               # of one warp's row; its neighbours in the block keep theirs
+    view[6, V - 1] = INF
+    again = answers(N, 0, k)
+    g.logprobs(view, scale=0.5, **again)
+    g.sync()
+    assert torch.isnan(again["entropy"][5:7]).all() and torch.isnan(again["stats"][5:7, 1]).all()
+    rest = [i for i in range(N) if i not in (5, 6)]
+    for x in ("stats", "entropy", "top_logp", "top_ids"):
+        assert again[x] is None or torch.equal(again[x][rest], out[x][rest])
+    if k:
+        ids = again["top_ids"].cpu().numpy()
+        assert ids[6, 0] == V - 1 and ((ids >= -1) & (ids < V)).all()
+    g.close()
+
+
+@pytest.mark.parametrize("order", ["ascending", "descending", "equal", "few values", "one warp's places"])
+@pytest.mark.parametrize("V,dtype,k", [(9000, "f32", 16), (5000, "f32", 32), (500, "f32", 128), (30_000, "bf16", 12), (20_000, "f32", 128), (90_000, "f32", 100)])
+def test_alternatives_that_crowd_together(V, dtype, k, order):
+    """Rows whose better logits fall to few threads, or tie, with a warp, a block and a cluster a row."""
+    i = np.arange(V)
+    z = {"ascending": i / 256.0, "descending": -i / 256.0, "equal": np.zeros(V), "few values": (i % 7) * 0.5,
+         "one warp's places": np.where(i // 4 % 32 == 3, 8.0 + (i % 11) / 16.0, -(i % 97) / 64.0)}[order]
+    for N in (1, 200, 2400):
+        flat, view, want = _tiled(z[None], N, dtype, 0, 0)
+        g = context()
+        out = answers(N, 0, k)
+        g.logprobs(view, **out)
+        g.sync()
+        check_answers({x: None if out[x] is None else out[x][:1] for x in out}, Rows(want, 1.0), None, k)
+        for x in ("stats", "entropy", "top_logp", "top_ids"):
+            _same(out[x], 1, x)
+        g.close()
+
+
+@pytest.mark.parametrize("k", [1, 17, 128])
+@pytest.mark.parametrize("V,dtype,pad,offset", [(1, "f32", 0, 0), (9, "bf16", 0, 1), (700, "f32", 0, 0), (1999, "bf16", 3, 5), (2048, "f32", 0, 0),
+                                                (3000, "f32", 0, 0), (2999, "f32", 1, 3), (6000, "bf16", 2, 1), (6144, "bf16", 0, 0)])
+def test_gradients_of_many_rows(V, dtype, pad, offset, k):
+    N = 2400
+    rng, few = _draw(16, V, V + k)
+    few[1] = -INF
+    few[2] = np.where(np.arange(V) % 2 == 0, float(torch.finfo(DT[dtype]).min), -INF)
+    n = len(few)
+    flat, view, z = _tiled(few, N, dtype, pad, offset)
+    r = Rows(z, 0.5)
+    ids = np.where(rng.random((n, k)) < 0.15, -1, rng.integers(0, V, (n, k))).astype(np.int32)
+    a = (rng.standard_normal((n, k)) * 3).astype(np.float32)
+    weight = rng.random(n).astype(np.float32)
+    ids[3], weight[4] = -1, 0.0
+    up = lambda x: torch.from_numpy(np.concatenate([x] * (N // n)).copy()).to(DEV)  # noqa: E731
+    loss, d_loss, want, bound = _distill_reference(r, ids, a.astype(float), weight)
+    if dtype == "bf16":
+        bound = bound * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(want)
+    g = context()
+    got = torch.full((N,), float("nan"), device=DEV)
+    out, dz = buffer(N, V, dtype, pad, offset)
+    g.distill(view, up(ids), up(a), got, scale=0.5, weight=up(weight), dlogits=dz)
+    g.sync()
+    near(got[:n], loss, d_loss, "loss")
+    near(dz[:n], want, bound, "gradient")
+    aligned = (V + pad) * view.element_size() % 16 == 0
+    _same(got, n, "loss", None if aligned else d_loss)
+    _same(dz, n, "gradient", None if aligned else bound)
+    stats, H = np.stack([r.m, r.log_s], 1).astype(np.float32), r.H.astype(np.float32)
+    dh = rng.standard_normal(n).astype(np.float32)
+    there = dz.clone()
+    g.logprobs_backward(view, up(stats), dz, scale=0.5, targets=up(ids), dlogp=up(a), entropy=up(H), dentropy=up(dh))
+    g.sync()
+    want, bound = _backward_reference(r, ids, a, dh, dtype)
+    near(dz[:n], want, bound, "backward")
+    _same(dz, n, "backward", None if aligned else bound)
+    g.distill(view, up(ids), up(a), got, scale=0.5, weight=up(weight), dlogits=view)      # in place
+    g.sync()
+    assert torch.equal(view, there)
+    dz.fill_(float("nan"))
+    assert torch.isnan(out).all()
+    g.close()
+
+
+@pytest.mark.parametrize("blocks", [1, 2, 4])
+def test_with_smaller_clusters(blocks):
+    """Where the device places no cluster of 8, or none at all, rows are cut into fewer slices."""
+    N, V, k = 5, 70_001, 40
+    rng, z = _draw(N, V, 2)
+    z[1] = -INF
+    view, z = place(z, "f32", 2, 1)
+    r = Rows(z, 0.5)
+    ids = rng.integers(0, V, (N, k)).astype(np.int32)
+    a = rng.standard_normal((N, k)).astype(np.float32)
+    up = lambda x: torch.from_numpy(x).to(DEV)  # noqa: E731
+    loss, d_loss, want, bound = _distill_reference(r, ids, a.astype(float), np.ones(N))
+    g = context()
+    g.selftest_cluster_blocks(blocks)
+    out = answers(N, k, k)
+    g.logprobs(view, scale=0.5, targets=up(ids), **out)
+    g.sync()
+    check_answers(out, r, ids, k)
+    dz, got = torch.empty(N, V, device=DEV), torch.empty(N, device=DEV)
+    dl, dh = up(a), up(a[:, 0].copy())
+    g.logprobs_backward(view, out["stats"], dz, scale=0.5, targets=up(ids), dlogp=dl, entropy=out["entropy"], dentropy=dh)
+    whole, back = context(), torch.empty_like(dz)
+    whole.logprobs_backward(view, out["stats"], back, scale=0.5, targets=up(ids), dlogp=dl, entropy=out["entropy"], dentropy=dh)
+    whole.sync()
+    g.sync()
+    assert torch.equal(dz, back)
+    whole.close()
+    g.distill(view, up(ids), up(a), got, scale=0.5, dlogits=view)
+    g.sync()
+    near(got, loss, d_loss, "loss")
+    near(view, want, bound, "gradient")
     g.close()
 
 

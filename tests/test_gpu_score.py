@@ -100,6 +100,64 @@ def test_score_with_ties_and_nothing_left(N):
     g.close()
 
 
+@pytest.mark.parametrize("N,V,k", [(128, 3000, 64), (128, 3000, 65), (63, 3000, 128), (65, 3000, 128), (129, 3000, 64), (1, 8_500_000, 10), (1, 8_300_000, 10),
+                                   (64, 32_768, 0), (64, 32_769, 0), (65, 32_768, 0)])
+def test_score_where_the_way_changes(N, V, k):
+    """Few users' logits are written and read again; more users, alternatives or items than the workspace holds are not."""
+    d = 8
+    rng = np.random.default_rng(N + k)
+    users, u = _codes(rng, N, d, 0)
+    items, w = _codes(rng, V, d, 0)
+    targets = np.where(rng.random((N, 2)) < 0.2, -1, rng.integers(0, V, (N, 2))).astype(np.int32)
+    g = context()
+    out = answers(N, 2, k)
+    g.score_logprobs(users, items, scale=0.3, targets=torch.from_numpy(targets).to(DEV), **out)
+    g.sync()
+    check_answers(out, Rows(u @ w.T, 0.3), targets, k)
+    g.close()
+
+
+@pytest.mark.parametrize("N", [3, 200])
+def test_items_out_of_range_are_recorded_and_count_as_none(N):
+    rng = np.random.default_rng(N)
+    users, u = _codes(rng, N, 64, 0)
+    items, w = _codes(rng, 500, 64, 0)
+    t = np.zeros((N, 1), np.int32)
+    t[1], t[2] = 500, -2
+    g = context()
+    for k in (0, 3):
+        out = answers(N, 1, k)
+        g.score_logprobs(users, items, scale=0.05, targets=torch.from_numpy(t).to(DEV), **out)
+        with pytest.raises(binding.GramError) as e:
+            g.sync()
+        assert e.value.status == 2
+        check_answers(out, Rows(u @ w.T, 0.05), np.where((t < 0) | (t >= 500), -1, t), k)
+    g.sync()
+    g.close()
+
+
+def test_score_on_another_stream_behind_its_work():
+    rng = np.random.default_rng(7)
+    for N in (20, 300):
+        users, u = _codes(rng, N, 64, 0)
+        items, w = _codes(rng, 5000, 64, 0)
+        late = torch.zeros_like(users)
+        g = context()
+        out = answers(N, 0, 3)
+        torch.cuda.synchronize()
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            a = torch.randn(4096, 4096, device=DEV)
+            for _ in range(20):
+                a = a @ a * 1e-3
+            late.copy_(users)
+            g.score_logprobs(late, items, scale=0.05, **out)
+            late.zero_()
+        g.sync(s)
+        check_answers(out, Rows(u @ w.T, 0.05), None, 3)
+        g.close()
+
+
 @pytest.mark.parametrize("order", [1, -1])
 def test_score_of_a_sorted_table(order):
     """Items in ascending and descending order of their score: every one, or none, is better than those before it."""
