@@ -334,8 +334,8 @@ gram_status gram_logprobs_backward(gram_ctx* ctx, const void* d_logits, int dtyp
                                    const float* d_dlogp, const float* d_dentropy, void* d_dlogits, int64_t ld_out,
                                    gram_stream stream);
 /* Distillation from a teacher's top logits: d_teacher_ids, d_teacher_logits [N, k] are a row's best entries by the teacher
- * (logits or log probabilities: gram_logprobs' alternatives as they stand).  An entry takes no part if its ID is -1, its own
- * logit is -inf, or the student's logit there is masked out.  With q the softmax of scale * teacher logits over the entries
+ * (logits, or log probabilities at scale 1: gram_logprobs' alternatives as they stand; they are scaled here, as the
+ * student's logits are).  An entry takes no part if its ID is -1, its own logit is -inf, or the student's logit there is masked out.  With q the softmax of scale * teacher logits over the entries
  * left (entries of one place add up) and p the student's softmax over the whole row,
  *   d_loss[n] = sum_j q_j (log q_j - log p(id_j)),     0 where no entry is left
  *   d_dlogits[n, v] = weight[n] scale (p_v - sum of q_j over id_j = v),  the gradient of sum_n weight[n] loss[n]
@@ -344,9 +344,11 @@ gram_status gram_logprobs_backward(gram_ctx* ctx, const void* d_logits, int dtyp
 gram_status gram_distill(gram_ctx* ctx, const void* d_logits, int dtype, int64_t ld, int64_t N, int32_t V, float scale,
                          const int32_t* d_teacher_ids, const float* d_teacher_logits, int32_t k, float* d_loss,
                          const float* d_weight, void* d_dlogits, int64_t ld_out, gram_stream stream);
-/* gram_logprobs of z[n, v] = users[n, :] . items[v, :] + bias[v] without the logits ever being written: d_users bf16 [N, d]
- * and d_items bf16 [V, d] with rows ld_users and ld_items elements apart (multiples of 8, addresses 16-byte aligned: else
- * GRAM_ERR_UNSUPPORTED), d_bias fp32 [V] or NULL (-inf takes an item out), products summed in fp32. */
+/* gram_logprobs of z[n, v] = users[n, :] . items[v, :] + bias[v] without an [N, V] array: d_users bf16 [N, d] and d_items
+ * bf16 [V, d] with rows ld_users and ld_items elements apart (multiples of 8, addresses 16-byte aligned: else
+ * GRAM_ERR_UNSUPPORTED), d_bias fp32 [V] or NULL (-inf takes an item out), products summed in fp32.  Lists of candidates, and the
+ * logits of few users, lie in the context's workspace for matrix products (32 MB at least), as the partial sums of a product
+ * do: calls of one context are ordered on one stream or by events. */
 gram_status gram_score_logprobs(gram_ctx* ctx, const void* d_users, int64_t ld_users, const void* d_items, int64_t ld_items,
                                 const float* d_bias, int64_t N, int32_t V, int32_t d, float scale, const int32_t* d_targets,
                                 int32_t C, float* d_logp, float* d_stats, float* d_entropy, float* d_top_logp,
