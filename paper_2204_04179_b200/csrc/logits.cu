@@ -117,7 +117,7 @@ template <typename T, int TPR> __device__ __forceinline__ RowLogs row_logs(const
 
 // ------------------------------ log probabilities ---------------------------------------------------------------------
 template <typename T, int TPR, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) logprobs_kernel(const T* logits, int64_t ld, int64_t N, int32_t V, float scale, int32_t shift,
+__global__ void __launch_bounds__(LP_THREADS, TOP && TPR == 32 ? 7 : LP_PER_SM) logprobs_kernel(const T* logits, int64_t ld, int64_t N, int32_t V, float scale, int32_t shift,
                                                                  RowAnswers ask, int32_t* status) {
   using G = Group<TPR>;
   constexpr int NV = LP_NV;
@@ -125,7 +125,8 @@ __global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) logprobs_kernel(const T
   __shared__ RowStat part[LP_WARPS], of_slice[MAX_SLICES];
   __shared__ float fpart[LP_WARPS];
   __shared__ __align__(16) uint8_t scratch[TOP ? sizeof(TopScratch<TPR>) * (LP_THREADS / TPR) : 16];
-  extern __shared__ uint64_t merged[];                  // [slices, k], sorted, in the first block of a cluster
+  extern __shared__ uint64_t merged[];                  // [slices, k]: every slice's best, sorted, zeros behind them
+  __shared__ uint64_t of_have[MAX_SLICES];
   const int slices = TPR == 32 ? 1 : 1 << shift, tid = G::tid(), rank = blockIdx.x & (slices - 1);
   const int64_t n = TPR == 32 ? (int64_t)blockIdx.x * LP_WARPS + G::row() : blockIdx.x >> shift;
   if (TPR > 32 && slices > 1) gram_cluster_sync();      // every block of the cluster runs before another writes to it
@@ -182,28 +183,29 @@ __global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) logprobs_kernel(const T
     if (edge_place >= 0) tops[0] = fmaxf(tops[0], edge);
     const float bar = top_bar<TPR>(tops, ask.k, sc);
     have = top_collect<T, TPR, NV>(sc, TopSource{s.vectors(), s.head, s.v0, s.v1, edge, edge_place}, group, group_shift, bar, ask.k);
+    top_sort<TPR>(sc.keys, have);
   }
   if (TPR > 32 && slices > 1) {
-    if (tid == 0) put_stat(&of_slice[rank], 0, r);
-    if constexpr (TOP) {                              // this slice's best, sorted, to the first block
-      for (int i = tid; i < have; i += TPR) {
-        const uint64_t key = list[i];
-        const int above = top_rank(list, have, key);
-        if (above < ask.k) put_key(&merged[rank * ask.k + above], 0, key);
+    if (TOP ? tid < slices : tid == 0) put_stat(&of_slice[rank], tid, r);
+    if constexpr (TOP) {                                // this slice's best to every block, whose places each block then finds for its own
+      if (tid < slices) put_key(&of_have[rank], tid, min(have, ask.k));
+      for (int i = tid; i < max(have, ask.k); i += TPR) {
+        const int at = i < have ? top_above<TPR>(list, have, i) : i;
+        if (at < ask.k)
+          for (int b = 0; b < slices; ++b) put_key(&merged[rank * ask.k + at], b, i < have ? list[i] : 0);
       }
-      for (int i = have + tid; i < ask.k; i += TPR) put_key(&merged[rank * ask.k + i], 0, 0);
     }
     gram_cluster_sync();
-    if (rank != 0) return;
+    if (!TOP && rank != 0) return;
     r = join_slices(of_slice, slices, c);
   }
   const RowLogs logs = row_logs<T, TPR>(r, s.z, V, c, fpart);
   const float log_s = logs.log_s;
-  if (tid == 0) {
+  if (tid == 0 && rank == 0) {
     if (ask.stats) { ask.stats[2 * n] = r.m; ask.stats[2 * n + 1] = log_s; }
     if (ask.entropy) ask.entropy[n] = logs.entropy;
   }
-  for (int i = tid; i < ask.C; i += TPR) {
+  for (int i = tid; rank == 0 && i < ask.C; i += TPR) {
     const int32_t t = ask.targets[n * ask.C + i];
     if (t < -1 || t >= V) gram_device_fail(status, GRAM_ERR_ID_RANGE);
     ask.logp[n * ask.C + i] = t >= 0 && t < V ? row_logp(row_load(s.z + t), r.m, log_s, scale) : 0.f;
@@ -216,31 +218,30 @@ __global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) logprobs_kernel(const T
     };
     if (TPR == 32 || slices == 1) {
       for (int i = tid; i < have; i += TPR) {
-        const uint64_t key = list[i];
-        const int above = top_rank(list, have, key);
-        if (above < ask.k) answer(above, key);
+        const int above = top_above<TPR>(list, have, i);
+        if (above < ask.k) answer(above, list[i]);
       }
       for (int i = have + tid; i < ask.k; i += TPR) answer(i, 0);
     } else {
+      const int first_step = 1 << (31 - __clz(ask.k));
       int found = 0;
-      for (int i = tid; i < slices * ask.k; i += TPR) {
-        const uint64_t key = merged[i];
-        if (!key) continue;
-        ++found;
+      for (int b = 0; b < slices; ++b) found += (int)of_have[b];
+      for (int i = tid; i < (int)of_have[rank]; i += TPR) {
+        const uint64_t key = merged[rank * ask.k + i];
         int at = 0;
-        for (int b = 0; b < slices; ++b) {            // keys of list b above this one: the lists descend, zeros last
-          int lo = 0, hi = ask.k;
-          while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (merged[b * ask.k + mid] > key) lo = mid + 1;
-            else hi = mid;
+        for (int b = 0; b < slices; b += 2) {           // there are two slices at least; keys of both lists above this one
+          int lo0 = 0, lo1 = 0;
+          const uint64_t *l0 = merged + b * ask.k, *l1 = l0 + ask.k;
+          for (int step = first_step; step > 0; step >>= 1) {
+            if (lo0 + step <= ask.k && l0[lo0 + step - 1] > key) lo0 += step;
+            if (lo1 + step <= ask.k && l1[lo1 + step - 1] > key) lo1 += step;
           }
-          at += lo;
+          at += lo0 + lo1;
         }
         if (at < ask.k) answer(at, key);
       }
-      found = G::sum(found, sc.part);
-      for (int i = found + tid; i < ask.k; i += TPR) answer(i, 0);
+      if (rank == 0)
+        for (int i = found + tid; i < ask.k; i += TPR) answer(i, 0);
     }
   }
 }
@@ -568,12 +569,15 @@ __global__ void __launch_bounds__(LP_THREADS, TPR == 32 ? 6 : LP_PER_SM) distill
 
 // ------------------------------ host side -----------------------------------------------------------------------------
 // Where rows are many a warp takes one: no barrier, and a quarter of the work per row that does not depend on its length.
-//   600 x 300 fp32 and more rows: 10 alternatives 5.5 us by blocks, 4.5 by warps; 25 600 x 900 122 and 40
+//   700 x 900 fp32 and more rows: 10 alternatives 6.2 us by blocks, 5.6 by warps; 20 000 x 900 93 and 35
 //   longer rows need more of them: 600 x 1800 3.0 and 3.4, 1500 x 1800 5.0 and 4.1 (no alternatives)
 //   rows that are written too, up to 12 KB: gradient 8192 x 2500 fp32 31.9 and 27.9, 10 000 x 3600 46 and 51; distillation
 //   8192 x 2500 fp32 55 and 40, 10 000 x 6000 bf16 77 and 59
-//   rows that are only read, up to 64 KB: 11 769 x 9248 bf16 54 and 43, with 10 alternatives 92 and 63, 1200 x 10 000 fp32
-//   9.6 and 11.1, 2500 x 10 000 with 10 29.5 and 24.8; with 32 alternatives 10 000 x 10 000 fp32 109 and 128, 20 000 x 5000 146 and 116
+//   rows that are only read, up to 40 KB: 10 000 x 5000 fp32 40 and 36, 25 600 x 10 000 157 and 152, with 10 alternatives 207 and
+//   193; rows of 64 KB 55 and 64
+//   with 32 alternatives up to 32 KB: 10 000 x 16 000 bf16 96 and 88, 40 KB 94 and 111
+//   with 64 alternatives up to 20 KB: 10 000 x 5000 fp32 84 and 79, 40 KB 108 and 146; with 128 up to 2 KB: 20 000 x 400 293 and 233,
+//   20 000 x 900 195 and 402 (a warp's lists run over)
 // Other rows go to a block, or to a cluster: slices of at most `most_bytes`, and more of them while the GPU has room for their
 // blocks and each thread still has a vector.
 struct RowPlan {
@@ -612,7 +616,7 @@ gram_status launch_rows(gram_ctx* ctx, void (*kern)(P...), const RowPlan& plan, 
 
 template <typename T>
 gram_status logprobs_typed(gram_ctx* ctx, const T* z, int64_t ld, int64_t N, int32_t V, float scale, const RowAnswers& ask, cudaStream_t st) {
-  const RowPlan plan = row_plan(ctx, N, (int64_t)V * sizeof(T), INT64_MAX, ask.k <= 16 ? 64 << 10 : ask.k <= 32 ? 20 << 10 : 2 << 10);
+  const RowPlan plan = row_plan(ctx, N, (int64_t)V * sizeof(T), INT64_MAX, ask.k <= 16 ? 40 << 10 : ask.k <= 32 ? 32 << 10 : ask.k <= 64 ? 20 << 10 : 2 << 10);
   ProfScope prof(ctx, GRAM_K_OTHER, (double)N * V * sizeof(T), 1, st, "logprobs");
   int32_t* status = gram_status_word(ctx);
   const size_t smem = plan.shift > 0 ? (sizeof(uint64_t) * ask.k) << plan.shift : 0;

@@ -98,9 +98,12 @@ __device__ __forceinline__ int warp_keep(uint64_t* keys, int have, int k) {
   return at;
 }
 
+// (20 KB a block: what eight of them leave of an SM's memory is L1, where loads in flight have their place.  With 26 KB rows of
+// 100 000 fp32 were read at 5100 GB/s instead of 6200; with half the groups, whose entries are then twice as long, 64 alternatives
+// of 2368 such rows take 189 us instead of 174.)
 template <int TPR> struct alignas(16) TopScratch {
   static constexpr int GROUPS = TPR == 32 ? 16 : 32;    // of a thread
-  static constexpr int KEYS = TPR == 32 ? 384 : 1024, ENTRIES = TPR == 32 ? 128 : 512;
+  static constexpr int KEYS = 384, ENTRIES = TPR == 32 ? 128 : 256;
   static_assert(KEYS >= GRAM_TOP_MAX, "an exact list fits");
   uint64_t keys[KEYS];
   float group[GROUPS * TPR];
@@ -244,7 +247,7 @@ template <int TPR> __device__ __noinline__ int top_keep(TopScratch<TPR>& sc, int
   __syncthreads();
   return left;
 }
-// The candidates of a row or slice, as keys in sc.keys: at least its best k, or all there are; a 0 behind an odd number of them.
+// The candidates of a row or slice, as keys in sc.keys: at least its best k, or all there are.
 // Group g holds the thread's vectors of chunks [g << shift, (g + 1) << shift), NV a chunk, TPR apart.  sc.entries and sc.found
 // are 0 before, behind a barrier; a barrier is behind what this leaves.
 template <typename T, int TPR, int NV>
@@ -274,29 +277,92 @@ __device__ __forceinline__ int top_collect(TopScratch<TPR>& sc, const TopSource&
   if (entries <= Sc::ENTRIES) {
     static_assert(NV == 4, "the vectors of a group are a power of two");
     const int per = 2 + shift;                           // 2^per of them
-    for (int i = tid; i < entries << per; i += TPR) {
-      const int e = sc.entry[i >> per], j = i & ((1 << per) - 1);
-      const int v = src.v0 + (((e / TPR) << per) + j) * TPR + e % TPR;
-      if (v < src.v1) each_of<T>(src.from[v], src.place0 + v * RowVec<T>::N, put);
+    constexpr int NL = TPR == 32 ? 2 : NV;               // vectors of a thread on their way before the first is looked at
+    for (int i0 = tid; i0 < entries << per; i0 += NL * TPR) {
+      uint4 q[NL];
+      int v[NL];
+#pragma unroll
+      for (int l = 0; l < NL; ++l) {
+        const int i = i0 + l * TPR;
+        constexpr uint32_t none = RowVec<T>::NONE;
+        q[l] = make_uint4(none, none, none, none);
+        v[l] = src.v1;
+        if (i < entries << per) {
+          const int e = sc.entry[i >> per];
+          v[l] = src.v0 + (((e / TPR) << per) + (i & ((1 << per) - 1))) * TPR + e % TPR;
+        }
+        if (v[l] < src.v1) q[l] = src.from[v[l]];
+      }
+#pragma unroll
+      for (int l = 0; l < NL; ++l) {
+        if (l > 0 && i0 - tid + l * TPR >= entries << per) break;
+        uint32_t in = 0;                                 // its entries that reach the bar (-FLT_MAX at least)
+        int bit = 0;
+        each_of<T>(q[l], 0, [&](float x, int) { in |= (x >= bar ? 1u : 0u) << bit++; });
+        if (!in) continue;
+        int at = atomicAdd(&sc.found, __popc(in));
+        const T* z = reinterpret_cast<const T*>(src.from + v[l]);
+        for (; in; in &= in - 1, ++at) {
+          const int j = __ffs(in) - 1;
+          if (at < Sc::KEYS) sc.keys[at] = row_key(row_load(z + j), src.place0 + v[l] * RowVec<T>::N + j);
+        }
+      }
     }
   }
   G::sync();
   int have = sc.found;
   if (entries > Sc::ENTRIES || have > Sc::KEYS) have = top_exact<T, TPR>(sc, src, k);
   else if (have > 2 * k + 96) have = top_keep<TPR>(sc, have, k);     // counting takes have^2 comparisons
-  if (have & 1) {                                        // read in pairs
-    if (tid == 0) sc.keys[have] = 0;
-    G::sync();
-  }
   return have;
 }
-// keys of the list above this one
-__device__ __forceinline__ int top_rank(const uint64_t* list, int have, uint64_t key) {
-  int above = 0;
+// The order of keys by counting, of few against all others.  A block's longer lists are sorted in segments of 32 first, a warp
+// each; a key's place is then its own in its segment plus those of the other segments' above it, found by bisection: 128
+// alternatives of 25 600 rows of 10 000 fp32 take 330 us so, 371 by counting alone.  A warp's lists are short (10 alternatives of
+// those rows 193 us by counting, 200 with the choice).  The keys' array holds a whole number of segments; barriers are ahead of
+// top_sort and behind it.
+constexpr int TOP_COUNTED = 64;
+template <int TPR> __device__ __forceinline__ void top_sort(uint64_t* keys, int have) {
+  const int lane = threadIdx.x & 31;
+  if (TPR == 32 || have <= TOP_COUNTED) {
+    if (!(have & 1)) return;
+    if (Group<TPR>::tid() == 0) keys[have] = 0;          // they are read in pairs
+  } else {
+    for (int base = Group<TPR>::tid() - lane; base < have; base += TPR) {
+      const uint64_t key = base + lane < have ? keys[base + lane] : 0;
+      if (!key) keys[base + lane] = 0;
+      __syncwarp();
+      int above = 0;
 #pragma unroll 4
-  for (int j = 0; j < have; j += 2) {
-    const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(list + j);
-    above += (v.x > key) + (v.y > key);
+      for (int j = 0; j < 32; j += 2) {
+        const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(keys + base + j);
+        above += (v.x > key) + (v.y > key);
+      }
+      __syncwarp();
+      if (key) keys[base + above] = key;
+    }
+  }
+  Group<TPR>::sync();
+}
+// how many keys are above the i-th
+template <int TPR> __device__ __forceinline__ int top_above(const uint64_t* keys, int have, int i) {
+  const uint64_t key = keys[i];
+  if (TPR == 32 || have <= TOP_COUNTED) {
+    int above = 0;
+#pragma unroll 4
+    for (int j = 0; j < have; j += 2) {
+      const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(keys + j);
+      above += (v.x > key) + (v.y > key);
+    }
+    return above;
+  }
+  int above = i & 31;
+  for (int base = 0; base < have; base += 32) {
+    if (base == (i & ~31)) continue;
+    int lo = 0;
+#pragma unroll
+    for (int step = 16; step > 0; step >>= 1)
+      if (keys[base + lo + step - 1] > key) lo += step;
+    above += lo + (keys[base + lo] > key);
   }
   return above;
 }

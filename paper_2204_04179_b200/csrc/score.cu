@@ -562,14 +562,11 @@ __global__ void __launch_bounds__(32 * (ALONE ? SJ_ALONE_WARPS : SJ_WARPS)) scor
     have += count;
   }
   if (ALONE && warp != 0) return;
-  if (have & 1) {
-    if (lane == 0) keys[have] = 0;                      // read in pairs
-    __syncwarp();
-  }
+  top_sort<32>(keys, have);
   const int64_t o = n * k;
   for (int i = lane; i < have; i += 32) {
     const uint64_t key = keys[i];
-    const int above = top_rank(keys, have, key);
+    const int above = top_above<32>(keys, have, i);
     if (above < k) {
       ask.top_ids[o + above] = row_key_place(key);
       ask.top_logp[o + above] = row_logp(row_key_logit(key), r.m, log_s, scale);
