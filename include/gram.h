@@ -347,7 +347,7 @@ gram_status gram_distill(gram_ctx* ctx, const void* d_logits, int dtype, int64_t
 /* gram_logprobs of z[n, v] = users[n, :] . items[v, :] + bias[v] without an [N, V] array: d_users bf16 [N, d] and d_items
  * bf16 [V, d] with rows ld_users and ld_items elements apart (multiples of 8, addresses 16-byte aligned: else
  * GRAM_ERR_UNSUPPORTED), d_bias fp32 [V] or NULL (-inf takes an item out), products summed in fp32.  Lists of candidates, and the
- * logits of few users, lie in the context's workspace for matrix products (32 MB at least), as the partial sums of a product
+ * logits where they are few, lie in the context's workspace for matrix products (32 MB at least), as the partial sums of a product
  * do: calls of one context are ordered on one stream or by events. */
 gram_status gram_score_logprobs(gram_ctx* ctx, const void* d_users, int64_t ld_users, const void* d_items, int64_t ld_items,
                                 const float* d_bias, int64_t N, int32_t V, int32_t d, float scale, const int32_t* d_targets,

@@ -15,7 +15,7 @@
 // runs, one for each pair.  A run touches at most two row tiles, so a user's statistics and lists lie with a few pairs;
 // score_join_kernel joins them.
 //
-// Up to 128 users the logits are written after all (score_kernel<LOGITS>) and gram_logprobs' kernel reads them.
+// Where logits are few they are written after all (score_kernel<LOGITS>) and gram_logprobs' kernel reads them.
 #include "logits.h"
 #include "row_softmax.cuh"
 #include "row_top.cuh"
@@ -598,6 +598,15 @@ template <int MODE> cudaError_t launch_score(const CUtensorMap& users, const CUt
   return cudaLaunchKernelEx(&cfg, kern, users, items, a);
 }
 
+// what is asked of the rows from the n-th on
+RowAnswers from(RowAnswers ask, int64_t n) {
+  if (ask.C) { ask.targets += n * ask.C; ask.logp += n * ask.C; }
+  if (ask.stats) ask.stats += 2 * n;
+  if (ask.entropy) ask.entropy += n;
+  if (ask.k) { ask.top_logp += n * ask.k; ask.top_ids += n * ask.k; }
+  return ask;
+}
+
 }  // namespace
 
 gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_users, const void* items, int64_t ld_items,
@@ -605,11 +614,6 @@ gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_u
                                   size_t ws_bytes, cudaStream_t st) {
   const int32_t all_units = ceil_div(V, SC_UNIT);
   if (all_units > (1 << 30) / (kNumSMs / 2)) return gram_set_error(ctx, "gram_score_logprobs: %d items", V), GRAM_ERR_UNSUPPORTED;
-  // Few users: their logits are written and read once more, in place of the sample, the bars and the joining.  Against 100 000
-  // items of 768, this way and the other: 10 alternatives, 1 user 39.9 and 52.4 us, 64 users 48.1 and 58.4; 128 users against
-  // 30 522 items 27.9 and 36.8.  100 alternatives of 64 users 72.9 and 88.6, but of 128 users against 30 522 items 60.9 and 50.3.
-  // Without alternatives the other way has no sample to take: 1 user 35.2 and 37.9, 64 users 42.5 and 39.0, but 17.4 and 21.0
-  // against 30 522 items.
   CUtensorMap map_u, map_i;
   // copies are no larger than the users (rows past the last are filled with zeros, which takes time: one user against 100 000
   // items of 768 46 us with boxes of 128 rows, 35 with boxes of 8)
@@ -626,20 +630,33 @@ gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_u
   a.c = scale * kLog2e;
   a.stride = 1;
   a.status = gram_status_word(ctx);
-  if (N <= SM_ROWS && (ask.k > 0 ? N * ask.k <= 64 * SM_ROWS : N * V <= (2 << 20)) && (int64_t)(ws_bytes / sizeof(float)) / ld_logits >= N) {
-    if (!make_map(&map_u, users, (uint64_t)d, (uint64_t)N, (uint64_t)ld_users, SC_BK, (uint32_t)box_rows))
-      return gram_set_error(ctx, "gram_score_logprobs: cannot describe the users"), GRAM_ERR_UNSUPPORTED;
-    a.N = N;
+  // Logits that the workspace holds (32 MB of it at most: they stay in L2) are written and read once more, in place of the sample,
+  // the bars and the joining.  This way and the other, in us, items of 768:
+  //   10 alternatives, 100 000 items, 1 user 41 and 53, 64 users 46 and 58; 30 522 items, 256 users 29 and 37; 128 alternatives of
+  //   800 users, 10 000 items 33 and 91
+  //   in several turns where the table is small: 10 alternatives, 1000 items, 20 000 users 78 and 156, 3000 items, 8192 users 87 and
+  //   87, 10 000 items, 4096 users 141 and 87, but with 128 alternatives 180 and 300
+  //   without alternatives the other way has no sample to take: 64 users, 30 522 items 17 and 21, 100 000 items 42 and 38
+  const int64_t room = (int64_t)(ws_bytes < (32u << 20) ? ws_bytes : 32u << 20) / (int64_t)sizeof(float) / ld_logits;
+  const int64_t at_once = room < SC_ROWS ? room : room / SC_ROWS * SC_ROWS;       // users of a turn
+  if (ask.k > 0 ? at_once > 0 && (N <= at_once || at_once >= (ask.k > 64 ? 768 : 2048)) : N <= at_once && N * V <= (2 << 20)) {
     a.V = V;
-    a.units = a.total = all_units;
-    a.per_run = ceil_div(all_units, kNumSMs / 2);
+    a.units = all_units;
     a.logits = (float*)ws;
     a.ld_logits = ld_logits;
-    {
-      ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * N * V * d, 1, st, "score");
-      GRAM_CUDA(ctx, launch_score<LOGITS>(map_u, map_i, a, ceil_div(a.total, a.per_run), st));
+    for (int64_t n = 0; n < N; n += at_once) {
+      a.N = N - n < at_once ? N - n : at_once;
+      if (!make_map(&map_u, (const bf16*)users + n * ld_users, (uint64_t)d, (uint64_t)a.N, (uint64_t)ld_users, SC_BK, (uint32_t)box_rows))
+        return gram_set_error(ctx, "gram_score_logprobs: cannot describe the users"), GRAM_ERR_UNSUPPORTED;
+      a.total = (int32_t)ceil_div64(a.N, SC_ROWS) * all_units;
+      a.per_run = ceil_div(a.total, kNumSMs / 2);
+      {
+        ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * a.N * V * d, 1, st, "score");
+        GRAM_CUDA(ctx, launch_score<LOGITS>(map_u, map_i, a, ceil_div(a.total, a.per_run), st));
+      }
+      GRAM_TRY(logprobs_launch(ctx, ws, GRAM_F32, ld_logits, a.N, V, scale, from(ask, n), st));
     }
-    return logprobs_launch(ctx, ws, GRAM_F32, ld_logits, N, V, scale, ask, st);
+    return GRAM_OK;
   }
   // The sample: so many items that about 256 entries of a user reach the bar, but 4096 at least and a third of the table at
   // most; its maxima by groups of 8 columns, by 32 where that is more than score_bar_kernel holds.
@@ -711,11 +728,7 @@ gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_u
       launch_chain(score_bar_kernel, dim3((unsigned)ceil_div64(now, SB_ROWS)), 32 * SB_ROWS, 0, st, a.sample, a.sample_rows,
                    a.units * (SC_UNIT / 32), fine, now, ask.k, bars);
     }
-    RowAnswers part = ask;
-    if (ask.C) { part.targets += n * ask.C; part.logp += n * ask.C; }
-    if (ask.stats) part.stats += 2 * n;
-    if (ask.entropy) part.entropy += n;
-    if (ask.k) { part.top_logp += n * ask.k; part.top_ids += n * ask.k; }
+    const RowAnswers part = from(ask, n);
     const int used = cut(all_units, 1, pairs);
     GRAM_CUDA(ctx, ask.k ? launch_score<LISTS>(map_u, map_i, a, used, st) : launch_score<STATISTICS>(map_u, map_i, a, used, st));
     if (now >= 4 * kNumSMs)

@@ -14,6 +14,8 @@ pytestmark = pytest.mark.gpu
 SIZES = [(1, 1, 8, 0, 0), (2, 3, 8, 8, 0), (1, 255, 16, 0, 16), (3, 256, 64, 0, 0), (64, 257, 72, 0, 8), (127, 1000, 100, 4, 28),
          (128, 300, 768, 0, 0), (129, 513, 64, 8, 0), (5, 10_007, 768, 0, 0), (300, 2603, 256, 0, 0), (1, 40_000, 128, 0, 0),
          (257, 5000, 1000, 24, 24), (700, 777, 64, 0, 0), (40, 30_522, 64, 0, 0), (20_000, 70, 32, 0, 0), (2, 200_003, 8, 0, 0)]
+# more logits than are written and read again: candidates are listed
+LISTED = [(300, 30_522, 64, 0, 0), (257, 40_000, 128, 24, 24), (1000, 10_007, 72, 0, 8), (90, 100_003, 8, 8, 0), (1600, 5500, 32, 0, 0)]
 
 
 def _codes(rng, rows, d, pad):
@@ -25,7 +27,7 @@ def _codes(rng, rows, d, pad):
 
 
 @pytest.mark.parametrize("k", [0, 1, 10, 128])
-@pytest.mark.parametrize("N,V,d,pad_u,pad_i", SIZES)
+@pytest.mark.parametrize("N,V,d,pad_u,pad_i", SIZES + LISTED)
 def test_score_of_codes(N, V, d, pad_u, pad_i, k):
     rng = np.random.default_rng(N + V + k)
     users, u = _codes(rng, N, d, pad_u)
@@ -71,13 +73,13 @@ def test_score_of_any_vectors(N, V, d):
     g.close()
 
 
-@pytest.mark.parametrize("N", [1, 70, 200])
-def test_score_with_ties_and_nothing_left(N):
-    V, d = 3000, 64
+@pytest.mark.parametrize("N,V", [(1, 3000), (70, 3000), (200, 3000), (300, 30_000)])
+def test_score_with_ties_and_nothing_left(N, V):
+    d = 64
     rng = np.random.default_rng(N)
     users, u = _codes(rng, N, d, 0)
     items, w = _codes(rng, 5, d, 0)
-    items = items.repeat(V // 5, 1)                       # every item 600 times
+    items = items.repeat(V // 5, 1)                       # every item a fifth of V times
     w = np.tile(w, (V // 5, 1))
     g = context()
     for k in (1, 30, 128):
@@ -101,9 +103,11 @@ def test_score_with_ties_and_nothing_left(N):
 
 
 @pytest.mark.parametrize("N,V,k", [(128, 3000, 64), (128, 3000, 65), (63, 3000, 128), (65, 3000, 128), (129, 3000, 64), (1, 8_500_000, 10), (1, 8_300_000, 10),
-                                   (64, 32_768, 0), (64, 32_769, 0), (65, 32_768, 0)])
+                                   (64, 32_768, 0), (64, 32_769, 0), (65, 32_768, 0),
+                                   (2560, 3000, 10), (2561, 3000, 10), (5000, 3000, 1), (1792, 4100, 10), (1793, 4100, 10), (900, 10_000, 64), (900, 10_000, 65),
+                                   (1000, 2000, 0), (1100, 2000, 0)])
 def test_score_where_the_way_changes(N, V, k):
-    """Few users' logits are written and read again; more users, alternatives or items than the workspace holds are not."""
+    """Few logits are written and read again, in turns where the table is small; else candidates are listed."""
     d = 8
     rng = np.random.default_rng(N + k)
     users, u = _codes(rng, N, d, 0)
@@ -117,13 +121,13 @@ def test_score_where_the_way_changes(N, V, k):
     g.close()
 
 
-@pytest.mark.parametrize("N", [3, 200])
-def test_items_out_of_range_are_recorded_and_count_as_none(N):
+@pytest.mark.parametrize("N,V", [(3, 500), (200, 500), (200, 50_000)])
+def test_items_out_of_range_are_recorded_and_count_as_none(N, V):
     rng = np.random.default_rng(N)
     users, u = _codes(rng, N, 64, 0)
-    items, w = _codes(rng, 500, 64, 0)
+    items, w = _codes(rng, V, 64, 0)
     t = np.zeros((N, 1), np.int32)
-    t[1], t[2] = 500, -2
+    t[1], t[2] = V, -2
     g = context()
     for k in (0, 3):
         out = answers(N, 1, k)
@@ -131,14 +135,14 @@ def test_items_out_of_range_are_recorded_and_count_as_none(N):
         with pytest.raises(binding.GramError) as e:
             g.sync()
         assert e.value.status == 2
-        check_answers(out, Rows(u @ w.T, 0.05), np.where((t < 0) | (t >= 500), -1, t), k)
+        check_answers(out, Rows(u @ w.T, 0.05), np.where((t < 0) | (t >= V), -1, t), k)
     g.sync()
     g.close()
 
 
 def test_score_on_another_stream_behind_its_work():
     rng = np.random.default_rng(7)
-    for N in (20, 300):
+    for N in (20, 300, 2000):
         users, u = _codes(rng, N, 64, 0)
         items, w = _codes(rng, 5000, 64, 0)
         late = torch.zeros_like(users)
@@ -166,7 +170,7 @@ def test_score_of_a_sorted_table(order):
     x[:, 0], x[:, 1] = np.arange(V) // 250, np.arange(V) % 250 / 256     # both exact in bf16
     x = x[::order]
     items = torch.from_numpy(np.ascontiguousarray(x)).to(torch.bfloat16).to(DEV)
-    for N in (1, 140):
+    for N in (1, 140, 200):
         users = torch.zeros(N, d, dtype=torch.bfloat16, device=DEV)
         users[:, :2] = 1.0
         g = context()
@@ -177,8 +181,9 @@ def test_score_of_a_sorted_table(order):
         g.close()
 
 
-def test_nan_in_a_vector_stays_with_its_rows():
-    N, V, d = 140, 900, 64
+@pytest.mark.parametrize("N,V", [(140, 900), (300, 30_522)])
+def test_nan_in_a_vector_stays_with_its_rows(N, V):
+    d = 64
     rng = np.random.default_rng(1)
     users, u = _codes(rng, N, d, 0)
     items, w = _codes(rng, V, d, 0)
