@@ -58,22 +58,40 @@ struct ScoreArgs {
   int32_t* status;
 };
 
-// The tiles of a run, as all roles walk over them.
+// The tiles of a run, as all roles walk over them.  A run is as long as all others, so it holds every residue of the unit's number
+// modulo that length once; it begins with residue 0 and turns to its start at its end.  All pairs are then at units of about the
+// same residue at any time, and the row tiles' reads of the table meet in L2: 1024 users against 100 000 items of 768 with 10
+// alternatives 195 us from end to end of the run and 166 so, 4096 users 496 and 448.
 struct ScoreRun {
-  int32_t units, stride, begin, at, end;
-  int32_t tm, unit, width;       // row tile, first unit and width in units of the current tile
-  bool first, last;              // of the run's part of this row tile
+  int units, stride, per_run, begin, at, end;    // at: what lies ahead of the current row tile's part
+  int lo, turn, stop;            // the part's first unit, where it begins, where its current piece ends
+  int tm, unit, width;           // row tile, first unit and width in units of the current tile
+  bool first, last, turned;      // of the run's part of this row tile
   __device__ __forceinline__ ScoreRun(const ScoreArgs& a, int pair)
-      : units(a.units), stride(a.stride), begin(pair * a.per_run), at(begin), end(min(begin + a.per_run, a.total)), tm(0), unit(0), width(0), first(false), last(false) {}
+      : units(a.units), stride(a.stride), per_run(a.per_run), begin(pair * a.per_run), at(begin), end(min(begin + a.per_run, a.total)), lo(0), turn(0),
+        stop(0), tm(0), unit(0), width(0), first(false), last(false), turned(false) {}
   __device__ __forceinline__ bool next() {
-    at += width;
-    if (at >= end) return false;
-    tm = at / units;
-    unit = at - tm * units;
-    const int left = min(units - unit, end - at);
+    unit += width;
+    if (unit == stop) {
+      turned = !turned && turn > lo;
+      if (turned) {
+        unit = lo;
+        stop = turn;
+      } else {
+        if (at >= end) return false;
+        tm = at / units;
+        lo = at - tm * units;
+        stop = min(units, lo + end - at);
+        at += stop - lo;
+        turn = (lo + per_run - 1) / per_run * per_run;
+        if (turn >= stop) turn = lo;
+        unit = turn;
+      }
+    }
+    const int left = stop - unit;
     width = min(left, stride > 1 && (unit & 1) ? 1 : SC_COLS / SC_UNIT);
-    first = at == begin || unit == 0;
-    last = left == width;
+    first = unit == turn;
+    last = left == width && (turned || turn == lo);
     return true;
   }
   __device__ __forceinline__ int column() const { return ((unit >> 1) * stride * 2 + (unit & 1)) * SC_UNIT; }   // first item
