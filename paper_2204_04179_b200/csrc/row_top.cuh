@@ -3,7 +3,7 @@
 // While a row is read each thread only notes the largest entry of every group of chunks (one to a few).  At the end, a bar is
 // set that at least k entries reach: the value that k of the threads' maxima reach, or a little less.  The best k lie in the
 // groups whose maximum reaches the bar, hardly more than k of all threads' groups; these few are read again, and the entries
-// that reach the bar become keys (row_key: larger logit first, then lower place), whose order is found by counting.  Where
+// that reach the bar become keys (row_key: larger logit first, then lower place), whose order is found by counting (top_sort).  Where
 // more groups or entries reach the bar than the lists hold (equal logits), the k-th key is found by bisection over the row.
 #pragma once
 #include "row_softmax.cuh"
@@ -52,7 +52,6 @@ __device__ __forceinline__ float warp_cut(uint64_t* keys, int have, int k) {
   }
   return row_order_logit(__reduce_min_sync(0xffffffffu, low) + 1u);
 }
-
 
 // of up to 512 keys (k at least) a warp keeps the best k or a few more, in no order; returns how many
 __device__ __forceinline__ int warp_keep(uint64_t* keys, int have, int k) {

@@ -16,6 +16,10 @@
 // score_join_kernel joins them.
 //
 // Where logits are few they are written after all (score_kernel<LOGITS>) and gram_logprobs' kernel reads them.
+//
+// Bounded by the products where users are many, by the table's bytes where they are few.  Measured against 100 000 items of 768:
+// 4096 users 380 us (1650 TFLOP/s), with 10 alternatives 448; 1024 users 107 and 152 to 166; 64 users with 10 alternatives 48, one
+// user 41 (the table's 154 MB at 6458 GB/s: 24).
 #include "logits.h"
 #include "row_softmax.cuh"
 #include "row_top.cuh"
