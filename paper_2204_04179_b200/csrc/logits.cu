@@ -576,8 +576,8 @@ __global__ void __launch_bounds__(LP_THREADS, TPR == 32 ? 6 : LP_PER_SM) distill
 // Where rows are many a warp takes one: no barrier, and a quarter of the work per row that does not depend on its length.
 //   700 x 900 fp32 and more rows: 10 alternatives 6.2 us by blocks, 5.6 by warps; 20 000 x 900 93 and 35
 //   longer rows need more of them: 600 x 1800 3.0 and 3.4, 1500 x 1800 5.0 and 4.1 (no alternatives)
-//   rows that are written too, up to 12 KB: gradient 8192 x 2500 fp32 31.9 and 27.9, 10 000 x 3600 46 and 51; distillation
-//   8192 x 2500 fp32 55 and 40, 10 000 x 6000 bf16 77 and 59
+//   gradients up to 12 KB: 8192 x 2500 fp32 31.9 and 27.9, 20 000 x 4000 100 and 106
+//   distillation up to 20 KB: 8192 x 2500 fp32 55 and 40, 20 000 x 5000 191 and 169, 3000 x 10 000 bf16 37 and 30; 32 KB 150 and 159
 //   rows that are only read, up to 40 KB: 10 000 x 5000 fp32 40 and 36, 25 600 x 10 000 157 and 152, with 10 alternatives 207 and
 //   193; rows of 64 KB 55 and 64
 //   with 32 alternatives up to 32 KB: 10 000 x 16 000 bf16 96 and 88, 40 KB 94 and 111
@@ -637,7 +637,7 @@ template <typename T> gram_status backward_typed(gram_ctx* ctx, const T* z, T* d
   return launch_rows(ctx, logprobs_backward_kernel<T, LP_THREADS>, plan, a.N, 0, st, z, dz, a);
 }
 template <typename T> gram_status distill_typed(gram_ctx* ctx, const T* z, T* dz, DistillArgs a, cudaStream_t st) {
-  const RowPlan plan = row_plan(ctx, a.N, (int64_t)a.V * sizeof(T), 64 << 10, 12 << 10);
+  const RowPlan plan = row_plan(ctx, a.N, (int64_t)a.V * sizeof(T), 64 << 10, 20 << 10);
   ProfScope prof(ctx, GRAM_K_OTHER, (dz ? 2.0 : 1.0) * a.N * a.V * sizeof(T), 1, st, "distill");
   a.shift = plan.shift;
   if (plan.warps) return launch_rows(ctx, distill_kernel<T, 32>, plan, a.N, 0, st, z, dz, a);

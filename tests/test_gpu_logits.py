@@ -407,7 +407,8 @@ def test_alternatives_that_crowd_together(V, dtype, k, order):
 
 @pytest.mark.parametrize("k", [1, 17, 128])
 @pytest.mark.parametrize("V,dtype,pad,offset", [(1, "f32", 0, 0), (9, "bf16", 0, 1), (700, "f32", 0, 0), (1999, "bf16", 3, 5), (2048, "f32", 0, 0),
-                                                (3000, "f32", 0, 0), (2999, "f32", 1, 3), (6000, "bf16", 2, 1), (6144, "bf16", 0, 0)])
+                                                (3000, "f32", 0, 0), (2999, "f32", 1, 3), (6000, "bf16", 2, 1), (6144, "bf16", 0, 0),
+                                                (5000, "f32", 0, 0), (10_001, "bf16", 3, 1)])
 def test_gradients_of_many_rows(V, dtype, pad, offset, k):
     N = 2400
     rng, few = _draw(16, V, V + k)
