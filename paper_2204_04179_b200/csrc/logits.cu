@@ -541,7 +541,9 @@ __global__ void __launch_bounds__(LP_THREADS, TPR == 32 ? 6 : LP_PER_SM) distill
     if (tid == 0) a.loss[n] = loss;
   }
   if (!dlogits) return;
-  const bool none = w == 0.f || t.s == 0.f;
+  // no teacher entry takes part: no largest one, and no NaN among them (the sum alone is 0 for large entries too, which were summed
+  // again above)
+  const bool none = w == 0.f || (t.m == ROW_NEG_INF && t.s == 0.f);
   T* dz = dlogits + n * a.ld_out;
   const int bytes = store_bytes(dz + s.head);
   const RowPower l(r.m, log_s, c);
