@@ -19,9 +19,11 @@ template <typename F> __device__ __forceinline__ uint64_t kth_key(int k, F at_le
   }
   return lo;
 }
-// `have` keys (k at least) cut to the best k by a warp; returns a bar that only better logits than theirs reach.  The keys are read
-// again in each step of the bisection (shared memory, or L1): no array of them lives in registers.
-__device__ __forceinline__ float warp_cut(uint64_t* keys, int have, int k) {
+// `have` keys (k at least) cut to the best k by a warp; returns a bar that all later entries reach which could still be among the
+// best, given that these have places of `from` on: the least of the logits kept where such an entry may have the lower place of two
+// equal ones, else the next value above it.  The keys are read again in each step of the bisection (shared memory, or L1): no array
+// of them lives in registers.
+__device__ __forceinline__ float warp_cut(uint64_t* keys, int have, int k, uint32_t from) {
   const int lane = threadIdx.x & 31;
   uint32_t low = 0xffffffffu, high = 0u;
   for (int i = lane; i < have; i += 32) {
@@ -38,19 +40,21 @@ __device__ __forceinline__ float warp_cut(uint64_t* keys, int have, int k) {
     return (int)__reduce_add_sync(0xffffffffu, c);
   }, (uint64_t)low << 32, (uint64_t)high << 32 | 0xffffffffu);
   int at = 0;
-  low = 0xffffffffu;
+  uint64_t least = ~0ull;                                // of a lane's keys that are kept: of equal logits the one with the highest place
   for (int i = 0; i < have; i += 32) {                   // what is kept moves down, behind what has been read
     const uint64_t key = i + lane < have ? keys[i + lane] : 0;
     const bool keep = key >= kth;                        // kth > 0
     const uint32_t who = __ballot_sync(0xffffffffu, keep);
     if (keep) {
       keys[at + __popc(who & ((1u << lane) - 1u))] = key;
-      low = min(low, (uint32_t)(key >> 32));
+      least = key < least ? key : least;
     }
     at += __popc(who);
     __syncwarp();
   }
-  return row_order_logit(__reduce_min_sync(0xffffffffu, low) + 1u);
+  low = __reduce_min_sync(0xffffffffu, (uint32_t)(least >> 32));
+  const uint32_t last = __reduce_max_sync(0xffffffffu, (uint32_t)(least >> 32) == low ? ~(uint32_t)least : 0u);
+  return row_order_logit(last >= from ? low : low + 1u);
 }
 
 // of up to 512 keys (k at least) a warp keeps the best k or a few more, in no order; returns how many

@@ -70,7 +70,7 @@ struct ScoreRun {
   int units, stride, per_run, begin, at, end;    // at: what lies ahead of the current row tile's part
   int lo, turn, stop;            // the part's first unit, where it begins, where its current piece ends
   int tm, unit, width;           // row tile, first unit and width in units of the current tile
-  bool first, last, turned;      // of the run's part of this row tile
+  bool first, last, turned;      // of the run's part of this row tile; turned: the places are below those seen before
   __device__ __forceinline__ ScoreRun(const ScoreArgs& a, int pair)
       : units(a.units), stride(a.stride), per_run(a.per_run), begin(pair * a.per_run), at(begin), end(min(begin + a.per_run, a.total)), lo(0), turn(0),
         stop(0), tm(0), unit(0), width(0), first(false), last(false), turned(false) {}
@@ -103,8 +103,8 @@ struct ScoreRun {
   __device__ __forceinline__ bool leaves() const { return (end - 1) / units != tm; }     // the run goes on with another row tile
 };
 
-// a list cut to its best k by the whole warp; returns (in every lane) the bar that better logits reach
-__device__ __noinline__ float score_cut(uint64_t* list, int have, int k) { return warp_cut(list, have, k); }
+// a list cut to its best k by the whole warp; returns (in every lane) the bar of the entries that follow, at places of `from` on
+__device__ __noinline__ float score_cut(uint64_t* list, int have, int k, uint32_t from) { return warp_cut(list, have, k, from); }
 
 // a block of 32 columns of this thread's row as it left tensor memory, plus the bias (the warp's 32 values in shared memory)
 __device__ __forceinline__ void score_bias(uint32_t (&v)[32], const float* b) {
@@ -158,7 +158,7 @@ __device__ __forceinline__ void score_list(const uint32_t (&v)[32], const float 
       const int of = __ffs(full) - 1;
       full &= full - 1;
       __syncwarp();
-      const float up = score_cut(warp_lists + (int64_t)of * cap, __shfl_sync(0xffffffffu, have, of), k);
+      const float up = score_cut(warp_lists + (int64_t)of * cap, __shfl_sync(0xffffffffu, have, of), k, col + 8 * g);
       if (lane == of) { have = k; bar = up; }
     }
     uint32_t bits = 0u;
@@ -311,6 +311,9 @@ __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_const
           have = 0;
           if (MODE == LISTS) bar = n < a.N ? a.bars[n] : __int_as_float(0x7fffffff);     // nothing reaches a NaN
         }
+        // Behind the turn places are lower than those of the list, and of equal logits the lower place is the better one: a cut list's bar,
+        // the next value above its least logit, goes back to that logit.
+        if (MODE == LISTS && run.turned && run.unit == run.lo && n < a.N) bar = fmaxf(a.bars[n], row_order_logit(row_order(bar) - 1u));
         for (int b = 0; b < blocks; ++b) {
           uint32_t v[32];
           tc_ld32_issue(taddr + b * 32, v);
@@ -356,7 +359,7 @@ __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_const
               uint64_t* from = warp_lists + (int64_t)of * a.cap;
               int n_of = __shfl_sync(0xffffffffu, have, of);
               if (n_of > a.early_cap) {
-                (void)score_cut(from, n_of, a.k);
+                (void)score_cut(from, n_of, a.k, 0u);
                 n_of = a.k;
                 if (lane == of) have = n_of;
               }
