@@ -470,9 +470,43 @@ __device__ __forceinline__ float score_dot(const bf16* u, const bf16* w, int d) 
   return sum;
 }
 
+// A user's logits as score_dot sums them, for rows of huge ones (out of line: with this in place the joining took 15 registers more).
+struct ScoreRow {
+  const bf16 *user, *items;
+  const float* bias;
+  int64_t ld_i;
+  int32_t V, d;
+  __device__ __forceinline__ float operator()(int v) const { return score_dot(user, items + (int64_t)v * ld_i, d) + (bias ? bias[v] : 0.f); }
+};
+__device__ __noinline__ float score_again(const ScoreRow& z, int v) { return z(v); }
+// of every step-th item from `first` on: the largest
+__device__ __noinline__ float score_largest(const ScoreRow& z, int first, int step) {
+  float m = ROW_NEG_INF;
+  for (int v = first; v < z.V; v += step) m = fmaxf(m, z(v));
+  return m;
+}
+// and the sums relative to m: of 64 items, and of these, so that chains of additions are short
+__device__ __noinline__ float2 score_sums(const ScoreRow& z, float m, float c, int first, int step) {
+  float s = 0.f, t = 0.f;
+  for (int v0 = first; v0 < z.V; v0 += 64 * step) {
+    float run_s = 0.f, run_t = 0.f;
+    for (int v = v0; v < z.V && v < v0 + 64 * step; v += step) {
+      const float y = (z(v) - m) * c, e = row_ex2(y);
+      run_s += e;
+      run_t = fmaf(e, fmaxf(y, -200.f), run_t);
+    }
+    s += run_s;
+    t += run_t;
+  }
+  return make_float2(s, t);
+}
+
 // Joins the statistics of the runs that crossed a user's row tile, and their lists.  A warp takes a user, four users a block; where
 // users are few a block takes one (ALONE): its eight warps share the given tokens and the reading of the lists.
 // About 256 keys come in; more than fit are taken in turns, the best k of each going into the next.
+// A row of huge logits (row_is_huge) is summed again, relative to its largest logit itself.  A last place of such logits is worth many
+// units of an exponent, so that all its answers are taken from one set of them: the products as score_dot sums them, not those of the
+// tensor cores, which add in another order.  (Once over the table for the largest and once for the sums.)
 constexpr int SJ_PARTS = (kNumSMs / 2 + 1) * SC_PARTS, SJ_KEYS = 512;          // parts of a user at most; keys of a turn
 constexpr int SJ_WARPS = 4, SJ_ALONE_WARPS = 8;
 template <bool ALONE>
@@ -483,6 +517,7 @@ __global__ void __launch_bounds__(32 * (ALONE ? SJ_ALONE_WARPS : SJ_WARPS)) scor
   __shared__ __align__(16) uint64_t keys_of[ROWS][SJ_KEYS];
   __shared__ const uint64_t* lists_of[ROWS][SJ_PARTS];
   __shared__ int starts_of[ROWS][SJ_PARTS + 1], kept;
+  __shared__ float huge_part[ALONE ? SJ_ALONE_WARPS : 1][3];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, slot = ALONE ? 0 : warp;
   const int64_t n = ALONE ? blockIdx.x : (int64_t)blockIdx.x * SJ_WARPS + warp;
   if (n >= a.N) return;                                 // whole warps; the block's barriers are in the other form only
@@ -544,24 +579,34 @@ __global__ void __launch_bounds__(32 * (ALONE ? SJ_ALONE_WARPS : SJ_WARPS)) scor
     take(0, have, 0);
   }
   float log_s = row_log_sum(r, a.c), entropy = row_entropy(r);
-  if (row_is_huge(r.m, a.c)) {                          // summed again, relative to m itself
-    float s = 0.f, t = 0.f;
-    for (int v = 0; v < a.V; ++v) {
-      const float z = score_dot(users + n * ld_u, items + (int64_t)v * ld_i, d) + (a.bias ? a.bias[v] : 0.f);
-      const float y = (z - r.m) * a.c, e = row_ex2(y);
-      s += e;
-      t = fmaf(e, fmaxf(y, -200.f), t);
+  const ScoreRow row_z{users + n * ld_u, items, a.bias, ld_i, a.V, d};
+  const bool huge = row_is_huge(r.m, a.c);
+  if (huge) {                                           // in all warps of a block or in none: each takes every WARPS-th item
+    constexpr int WARPS = ALONE ? SJ_ALONE_WARPS : 1;
+    const int w = ALONE ? warp : 0;
+    r.m = score_largest(row_z, w, WARPS);
+    if (ALONE) {
+      if (lane == 0) huge_part[w][0] = r.m;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < WARPS; ++i) r.m = fmaxf(r.m, huge_part[i][0]);
     }
-    log_s = logf(s);
-    entropy = log_s - kLn2 * (t / s);
+    float2 st = score_sums(row_z, r.m, a.c, w, WARPS);
+    if (ALONE) {
+      if (lane == 0) { huge_part[w][1] = st.x; huge_part[w][2] = st.y; }
+      __syncthreads();
+      st = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < WARPS; ++i) { st.x += huge_part[i][1]; st.y += huge_part[i][2]; }
+    }
+    log_s = logf(st.x);
+    entropy = log_s - kLn2 * (st.y / st.x);
   }
   for (int i = ALONE ? warp : 0; i < ask.C; i += ALONE ? SJ_ALONE_WARPS : 1) {
     const int32_t t = ask.targets[n * ask.C + i];
     float lp = 0.f;
     if (t >= 0 && t < a.V) {
-      float z = score_dot(users + n * ld_u, items + (int64_t)t * ld_i, d);
-      if (a.bias) z += a.bias[t];
-      lp = row_logp(z, r.m, log_s, scale);
+      lp = row_logp(row_z(t), r.m, log_s, scale);
     } else if (t != -1) {
       gram_device_fail(a.status, GRAM_ERR_ID_RANGE);
     }
@@ -589,12 +634,19 @@ __global__ void __launch_bounds__(32 * (ALONE ? SJ_ALONE_WARPS : SJ_WARPS)) scor
   if (ALONE && warp != 0) return;
   top_sort<32>(keys, have);
   const int64_t o = n * k;
-  for (int i = lane; i < have; i += 32) {
-    const uint64_t key = keys[i];
-    const int above = top_above<32>(keys, have, i);
+  for (int i0 = 0; i0 < have; i0 += 32) {
+    const int i = i0 + lane;
+    const uint64_t key = i < have ? keys[i] : 0;
+    float z = row_key_logit(key);
+    if (huge)
+      for (int j = 0; j < 32 && i0 + j < have; ++j) {
+        const float x = score_again(row_z, row_key_place(keys[i0 + j]));
+        if (lane == j) z = x;
+      }
+    const int above = i < have ? top_above<32>(keys, have, i) : k;
     if (above < k) {
       ask.top_ids[o + above] = row_key_place(key);
-      ask.top_logp[o + above] = row_logp(row_key_logit(key), r.m, log_s, scale);
+      ask.top_logp[o + above] = row_logp(z, r.m, log_s, scale);
     }
   }
   for (int i = have + lane; i < k; i += 32) {

@@ -1,9 +1,10 @@
-"""Scores whose candidates are listed (more logits than are written and read again): equal ones in all row tiles."""
+"""Scores whose candidates are listed (more logits than are written and read again): equal ones in all row tiles, and rows of large
+logits."""
 import numpy as np
 import pytest
 import torch
 
-from tests.logits_helpers import DEV, INF, Rows, answers, check_answers, context
+from tests.logits_helpers import DEV, INF, U, Rows, answers, check_answers, context, near
 
 pytestmark = pytest.mark.gpu
 
@@ -67,4 +68,50 @@ def test_whole_number_scores(N, V, k):
     for n in range(0, N, 500):
         key = ((users[n:n + 500].double() @ items.double().T).long() << 32) - place
         assert torch.equal(out["top_ids"][n:n + 500].long(), (-key.topk(k, dim=1).values) & 0xFFFFFFFF), n
+    g.close()
+
+
+# ------------------------------ rows of large logits ------------------------------
+@pytest.mark.parametrize("size,common", [(1e7, False), (1e10, False), (1e18, False), (1e7, True), (1e10, True)])
+@pytest.mark.parametrize("k", [0, 10, 128])
+@pytest.mark.parametrize("N,V,d", [(300, 30_522, 768), (700, 12_500, 72)])
+def test_scores_of_large_vectors(N, V, d, k, size, common):
+    """Logits so large that 32 bits hold no fraction of theirs, and of which 128 items are offered: the answers belong to one set of
+    logits.  The best item's log probability is then -log s to the bit, the 128 probabilities add up to 1, and the entropy is theirs.
+    Bounds: a log probability is off by 2^-22 + (V / 128 + 64) u < 2e-5 and 4 u of its difference to the best; with
+    sum p |y| <= 128 / e < 48 the sum of the probabilities by less than 1e-4 and the entropy by less than 2e-3."""
+    rng = np.random.default_rng(N + k)
+    step = 1.0 if common else np.sqrt(size / np.sqrt(d))
+    users = _up(rng.standard_normal((N, d)) * step, torch.bfloat16)
+    items = _up(rng.standard_normal((V, d)) * step, torch.bfloat16)
+    if common:                                           # the size is all items' alike, their differences those of the other columns
+        users[:, 0] = items[:, 0] = float(np.sqrt(size))
+    offered = np.sort(rng.permutation(V)[:128]).astype(np.int32)
+    bias = np.full(V, -INF)
+    bias[offered] = 0.0
+    targets = np.tile(offered, (N, 1))
+    g = context()
+    for scale in (1.0, 4.0 / size, 1e8 / size):
+        out = answers(N, 128, k)
+        g.score_logprobs(users, items, bias=_up(bias), scale=scale, targets=_up(targets, torch.int32), **out)
+        g.sync()
+        logp, log_s, entropy = out["logp"].double().cpu().numpy(), out["stats"][:, 1].double().cpu().numpy(), out["entropy"].double().cpu().numpy()
+        assert np.isfinite(log_s).all() and (log_s >= 0).all() and (log_s <= np.log(128) + 1e-4).all()
+        if scale * size >= 1e7:                          # others have sums of the products' own order
+            assert np.array_equal(logp.max(1), -log_s)
+            p = np.exp(logp)
+            assert (np.abs(p.sum(1) - 1) <= 1e-4).all()
+            assert (np.abs(-np.where(p > 0, p * logp, 0.0).sum(1) - entropy) <= 2e-3).all()
+        u, w = users.double().cpu().numpy(), items[torch.from_numpy(offered).to(DEV).long()].double().cpu().numpy()
+        dz = 2 * d * U * (np.abs(u) @ np.abs(w).T).max()
+        z = u @ w.T
+        near(out["stats"][:, 0], z.max(1), dz, "m")
+        if k:
+            ids, top = out["top_ids"].cpu().numpy(), out["top_logp"].double().cpu().numpy()
+            where = np.searchsorted(offered, ids)
+            assert np.array_equal(offered[where], ids) and all(len(set(row)) == k for row in ids)
+            best = -np.sort(-z, 1)[:, :k]
+            assert (np.abs(np.take_along_axis(z, where, 1) - best) <= 2 * dz).all()
+            if scale * size >= 1e7:
+                assert np.array_equal(top, np.take_along_axis(logp, where, 1))
     g.close()
