@@ -79,9 +79,9 @@ __device__ __forceinline__ float row_log_sum(const RowStat& r, float c) {
 __device__ __forceinline__ float row_entropy(const RowStat& r) { return r.s == 0.f ? 0.f : logf(r.s) - kLn2 * (r.t / r.s); }
 __device__ __forceinline__ float row_logp(float z, float m, float log_s, float scale) {
   if (z == ROW_NEG_INF) return log_s != log_s ? log_s : z;
-  float y = (z - m) * scale;
-  if (y == ROW_NEG_INF) y = z * scale - m * scale;   // only the difference may have left 32 bits (the two are of opposite signs then)
-  return y - log_s;
+  const float d = z - m;
+  // where only the difference has left 32 bits the two are of opposite signs, and the difference of their products is no NaN
+  return (d == ROW_NEG_INF ? z * scale - m * scale : d * scale) - log_s;
 }
 
 // The order of alternatives: larger logits first, then lower places.  -0 counts as 0.

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from tests.logits_helpers import DEV, INF, Rows, context, near, place
+from tests.logits_helpers import DEV, DT, INF, Rows, answers, check_answers, context, near, place
 from tests.test_gpu_logits import _distill_reference
 
 pytestmark = pytest.mark.gpu
@@ -91,4 +91,29 @@ def test_distill_from_a_teacher_of_large_logits_against_differences():
     g.distill(view, _up(ids), _up(a), loss, scale=scale, dlogits=dz)
     near(dz, want, 2.0 ** -8 / 6 + 2.0 ** -15, "differences")
     g.sync()
+    g.close()
+
+
+# ------------------------------ log probabilities that leave 32 bits ------------------------------
+@pytest.mark.parametrize("scale", [0.5, 2.0, 10.0, 1e6])
+@pytest.mark.parametrize("N,V,dtype", FORMS + [(3, 4, "f32")])
+def test_log_probabilities_beyond_32_bits(N, V, dtype, scale):
+    """Rows of logits near the type's lowest value, the largest among them too: an entry whose log probability leaves 32 bits has
+    -inf, never NaN."""
+    lowest = float(torch.finfo(DT[dtype]).min)
+    i = np.arange(V)
+    few = np.stack([np.where(i % 2 == 0, -1e38, lowest), np.where(i == V - 1, -2e38, lowest), np.where(i % 3 == 0, 1e38, lowest)])
+    base, z = place(few, dtype)
+    view = base.repeat(-(-N // 3), 1)[:N].contiguous()
+    targets = np.tile(np.array([[0, 1, V - 1]], np.int32), (3, 1))
+    r = Rows(z, scale)
+    with np.errstate(all="ignore"):
+        r.logp = np.where(r.logp < -LARGEST, -INF, r.logp)
+    g = context()
+    out = answers(N, 3, V if V <= 128 else 128)
+    g.logprobs(view, scale=scale, targets=_up(_tile(targets, N)), **out)
+    g.sync()
+    k = out["top_ids"].shape[1]
+    for first in (0, N - N % 3 - 3):
+        check_answers({x: out[x][first:first + 3] for x in out}, r, targets, k)
     g.close()
