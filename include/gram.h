@@ -302,7 +302,7 @@ gram_status gram_get_window(gram_ctx* ctx, float* h_table, uint32_t* h_touched, 
 /* --- answers over a pool, and learning from them -----------------------------
  * Where the task module of Section 3.1 scores a few candidates, a deployed model answers over the whole pool (Table 3:
  * 2.6k to 104k items) or the encoder's vocabulary, and a smaller encoder is trained on a larger one's answers.  A row of
- * logits z[v], v < V, is scaled first, x = scale * z (scale finite and > 0: one over the temperature).  A place at -inf is
+ * logits z[v], v < V, is scaled first, x = scale * z (scale in [1e-30, 1e30]: one over the temperature).  A place at -inf is
  * masked out: it has no probability, is never an alternative, and a gradient there is 0.  In a row with nothing left
  * log probabilities are -inf, the entropy is 0, there are no alternatives, and all gradients are 0.  A row that holds NaN or
  * +inf has NaN statistics, log probabilities, entropy, loss and gradients (alternatives: the largest of its other entries

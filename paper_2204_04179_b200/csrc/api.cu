@@ -1,5 +1,4 @@
 // The C ABI of libgram: context life cycle, argument checks, and the calls of include/gram.h.
-#include <math.h>
 #include <stdarg.h>
 
 #include <new>
@@ -468,7 +467,7 @@ gram_status gram_gemm_bf16_epilogue(gram_ctx* ctx, const void* d_A, int a_kmajor
 static gram_status check_rows(gram_ctx* ctx, const char* name, int64_t N, int32_t V, float scale) {
   ROWS_ARG(N >= 0 && N <= INT32_MAX, "N must be in [0, 2^31)");
   ROWS_ARG(V >= 1, "V must be positive");
-  ROWS_ARG(isfinite(scale) && scale > 0.f, "scale must be finite and positive");
+  ROWS_ARG(scale >= 1e-30f && scale <= 1e30f, "scale must be in [1e-30, 1e30]");      // no NaN either
   return GRAM_OK;
 }
 static gram_status check_logits(gram_ctx* ctx, const char* name, const void* p, int dtype, int64_t ld, int64_t N, int32_t V) {

@@ -7,7 +7,8 @@
 // A masked place (-inf) has e = 0; in t its y is held at -200, so that e y is 0 and not NaN.  A NaN (or +inf, whose c z - R is
 // one) reaches s and everything computed from it.
 // Logits so large that c m has no place left for a fraction (all places of a row at the type's lowest value) are the exception,
-// row_is_huge: their rows are summed again with the difference z - m taken first.
+// row_is_huge: their rows are summed again with the difference z - m taken first.  So are rows at a scale so far from 1 that c times
+// the value at which masked places are held (row_held) is no longer a finite number far below all others.
 #pragma once
 #include <float.h>
 
@@ -26,7 +27,9 @@ __device__ __forceinline__ float row_ex2(float x) {
 }
 // R(m), held at -2^23: a thread that has seen nothing, or only logits of the type's lowest value, keeps sums of 0
 __device__ __forceinline__ float row_ref(float m, float c) { return fmaxf(rintf(m * c), -8388608.f); }
-__device__ __forceinline__ bool row_is_huge(float m, float c) { return fabsf(m) <= FLT_MAX && !(fabsf(m * c) <= 4194304.f); }
+__device__ __forceinline__ bool row_is_huge(float m, float c) {
+  return fabsf(m) <= FLT_MAX && !(fabsf(m * c) <= 4194304.f && c >= 1e-20f && c <= 1e8f);
+}
 __device__ __forceinline__ RowStat row_empty() { return RowStat{ROW_NEG_INF, 0.f, 0.f}; }
 // r's statistics as they are with a larger m
 __device__ __forceinline__ void row_raise(RowStat& r, float m, float c) {
@@ -73,10 +76,12 @@ template <int L> __device__ __forceinline__ RowStat row_join_lanes(RowStat r, fl
   }
   return r;
 }
+// the sum of a row with nothing left (m = -inf): 0 at any scale, or NaN where the row holds one
+__device__ __forceinline__ float row_none(const RowStat& r) { return r.s != r.s ? r.s : 0.f; }
 __device__ __forceinline__ float row_log_sum(const RowStat& r, float c) {
-  return r.m == ROW_NEG_INF ? logf(r.s) : fmaf(fmaf(-r.m, c, row_ref(r.m, c)), kLn2, logf(r.s));
+  return r.m == ROW_NEG_INF ? logf(row_none(r)) : fmaf(fmaf(-r.m, c, row_ref(r.m, c)), kLn2, logf(r.s));
 }
-__device__ __forceinline__ float row_entropy(const RowStat& r) { return r.s == 0.f ? 0.f : logf(r.s) - kLn2 * (r.t / r.s); }
+__device__ __forceinline__ float row_entropy(const RowStat& r) { return r.m == ROW_NEG_INF ? row_none(r) : logf(r.s) - kLn2 * (r.t / r.s); }
 __device__ __forceinline__ float row_logp(float z, float m, float log_s, float scale) {
   if (z == ROW_NEG_INF) return log_s != log_s ? log_s : z;
   const float d = z - m;

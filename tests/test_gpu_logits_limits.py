@@ -5,7 +5,8 @@ import pytest
 import torch
 
 from tests.logits_helpers import DEV, DT, INF, Rows, answers, check_answers, context, near, place
-from tests.test_gpu_logits import _distill_reference
+from tests.test_gpu_logits import _backward_reference, _distill_reference, _special
+from paper_2204_04179_b200 import binding
 
 pytestmark = pytest.mark.gpu
 
@@ -116,4 +117,100 @@ def test_log_probabilities_beyond_32_bits(N, V, dtype, scale):
     k = out["top_ids"].shape[1]
     for first in (0, N - N % 3 - 3):
         check_answers({x: out[x][first:first + 3] for x in out}, r, targets, k)
+    g.close()
+
+
+# ------------------------------ scales far from 1 ------------------------------
+SCALES = [1e-30, 3e-24, 1e-12, 3e7, 1e9, 1e17, 1e30]
+
+
+def _rows_of_scales(V, dtype):
+    """Rows with masked places: ordinary ones, ones whose largest logit is 0, and those of _special."""
+    rng = np.random.default_rng(V)
+    z = rng.standard_normal((4, V)) * 3
+    z[rng.random((4, V)) < 0.3] = -INF
+    z[2] = np.where(np.isneginf(z[2]), -INF, -np.abs(z[2]))
+    z[2, V // 2] = 0.0
+    z[3] = np.where(np.arange(V) % 2 == 0, 0.0, -INF)
+    return np.concatenate([z, _special(V, float(torch.finfo(DT[dtype]).min))])
+
+
+@pytest.mark.parametrize("scale", SCALES)
+@pytest.mark.parametrize("N,V,dtype", FORMS + [(17, 3, "f32"), (17, 130, "bf16")])
+def test_scales_far_from_one(N, V, dtype, scale):
+    """A masked place has no weight, and an entry's share is that of the definition, however small or large the scale is."""
+    base, z = place(_rows_of_scales(V, dtype), dtype)
+    n, k, nc = len(z), 8, 3
+    N = max(N, n)
+    rng = np.random.default_rng(V)
+    view = base.repeat(-(-N // n), 1)[:N].contiguous()
+    r = Rows(z, scale)
+    with np.errstate(all="ignore"):                      # what leaves 32 bits is -inf there
+        r.logp = np.where(r.logp < -LARGEST, -INF, r.logp)
+    targets = np.where(rng.random((n, nc)) < 0.2, -1, rng.integers(0, V, (n, nc))).astype(np.int32)
+    g = context()
+    with_top, without = answers(N, nc, k), answers(N, nc)
+    for out in (with_top, without):
+        g.logprobs(view, scale=scale, targets=_up(_tile(targets, N)), **out)
+        g.sync()
+        for first in {0, N // n // 2 * n, (N // n - 1) * n}:
+            check_answers({x: None if out[x] is None else out[x][first:first + n] for x in out}, r, targets, k if out is with_top else 0)
+    # gradients: powers below 2^-126 are 0, which with the scale ahead of them is scale 1e-37 at most
+    stats, H = np.stack([r.m, r.log_s], 1).astype(np.float32), r.H.astype(np.float32)
+    dlogp, dH = rng.standard_normal((n, nc)).astype(np.float32), rng.standard_normal(n).astype(np.float32)
+    more = lambda bound, want: (bound * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(want) if dtype == "bf16" else bound) + r.scale * 1e-37  # noqa: E731
+    dz = torch.full_like(view, float("nan"))
+    g.logprobs_backward(view, _up(_tile(stats, N)), dz, scale=scale, targets=_up(_tile(targets, N)), dlogp=_up(_tile(dlogp, N)),
+                        entropy=_up(_tile(H, N)), dentropy=_up(_tile(dH, N)))
+    g.sync()
+    want, bound = _backward_reference(r, targets, dlogp, dH, "f32")
+    near(dz[:n], want, more(bound, want), "gradient")
+    assert (dz[:n][torch.from_numpy(np.isneginf(z)).to(DEV)] == 0).all()
+    a = rng.standard_normal((n, nc)).astype(np.float32)
+    a[:, 1] = a[:, 0]
+    loss = torch.empty(N, device=DEV)
+    with np.errstate(all="ignore"):
+        want_loss, d_loss, want, bound = _distill_reference(r, targets, a.astype(float), np.ones(n))
+    g.distill(view, _up(_tile(targets, N)), _up(_tile(a, N)), loss, scale=scale, dlogits=dz)
+    g.sync()
+    fits = np.abs(want_loss) < LARGEST
+    near(loss[:n][torch.from_numpy(fits).to(DEV)], want_loss[fits], d_loss[fits], "loss")
+    near(dz[:n], want, more(bound, want), "gradient of distillation")
+    g.close()
+
+
+@pytest.mark.parametrize("scale", SCALES[::2])
+@pytest.mark.parametrize("N,V", [(5, 3000), (300, 30_522), (700, 12_500)])
+def test_scores_of_scales_far_from_one(N, V, scale):
+    """Of small whole numbers, whose products are exact in any order: as logits that are written, and as lists of candidates."""
+    d, k = 8, 5
+    rng = np.random.default_rng(N)
+    u, w = rng.integers(-3, 4, (N, d)).astype(float), rng.integers(-3, 4, (V, d)).astype(float)
+    bias = np.where(rng.random(V) < 0.3, -INF, np.round(rng.standard_normal(V) * 256) / 256)
+    bias[0] = 0.0
+    targets = rng.integers(0, V, (N, 2)).astype(np.int32)
+    r = Rows(u @ w.T + bias, scale)
+    with np.errstate(all="ignore"):
+        r.logp = np.where(r.logp < -LARGEST, -INF, r.logp)
+    g = context()
+    for kk in (k, 0):
+        out = answers(N, 2, kk)
+        g.score_logprobs(_up(u).to(torch.bfloat16), _up(w).to(torch.bfloat16), bias=_up(bias.astype(np.float32)), scale=scale, targets=_up(targets), **out)
+        g.sync()
+        check_answers(out, r, targets, kk)
+    g.close()
+
+
+def test_scales_that_are_refused():
+    """Beyond 1e-30 and 1e30 differences of finite logits, and their gradients, leave 32 bits."""
+    g = context()
+    z, st = torch.zeros(4, 16, device=DEV), torch.zeros(4, 2, device=DEV)
+    for scale in (9e-31, 1.1e30, 1e-45, 3e38):
+        for call in (lambda: g.logprobs(z, scale=scale, stats=st), lambda: g.logprobs_backward(z, st, z, scale=scale),
+                     lambda: g.distill(z, torch.zeros(4, 1, dtype=torch.int32, device=DEV), st[:, :1].contiguous(), st[:, 0].contiguous(), scale=scale),
+                     lambda: g.score_logprobs(z.to(torch.bfloat16), z.to(torch.bfloat16), scale=scale, stats=st)):
+            with pytest.raises(binding.GramError) as e:
+                call()
+            assert e.value.status == 1
+    g.sync()
     g.close()
