@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(LP_THREADS, TOP && TPR == 32 ? 7 : LP_PER_SM) 
   const RowLogs logs = row_logs<T, TPR>(r, s.z, V, c, fpart);
   const float log_s = logs.log_s;
   if (tid == 0 && rank == 0) {
-    if (ask.stats) { ask.stats[2 * n] = r.m; ask.stats[2 * n + 1] = log_s; }
+    if (ask.stats) { ask.stats[2 * n] = row_largest(r.m, log_s); ask.stats[2 * n + 1] = log_s; }
     if (ask.entropy) ask.entropy[n] = logs.entropy;
   }
   for (int i = tid; rank == 0 && i < ask.C; i += TPR) {
@@ -417,7 +417,8 @@ __global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) logprobs_backward_kerne
     for (int i = 0; i < a.C; ++i) sum += here.value[i];
   }
   const float A = -a.scale * fmaf(h, H, sum), B = -a.scale * h * kLn2;
-  const bool none = (sum == 0.f && h == 0.f) || log_s == ROW_NEG_INF;    // nothing asked, or nothing left in the row
+  // nothing asked of a row without NaN, or nothing left in the row
+  const bool none = (sum == 0.f && h == 0.f && log_s == log_s) || log_s == ROW_NEG_INF;
   const RowPower l(m, log_s, c);
   const float inv = exp2f(-l.log2_s), Ay = inv * fmaf(-B, l.log2_s, A), By = inv * B;
   auto value = [&](float2 y) {
@@ -425,7 +426,7 @@ __global__ void __launch_bounds__(LP_THREADS, LP_PER_SM) logprobs_backward_kerne
   };
   auto plain = [&](float2 x) { return value(l.plain(x)); };
   auto any = [&](float2 x) { return none ? make_float2(0.f, 0.f) : value(l.is_huge ? l.huge(x) : l.plain(x)); };
-  auto one = [&](float x) { return x == ROW_NEG_INF ? 0.f : any(make_float2(x, x)).x; };
+  auto one = [&](float x) { return any(make_float2(x, x)).x; };
   const int chunks = s.template chunks<TPR, NV>();
   const bool fast = bytes == 16 && !none && !l.is_huge;
 #pragma unroll 2

@@ -82,6 +82,8 @@ __device__ __forceinline__ float row_log_sum(const RowStat& r, float c) {
   return r.m == ROW_NEG_INF ? logf(row_none(r)) : fmaf(fmaf(-r.m, c, row_ref(r.m, c)), kLn2, logf(r.s));
 }
 __device__ __forceinline__ float row_entropy(const RowStat& r) { return r.m == ROW_NEG_INF ? row_none(r) : logf(r.s) - kLn2 * (r.t / r.s); }
+// the largest logit as it is answered: a maximum passes over NaN
+__device__ __forceinline__ float row_largest(float m, float log_s) { return log_s != log_s ? log_s : m; }
 __device__ __forceinline__ float row_logp(float z, float m, float log_s, float scale) {
   if (z == ROW_NEG_INF) return log_s != log_s ? log_s : z;
   const float d = z - m;

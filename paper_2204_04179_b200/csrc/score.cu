@@ -613,7 +613,7 @@ __global__ void __launch_bounds__(32 * (ALONE ? SJ_ALONE_WARPS : SJ_WARPS)) scor
     if (lane == 0) ask.logp[n * ask.C + i] = lp;
   }
   if (lane == 0 && (!ALONE || warp == 0)) {
-    if (ask.stats) { ask.stats[2 * n] = r.m; ask.stats[2 * n + 1] = log_s; }
+    if (ask.stats) { ask.stats[2 * n] = row_largest(r.m, log_s); ask.stats[2 * n + 1] = log_s; }
     if (ask.entropy) ask.entropy[n] = entropy;
   }
   if (k == 0) return;

@@ -214,3 +214,66 @@ def test_scales_that_are_refused():
             assert e.value.status == 1
     g.sync()
     g.close()
+
+
+# ------------------------------ rows that hold NaN or +inf ------------------------------
+@pytest.mark.parametrize("asked", ["none", "sum of 0", "tokens", "entropy", "no tokens"])
+@pytest.mark.parametrize("N,V,dtype", FORMS + [(9, 5, "f32"), (9, 700, "bf16")])
+def test_gradients_of_rows_with_nan_or_infinity(N, V, dtype, asked):
+    """Their statistics and gradients are NaN whatever is asked of them, and those of the other rows as always."""
+    rng = np.random.default_rng(V)
+    n = 7
+    few = rng.standard_normal((n, V)) * 3
+    few[1, V // 2], few[4, V - 1], few[6] = np.nan, INF, -INF
+    few[6, V - 1] = np.nan
+    base, z = place(few, dtype)
+    view = base.repeat(-(-N // n), 1)[:N].contiguous()
+    bad, good = [1, 4, 6], [0, 2, 3, 5]
+    targets = np.zeros((n, 2), np.int32)
+    targets[:, 1] = V - 1
+    dlogp = np.ones((n, 2), np.float32)
+    dH = np.full(n, 0.5, np.float32) if asked == "entropy" else None
+    if asked == "none":
+        targets[:] = -1
+    if asked == "sum of 0":
+        dlogp[:, 1] = -1.0
+    if asked == "no tokens":
+        targets = dlogp = None
+    g = context()
+    out = answers(N, 0, 3)
+    g.logprobs(view, **out)
+    g.sync()
+    stats = out["stats"][:n].cpu().numpy()
+    assert np.isnan(stats[bad]).all() and np.isfinite(stats[good]).all()
+    r = Rows(z[good], 1.0)
+    entropy = out["entropy"][:n].cpu().numpy()
+    stats[good], entropy[good] = np.stack([r.m, r.log_s], 1), r.H
+    stats, entropy = _up(_tile(stats, N)), _up(_tile(entropy, N))
+    dz = torch.full_like(view, 7.0)
+    t, dl, dh = (_up(None if x is None else _tile(x, N)) for x in (targets, dlogp, dH))
+    g.logprobs_backward(view, stats, dz, targets=t, dlogp=dl, entropy=entropy, dentropy=dh)
+    g.sync()
+    assert torch.isnan(dz[:n][bad]).all()
+    want, bound = _backward_reference(r, None if targets is None else targets[good], None if dlogp is None else dlogp[good],
+                                      None if dH is None else dH[good], dtype)
+    near(dz[:n][good], want, bound, "gradient of the other rows")
+    g.logprobs_backward(view, stats, view, targets=t, dlogp=dl, entropy=entropy, dentropy=dh)
+    g.sync()
+    assert torch.equal(torch.nan_to_num(view, nan=1e3), torch.nan_to_num(dz, nan=1e3))
+    g.close()
+
+
+@pytest.mark.parametrize("N,V", [(6, 900), (300, 30_522), (700, 12_500)])
+def test_scores_with_nan_have_nan_statistics(N, V):
+    rng = np.random.default_rng(1)
+    users = torch.from_numpy(rng.integers(-3, 4, (N, 16)).astype(np.float32)).to(torch.bfloat16).to(DEV)
+    items = torch.from_numpy(rng.integers(-3, 4, (V, 16)).astype(np.float32)).to(torch.bfloat16).to(DEV)
+    users[3, 5] = float("nan")
+    g = context()
+    for k in (0, 4):
+        out = answers(N, 0, k)
+        g.score_logprobs(users, items, scale=0.05, **out)
+        g.sync()
+        assert torch.isnan(out["stats"][3]).all() and torch.isnan(out["entropy"][3])
+        assert torch.isfinite(out["stats"][[0, 1, 2, 4, 5]]).all()
+    g.close()
