@@ -136,41 +136,74 @@ def _ptr(t) -> C.c_void_p:
     return C.c_void_p(t.data_ptr())
 
 
-def _rows(t):
-    """(address, dtype, elements between rows) of a matrix whose rows are contiguous but may lie further apart."""
-    N, V = t.shape
-    ld, step = t.stride()
-    assert step == 1 or V <= 1, "rows must be contiguous"
-    return t.data_ptr(), _row_types()[t.dtype], ld if N > 1 else max(ld, V)
-
-
+# The calls on rows of logits take tensors that the device can read: in its memory, or in pinned host memory.  A serving loop makes them
+# for single rows: what is wrong with a tensor is looked for only where the tests fail.
 _ROW_TYPES = {}
+_current_stream = None
 
 
-def _row_types():
+def _row_setup():
+    import torch
+    global _current_stream
+    _ROW_TYPES.update({torch.float32: GRAM_F32, torch.bfloat16: GRAM_BF16, "f": torch.float32, "i": torch.int32})
+    raw, device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+    _current_stream = lambda: raw(device())  # noqa: E731
+
+
+def _no_matrix(t, what: str):
+    raise GramError(1, f"{what}: a matrix is needed, not shape {tuple(t.shape)}")
+
+
+def _rows(t, what: str):
+    """(address, dtype, elements between rows) of a matrix whose rows are contiguous but may lie further apart."""
     if not _ROW_TYPES:
-        import torch
-        _ROW_TYPES.update({torch.float32: GRAM_F32, torch.bfloat16: GRAM_BF16, "f": torch.float32, "i": torch.int32})
-    return _ROW_TYPES
+        _row_setup()
+    dtype = _ROW_TYPES.get(t.dtype)
+    try:
+        N, V = t.shape
+    except ValueError:
+        _no_matrix(t, what)
+    ld, step = t.stride()
+    if dtype is None or (step != 1 and V > 1) or not (t.is_cuda or t.is_pinned()):
+        raise GramError(1, f"{what}: float32 or bfloat16 is needed, not {t.dtype}" if dtype is None else
+                        f"{what}: the elements of a row must be contiguous, not {step} apart" if step != 1 and V > 1 else
+                        f"{what}: device or pinned host memory is needed, not {t.device}")
+    return t.data_ptr(), dtype, ld if N > 1 else max(ld, V)
 
 
-def _width(t) -> int:
-    return 0 if t is None else t.shape[1]
+def _gradient(logits, dlogits):
+    """(address, elements between rows) of a gradient of these logits."""
+    q, _, ld_out = _rows(dlogits, "dlogits")
+    if dlogits.shape != logits.shape or dlogits.dtype is not logits.dtype:
+        raise GramError(1, f"dlogits: {logits.dtype} {tuple(logits.shape)} is needed, not {dlogits.dtype} {tuple(dlogits.shape)}")
+    return q, ld_out
 
 
-def _array(t, kind: str, count: int):
+def _width(t, what: str) -> int:
+    if t is None:
+        return 0
+    try:
+        _, n = t.shape
+    except ValueError:
+        _no_matrix(t, what)
+    return n
+
+
+def _array(t, kind: str, count: int, what: str):
     """Address of a contiguous array of this type ("f" or "i") and number of elements; None -> NULL."""
     if t is None:
         return None
-    assert t.dtype is _ROW_TYPES[kind] and t.numel() == count and t.is_contiguous(), (t.dtype, t.shape, kind, count)
+    fits = t.dtype is _ROW_TYPES[kind] and t.numel() == count and t.is_contiguous()
+    if not fits or not (t.is_cuda or t.is_pinned()):
+        raise GramError(1, f"{what}: device or pinned host memory is needed, not {t.device}" if fits else
+                        f"{what}: a contiguous array of {count} {_ROW_TYPES[kind]} is needed, not {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
     return t.data_ptr()
 
 
 def _raw_stream(stream) -> int:
     """The stream's handle for a call with declared argument types."""
     if stream is None:
-        import torch
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        return _current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -312,40 +345,41 @@ class Gram:
 
     # answers over a pool, and learning from them: logits [N, V] fp32 or bf16, rows may lie further apart
     def logprobs(self, logits, scale=1.0, targets=None, logp=None, stats=None, entropy=None, top_logp=None, top_ids=None, stream=None):
-        p, dtype, ld = _rows(logits)
-        (N, V), nc, k = logits.shape, _width(targets), _width(top_ids)
-        self._ck(lib().gram_logprobs(self._h, p, dtype, ld, N, V, scale, _array(targets, "i", N * nc), nc, _array(logp, "f", N * nc),
-                                     _array(stats, "f", N * 2), _array(entropy, "f", N), _array(top_logp, "f", N * k),
-                                     _array(top_ids, "i", N * k), k, _raw_stream(stream)))
+        p, dtype, ld = _rows(logits, "logits")
+        (N, V), nc, k = logits.shape, _width(targets, "targets"), _width(top_ids, "top_ids")
+        self._ck(lib().gram_logprobs(self._h, p, dtype, ld, N, V, scale, _array(targets, "i", N * nc, "targets"), nc, _array(logp, "f", N * nc, "logp"),
+                                     _array(stats, "f", N * 2, "stats"), _array(entropy, "f", N, "entropy"),
+                                     _array(top_logp, "f", N * k, "top_logp"), _array(top_ids, "i", N * k, "top_ids"), k, _raw_stream(stream)))
 
     def logprobs_backward(self, logits, stats, dlogits, scale=1.0, targets=None, dlogp=None, entropy=None, dentropy=None, stream=None):
-        p, dtype, ld = _rows(logits)
-        q, dtype_out, ld_out = _rows(dlogits)
-        (N, V), nc = logits.shape, _width(targets)
-        assert dlogits.shape == logits.shape and dtype_out == dtype
-        self._ck(lib().gram_logprobs_backward(self._h, p, dtype, ld, N, V, scale, _array(targets, "i", N * nc), nc, _array(stats, "f", N * 2),
-                                              _array(entropy, "f", N), _array(dlogp, "f", N * nc), _array(dentropy, "f", N), q, ld_out,
+        p, dtype, ld = _rows(logits, "logits")
+        q, ld_out = _gradient(logits, dlogits)
+        (N, V), nc = logits.shape, _width(targets, "targets")
+        self._ck(lib().gram_logprobs_backward(self._h, p, dtype, ld, N, V, scale, _array(targets, "i", N * nc, "targets"), nc,
+                                              _array(stats, "f", N * 2, "stats"), _array(entropy, "f", N, "entropy"),
+                                              _array(dlogp, "f", N * nc, "dlogp"), _array(dentropy, "f", N, "dentropy"), q, ld_out,
                                               _raw_stream(stream)))
 
     def distill(self, logits, teacher_ids, teacher_logits, loss, scale=1.0, weight=None, dlogits=None, stream=None):
-        p, dtype, ld = _rows(logits)
-        (N, V), k = logits.shape, teacher_ids.shape[1]
-        q, ld_out = None, 0
-        if dlogits is not None:
-            q, dtype_out, ld_out = _rows(dlogits)
-            assert dlogits.shape == logits.shape and dtype_out == dtype
-        self._ck(lib().gram_distill(self._h, p, dtype, ld, N, V, scale, _array(teacher_ids, "i", N * k), _array(teacher_logits, "f", N * k), k,
-                                    _array(loss, "f", N), _array(weight, "f", N), q, ld_out, _raw_stream(stream)))
+        p, dtype, ld = _rows(logits, "logits")
+        (N, V), k = logits.shape, _width(teacher_ids, "teacher_ids")
+        q, ld_out = (None, 0) if dlogits is None else _gradient(logits, dlogits)
+        self._ck(lib().gram_distill(self._h, p, dtype, ld, N, V, scale, _array(teacher_ids, "i", N * k, "teacher_ids"),
+                                    _array(teacher_logits, "f", N * k, "teacher_logits"), k, _array(loss, "f", N, "loss"),
+                                    _array(weight, "f", N, "weight"), q, ld_out, _raw_stream(stream)))
 
     def score_logprobs(self, users, items, bias=None, scale=1.0, targets=None, logp=None, stats=None, entropy=None, top_logp=None,
                        top_ids=None, stream=None):
-        p, dtype, ld = _rows(users)
-        q, dtype_items, ld_items = _rows(items)
-        assert dtype == GRAM_BF16 and dtype_items == GRAM_BF16 and users.shape[1] == items.shape[1]
-        (N, d), V, nc, k = users.shape, items.shape[0], _width(targets), _width(top_ids)
-        self._ck(lib().gram_score_logprobs(self._h, p, ld, q, ld_items, _array(bias, "f", V), N, V, d, scale, _array(targets, "i", N * nc), nc,
-                                           _array(logp, "f", N * nc), _array(stats, "f", N * 2), _array(entropy, "f", N),
-                                           _array(top_logp, "f", N * k), _array(top_ids, "i", N * k), k, _raw_stream(stream)))
+        p, dtype, ld = _rows(users, "users")
+        q, dtype_items, ld_items = _rows(items, "items")
+        if dtype != GRAM_BF16 or dtype_items != GRAM_BF16 or users.shape[1] != items.shape[1]:
+            raise GramError(1, f"users and items: bfloat16 rows of one length are needed, not {users.dtype} {tuple(users.shape)} and {items.dtype} "
+                               f"{tuple(items.shape)}")
+        (N, d), V, nc, k = users.shape, items.shape[0], _width(targets, "targets"), _width(top_ids, "top_ids")
+        self._ck(lib().gram_score_logprobs(self._h, p, ld, q, ld_items, _array(bias, "f", V, "bias"), N, V, d, scale,
+                                           _array(targets, "i", N * nc, "targets"), nc, _array(logp, "f", N * nc, "logp"),
+                                           _array(stats, "f", N * 2, "stats"), _array(entropy, "f", N, "entropy"),
+                                           _array(top_logp, "f", N * k, "top_logp"), _array(top_ids, "i", N * k, "top_ids"), k, _raw_stream(stream)))
 
     def encoder_backward(self, G, items, U, stream=None):
         self._ck(lib().gram_encoder_backward(self._h, _ptr(G), _ptr(items), C.c_int32(U), _stream(stream)))
