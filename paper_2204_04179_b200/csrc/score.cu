@@ -9,7 +9,8 @@
 // Alternatives take a first pass over a part of the items (score_kernel<SAMPLE>), units of 128 spread over the table, which
 // writes the maxima of groups of 8 or 32 columns; score_bar_kernel takes from them a bar that at least k entries of a user
 // reach, and in the main pass a thread puts entries that reach its user's bar on a list of its own.  With a sample of S items
-// about k V / S entries of a user do.
+// about k V / S entries of a user do.  A sum of products is the same to the bit in both passes: it is formed in the order of d
+// whatever the tile's width and the item's place in it.
 //
 // Work is cut evenly: the units of 128 items of all row tiles, one row tile after another, are divided into contiguous
 // runs, one for each pair.  A run touches at most two row tiles, so a user's statistics and lists lie with a few pairs;

@@ -1,5 +1,5 @@
-"""Scores whose candidates are listed (more logits than are written and read again): equal ones in all row tiles, and rows of large
-logits."""
+"""Scores whose candidates are listed (more logits than are written and read again): equal ones in all row tiles, rows of large
+logits, and products that 32 bits round."""
 import numpy as np
 import pytest
 import torch
@@ -114,4 +114,56 @@ def test_scores_of_large_vectors(N, V, d, k, size, common):
             assert (np.abs(np.take_along_axis(z, where, 1) - best) <= 2 * dz).all()
             if scale * size >= 1e7:
                 assert np.array_equal(top, np.take_along_axis(logp, where, 1))
+    g.close()
+
+
+# ------------------------------ products that 32 bits round ------------------------------
+@pytest.mark.parametrize("k", [0, 1, 10, 50, 128])
+@pytest.mark.parametrize("N,V,d", [(300, 30_522, 768), (300, 30_522, 64), (257, 40_000, 100), (1000, 10_007, 1000), (1600, 5500, 328), (64, 140_001, 768)])
+def test_listed_scores_of_any_vectors(N, V, d, k):
+    """A sum of d products of bf16 values in 32 bits is off by at most d u times the sum of their sizes, however it is ordered.  The bar that
+    the sample of the table gives is reached by k entries of the main pass as well, whatever the width of their tiles."""
+    rng = np.random.default_rng(d + k)
+    pad = -d % 8
+    users = torch.nn.functional.pad(_up(rng.standard_normal((N, d)), torch.bfloat16), (0, pad), value=float("nan"))[:, :d]
+    items = torch.nn.functional.pad(_up(rng.standard_normal((V, d)) * 0.2, torch.bfloat16), (0, pad), value=float("nan"))[:, :d]
+    targets = rng.integers(0, V, (N, 2)).astype(np.int32)
+    scale = float(2.0 / np.sqrt(d))
+    g = context()
+    out = answers(N, 2, k)
+    g.score_logprobs(users, items, scale=scale, targets=_up(targets, torch.int32), **out)
+    g.sync()
+    u, w = users.double(), items.double()
+    dz = 2 * d * U * float((u.abs() @ w.abs().T).max())
+    r = Rows((u @ w.T).cpu().numpy(), scale)
+    check_answers(out, r, targets, 0, dz)
+    if k:
+        ids = out["top_ids"].cpu().numpy().astype(np.int64)
+        assert (ids >= 0).all() and all(len(set(row)) == k for row in ids)
+        best = -np.sort(-r.z, 1)[:, :k]
+        assert (np.abs(np.take_along_axis(r.z, ids, 1) - best) <= 2 * dz).all()
+        top = out["top_logp"].double().cpu().numpy()
+        assert (top[:, 1:] <= top[:, :-1]).all()
+        near(top, np.take_along_axis(r.logp, ids, 1), np.take_along_axis(r.d_logp, ids, 1) + 4 * r.scale * dz, "log p of alternatives")
+    g.close()
+
+
+@pytest.mark.parametrize("d", [72, 768, 1000])
+def test_a_product_is_the_same_in_every_pass_and_tile(d):
+    """What the bars rest on: the sum of a user and an item does not depend on the item's place in the table, on the width of its tile, on
+    the other users, nor on whether logits are written, listed or only summed.  The largest logit of a row shows it to the bit."""
+    N, V = 300, 30_522
+    rng = np.random.default_rng(d)
+    users, items = _up(rng.standard_normal((N, d)), torch.bfloat16), _up(rng.standard_normal((V, d)), torch.bfloat16)
+    g = context()
+    want = None
+    for shift in (0, 1, 128, 4000, 20_011):
+        table = items.roll(shift, 0)
+        for k in (0, 1, 10, 40, 128):
+            for rows in (slice(0, N), slice(40, N), slice(0, 20), slice(250, 270)):
+                out = answers(len(range(*rows.indices(N))), 0, k)
+                g.score_logprobs(users[rows], table, scale=0.1, **out)
+                g.sync()
+                want = out["stats"][:, 0] if want is None else want
+                assert torch.equal(out["stats"][:, 0], want[rows]), (shift, k, rows)
     g.close()
