@@ -452,62 +452,100 @@ __global__ void __launch_bounds__(32 * SB_ROWS) score_bar_kernel(const float* sa
   if (lane == 0) bars[n0 + r] = bar;
 }
 
-// users[n] . items[v], by a warp
-__device__ __forceinline__ float score_dot(const bf16* u, const bf16* w, int d) {
+// users[n] . items[v], by a warp: of M items at once, `apart` elements from one to the next
+template <int M> __device__ __forceinline__ void score_dots(const bf16* u, const bf16* w, int64_t apart, int d, float (&sum)[M]) {
   const int lane = threadIdx.x & 31;
-  float sum = 0.f;
+#pragma unroll
+  for (int m = 0; m < M; ++m) sum[m] = 0.f;
   for (int i = lane; i < d / 8; i += 32) {
-    const uint4 a = __ldg(reinterpret_cast<const uint4*>(u) + i), b = __ldg(reinterpret_cast<const uint4*>(w) + i);
+    const uint4 a = __ldg(reinterpret_cast<const uint4*>(u) + i);
+    uint4 b[M];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float2 x = RowVec<bf16>::pair(a, j), y = RowVec<bf16>::pair(b, j);
-      sum = fmaf(x.x, y.x, sum);
-      sum = fmaf(x.y, y.y, sum);
-    }
+    for (int m = 0; m < M; ++m) b[m] = __ldg(reinterpret_cast<const uint4*>(w + m * apart) + i);
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 x = RowVec<bf16>::pair(a, j), y = RowVec<bf16>::pair(b[m], j);
+        sum[m] = fmaf(x.x, y.x, sum[m]);
+        sum[m] = fmaf(x.y, y.y, sum[m]);
+      }
   }
-  if (lane < d % 8) sum = fmaf(__bfloat162float(u[d / 8 * 8 + lane]), __bfloat162float(w[d / 8 * 8 + lane]), sum);
+  if (lane < d % 8) {
+    const int i = d / 8 * 8 + lane;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  return sum;
+    for (int m = 0; m < M; ++m) sum[m] = fmaf(__bfloat162float(u[i]), __bfloat162float(w[m * apart + i]), sum[m]);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+    for (int m = 0; m < M; ++m) sum[m] += __shfl_xor_sync(0xffffffffu, sum[m], o);
 }
 
-// A user's logits as score_dot sums them, for rows of huge ones (out of line: with this in place the joining took 15 registers more).
+// A user's logits as score_dots sums them, for rows of huge ones (out of line: with this in place the joining took 15 registers more).
+// They are taken four at a time, once: of 4096 rows against 100 000 items of 768 in 109 ms (one at a time, once for the largest and once
+// for the sums: 255; a call on other rows: 0.5), of 300 rows, a block each, in 10.
 struct ScoreRow {
   const bf16 *user, *items;
   const float* bias;
   int64_t ld_i;
   int32_t V, d;
-  __device__ __forceinline__ float operator()(int v) const { return score_dot(user, items + (int64_t)v * ld_i, d) + (bias ? bias[v] : 0.f); }
+  __device__ __forceinline__ float operator()(int v) const {
+    float z[1];
+    score_dots<1>(user, items + (int64_t)v * ld_i, 0, d, z);
+    return z[0] + (bias ? bias[v] : 0.f);
+  }
+  // f(logit) of every step-th item of [v, end)
+  template <typename F> __device__ __forceinline__ void each(int v, int end, int step, F f) const {
+    for (; end - v > 3 * step; v += 4 * step) {
+      float z[4];
+      score_dots<4>(user, items + (int64_t)v * ld_i, step * ld_i, d, z);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f(z[j] + (bias ? bias[v + j * step] : 0.f));
+    }
+    for (; v < end; v += step) f((*this)(v));
+  }
 };
 __device__ __noinline__ float score_again(const ScoreRow& z, int v) { return z(v); }
-// of every step-th item from `first` on: the largest
-__device__ __noinline__ float score_largest(const ScoreRow& z, int first, int step) {
-  float m = ROW_NEG_INF;
-  for (int v = first; v < z.V; v += step) m = fmaxf(m, z(v));
-  return m;
+// sums of e = 2^y and e y as they are when every y moves by d <= 0
+__device__ __forceinline__ void score_raise(float& s, float& t, float d) {
+  d = fmaxf(d, -200.f);
+  const float f = row_ex2(d);
+  t = f * fmaf(s, d, t);
+  s *= f;
 }
-// and the sums relative to m: of 64 items, and of these, so that chains of additions are short
-__device__ __noinline__ float2 score_sums(const ScoreRow& z, float m, float c, int first, int step) {
-  float s = 0.f, t = 0.f;
+// The statistics of every step-th item from `first` on, relative to their largest logit.  The reference lags behind it as in RowSums: it
+// is raised by 2^4 at least, so that the roundings of these steps fade.  Sums are of 64 items, and of these: short chains of additions.
+__device__ __noinline__ RowStat score_sums(const ScoreRow& z, float c, int first, int step) {
+  RowStat r = row_empty();
+  float ref = ROW_NEG_INF;
   for (int v0 = first; v0 < z.V; v0 += 64 * step) {
-    float run_s = 0.f, run_t = 0.f;
-    for (int v = v0; v < z.V && v < v0 + 64 * step; v += step) {
-      const float y = (z(v) - m) * c, e = row_ex2(y);
-      run_s += e;
-      run_t = fmaf(e, fmaxf(y, -200.f), run_t);
-    }
-    s += run_s;
-    t += run_t;
+    float s = 0.f, t = 0.f;
+    z.each(v0, min(z.V, v0 + 64 * step), step, [&](float x) {
+      if (x == ROW_NEG_INF) return;
+      r.m = fmaxf(r.m, x);
+      if ((x - ref) * c > 4.f) {
+        score_raise(r.s, r.t, (ref - x) * c);
+        score_raise(s, t, (ref - x) * c);
+        ref = x;
+      }
+      const float y = (x - ref) * c, e = row_ex2(y);
+      s += e;
+      t = fmaf(e, fmaxf(y, -200.f), t);
+    });
+    r.s += s;
+    r.t += t;
   }
-  return make_float2(s, t);
+  if (r.m > ROW_NEG_INF) score_raise(r.s, r.t, (ref - r.m) * c);
+  return r;
 }
 
 // Joins the statistics of the runs that crossed a user's row tile, and their lists.  A warp takes a user, four users a block; where
 // users are few a block takes one (ALONE): its eight warps share the given tokens and the reading of the lists.
 // About 256 keys come in; more than fit are taken in turns, the best k of each going into the next.
 // A row of huge logits (row_is_huge) is summed again, relative to its largest logit itself.  A last place of such logits is worth many
-// units of an exponent, so that all its answers are taken from one set of them: the products as score_dot sums them, not those of the
-// tensor cores, which add in another order.  (Once over the table for the largest and once for the sums.)
+// units of an exponent, so that all its answers are taken from one set of them: the products as score_dots sums them, not those of the
+// tensor cores, which add in another order.
 constexpr int SJ_PARTS = (kNumSMs / 2 + 1) * SC_PARTS, SJ_KEYS = 512;          // parts of a user at most; keys of a turn
 constexpr int SJ_WARPS = 4, SJ_ALONE_WARPS = 8;
 template <bool ALONE>
@@ -518,7 +556,7 @@ __global__ void __launch_bounds__(32 * (ALONE ? SJ_ALONE_WARPS : SJ_WARPS)) scor
   __shared__ __align__(16) uint64_t keys_of[ROWS][SJ_KEYS];
   __shared__ const uint64_t* lists_of[ROWS][SJ_PARTS];
   __shared__ int starts_of[ROWS][SJ_PARTS + 1], kept;
-  __shared__ float huge_part[ALONE ? SJ_ALONE_WARPS : 1][3];
+  __shared__ RowStat huge_part[ALONE ? SJ_ALONE_WARPS : 1];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, slot = ALONE ? 0 : warp;
   const int64_t n = ALONE ? blockIdx.x : (int64_t)blockIdx.x * SJ_WARPS + warp;
   if (n >= a.N) return;                                 // whole warps; the block's barriers are in the other form only
@@ -582,26 +620,24 @@ __global__ void __launch_bounds__(32 * (ALONE ? SJ_ALONE_WARPS : SJ_WARPS)) scor
   float log_s = row_log_sum(r, a.c), entropy = row_entropy(r);
   const ScoreRow row_z{users + n * ld_u, items, a.bias, ld_i, a.V, d};
   const bool huge = row_is_huge(r.m, a.c);
-  if (huge) {                                           // in all warps of a block or in none: each takes every WARPS-th item
-    constexpr int WARPS = ALONE ? SJ_ALONE_WARPS : 1;
-    const int w = ALONE ? warp : 0;
-    r.m = score_largest(row_z, w, WARPS);
+  if (huge) {                                           // in all warps of a block or in none: each takes every eighth item
+    r = score_sums(row_z, a.c, ALONE ? warp : 0, ALONE ? SJ_ALONE_WARPS : 1);
     if (ALONE) {
-      if (lane == 0) huge_part[w][0] = r.m;
+      if (lane == 0) huge_part[warp] = r;
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < WARPS; ++i) r.m = fmaxf(r.m, huge_part[i][0]);
-    }
-    float2 st = score_sums(row_z, r.m, a.c, w, WARPS);
-    if (ALONE) {
-      if (lane == 0) { huge_part[w][1] = st.x; huge_part[w][2] = st.y; }
-      __syncthreads();
-      st = make_float2(0.f, 0.f);
+      for (int i = 0; i < SJ_ALONE_WARPS; ++i) r.m = fmaxf(r.m, huge_part[i].m);
+      r.s = r.t = 0.f;
 #pragma unroll
-      for (int i = 0; i < WARPS; ++i) { st.x += huge_part[i][1]; st.y += huge_part[i][2]; }
+      for (int i = 0; i < SJ_ALONE_WARPS; ++i) {
+        RowStat x = huge_part[i];
+        if (x.m > ROW_NEG_INF) score_raise(x.s, x.t, (x.m - r.m) * a.c);
+        r.s += x.s;
+        r.t += x.t;
+      }
     }
-    log_s = logf(st.x);
-    entropy = log_s - kLn2 * (st.y / st.x);
+    log_s = logf(r.s);
+    entropy = log_s - kLn2 * (r.t / r.s);
   }
   for (int i = ALONE ? warp : 0; i < ask.C; i += ALONE ? SJ_ALONE_WARPS : 1) {
     const int32_t t = ask.targets[n * ask.C + i];
