@@ -40,7 +40,7 @@ template <typename T> struct Slice {
   // A thread's single element: threads 0 .. 7 those at the row's start, 8 .. 15 those at its end.  -1: none
   __device__ __forceinline__ int edge(int tid) const {
     if (tid < 8) return first && tid < head ? tid : -1;
-    return last && tid < 16 && tail + tid - 8 < V ? tail + tid - 8 : -1;
+    return last && tid < 16 && tid - 8 < V - tail ? tail + (tid - 8) : -1;        // (tail + tid may leave 32 bits)
   }
   __device__ __forceinline__ int place(int v) const { return head + v * N; }
   __device__ __forceinline__ const uint4* vectors() const { return reinterpret_cast<const uint4*>(z + head); }
@@ -101,7 +101,7 @@ __device__ __forceinline__ RowStat join_slices(const RowStat* of, int slices, fl
 template <typename T, int TPR> __device__ __noinline__ float2 huge_sums(const T* z, int V, float m, float c, float* part) {
   using G = Group<TPR>;
   float s = 0.f, t = 0.f;
-  for (int v = G::tid(); v < V; v += TPR) {
+  for (uint32_t v = G::tid(); v < (uint32_t)V; v += TPR) {          // V + TPR may leave 31 bits
     const float y = (row_load(z + v) - m) * c, e = row_ex2(y);
     s += e;
     t = fmaf(e, fmaxf(y, -200.f), t);
@@ -281,7 +281,7 @@ template <typename T> __device__ __forceinline__ void store_vector(T* at, const 
 template <typename T, int TPR, int NV, typename F, typename A>
 __device__ __forceinline__ void store_chunk(const Slice<T>& s, int ch, int tid, const uint4 (&q)[NV], T* dz, int bytes, bool fast, F plain, A any) {
   const int v = s.v0 + ch * (TPR * NV) + tid;
-  T* at = dz + s.place(v);
+  T* at = dz + ((uint32_t)s.head + (uint32_t)v * RowVec<T>::N);       // v may lie past the slice, and its place past 31 bits
   if (fast && v - tid + TPR * NV <= s.v1) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {

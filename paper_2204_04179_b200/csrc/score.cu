@@ -726,8 +726,8 @@ RowAnswers from(RowAnswers ask, int64_t n) {
 gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_users, const void* items, int64_t ld_items,
                                   const float* bias, int64_t N, int32_t V, int32_t d, float scale, const RowAnswers& ask, void* ws,
                                   size_t ws_bytes, cudaStream_t st) {
+  if (V > (1 << 30) / (kNumSMs / 2) * SC_UNIT) return gram_set_error(ctx, "gram_score_logprobs: %d items", V), GRAM_ERR_UNSUPPORTED;   // units of all row tiles, in 32 bits
   const int32_t all_units = ceil_div(V, SC_UNIT);
-  if (all_units > (1 << 30) / (kNumSMs / 2)) return gram_set_error(ctx, "gram_score_logprobs: %d items", V), GRAM_ERR_UNSUPPORTED;
   CUtensorMap map_u, map_i;
   // copies are no larger than the users (rows past the last are filled with zeros, which takes time: one user against 100 000
   // items of 768 46 us with boxes of 128 rows, 35 with boxes of 8)

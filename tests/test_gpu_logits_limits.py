@@ -277,3 +277,64 @@ def test_scores_with_nan_have_nan_statistics(N, V):
         assert torch.isnan(out["stats"][3]).all() and torch.isnan(out["entropy"][3])
         assert torch.isfinite(out["stats"][[0, 1, 2, 4, 5]]).all()
     g.close()
+
+
+# ------------------------------ rows of 2^31 - 1 elements ------------------------------
+@pytest.mark.parametrize("dtype,offset", [("bf16", 3), ("f32", 1)])
+def test_a_row_of_the_most_elements(dtype, offset):
+    """Places, vectors and single elements at the row's end count to 2^31 - 1 without leaving 32 bits; nothing behind the row is
+    touched.  Places of -4 and a few hundred others, the last ones among them.  A thread of eight blocks adds up V / 2^10 elements, 16 or
+    32 of them at a time: the sum is off by less than V 2^-14 u = 2^-7 of itself."""
+    V, k, scale = 2 ** 31 - 1, 10, 0.5
+    rng = np.random.default_rng(1)
+    at = np.unique(np.concatenate([np.arange(V - 20, V), np.arange(20), rng.integers(0, V, 300)]))
+    value = rng.permutation(len(at)) / 64.0               # exact in bf16 up to 4
+    value = np.where(value < 4, value, -4.0)
+    value[-1] = 3.875                                     # in the last place
+    flat = torch.full((V + offset + 64,), -4.0, dtype=DT[dtype], device=DEV)
+    flat[:offset], flat[offset + V:] = 9.0, 9.0
+    row = flat[offset:offset + V].view(1, V)
+    where = _up(at.astype(np.int64))
+    row[0, where] = _up(value).to(DT[dtype])
+    y = scale * (value - value.max())
+    base = np.exp(scale * (-4.0 - value.max()))
+    s = (V - len(at)) * base + np.exp(y).sum()
+    order = np.lexsort((at, -value))[:k]
+    g = context()
+    out = answers(1, 2, k)
+    targets = _up(np.array([[V - 1, at[len(at) // 2]]], np.int32))
+    g.logprobs(row, scale=scale, targets=targets, **out)
+    g.sync()
+    assert out["top_ids"][0].tolist() == at[order].tolist()
+    near(out["stats"][0], np.array([value.max(), np.log(s)]), np.array([0.0, 2.0 ** -6]), "statistics")
+    near(out["logp"][0], np.array([y[-1], y[len(at) // 2]]) - np.log(s), 2.0 ** -6, "log p")
+    p = np.exp(y) / s
+    loss, ids = torch.empty(1, device=DEV), np.concatenate([at[-1:], at[:1]]).astype(np.int32)[None]
+    g.distill(row, _up(ids), torch.zeros(1, 2, device=DEV), loss, scale=scale, dlogits=row)      # in place
+    g.sync()
+    want = p.copy()
+    want[[-1, 0]] -= 0.5
+    near(row[0, where], scale * want, 2.0 ** -6 * scale * np.abs(want), "gradient")
+    rest = row[0, 21:10 ** 9 + 7:9973]
+    rest = rest[(rest - float(scale * base / s)).abs() > 2.0 ** -6 * float(scale * base / s)]
+    assert len(rest) <= 300                               # those of other values
+    assert (flat[:offset] == 9).all() and (flat[offset + V:] == 9).all()
+    row.fill_(-4.0)
+    row[0, where] = _up(value).to(DT[dtype])
+    g.logprobs_backward(row, out["stats"], row, scale=scale, targets=targets[:, :1].contiguous(), dlogp=torch.ones(1, 1, device=DEV))
+    g.sync()
+    want = -p
+    want[-1] += 1.0
+    near(row[0, where], scale * want, 2.0 ** -6 * scale * np.abs(want), "gradient of log p")
+    assert (flat[:offset] == 9).all() and (flat[offset + V:] == 9).all()
+    g.close()
+
+
+def test_tables_of_too_many_items_are_refused():
+    g = context()
+    u, st = torch.zeros(4, 8, dtype=torch.bfloat16, device=DEV), torch.zeros(4, 2, device=DEV)
+    P = lambda t: t.data_ptr()  # noqa: E731
+    for V in (2 ** 31 - 1, 2 ** 31 - 127, 1_857_283_073):    # refused before anything is read
+        assert binding.lib().gram_score_logprobs(g._h, P(u), 8, P(u), 8, None, 4, V, 8, 1.0, None, 0, None, P(st), None, None, None, 0, 0) == 4
+    g.sync()
+    g.close()
