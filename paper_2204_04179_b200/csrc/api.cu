@@ -484,13 +484,17 @@ static gram_status check_answers(gram_ctx* ctx, const char* name, const RowAnswe
   ROWS_ARG(N == 0 || ask.k == 0 || (ask.top_ids && ask.top_logp), "alternatives need both arrays");
   return GRAM_OK;
 }
-// a gradient may take the logits' own place, row on row; another overlap would be overwritten before it is read
+// a gradient may take the logits' own place, row on row, or lie beside them in rows of one buffer; another overlap would be
+// overwritten before it is read
 static gram_status check_overlap(gram_ctx* ctx, const char* name, const void* z, int64_t ld, const void* dz, int64_t ld_out, int dtype,
                                  int64_t N, int32_t V) {
   const int64_t size = dtype == GRAM_F32 ? 4 : 2;
   const uintptr_t a = reinterpret_cast<uintptr_t>(z), b = reinterpret_cast<uintptr_t>(dz);
   const uintptr_t a_end = a + (uintptr_t)(((N - 1) * ld + V) * size), b_end = b + (uintptr_t)(((N - 1) * ld_out + V) * size);
-  ROWS_ARG(N == 0 || (a == b && (ld == ld_out || N == 1)) || a_end <= b || b_end <= a, "the gradient overlaps the logits");
+  if (N == 0 || (a == b && (ld == ld_out || N == 1)) || a_end <= b || b_end <= a) return GRAM_OK;
+  const uintptr_t row = (uintptr_t)V * size, pitch = (uintptr_t)ld * size;
+  const uintptr_t past = b > a ? (b - a) % pitch : (pitch - (a - b) % pitch) % pitch;      // where a row of the one begins in those of the other
+  ROWS_ARG(ld == ld_out && past >= row && past + row <= pitch, "the gradient overlaps the logits");
   return GRAM_OK;
 }
 

@@ -338,3 +338,36 @@ def test_tables_of_too_many_items_are_refused():
         assert binding.lib().gram_score_logprobs(g._h, P(u), 8, P(u), 8, None, 4, V, 8, 1.0, None, 0, None, P(st), None, None, None, 0, 0) == 4
     g.sync()
     g.close()
+
+
+# ------------------------------ a gradient beside its logits ------------------------------
+@pytest.mark.parametrize("N,V", [(5, 64), (2400, 300), (7, 20_001)])
+def test_gradients_beside_their_logits(N, V):
+    """Logits and gradients as the halves of one buffer's rows do not overlap, whichever comes first; what does is refused."""
+    rng = np.random.default_rng(V)
+    z = rng.standard_normal((N, V))
+    a, ids = rng.standard_normal((N, 4)).astype(np.float32), rng.integers(0, V, (N, 4)).astype(np.int32)
+    g = context()
+    r = Rows(z.astype(np.float32).astype(np.float64), 1.0)
+    _, _, want, bound = _distill_reference(r, ids, a.astype(float), np.ones(N))
+    back, back_bound = _backward_reference(r, ids[:, :1], a[:, :1], None, "f32")
+    stats, loss = _up(np.stack([r.m, r.log_s], 1).astype(np.float32)), torch.empty(N, device=DEV)
+    flat = torch.zeros(N * (2 * V + 4) + 8, device=DEV)
+    both = flat[:N * (2 * V + 3)].view(N, 2 * V + 3)
+    left, right, middle = both[:, :V], both[:, V + 3:], both[:, V:2 * V]
+    for logits, dz in ((left, right), (right, left), (left, middle)):
+        logits.copy_(_up(z.astype(np.float32)))
+        g.distill(logits, _up(ids), _up(a), loss, dlogits=dz)
+        g.sync()
+        near(dz, want, bound, "gradient")
+        g.logprobs_backward(logits, stats, dz, targets=_up(ids[:, :1]), dlogp=_up(a[:, :1]))
+        g.sync()
+        near(dz, back, back_bound, "gradient of log p")
+        assert torch.equal(logits, _up(z.astype(np.float32)))
+    wide = flat[1:].as_strided((N, V), (2 * V + 4, 1))                    # rows of another distance run into the logits
+    for logits, dz in ((left, both[:, V - 1:2 * V - 1]), (right, both[:, 4:V + 4]), (left, both[:, 1:V + 1]), (right, wide)):
+        with pytest.raises(binding.GramError) as e:
+            g.distill(logits, _up(ids), _up(a), loss, dlogits=dz)
+        assert e.value.status == 1
+    g.sync()
+    g.close()
