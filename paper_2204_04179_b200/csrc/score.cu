@@ -18,9 +18,11 @@
 //
 // Where logits are few they are written after all (score_kernel<LOGITS>) and gram_logprobs' kernel reads them.
 //
-// Bounded by the products where users are many, by the table's bytes where they are few.  Measured against 100 000 items of 768:
-// 4096 users 380 us (1650 TFLOP/s), with 10 alternatives 448; 1024 users 107 and 152 to 166; 64 users with 10 alternatives 48, one
-// user 41 (the table's 154 MB at 6458 GB/s: 24).
+// Bounded by the products where users are many, by the table's bytes where they are few.  Measured against 100 000 items of 768 (8-bit
+// codes; calls in a chain, on two tables in turn): 4096 users 373 us (1690 TFLOP/s), with 10 alternatives 475 to 500, on the same
+// inputs 454, among calls whose inputs all differ 520; 1024 users 105 and 149; 64 users with 10 alternatives 46, one user 40 (the
+// table's 154 MB at 6458 GB/s: 24).  Vectors of normal values take more power: 4096 users 400 and 515.  Where all scores are equal, so
+// that lists are cut again and again, 4096 users with 10 alternatives take 1320, with 50 2350.
 #include "logits.h"
 #include "row_softmax.cuh"
 #include "row_top.cuh"
@@ -66,7 +68,7 @@ struct ScoreArgs {
 // The tiles of a run, as all roles walk over them.  A run is as long as all others, so it holds every residue of the unit's number
 // modulo that length once; it begins with residue 0 and turns to its start at its end.  All pairs are then at units of about the
 // same residue at any time, and the row tiles' reads of the table meet in L2: 1024 users against 100 000 items of 768 with 10
-// alternatives 195 us from end to end of the run and 166 so, 4096 users 496 and 448.
+// alternatives 165 us from end to end of the run and 149 so, 4096 users 490 and 454 (calls one after another on the same inputs).
 struct ScoreRun {
   int units, stride, per_run, begin, at, end;    // at: what lies ahead of the current row tile's part
   int lo, turn, stop;            // the part's first unit, where it begins, where its current piece ends
