@@ -207,7 +207,8 @@ gram_status gram_selftest_bounded_wait(gram_ctx* ctx, gram_stream stream);
  * segment sums of many wide rows): in the context's later
  * calls a warp gives up on its wait for row number `rows` (from 0) of those it has to read, as if the copy never arrived.
  * The calls return GRAM_OK, what the kernels add to is left without the rows' sums, and the next gram_sync returns
- * GRAM_ERR_TIMEOUT.  rows < 0: no such limit (as created). */
+ * GRAM_ERR_TIMEOUT.  In gram_score_logprobs the copies give up on tile number `rows` of a pair of multiprocessors; the call's answers
+ * are not defined then.  rows < 0: no such limit (as created). */
 gram_status gram_selftest_ring_rows(gram_ctx* ctx, int32_t rows);
 /* Small batches of gram_dedup and the fp32 matrix products use clusters of up to 16 thread blocks, sums of partial column sums
  * clusters of 8.  Where a process has too few multiprocessors for that, a context uses the largest clusters that can be placed

@@ -62,6 +62,7 @@ struct ScoreArgs {
   int64_t sample_rows;
   int32_t fine;                  // groups of 8
   int32_t stride;                // the pass takes every stride-th two units of the table
+  int32_t give_up;               // tile of a run at which its copies stop (gram_selftest_ring_rows)
   int32_t* status;
 };
 
@@ -228,7 +229,8 @@ __global__ void __launch_bounds__(SC_THREADS, 1) score_kernel(const __grid_const
     int s = 0;
     uint32_t ph = 0;
     const uint32_t lead_bar0 = map_to_cta(bar0, 0);
-    while (!failed && run.next()) {
+    for (int tile = 0; !failed && run.next(); ++tile) {
+      if (tile == a.give_up) { failed = true; break; }
       const int m0 = run.tm * SC_ROWS + (int)rank * SM_ROWS;
       const int n0 = run.column() + (int)rank * (run.width * SC_UNIT / 2);     // this block's half of the items: boxes of 64
       // a block whose users are all past the last fetches none; what its rows of the product hold is not looked at
@@ -545,6 +547,8 @@ __device__ __noinline__ RowStat score_sums(const ScoreRow& z, float c, int first
 // Joins the statistics of the runs that crossed a user's row tile, and their lists.  A warp takes a user, four users a block; where
 // users are few a block takes one (ALONE): its eight warps share the given tokens and the reading of the lists.
 // About 256 keys come in; more than fit are taken in turns, the best k of each going into the next.
+// Where a wait of the main pass ran out (the call's answers are not defined then) parts of the statistics and lists were never written: how
+// many entries a list holds, and which item one names, are held within their arrays, and a turn that has no room ends the reading.
 // A row of huge logits (row_is_huge) is summed again, relative to its largest logit itself.  A last place of such logits is worth many
 // units of an exponent, so that all its answers are taken from one set of them: the products as score_dots sums them, not those of the
 // tensor cores, which add in another order.
@@ -577,7 +581,6 @@ __global__ void __launch_bounds__(32 * (ALONE ? SJ_ALONE_WARPS : SJ_WARPS)) scor
     int have = 0;
     if (i < parts) {
       const float4 f = a.stats[((int64_t)(p * 2 + (p == p0 && p * a.per_run < tm * a.units ? 1 : 0)) * SC_PARTS + part) * SC_ROWS + row];
-      have = __float_as_int(f.w);
       RowStat x{f.x, f.y, f.z};
       const float m = fmaxf(r.m, x.m);
       if (m > r.m) row_raise(r, m, a.c);
@@ -585,6 +588,7 @@ __global__ void __launch_bounds__(32 * (ALONE ? SJ_ALONE_WARPS : SJ_WARPS)) scor
       r.s += x.s;
       r.t += x.t;
       const bool early = p == p1 && min((p + 1) * a.per_run, a.total) > (tm + 1) * a.units;      // the run goes on with the next row tile
+      have = max(0, min(__float_as_int(f.w), early ? a.early_cap : a.cap));
       lists_of[slot][i] = early ? a.early + ((int64_t)(tm * SC_PARTS + part) * SC_ROWS + row) * a.early_cap
                                 : a.lists + ((int64_t)(p * SC_PARTS + part) * SC_ROWS + row) * a.cap;
     }
@@ -664,7 +668,7 @@ __global__ void __launch_bounds__(32 * (ALONE ? SJ_ALONE_WARPS : SJ_WARPS)) scor
     }
     sync();
     if (ALONE) have = kept;
-    if (from == all) break;
+    if (from == all || have == SJ_KEYS) break;
     const int count = min(all - from, SJ_KEYS - have);
     take(from, count, have);
     from += count;
@@ -679,7 +683,7 @@ __global__ void __launch_bounds__(32 * (ALONE ? SJ_ALONE_WARPS : SJ_WARPS)) scor
     float z = row_key_logit(key);
     if (huge)
       for (int j = 0; j < 32 && i0 + j < have; ++j) {
-        const float x = score_again(row_z, row_key_place(keys[i0 + j]));
+        const float x = score_again(row_z, (int)min((uint32_t)row_key_place(keys[i0 + j]), (uint32_t)a.V - 1u));
         if (lane == j) z = x;
       }
     const int above = i < have ? top_above<32>(keys, have, i) : k;
@@ -745,6 +749,7 @@ gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_u
   a.k = ask.k;
   a.c = scale * kLog2e;
   a.stride = 1;
+  a.give_up = gram_ring_rows(ctx);
   a.status = gram_status_word(ctx);
   // Logits that the workspace holds (32 MB of it at most: they stay in L2) are written and read once more, in place of the sample,
   // the bars and the joining.  This way and the other, in us, items of 768:
