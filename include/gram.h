@@ -359,6 +359,27 @@ gram_status gram_score_logprobs(gram_ctx* ctx, const void* d_users, int64_t ld_u
                                 const float* d_bias, int64_t N, int32_t V, int32_t d, float scale, const int32_t* d_targets,
                                 int32_t C, float* d_logp, float* d_stats, float* d_entropy, float* d_top_logp,
                                 int32_t* d_top_ids, int32_t k, gram_stream stream);
+/* Softmax cross entropy of users against the item table, and its gradients, without an [N, V] array: with z as in gram_score_logprobs and
+ * p the softmax of scale z,
+ *   d_loss[n]      = -log p[n, d_targets[n]];  0 for a target of -1 ("none"), +inf for one that d_bias takes out
+ * and, each where its array is given, the gradients of sum_n weight[n] loss[n], with g[n, v] = weight[n] scale (p[n, v] - [v = d_targets[n]]):
+ *   d_dusers[n, :] = sum_v g[n, v] items[v, :]     d_ditems[v, :] = sum_n g[n, v] users[n, :]     d_dbias[v] = sum_n g[n, v]
+ * d_targets int32 [N], d_weight fp32 [N] or NULL (all 1), d_loss fp32 [N], d_dbias fp32 [V] (asked without d_bias too: that of zeros).  A row
+ * takes no part in the gradients if its target is "none" or taken out or its weight 0: its row of d_dusers is 0, and its vector, whatever
+ * it holds, reaches nothing else.  A row that holds NaN or +inf has loss NaN, and so have the gradients it takes part in.
+ * d_dusers and d_ditems are `grad_dtype`, rows a multiple of 16 bytes apart, 16-byte aligned, d a multiple of 8 (GRAM_ERR_UNSUPPORTED
+ * else); they must not overlap the inputs or each other.  For GRAM_BF16 g is rounded to bf16 before the two products, as a gradient that passes through
+ * bf16 is; for GRAM_F32 it enters them as the sum of two bf16 (to 2^-16 of itself), at half again the cost.
+ * g is formed for a piece of the items at a time in d_workspace, 256-byte aligned device memory of the caller's: as large a piece as
+ * workspace_bytes allow.  Its content means nothing before and after; calls that may run at the same time need one each.  The call also uses the
+ * context's workspace for matrix products.  Results depend, within rounding, on the size of the workspace, and repeat bit for bit. */
+gram_status gram_score_loss(gram_ctx* ctx, const void* d_users, int64_t ld_users, const void* d_items, int64_t ld_items, const float* d_bias,
+                            int64_t N, int32_t V, int32_t d, float scale, const int32_t* d_targets, const float* d_weight, float* d_loss,
+                            int grad_dtype, void* d_dusers, int64_t ld_dusers, void* d_ditems, int64_t ld_ditems, float* d_dbias,
+                            void* d_workspace, int64_t workspace_bytes, gram_stream stream);
+/* Bytes of workspace for a call of these sizes with all gradients (host only): the least that serves, and the size beyond which nothing
+ * is gained.  Either pointer may be NULL. */
+gram_status gram_score_loss_workspace(int64_t N, int32_t V, int32_t d, int grad_dtype, int64_t* h_least, int64_t* h_best);
 
 /* --- checkpoint / resume (the paper keeps the checkpoint of the best validation epoch, Appendix D) ------------------
  * Everything a context holds besides what the caller gave it: parameters (gram_get_params / gram_set_params), the

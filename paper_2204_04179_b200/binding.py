@@ -36,13 +36,14 @@ SYMBOLS = ["gram_create", "gram_destroy", "gram_sync", "gram_last_error", "gram_
            "gram_launch_count", "gram_profile_dump", "gram_accumulate_static", "gram_optimizer_step",
            "gram_optimizer_reset", "gram_noam_rate", "gram_adam_update", "gram_state_export", "gram_state_import",
            "gram_optimizer_export", "gram_optimizer_import", "gram_selftest_bounded_wait", "gram_selftest_ring_rows", "gram_selftest_cluster_blocks", "gram_selftest_column_sums", "gram_grads_device",
-           "gram_gemm_bf16_epilogue", "gram_logprobs", "gram_logprobs_backward", "gram_distill", "gram_score_logprobs"]
+           "gram_gemm_bf16_epilogue", "gram_logprobs", "gram_logprobs_backward", "gram_distill", "gram_score_logprobs",
+           "gram_score_loss", "gram_score_loss_workspace"]
 
 # argument types of the calls on rows of logits, which a serving loop makes for single rows: declared once, so that a call passes
 # plain numbers and addresses (p: address, i: int32, l: int64, f: float)
 _TYPES = {"p": C.c_void_p, "i": C.c_int32, "l": C.c_int64, "f": C.c_float}
 _ROW_CALLS = {"gram_logprobs": "ppillifpipppppip", "gram_logprobs_backward": "ppillifpippppplp", "gram_distill": "ppillifppippplp",
-              "gram_score_logprobs": "pplplpliifpipppppip"}
+              "gram_score_logprobs": "pplplpliifpipppppip", "gram_score_loss": "pplplpliifpppiplplpplp"}
 
 KINDS = ["gemm", "attention", "layernorm", "colsum", "embed_pool", "dedup", "gather", "accumulate", "task_head", "other",
          "optimizer"]
@@ -145,7 +146,7 @@ _current_stream = None
 def _row_setup():
     import torch
     global _current_stream
-    _ROW_TYPES.update({torch.float32: GRAM_F32, torch.bfloat16: GRAM_BF16, "f": torch.float32, "i": torch.int32})
+    _ROW_TYPES.update({torch.float32: GRAM_F32, torch.bfloat16: GRAM_BF16, "f": torch.float32, "i": torch.int32, "b": torch.uint8})
     raw, device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
     _current_stream = lambda: raw(device())  # noqa: E731
 
@@ -177,6 +178,26 @@ def _gradient(logits, dlogits):
     if dlogits.shape != logits.shape or dlogits.dtype is not logits.dtype:
         raise GramError(1, f"dlogits: {logits.dtype} {tuple(logits.shape)} is needed, not {dlogits.dtype} {tuple(dlogits.shape)}")
     return q, ld_out
+
+
+def _vectors(users, items):
+    """(address, elements between rows) of users and of items, bfloat16 rows of one length."""
+    p, dtype, ld = _rows(users, "users")
+    q, dtype_items, ld_items = _rows(items, "items")
+    if dtype != GRAM_BF16 or dtype_items != GRAM_BF16 or users.shape[1] != items.shape[1]:
+        raise GramError(1, f"users and items: bfloat16 rows of one length are needed, not {users.dtype} {tuple(users.shape)} and {items.dtype} "
+                           f"{tuple(items.shape)}")
+    return p, ld, q, ld_items
+
+
+def _vector_gradient(vectors, grad, what: str):
+    """(address, elements between rows, type) of a gradient of these vectors; None -> NULL."""
+    if grad is None:
+        return None, 0, None
+    q, dtype, ld = _rows(grad, what)
+    if grad.shape != vectors.shape:
+        raise GramError(1, f"{what}: shape {tuple(vectors.shape)} is needed, not {tuple(grad.shape)}")
+    return q, ld, dtype
 
 
 def _width(t, what: str) -> int:
@@ -370,16 +391,36 @@ class Gram:
 
     def score_logprobs(self, users, items, bias=None, scale=1.0, targets=None, logp=None, stats=None, entropy=None, top_logp=None,
                        top_ids=None, stream=None):
-        p, dtype, ld = _rows(users, "users")
-        q, dtype_items, ld_items = _rows(items, "items")
-        if dtype != GRAM_BF16 or dtype_items != GRAM_BF16 or users.shape[1] != items.shape[1]:
-            raise GramError(1, f"users and items: bfloat16 rows of one length are needed, not {users.dtype} {tuple(users.shape)} and {items.dtype} "
-                               f"{tuple(items.shape)}")
+        p, ld, q, ld_items = _vectors(users, items)
         (N, d), V, nc, k = users.shape, items.shape[0], _width(targets, "targets"), _width(top_ids, "top_ids")
         self._ck(lib().gram_score_logprobs(self._h, p, ld, q, ld_items, _array(bias, "f", V, "bias"), N, V, d, scale,
                                            _array(targets, "i", N * nc, "targets"), nc, _array(logp, "f", N * nc, "logp"),
                                            _array(stats, "f", N * 2, "stats"), _array(entropy, "f", N, "entropy"),
                                            _array(top_logp, "f", N * k, "top_logp"), _array(top_ids, "i", N * k, "top_ids"), k, _raw_stream(stream)))
+
+    def score_loss(self, users, items, targets, loss, workspace, bias=None, scale=1.0, weight=None, dusers=None, ditems=None, dbias=None, stream=None):
+        """workspace: uint8, at least score_loss_workspace(...)[0] bytes."""
+        p, ld, q, ld_items = _vectors(users, items)
+        (N, d), V = users.shape, items.shape[0]
+        gu, ld_gu, type_u = _vector_gradient(users, dusers, "dusers")
+        gi, ld_gi, type_i = _vector_gradient(items, ditems, "ditems")
+        if type_u is not None and type_i is not None and type_u != type_i:
+            raise GramError(1, f"dusers and ditems: one type is needed, not {dusers.dtype} and {ditems.dtype}")
+        self._ck(lib().gram_score_loss(self._h, p, ld, q, ld_items, _array(bias, "f", V, "bias"), N, V, d, scale, _array(targets, "i", N, "targets"),
+                                       _array(weight, "f", N, "weight"), _array(loss, "f", N, "loss"), (type_u if type_u is not None else type_i) or 0,
+                                       gu, ld_gu, gi, ld_gi, _array(dbias, "f", V, "dbias"), _array(workspace, "b", workspace.numel(), "workspace"),
+                                       workspace.numel(), _raw_stream(stream)))
+
+    @staticmethod
+    def score_loss_workspace(N: int, V: int, d: int, grad_dtype):
+        """(least, best) bytes of score_loss's workspace; grad_dtype: the gradients' torch type."""
+        if not _ROW_TYPES:
+            _row_setup()
+        least, best = C.c_int64(0), C.c_int64(0)
+        st = lib().gram_score_loss_workspace(C.c_int64(N), C.c_int32(V), C.c_int32(d), C.c_int(_ROW_TYPES.get(grad_dtype, -1)), C.byref(least), C.byref(best))
+        if st != 0:
+            raise GramError(st, f"score_loss_workspace: N = {N}, V = {V}, d = {d}, {grad_dtype}")
+        return least.value, best.value
 
     def encoder_backward(self, G, items, U, stream=None):
         self._ck(lib().gram_encoder_backward(self._h, _ptr(G), _ptr(items), C.c_int32(U), _stream(stream)))

@@ -8,6 +8,7 @@
 #include "model.h"
 #include "layers.h"
 #include "logits.h"
+#include "score_loss.h"
 
 constexpr int kProfSlots = 16384;
 struct ProfRec {
@@ -484,6 +485,27 @@ static gram_status check_answers(gram_ctx* ctx, const char* name, const RowAnswe
   ROWS_ARG(N == 0 || ask.k == 0 || (ask.top_ids && ask.top_logp), "alternatives need both arrays");
   return GRAM_OK;
 }
+// users and items of bf16, as bulk copies read them
+static gram_status check_vectors(gram_ctx* ctx, const char* name, const void* users, int64_t* ld_users, const void* items, int64_t* ld_items,
+                                 int64_t N, int32_t V, int32_t d) {
+  ROWS_ARG(d >= 1 && *ld_users >= d && *ld_items >= d, "rows must be at least d elements apart, d positive");
+  ROWS_ARG(*ld_items <= INT64_MAX / 8 / V && *ld_users <= INT64_MAX / 8 / (N > 0 ? N : 1), "rows too far apart");
+  ROWS_ARG(N == 0 || (users && items), "null vectors");
+  if (N == 1) *ld_users = (*ld_users + 7) / 8 * 8;      // of a single row the distance means nothing
+  if (V == 1) *ld_items = (*ld_items + 7) / 8 * 8;
+  if (*ld_users % 8 || *ld_items % 8 || reinterpret_cast<uintptr_t>(users) % 16 || reinterpret_cast<uintptr_t>(items) % 16)
+    return gram_set_error(ctx, "%s: vectors must be 16-byte aligned, rows a multiple of 8 elements apart", name), GRAM_ERR_UNSUPPORTED;
+  return GRAM_OK;
+}
+// their gradients, which leave in pieces of 16 bytes (null: not asked)
+static gram_status check_gradient(gram_ctx* ctx, const char* name, const void* p, int64_t* ld, int64_t rows, int32_t d, int dtype) {
+  if (!p) return GRAM_OK;
+  ROWS_ARG(*ld >= d && *ld <= INT64_MAX / 8 / (rows > 0 ? rows : 1), "a gradient's rows must be at least d elements apart");
+  if (rows == 1) *ld = (*ld + 7) / 8 * 8;
+  if (reinterpret_cast<uintptr_t>(p) % 16 || *ld % (dtype == GRAM_F32 ? 4 : 8))
+    return gram_set_error(ctx, "%s: gradients must be 16-byte aligned, rows a multiple of 16 bytes apart", name), GRAM_ERR_UNSUPPORTED;
+  return GRAM_OK;
+}
 // a gradient may take the logits' own place, row on row, or lie beside them in rows of one buffer; another overlap would be
 // overwritten before it is read
 static gram_status check_overlap(gram_ctx* ctx, const char* name, const void* z, int64_t ld, const void* dz, int64_t ld_out, int dtype,
@@ -551,16 +573,45 @@ gram_status gram_score_logprobs(gram_ctx* ctx, const void* d_users, int64_t ld_u
   const RowAnswers ask{d_targets, d_logp, d_stats, d_entropy, d_top_logp, d_top_ids, C, k};
   GRAM_TRY(check_rows(ctx, name, N, V, scale));
   GRAM_TRY(check_answers(ctx, name, ask, N));
-  ROWS_ARG(d >= 1 && ld_users >= d && ld_items >= d, "rows must be at least d elements apart, d positive");
-  ROWS_ARG(ld_items <= INT64_MAX / 8 / V && ld_users <= INT64_MAX / 8 / (N > 0 ? N : 1), "rows too far apart");
-  ROWS_ARG(N == 0 || (d_users && d_items), "null vectors");
-  if (N == 1) ld_users = (ld_users + 7) / 8 * 8;        // of a single row the distance means nothing
-  if (V == 1) ld_items = (ld_items + 7) / 8 * 8;
-  if (ld_users % 8 || ld_items % 8 || reinterpret_cast<uintptr_t>(d_users) % 16 || reinterpret_cast<uintptr_t>(d_items) % 16)
-    return gram_set_error(ctx, "%s: vectors must be 16-byte aligned, rows a multiple of 8 elements apart", name), GRAM_ERR_UNSUPPORTED;
+  GRAM_TRY(check_vectors(ctx, name, d_users, &ld_users, d_items, &ld_items, N, V, d));
   if (N == 0) return GRAM_OK;
   return score_logprobs_launch(ctx, d_users, ld_users, d_items, ld_items, d_bias, N, V, d, scale, ask, ctx->gws.splitk,
                                ctx->gws.splitk_bytes, S(stream));
+}
+gram_status gram_score_loss_workspace(int64_t N, int32_t V, int32_t d, int grad_dtype, int64_t* h_least, int64_t* h_best) {
+  if (N < 0 || N > INT32_MAX || V < 1 || d < 1 || (grad_dtype != GRAM_F32 && grad_dtype != GRAM_BF16)) return GRAM_ERR_ARG;
+  size_t least, best;
+  score_loss_workspace(N, V, d, grad_dtype, &least, &best);
+  if (h_least) *h_least = (int64_t)least;
+  if (h_best) *h_best = (int64_t)best;
+  return GRAM_OK;
+}
+gram_status gram_score_loss(gram_ctx* ctx, const void* d_users, int64_t ld_users, const void* d_items, int64_t ld_items, const float* d_bias,
+                            int64_t N, int32_t V, int32_t d, float scale, const int32_t* d_targets, const float* d_weight, float* d_loss,
+                            int grad_dtype, void* d_dusers, int64_t ld_dusers, void* d_ditems, int64_t ld_ditems, float* d_dbias,
+                            void* d_workspace, int64_t workspace_bytes, gram_stream stream) {
+  if (!ctx) return GRAM_ERR_ARG;
+  const char* name = "gram_score_loss";
+  GRAM_TRY(check_rows(ctx, name, N, V, scale));
+  GRAM_TRY(check_vectors(ctx, name, d_users, &ld_users, d_items, &ld_items, N, V, d));
+  ROWS_ARG(N == 0 || (d_targets && d_loss), "null targets or loss");
+  if (d_dusers || d_ditems) {
+    ROWS_ARG(grad_dtype == GRAM_F32 || grad_dtype == GRAM_BF16, "unknown type of the gradients");
+    GRAM_TRY(check_gradient(ctx, name, d_dusers, &ld_dusers, N, d, grad_dtype));
+    GRAM_TRY(check_gradient(ctx, name, d_ditems, &ld_ditems, V, d, grad_dtype));
+    if (d % 8) return gram_set_error(ctx, "%s: gradients of vectors of %d elements (no multiple of 8)", name, d), GRAM_ERR_UNSUPPORTED;
+  }
+  ROWS_ARG(reinterpret_cast<uintptr_t>(d_workspace) % 256 == 0, "the workspace must be 256-byte aligned");
+  ROWS_ARG(workspace_bytes >= 0 && (N == 0 || d_workspace), "null workspace");
+  if (N == 0) {                                          // a sum over no rows
+    if (d_ditems) GRAM_CUDA(ctx, cudaMemset2DAsync(d_ditems, (size_t)ld_ditems * (grad_dtype == GRAM_F32 ? 4 : 2), 0,
+                                                   (size_t)d * (grad_dtype == GRAM_F32 ? 4 : 2), (size_t)V, S(stream)));
+    if (d_dbias) GRAM_CUDA(ctx, cudaMemsetAsync(d_dbias, 0, (size_t)V * 4, S(stream)));
+    return GRAM_OK;
+  }
+  const ScoreLoss a{d_users, d_items, ld_users, ld_items, d_bias, N, V, d, scale, d_targets, d_weight, d_loss, grad_dtype, d_dusers, d_ditems,
+                    ld_dusers, ld_ditems, d_dbias};
+  return score_loss_launch(ctx, a, d_workspace, (size_t)workspace_bytes, ctx->gws.splitk, ctx->gws.splitk_bytes, S(stream));
 }
 
 }  // extern "C"
