@@ -381,6 +381,24 @@ gram_status gram_score_loss(gram_ctx* ctx, const void* d_users, int64_t ld_users
  * is gained.  Either pointer may be NULL. */
 gram_status gram_score_loss_workspace(int64_t N, int32_t V, int32_t d, int grad_dtype, int64_t* h_least, int64_t* h_best);
 
+/* --- tables in 8 bits --------------------------------------------------------
+ * A table of encodings that is only read (a pool that is answered from, a projection's weights) takes half the memory of bf16 as codes of 8 bits with a
+ * scale for each row, and its products twice the rate.  Users' vectors take the same form on their way to it; gram_logprobs answers from
+ * the products. */
+enum { GRAM_I8_K_MAX = 131071 };         /* longest rows whose sums of products 32-bit whole numbers hold */
+/* Rows x [rows, cols] of `dtype` (GRAM_F32 or GRAM_BF16), `ld` elements between them, at any address and stride that the type allows:
+ *   d_scale[r] = max |x[r, :]| / 127 (fp32 [rows])      d_codes[r, c] = x[r, c] (127 / max |x[r, :]|), rounded to the nearest whole number, ties to even
+ * quotients and product rounded to fp32, codes int8 in [-127, 127], rows ld_codes apart (what lies between is left alone).  A row whose
+ * largest size is below 1e-30 has scale 0 and codes 0; one that holds NaN or an infinity scale NaN and codes 0. */
+gram_status gram_quantize_rows(gram_ctx* ctx, const void* d_x, int dtype, int64_t ld, int64_t rows, int32_t cols, int8_t* d_codes,
+                               int64_t ld_codes, float* d_scale, gram_stream stream);
+/* C[m, n] = d_scale_a[m] d_scale_b[n] sum_k A[m, k] B[n, k] + d_bias[n]: A int8 [M, K], B int8 [N, K], the sum a whole number of 32 bits (exact),
+ * the rest in fp32, C fp32 or bf16 (c_dtype) [M, N] with rows ldc apart at any address and stride that its type allows; d_bias fp32 [N] or
+ * NULL.  A and B 16-byte aligned, rows a multiple of 16 apart (GRAM_ERR_UNSUPPORTED else); K at most GRAM_I8_K_MAX, any M, N and K. */
+gram_status gram_gemm_i8(gram_ctx* ctx, const int8_t* d_A, int64_t lda, const float* d_scale_a, const int8_t* d_B, int64_t ldb,
+                         const float* d_scale_b, const float* d_bias, void* d_C, int c_dtype, int64_t ldc, int64_t M, int32_t N, int32_t K,
+                         gram_stream stream);
+
 /* --- checkpoint / resume (the paper keeps the checkpoint of the best validation epoch, Appendix D) ------------------
  * Everything a context holds besides what the caller gave it: parameters (gram_get_params / gram_set_params), the
  * optimiser's state, and for K > 1 the open window.  Exported by one context and imported into another context of the

@@ -23,6 +23,7 @@ GRAM_MODULE_CE, GRAM_MODULE_TASK = 0, 1
 GRAM_OPT_SGD, GRAM_OPT_ADAM = 0, 1
 GRAM_MULTI_TABLE, GRAM_MULTI_PSEUDO_TARGET = 0, 1
 GRAM_TOP_MAX = 128
+GRAM_I8_K_MAX = 131071
 STATUS = {0: "GRAM_OK", 1: "GRAM_ERR_ARG", 2: "GRAM_ERR_ID_RANGE", 3: "GRAM_ERR_WORKSPACE", 4: "GRAM_ERR_UNSUPPORTED",
           5: "GRAM_ERR_CUDA", 6: "GRAM_ERR_TIMEOUT"}
 
@@ -37,13 +38,14 @@ SYMBOLS = ["gram_create", "gram_destroy", "gram_sync", "gram_last_error", "gram_
            "gram_optimizer_reset", "gram_noam_rate", "gram_adam_update", "gram_state_export", "gram_state_import",
            "gram_optimizer_export", "gram_optimizer_import", "gram_selftest_bounded_wait", "gram_selftest_ring_rows", "gram_selftest_cluster_blocks", "gram_selftest_column_sums", "gram_grads_device",
            "gram_gemm_bf16_epilogue", "gram_logprobs", "gram_logprobs_backward", "gram_distill", "gram_score_logprobs",
-           "gram_score_loss", "gram_score_loss_workspace"]
+           "gram_score_loss", "gram_score_loss_workspace", "gram_quantize_rows", "gram_gemm_i8"]
 
 # argument types of the calls on rows of logits, which a serving loop makes for single rows: declared once, so that a call passes
 # plain numbers and addresses (p: address, i: int32, l: int64, f: float)
 _TYPES = {"p": C.c_void_p, "i": C.c_int32, "l": C.c_int64, "f": C.c_float}
 _ROW_CALLS = {"gram_logprobs": "ppillifpipppppip", "gram_logprobs_backward": "ppillifpippppplp", "gram_distill": "ppillifppippplp",
-              "gram_score_logprobs": "pplplpliifpipppppip", "gram_score_loss": "pplplpliifpppiplplpplp"}
+              "gram_score_logprobs": "pplplpliifpipppppip", "gram_score_loss": "pplplpliifpppiplplpplp",
+              "gram_quantize_rows": "ppilliplpp", "gram_gemm_i8": "pplpplpppilliip"}
 
 KINDS = ["gemm", "attention", "layernorm", "colsum", "embed_pool", "dedup", "gather", "accumulate", "task_head", "other",
          "optimizer"]
@@ -146,7 +148,7 @@ _current_stream = None
 def _row_setup():
     import torch
     global _current_stream
-    _ROW_TYPES.update({torch.float32: GRAM_F32, torch.bfloat16: GRAM_BF16, "f": torch.float32, "i": torch.int32, "b": torch.uint8})
+    _ROW_TYPES.update({torch.float32: GRAM_F32, torch.bfloat16: GRAM_BF16, "f": torch.float32, "i": torch.int32, "b": torch.uint8, "c": torch.int8})
     raw, device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
     _current_stream = lambda: raw(device())  # noqa: E731
 
@@ -198,6 +200,18 @@ def _vector_gradient(vectors, grad, what: str):
     if grad.shape != vectors.shape:
         raise GramError(1, f"{what}: shape {tuple(vectors.shape)} is needed, not {tuple(grad.shape)}")
     return q, ld, dtype
+
+
+def _codes(t, what: str):
+    """(address, elements between rows) of an int8 matrix whose rows are contiguous but may lie further apart."""
+    try:
+        N, K = t.shape
+    except ValueError:
+        _no_matrix(t, what)
+    ld, step = t.stride()
+    if t.dtype is not _ROW_TYPES["c"] or (step != 1 and K > 1) or not (t.is_cuda or t.is_pinned()):
+        raise GramError(1, f"{what}: int8 rows of contiguous elements in device or pinned host memory are needed, not {t.dtype} with strides {t.stride()} on {t.device}")
+    return t.data_ptr(), ld if N > 1 else max(ld, K)
 
 
 def _width(t, what: str) -> int:
@@ -421,6 +435,26 @@ class Gram:
         if st != 0:
             raise GramError(st, f"score_loss_workspace: N = {N}, V = {V}, d = {d}, {grad_dtype}")
         return least.value, best.value
+
+    # tables in 8 bits
+    def quantize_rows(self, x, codes, scale, stream=None):
+        p, dtype, ld = _rows(x, "x")
+        q, ld_codes = _codes(codes, "codes")
+        if codes.shape != x.shape:
+            raise GramError(1, f"codes: shape {tuple(x.shape)} is needed, not {tuple(codes.shape)}")
+        rows, cols = x.shape
+        self._ck(lib().gram_quantize_rows(self._h, p, dtype, ld, rows, cols, q, ld_codes, _array(scale, "f", rows, "scale"), _raw_stream(stream)))
+
+    def gemm_i8(self, A, scale_a, B, scale_b, C, bias=None, stream=None):
+        """C [M, N] (float32 or bfloat16) from A int8 [M, K] and B int8 [N, K]."""
+        r, c_dtype, ldc = _rows(C, "C")
+        p, lda = _codes(A, "A")
+        q, ldb = _codes(B, "B")
+        (M, K), N = A.shape, B.shape[0]
+        if B.shape[1] != K or tuple(C.shape) != (M, N):
+            raise GramError(1, f"A, B and C: [M, K], [N, K] and [M, N] are needed, not {tuple(A.shape)}, {tuple(B.shape)} and {tuple(C.shape)}")
+        self._ck(lib().gram_gemm_i8(self._h, p, lda, _array(scale_a, "f", M, "scale_a"), q, ldb, _array(scale_b, "f", N, "scale_b"),
+                                    _array(bias, "f", N, "bias"), r, c_dtype, ldc, M, N, K, _raw_stream(stream)))
 
     def encoder_backward(self, G, items, U, stream=None):
         self._ck(lib().gram_encoder_backward(self._h, _ptr(G), _ptr(items), C.c_int32(U), _stream(stream)))

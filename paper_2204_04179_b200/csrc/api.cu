@@ -9,6 +9,7 @@
 #include "layers.h"
 #include "logits.h"
 #include "score_loss.h"
+#include "gemm_i8.h"
 
 constexpr int kProfSlots = 16384;
 struct ProfRec {
@@ -612,6 +613,37 @@ gram_status gram_score_loss(gram_ctx* ctx, const void* d_users, int64_t ld_users
   const ScoreLoss a{d_users, d_items, ld_users, ld_items, d_bias, N, V, d, scale, d_targets, d_weight, d_loss, grad_dtype, d_dusers, d_ditems,
                     ld_dusers, ld_ditems, d_dbias};
   return score_loss_launch(ctx, a, d_workspace, (size_t)workspace_bytes, ctx->gws.splitk, ctx->gws.splitk_bytes, S(stream));
+}
+gram_status gram_quantize_rows(gram_ctx* ctx, const void* d_x, int dtype, int64_t ld, int64_t rows, int32_t cols, int8_t* d_codes,
+                               int64_t ld_codes, float* d_scale, gram_stream stream) {
+  if (!ctx) return GRAM_ERR_ARG;
+  const char* name = "gram_quantize_rows";
+  ROWS_ARG(rows >= 0 && rows <= INT32_MAX, "rows must be in [0, 2^31)");
+  ROWS_ARG(cols >= 1, "cols must be positive");
+  GRAM_TRY(check_logits(ctx, name, d_x, dtype, ld, rows, cols));
+  ROWS_ARG(ld_codes >= cols && ld_codes <= INT64_MAX / 8 / (rows > 0 ? rows : 1), "rows of codes must be at least cols apart");
+  ROWS_ARG(rows == 0 || (d_codes && d_scale), "null codes or scales");
+  if (rows == 0) return GRAM_OK;
+  return quantize_rows_launch(ctx, d_x, dtype, ld, rows, cols, d_codes, ld_codes, d_scale, S(stream));
+}
+gram_status gram_gemm_i8(gram_ctx* ctx, const int8_t* d_A, int64_t lda, const float* d_scale_a, const int8_t* d_B, int64_t ldb,
+                         const float* d_scale_b, const float* d_bias, void* d_C, int c_dtype, int64_t ldc, int64_t M, int32_t N, int32_t K,
+                         gram_stream stream) {
+  if (!ctx) return GRAM_ERR_ARG;
+  const char* name = "gram_gemm_i8";
+  ROWS_ARG(M >= 0 && M <= INT32_MAX && N >= 1, "M must be in [0, 2^31), N positive");
+  ROWS_ARG(K >= 1 && K <= GRAM_I8_K_MAX, "K must be in [1, 131071]");
+  ROWS_ARG(c_dtype == GRAM_F32 || c_dtype == GRAM_BF16, "unknown type of the result");
+  ROWS_ARG(lda >= K && ldb >= K && lda <= INT64_MAX / 8 / (M > 0 ? M : 1) && ldb <= INT64_MAX / 8 / N, "operands' rows must be at least K apart");
+  ROWS_ARG(ldc >= N && ldc <= INT64_MAX / 8 / (M > 0 ? M : 1), "the result's rows must be at least N apart");
+  ROWS_ARG(M == 0 || (d_A && d_B && d_scale_a && d_scale_b && d_C), "null buffer");
+  ROWS_ARG(reinterpret_cast<uintptr_t>(d_C) % (c_dtype == GRAM_F32 ? 4 : 2) == 0, "an address that the result's type does not allow");
+  if (M == 1) lda = (lda + 15) / 16 * 16;               // of a single row the distance means nothing
+  if (N == 1) ldb = (ldb + 15) / 16 * 16;
+  if (lda % 16 || ldb % 16 || reinterpret_cast<uintptr_t>(d_A) % 16 || reinterpret_cast<uintptr_t>(d_B) % 16)
+    return gram_set_error(ctx, "%s: operands must be 16-byte aligned, rows a multiple of 16 apart", name), GRAM_ERR_UNSUPPORTED;
+  if (M == 0) return GRAM_OK;
+  return gemm_i8_launch(ctx, d_A, lda, d_scale_a, d_B, ldb, d_scale_b, d_bias, d_C, c_dtype, ldc, M, N, K, S(stream));
 }
 
 }  // extern "C"

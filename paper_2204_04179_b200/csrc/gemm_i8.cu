@@ -1,0 +1,310 @@
+// Tables in 8 bits: rows of codes with a scale each (gram_quantize_rows) and their products (gram_gemm_i8).
+#include "gemm_i8.h"
+
+#include "pair_pipe.cuh"
+
+namespace {
+using namespace tc;
+
+constexpr int kPairs = kNumSMs / 2;
+
+// ============================================================================================
+// codes = x (127 / max |x|) to the nearest whole number, scale = max |x| / 127
+// ============================================================================================
+// A warp a row.  Rows of up to QR_HELD elements a lane are read once, longer ones twice (the second time out of L1 or L2).
+// Bounded by HBM.
+constexpr int QR_HELD = 32, QR_ROWS = 8;
+
+template <typename T> struct QuantVec;                  // 16 bytes of a row, and their codes
+template <> struct QuantVec<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void load(const float* p, float* x) {
+    const float4 v = __ldg(reinterpret_cast<const float4*>(p));
+    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+  }
+};
+template <> struct QuantVec<bf16> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void load(const bf16* p, float* x) {
+    const uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
+    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = unpack_bf16x2(u[i]);
+      x[2 * i] = f.x;
+      x[2 * i + 1] = f.y;
+    }
+  }
+};
+__device__ __forceinline__ float quant_value(const float* p) { return __ldg(p); }
+__device__ __forceinline__ float quant_value(const bf16* p) { return __bfloat162float(*p); }
+
+// A maximum that NaN stays in: of bits without the sign, which order like whole numbers (NaN above infinity).
+__device__ __forceinline__ uint32_t quant_size(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+__device__ __forceinline__ uint32_t quant_code(float x, float inv) { return (uint32_t)__float2int_rn(fminf(fmaxf(x * inv, -127.f), 127.f)) & 0xffu; }
+struct QuantScale {
+  float inv, scale;
+};
+// Rows below 1e-30 count as zeros (127 / max would leave 32 bits); in a row with infinity or NaN the scale is NaN and says so.
+__device__ __forceinline__ QuantScale quant_scale(uint32_t top) {
+  const float m = __uint_as_float(top);
+  if (top >= 0x7f800000u) return QuantScale{0.f, __int_as_float(0x7fffffff)};
+  if (m < 1e-30f) return QuantScale{0.f, 0.f};
+  return QuantScale{__fdiv_rn(127.f, m), __fdiv_rn(m, 127.f)};
+}
+
+// VEC: rows and codes allow 16-byte loads and stores of as many codes
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(32 * QR_ROWS) quantize_rows_kernel(const T* x, int64_t ld, int64_t rows, int32_t cols, int8_t* codes, int64_t ld_codes,
+                                                                     float* scale) {
+  if (!chain_begin()) return;
+  constexpr int W = VEC ? QuantVec<T>::N : 1, HELD = QR_HELD / W;          // elements of a piece; pieces that a lane holds
+  const int lane = threadIdx.x & 31;
+  const int64_t r = (int64_t)blockIdx.x * QR_ROWS + (threadIdx.x >> 5);
+  if (r >= rows) return;
+  const T* row = x + r * ld;
+  int8_t* out = codes + r * ld_codes;
+  const int pieces = cols / W;                          // VEC: the rest is taken one by one
+  float v[HELD][W];
+  uint32_t top = 0u;
+  auto load = [&](int i, float* to) {
+    if constexpr (VEC) QuantVec<T>::load(row + i * W, to);
+    else to[0] = quant_value(row + i);
+  };
+#pragma unroll
+  for (int h = 0; h < HELD; ++h)
+    if (h * 32 + lane < pieces) load(h * 32 + lane, v[h]);
+#pragma unroll
+  for (int h = 0; h < HELD; ++h)
+    if (h * 32 + lane < pieces) {
+#pragma unroll
+      for (int j = 0; j < W; ++j) top = max(top, quant_size(v[h][j]));
+    }
+  for (int i = HELD * 32 + lane; i < pieces; i += 32) {
+    float y[W];
+    load(i, y);
+#pragma unroll
+    for (int j = 0; j < W; ++j) top = max(top, quant_size(y[j]));
+  }
+  for (int i = pieces * W + lane; i < cols; i += 32) top = max(top, quant_size(quant_value(row + i)));
+  const QuantScale s = quant_scale(__reduce_max_sync(0xffffffffu, top));
+  // a row of infinities or NaN has codes 0 (0 times them would be NaN)
+  const bool none = s.inv == 0.f;
+  auto store = [&](int i, const float* y) {
+    if constexpr (VEC) {
+      uint32_t c[W / 4];
+#pragma unroll
+      for (int j = 0; j < W / 4; ++j)
+        c[j] = none ? 0u : quant_code(y[4 * j], s.inv) | quant_code(y[4 * j + 1], s.inv) << 8 | quant_code(y[4 * j + 2], s.inv) << 16 |
+                           quant_code(y[4 * j + 3], s.inv) << 24;
+      if constexpr (W == 4) *reinterpret_cast<uint32_t*>(out + i * 4) = c[0];
+      else *reinterpret_cast<uint2*>(out + i * 8) = make_uint2(c[0], c[1]);
+    } else {
+      out[i] = none ? (int8_t)0 : (int8_t)quant_code(y[0], s.inv);
+    }
+  };
+#pragma unroll
+  for (int h = 0; h < HELD; ++h)
+    if (h * 32 + lane < pieces) store(h * 32 + lane, v[h]);
+  for (int i = HELD * 32 + lane; i < pieces; i += 32) {
+    float y[W];
+    load(i, y);
+    store(i, y);
+  }
+  for (int i = pieces * W + lane; i < cols; i += 32) out[i] = none ? (int8_t)0 : (int8_t)quant_code(quant_value(row + i), s.inv);
+  if (lane == 0) scale[r] = s.scale;
+}
+
+template <typename T>
+void launch_quantize(const void* x, int64_t ld, int64_t rows, int32_t cols, int8_t* codes, int64_t ld_codes, float* scale, cudaStream_t st) {
+  constexpr int W = QuantVec<T>::N;
+  const bool vec = (uintptr_t)x % 16 == 0 && (ld % W == 0 || rows == 1) && (uintptr_t)codes % W == 0 && (ld_codes % W == 0 || rows == 1);
+  auto kern = vec ? quantize_rows_kernel<T, true> : quantize_rows_kernel<T, false>;
+  launch_chain(kern, dim3((unsigned)ceil_div64(rows, QR_ROWS)), 32 * QR_ROWS, 0, st, (const T*)x, ld, rows, cols, codes, ld_codes, scale);
+}
+
+// ============================================================================================
+// the product
+// ============================================================================================
+// A pair of SMs owns a tile of 256 channels (rows of B, columns of C) x `width` tokens (rows of A): the channels are the MMA's rows, so
+// that the lanes of tensor memory, and with them a warp's stores, run along C's rows whatever C's address and stride, and a few tokens
+// are a narrow tile.  Sums are whole numbers of 32 bits, exact up to K = 131 071.
+constexpr int I8_STAGES = 6, I8_EPI_WARPS = 16, I8_BK = 128;
+constexpr int I8_SCALE_BYTES = I8_EPI_WARPS * 64 * 4;   // a warp's tokens
+using I8Pipe = PairPipe<I8_STAGES, I8_EPI_WARPS, I8_SCALE_BYTES>;
+
+struct I8Args {
+  const float *scale_a, *scale_b, *bias;
+  void* C;
+  int64_t ldc, M;
+  int32_t N, num_kb, tiles_n, total, width;             // tiles of 256 channels; tokens of a tile
+  int32_t give_up;
+  int32_t* status;
+};
+
+__device__ __forceinline__ void i8_mma_pair(uint32_t tmem_d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accum) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d),
+      "l"(da), "l"(db), "r"(idesc), "r"(accum)
+      : "memory");
+}
+
+template <typename CT>
+__global__ void __launch_bounds__(I8Pipe::THREADS, 1) gemm_i8_kernel(const __grid_constant__ CUtensorMap channels, const __grid_constant__ CUtensorMap tokens,
+                                                                     const __grid_constant__ I8Args a) {
+  extern __shared__ uint8_t smem_raw[];
+  I8Pipe pipe;
+  const bool go = pipe.open(smem_raw);
+  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  bool failed = false;
+  if (pipe.warp == 0 && go) {
+    // ------------------------------ copies (both blocks) ------------------------------
+    int s = 0, tile = 0;
+    uint32_t ph = 0;
+    const uint32_t bytes = PAIR_OPERAND + (uint32_t)a.width * (I8_BK / 2);
+    for (int t = pair; t < a.total && !failed; t += pairs, ++tile) {
+      if (tile == a.give_up) { failed = true; break; }
+      const int n0 = (t % a.tiles_n) * 2 * PAIR_ROWS + (int)pipe.rank * PAIR_ROWS;
+      const int m0 = (t / a.tiles_n) * a.width + (int)pipe.rank * (a.width / 2);
+      for (int kb = 0; kb < a.num_kb; ++kb) {
+        if (!mbar_wait_warp(pipe.empty(s), ph ^ 1u, pipe.abort_flag)) { failed = true; break; }
+        const uint32_t bar = pipe.lead_full(s);
+        if (elect_one()) {
+          mbar_arrive_expect_tx_remote(bar, bytes);
+          tma_load_2d_pair(pipe.a_of(s), &channels, kb * I8_BK, n0, bar);
+          tma_load_2d_pair(pipe.b_of(s), &tokens, kb * I8_BK, m0, bar);
+        }
+        __syncwarp();
+        if (++s == I8_STAGES) { s = 0; ph ^= 1u; }
+      }
+    }
+  } else if (pipe.warp == 1 && go) {
+    // ------------------------------ products (leader): signed 8-bit operands, sums in 32-bit whole numbers ------------------------------
+    if (pipe.rank == 0) {
+      const uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(a.width >> 3) << 17) | ((uint32_t)(2 * PAIR_ROWS >> 4) << 24);
+      const uint64_t da0 = make_desc(pipe.a_of(0), 16, 1024), db0 = make_desc(pipe.b_of(0), 16, 1024);
+      int s = 0;
+      uint32_t ph = 0, it = 0;
+      for (int t = pair; t < a.total && !failed; t += pairs, ++it) {
+        const int buf = (int)(it & 1);
+        if (!mbar_wait_warp(pipe.tempty(buf), ((it >> 1) & 1) ^ 1u, pipe.abort_flag)) { failed = true; break; }
+        tc_fence_after();
+        const uint32_t tmem_d = pipe.tmem + (uint32_t)(buf * PAIR_COLS);
+        for (int kb = 0; kb < a.num_kb; ++kb) {
+          if (!mbar_wait_warp(pipe.full(s), ph, pipe.abort_flag)) { failed = true; break; }
+          tc_fence_after();
+          const uint32_t soff = (uint32_t)(s * (PAIR_STAGE >> 4));
+          if (elect_one()) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)                 // 32 bytes of the rows each
+              i8_mma_pair(tmem_d, da0 + soff + (uint64_t)(k * 2), db0 + soff + (uint64_t)(k * 2), idesc, (kb > 0 || k > 0) ? 1u : 0u);
+            tc_commit_pair(pipe.empty(s));
+            if (kb == a.num_kb - 1) tc_commit_pair(pipe.tfull(buf));
+          }
+          __syncwarp();
+          if (++s == I8_STAGES) { s = 0; ph ^= 1u; }
+        }
+      }
+    }
+  } else if (go) {
+    // ------------------------------ results (both blocks): a channel a thread ------------------------------
+    const int lane = pipe.lane, q = pipe.warp & 3, part = (pipe.warp - 2) >> 2;
+    float* scale_w = reinterpret_cast<float*>(pipe.extra) + (pipe.warp - 2) * 64;
+    const int blocks = (a.width + 127) / 128;           // of 32 tokens of this warp, one where the tile is narrow
+    const int tok0 = part * blocks * 32;
+    uint32_t it = 0;
+    for (int t = pair; t < a.total && !failed; t += pairs, ++it) {
+      const int buf = (int)(it & 1);
+      const int64_t n = (int64_t)(t % a.tiles_n) * 2 * PAIR_ROWS + (int)pipe.rank * PAIR_ROWS + q * 32 + lane;
+      const int64_t m0 = (int64_t)(t / a.tiles_n) * a.width + tok0;
+      const bool active = n - lane < a.N && tok0 < a.width && m0 < a.M;         // of the warp
+      float sb = 0.f, bias = 0.f;
+      if (active) {
+        if (n < a.N) {
+          sb = __ldg(a.scale_b + n);
+          if (a.bias) bias = __ldg(a.bias + n);
+        }
+        __syncwarp();
+        for (int b = 0; b < blocks; ++b) scale_w[b * 32 + lane] = m0 + b * 32 + lane < a.M ? __ldg(a.scale_a + m0 + b * 32 + lane) : 0.f;
+        __syncwarp();
+      }
+      if (!mbar_wait_warp(pipe.tfull(buf), (it >> 1) & 1, pipe.abort_flag)) { failed = true; break; }
+      tc_fence_after();
+      if (active) {
+        const uint32_t taddr = pipe.tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * PAIR_COLS + tok0);
+        for (int b = 0; b < blocks; ++b) {
+          uint32_t v[32];
+          tc_ld32_issue(taddr + b * 32, v);
+          tc_ld32_wait(v);
+          CT* to = reinterpret_cast<CT*>(a.C) + (m0 + b * 32) * a.ldc + n;
+          const int left = n < a.N ? (int)min((int64_t)32, a.M - m0 - b * 32) : 0;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            const float x = fmaf((float)(int32_t)v[j] * scale_w[b * 32 + j], sb, bias);
+            if (j < left) {
+              if constexpr (sizeof(CT) == 4) to[j * a.ldc] = x;
+              else to[j * a.ldc] = __float2bfloat16_rn(x);
+            }
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_remote(pipe.lead_tempty(buf));
+    }
+  }
+  pipe.close(failed, a.status);
+}
+
+// 2-D map of 8-bit elements: `inner` contiguous ones per row, rows `ld` apart; boxes of 128 of them x `rows`
+bool make_map_i8(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer, uint64_t ld, uint32_t rows) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {inner, outer};
+  cuuint64_t strides[1] = {ld};
+  cuuint32_t box[2] = {I8_BK, rows};
+  cuuint32_t es[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace
+
+gram_status quantize_rows_launch(gram_ctx* ctx, const void* x, int dtype, int64_t ld, int64_t rows, int32_t cols, int8_t* codes, int64_t ld_codes,
+                                 float* scale, cudaStream_t st) {
+  ProfScope prof(ctx, GRAM_K_OTHER, (double)rows * cols * (dtype == GRAM_F32 ? 5 : 3), 1, st, "quantize_rows");
+  if (dtype == GRAM_F32) launch_quantize<float>(x, ld, rows, cols, codes, ld_codes, scale, st);
+  else launch_quantize<bf16>(x, ld, rows, cols, codes, ld_codes, scale, st);
+  GRAM_LAUNCH_CHECK(ctx);
+  return GRAM_OK;
+}
+
+gram_status gemm_i8_launch(gram_ctx* ctx, const int8_t* A, int64_t lda, const float* scale_a, const int8_t* B, int64_t ldb, const float* scale_b,
+                           const float* bias, void* C, int c_dtype, int64_t ldc, int64_t M, int32_t N, int32_t K, cudaStream_t st) {
+  I8Args a = {};
+  a.scale_a = scale_a;
+  a.scale_b = scale_b;
+  a.bias = bias;
+  a.C = C;
+  a.ldc = ldc;
+  a.M = M;
+  a.N = N;
+  a.num_kb = ceil_div(K, I8_BK);
+  a.tiles_n = ceil_div(N, 2 * PAIR_ROWS);
+  a.width = M > 128 ? 256 : M > 64 ? 128 : M > 32 ? 64 : 32;
+  const int64_t total = a.tiles_n * ceil_div64(M, a.width);
+  if (total > INT32_MAX - kPairs) return gram_set_error(ctx, "gram_gemm_i8: %lld x %d are too many results", (long long)M, N), GRAM_ERR_UNSUPPORTED;
+  a.total = (int32_t)total;
+  a.give_up = gram_ring_rows(ctx);
+  a.status = gram_status_word(ctx);
+  CUtensorMap channels, tokens;
+  if (!make_map_i8(&channels, B, (uint64_t)K, (uint64_t)N, (uint64_t)ldb, PAIR_ROWS) ||
+      !make_map_i8(&tokens, A, (uint64_t)K, (uint64_t)M, (uint64_t)lda, (uint32_t)a.width / 2))
+    return gram_set_error(ctx, "gram_gemm_i8: cannot describe the operands"), GRAM_ERR_UNSUPPORTED;
+  ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * M * N * K, 1, st, "gemm_i8");
+  const int pairs = a.total < kPairs ? a.total : kPairs;
+  if (c_dtype == GRAM_F32) GRAM_CUDA(ctx, launch_pairs(gemm_i8_kernel<float>, pairs, I8Pipe::THREADS, I8Pipe::SMEM, st, channels, tokens, a));
+  else GRAM_CUDA(ctx, launch_pairs(gemm_i8_kernel<bf16>, pairs, I8Pipe::THREADS, I8Pipe::SMEM, st, channels, tokens, a));
+  return GRAM_OK;
+}
