@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(I8Pipe::THREADS, 1) gemm_i8_kernel(const __gri
         for (int kb = 0; kb < a.num_kb; ++kb) {
           if (!mbar_wait_warp(pipe.full(s), ph, pipe.abort_flag)) { failed = true; break; }
           tc_fence_after();
-          const uint32_t soff = (uint32_t)(s * (PAIR_STAGE >> 4));
+          const uint32_t soff = (uint32_t)(s * (I8Pipe::STAGE >> 4));
           if (elect_one()) {
 #pragma unroll
             for (int k = 0; k < 4; ++k)                 // 32 bytes of the rows each

@@ -10,12 +10,12 @@ namespace tc {
 constexpr int PAIR_ROWS = 128;                          // rows of a block; a pair has twice as many
 constexpr int PAIR_COLS = 256;                          // columns of the widest tile, and of an accumulator
 constexpr int PAIR_OPERAND = PAIR_ROWS * 128;           // bytes of 128 rows of 128, the swizzle's width
-constexpr int PAIR_STAGE = 2 * PAIR_OPERAND;
 constexpr int PAIR_BOX = 64 * 128;                      // bytes of a copy's box: 64 rows of 128
 
-template <int STAGES_, int EPI_WARPS_, int EXTRA = 0> struct PairPipe {
-  static constexpr int STAGES = STAGES_, EPI_WARPS = EPI_WARPS_, THREADS = 64 + 32 * EPI_WARPS_;
-  static constexpr int SMEM = STAGES * PAIR_STAGE + EXTRA + 1024 + 256;       // EXTRA: the kernel's own, behind the stages
+// A stage holds `A` operands of the MMA's rows and one of its columns.  EXTRA: bytes of the kernel's own, behind the stages.
+template <int STAGES_, int EPI_WARPS_, int EXTRA = 0, int A = 1> struct PairPipe {
+  static constexpr int STAGES = STAGES_, EPI_WARPS = EPI_WARPS_, THREADS = 64 + 32 * EPI_WARPS_, STAGE = (A + 1) * PAIR_OPERAND;
+  static constexpr int SMEM = STAGES * STAGE + EXTRA + 1024 + 256;
   static_assert(SMEM <= 232448 && EXTRA % 16 == 0 && 8 * (2 * STAGES + 4) + 8 <= 256, "shared memory of a block");
   uint32_t tiles, bar0, tmem, rank, lead_bar0;
   uint8_t* extra;
@@ -29,15 +29,15 @@ template <int STAGES_, int EPI_WARPS_, int EXTRA = 0> struct PairPipe {
   // the leader's, as seen from either block
   __device__ __forceinline__ uint32_t lead_full(int s) const { return lead_bar0 + 8u * s; }
   __device__ __forceinline__ uint32_t lead_tempty(int b) const { return lead_bar0 + 8u * (2 * STAGES + 2 + b); }
-  __device__ __forceinline__ uint32_t a_of(int s) const { return tiles + s * PAIR_STAGE; }
-  __device__ __forceinline__ uint32_t b_of(int s) const { return tiles + s * PAIR_STAGE + PAIR_OPERAND; }
+  __device__ __forceinline__ uint32_t a_of(int s, int i = 0) const { return tiles + s * STAGE + i * PAIR_OPERAND; }
+  __device__ __forceinline__ uint32_t b_of(int s) const { return tiles + s * STAGE + A * PAIR_OPERAND; }
 
   // All threads; memory of the kernels before may be touched after it.
   __device__ __forceinline__ bool open(uint8_t* smem_raw) {
     const uint32_t raw = smem_u32(smem_raw);
     tiles = (raw + 1023u) & ~1023u;                     // the same offset in both blocks of the pair
-    extra = smem_raw + (tiles - raw) + STAGES * PAIR_STAGE;
-    bar0 = tiles + STAGES * PAIR_STAGE + EXTRA;
+    extra = smem_raw + (tiles - raw) + STAGES * STAGE;
+    bar0 = tiles + STAGES * STAGE + EXTRA;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(extra + EXTRA + 8 * (2 * STAGES + 4));
     abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     warp = threadIdx.x >> 5;

@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(GradPipe::THREADS, 1) loss_grad_kernel(const _
         for (int kb = 0; kb < a.num_kb; ++kb) {
           if (!mbar_wait_warp(pipe.full(s), ph, pipe.abort_flag)) { failed = true; break; }
           tc_fence_after();
-          const uint32_t soff = (uint32_t)(s * (PAIR_STAGE >> 4));
+          const uint32_t soff = (uint32_t)(s * (GradPipe::STAGE >> 4));
           if (elect_one()) {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
@@ -259,8 +259,12 @@ __global__ void __launch_bounds__(256) loss_bias_kernel(const float* part, int64
 // ============================================================================================
 // both products of a piece's g
 // ============================================================================================
-constexpr int LP_STAGES = 6, LP_EPI_WARPS = 8;
-using ProdPipe = PairPipe<LP_STAGES, LP_EPI_WARPS>;
+// PLANES: bf16 that g is the sum of; a stage holds all of them beside one piece of the vectors.  CHAINED: the sum of a unit comes as several
+// accumulators, which eight warps add up in registers; else sixteen warps take one.
+template <int PLANES, bool CHAINED> using ProdPipe = PairPipe<PLANES == 2 ? 4 : 6, CHAINED ? 8 : 16, 0, PLANES>;
+
+// Blocks of 64 whose products (of both planes) are added up in one accumulator for fp32 gradients.  bf16 results hide the error of any length.
+constexpr int LP_CHAIN = 24;
 
 struct ProdArgs {
   int64_t N;
@@ -284,9 +288,8 @@ struct ProdArgs {
 // A unit: a tile of dI over all users, or a tile of dU over a part of the piece's items.
 struct ProdUnit {
   bool users;
-  int m0, n0, width, split, k0, blocks;      // first row and column; k0: the first block of the sum's range; blocks: of all planes
-  int per_plane;
-  __device__ __forceinline__ ProdUnit(const ProdArgs& a, int t, int planes) {
+  int m0, n0, width, split, k0, blocks;      // first row and column; the sum's range in blocks of 64
+  __device__ __forceinline__ ProdUnit(const ProdArgs& a, int t) {
     users = a.users_first ? t < a.units_u : t >= a.total - a.units_u;
     if (a.users_first ? !users : users) t -= a.users_first ? a.units_u : a.total - a.units_u;
     const int tn = t % a.tiles_n, r = t / a.tiles_n;
@@ -296,14 +299,13 @@ struct ProdUnit {
       split = r / a.users_m;
       m0 = (r - split * a.users_m) * 2 * PAIR_ROWS;
       k0 = split * a.kb_split;
-      per_plane = min(a.kb_split, a.kb_items - k0);
+      blocks = min(a.kb_split, a.kb_items - k0);
     } else {
       split = 0;
       m0 = r * 2 * PAIR_ROWS;
       k0 = 0;
-      per_plane = a.kb_users;
+      blocks = a.kb_users;
     }
-    blocks = per_plane * planes;
   }
 };
 
@@ -345,47 +347,45 @@ __device__ __forceinline__ void put_row(bf16* p, const float (&x)[32], int some,
   }
 }
 
-template <typename GT>
-__global__ void __launch_bounds__(ProdPipe::THREADS, 1) loss_products_kernel(const __grid_constant__ CUtensorMap g0, const __grid_constant__ CUtensorMap g1,
-                                                                             const __grid_constant__ CUtensorMap users,
-                                                                             const __grid_constant__ CUtensorMap items,
-                                                                             const __grid_constant__ ProdArgs a) {
-  constexpr int PLANES = sizeof(GT) == 4 ? 2 : 1;
+template <typename GT, bool CHAINED>
+__global__ void __launch_bounds__(ProdPipe<sizeof(GT) / 2, CHAINED>::THREADS, 1)
+    loss_products_kernel(const __grid_constant__ CUtensorMap g0, const __grid_constant__ CUtensorMap g1, const __grid_constant__ CUtensorMap users,
+                         const __grid_constant__ CUtensorMap items, const __grid_constant__ ProdArgs a) {
+  constexpr int PLANES = sizeof(GT) / 2;
+  using Pipe = ProdPipe<PLANES, CHAINED>;
   extern __shared__ uint8_t smem_raw[];
-  ProdPipe pipe;
+  Pipe pipe;
   const bool go = pipe.open(smem_raw);
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   bool failed = false;
   if (pipe.warp == 0 && go) {
-    // ------------------------------ copies (both blocks): two boxes of 64 x 64 of g, one or two of the vectors ------------------------------
+    // ------------------------------ copies (both blocks): two boxes of 64 x 64 of each plane of g, one or two of the vectors ------------------------------
     int s = 0, tile = 0;
     uint32_t ph = 0;
     for (int t = pair; t < a.total && !failed; t += pairs, ++tile) {
       if (tile == a.give_up) { failed = true; break; }
-      const ProdUnit u(a, t, PLANES);
+      const ProdUnit u(a, t);
       const int m0 = u.m0 + (int)pipe.rank * PAIR_ROWS, n0 = u.n0 + (int)pipe.rank * (u.width / 2);
-      const uint32_t bytes = 2 * PAIR_BOX + (uint32_t)(u.width / PAIR_ROWS) * PAIR_BOX;
+      const uint32_t bytes = PLANES * 2 * PAIR_BOX + (uint32_t)(u.width / PAIR_ROWS) * PAIR_BOX;
       const CUtensorMap* vectors = u.users ? &items : &users;
       for (int kb = 0; kb < u.blocks; ++kb) {
-        const int plane = PLANES == 2 && kb >= u.per_plane, k = (u.k0 + kb - (plane ? u.per_plane : 0)) * 64;
-        const CUtensorMap* g = plane ? &g1 : &g0;
+        const int k = (u.k0 + kb) * 64, row = (u.users ? a.first : 0) + k;
         if (!mbar_wait_warp(pipe.empty(s), ph ^ 1u, pipe.abort_flag)) { failed = true; break; }
-        const uint32_t bar = pipe.lead_full(s), sa = pipe.a_of(s), sb = pipe.b_of(s);
-        const int row = (u.users ? a.first : 0) + k;
+        const uint32_t bar = pipe.lead_full(s), sb = pipe.b_of(s);
         if (elect_one()) {
           mbar_arrive_expect_tx_remote(bar, bytes);
-          if (u.users) {
-            tma_load_2d_pair(sa, g, k, m0, bar);
-            tma_load_2d_pair(sa + PAIR_BOX, g, k, m0 + 64, bar);
-          } else {
-            tma_load_2d_pair(sa, g, m0, k, bar);
-            tma_load_2d_pair(sa + PAIR_BOX, g, m0 + 64, k, bar);
+#pragma unroll
+          for (int i = 0; i < PLANES; ++i) {
+            const CUtensorMap* g = i ? &g1 : &g0;
+            const uint32_t sa = pipe.a_of(s, i);
+            tma_load_2d_pair(sa, g, u.users ? k : m0, u.users ? m0 : k, bar);
+            tma_load_2d_pair(sa + PAIR_BOX, g, u.users ? k : m0 + 64, u.users ? m0 + 64 : k, bar);
           }
           tma_load_2d_pair(sb, vectors, n0, row, bar);
           if (u.width == PAIR_COLS) tma_load_2d_pair(sb + PAIR_BOX, vectors, n0 + 64, row, bar);
         }
         __syncwarp();
-        if (++s == LP_STAGES) { s = 0; ph ^= 1u; }
+        if (++s == Pipe::STAGES) { s = 0; ph ^= 1u; }
       }
     }
   } else if (pipe.warp == 1 && go) {
@@ -398,70 +398,103 @@ __global__ void __launch_bounds__(ProdPipe::THREADS, 1) loss_products_kernel(con
       int s = 0;
       uint32_t ph = 0, it = 0;
       for (int t = pair; t < a.total && !failed; t += pairs) {
-        const ProdUnit u(a, t, PLANES);
+        const ProdUnit u(a, t);
         const uint32_t idesc = idesc0 | (u.users ? 0u : 1u << 15) | ((uint32_t)(u.width >> 3) << 17);
         const uint64_t da0 = u.users ? da_k : da_mn;
         const uint32_t step_a = (u.users ? 32u : 2048u) >> 4;
-        for (int c0 = 0; c0 < u.blocks && !failed; c0 += a.chain, ++it) {          // an accumulator each
-          const int c1 = min(c0 + a.chain, u.blocks), buf = (int)(it & 1);
+        const int chain = CHAINED ? a.chain : u.blocks;
+        for (int c0 = 0; c0 < u.blocks && !failed; c0 += chain, ++it) {            // an accumulator each
+          const int c1 = min(c0 + chain, u.blocks), buf = (int)(it & 1);
           if (!mbar_wait_warp(pipe.tempty(buf), ((it >> 1) & 1) ^ 1u, pipe.abort_flag)) { failed = true; break; }
           tc_fence_after();
           const uint32_t tmem_d = pipe.tmem + (uint32_t)(buf * PAIR_COLS);
           for (int kb = c0; kb < c1; ++kb) {
             if (!mbar_wait_warp(pipe.full(s), ph, pipe.abort_flag)) { failed = true; break; }
             tc_fence_after();
-            const uint32_t soff = (uint32_t)(s * (PAIR_STAGE >> 4));
+            const uint32_t soff = (uint32_t)(s * (Pipe::STAGE >> 4));
             if (elect_one()) {
 #pragma unroll
-              for (uint32_t k = 0; k < 4; ++k)
-                tc_mma_pair(tmem_d, da0 + soff + k * step_a, db0 + soff + k * (2048u >> 4), idesc, (kb > c0 || k > 0) ? 1u : 0u);
+              for (uint32_t i = 0; i < PLANES; ++i)
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k)
+                  tc_mma_pair(tmem_d, da0 + soff + i * (PAIR_OPERAND >> 4) + k * step_a, db0 + soff + k * (2048u >> 4), idesc,
+                              (kb > c0 || k > 0 || i > 0) ? 1u : 0u);
               tc_commit_pair(pipe.empty(s));
               if (kb == c1 - 1) tc_commit_pair(pipe.tfull(buf));
             }
             __syncwarp();
-            if (++s == LP_STAGES) { s = 0; ph ^= 1u; }
+            if (++s == Pipe::STAGES) { s = 0; ph ^= 1u; }
           }
         }
       }
     }
   } else if (go) {
-    // ------------------------------ results (both blocks): a row and half of the columns a thread ------------------------------
-    const int lane = pipe.lane, q = pipe.warp & 3, half = (pipe.warp - 2) >> 2;
+    // ------------------------------ results (both blocks): a row and a part of the columns a thread ------------------------------
+    constexpr int PARTS = Pipe::EPI_WARPS / 4;
+    const int lane = pipe.lane, q = pipe.warp & 3, part = (pipe.warp - 2) >> 2;
+    const uint32_t lane_addr = pipe.tmem + ((uint32_t)(q * 32) << 16);
     uint32_t it = 0;
     for (int t = pair; t < a.total && !failed; t += pairs) {
-      const ProdUnit u(a, t, PLANES);
-      const int row = (int)pipe.rank * PAIR_ROWS + q * 32 + lane, blocks = u.width / 64;        // of 32 columns
-      const int col = half * blocks * 32;
-      // The tensor cores cut off where this adds with rounding: a chain's length sets the sum's precision.
-      float acc[4][32];
-      for (int c0 = 0; c0 < u.blocks; c0 += a.chain, ++it) {
+      const ProdUnit u(a, t);
+      const int64_t m = u.m0 + (int)pipe.rank * PAIR_ROWS + q * 32 + lane;
+      const int blocks = u.width / 32 / PARTS, col = part * blocks * 32;                // of 32 columns
+      const bool there = m < (u.users ? a.N : (int64_t)a.cols);
+      auto put = [&](int b, const float (&x)[32]) {
+        const int n = u.n0 + col + b * 32, some = a.d - n;
+        if (!there || some <= 0) return;
+        if (!u.users) put_row(reinterpret_cast<GT*>(a.dI) + m * a.ld_dI + n, x, some, a.wide_I, false);
+        else if (a.direct) put_row(reinterpret_cast<GT*>(a.dU) + m * a.ld_dU + n, x, some, a.wide_U, false);
+        else put_row(reinterpret_cast<float*>(a.dU) + ((int64_t)u.split * a.N + m) * a.d + n, x, some, a.wide_U, a.add);
+      };
+      if constexpr (CHAINED) {
+        // The tensor cores cut off where this adds with rounding: a chain's length sets the sum's precision.
+        float acc[4][32];
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+          for (int j = 0; j < 32; ++j) acc[b][j] = 0.f;
+#pragma unroll 1
+        for (int c0 = 0; c0 < u.blocks; c0 += a.chain, ++it) {
+          const int buf = (int)(it & 1);
+          if (!mbar_wait_warp(pipe.tfull(buf), (it >> 1) & 1, pipe.abort_flag)) { failed = true; break; }
+          tc_fence_after();
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            if (b >= blocks) break;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              uint32_t v[16];
+              tc_ld16(lane_addr + (uint32_t)(buf * PAIR_COLS + col + b * 32 + h * 16), v);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) acc[b][h * 16 + j] += __uint_as_float(v[j]);
+            }
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_remote(pipe.lead_tempty(buf));
+        }
+        if (failed) break;
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+          if (b < blocks) put(b, acc[b]);
+      } else {
         const int buf = (int)(it & 1);
         if (!mbar_wait_warp(pipe.tfull(buf), (it >> 1) & 1, pipe.abort_flag)) { failed = true; break; }
         tc_fence_after();
-        const uint32_t taddr = pipe.tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * PAIR_COLS + col);
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          if (b >= blocks) break;
+        for (int b = 0; b < blocks; ++b) {
           uint32_t v[32];
-          tc_ld32_issue(taddr + b * 32, v);
+          tc_ld32_issue(lane_addr + (uint32_t)(buf * PAIR_COLS + col + b * 32), v);
           tc_ld32_wait(v);
+          float x[32];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) acc[b][j] = c0 == 0 ? __uint_as_float(v[j]) : acc[b][j] + __uint_as_float(v[j]);
+          for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(v[j]);
+          put(b, x);
+          __syncwarp();
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_remote(pipe.lead_tempty(buf));
-      }
-      if (failed) break;
-      const int64_t m = u.m0 + row;
-      const bool there = m < (u.users ? a.N : (int64_t)a.cols);
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const int n = u.n0 + col + b * 32, some = a.d - n;
-        if (!there || b >= blocks || some <= 0) break;
-        if (!u.users) put_row(reinterpret_cast<GT*>(a.dI) + m * a.ld_dI + n, acc[b], some, a.wide_I, false);
-        else if (a.direct) put_row(reinterpret_cast<GT*>(a.dU) + m * a.ld_dU + n, acc[b], some, a.wide_U, false);
-        else put_row(reinterpret_cast<float*>(a.dU) + ((int64_t)u.split * a.N + m) * a.d + n, acc[b], some, a.wide_U, a.add);
+        ++it;
       }
       __syncwarp();
     }
@@ -681,7 +714,7 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
     w.units_u = w.users_m * w.tiles_n * w.splits;
     w.total = w.units_u + w.items_m * w.tiles_n;
     w.users_first = w.kb_split >= w.kb_users;
-    w.chain = planes == 2 ? 32 : 192;
+    w.chain = LP_CHAIN;
     w.dI = a.ditems ? (uint8_t*)a.ditems + (size_t)first * a.ld_ditems * size : nullptr;
     w.ld_dI = a.ld_ditems;
     w.dU = w.direct ? a.dusers : (void*)(base + p.parts);
@@ -693,8 +726,14 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
     w.status = e.status;
     ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * planes * a.N * cols * a.d * ((a.dusers != nullptr) + (a.ditems != nullptr)), 1, st, "loss_products");
     const int pairs = w.total < kPairs ? w.total : kPairs;
-    if (planes == 2) GRAM_CUDA(ctx, launch_pairs(loss_products_kernel<float>, pairs, ProdPipe::THREADS, ProdPipe::SMEM, st, map_g[0], map_g[1], map_clean, map_items, w));
-    else GRAM_CUDA(ctx, launch_pairs(loss_products_kernel<bf16>, pairs, ProdPipe::THREADS, ProdPipe::SMEM, st, map_g[0], map_g[1], map_clean, map_items, w));
+    const int longest = w.units_u && w.kb_split > w.kb_users ? w.kb_split : w.kb_users;
+    auto launch = [&](auto kern, auto pipe) {
+      using Pipe = decltype(pipe);
+      return launch_pairs(kern, pairs, Pipe::THREADS, Pipe::SMEM, st, map_g[0], map_g[1], map_clean, map_items, w);
+    };
+    if (planes == 1) GRAM_CUDA(ctx, launch(loss_products_kernel<bf16, false>, ProdPipe<1, false>()));
+    else if (longest <= LP_CHAIN) GRAM_CUDA(ctx, launch(loss_products_kernel<float, false>, ProdPipe<2, false>()));
+    else GRAM_CUDA(ctx, launch(loss_products_kernel<float, true>, ProdPipe<2, true>()));
   }
   if (a.dusers && !(p.splits == 1 && pieces == 1)) {
     ProfScope prof(ctx, GRAM_K_OTHER, (double)a.N * a.d * 4 * (p.splits + 1), 1, st, "loss_finish");
