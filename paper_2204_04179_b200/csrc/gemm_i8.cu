@@ -126,21 +126,29 @@ void launch_quantize(const void* x, int64_t ld, int64_t rows, int32_t cols, int8
 // ============================================================================================
 // the product
 // ============================================================================================
-// A pair of SMs owns a tile of 256 channels (rows of B, columns of C) x `width` tokens (rows of A): the channels are the MMA's rows, so
-// that the lanes of tensor memory, and with them a warp's stores, run along C's rows whatever C's address and stride, and a few tokens
-// are a narrow tile.  Sums are whole numbers of 32 bits, exact up to K = 131 071.
-constexpr int I8_STAGES = 6, I8_EPI_WARPS = 16, I8_BK = 128;
-constexpr int I8_SCALE_BYTES = I8_EPI_WARPS * 64 * 4;   // a warp's tokens
-using I8Pipe = PairPipe<I8_STAGES, I8_EPI_WARPS, I8_SCALE_BYTES>;
+// C's rows are tokens, its columns channels (rows of A and of B).  Sums are whole numbers of 32 bits, exact up to K = 131 071.  Two forms:
+//   ROWS      a pair of SMs owns 256 tokens x 256 channels, tokens are the MMA's rows: a thread holds 32 neighbouring results of a row, which
+//             leave by bulk stores.  Many tokens, C aligned to 16 bytes.
+//   CHANNELS  256 channels x `width` tokens, channels are the MMA's rows: a warp's lanes run along C's rows, whatever its address and stride,
+//             and a few tokens are a narrow tile.
+// The tiles of the operand with fewer rows vary fastest: it stays in L2 while the other is read once.
+constexpr int I8_BK = 128, I8_EPI_WARPS = 16;
+using I8Rows = PairPipe<4, I8_EPI_WARPS, I8_EPI_WARPS * (4096 + 512)>;      // a warp's box of results, and its channels' scales and biases
+using I8Channels = PairPipe<6, I8_EPI_WARPS, I8_EPI_WARPS * 64 * 4>;        // a warp's tokens' scales
 
 struct I8Args {
   const float *scale_a, *scale_b, *bias;
   void* C;
   int64_t ldc, M;
-  int32_t N, num_kb, tiles_n, total, width;             // tiles of 256 channels; tokens of a tile
+  int32_t N, num_kb, width;      // width: columns of the MMA's tile
+  int32_t fast, total;           // tiles that vary fastest
+  int32_t rows_fast;             // those of the MMA's rows
   int32_t give_up;
   int32_t* status;
 };
+// first row of tile t's MMA rows and of its columns
+__device__ __forceinline__ int i8_row(const I8Args& a, int t) { return (a.rows_fast ? t % a.fast : t / a.fast) * 2 * PAIR_ROWS; }
+__device__ __forceinline__ int i8_col(const I8Args& a, int t) { return (a.rows_fast ? t / a.fast : t % a.fast) * a.width; }
 
 __device__ __forceinline__ void i8_mma_pair(uint32_t tmem_d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accum) {
   asm volatile(
@@ -150,65 +158,161 @@ __device__ __forceinline__ void i8_mma_pair(uint32_t tmem_d, uint64_t da, uint64
       : "memory");
 }
 
-template <typename CT>
-__global__ void __launch_bounds__(I8Pipe::THREADS, 1) gemm_i8_kernel(const __grid_constant__ CUtensorMap channels, const __grid_constant__ CUtensorMap tokens,
-                                                                     const __grid_constant__ I8Args a) {
-  extern __shared__ uint8_t smem_raw[];
-  I8Pipe pipe;
-  const bool go = pipe.open(smem_raw);
+// the copies and products of all of a pair's tiles: both blocks' first warp and the leader's second
+template <typename Pipe>
+__device__ __forceinline__ bool i8_copies(const Pipe& pipe, const I8Args& a, const CUtensorMap& rows, const CUtensorMap& cols) {
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  const uint32_t bytes = PAIR_OPERAND + (uint32_t)a.width * (I8_BK / 2);
+  int s = 0, tile = 0;
+  uint32_t ph = 0;
+  for (int t = pair; t < a.total; t += pairs, ++tile) {
+    if (tile == a.give_up) return false;
+    const int r0 = i8_row(a, t) + (int)pipe.rank * PAIR_ROWS, c0 = i8_col(a, t) + (int)pipe.rank * (a.width / 2);
+    for (int kb = 0; kb < a.num_kb; ++kb) {
+      if (!mbar_wait_warp(pipe.empty(s), ph ^ 1u, pipe.abort_flag)) return false;
+      const uint32_t bar = pipe.lead_full(s);
+      if (elect_one()) {
+        mbar_arrive_expect_tx_remote(bar, bytes);
+        tma_load_2d_pair(pipe.a_of(s), &rows, kb * I8_BK, r0, bar);
+        tma_load_2d_pair(pipe.b_of(s), &cols, kb * I8_BK, c0, bar);
+      }
+      __syncwarp();
+      if (++s == Pipe::STAGES) { s = 0; ph ^= 1u; }
+    }
+  }
+  return true;
+}
+template <typename Pipe> __device__ __forceinline__ bool i8_products(const Pipe& pipe, const I8Args& a) {
+  // signed 8-bit operands, sums in 32-bit whole numbers
+  const uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(a.width >> 3) << 17) | ((uint32_t)(2 * PAIR_ROWS >> 4) << 24);
+  const uint64_t da0 = make_desc(pipe.a_of(0), 16, 1024), db0 = make_desc(pipe.b_of(0), 16, 1024);
+  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  int s = 0;
+  uint32_t ph = 0, it = 0;
+  for (int t = pair; t < a.total; t += pairs, ++it) {
+    const int buf = (int)(it & 1);
+    if (!mbar_wait_warp(pipe.tempty(buf), ((it >> 1) & 1) ^ 1u, pipe.abort_flag)) return false;
+    tc_fence_after();
+    const uint32_t tmem_d = pipe.tmem + (uint32_t)(buf * PAIR_COLS);
+    for (int kb = 0; kb < a.num_kb; ++kb) {
+      if (!mbar_wait_warp(pipe.full(s), ph, pipe.abort_flag)) return false;
+      tc_fence_after();
+      const uint32_t soff = (uint32_t)(s * (Pipe::STAGE >> 4));
+      if (elect_one()) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)                     // 32 bytes of the rows each
+          i8_mma_pair(tmem_d, da0 + soff + (uint64_t)(k * 2), db0 + soff + (uint64_t)(k * 2), idesc, (kb > 0 || k > 0) ? 1u : 0u);
+        tc_commit_pair(pipe.empty(s));
+        if (kb == a.num_kb - 1) tc_commit_pair(pipe.tfull(buf));
+      }
+      __syncwarp();
+      if (++s == Pipe::STAGES) { s = 0; ph ^= 1u; }
+    }
+  }
+  return true;
+}
+
+template <typename CT>
+__global__ void __launch_bounds__(I8Rows::THREADS, 1) gemm_i8_rows_kernel(const __grid_constant__ CUtensorMap tokens, const __grid_constant__ CUtensorMap channels,
+                                                                          const __grid_constant__ CUtensorMap result, const __grid_constant__ I8Args a) {
+  extern __shared__ uint8_t smem_raw[];
+  I8Rows pipe;
+  const bool go = pipe.open(smem_raw);
   bool failed = false;
   if (pipe.warp == 0 && go) {
-    // ------------------------------ copies (both blocks) ------------------------------
-    int s = 0, tile = 0;
-    uint32_t ph = 0;
-    const uint32_t bytes = PAIR_OPERAND + (uint32_t)a.width * (I8_BK / 2);
-    for (int t = pair; t < a.total && !failed; t += pairs, ++tile) {
-      if (tile == a.give_up) { failed = true; break; }
-      const int n0 = (t % a.tiles_n) * 2 * PAIR_ROWS + (int)pipe.rank * PAIR_ROWS;
-      const int m0 = (t / a.tiles_n) * a.width + (int)pipe.rank * (a.width / 2);
-      for (int kb = 0; kb < a.num_kb; ++kb) {
-        if (!mbar_wait_warp(pipe.empty(s), ph ^ 1u, pipe.abort_flag)) { failed = true; break; }
-        const uint32_t bar = pipe.lead_full(s);
-        if (elect_one()) {
-          mbar_arrive_expect_tx_remote(bar, bytes);
-          tma_load_2d_pair(pipe.a_of(s), &channels, kb * I8_BK, n0, bar);
-          tma_load_2d_pair(pipe.b_of(s), &tokens, kb * I8_BK, m0, bar);
+    failed = !i8_copies(pipe, a, tokens, channels);
+  } else if (pipe.warp == 1 && go) {
+    if (pipe.rank == 0) failed = !i8_products(pipe, a);
+  } else if (go) {
+    // ------------------------------ results (both blocks): a token and 64 channels a thread ------------------------------
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int lane = pipe.lane, q = pipe.warp & 3, part = (pipe.warp - 2) >> 2, w = pipe.warp - 2;
+    const uint32_t box = pipe.tiles + I8Rows::STAGES * I8Rows::STAGE + (uint32_t)w * 4096u, row_at = box + (uint32_t)lane * 128u;
+    float* of = reinterpret_cast<float*>(pipe.extra + I8_EPI_WARPS * 4096) + w * 128;        // 64 scales, 64 biases
+    uint32_t it = 0;
+    for (int t = pair; t < a.total; t += pairs, ++it) {
+      const int buf = (int)(it & 1), col0 = i8_col(a, t) + part * 64;
+      const int row0 = i8_row(a, t) + (int)pipe.rank * PAIR_ROWS + q * 32;
+      const bool active = row0 < a.M && col0 < a.N;     // of the warp
+      float sa = 0.f;
+      if (active) {
+        if (row0 + lane < a.M) sa = __ldg(a.scale_a + row0 + lane);
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int n = col0 + i * 32 + lane;
+          of[i * 32 + lane] = n < a.N ? __ldg(a.scale_b + n) : 0.f;
+          of[64 + i * 32 + lane] = n < a.N && a.bias ? __ldg(a.bias + n) : 0.f;
         }
         __syncwarp();
-        if (++s == I8_STAGES) { s = 0; ph ^= 1u; }
       }
-    }
-  } else if (pipe.warp == 1 && go) {
-    // ------------------------------ products (leader): signed 8-bit operands, sums in 32-bit whole numbers ------------------------------
-    if (pipe.rank == 0) {
-      const uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(a.width >> 3) << 17) | ((uint32_t)(2 * PAIR_ROWS >> 4) << 24);
-      const uint64_t da0 = make_desc(pipe.a_of(0), 16, 1024), db0 = make_desc(pipe.b_of(0), 16, 1024);
-      int s = 0;
-      uint32_t ph = 0, it = 0;
-      for (int t = pair; t < a.total && !failed; t += pairs, ++it) {
-        const int buf = (int)(it & 1);
-        if (!mbar_wait_warp(pipe.tempty(buf), ((it >> 1) & 1) ^ 1u, pipe.abort_flag)) { failed = true; break; }
-        tc_fence_after();
-        const uint32_t tmem_d = pipe.tmem + (uint32_t)(buf * PAIR_COLS);
-        for (int kb = 0; kb < a.num_kb; ++kb) {
-          if (!mbar_wait_warp(pipe.full(s), ph, pipe.abort_flag)) { failed = true; break; }
-          tc_fence_after();
-          const uint32_t soff = (uint32_t)(s * (I8Pipe::STAGE >> 4));
-          if (elect_one()) {
+      if (!mbar_wait_warp(pipe.tfull(buf), (it >> 1) & 1, pipe.abort_flag)) { failed = true; break; }
+      tc_fence_after();
+      if (active) {
+        const uint32_t taddr = pipe.tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * PAIR_COLS + part * 64);
 #pragma unroll
-            for (int k = 0; k < 4; ++k)                 // 32 bytes of the rows each
-              i8_mma_pair(tmem_d, da0 + soff + (uint64_t)(k * 2), db0 + soff + (uint64_t)(k * 2), idesc, (kb > 0 || k > 0) ? 1u : 0u);
-            tc_commit_pair(pipe.empty(s));
-            if (kb == a.num_kb - 1) tc_commit_pair(pipe.tfull(buf));
+        for (int b = 0; b < 2; ++b) {
+          uint32_t v[32];
+          tc_ld32_issue(taddr + b * 32, v);
+          tc_ld32_wait(v);
+          if (b == 0 || sizeof(CT) == 4) {              // the box's last store has read it
+            if (lane == 0) bulk_wait_read_all();
+            __syncwarp();
           }
-          __syncwarp();
-          if (++s == I8_STAGES) { s = 0; ph ^= 1u; }
+#pragma unroll
+          for (int j = 0; j < 32; j += 4) {
+            const float4 sb = *reinterpret_cast<const float4*>(of + b * 32 + j), bias = *reinterpret_cast<const float4*>(of + 64 + b * 32 + j);
+            v[j] = __float_as_uint(fmaf((float)(int32_t)v[j] * sa, sb.x, bias.x));
+            v[j + 1] = __float_as_uint(fmaf((float)(int32_t)v[j + 1] * sa, sb.y, bias.y));
+            v[j + 2] = __float_as_uint(fmaf((float)(int32_t)v[j + 2] * sa, sb.z, bias.z));
+            v[j + 3] = __float_as_uint(fmaf((float)(int32_t)v[j + 3] * sa, sb.w, bias.w));
+          }
+          if constexpr (sizeof(CT) == 4) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sts128(row_at + ((uint32_t)(j ^ (lane & 7)) << 4), v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              uint32_t h[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) h[i] = pack_bf16x2(__uint_as_float(v[8 * j + 2 * i]), __uint_as_float(v[8 * j + 2 * i + 1]));
+              sts128(row_at + ((uint32_t)((b * 4 + j) ^ (lane & 7)) << 4), h[0], h[1], h[2], h[3]);
+            }
+          }
+          if (b == 1 || sizeof(CT) == 4) {
+            fence_proxy_async_smem();
+            __syncwarp();
+            const int n = col0 + (sizeof(CT) == 4 ? b * 32 : 0);
+            if (lane == 0 && n < a.N) {
+              tma_store_2d(&result, box, n, row0);
+              bulk_commit();
+            }
+          }
         }
       }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_remote(pipe.lead_tempty(buf));
     }
+    if (lane == 0) bulk_wait_all();                     // its stores are complete before the block may exit
+  }
+  pipe.close(failed, a.status);
+}
+
+template <typename CT>
+__global__ void __launch_bounds__(I8Channels::THREADS, 1) gemm_i8_channels_kernel(const __grid_constant__ CUtensorMap channels,
+                                                                                  const __grid_constant__ CUtensorMap tokens, const __grid_constant__ I8Args a) {
+  extern __shared__ uint8_t smem_raw[];
+  I8Channels pipe;
+  const bool go = pipe.open(smem_raw);
+  bool failed = false;
+  if (pipe.warp == 0 && go) {
+    failed = !i8_copies(pipe, a, channels, tokens);
+  } else if (pipe.warp == 1 && go) {
+    if (pipe.rank == 0) failed = !i8_products(pipe, a);
   } else if (go) {
     // ------------------------------ results (both blocks): a channel a thread ------------------------------
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const int lane = pipe.lane, q = pipe.warp & 3, part = (pipe.warp - 2) >> 2;
     float* scale_w = reinterpret_cast<float*>(pipe.extra) + (pipe.warp - 2) * 64;
     const int blocks = (a.width + 127) / 128;           // of 32 tokens of this warp, one where the tile is narrow
@@ -216,8 +320,8 @@ __global__ void __launch_bounds__(I8Pipe::THREADS, 1) gemm_i8_kernel(const __gri
     uint32_t it = 0;
     for (int t = pair; t < a.total && !failed; t += pairs, ++it) {
       const int buf = (int)(it & 1);
-      const int64_t n = (int64_t)(t % a.tiles_n) * 2 * PAIR_ROWS + (int)pipe.rank * PAIR_ROWS + q * 32 + lane;
-      const int64_t m0 = (int64_t)(t / a.tiles_n) * a.width + tok0;
+      const int64_t n = (int64_t)i8_row(a, t) + (int)pipe.rank * PAIR_ROWS + q * 32 + lane;
+      const int64_t m0 = (int64_t)i8_col(a, t) + tok0;
       const bool active = n - lane < a.N && tok0 < a.width && m0 < a.M;         // of the warp
       float sb = 0.f, bias = 0.f;
       if (active) {
@@ -247,6 +351,7 @@ __global__ void __launch_bounds__(I8Pipe::THREADS, 1) gemm_i8_kernel(const __gri
               else to[j * a.ldc] = __float2bfloat16_rn(x);
             }
           }
+          __syncwarp();
         }
       }
       tc_fence_before();
@@ -291,20 +396,30 @@ gram_status gemm_i8_launch(gram_ctx* ctx, const int8_t* A, int64_t lda, const fl
   a.M = M;
   a.N = N;
   a.num_kb = ceil_div(K, I8_BK);
-  a.tiles_n = ceil_div(N, 2 * PAIR_ROWS);
-  a.width = M > 128 ? 256 : M > 64 ? 128 : M > 32 ? 64 : 32;
-  const int64_t total = a.tiles_n * ceil_div64(M, a.width);
-  if (total > INT32_MAX - kPairs) return gram_set_error(ctx, "gram_gemm_i8: %lld x %d are too many results", (long long)M, N), GRAM_ERR_UNSUPPORTED;
-  a.total = (int32_t)total;
+  const size_t size = c_dtype == GRAM_F32 ? 4 : 2;
+  const bool rows = M > PAIR_ROWS && (uintptr_t)C % 16 == 0 && ldc * size % 16 == 0;
+  a.width = rows || M > 128 ? 256 : M > 64 ? 128 : M > 32 ? 64 : 32;
+  const int64_t tiles_r = ceil_div64(rows ? M : N, 2 * PAIR_ROWS), tiles_c = ceil_div64(rows ? N : M, a.width);
+  if (tiles_r * tiles_c > INT32_MAX - kPairs) return gram_set_error(ctx, "gram_gemm_i8: %lld x %d are too many results", (long long)M, N), GRAM_ERR_UNSUPPORTED;
+  a.total = (int32_t)(tiles_r * tiles_c);
+  a.rows_fast = tiles_r < tiles_c;
+  a.fast = (int32_t)(a.rows_fast ? tiles_r : tiles_c);
   a.give_up = gram_ring_rows(ctx);
   a.status = gram_status_word(ctx);
-  CUtensorMap channels, tokens;
-  if (!make_map_i8(&channels, B, (uint64_t)K, (uint64_t)N, (uint64_t)ldb, PAIR_ROWS) ||
-      !make_map_i8(&tokens, A, (uint64_t)K, (uint64_t)M, (uint64_t)lda, (uint32_t)a.width / 2))
-    return gram_set_error(ctx, "gram_gemm_i8: cannot describe the operands"), GRAM_ERR_UNSUPPORTED;
+  const uint32_t rows_a = rows ? PAIR_ROWS : (uint32_t)a.width / 2, rows_b = rows ? (uint32_t)a.width / 2 : PAIR_ROWS;
+  CUtensorMap channels, tokens, result = {};
+  if (!make_map_i8(&channels, B, (uint64_t)K, (uint64_t)N, (uint64_t)ldb, rows_b) || !make_map_i8(&tokens, A, (uint64_t)K, (uint64_t)M, (uint64_t)lda, rows_a) ||
+      (rows && !(c_dtype == GRAM_F32 ? make_map_f32(&result, C, (uint64_t)N, (uint64_t)M, (uint64_t)ldc, 32, 32)
+                                     : make_map(&result, C, (uint64_t)N, (uint64_t)M, (uint64_t)ldc, 64, 32))))
+    return gram_set_error(ctx, "gram_gemm_i8: cannot describe the matrices"), GRAM_ERR_UNSUPPORTED;
   ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * M * N * K, 1, st, "gemm_i8");
   const int pairs = a.total < kPairs ? a.total : kPairs;
-  if (c_dtype == GRAM_F32) GRAM_CUDA(ctx, launch_pairs(gemm_i8_kernel<float>, pairs, I8Pipe::THREADS, I8Pipe::SMEM, st, channels, tokens, a));
-  else GRAM_CUDA(ctx, launch_pairs(gemm_i8_kernel<bf16>, pairs, I8Pipe::THREADS, I8Pipe::SMEM, st, channels, tokens, a));
+  if (rows) {
+    auto kern = c_dtype == GRAM_F32 ? gemm_i8_rows_kernel<float> : gemm_i8_rows_kernel<bf16>;
+    GRAM_CUDA(ctx, launch_pairs(kern, pairs, I8Rows::THREADS, I8Rows::SMEM, st, tokens, channels, result, a));
+  } else {
+    auto kern = c_dtype == GRAM_F32 ? gemm_i8_channels_kernel<float> : gemm_i8_channels_kernel<bf16>;
+    GRAM_CUDA(ctx, launch_pairs(kern, pairs, I8Channels::THREADS, I8Channels::SMEM, st, channels, tokens, a));
+  }
   return GRAM_OK;
 }

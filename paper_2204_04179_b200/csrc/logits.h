@@ -25,3 +25,6 @@ gram_status distill_launch(gram_ctx* ctx, const void* logits, int dtype, int64_t
 gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_users, const void* items, int64_t ld_items,
                                   const float* bias, int64_t N, int32_t V, int32_t d, float scale, const RowAnswers& ask, void* ws,
                                   size_t ws_bytes, cudaStream_t st);
+// the logits themselves, [N, ld_logits] (ld_logits >= V, a multiple of 8, 32-byte aligned): what N x V are few enough for
+gram_status score_logits_launch(gram_ctx* ctx, const void* users, int64_t ld_users, const void* items, int64_t ld_items, const float* bias, int64_t N,
+                                int32_t V, int32_t d, float* logits, int64_t ld_logits, cudaStream_t st);

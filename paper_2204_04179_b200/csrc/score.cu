@@ -729,16 +729,47 @@ RowAnswers from(RowAnswers ask, int64_t n) {
 
 }  // namespace
 
+// copies are no larger than the users (rows past the last are filled with zeros, which takes time: one user against 100 000
+// items of 768 46 us with boxes of 128 rows, 35 with boxes of 8)
+static int score_box_rows(int64_t N) {
+  int rows = SM_ROWS;
+  while (rows > 8 && rows / 2 >= N) rows /= 2;
+  return rows;
+}
+
+gram_status score_logits_launch(gram_ctx* ctx, const void* users, int64_t ld_users, const void* items, int64_t ld_items, const float* bias, int64_t N,
+                                int32_t V, int32_t d, float* logits, int64_t ld_logits, cudaStream_t st) {
+  CUtensorMap map_u, map_i;
+  const int box_rows = score_box_rows(N);
+  if (!make_map(&map_u, users, (uint64_t)d, (uint64_t)N, (uint64_t)ld_users, SC_BK, (uint32_t)box_rows) ||
+      !make_map(&map_i, items, (uint64_t)d, (uint64_t)V, (uint64_t)ld_items, SC_BK, 64))
+    return gram_set_error(ctx, "scores: cannot describe the vectors"), GRAM_ERR_UNSUPPORTED;
+  ScoreArgs a = {};
+  a.bias = bias;
+  a.N = N;
+  a.V = V;
+  a.box_rows = box_rows;
+  a.num_kb = ceil_div(d, SC_BK);
+  a.stride = 1;
+  a.units = ceil_div(V, SC_UNIT);
+  a.total = (int32_t)ceil_div64(N, SC_ROWS) * a.units;
+  a.per_run = ceil_div(a.total, kNumSMs / 2);
+  a.logits = logits;
+  a.ld_logits = ld_logits;
+  a.give_up = gram_ring_rows(ctx);
+  a.status = gram_status_word(ctx);
+  ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * N * V * d, 1, st, "score");
+  GRAM_CUDA(ctx, launch_score<LOGITS>(map_u, map_i, a, ceil_div(a.total, a.per_run), st));
+  return GRAM_OK;
+}
+
 gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_users, const void* items, int64_t ld_items,
                                   const float* bias, int64_t N, int32_t V, int32_t d, float scale, const RowAnswers& ask, void* ws,
                                   size_t ws_bytes, cudaStream_t st) {
   if (V > (1 << 30) / (kNumSMs / 2) * SC_UNIT) return gram_set_error(ctx, "gram_score_logprobs: %d items", V), GRAM_ERR_UNSUPPORTED;   // units of all row tiles, in 32 bits
   const int32_t all_units = ceil_div(V, SC_UNIT);
   CUtensorMap map_u, map_i;
-  // copies are no larger than the users (rows past the last are filled with zeros, which takes time: one user against 100 000
-  // items of 768 46 us with boxes of 128 rows, 35 with boxes of 8)
-  int box_rows = SM_ROWS;
-  while (box_rows > 8 && box_rows / 2 >= N) box_rows /= 2;
+  const int box_rows = score_box_rows(N);
   if (!make_map(&map_i, items, (uint64_t)d, (uint64_t)V, (uint64_t)ld_items, SC_BK, 64))
     return gram_set_error(ctx, "gram_score_logprobs: cannot describe the items"), GRAM_ERR_UNSUPPORTED;
   const int64_t ld_logits = ((int64_t)V + 7) / 8 * 8;
@@ -761,21 +792,10 @@ gram_status score_logprobs_launch(gram_ctx* ctx, const void* users, int64_t ld_u
   const int64_t room = (int64_t)(ws_bytes < (32u << 20) ? ws_bytes : 32u << 20) / (int64_t)sizeof(float) / ld_logits;
   const int64_t at_once = room < SC_ROWS ? room : room / SC_ROWS * SC_ROWS;       // users of a turn
   if (ask.k > 0 ? at_once > 0 && (N <= at_once || at_once >= (ask.k > 64 ? 768 : 2048)) : N <= at_once && N * V <= (2 << 20)) {
-    a.V = V;
-    a.units = all_units;
-    a.logits = (float*)ws;
-    a.ld_logits = ld_logits;
     for (int64_t n = 0; n < N; n += at_once) {
-      a.N = N - n < at_once ? N - n : at_once;
-      if (!make_map(&map_u, (const bf16*)users + n * ld_users, (uint64_t)d, (uint64_t)a.N, (uint64_t)ld_users, SC_BK, (uint32_t)box_rows))
-        return gram_set_error(ctx, "gram_score_logprobs: cannot describe the users"), GRAM_ERR_UNSUPPORTED;
-      a.total = (int32_t)ceil_div64(a.N, SC_ROWS) * all_units;
-      a.per_run = ceil_div(a.total, kNumSMs / 2);
-      {
-        ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * a.N * V * d, 1, st, "score");
-        GRAM_CUDA(ctx, launch_score<LOGITS>(map_u, map_i, a, ceil_div(a.total, a.per_run), st));
-      }
-      GRAM_TRY(logprobs_launch(ctx, ws, GRAM_F32, ld_logits, a.N, V, scale, from(ask, n), st));
+      const int64_t now = N - n < at_once ? N - n : at_once;
+      GRAM_TRY(score_logits_launch(ctx, (const bf16*)users + n * ld_users, ld_users, items, ld_items, bias, now, V, d, (float*)ws, ld_logits, st));
+      GRAM_TRY(logprobs_launch(ctx, ws, GRAM_F32, ld_logits, now, V, scale, from(ask, n), st));
     }
     return GRAM_OK;
   }

@@ -22,6 +22,7 @@ namespace {
 using namespace tc;
 
 constexpr int kPairs = kNumSMs / 2;
+constexpr int LOSS_FEW = 256;                           // users whose logits are kept where 32 MB hold them
 
 // ============================================================================================
 // rows: loss, and the constants of g
@@ -34,31 +35,101 @@ struct RowConst {
 };
 static_assert(sizeof(RowConst) == 16, "read as one float4");
 
-// A warp a user.  clean: the users' vectors with those of rows that take no part as zeros, so that whatever a padded row holds does
-// not reach dI (0 times NaN).
+// A row's statistics, log p of its target and weight.
+__device__ __forceinline__ RowConst loss_row(const ScoreLoss& a, const float* logp, const float2* stats, int64_t n) {
+  const int32_t t = a.targets[n];
+  const float lp = logp[n], w = a.weight ? a.weight[n] : 1.f;
+  const float2 s = stats[n];
+  const bool part = t >= 0 && t < a.V && w != 0.f && lp != ROW_NEG_INF;
+  return RowConst{s.x, s.y * kLog2e, lp != lp ? lp : w * a.scale, part ? t : -1};
+}
+__device__ __forceinline__ float loss_of(const ScoreLoss& a, const float* logp, int64_t n, int32_t* status) {
+  const int32_t t = a.targets[n];
+  if (t >= 0 && t < a.V) return 0.f - logp[n];
+  if (t != -1) gram_device_fail(status, GRAM_ERR_ID_RANGE);
+  return 0.f;
+}
+// The user's vector, by a warp: zeros for a row that takes no part, so that whatever a padded row holds does not reach dI (0 times NaN).
+__device__ __forceinline__ void loss_clean(const ScoreLoss& a, int64_t n, bool part, bf16* clean) {
+  const uint4* from = reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(a.users) + n * a.ld_users);
+  uint4* to = reinterpret_cast<uint4*>(clean + n * a.d);
+  for (int i = threadIdx.x & 31; i < a.d / 8; i += 32) to[i] = part ? __ldg(from + i) : make_uint4(0u, 0u, 0u, 0u);
+}
+
+// A warp a user.  rows, clean: null where they are not needed.
 __global__ void __launch_bounds__(256) loss_rows_kernel(const ScoreLoss a, const float* logp, const float2* stats, RowConst* rows, bf16* clean,
                                                         int32_t* status) {
   if (!chain_begin()) return;
-  const int lane = threadIdx.x & 31;
   const int64_t n = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (n >= a.N) return;
-  const int32_t t = a.targets[n];
-  const bool in = t >= 0 && t < a.V;
-  const float lp = logp[n], w = a.weight ? a.weight[n] : 1.f;
-  const bool part = in && w != 0.f && lp != ROW_NEG_INF;
-  if (lane == 0) {
-    if (!in && t != -1) gram_device_fail(status, GRAM_ERR_ID_RANGE);
-    a.loss[n] = in ? 0.f - lp : 0.f;
-    if (rows) {
-      const float2 s = stats[n];
-      rows[n] = RowConst{s.x, s.y * kLog2e, lp != lp ? lp : w * a.scale, part ? t : -1};
+  const RowConst r = loss_row(a, logp, stats, n);
+  if ((threadIdx.x & 31) == 0) {
+    a.loss[n] = loss_of(a, logp, n, status);
+    if (rows) rows[n] = r;
+  }
+  if (clean) loss_clean(a, n, r.t >= 0, clean);
+}
+
+// p, and g of a row's entry
+__device__ __forceinline__ float loss_p(const RowConst& r, float z, float c) { return row_ex2(fminf(fmaf(z - r.m, c, -r.l), 0.f)); }
+
+// Few users: g from logits that lie in L2, with the loss, the users' vectors and db, in one launch.  A block takes 128 columns, four a lane,
+// its warps the rows in turn; of the first piece it also takes the rows of its own number's residue.
+struct FewArgs {
+  const float* z;                // [N, ldz]
+  int64_t ldz;
+  const float* logp;
+  const float2* stats;
+  int32_t first, cols;
+  bf16* g;                       // [planes, N, ldg]
+  int64_t ldg, plane;
+  bf16* clean;                   // or null
+  int32_t* status;
+};
+template <int PLANES> __global__ void __launch_bounds__(256) loss_few_kernel(const ScoreLoss a, const FewArgs f) {
+  if (!chain_begin()) return;
+  __shared__ float4 sums[8][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 128 + 4 * lane;
+  if (f.first == 0)
+    for (int64_t n = blockIdx.x + (int64_t)warp * gridDim.x; n < a.N; n += 8 * (int64_t)gridDim.x) {
+      if (lane == 0) a.loss[n] = loss_of(a, f.logp, n, f.status);
+      if (f.clean) loss_clean(a, n, loss_row(a, f.logp, f.stats, n).t >= 0, f.clean);
+    }
+  const float c = a.scale * kLog2e;
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (col < f.cols) {
+#pragma unroll 4
+    for (int64_t n = warp; n < a.N; n += 8) {
+      const float4 z = *reinterpret_cast<const float4*>(f.z + n * f.ldz + f.first + col);
+      const RowConst r = loss_row(a, f.logp, f.stats, n);
+      float g[4] = {loss_p(r, z.x, c), loss_p(r, z.y, c), loss_p(r, z.z, c), loss_p(r, z.w, c)};
+      const int hot = r.t - f.first - col;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) g[j] = r.t < 0 ? 0.f : r.f * (j == hot ? g[j] - 1.f : g[j]);
+      const uint2 h = make_uint2(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]));
+      bf16* to = f.g + n * f.ldg + col;
+      *reinterpret_cast<uint2*>(to) = h;
+      if constexpr (PLANES == 2) {
+        const float2 u = unpack_bf16x2(h.x), v = unpack_bf16x2(h.y);
+        *reinterpret_cast<uint2*>(to + f.plane) = make_uint2(pack_bf16x2(g[0] - u.x, g[1] - u.y), pack_bf16x2(g[2] - v.x, g[3] - v.y));
+      }
+      sum.x += g[0]; sum.y += g[1]; sum.z += g[2]; sum.w += g[3];
     }
   }
-  if (clean) {
-    const uint4* from = reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(a.users) + n * a.ld_users);
-    uint4* to = reinterpret_cast<uint4*>(clean + n * a.d);
-    for (int i = lane; i < a.d / 8; i += 32) to[i] = part ? __ldg(from + i) : make_uint4(0u, 0u, 0u, 0u);
+  if (!a.dbias) return;
+  sums[warp][lane] = sum;
+  __syncthreads();
+  if (warp != 0) return;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) {
+    const float4 x = sums[i][lane];
+    sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
   }
+  float* to = a.dbias + f.first + col;
+  if (col < f.cols) to[0] = sum.x;
+  if (col + 1 < f.cols) to[1] = sum.y;
+  if (col + 2 < f.cols) to[2] = sum.z;
+  if (col + 3 < f.cols) to[3] = sum.w;
 }
 
 // ============================================================================================
@@ -204,7 +275,7 @@ __global__ void __launch_bounds__(GradPipe::THREADS, 1) loss_grad_kernel(const _
           for (int j = 0; j < 32; ++j) {
             float z = __uint_as_float(v[j]);
             if (bias) z += bias[b * 32 + j];
-            g[j] = row_ex2(fminf(fmaf(z - r.m, a.c, -r.l), 0.f));
+            g[j] = loss_p(r, z, a.c);
           }
           if (r.t >= 0 && (unsigned)(hot - b * 32) < 32u) {
 #pragma unroll
@@ -273,7 +344,8 @@ struct ProdArgs {
   int32_t items_m;               // tiles of 256 items (0: dI is not asked)
   int32_t users_m, splits;       // tiles of 256 users (0: dU is not asked); parts of the piece's items that a unit of dU sums over
   int32_t kb_users, kb_items, kb_split;      // blocks of 64 users, of 64 items, of a part's items
-  int32_t units_u, total, users_first;       // units of dU, of both; which come first
+  int32_t units_u, total, users_first;       // units of dU, of both; whether those of dU are the heavier ones, which are dealt first
+  int32_t extra;                 // lighter units that a pair gets for each heavier one that others have more
   int32_t chain;                 // blocks that are added up in one accumulator
   void* dI;                      // rows of the piece's items
   int64_t ld_dI;
@@ -283,6 +355,27 @@ struct ProdArgs {
   int32_t wide_I, wide_U;        // rows begin on 32 bytes
   int32_t give_up;
   int32_t* status;
+};
+
+// Which units a pair takes, its i-th: the heavier ones are dealt first; pairs that get one less take `extra` lighter ones instead; the rest is dealt
+// from the pairs with less on.  (The same in loss_span.)
+struct ProdWalk {
+  int pair, pairs, heavy, mine, extra, other, base, at, total;
+  __device__ __forceinline__ explicit ProdWalk(const ProdArgs& a) : pair(blockIdx.x >> 1), pairs(gridDim.x >> 1), total(a.total) {
+    heavy = a.users_first ? a.units_u : a.total - a.units_u;
+    const int more = heavy % pairs;                     // pairs with one more
+    mine = heavy / pairs + (pair < more);
+    other = pairs - more;
+    extra = pair < more ? 0 : a.extra;
+    base = heavy + a.extra * other;
+    at = pair < more ? pair + other : pair - more;
+  }
+  __device__ __forceinline__ int operator()(int i) const {
+    if (i < mine) return pair + i * pairs;
+    i -= mine;
+    if (i < extra) return heavy + i * other + (pairs - other > pair ? 0 : pair - (pairs - other));
+    return base + at + (i - extra) * pairs;
+  }
 };
 
 // A unit: a tile of dI over all users, or a tile of dU over a part of the piece's items.
@@ -356,13 +449,13 @@ __global__ void __launch_bounds__(ProdPipe<sizeof(GT) / 2, CHAINED>::THREADS, 1)
   extern __shared__ uint8_t smem_raw[];
   Pipe pipe;
   const bool go = pipe.open(smem_raw);
-  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  const ProdWalk walk(a);
   bool failed = false;
   if (pipe.warp == 0 && go) {
     // ------------------------------ copies (both blocks): two boxes of 64 x 64 of each plane of g, one or two of the vectors ------------------------------
-    int s = 0, tile = 0;
+    int s = 0;
     uint32_t ph = 0;
-    for (int t = pair; t < a.total && !failed; t += pairs, ++tile) {
+    for (int tile = 0, t; (t = walk(tile)) < a.total && !failed; ++tile) {
       if (tile == a.give_up) { failed = true; break; }
       const ProdUnit u(a, t);
       const int m0 = u.m0 + (int)pipe.rank * PAIR_ROWS, n0 = u.n0 + (int)pipe.rank * (u.width / 2);
@@ -397,7 +490,7 @@ __global__ void __launch_bounds__(ProdPipe<sizeof(GT) / 2, CHAINED>::THREADS, 1)
       const uint64_t db0 = make_desc(pipe.b_of(0), PAIR_BOX, 1024);
       int s = 0;
       uint32_t ph = 0, it = 0;
-      for (int t = pair; t < a.total && !failed; t += pairs) {
+      for (int tile = 0, t; (t = walk(tile)) < a.total && !failed; ++tile) {
         const ProdUnit u(a, t);
         const uint32_t idesc = idesc0 | (u.users ? 0u : 1u << 15) | ((uint32_t)(u.width >> 3) << 17);
         const uint64_t da0 = u.users ? da_k : da_mn;
@@ -434,7 +527,7 @@ __global__ void __launch_bounds__(ProdPipe<sizeof(GT) / 2, CHAINED>::THREADS, 1)
     const int lane = pipe.lane, q = pipe.warp & 3, part = (pipe.warp - 2) >> 2;
     const uint32_t lane_addr = pipe.tmem + ((uint32_t)(q * 32) << 16);
     uint32_t it = 0;
-    for (int t = pair; t < a.total && !failed; t += pairs) {
+    for (int tile = 0, t; (t = walk(tile)) < a.total && !failed; ++tile) {
       const ProdUnit u(a, t);
       const int64_t m = u.m0 + (int)pipe.rank * PAIR_ROWS + q * 32 + lane;
       const int blocks = u.width / 32 / PARTS, col = part * blocks * 32;                // of 32 columns
@@ -531,30 +624,37 @@ struct LossPlan {
   int64_t ldg;
 };
 
-// blocks of 64 that the busiest pair works through in a piece, when dU's sums are cut in `splits`
-int64_t loss_span(int64_t units_u, int64_t cost_u, int64_t units_i, int64_t cost_i) {
+// How the units of a piece's products are dealt to the pairs (ProdWalk), and the blocks of 64 that the busiest one works through.
+struct LossSpan {
+  int64_t most;
+  int32_t extra;
+};
+LossSpan loss_span(int64_t units_u, int64_t cost_u, int64_t units_i, int64_t cost_i) {
   const bool users_first = cost_u >= cost_i;
-  const int64_t first = users_first ? units_u : units_i, total = units_u + units_i;
-  const int64_t c1 = users_first ? cost_u : cost_i, c2 = users_first ? cost_i : cost_u;
-  int64_t most = 0;
-  for (const int64_t p : {(int64_t)0, first % kPairs, total % kPairs}) {        // the loads change at these pairs
-    const int64_t of_first = first / kPairs + (p < first % kPairs), of_all = total / kPairs + (p < total % kPairs);
-    const int64_t load = of_first * c1 + (of_all - of_first) * c2;
-    if (load > most) most = load;
-  }
-  return most;
+  const int64_t n1 = users_first ? units_u : units_i, c1 = users_first ? cost_u : cost_i, n2 = users_first ? units_i : units_u;
+  const int64_t c2 = users_first ? cost_i : cost_u, pairs = n1 + n2 < kPairs ? n1 + n2 : kPairs;
+  const int64_t more = n1 % pairs, other = pairs - more;
+  int64_t extra = more ? c1 / c2 : 0;                   // rounded down: those pairs are dealt to first
+  if (extra > n2 / other) extra = n2 / other;
+  const int64_t rest = n2 - extra * other;
+  const int64_t load_other = (n1 / pairs) * c1 + (extra + rest / pairs + (rest % pairs > 0)) * c2;
+  const int64_t load_more = more ? (n1 / pairs + 1) * c1 + (rest / pairs + (rest % pairs > other)) * c2 : 0;
+  return LossSpan{load_other > load_more ? load_other : load_more, (int32_t)extra};
 }
 
-int loss_splits(int64_t N, int32_t cols, int32_t d, bool users, bool items) {
+// Parts that the sums of dU over a piece's items are cut into, so that the pairs are evenly busy.  A part costs its place in the sum: 8 N d
+// bytes, in blocks of 64 of a pair (0.37 us for each bf16 of g).
+int loss_splits(int64_t N, int32_t cols, int32_t d, int planes, bool users, bool items) {
   if (!users) return 0;
   const int64_t tiles_n = ceil_div(d, PAIR_COLS), kb_items = ceil_div(cols, 64), kb_users = ceil_div64(N, 64);
   const int64_t units_i = items ? ceil_div(cols, PAIR_COLS) * tiles_n : 0, tiles_u = ceil_div64(N, PAIR_COLS) * tiles_n;
+  const double part = 8.0 * N * d / (5e6 * 0.37 * planes);
   int best = 1;
-  int64_t least = INT64_MAX;
+  double least = 1e300;
   for (int s = 1; s <= 32 && s * 4 <= (kb_items > 4 ? kb_items : 4); ++s) {
-    const int64_t cost = ceil_div64(kb_items, s);
-    const int64_t span = loss_span(tiles_u * ceil_div64(kb_items, cost), cost, units_i, kb_users) + s / 2;      // a part costs its place in the sum
-    if (span < least) { least = span; best = (int)ceil_div64(kb_items, cost); }
+    const int64_t cost = ceil_div64(kb_items, s), parts = ceil_div64(kb_items, cost);
+    const double time = (double)loss_span(tiles_u * parts, cost, units_i, kb_users).most + (parts > 1 ? parts * part : 0.0);
+    if (time < least) { least = time; best = (int)parts; }
   }
   return best;
 }
@@ -580,7 +680,7 @@ LossPlan loss_plan(int64_t N, int32_t V, int32_t d, int planes, bool users, bool
   };
   auto with = [&](int32_t c) {
     const int32_t kb_items = ceil_div(c < V ? c : V, 64);
-    int s = loss_splits(N, c < V ? c : V, d, users, items);
+    int s = loss_splits(N, c < V ? c : V, d, planes, users, items);
     place(c, s);
     while (room && p.bytes > room && s > 1) place(c, s = ceil_div(kb_items, ceil_div(kb_items, s - 1)));      // as many as are not empty
   };
@@ -634,10 +734,16 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
   ask.logp = logp;
   ask.stats = (float*)stats;
   ask.C = 1;
-  GRAM_TRY(score_logprobs_launch(ctx, a.users, a.ld_users, a.items, a.ld_items, a.bias, a.N, a.V, a.d, a.scale, ask, score_ws, score_ws_bytes, st));
   RowConst* rows = grads ? (RowConst*)(base + p.rows) : nullptr;
   bf16* clean = a.ditems ? (bf16*)(base + p.clean) : nullptr;
-  {
+  // Few logits stay in the context's workspace, out of L2, in place of a second product for each piece.
+  const int64_t ldz = ((int64_t)a.V + 7) / 8 * 8;
+  const bool few = grads && a.N <= LOSS_FEW && (size_t)a.N * ldz * sizeof(float) <= (score_ws_bytes < (32u << 20) ? score_ws_bytes : 32u << 20);
+  if (few) {
+    GRAM_TRY(score_logits_launch(ctx, a.users, a.ld_users, a.items, a.ld_items, a.bias, a.N, a.V, a.d, (float*)score_ws, ldz, st));
+    GRAM_TRY(logprobs_launch(ctx, score_ws, GRAM_F32, ldz, a.N, a.V, a.scale, ask, st));
+  } else {
+    GRAM_TRY(score_logprobs_launch(ctx, a.users, a.ld_users, a.items, a.ld_items, a.bias, a.N, a.V, a.d, a.scale, ask, score_ws, score_ws_bytes, st));
     ProfScope prof(ctx, GRAM_K_OTHER, (double)a.N * (32 + (clean ? 4.0 * a.d : 0.0)), 1, st, "loss_rows");
     launch_chain(loss_rows_kernel, dim3((unsigned)ceil_div64(a.N, 8)), 256, 0, st, a, (const float*)logp, (const float2*)stats, rows, clean,
                  gram_status_word(ctx));
@@ -661,36 +767,43 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
   const int32_t pieces = ceil_div(a.V, p.cols);
   for (int32_t piece = 0; piece < pieces; ++piece) {
     const int32_t first = piece * p.cols, cols = a.V - first < p.cols ? a.V - first : p.cols;
-    GradArgs e = {};
-    e.rows = rows;
-    e.bias = a.bias;
-    e.N = a.N;
-    e.V = a.V;
-    e.first = first;
-    e.cols = cols;
-    e.num_kb = ceil_div(a.d, 64);
-    e.tiles_m = (int32_t)ceil_div64(a.N, 2 * PAIR_ROWS);
-    e.width = (int64_t)e.tiles_m * ceil_div(cols, PAIR_COLS) < kPairs ? PAIR_COLS / 2 : PAIR_COLS;      // tiles of half the width where they leave pairs idle
-    e.total = e.tiles_m * ceil_div(cols, e.width);
-    e.box_rows = box_rows;
-    e.c = a.scale * kLog2e;
-    e.g = g;
-    e.ldg = p.ldg;
-    e.plane = plane;
-    e.bias_part = a.dbias ? (float*)(base + p.bias) : nullptr;
-    e.give_up = gram_ring_rows(ctx);
-    e.status = gram_status_word(ctx);
-    {
-      ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * a.N * cols * a.d, 1, st, "loss_grad");
-      const int pairs = e.total < kPairs ? e.total : kPairs;
-      auto kern = planes == 2 ? loss_grad_kernel<2> : loss_grad_kernel<1>;
-      GRAM_CUDA(ctx, launch_pairs(kern, pairs, GradPipe::THREADS, GradPipe::SMEM, st, map_u, map_i, e));
-    }
-    if (a.dbias) {
-      ProfScope prof(ctx, GRAM_K_COLSUM, (double)a.N / 8 * cols, 1, st, "loss_bias");
-      launch_chain(loss_bias_kernel, dim3((unsigned)ceil_div(cols, 32)), 256, 0, st, (const float*)e.bias_part, p.ldg, (int32_t)ceil_div64(a.N, 32), cols,
-                   a.dbias + first);
+    if (few) {
+      const FewArgs e{(const float*)score_ws, ldz, logp, stats, first, cols, g, p.ldg, plane, clean, gram_status_word(ctx)};
+      ProfScope prof(ctx, GRAM_K_OTHER, (4.0 + 2 * planes) * a.N * cols, 1, st, "loss_few");
+      launch_chain(planes == 2 ? loss_few_kernel<2> : loss_few_kernel<1>, dim3((unsigned)ceil_div(cols, 128)), 256, 0, st, a, e);
       GRAM_LAUNCH_CHECK(ctx);
+    } else {
+      GradArgs e = {};
+      e.rows = rows;
+      e.bias = a.bias;
+      e.N = a.N;
+      e.V = a.V;
+      e.first = first;
+      e.cols = cols;
+      e.num_kb = ceil_div(a.d, 64);
+      e.tiles_m = (int32_t)ceil_div64(a.N, 2 * PAIR_ROWS);
+      e.width = (int64_t)e.tiles_m * ceil_div(cols, PAIR_COLS) < kPairs ? PAIR_COLS / 2 : PAIR_COLS;      // tiles of half the width where they leave pairs idle
+      e.total = e.tiles_m * ceil_div(cols, e.width);
+      e.box_rows = box_rows;
+      e.c = a.scale * kLog2e;
+      e.g = g;
+      e.ldg = p.ldg;
+      e.plane = plane;
+      e.bias_part = a.dbias ? (float*)(base + p.bias) : nullptr;
+      e.give_up = gram_ring_rows(ctx);
+      e.status = gram_status_word(ctx);
+      {
+        ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * a.N * cols * a.d, 1, st, "loss_grad");
+        const int pairs = e.total < kPairs ? e.total : kPairs;
+        auto kern = planes == 2 ? loss_grad_kernel<2> : loss_grad_kernel<1>;
+        GRAM_CUDA(ctx, launch_pairs(kern, pairs, GradPipe::THREADS, GradPipe::SMEM, st, map_u, map_i, e));
+      }
+      if (a.dbias) {
+        ProfScope prof(ctx, GRAM_K_COLSUM, (double)a.N / 8 * cols, 1, st, "loss_bias");
+        launch_chain(loss_bias_kernel, dim3((unsigned)ceil_div(cols, 32)), 256, 0, st, (const float*)e.bias_part, p.ldg, (int32_t)ceil_div64(a.N, 32), cols,
+                     a.dbias + first);
+        GRAM_LAUNCH_CHECK(ctx);
+      }
     }
     if (!a.dusers && !a.ditems) continue;
     for (int i = 0; i < 2; ++i)
@@ -714,6 +827,7 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
     w.units_u = w.users_m * w.tiles_n * w.splits;
     w.total = w.units_u + w.items_m * w.tiles_n;
     w.users_first = w.kb_split >= w.kb_users;
+    w.extra = loss_span(w.units_u, w.kb_split ? w.kb_split : 1, w.total - w.units_u, w.kb_users).extra;
     w.chain = LP_CHAIN;
     w.dI = a.ditems ? (uint8_t*)a.ditems + (size_t)first * a.ld_ditems * size : nullptr;
     w.ld_dI = a.ld_ditems;
@@ -722,8 +836,8 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
     w.add = piece > 0;
     w.wide_I = (uintptr_t)a.ditems % 32 == 0 && a.ld_ditems * size % 32 == 0;
     w.wide_U = w.direct ? (uintptr_t)a.dusers % 32 == 0 && a.ld_dusers * size % 32 == 0 : 1;
-    w.give_up = e.give_up;
-    w.status = e.status;
+    w.give_up = gram_ring_rows(ctx);
+    w.status = gram_status_word(ctx);
     ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * planes * a.N * cols * a.d * ((a.dusers != nullptr) + (a.ditems != nullptr)), 1, st, "loss_products");
     const int pairs = w.total < kPairs ? w.total : kPairs;
     const int longest = w.units_u && w.kb_split > w.kb_users ? w.kb_split : w.kb_users;
