@@ -415,11 +415,11 @@ gram_status gemm_i8_launch(gram_ctx* ctx, const int8_t* A, int64_t lda, const fl
   ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * M * N * K, 1, st, "gemm_i8");
   const int pairs = a.total < kPairs ? a.total : kPairs;
   if (rows) {
-    auto kern = c_dtype == GRAM_F32 ? gemm_i8_rows_kernel<float> : gemm_i8_rows_kernel<bf16>;
-    GRAM_CUDA(ctx, launch_pairs(kern, pairs, I8Rows::THREADS, I8Rows::SMEM, st, tokens, channels, result, a));
+    if (c_dtype == GRAM_F32) GRAM_CUDA(ctx, launch_pairs<gemm_i8_rows_kernel<float>>(pairs, I8Rows::THREADS, I8Rows::SMEM, st, tokens, channels, result, a));
+    else GRAM_CUDA(ctx, launch_pairs<gemm_i8_rows_kernel<bf16>>(pairs, I8Rows::THREADS, I8Rows::SMEM, st, tokens, channels, result, a));
   } else {
-    auto kern = c_dtype == GRAM_F32 ? gemm_i8_channels_kernel<float> : gemm_i8_channels_kernel<bf16>;
-    GRAM_CUDA(ctx, launch_pairs(kern, pairs, I8Channels::THREADS, I8Channels::SMEM, st, channels, tokens, a));
+    if (c_dtype == GRAM_F32) GRAM_CUDA(ctx, launch_pairs<gemm_i8_channels_kernel<float>>(pairs, I8Channels::THREADS, I8Channels::SMEM, st, channels, tokens, a));
+    else GRAM_CUDA(ctx, launch_pairs<gemm_i8_channels_kernel<bf16>>(pairs, I8Channels::THREADS, I8Channels::SMEM, st, channels, tokens, a));
   }
   return GRAM_OK;
 }

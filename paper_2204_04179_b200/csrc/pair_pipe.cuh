@@ -3,6 +3,8 @@
 // memory receives 128 rows of the result, two tiles in turn.  Warp 0 issues copies, warp 1 the MMAs, the others take results.
 // All waits are bounded; a role that gives up sets the block's flag and the context's status, and all end.
 #pragma once
+#include <atomic>
+
 #include "tc_common.cuh"
 
 namespace tc {
@@ -91,10 +93,21 @@ template <int STAGES_, int EPI_WARPS_, int EXTRA = 0, int A = 1> struct PairPipe
   }
 };
 
-// a launch of `pairs` clusters of two blocks; errors are left for the caller's GRAM_LAUNCH_CHECK
-template <typename... P, typename... A>
-inline cudaError_t launch_pairs(void (*kern)(P...), int pairs, int threads, int smem, cudaStream_t st, const A&... args) {
-  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+// The kernel's shared memory is asked for once on each device (of the first 64; then every time): the call takes as long as a launch.
+template <auto KERN> inline cudaError_t allow_smem(int smem) {
+  static std::atomic<uint64_t> done{0};
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = device < 64 ? (uint64_t)1 << device : 0;
+  if (bit && (done.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+  e = cudaFuncSetAttribute(KERN, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+// a launch of `pairs` clusters of two blocks
+template <auto KERN, typename... A> inline cudaError_t launch_pairs(int pairs, int threads, int smem, cudaStream_t st, const A&... args) {
+  const cudaError_t e = allow_smem<KERN>(smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(2 * pairs));
@@ -109,7 +122,7 @@ inline cudaError_t launch_pairs(void (*kern)(P...), int pairs, int threads, int 
   attr[1] = chain_attribute();
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kern, args...);
+  return cudaLaunchKernelEx(&cfg, KERN, args...);
 }
 
 }  // namespace tc

@@ -3,13 +3,14 @@
 // With z = U I^T + b, p the softmax of scale z and t the rows' targets, loss_n = log sum_v exp(scale z_nv) - scale z_n,t, and the
 // gradient of sum_n w_n loss_n with respect to z is g_nv = w_n scale (p_nv - [v = t_n]); then dU = g I, dI = g^T U, db_v = sum_n g_nv.
 //
-// g has as many entries as the logits, which are never kept: it is formed for a piece of the items at a time.
+// g has as many entries as the logits, which are never kept: it is formed for a piece at a time, some of the items and all users, or some of
+// the users and all items where users are more.
 //   1. The statistics of the rows (m and log s) come from the kernels of gram_score_logprobs: one product.
 //   2. loss_rows_kernel: the loss, and what a row's g needs, in one float4.
 //   3. Of each piece: loss_grad_kernel forms its logits again on the tensor cores and writes g to the workspace in bf16 (for fp32
-//      gradients as the sum of two bf16: 2^-16 of each entry); loss_products_kernel takes both products of it, dU += g I and dI = g^T U,
-//      in one launch of tiles of either kind.
-//   4. loss_finish_kernel: dU from its parts.
+//      gradients as the sum of two bf16: 2^-16 of each entry); loss_products_kernel takes both products of it, g I and g^T U, in one launch of tiles
+//      of either kind.  Where pieces are of items, those of g^T U are done with the piece and g I is summed over all; else the other way round.
+//   4. loss_finish_kernel: the summed gradient from its parts.
 // Bounded by the tensor cores where users are many: 8 N V d flops (12 with fp32 gradients), of which the products that cannot be done
 // without are 6; by the table's bytes, read three times and written once, where they are few.
 #include "score_loss.h"
@@ -73,16 +74,22 @@ __global__ void __launch_bounds__(256) loss_rows_kernel(const ScoreLoss a, const
 // p, and g of a row's entry
 __device__ __forceinline__ float loss_p(const RowConst& r, float z, float c) { return row_ex2(fminf(fmaf(z - r.m, c, -r.l), 0.f)); }
 
+// A piece: users [n0, n0 + rows) and items [first, first + cols), all of them or all of the others.
+struct Piece {
+  int64_t n0, rows;
+  int32_t first, cols;
+  bf16* g;                       // [planes, rows, ldg]
+  int64_t ldg, plane;            // elements between rows (a multiple of 256) and between planes
+};
+
 // Few users: g from logits that lie in L2, with the loss, the users' vectors and db, in one launch.  A block takes 128 columns, four a lane,
-// its warps the rows in turn; of the first piece it also takes the rows of its own number's residue.
+// its warps the rows in turn; where the piece is the row's first, the block also takes the rows of its own number's residue.
 struct FewArgs {
+  Piece at;
   const float* z;                // [N, ldz]
   int64_t ldz;
   const float* logp;
   const float2* stats;
-  int32_t first, cols;
-  bf16* g;                       // [planes, N, ldg]
-  int64_t ldg, plane;
   bf16* clean;                   // or null
   int32_t* status;
 };
@@ -90,28 +97,30 @@ template <int PLANES> __global__ void __launch_bounds__(256) loss_few_kernel(con
   if (!chain_begin()) return;
   __shared__ float4 sums[8][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 128 + 4 * lane;
-  if (f.first == 0)
-    for (int64_t n = blockIdx.x + (int64_t)warp * gridDim.x; n < a.N; n += 8 * (int64_t)gridDim.x) {
+  const Piece& at = f.at;
+  if (at.first == 0)
+    for (int64_t i = blockIdx.x + (int64_t)warp * gridDim.x; i < at.rows; i += 8 * (int64_t)gridDim.x) {
+      const int64_t n = at.n0 + i;
       if (lane == 0) a.loss[n] = loss_of(a, f.logp, n, f.status);
       if (f.clean) loss_clean(a, n, loss_row(a, f.logp, f.stats, n).t >= 0, f.clean);
     }
   const float c = a.scale * kLog2e;
   float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (col < f.cols) {
+  if (col < at.cols) {
 #pragma unroll 4
-    for (int64_t n = warp; n < a.N; n += 8) {
-      const float4 z = *reinterpret_cast<const float4*>(f.z + n * f.ldz + f.first + col);
-      const RowConst r = loss_row(a, f.logp, f.stats, n);
+    for (int64_t i = warp; i < at.rows; i += 8) {
+      const float4 z = *reinterpret_cast<const float4*>(f.z + (at.n0 + i) * f.ldz + at.first + col);
+      const RowConst r = loss_row(a, f.logp, f.stats, at.n0 + i);
       float g[4] = {loss_p(r, z.x, c), loss_p(r, z.y, c), loss_p(r, z.z, c), loss_p(r, z.w, c)};
-      const int hot = r.t - f.first - col;
+      const int hot = r.t - at.first - col;
 #pragma unroll
       for (int j = 0; j < 4; ++j) g[j] = r.t < 0 ? 0.f : r.f * (j == hot ? g[j] - 1.f : g[j]);
       const uint2 h = make_uint2(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]));
-      bf16* to = f.g + n * f.ldg + col;
+      bf16* to = at.g + i * at.ldg + col;
       *reinterpret_cast<uint2*>(to) = h;
       if constexpr (PLANES == 2) {
         const float2 u = unpack_bf16x2(h.x), v = unpack_bf16x2(h.y);
-        *reinterpret_cast<uint2*>(to + f.plane) = make_uint2(pack_bf16x2(g[0] - u.x, g[1] - u.y), pack_bf16x2(g[2] - v.x, g[3] - v.y));
+        *reinterpret_cast<uint2*>(to + at.plane) = make_uint2(pack_bf16x2(g[0] - u.x, g[1] - u.y), pack_bf16x2(g[2] - v.x, g[3] - v.y));
       }
       sum.x += g[0]; sum.y += g[1]; sum.z += g[2]; sum.w += g[3];
     }
@@ -125,11 +134,11 @@ template <int PLANES> __global__ void __launch_bounds__(256) loss_few_kernel(con
     const float4 x = sums[i][lane];
     sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
   }
-  float* to = a.dbias + f.first + col;
-  if (col < f.cols) to[0] = sum.x;
-  if (col + 1 < f.cols) to[1] = sum.y;
-  if (col + 2 < f.cols) to[2] = sum.z;
-  if (col + 3 < f.cols) to[3] = sum.w;
+  float* to = a.dbias + at.first + col;
+  const float all[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (col + j < at.cols) to[j] = at.n0 > 0 ? to[j] + all[j] : all[j];
 }
 
 // ============================================================================================
@@ -140,16 +149,14 @@ constexpr int LG_BIAS_BYTES = LG_EPI_WARPS * 64 * 4;    // a warp's columns
 using GradPipe = PairPipe<LG_STAGES, LG_EPI_WARPS, LG_BIAS_BYTES>;
 
 struct GradArgs {
-  const RowConst* rows;
+  Piece at;
+  const RowConst* rows;          // [N]
   const float* bias;             // [V] or null
-  int64_t N;
-  int32_t V, first, cols;        // of the table; the piece's first item and its columns (a multiple of 256, or up to the table's end)
+  int32_t V;
   int32_t num_kb, tiles_m, total, width;
   int32_t box_rows;              // users of a copy
   float c;
-  bf16* g;                       // [planes, N, ldg]
-  int64_t ldg, plane;            // elements between rows (a multiple of 256) and between planes
-  float* bias_part;              // [32-row blocks, ldg] or null
+  float* bias_part;              // [32-row blocks of the piece, ldg] or null
   int32_t give_up;
   int32_t* status;
 };
@@ -189,15 +196,15 @@ __global__ void __launch_bounds__(GradPipe::THREADS, 1) loss_grad_kernel(const _
     for (int t = pair; t < a.total && !failed; t += pairs, ++tile) {
       if (tile == a.give_up) { failed = true; break; }
       const int m0 = (t % a.tiles_m) * 2 * PAIR_ROWS + (int)pipe.rank * PAIR_ROWS;
-      const int n0 = a.first + (t / a.tiles_m) * a.width + (int)pipe.rank * (a.width / 2);
-      const bool some = m0 < a.N;                       // what the rows of users past the last hold is not looked at
+      const int n0 = a.at.first + (t / a.tiles_m) * a.width + (int)pipe.rank * (a.width / 2);
+      const bool some = m0 < a.at.rows;                 // what the rows of users past the last hold is not looked at
       const uint32_t bytes = (some ? (uint32_t)a.box_rows * 128u : 0u) + (uint32_t)a.width * 64u;
       for (int kb = 0; kb < a.num_kb; ++kb) {
         if (!mbar_wait_warp(pipe.empty(s), ph ^ 1u, pipe.abort_flag)) { failed = true; break; }
         const uint32_t bar = pipe.lead_full(s);
         if (elect_one()) {
           mbar_arrive_expect_tx_remote(bar, bytes);
-          if (some) tma_load_2d_pair(pipe.a_of(s), &users, kb * 64, m0, bar);
+          if (some) tma_load_2d_pair(pipe.a_of(s), &users, kb * 64, (int)a.at.n0 + m0, bar);
           tma_load_2d_pair(pipe.b_of(s), &items, kb * 64, n0, bar);
           if (a.width == PAIR_COLS) tma_load_2d_pair(pipe.b_of(s) + PAIR_BOX, &items, kb * 64, n0 + 64, bar);
         }
@@ -238,30 +245,33 @@ __global__ void __launch_bounds__(GradPipe::THREADS, 1) loss_grad_kernel(const _
     const int lane = pipe.lane, q = pipe.warp & 3, part = (pipe.warp - 2) >> 2;
     float* bias_w = reinterpret_cast<float*>(pipe.extra) + (pipe.warp - 2) * 64;
     const int blocks = a.width / PAIR_ROWS;             // of 32 columns of this warp
+    const f32x2 cc = x2_pack(a.c, a.c);
     uint32_t it = 0;
     for (int t = pair; t < a.total && !failed; t += pairs, ++it) {
       const int buf = (int)(it & 1);
       const int col_t = part * blocks * 32, col0 = (t / a.tiles_m) * a.width + col_t;      // of the tile, of the piece
-      const int64_t n = (int64_t)(t % a.tiles_m) * 2 * PAIR_ROWS + (int)pipe.rank * PAIR_ROWS + q * 32 + lane;
-      const bool active = n - lane < a.N;               // of the warp
+      const int64_t n = (int64_t)(t % a.tiles_m) * 2 * PAIR_ROWS + (int)pipe.rank * PAIR_ROWS + q * 32 + lane;      // of the piece
+      const bool active = n - lane < a.at.rows;         // of the warp
       RowConst r{0.f, 0.f, 0.f, -1};
       const float* bias = nullptr;
       if (active) {
-        if (n < a.N) {
-          const float4 f = __ldg(reinterpret_cast<const float4*>(a.rows) + n);
+        if (n < a.at.rows) {
+          const float4 f = __ldg(reinterpret_cast<const float4*>(a.rows) + a.at.n0 + n);
           r = RowConst{f.x, f.y, f.z, __float_as_int(f.w)};
         }
-        if (a.bias || a.first + col0 + blocks * 32 > a.V) {        // columns past the table count as masked out
+        if (a.bias || a.at.first + col0 + blocks * 32 > a.V) {     // columns past the table count as masked out
           __syncwarp();
           for (int b = 0; b < blocks; ++b) {
-            const int v = a.first + col0 + b * 32 + lane;
+            const int v = a.at.first + col0 + b * 32 + lane;
             bias_w[b * 32 + lane] = v >= a.V ? ROW_NEG_INF : a.bias ? __ldg(a.bias + v) : 0.f;
           }
           __syncwarp();
           bias = bias_w;
         }
       }
-      const int hot = r.t - a.first - col0;             // the target's place among the warp's columns
+      const int hot = r.t - a.at.first - col0;          // the target's place among the warp's columns
+      const f32x2 m2 = x2_pack(-r.m, -r.m), l2 = x2_pack(-r.l, -r.l), f2 = x2_pack(r.f, r.f);
+      const bool hold = __any_sync(0xffffffffu, row_is_huge(r.m, a.c));
       if (!mbar_wait_warp(pipe.tfull(buf), (it >> 1) & 1, pipe.abort_flag)) { failed = true; break; }
       tc_fence_after();
       if (active) {
@@ -270,22 +280,46 @@ __global__ void __launch_bounds__(GradPipe::THREADS, 1) loss_grad_kernel(const _
           uint32_t v[32];
           tc_ld32_issue(taddr + b * 32, v);
           tc_ld32_wait(v);
+          if (bias) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+              const float4 f = *reinterpret_cast<const float4*>(bias + b * 32 + j);
+              v[j] = __float_as_uint(__uint_as_float(v[j]) + f.x);
+              v[j + 1] = __float_as_uint(__uint_as_float(v[j + 1]) + f.y);
+              v[j + 2] = __float_as_uint(__uint_as_float(v[j + 2]) + f.z);
+              v[j + 3] = __float_as_uint(__uint_as_float(v[j + 3]) + f.w);
+            }
+          }
           float g[32];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            float z = __uint_as_float(v[j]);
-            if (bias) z += bias[b * 32 + j];
-            g[j] = loss_p(r, z, a.c);
+          for (int j = 0; j < 32; j += 2) {
+            const float2 y = x2_unpack(x2_fma(x2_add(x2_pack(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), m2), cc, l2));
+            g[j] = y.x;
+            g[j + 1] = y.y;
           }
+          if (hold) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) g[j] = fminf(g[j], 0.f);
+          }
+#pragma unroll
+          for (int j = 0; j < 32; ++j) g[j] = row_ex2(g[j]);
           if (r.t >= 0 && (unsigned)(hot - b * 32) < 32u) {
 #pragma unroll
             for (int j = 0; j < 32; ++j)
               if (j == hot - b * 32) g[j] -= 1.f;
           }
 #pragma unroll
-          for (int j = 0; j < 32; ++j) g[j] = r.t >= 0 ? g[j] * r.f : 0.f;
-          if (n < a.N) {
-            bf16* to = a.g + n * a.ldg + col0 + b * 32;
+          for (int j = 0; j < 32; j += 2) {
+            const float2 x = x2_unpack(x2_mul(x2_pack(g[j], g[j + 1]), f2));
+            g[j] = x.x;
+            g[j + 1] = x.y;
+          }
+          if (__any_sync(0xffffffffu, r.t < 0)) {       // rows that take no part
+#pragma unroll
+            for (int j = 0; j < 32; ++j) g[j] = r.t < 0 ? 0.f : g[j];
+          }
+          if (n < a.at.rows) {
+            bf16* to = a.at.g + n * a.at.ldg + col0 + b * 32;
             uint32_t h[16];
 #pragma unroll
             for (int j = 0; j < 16; ++j) h[j] = pack_bf16x2(g[2 * j], g[2 * j + 1]);
@@ -297,11 +331,11 @@ __global__ void __launch_bounds__(GradPipe::THREADS, 1) loss_grad_kernel(const _
                 const float2 f = unpack_bf16x2(h[j]);
                 h[j] = pack_bf16x2(g[2 * j] - f.x, g[2 * j + 1] - f.y);
               }
-              st32(to + a.plane, h);
-              st32(to + a.plane + 16, h + 8);
+              st32(to + a.at.plane, h);
+              st32(to + a.at.plane + 16, h + 8);
             }
           }
-          if (a.bias_part) a.bias_part[(n >> 5) * a.ldg + col0 + b * 32 + lane] = column_sums(g);
+          if (a.bias_part) a.bias_part[(n >> 5) * a.at.ldg + col0 + b * 32 + lane] = column_sums(g);
         }
       }
       tc_fence_before();
@@ -313,18 +347,19 @@ __global__ void __launch_bounds__(GradPipe::THREADS, 1) loss_grad_kernel(const _
 }
 
 // db of a piece: the sum of its 32-row blocks, eight groups of them side by side
-__global__ void __launch_bounds__(256) loss_bias_kernel(const float* part, int64_t ldg, int32_t blocks, int32_t cols, float* dbias) {
+__global__ void __launch_bounds__(256) loss_bias_kernel(const float* part, int64_t ldg, int64_t blocks, int32_t cols, int32_t add, float* dbias) {
   if (!chain_begin()) return;
   __shared__ float sums[8][32];
   const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, v = blockIdx.x * 32 + lane;
   float s = 0.f;
-  for (int i = group; i < blocks; i += 8) s += part[i * ldg + v];          // the rows reach past the last column
+#pragma unroll 8
+  for (int64_t i = group; i < blocks; i += 8) s += part[i * ldg + v];      // the rows reach past the last column
   sums[group][lane] = s;
   __syncthreads();
   if (group != 0 || v >= cols) return;
 #pragma unroll
   for (int i = 1; i < 8; ++i) s += sums[i][lane];
-  dbias[v] = s;
+  dbias[v] = add ? dbias[v] + s : s;
 }
 
 // ============================================================================================
@@ -337,22 +372,24 @@ template <int PLANES, bool CHAINED> using ProdPipe = PairPipe<PLANES == 2 ? 4 : 
 // Blocks of 64 whose products (of both planes) are added up in one accumulator for fp32 gradients.  bf16 results hide the error of any length.
 constexpr int LP_CHAIN = 24;
 
+// One gradient's share in a piece.
+struct ProdSide {
+  int32_t tiles_m, rows;         // tiles of 256 of the piece's rows (0: not asked)
+  int32_t kb, kb_split;          // blocks of 64 that the sums run over, and those of a part
+  int32_t vec0;                  // the first of the vectors that they run over
+  int32_t units, cost;           // tiles of all parts; what one costs, in blocks
+  void* out;                     // of the piece's rows: the result, or
+  int32_t partial;               // fp32 sums [parts, rows, d] that are joined later
+  int32_t add;                   // to what is there (partial)
+  int32_t wide;                  // rows begin on 32 bytes
+  int64_t ld, part;              // elements between rows and between parts
+};
 struct ProdArgs {
-  int64_t N;
-  int32_t cols, first, d;        // the piece's columns, its first item
-  int32_t tiles_n;               // tiles of 256 columns of d
-  int32_t items_m;               // tiles of 256 items (0: dI is not asked)
-  int32_t users_m, splits;       // tiles of 256 users (0: dU is not asked); parts of the piece's items that a unit of dU sums over
-  int32_t kb_users, kb_items, kb_split;      // blocks of 64 users, of 64 items, of a part's items
-  int32_t units_u, total, users_first;       // units of dU, of both; whether those of dU are the heavier ones, which are dealt first
+  ProdSide of[2];                // users' and items' gradient
+  int32_t d, tiles_n;            // tiles of 256 columns of d
+  int32_t total, heavy;          // units of both; whose are the heavier ones, which are dealt first
   int32_t extra;                 // lighter units that a pair gets for each heavier one that others have more
   int32_t chain;                 // blocks that are added up in one accumulator
-  void* dI;                      // rows of the piece's items
-  int64_t ld_dI;
-  void* dU;                      // direct: the result; else fp32 [splits, N, d]
-  int64_t ld_dU;
-  int32_t direct, add;           // add: to what is there (not direct)
-  int32_t wide_I, wide_U;        // rows begin on 32 bytes
   int32_t give_up;
   int32_t* status;
 };
@@ -362,7 +399,7 @@ struct ProdArgs {
 struct ProdWalk {
   int pair, pairs, heavy, mine, extra, other, base, at, total;
   __device__ __forceinline__ explicit ProdWalk(const ProdArgs& a) : pair(blockIdx.x >> 1), pairs(gridDim.x >> 1), total(a.total) {
-    heavy = a.users_first ? a.units_u : a.total - a.units_u;
+    heavy = a.of[a.heavy].units;
     const int more = heavy % pairs;                     // pairs with one more
     mine = heavy / pairs + (pair < more);
     other = pairs - more;
@@ -378,27 +415,23 @@ struct ProdWalk {
   }
 };
 
-// A unit: a tile of dI over all users, or a tile of dU over a part of the piece's items.
+// A unit: a tile of one of the gradients over a part of its sums.
 struct ProdUnit {
-  bool users;
-  int m0, n0, width, split, k0, blocks;      // first row and column; the sum's range in blocks of 64
+  int side, m0, n0, width, split, k0, blocks;           // first row and column; the sum's range in blocks of 64
   __device__ __forceinline__ ProdUnit(const ProdArgs& a, int t) {
-    users = a.users_first ? t < a.units_u : t >= a.total - a.units_u;
-    if (a.users_first ? !users : users) t -= a.users_first ? a.units_u : a.total - a.units_u;
-    const int tn = t % a.tiles_n, r = t / a.tiles_n;
-    n0 = tn * PAIR_COLS;
-    width = a.d - n0 > PAIR_COLS / 2 ? PAIR_COLS : PAIR_COLS / 2;
-    if (users) {
-      split = r / a.users_m;
-      m0 = (r - split * a.users_m) * 2 * PAIR_ROWS;
-      k0 = split * a.kb_split;
-      blocks = min(a.kb_split, a.kb_items - k0);
-    } else {
-      split = 0;
-      m0 = r * 2 * PAIR_ROWS;
-      k0 = 0;
-      blocks = a.kb_users;
+    side = a.heavy;
+    if (t >= a.of[side].units) {
+      t -= a.of[side].units;
+      side ^= 1;
     }
+    const ProdSide& o = a.of[side];
+    const int r = t / a.tiles_n;
+    n0 = (t - r * a.tiles_n) * PAIR_COLS;
+    width = a.d - n0 > PAIR_COLS / 2 ? PAIR_COLS : PAIR_COLS / 2;
+    split = r / o.tiles_m;
+    m0 = (r - split * o.tiles_m) * 2 * PAIR_ROWS;
+    k0 = split * o.kb_split;
+    blocks = min(o.kb_split, o.kb - k0);
   }
 };
 
@@ -460,9 +493,11 @@ __global__ void __launch_bounds__(ProdPipe<sizeof(GT) / 2, CHAINED>::THREADS, 1)
       const ProdUnit u(a, t);
       const int m0 = u.m0 + (int)pipe.rank * PAIR_ROWS, n0 = u.n0 + (int)pipe.rank * (u.width / 2);
       const uint32_t bytes = PLANES * 2 * PAIR_BOX + (uint32_t)(u.width / PAIR_ROWS) * PAIR_BOX;
-      const CUtensorMap* vectors = u.users ? &items : &users;
+      const bool of_users = u.side == 0;                 // its rows are g's rows
+      const CUtensorMap* vectors = of_users ? &items : &users;
+      const int vec0 = a.of[u.side].vec0;
       for (int kb = 0; kb < u.blocks; ++kb) {
-        const int k = (u.k0 + kb) * 64, row = (u.users ? a.first : 0) + k;
+        const int k = (u.k0 + kb) * 64, row = vec0 + k;
         if (!mbar_wait_warp(pipe.empty(s), ph ^ 1u, pipe.abort_flag)) { failed = true; break; }
         const uint32_t bar = pipe.lead_full(s), sb = pipe.b_of(s);
         if (elect_one()) {
@@ -471,8 +506,8 @@ __global__ void __launch_bounds__(ProdPipe<sizeof(GT) / 2, CHAINED>::THREADS, 1)
           for (int i = 0; i < PLANES; ++i) {
             const CUtensorMap* g = i ? &g1 : &g0;
             const uint32_t sa = pipe.a_of(s, i);
-            tma_load_2d_pair(sa, g, u.users ? k : m0, u.users ? m0 : k, bar);
-            tma_load_2d_pair(sa + PAIR_BOX, g, u.users ? k : m0 + 64, u.users ? m0 + 64 : k, bar);
+            tma_load_2d_pair(sa, g, of_users ? k : m0, of_users ? m0 : k, bar);
+            tma_load_2d_pair(sa + PAIR_BOX, g, of_users ? k : m0 + 64, of_users ? m0 + 64 : k, bar);
           }
           tma_load_2d_pair(sb, vectors, n0, row, bar);
           if (u.width == PAIR_COLS) tma_load_2d_pair(sb + PAIR_BOX, vectors, n0 + 64, row, bar);
@@ -492,9 +527,9 @@ __global__ void __launch_bounds__(ProdPipe<sizeof(GT) / 2, CHAINED>::THREADS, 1)
       uint32_t ph = 0, it = 0;
       for (int tile = 0, t; (t = walk(tile)) < a.total && !failed; ++tile) {
         const ProdUnit u(a, t);
-        const uint32_t idesc = idesc0 | (u.users ? 0u : 1u << 15) | ((uint32_t)(u.width >> 3) << 17);
-        const uint64_t da0 = u.users ? da_k : da_mn;
-        const uint32_t step_a = (u.users ? 32u : 2048u) >> 4;
+        const uint32_t idesc = idesc0 | (u.side == 0 ? 0u : 1u << 15) | ((uint32_t)(u.width >> 3) << 17);
+        const uint64_t da0 = u.side == 0 ? da_k : da_mn;
+        const uint32_t step_a = (u.side == 0 ? 32u : 2048u) >> 4;
         const int chain = CHAINED ? a.chain : u.blocks;
         for (int c0 = 0; c0 < u.blocks && !failed; c0 += chain, ++it) {            // an accumulator each
           const int c1 = min(c0 + chain, u.blocks), buf = (int)(it & 1);
@@ -529,15 +564,14 @@ __global__ void __launch_bounds__(ProdPipe<sizeof(GT) / 2, CHAINED>::THREADS, 1)
     uint32_t it = 0;
     for (int tile = 0, t; (t = walk(tile)) < a.total && !failed; ++tile) {
       const ProdUnit u(a, t);
-      const int64_t m = u.m0 + (int)pipe.rank * PAIR_ROWS + q * 32 + lane;
+      const ProdSide& o = a.of[u.side];
+      const int m = u.m0 + (int)pipe.rank * PAIR_ROWS + q * 32 + lane;
       const int blocks = u.width / 32 / PARTS, col = part * blocks * 32;                // of 32 columns
-      const bool there = m < (u.users ? a.N : (int64_t)a.cols);
       auto put = [&](int b, const float (&x)[32]) {
         const int n = u.n0 + col + b * 32, some = a.d - n;
-        if (!there || some <= 0) return;
-        if (!u.users) put_row(reinterpret_cast<GT*>(a.dI) + m * a.ld_dI + n, x, some, a.wide_I, false);
-        else if (a.direct) put_row(reinterpret_cast<GT*>(a.dU) + m * a.ld_dU + n, x, some, a.wide_U, false);
-        else put_row(reinterpret_cast<float*>(a.dU) + ((int64_t)u.split * a.N + m) * a.d + n, x, some, a.wide_U, a.add);
+        if (m >= o.rows || some <= 0) return;
+        if (o.partial) put_row(reinterpret_cast<float*>(o.out) + u.split * o.part + m * o.ld + n, x, some, o.wide, o.add);
+        else put_row(reinterpret_cast<GT*>(o.out) + m * o.ld + n, x, some, o.wide, false);
       };
       if constexpr (CHAINED) {
         // The tensor cores cut off where this adds with rounding: a chain's length sets the sum's precision.
@@ -595,19 +629,19 @@ __global__ void __launch_bounds__(ProdPipe<sizeof(GT) / 2, CHAINED>::THREADS, 1)
   pipe.close(failed, a.status);
 }
 
-// dU as the sum of its parts
-template <typename GT> __global__ void __launch_bounds__(256) loss_finish_kernel(const float* parts, int splits, int64_t N, int32_t d, GT* dU, int64_t ld) {
+// a gradient [N, d] as the sum of its parts
+template <typename GT> __global__ void __launch_bounds__(256) loss_finish_kernel(const float* parts, int splits, int64_t N, int32_t d, GT* grad, int64_t ld) {
   if (!chain_begin()) return;
   const int64_t n4 = N * (d / 4);
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n4; i += (int64_t)gridDim.x * 256) {
     float4 s = reinterpret_cast<const float4*>(parts)[i];
-#pragma unroll 4
+#pragma unroll 8
     for (int k = 1; k < splits; ++k) {
       const float4 x = reinterpret_cast<const float4*>(parts)[k * n4 + i];
       s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
     }
     const int64_t n = i / (d / 4);
-    GT* to = dU + n * ld + 4 * (i - n * (d / 4));
+    GT* to = grad + n * ld + 4 * (i - n * (d / 4));
     if constexpr (sizeof(GT) == 4) *reinterpret_cast<float4*>(to) = s;
     else *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w));
   }
@@ -620,109 +654,117 @@ size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
 struct LossPlan {
   size_t logp, stats, rows, clean, parts, bias, g, bytes;       // places in the workspace
-  int32_t cols, splits;                                         // of a piece; parts of dU
+  bool cut_users;                                               // pieces are of users, else of items
+  int32_t step, splits;                                         // users or items of a piece; parts of the summed gradient
   int64_t ldg;
 };
 
-// How the units of a piece's products are dealt to the pairs (ProdWalk), and the blocks of 64 that the busiest one works through.
+// What a unit over `kb` blocks costs, in blocks of a pair (0.37 us): the products of all planes, or the way of 256 x 256 results out where that takes longer.
+int64_t loss_cost(int64_t kb, int planes, bool f32) {
+  const int64_t out = f32 ? 13 : 7;
+  return kb * planes > out ? kb * planes : out;
+}
+
+// How the units of a piece's products are dealt to the pairs (ProdWalk), and the blocks that the busiest one works through.
 struct LossSpan {
   int64_t most;
-  int32_t extra;
+  int32_t heavy, extra;          // whether the second kind is the heavier one
 };
-LossSpan loss_span(int64_t units_u, int64_t cost_u, int64_t units_i, int64_t cost_i) {
-  const bool users_first = cost_u >= cost_i;
-  const int64_t n1 = users_first ? units_u : units_i, c1 = users_first ? cost_u : cost_i, n2 = users_first ? units_i : units_u;
-  const int64_t c2 = users_first ? cost_i : cost_u, pairs = n1 + n2 < kPairs ? n1 + n2 : kPairs;
+LossSpan loss_span(int64_t units_a, int64_t cost_a, int64_t units_b, int64_t cost_b) {
+  const bool second = units_a == 0 || (units_b > 0 && cost_b > cost_a);
+  const int64_t n1 = second ? units_b : units_a, c1 = second ? cost_b : cost_a, n2 = second ? units_a : units_b;
+  const int64_t c2 = second ? cost_a : cost_b, pairs = n1 + n2 < kPairs ? n1 + n2 : kPairs;
   const int64_t more = n1 % pairs, other = pairs - more;
   int64_t extra = more ? c1 / c2 : 0;                   // rounded down: those pairs are dealt to first
   if (extra > n2 / other) extra = n2 / other;
   const int64_t rest = n2 - extra * other;
   const int64_t load_other = (n1 / pairs) * c1 + (extra + rest / pairs + (rest % pairs > 0)) * c2;
   const int64_t load_more = more ? (n1 / pairs + 1) * c1 + (rest / pairs + (rest % pairs > other)) * c2 : 0;
-  return LossSpan{load_other > load_more ? load_other : load_more, (int32_t)extra};
+  return LossSpan{load_other > load_more ? load_other : load_more, (int32_t)second, (int32_t)extra};
 }
 
-// Parts that the sums of dU over a piece's items are cut into, so that the pairs are evenly busy.  A part costs its place in the sum: 8 N d
-// bytes, in blocks of 64 of a pair (0.37 us for each bf16 of g).
-int loss_splits(int64_t N, int32_t cols, int32_t d, int planes, bool users, bool items) {
-  if (!users) return 0;
-  const int64_t tiles_n = ceil_div(d, PAIR_COLS), kb_items = ceil_div(cols, 64), kb_users = ceil_div64(N, 64);
-  const int64_t units_i = items ? ceil_div(cols, PAIR_COLS) * tiles_n : 0, tiles_u = ceil_div64(N, PAIR_COLS) * tiles_n;
-  const double part = 8.0 * N * d / (5e6 * 0.37 * planes);
+// Parts that the summed gradient's sums over a piece are cut into, so that the pairs are evenly busy.  `step` rows of the piece's own
+// gradient, `all` of the summed one.  A part costs its place in the sum: 8 `all` d bytes, in blocks.
+int loss_splits(int64_t step, int64_t all, int32_t d, int planes, bool own, bool summed) {
+  if (!summed) return 0;
+  const int64_t tiles_n = ceil_div(d, PAIR_COLS), kb = ceil_div64(step, 64);
+  const int64_t units_own = own ? ceil_div64(step, PAIR_COLS) * tiles_n : 0, tiles = ceil_div64(all, PAIR_COLS) * tiles_n;
+  const int64_t cost_own = loss_cost(ceil_div64(all, 64), planes, planes == 2);
+  const double part = 8.0 * all * d / (5e6 * 0.37);
   int best = 1;
   double least = 1e300;
-  for (int s = 1; s <= 32 && s * 4 <= (kb_items > 4 ? kb_items : 4); ++s) {
-    const int64_t cost = ceil_div64(kb_items, s), parts = ceil_div64(kb_items, cost);
-    const double time = (double)loss_span(tiles_u * parts, cost, units_i, kb_users).most + (parts > 1 ? parts * part : 0.0);
+  for (int s = 1; s <= 32 && s * 4 <= (kb > 4 ? kb : 4); ++s) {
+    const int64_t of = ceil_div64(kb, s), parts = ceil_div64(kb, of);
+    const double time = (double)loss_span(tiles * parts, loss_cost(of, planes, true), units_own, cost_own).most + (parts > 1 ? parts * part : 0.0);
     if (time < least) { least = time; best = (int)parts; }
   }
   return best;
 }
 
-// Lays out a workspace of `room` bytes (0: of `cols` columns a piece).
-LossPlan loss_plan(int64_t N, int32_t V, int32_t d, int planes, bool users, bool items, bool bias, int32_t cols, size_t room) {
+// Lays out a workspace of `room` bytes, or the one of pieces of `step`.
+LossPlan loss_plan(int64_t N, int32_t V, int32_t d, int planes, bool users, bool items, bool bias, int64_t step, size_t room) {
   LossPlan p = {};
-  const int32_t all = (int32_t)(((int64_t)V + 255) / 256 * 256 < INT32_MAX / 256 * 256 ? ((int64_t)V + 255) / 256 * 256 : INT32_MAX / 256 * 256);
-  auto place = [&](int32_t c, int splits) {
+  p.cut_users = N > V;
+  const int64_t axis = p.cut_users ? N : V, all = p.cut_users ? V : N, all_up = (all + 255) / 256 * 256;
+  const bool own = p.cut_users ? users : items, summed = p.cut_users ? items : users;
+  const int64_t most = (axis + 255) / 256 * 256 < INT32_MAX / 256 * 256 ? (axis + 255) / 256 * 256 : INT32_MAX / 256 * 256;
+  auto place = [&](int64_t c, int splits) {
     size_t at = 0;
     auto take = [&](size_t n) { const size_t was = at; at += up(n); return was; };
+    const int64_t rows = p.cut_users ? c : N;
+    p.ldg = p.cut_users ? all_up : c;
     p.logp = take((size_t)N * 4);
     p.stats = take((size_t)N * 8);
     p.rows = take((size_t)N * sizeof(RowConst));
     p.clean = take(items ? (size_t)N * d * 2 : 0);
-    p.parts = take((size_t)splits * N * d * 4);
-    p.bias = take(bias ? (size_t)ceil_div64(N, 32) * c * 4 : 0);
-    p.g = take((size_t)planes * N * c * 2);
+    p.parts = take((size_t)splits * all * d * 4);
+    p.bias = take(bias ? (size_t)ceil_div64(rows, 32) * p.ldg * 4 : 0);
+    p.g = take((size_t)planes * rows * p.ldg * 2);
     p.bytes = at;
-    p.cols = c;
-    p.ldg = c;
+    p.step = (int32_t)c;
     p.splits = splits;
   };
-  auto with = [&](int32_t c) {
-    const int32_t kb_items = ceil_div(c < V ? c : V, 64);
-    int s = loss_splits(N, c < V ? c : V, d, planes, users, items);
+  auto with = [&](int64_t c) {
+    const int64_t real = c < axis ? c : axis;
+    const int kb = (int)ceil_div64(real, 64);
+    int s = loss_splits(real, all, d, planes, own, summed);
     place(c, s);
-    while (room && p.bytes > room && s > 1) place(c, s = ceil_div(kb_items, ceil_div(kb_items, s - 1)));      // as many as are not empty
+    while (room && p.bytes > room && s > 1) place(c, s = ceil_div(kb, ceil_div(kb, s - 1)));      // as many as are not empty
   };
   if (!room) {
-    with(cols < all ? cols : all);
+    with(step < most ? step : most);
     return p;
   }
-  const size_t per = (size_t)planes * N * 2 + (bias ? (size_t)ceil_div64(N, 32) * 4 : 0);
-  place(0, 0);
-  int64_t c = room > p.bytes ? (int64_t)((room - p.bytes) / per) / 256 * 256 : 0;
-  if (c > all) c = all;
+  place(0, summed ? 1 : 0);
+  const size_t per = (size_t)planes * (p.cut_users ? all_up : N) * 2 * 256 + (bias ? (p.cut_users ? (size_t)all_up * 32 : (size_t)ceil_div64(N, 32) * 1024) : 0);
+  int64_t c = room > p.bytes ? (int64_t)((room - p.bytes) / per) * 256 : 0;
+  if (c > most) c = most;
   if (c < 256) c = 256;
-  // pieces of about equal size
-  const int64_t pieces = ceil_div64(V, c);
-  c = ceil_div64(ceil_div64(V, pieces), 256) * 256;
-  with((int32_t)c);
-  while (p.bytes > room && p.cols > 256) with(p.cols - 256);
+  c = ceil_div64(ceil_div64(axis, ceil_div64(axis, c)), 256) * 256;          // pieces of about equal size
+  with(c);
+  while (p.bytes > room && p.step > 256) with(p.step - 256);
   return p;
 }
 
-constexpr int64_t kGoodG = (int64_t)192 << 20;            // bytes of a piece's g
+constexpr int64_t kGoodG = (int64_t)256 << 20;            // bytes of a piece's g
 
 }  // namespace
 
 void score_loss_workspace(int64_t N, int32_t V, int32_t d, int grad_dtype, size_t* least, size_t* best) {
   const int planes = grad_dtype == GRAM_F32 ? 2 : 1;
-  const int64_t n = N > 0 ? N : 1;
+  const int64_t n = N > 0 ? N : 1, all = n > V ? (int64_t)V : n;
   LossPlan p = loss_plan(n, V, d, planes, true, true, true, 256, 0);
-  // the least: one part of dU
-  const size_t parts = up((size_t)p.splits * n * d * 4), one = up((size_t)n * d * 4);
-  *least = p.bytes - parts + one;
-  int64_t cols = kGoodG / (2 * planes * n) / 256 * 256;
-  if (cols < 256) cols = 256;
-  if (cols > INT32_MAX / 2) cols = INT32_MAX / 2 / 256 * 256;
-  p = loss_plan(n, V, d, planes, true, true, true, (int32_t)cols, 0);
+  *least = p.bytes - up((size_t)p.splits * all * d * 4) + up((size_t)all * d * 4);      // with one part of the summed gradient
+  int64_t step = kGoodG / (2 * planes * ((all + 255) / 256 * 256)) / 256 * 256;
+  if (step < 256) step = 256;
+  p = loss_plan(n, V, d, planes, true, true, true, step, 0);
   *best = p.bytes > *least ? p.bytes : *least;
 }
 
 gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_t ws_bytes, void* score_ws, size_t score_ws_bytes, cudaStream_t st) {
   const bool grads = a.dusers || a.ditems || a.dbias;
   const int planes = a.grad_dtype == GRAM_F32 ? 2 : 1;
-  LossPlan p = loss_plan(a.N, a.V, a.d, planes, a.dusers != nullptr, a.ditems != nullptr, a.dbias != nullptr, 0, ws_bytes ? ws_bytes : 1);
+  const LossPlan p = loss_plan(a.N, a.V, a.d, planes, a.dusers != nullptr, a.ditems != nullptr, a.dbias != nullptr, 0, ws_bytes ? ws_bytes : 1);
   const size_t need = grads ? p.bytes : p.rows;
   if (need > ws_bytes)
     return gram_set_error(ctx, "gram_score_loss: a workspace of %zu bytes is needed, not %zu", need, ws_bytes), GRAM_ERR_WORKSPACE;
@@ -752,110 +794,116 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
   if (!grads) return GRAM_OK;
 
   const char* what = "gram_score_loss: cannot describe the vectors";
-  CUtensorMap map_u, map_i, map_clean, map_items, map_g[2];
+  CUtensorMap map_u, map_i, map_clean, map_g[2];
   int box_rows = PAIR_ROWS;                              // copies are no larger than the users
   while (box_rows > 8 && box_rows / 2 >= a.N) box_rows /= 2;
-  if (!make_map(&map_u, a.users, (uint64_t)a.d, (uint64_t)a.N, (uint64_t)a.ld_users, 64, (uint32_t)box_rows) ||
+  if ((!few && !make_map(&map_u, a.users, (uint64_t)a.d, (uint64_t)a.N, (uint64_t)a.ld_users, 64, (uint32_t)box_rows)) ||
       !make_map(&map_i, a.items, (uint64_t)a.d, (uint64_t)a.V, (uint64_t)a.ld_items, 64, 64))
     return gram_set_error(ctx, what), GRAM_ERR_UNSUPPORTED;
-  map_items = map_i;
   map_clean = map_i;
   if (clean && !make_map(&map_clean, clean, (uint64_t)a.d, (uint64_t)a.N, (uint64_t)a.d, 64, 64)) return gram_set_error(ctx, what), GRAM_ERR_UNSUPPORTED;
 
-  bf16* g = (bf16*)(base + p.g);
-  const int64_t plane = a.N * p.ldg;
-  const int32_t pieces = ceil_div(a.V, p.cols);
-  for (int32_t piece = 0; piece < pieces; ++piece) {
-    const int32_t first = piece * p.cols, cols = a.V - first < p.cols ? a.V - first : p.cols;
+  const int64_t axis = p.cut_users ? a.N : a.V, pieces = ceil_div64(axis, p.step);
+  const int own = p.cut_users ? 0 : 1;                   // whose gradient is done with the piece
+  const bool joined = p.splits > 0 && (p.splits > 1 || pieces > 1);
+  for (int64_t i = 0; i < pieces; ++i) {
+    const int64_t at = i * p.step, now = axis - at < p.step ? axis - at : p.step;
+    Piece e;
+    e.n0 = p.cut_users ? at : 0;
+    e.rows = p.cut_users ? now : a.N;
+    e.first = p.cut_users ? 0 : (int32_t)at;
+    e.cols = p.cut_users ? a.V : (int32_t)now;
+    e.g = (bf16*)(base + p.g);
+    e.ldg = p.ldg;
+    e.plane = e.rows * p.ldg;
     if (few) {
-      const FewArgs e{(const float*)score_ws, ldz, logp, stats, first, cols, g, p.ldg, plane, clean, gram_status_word(ctx)};
-      ProfScope prof(ctx, GRAM_K_OTHER, (4.0 + 2 * planes) * a.N * cols, 1, st, "loss_few");
-      launch_chain(planes == 2 ? loss_few_kernel<2> : loss_few_kernel<1>, dim3((unsigned)ceil_div(cols, 128)), 256, 0, st, a, e);
+      const FewArgs f{e, (const float*)score_ws, ldz, logp, stats, clean, gram_status_word(ctx)};
+      ProfScope prof(ctx, GRAM_K_OTHER, (4.0 + 2 * planes) * e.rows * e.cols, 1, st, "loss_few");
+      launch_chain(planes == 2 ? loss_few_kernel<2> : loss_few_kernel<1>, dim3((unsigned)ceil_div(e.cols, 128)), 256, 0, st, a, f);
       GRAM_LAUNCH_CHECK(ctx);
     } else {
-      GradArgs e = {};
-      e.rows = rows;
-      e.bias = a.bias;
-      e.N = a.N;
-      e.V = a.V;
-      e.first = first;
-      e.cols = cols;
-      e.num_kb = ceil_div(a.d, 64);
-      e.tiles_m = (int32_t)ceil_div64(a.N, 2 * PAIR_ROWS);
-      e.width = (int64_t)e.tiles_m * ceil_div(cols, PAIR_COLS) < kPairs ? PAIR_COLS / 2 : PAIR_COLS;      // tiles of half the width where they leave pairs idle
-      e.total = e.tiles_m * ceil_div(cols, e.width);
-      e.box_rows = box_rows;
-      e.c = a.scale * kLog2e;
-      e.g = g;
-      e.ldg = p.ldg;
-      e.plane = plane;
-      e.bias_part = a.dbias ? (float*)(base + p.bias) : nullptr;
-      e.give_up = gram_ring_rows(ctx);
-      e.status = gram_status_word(ctx);
+      GradArgs f = {};
+      f.at = e;
+      f.rows = rows;
+      f.bias = a.bias;
+      f.V = a.V;
+      f.num_kb = ceil_div(a.d, 64);
+      f.tiles_m = (int32_t)ceil_div64(e.rows, 2 * PAIR_ROWS);
+      f.width = (int64_t)f.tiles_m * ceil_div(e.cols, PAIR_COLS) < kPairs ? PAIR_COLS / 2 : PAIR_COLS;    // tiles of half the width where they leave pairs idle
+      f.total = f.tiles_m * ceil_div(e.cols, f.width);
+      f.box_rows = box_rows;
+      f.c = a.scale * kLog2e;
+      f.bias_part = a.dbias ? (float*)(base + p.bias) : nullptr;
+      f.give_up = gram_ring_rows(ctx);
+      f.status = gram_status_word(ctx);
       {
-        ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * a.N * cols * a.d, 1, st, "loss_grad");
-        const int pairs = e.total < kPairs ? e.total : kPairs;
-        auto kern = planes == 2 ? loss_grad_kernel<2> : loss_grad_kernel<1>;
-        GRAM_CUDA(ctx, launch_pairs(kern, pairs, GradPipe::THREADS, GradPipe::SMEM, st, map_u, map_i, e));
+        ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * e.rows * e.cols * a.d, 1, st, "loss_grad");
+        const int pairs = f.total < kPairs ? f.total : kPairs;
+        if (planes == 2) GRAM_CUDA(ctx, launch_pairs<loss_grad_kernel<2>>(pairs, GradPipe::THREADS, GradPipe::SMEM, st, map_u, map_i, f));
+        else GRAM_CUDA(ctx, launch_pairs<loss_grad_kernel<1>>(pairs, GradPipe::THREADS, GradPipe::SMEM, st, map_u, map_i, f));
       }
       if (a.dbias) {
-        ProfScope prof(ctx, GRAM_K_COLSUM, (double)a.N / 8 * cols, 1, st, "loss_bias");
-        launch_chain(loss_bias_kernel, dim3((unsigned)ceil_div(cols, 32)), 256, 0, st, (const float*)e.bias_part, p.ldg, (int32_t)ceil_div64(a.N, 32), cols,
-                     a.dbias + first);
+        ProfScope prof(ctx, GRAM_K_COLSUM, (double)e.rows / 8 * e.cols, 1, st, "loss_bias");
+        launch_chain(loss_bias_kernel, dim3((unsigned)ceil_div(e.cols, 32)), 256, 0, st, (const float*)f.bias_part, p.ldg, ceil_div64(e.rows, 32), e.cols,
+                     (int32_t)(e.n0 > 0), a.dbias + e.first);
         GRAM_LAUNCH_CHECK(ctx);
       }
     }
     if (!a.dusers && !a.ditems) continue;
-    for (int i = 0; i < 2; ++i)
-      if (!make_map(&map_g[i], g + (i < planes ? i : 0) * plane, (uint64_t)cols, (uint64_t)a.N, (uint64_t)p.ldg, 64, 64))
+    for (int k = 0; k < planes; ++k)
+      if (!make_map(&map_g[k], e.g + k * e.plane, (uint64_t)e.cols, (uint64_t)e.rows, (uint64_t)p.ldg, 64, 64))
         return gram_set_error(ctx, what), GRAM_ERR_UNSUPPORTED;
+    if (planes == 1) map_g[1] = map_g[0];
     ProdArgs w = {};
     const size_t size = planes == 2 ? 4 : 2;
-    w.N = a.N;
-    w.cols = cols;
-    w.first = first;
     w.d = a.d;
     w.tiles_n = ceil_div(a.d, PAIR_COLS);
-    w.items_m = a.ditems ? ceil_div(cols, 2 * PAIR_ROWS) : 0;
-    w.users_m = a.dusers ? (int32_t)ceil_div64(a.N, 2 * PAIR_ROWS) : 0;
-    w.kb_users = (int32_t)ceil_div64(a.N, 64);
-    w.kb_items = ceil_div(cols, 64);
-    w.direct = p.splits == 1 && pieces == 1;
-    // the last piece may have fewer parts; the sums of the others stay
-    w.kb_split = p.splits ? ceil_div(w.kb_items, p.splits) : 0;
-    w.splits = p.splits ? ceil_div(w.kb_items, w.kb_split) : 0;
-    w.units_u = w.users_m * w.tiles_n * w.splits;
-    w.total = w.units_u + w.items_m * w.tiles_n;
-    w.users_first = w.kb_split >= w.kb_users;
-    w.extra = loss_span(w.units_u, w.kb_split ? w.kb_split : 1, w.total - w.units_u, w.kb_users).extra;
+    for (int k = 0; k < 2; ++k) {
+      ProdSide& o = w.of[k];
+      void* grad = k ? a.ditems : a.dusers;
+      const int64_t ld = k ? a.ld_ditems : a.ld_dusers;
+      o.rows = (int32_t)(k ? e.cols : e.rows);
+      o.tiles_m = grad ? ceil_div(o.rows, 2 * PAIR_ROWS) : 0;
+      o.kb = (int32_t)ceil_div64(k ? e.rows : e.cols, 64);
+      // the last piece may have fewer parts; the sums of the others stay
+      o.kb_split = k == own || p.splits == 0 ? o.kb : ceil_div(o.kb, p.splits);
+      o.vec0 = (int32_t)(k ? e.n0 : e.first);
+      o.units = o.tiles_m * w.tiles_n * ceil_div(o.kb, o.kb_split);
+      o.partial = k != own && joined;
+      o.add = i > 0;
+      o.out = o.partial ? (void*)(base + p.parts) : grad ? (uint8_t*)grad + (size_t)(k ? e.first : e.n0) * ld * size : nullptr;
+      o.ld = o.partial ? a.d : ld;
+      o.part = (int64_t)o.rows * a.d;
+      o.wide = o.partial ? 1 : (uintptr_t)grad % 32 == 0 && ld * size % 32 == 0;
+      o.cost = (int32_t)loss_cost(o.kb_split, planes, o.partial || planes == 2);
+    }
+    const LossSpan span = loss_span(w.of[0].units, w.of[0].cost, w.of[1].units, w.of[1].cost);
+    w.heavy = span.heavy;
+    w.extra = span.extra;
+    w.total = w.of[0].units + w.of[1].units;
     w.chain = LP_CHAIN;
-    w.dI = a.ditems ? (uint8_t*)a.ditems + (size_t)first * a.ld_ditems * size : nullptr;
-    w.ld_dI = a.ld_ditems;
-    w.dU = w.direct ? a.dusers : (void*)(base + p.parts);
-    w.ld_dU = a.ld_dusers;
-    w.add = piece > 0;
-    w.wide_I = (uintptr_t)a.ditems % 32 == 0 && a.ld_ditems * size % 32 == 0;
-    w.wide_U = w.direct ? (uintptr_t)a.dusers % 32 == 0 && a.ld_dusers * size % 32 == 0 : 1;
     w.give_up = gram_ring_rows(ctx);
     w.status = gram_status_word(ctx);
-    ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * planes * a.N * cols * a.d * ((a.dusers != nullptr) + (a.ditems != nullptr)), 1, st, "loss_products");
+    ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * planes * e.rows * e.cols * a.d * ((a.dusers != nullptr) + (a.ditems != nullptr)), 1, st, "loss_products");
     const int pairs = w.total < kPairs ? w.total : kPairs;
-    const int longest = w.units_u && w.kb_split > w.kb_users ? w.kb_split : w.kb_users;
-    auto launch = [&](auto kern, auto pipe) {
-      using Pipe = decltype(pipe);
-      return launch_pairs(kern, pairs, Pipe::THREADS, Pipe::SMEM, st, map_g[0], map_g[1], map_clean, map_items, w);
-    };
-    if (planes == 1) GRAM_CUDA(ctx, launch(loss_products_kernel<bf16, false>, ProdPipe<1, false>()));
-    else if (longest <= LP_CHAIN) GRAM_CUDA(ctx, launch(loss_products_kernel<float, false>, ProdPipe<2, false>()));
-    else GRAM_CUDA(ctx, launch(loss_products_kernel<float, true>, ProdPipe<2, true>()));
+    const bool chained = (w.of[0].units && w.of[0].kb_split > LP_CHAIN) || (w.of[1].units && w.of[1].kb_split > LP_CHAIN);
+#define LOSS_PRODUCTS(GT, CHAINED)                                                                                                       \
+  launch_pairs<loss_products_kernel<GT, CHAINED>>(pairs, ProdPipe<sizeof(GT) / 2, CHAINED>::THREADS, ProdPipe<sizeof(GT) / 2, CHAINED>::SMEM, st, map_g[0], \
+                                                  map_g[1], map_clean, map_i, w)
+    if (planes == 1) GRAM_CUDA(ctx, LOSS_PRODUCTS(bf16, false));
+    else if (chained) GRAM_CUDA(ctx, LOSS_PRODUCTS(float, true));
+    else GRAM_CUDA(ctx, LOSS_PRODUCTS(float, false));
+#undef LOSS_PRODUCTS
   }
-  if (a.dusers && !(p.splits == 1 && pieces == 1)) {
-    ProfScope prof(ctx, GRAM_K_OTHER, (double)a.N * a.d * 4 * (p.splits + 1), 1, st, "loss_finish");
+  if (joined) {
+    void* grad = own ? a.dusers : a.ditems;
+    const int64_t n = own ? a.N : a.V, ld = own ? a.ld_dusers : a.ld_ditems;
+    ProfScope prof(ctx, GRAM_K_OTHER, (double)n * a.d * 4 * (p.splits + 1), 1, st, "loss_finish");
     const float* parts = (const float*)(base + p.parts);
-    int64_t blocks = ceil_div64(a.N * (a.d / 4), 256);
+    int64_t blocks = ceil_div64(n * (a.d / 4), 256);
     if (blocks > kNumSMs * 8) blocks = kNumSMs * 8;
-    if (planes == 2) launch_chain(loss_finish_kernel<float>, dim3((unsigned)blocks), 256, 0, st, parts, (int)p.splits, a.N, a.d, (float*)a.dusers, a.ld_dusers);
-    else launch_chain(loss_finish_kernel<bf16>, dim3((unsigned)blocks), 256, 0, st, parts, (int)p.splits, a.N, a.d, (bf16*)a.dusers, a.ld_dusers);
+    if (planes == 2) launch_chain(loss_finish_kernel<float>, dim3((unsigned)blocks), 256, 0, st, parts, (int)p.splits, n, a.d, (float*)grad, ld);
+    else launch_chain(loss_finish_kernel<bf16>, dim3((unsigned)blocks), 256, 0, st, parts, (int)p.splits, n, a.d, (bf16*)grad, ld);
     GRAM_LAUNCH_CHECK(ctx);
   }
   return GRAM_OK;
