@@ -24,6 +24,7 @@ using namespace tc;
 
 constexpr int kPairs = kNumSMs / 2;
 constexpr int LOSS_FEW = 256;                           // users whose logits are kept where 32 MB hold them
+constexpr int LOSS_SHORT = 8 * kPairs;                  // blocks of 64 items x 256 columns that an SM pair takes a plane of in 2 us
 
 // ============================================================================================
 // rows: loss, and the constants of g
@@ -115,14 +116,15 @@ template <int PLANES> __global__ void __launch_bounds__(256) loss_few_kernel(con
       const int hot = r.t - at.first - col;
 #pragma unroll
       for (int j = 0; j < 4; ++j) g[j] = r.t < 0 ? 0.f : r.f * (j == hot ? g[j] - 1.f : g[j]);
-      const uint2 h = make_uint2(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]));
-      bf16* to = at.g + i * at.ldg + col;
-      *reinterpret_cast<uint2*>(to) = h;
-      if constexpr (PLANES == 2) {
-        const float2 u = unpack_bf16x2(h.x), v = unpack_bf16x2(h.y);
-        *reinterpret_cast<uint2*>(to + at.plane) = make_uint2(pack_bf16x2(g[0] - u.x, g[1] - u.y), pack_bf16x2(g[2] - v.x, g[3] - v.y));
-      }
       sum.x += g[0]; sum.y += g[1]; sum.z += g[2]; sum.w += g[3];
+      bf16* to = at.g + i * at.ldg + col;
+#pragma unroll
+      for (int k = 0; k < PLANES; ++k) {
+        const uint2 h = make_uint2(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]));
+        *reinterpret_cast<uint2*>(to + k * at.plane) = h;
+        const float2 u = unpack_bf16x2(h.x), v = unpack_bf16x2(h.y);
+        g[0] -= u.x; g[1] -= u.y; g[2] -= v.x; g[3] -= v.y;
+      }
     }
   }
   if (!a.dbias) return;
@@ -365,9 +367,9 @@ __global__ void __launch_bounds__(256) loss_bias_kernel(const float* part, int64
 // ============================================================================================
 // both products of a piece's g
 // ============================================================================================
-// PLANES: bf16 that g is the sum of; a stage holds all of them beside one piece of the vectors.  CHAINED: the sum of a unit comes as several
-// accumulators, which eight warps add up in registers; else sixteen warps take one.
-template <int PLANES, bool CHAINED> using ProdPipe = PairPipe<PLANES == 2 ? 4 : 6, CHAINED ? 8 : 16, 0, PLANES>;
+// PLANES: bf16 that g is the sum of; a stage holds all of them beside one piece of the vectors.  With one, sixteen warps take the results, 64 columns
+// each; else eight with 128, which can add up several accumulators in registers.  A warp has a box of 32 rows x 128 bytes for its results.
+template <int PLANES> using ProdPipe = PairPipe<6 - PLANES, PLANES == 1 ? 16 : 8, (PLANES == 1 ? 16 : 8) * 4096, PLANES>;
 
 // Blocks of 64 whose products (of both planes) are added up in one accumulator for fp32 gradients.  bf16 results hide the error of any length.
 constexpr int LP_CHAIN = 24;
@@ -378,27 +380,26 @@ struct ProdSide {
   int32_t kb, kb_split;          // blocks of 64 that the sums run over, and those of a part
   int32_t vec0;                  // the first of the vectors that they run over
   int32_t units, cost;           // tiles of all parts; what one costs, in blocks
-  void* out;                     // of the piece's rows: the result, or
-  int32_t partial;               // fp32 sums [parts, rows, d] that are joined later
+  int32_t partial;               // fp32 sums that are joined later, in place of the result
   int32_t add;                   // to what is there (partial)
-  int32_t wide;                  // rows begin on 32 bytes
-  int64_t ld, part;              // elements between rows and between parts
+  int32_t part;                  // rows from one part to the next, a multiple of 256
 };
 struct ProdArgs {
   ProdSide of[2];                // users' and items' gradient
   int32_t d, tiles_n;            // tiles of 256 columns of d
   int32_t total, heavy;          // units of both; whose are the heavier ones, which are dealt first
   int32_t extra;                 // lighter units that a pair gets for each heavier one that others have more
+  int32_t halves;                // units at the end that are dealt as two of half the columns each
   int32_t chain;                 // blocks that are added up in one accumulator
   int32_t give_up;
   int32_t* status;
 };
 
 // Which units a pair takes, its i-th: the heavier ones are dealt first; pairs that get one less take `extra` lighter ones instead; the rest is dealt
-// from the pairs with less on.  (The same in loss_span.)
+// from the pairs with less on, the last round as halves where twice as many are no more than the pairs.  (The same in loss_span.)
 struct ProdWalk {
-  int pair, pairs, heavy, mine, extra, other, base, at, total;
-  __device__ __forceinline__ explicit ProdWalk(const ProdArgs& a) : pair(blockIdx.x >> 1), pairs(gridDim.x >> 1), total(a.total) {
+  int pair, pairs, heavy, mine, extra, other, base, at, total;       // total: halves count as units
+  __device__ __forceinline__ explicit ProdWalk(const ProdArgs& a) : pair(blockIdx.x >> 1), pairs(gridDim.x >> 1), total(a.total + a.halves) {
     heavy = a.of[a.heavy].units;
     const int more = heavy % pairs;                     // pairs with one more
     mine = heavy / pairs + (pair < more);
@@ -419,6 +420,12 @@ struct ProdWalk {
 struct ProdUnit {
   int side, m0, n0, width, split, k0, blocks;           // first row and column; the sum's range in blocks of 64
   __device__ __forceinline__ ProdUnit(const ProdArgs& a, int t) {
+    int half = -1;
+    const int whole = a.total - a.halves;
+    if (t >= whole) {
+      half = (t - whole) & 1;
+      t = whole + ((t - whole) >> 1);
+    }
     side = a.heavy;
     if (t >= a.of[side].units) {
       t -= a.of[side].units;
@@ -427,7 +434,8 @@ struct ProdUnit {
     const ProdSide& o = a.of[side];
     const int r = t / a.tiles_n;
     n0 = (t - r * a.tiles_n) * PAIR_COLS;
-    width = a.d - n0 > PAIR_COLS / 2 ? PAIR_COLS : PAIR_COLS / 2;
+    width = a.d - n0 > PAIR_COLS / 2 && half < 0 ? PAIR_COLS : PAIR_COLS / 2;
+    if (half > 0) n0 += PAIR_COLS / 2;                  // perhaps past the last column
     split = r / o.tiles_m;
     m0 = (r - split * o.tiles_m) * 2 * PAIR_ROWS;
     k0 = split * o.kb_split;
@@ -435,50 +443,28 @@ struct ProdUnit {
   }
 };
 
-// 32 columns of one row, `some` of them there (a multiple of 8)
-__device__ __forceinline__ void put_row(float* p, const float (&x)[32], int some, bool wide, bool add) {
+// 32 fp32 columns of a row to its place in a box of 32 rows x 128 bytes (128-byte swizzle); 32 of 64 bf16 columns
+__device__ __forceinline__ void box_row(uint32_t box, const float (&x)[32]) {
+  const uint32_t lane = threadIdx.x & 31, row = box + lane * 128u;
 #pragma unroll
-  for (int j = 0; j < 32; j += 8) {
-    if (j >= some) break;
-    float4 u = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]), v = make_float4(x[j + 4], x[j + 5], x[j + 6], x[j + 7]);
-    float4* q = reinterpret_cast<float4*>(p + j);
-    if (add) {
-      const float4 a = q[0], b = q[1];
-      u.x += a.x; u.y += a.y; u.z += a.z; u.w += a.w;
-      v.x += b.x; v.y += b.y; v.z += b.z; v.w += b.w;
-    }
-    if (wide) {
-      const uint32_t h[8] = {__float_as_uint(u.x), __float_as_uint(u.y), __float_as_uint(u.z), __float_as_uint(u.w),
-                             __float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)};
-      st32(p + j, h);
-    } else {
-      q[0] = u;
-      q[1] = v;
-    }
-  }
+  for (uint32_t j = 0; j < 8; ++j)
+    sts128(row + ((j ^ (lane & 7)) << 4), __float_as_uint(x[4 * j]), __float_as_uint(x[4 * j + 1]), __float_as_uint(x[4 * j + 2]), __float_as_uint(x[4 * j + 3]));
 }
-__device__ __forceinline__ void put_row(bf16* p, const float (&x)[32], int some, bool wide, bool) {
+__device__ __forceinline__ void box_row(uint32_t box, const float (&x)[32], uint32_t half) {
+  const uint32_t lane = threadIdx.x & 31, row = box + lane * 128u;
 #pragma unroll
-  for (int j = 0; j < 32; j += 16) {
-    uint32_t h[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) h[i] = pack_bf16x2(x[j + 2 * i], x[j + 2 * i + 1]);
-    if (wide && j + 16 <= some) {
-      st32(p + j, h);
-    } else {
-      uint4* q = reinterpret_cast<uint4*>(p + j);
-      if (j < some) q[0] = make_uint4(h[0], h[1], h[2], h[3]);
-      if (j + 8 < some) q[1] = make_uint4(h[4], h[5], h[6], h[7]);
-    }
-  }
+  for (uint32_t j = 0; j < 4; ++j)
+    sts128(row + (((half * 4 + j) ^ (lane & 7)) << 4), pack_bf16x2(x[8 * j], x[8 * j + 1]), pack_bf16x2(x[8 * j + 2], x[8 * j + 3]),
+           pack_bf16x2(x[8 * j + 4], x[8 * j + 5]), pack_bf16x2(x[8 * j + 6], x[8 * j + 7]));
 }
 
-template <typename GT, bool CHAINED>
-__global__ void __launch_bounds__(ProdPipe<sizeof(GT) / 2, CHAINED>::THREADS, 1)
-    loss_products_kernel(const __grid_constant__ CUtensorMap g0, const __grid_constant__ CUtensorMap g1, const __grid_constant__ CUtensorMap users,
-                         const __grid_constant__ CUtensorMap items, const __grid_constant__ ProdArgs a) {
-  constexpr int PLANES = sizeof(GT) / 2;
-  using Pipe = ProdPipe<PLANES, CHAINED>;
+template <typename GT, int PLANES>
+__global__ void __launch_bounds__(ProdPipe<PLANES>::THREADS, 1)
+    loss_products_kernel(const __grid_constant__ CUtensorMap g0, const __grid_constant__ CUtensorMap g1, const __grid_constant__ CUtensorMap g2,
+                         const __grid_constant__ CUtensorMap users, const __grid_constant__ CUtensorMap items, const __grid_constant__ CUtensorMap out_u,
+                         const __grid_constant__ CUtensorMap out_i, const __grid_constant__ ProdArgs a) {
+  constexpr bool CHAINED = sizeof(GT) == 4;
+  using Pipe = ProdPipe<PLANES>;
   extern __shared__ uint8_t smem_raw[];
   Pipe pipe;
   const bool go = pipe.open(smem_raw);
@@ -488,7 +474,7 @@ __global__ void __launch_bounds__(ProdPipe<sizeof(GT) / 2, CHAINED>::THREADS, 1)
     // ------------------------------ copies (both blocks): two boxes of 64 x 64 of each plane of g, one or two of the vectors ------------------------------
     int s = 0;
     uint32_t ph = 0;
-    for (int tile = 0, t; (t = walk(tile)) < a.total && !failed; ++tile) {
+    for (int tile = 0, t; (t = walk(tile)) < walk.total && !failed; ++tile) {
       if (tile == a.give_up) { failed = true; break; }
       const ProdUnit u(a, t);
       const int m0 = u.m0 + (int)pipe.rank * PAIR_ROWS, n0 = u.n0 + (int)pipe.rank * (u.width / 2);
@@ -504,7 +490,7 @@ __global__ void __launch_bounds__(ProdPipe<sizeof(GT) / 2, CHAINED>::THREADS, 1)
           mbar_arrive_expect_tx_remote(bar, bytes);
 #pragma unroll
           for (int i = 0; i < PLANES; ++i) {
-            const CUtensorMap* g = i ? &g1 : &g0;
+            const CUtensorMap* g = i == 0 ? &g0 : i == 1 ? &g1 : &g2;
             const uint32_t sa = pipe.a_of(s, i);
             tma_load_2d_pair(sa, g, of_users ? k : m0, of_users ? m0 : k, bar);
             tma_load_2d_pair(sa + PAIR_BOX, g, of_users ? k : m0 + 64, of_users ? m0 + 64 : k, bar);
@@ -525,7 +511,7 @@ __global__ void __launch_bounds__(ProdPipe<sizeof(GT) / 2, CHAINED>::THREADS, 1)
       const uint64_t db0 = make_desc(pipe.b_of(0), PAIR_BOX, 1024);
       int s = 0;
       uint32_t ph = 0, it = 0;
-      for (int tile = 0, t; (t = walk(tile)) < a.total && !failed; ++tile) {
+      for (int tile = 0, t; (t = walk(tile)) < walk.total && !failed; ++tile) {
         const ProdUnit u(a, t);
         const uint32_t idesc = idesc0 | (u.side == 0 ? 0u : 1u << 15) | ((uint32_t)(u.width >> 3) << 17);
         const uint64_t da0 = u.side == 0 ? da_k : da_mn;
@@ -557,21 +543,42 @@ __global__ void __launch_bounds__(ProdPipe<sizeof(GT) / 2, CHAINED>::THREADS, 1)
       }
     }
   } else if (go) {
-    // ------------------------------ results (both blocks): a row and a part of the columns a thread ------------------------------
-    constexpr int PARTS = Pipe::EPI_WARPS / 4;
+    // ------------------------------ results (both blocks): a row and 64 or 128 columns a thread ------------------------------
+    constexpr int BLOCKS = PLANES == 1 ? 2 : 4;         // of 32 columns
     const int lane = pipe.lane, q = pipe.warp & 3, part = (pipe.warp - 2) >> 2;
-    const uint32_t lane_addr = pipe.tmem + ((uint32_t)(q * 32) << 16);
+    const uint32_t lane_addr = pipe.tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(part * BLOCKS * 32);
+    const uint32_t box = pipe.tiles + Pipe::STAGES * Pipe::STAGE + (uint32_t)(pipe.warp - 2) * 4096u;
     uint32_t it = 0;
-    for (int tile = 0, t; (t = walk(tile)) < a.total && !failed; ++tile) {
+    for (int tile = 0, t; (t = walk(tile)) < walk.total && !failed; ++tile) {
       const ProdUnit u(a, t);
       const ProdSide& o = a.of[u.side];
-      const int m = u.m0 + (int)pipe.rank * PAIR_ROWS + q * 32 + lane;
-      const int blocks = u.width / 32 / PARTS, col = part * blocks * 32;                // of 32 columns
-      auto put = [&](int b, const float (&x)[32]) {
-        const int n = u.n0 + col + b * 32, some = a.d - n;
-        if (m >= o.rows || some <= 0) return;
-        if (o.partial) put_row(reinterpret_cast<float*>(o.out) + u.split * o.part + m * o.ld + n, x, some, o.wide, o.add);
-        else put_row(reinterpret_cast<GT*>(o.out) + m * o.ld + n, x, some, o.wide, false);
+      const CUtensorMap* out = u.side == 0 ? &out_u : &out_i;
+      const int m = u.m0 + (int)pipe.rank * PAIR_ROWS + q * 32, n = u.n0 + part * BLOCKS * 32;        // of the warp
+      const bool there = m < o.rows && n < a.d && part * BLOCKS * 32 < u.width;
+      const int row = m + u.split * o.part;
+      auto free_box = [&]() {                           // its last store has read it
+        if (lane == 0) bulk_wait_read_all();
+        __syncwarp();
+      };
+      auto send = [&](int col, bool add) {
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0 && col < a.d) {
+          if (add) tma_reduce_add_2d(out, box, col, row);
+          else tma_store_2d(out, box, col, row);
+          bulk_commit();
+        }
+      };
+      auto put = [&](int b, const float (&x)[32]) {     // block b of the warp's columns
+        if (sizeof(GT) == 4 || o.partial) {
+          free_box();
+          box_row(box, x);
+          send(n + b * 32, o.partial && o.add);
+        } else {
+          if (b % 2 == 0) free_box();
+          box_row(box, x, (uint32_t)b % 2);
+          if (b % 2 == 1) send(n + (b - 1) * 32, false);
+        }
       };
       if constexpr (CHAINED) {
         // The tensor cores cut off where this adds with rounding: a chain's length sets the sum's precision.
@@ -585,59 +592,62 @@ __global__ void __launch_bounds__(ProdPipe<sizeof(GT) / 2, CHAINED>::THREADS, 1)
           const int buf = (int)(it & 1);
           if (!mbar_wait_warp(pipe.tfull(buf), (it >> 1) & 1, pipe.abort_flag)) { failed = true; break; }
           tc_fence_after();
+          if (there) {
 #pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            if (b >= blocks) break;
+            for (int b = 0; b < 4; ++b)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              uint32_t v[16];
-              tc_ld16(lane_addr + (uint32_t)(buf * PAIR_COLS + col + b * 32 + h * 16), v);
+              for (int h = 0; h < 2; ++h) {
+                uint32_t v[16];
+                tc_ld16(lane_addr + (uint32_t)(buf * PAIR_COLS + b * 32 + h * 16), v);
 #pragma unroll
-              for (int j = 0; j < 16; ++j) acc[b][h * 16 + j] += __uint_as_float(v[j]);
-            }
+                for (int j = 0; j < 16; ++j) acc[b][h * 16 + j] += __uint_as_float(v[j]);
+              }
           }
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive_remote(pipe.lead_tempty(buf));
         }
         if (failed) break;
+        if (there) {
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
-          if (b < blocks) put(b, acc[b]);
+          for (int b = 0; b < 4; ++b) put(b, acc[b]);
+        }
       } else {
         const int buf = (int)(it & 1);
         if (!mbar_wait_warp(pipe.tfull(buf), (it >> 1) & 1, pipe.abort_flag)) { failed = true; break; }
         tc_fence_after();
-        for (int b = 0; b < blocks; ++b) {
-          uint32_t v[32];
-          tc_ld32_issue(lane_addr + (uint32_t)(buf * PAIR_COLS + col + b * 32), v);
-          tc_ld32_wait(v);
-          float x[32];
+        if (there) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(v[j]);
-          put(b, x);
-          __syncwarp();
+          for (int b = 0; b < BLOCKS; ++b) {
+            uint32_t v[32];
+            tc_ld32_issue(lane_addr + (uint32_t)(buf * PAIR_COLS + b * 32), v);
+            tc_ld32_wait(v);
+            float x[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(v[j]);
+            put(b, x);
+          }
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_remote(pipe.lead_tempty(buf));
         ++it;
       }
-      __syncwarp();
     }
+    if (lane == 0) bulk_wait_all();                     // its stores are complete before the block may exit
   }
   pipe.close(failed, a.status);
 }
 
-// a gradient [N, d] as the sum of its parts
-template <typename GT> __global__ void __launch_bounds__(256) loss_finish_kernel(const float* parts, int splits, int64_t N, int32_t d, GT* grad, int64_t ld) {
+// a gradient [N, d] as the sum of its parts, `part` elements from one to the next
+template <typename GT> __global__ void __launch_bounds__(256) loss_finish_kernel(const float* parts, int splits, int64_t part, int64_t N, int32_t d, GT* grad, int64_t ld) {
   if (!chain_begin()) return;
   const int64_t n4 = N * (d / 4);
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n4; i += (int64_t)gridDim.x * 256) {
     float4 s = reinterpret_cast<const float4*>(parts)[i];
 #pragma unroll 8
     for (int k = 1; k < splits; ++k) {
-      const float4 x = reinterpret_cast<const float4*>(parts)[k * n4 + i];
+      const float4 x = reinterpret_cast<const float4*>(parts + k * part)[i];
       s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
     }
     const int64_t n = i / (d / 4);
@@ -661,14 +671,14 @@ struct LossPlan {
 
 // What a unit over `kb` blocks costs, in blocks of a pair (0.37 us): the products of all planes, or the way of 256 x 256 results out where that takes longer.
 int64_t loss_cost(int64_t kb, int planes, bool f32) {
-  const int64_t out = f32 ? 13 : 7;
+  const int64_t out = f32 ? 6 : 3;
   return kb * planes > out ? kb * planes : out;
 }
 
 // How the units of a piece's products are dealt to the pairs (ProdWalk), and the blocks that the busiest one works through.
 struct LossSpan {
   int64_t most;
-  int32_t heavy, extra;          // whether the second kind is the heavier one
+  int32_t heavy, extra, halves;  // heavy: whether the second kind is the heavier one
 };
 LossSpan loss_span(int64_t units_a, int64_t cost_a, int64_t units_b, int64_t cost_b) {
   const bool second = units_a == 0 || (units_b > 0 && cost_b > cost_a);
@@ -677,32 +687,37 @@ LossSpan loss_span(int64_t units_a, int64_t cost_a, int64_t units_b, int64_t cos
   const int64_t more = n1 % pairs, other = pairs - more;
   int64_t extra = more ? c1 / c2 : 0;                   // rounded down: those pairs are dealt to first
   if (extra > n2 / other) extra = n2 / other;
-  const int64_t rest = n2 - extra * other;
-  const int64_t load_other = (n1 / pairs) * c1 + (extra + rest / pairs + (rest % pairs > 0)) * c2;
-  const int64_t load_more = more ? (n1 / pairs + 1) * c1 + (rest / pairs + (rest % pairs > other)) * c2 : 0;
-  return LossSpan{load_other > load_more ? load_other : load_more, (int32_t)second, (int32_t)extra};
+  const int64_t rest = n2 - extra * other, last = rest % pairs;
+  const bool half = last > 0 && 2 * last <= pairs && n1 + n2 > pairs;
+  const int64_t round = half ? 2 * last : last, cost = half ? (c2 + 1) / 2 : c2;         // the last round
+  const int64_t load_other = (n1 / pairs) * c1 + (extra + rest / pairs) * c2 + (round > 0 ? cost : 0);
+  const int64_t load_more = more ? (n1 / pairs + 1) * c1 + (rest / pairs) * c2 + (round > other ? cost : 0) : 0;
+  return LossSpan{load_other > load_more ? load_other : load_more, (int32_t)second, (int32_t)extra, (int32_t)(half ? last : 0)};
 }
 
 // Parts that the summed gradient's sums over a piece are cut into, so that the pairs are evenly busy.  `step` rows of the piece's own
 // gradient, `all` of the summed one.  A part costs its place in the sum: 8 `all` d bytes, in blocks.
-int loss_splits(int64_t step, int64_t all, int32_t d, int planes, bool own, bool summed) {
-  if (!summed) return 0;
+struct LossSplits {
+  int parts;
+  double time;                   // of the piece, in blocks
+};
+LossSplits loss_splits(int64_t step, int64_t all, int32_t d, int planes, bool f32, bool own, bool summed) {
   const int64_t tiles_n = ceil_div(d, PAIR_COLS), kb = ceil_div64(step, 64);
   const int64_t units_own = own ? ceil_div64(step, PAIR_COLS) * tiles_n : 0, tiles = ceil_div64(all, PAIR_COLS) * tiles_n;
-  const int64_t cost_own = loss_cost(ceil_div64(all, 64), planes, planes == 2);
+  const int64_t cost_own = loss_cost(ceil_div64(all, 64), planes, f32);
+  if (!summed) return LossSplits{0, units_own ? (double)loss_span(units_own, cost_own, 0, 1).most : 0.0};
   const double part = 8.0 * all * d / (5e6 * 0.37);
-  int best = 1;
-  double least = 1e300;
-  for (int s = 1; s <= 32 && s * 4 <= (kb > 4 ? kb : 4); ++s) {
+  LossSplits best{1, 1e300};
+  for (int s = 1; s <= 32 && s * 4 <= (kb > 4 ? kb : 4) && s * all < (1 << 30); ++s) {
     const int64_t of = ceil_div64(kb, s), parts = ceil_div64(kb, of);
     const double time = (double)loss_span(tiles * parts, loss_cost(of, planes, true), units_own, cost_own).most + (parts > 1 ? parts * part : 0.0);
-    if (time < least) { least = time; best = (int)parts; }
+    if (time < best.time) best = LossSplits{(int)parts, time};
   }
   return best;
 }
 
 // Lays out a workspace of `room` bytes, or the one of pieces of `step`.
-LossPlan loss_plan(int64_t N, int32_t V, int32_t d, int planes, bool users, bool items, bool bias, int64_t step, size_t room) {
+LossPlan loss_plan(int64_t N, int32_t V, int32_t d, int planes, bool f32, bool users, bool items, bool bias, int64_t step, size_t room) {
   LossPlan p = {};
   p.cut_users = N > V;
   const int64_t axis = p.cut_users ? N : V, all = p.cut_users ? V : N, all_up = (all + 255) / 256 * 256;
@@ -717,7 +732,7 @@ LossPlan loss_plan(int64_t N, int32_t V, int32_t d, int planes, bool users, bool
     p.stats = take((size_t)N * 8);
     p.rows = take((size_t)N * sizeof(RowConst));
     p.clean = take(items ? (size_t)N * d * 2 : 0);
-    p.parts = take((size_t)splits * all * d * 4);
+    p.parts = take((size_t)splits * all_up * d * 4);
     p.bias = take(bias ? (size_t)ceil_div64(rows, 32) * p.ldg * 4 : 0);
     p.g = take((size_t)planes * rows * p.ldg * 2);
     p.bytes = at;
@@ -727,7 +742,7 @@ LossPlan loss_plan(int64_t N, int32_t V, int32_t d, int planes, bool users, bool
   auto with = [&](int64_t c) {
     const int64_t real = c < axis ? c : axis;
     const int kb = (int)ceil_div64(real, 64);
-    int s = loss_splits(real, all, d, planes, own, summed);
+    int s = loss_splits(real, all, d, planes, f32, own, summed).parts;
     place(c, s);
     while (room && p.bytes > room && s > 1) place(c, s = ceil_div(kb, ceil_div(kb, s - 1)));      // as many as are not empty
   };
@@ -740,7 +755,16 @@ LossPlan loss_plan(int64_t N, int32_t V, int32_t d, int planes, bool users, bool
   int64_t c = room > p.bytes ? (int64_t)((room - p.bytes) / per) * 256 : 0;
   if (c > most) c = most;
   if (c < 256) c = 256;
-  c = ceil_div64(ceil_div64(axis, ceil_div64(axis, c)), 256) * 256;          // pieces of about equal size
+  // Pieces of about equal size: as few as fit or up to half as many again, whichever count deals their units out most evenly (a piece costs
+  // its launches, some 16 blocks).  4096 users, 100 000 items of 768: four pieces leave the pairs 3 % idle, three 6 %, five 9 %.
+  const int64_t few = ceil_div64(axis, c);
+  double least = 1e300;
+  for (int64_t pieces = few; pieces <= few + few / 2 && pieces <= few + 4; ++pieces) {
+    const int64_t size = ceil_div64(ceil_div64(axis, pieces), 256) * 256, whole = axis / size, rest = axis - whole * size;
+    double time = few == 1 ? 0.0 : whole * (loss_splits(size, all, d, planes, f32, own, summed).time + 16);
+    if (few > 1 && rest) time += loss_splits(rest, all, d, planes, f32, own, summed).time + 16;
+    if (time < least) { least = time; c = size; }
+  }
   with(c);
   while (p.bytes > room && p.step > 256) with(p.step - 256);
   return p;
@@ -748,23 +772,33 @@ LossPlan loss_plan(int64_t N, int32_t V, int32_t d, int planes, bool users, bool
 
 constexpr int64_t kGoodG = (int64_t)256 << 20;            // bytes of a piece's g
 
+// Few users' logits stay in the context's workspace (32 MB of it at most: they stay in L2), in place of a second product for each piece.
+bool loss_few(int64_t N, int32_t V) { return N <= LOSS_FEW && N * (((int64_t)V + 7) / 8 * 8) * (int64_t)sizeof(float) <= (32 << 20); }
+// bf16 that g is the sum of: fp32 gradients take one more where users are few and the products short, so that it costs little.
+int loss_planes(int64_t N, int32_t V, int32_t d, int grad_dtype) {
+  if (grad_dtype == GRAM_BF16) return 1;
+  return loss_few(N, V) && ceil_div64(V, 64) * ceil_div(d, PAIR_COLS) <= LOSS_SHORT ? 3 : 2;
+}
+
 }  // namespace
 
 void score_loss_workspace(int64_t N, int32_t V, int32_t d, int grad_dtype, size_t* least, size_t* best) {
-  const int planes = grad_dtype == GRAM_F32 ? 2 : 1;
-  const int64_t n = N > 0 ? N : 1, all = n > V ? (int64_t)V : n;
-  LossPlan p = loss_plan(n, V, d, planes, true, true, true, 256, 0);
-  *least = p.bytes - up((size_t)p.splits * all * d * 4) + up((size_t)all * d * 4);      // with one part of the summed gradient
-  int64_t step = kGoodG / (2 * planes * ((all + 255) / 256 * 256)) / 256 * 256;
+  const bool f32 = grad_dtype == GRAM_F32;
+  const int planes = loss_planes(N, V, d, grad_dtype);
+  const int64_t n = N > 0 ? N : 1, all_up = ((n > V ? (int64_t)V : n) + 255) / 256 * 256;
+  LossPlan p = loss_plan(n, V, d, planes, f32, true, true, true, 256, 0);
+  *least = p.bytes - up((size_t)p.splits * all_up * d * 4) + up((size_t)all_up * d * 4);      // with one part of the summed gradient
+  int64_t step = kGoodG / (2 * planes * all_up) / 256 * 256;
   if (step < 256) step = 256;
-  p = loss_plan(n, V, d, planes, true, true, true, step, 0);
+  p = loss_plan(n, V, d, planes, f32, true, true, true, step, 0);
   *best = p.bytes > *least ? p.bytes : *least;
 }
 
 gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_t ws_bytes, void* score_ws, size_t score_ws_bytes, cudaStream_t st) {
   const bool grads = a.dusers || a.ditems || a.dbias;
-  const int planes = a.grad_dtype == GRAM_F32 ? 2 : 1;
-  const LossPlan p = loss_plan(a.N, a.V, a.d, planes, a.dusers != nullptr, a.ditems != nullptr, a.dbias != nullptr, 0, ws_bytes ? ws_bytes : 1);
+  const bool f32 = a.grad_dtype == GRAM_F32;
+  const int planes = loss_planes(a.N, a.V, a.d, a.grad_dtype);
+  const LossPlan p = loss_plan(a.N, a.V, a.d, planes, f32, a.dusers != nullptr, a.ditems != nullptr, a.dbias != nullptr, 0, ws_bytes ? ws_bytes : 1);
   const size_t need = grads ? p.bytes : p.rows;
   if (need > ws_bytes)
     return gram_set_error(ctx, "gram_score_loss: a workspace of %zu bytes is needed, not %zu", need, ws_bytes), GRAM_ERR_WORKSPACE;
@@ -778,9 +812,8 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
   ask.C = 1;
   RowConst* rows = grads ? (RowConst*)(base + p.rows) : nullptr;
   bf16* clean = a.ditems ? (bf16*)(base + p.clean) : nullptr;
-  // Few logits stay in the context's workspace, out of L2, in place of a second product for each piece.
   const int64_t ldz = ((int64_t)a.V + 7) / 8 * 8;
-  const bool few = grads && a.N <= LOSS_FEW && (size_t)a.N * ldz * sizeof(float) <= (score_ws_bytes < (32u << 20) ? score_ws_bytes : 32u << 20);
+  const bool few = grads && loss_few(a.N, a.V);
   if (few) {
     GRAM_TRY(score_logits_launch(ctx, a.users, a.ld_users, a.items, a.ld_items, a.bias, a.N, a.V, a.d, (float*)score_ws, ldz, st));
     GRAM_TRY(logprobs_launch(ctx, score_ws, GRAM_F32, ldz, a.N, a.V, a.scale, ask, st));
@@ -794,7 +827,7 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
   if (!grads) return GRAM_OK;
 
   const char* what = "gram_score_loss: cannot describe the vectors";
-  CUtensorMap map_u, map_i, map_clean, map_g[2];
+  CUtensorMap map_u, map_i, map_clean, map_g[3], map_out[2];
   int box_rows = PAIR_ROWS;                              // copies are no larger than the users
   while (box_rows > 8 && box_rows / 2 >= a.N) box_rows /= 2;
   if ((!few && !make_map(&map_u, a.users, (uint64_t)a.d, (uint64_t)a.N, (uint64_t)a.ld_users, 64, (uint32_t)box_rows)) ||
@@ -819,7 +852,7 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
     if (few) {
       const FewArgs f{e, (const float*)score_ws, ldz, logp, stats, clean, gram_status_word(ctx)};
       ProfScope prof(ctx, GRAM_K_OTHER, (4.0 + 2 * planes) * e.rows * e.cols, 1, st, "loss_few");
-      launch_chain(planes == 2 ? loss_few_kernel<2> : loss_few_kernel<1>, dim3((unsigned)ceil_div(e.cols, 128)), 256, 0, st, a, f);
+      launch_chain(planes == 3 ? loss_few_kernel<3> : planes == 2 ? loss_few_kernel<2> : loss_few_kernel<1>, dim3((unsigned)ceil_div(e.cols, 128)), 256, 0, st, a, f);
       GRAM_LAUNCH_CHECK(ctx);
     } else {
       GradArgs f = {};
@@ -853,9 +886,9 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
     for (int k = 0; k < planes; ++k)
       if (!make_map(&map_g[k], e.g + k * e.plane, (uint64_t)e.cols, (uint64_t)e.rows, (uint64_t)p.ldg, 64, 64))
         return gram_set_error(ctx, what), GRAM_ERR_UNSUPPORTED;
-    if (planes == 1) map_g[1] = map_g[0];
+    for (int k = planes; k < 3; ++k) map_g[k] = map_g[0];
     ProdArgs w = {};
-    const size_t size = planes == 2 ? 4 : 2;
+    const size_t size = f32 ? 4 : 2;
     w.d = a.d;
     w.tiles_n = ceil_div(a.d, PAIR_COLS);
     for (int k = 0; k < 2; ++k) {
@@ -871,39 +904,45 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
       o.units = o.tiles_m * w.tiles_n * ceil_div(o.kb, o.kb_split);
       o.partial = k != own && joined;
       o.add = i > 0;
-      o.out = o.partial ? (void*)(base + p.parts) : grad ? (uint8_t*)grad + (size_t)(k ? e.first : e.n0) * ld * size : nullptr;
-      o.ld = o.partial ? a.d : ld;
-      o.part = (int64_t)o.rows * a.d;
-      o.wide = o.partial ? 1 : (uintptr_t)grad % 32 == 0 && ld * size % 32 == 0;
-      o.cost = (int32_t)loss_cost(o.kb_split, planes, o.partial || planes == 2);
+      o.part = (o.rows + 255) / 256 * 256;
+      if (grad) {                                        // boxes of 32 rows x 128 bytes; those of a part end with the part's last tile
+        uint8_t* to = o.partial ? base + p.parts : (uint8_t*)grad + (size_t)(k ? e.first : e.n0) * ld * size;
+        const uint64_t out_rows = o.partial ? (uint64_t)p.splits * o.part : (uint64_t)o.rows, out_ld = o.partial ? (uint64_t)a.d : (uint64_t)ld;
+        if (!(o.partial || f32 ? make_map_f32(&map_out[k], to, (uint64_t)a.d, out_rows, out_ld, 32, 32)
+                                       : make_map(&map_out[k], to, (uint64_t)a.d, out_rows, out_ld, 64, 32)))
+          return gram_set_error(ctx, "gram_score_loss: cannot describe the gradients"), GRAM_ERR_UNSUPPORTED;
+      } else {
+        map_out[k] = map_i;
+      }
+      o.cost = (int32_t)loss_cost(o.kb_split, planes, o.partial || f32);
     }
     const LossSpan span = loss_span(w.of[0].units, w.of[0].cost, w.of[1].units, w.of[1].cost);
     w.heavy = span.heavy;
     w.extra = span.extra;
+    w.halves = span.halves;
     w.total = w.of[0].units + w.of[1].units;
     w.chain = LP_CHAIN;
     w.give_up = gram_ring_rows(ctx);
     w.status = gram_status_word(ctx);
     ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * planes * e.rows * e.cols * a.d * ((a.dusers != nullptr) + (a.ditems != nullptr)), 1, st, "loss_products");
     const int pairs = w.total < kPairs ? w.total : kPairs;
-    const bool chained = (w.of[0].units && w.of[0].kb_split > LP_CHAIN) || (w.of[1].units && w.of[1].kb_split > LP_CHAIN);
-#define LOSS_PRODUCTS(GT, CHAINED)                                                                                                       \
-  launch_pairs<loss_products_kernel<GT, CHAINED>>(pairs, ProdPipe<sizeof(GT) / 2, CHAINED>::THREADS, ProdPipe<sizeof(GT) / 2, CHAINED>::SMEM, st, map_g[0], \
-                                                  map_g[1], map_clean, map_i, w)
-    if (planes == 1) GRAM_CUDA(ctx, LOSS_PRODUCTS(bf16, false));
-    else if (chained) GRAM_CUDA(ctx, LOSS_PRODUCTS(float, true));
-    else GRAM_CUDA(ctx, LOSS_PRODUCTS(float, false));
+#define LOSS_PRODUCTS(GT, PLANES)                                                                                                                   \
+  launch_pairs<loss_products_kernel<GT, PLANES>>(pairs, ProdPipe<PLANES>::THREADS, ProdPipe<PLANES>::SMEM, st, map_g[0], map_g[1], map_g[2], map_clean, map_i, \
+                                                 map_out[0], map_out[1], w)
+    if (planes == 1) GRAM_CUDA(ctx, LOSS_PRODUCTS(bf16, 1));
+    else if (planes == 2) GRAM_CUDA(ctx, LOSS_PRODUCTS(float, 2));
+    else GRAM_CUDA(ctx, LOSS_PRODUCTS(float, 3));
 #undef LOSS_PRODUCTS
   }
   if (joined) {
     void* grad = own ? a.dusers : a.ditems;
-    const int64_t n = own ? a.N : a.V, ld = own ? a.ld_dusers : a.ld_ditems;
+    const int64_t n = own ? a.N : a.V, ld = own ? a.ld_dusers : a.ld_ditems, part = (n + 255) / 256 * 256 * a.d;
     ProfScope prof(ctx, GRAM_K_OTHER, (double)n * a.d * 4 * (p.splits + 1), 1, st, "loss_finish");
     const float* parts = (const float*)(base + p.parts);
     int64_t blocks = ceil_div64(n * (a.d / 4), 256);
     if (blocks > kNumSMs * 8) blocks = kNumSMs * 8;
-    if (planes == 2) launch_chain(loss_finish_kernel<float>, dim3((unsigned)blocks), 256, 0, st, parts, (int)p.splits, n, a.d, (float*)grad, ld);
-    else launch_chain(loss_finish_kernel<bf16>, dim3((unsigned)blocks), 256, 0, st, parts, (int)p.splits, n, a.d, (bf16*)grad, ld);
+    if (f32) launch_chain(loss_finish_kernel<float>, dim3((unsigned)blocks), 256, 0, st, parts, (int)p.splits, part, n, a.d, (float*)grad, ld);
+    else launch_chain(loss_finish_kernel<bf16>, dim3((unsigned)blocks), 256, 0, st, parts, (int)p.splits, part, n, a.d, (bf16*)grad, ld);
     GRAM_LAUNCH_CHECK(ctx);
   }
   return GRAM_OK;
