@@ -183,22 +183,24 @@ def _gradient(logits, dlogits):
 
 
 def _vectors(users, items):
-    """(address, elements between rows) of users and of items, bfloat16 rows of one length."""
+    """(address, elements between rows) of users and of items, bfloat16 rows of one length; (N, d) and V."""
     p, dtype, ld = _rows(users, "users")
     q, dtype_items, ld_items = _rows(items, "items")
-    if dtype != GRAM_BF16 or dtype_items != GRAM_BF16 or users.shape[1] != items.shape[1]:
+    N, d = users.shape
+    V, d_items = items.shape
+    if dtype != GRAM_BF16 or dtype_items != GRAM_BF16 or d != d_items:
         raise GramError(1, f"users and items: bfloat16 rows of one length are needed, not {users.dtype} {tuple(users.shape)} and {items.dtype} "
                            f"{tuple(items.shape)}")
-    return p, ld, q, ld_items
+    return p, ld, q, ld_items, N, d, V
 
 
-def _vector_gradient(vectors, grad, what: str):
-    """(address, elements between rows, type) of a gradient of these vectors; None -> NULL."""
+def _vector_gradient(grad, n: int, d: int, what: str):
+    """(address, elements between rows, type) of a gradient [n, d]; None -> NULL."""
     if grad is None:
         return None, 0, None
     q, dtype, ld = _rows(grad, what)
-    if grad.shape != vectors.shape:
-        raise GramError(1, f"{what}: shape {tuple(vectors.shape)} is needed, not {tuple(grad.shape)}")
+    if grad.shape != (n, d):
+        raise GramError(1, f"{what}: shape {(n, d)} is needed, not {tuple(grad.shape)}")
     return q, ld, dtype
 
 
@@ -405,8 +407,8 @@ class Gram:
 
     def score_logprobs(self, users, items, bias=None, scale=1.0, targets=None, logp=None, stats=None, entropy=None, top_logp=None,
                        top_ids=None, stream=None):
-        p, ld, q, ld_items = _vectors(users, items)
-        (N, d), V, nc, k = users.shape, items.shape[0], _width(targets, "targets"), _width(top_ids, "top_ids")
+        p, ld, q, ld_items, N, d, V = _vectors(users, items)
+        nc, k = _width(targets, "targets"), _width(top_ids, "top_ids")
         self._ck(lib().gram_score_logprobs(self._h, p, ld, q, ld_items, _array(bias, "f", V, "bias"), N, V, d, scale,
                                            _array(targets, "i", N * nc, "targets"), nc, _array(logp, "f", N * nc, "logp"),
                                            _array(stats, "f", N * 2, "stats"), _array(entropy, "f", N, "entropy"),
@@ -414,16 +416,16 @@ class Gram:
 
     def score_loss(self, users, items, targets, loss, workspace, bias=None, scale=1.0, weight=None, dusers=None, ditems=None, dbias=None, stream=None):
         """workspace: uint8, at least score_loss_workspace(...)[0] bytes."""
-        p, ld, q, ld_items = _vectors(users, items)
-        (N, d), V = users.shape, items.shape[0]
-        gu, ld_gu, type_u = _vector_gradient(users, dusers, "dusers")
-        gi, ld_gi, type_i = _vector_gradient(items, ditems, "ditems")
+        p, ld, q, ld_items, N, d, V = _vectors(users, items)
+        gu, ld_gu, type_u = _vector_gradient(dusers, N, d, "dusers")
+        gi, ld_gi, type_i = _vector_gradient(ditems, V, d, "ditems")
+        room = workspace.numel()
         if type_u is not None and type_i is not None and type_u != type_i:
             raise GramError(1, f"dusers and ditems: one type is needed, not {dusers.dtype} and {ditems.dtype}")
         self._ck(lib().gram_score_loss(self._h, p, ld, q, ld_items, _array(bias, "f", V, "bias"), N, V, d, scale, _array(targets, "i", N, "targets"),
                                        _array(weight, "f", N, "weight"), _array(loss, "f", N, "loss"), (type_u if type_u is not None else type_i) or 0,
-                                       gu, ld_gu, gi, ld_gi, _array(dbias, "f", V, "dbias"), _array(workspace, "b", workspace.numel(), "workspace"),
-                                       workspace.numel(), _raw_stream(stream)))
+                                       gu, ld_gu, gi, ld_gi, _array(dbias, "f", V, "dbias"), _array(workspace, "b", room, "workspace"), room,
+                                       _raw_stream(stream)))
 
     @staticmethod
     def score_loss_workspace(N: int, V: int, d: int, grad_dtype):

@@ -49,6 +49,9 @@ __device__ __forceinline__ bool chain_begin() {
   asm volatile("griddepcontrol.wait;\n\tmov.u32 %0, %%nctaid.x;" : "=r"(n)::"memory");
   return n != 0u;
 }
+// Lets the blocks of the next launch in while this one runs, where they fit beside it: they set up what needs no memory of others and wait
+// in chain_begin(), which still waits for the whole of this launch.
+__device__ __forceinline__ void chain_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 static inline cudaLaunchAttribute chain_attribute() {
   cudaLaunchAttribute a = {};
   a.id = cudaLaunchAttributeProgrammaticStreamSerialization;

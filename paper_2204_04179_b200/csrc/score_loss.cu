@@ -95,6 +95,7 @@ struct FewArgs {
   int32_t* status;
 };
 template <int PLANES> __global__ void __launch_bounds__(256) loss_few_kernel(const ScoreLoss a, const FewArgs f) {
+  chain_next();
   if (!chain_begin()) return;
   __shared__ float4 sums[8][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 128 + 4 * lane;
@@ -141,6 +142,84 @@ template <int PLANES> __global__ void __launch_bounds__(256) loss_few_kernel(con
 #pragma unroll
   for (int j = 0; j < 4; ++j)
     if (col + j < at.cols) to[j] = at.n0 > 0 ? to[j] + all[j] : all[j];
+}
+
+// Few users and few items, all of g in one piece and db not asked: a block takes a row of logits into registers, with its statistics, the loss,
+// the user's vector and g, in place of gram_logprobs' kernel and the one above.
+constexpr int LR_THREADS = 512, LR_EACH = 32;           // logits of a thread: rows of up to 16 384
+template <int PLANES> __global__ void __launch_bounds__(LR_THREADS) loss_row_kernel(const ScoreLoss a, const FewArgs f) {
+  chain_next();
+  if (!chain_begin()) return;
+  __shared__ float part[2][LR_THREADS / 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t n = blockIdx.x;
+  const float c = a.scale * kLog2e;
+  const float* row = f.z + n * f.ldz;
+  const int32_t t = a.targets[n];
+  const bool in = t >= 0 && t < a.V;
+  const float w = a.weight ? a.weight[n] : 1.f, zt = in ? row[t] : 0.f;
+  float4 z[LR_EACH / 4];
+  float m = ROW_NEG_INF;
+#pragma unroll
+  for (int i = 0; i < LR_EACH / 4; ++i) {
+    const int v = 4 * (i * LR_THREADS + (int)threadIdx.x);
+    z[i] = make_float4(ROW_NEG_INF, ROW_NEG_INF, ROW_NEG_INF, ROW_NEG_INF);
+    if (v < a.V) {                                      // the row reaches to the next multiple of 8
+      z[i] = *reinterpret_cast<const float4*>(row + v);
+      if (v + 1 >= a.V) z[i].y = ROW_NEG_INF;
+      if (v + 2 >= a.V) z[i].z = ROW_NEG_INF;
+      if (v + 3 >= a.V) z[i].w = ROW_NEG_INF;
+    }
+    m = fmaxf(m, fmaxf(fmaxf(z[i].x, z[i].y), fmaxf(z[i].z, z[i].w)));
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (lane == 0) part[0][warp] = m;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < LR_THREADS / 32; ++i) m = fmaxf(m, part[0][i]);
+  const float ref = m == ROW_NEG_INF ? 0.f : m;         // a row with nothing left has a sum of 0
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < LR_EACH / 4; ++i) {
+    z[i].x = row_ex2((z[i].x - ref) * c);
+    z[i].y = row_ex2((z[i].y - ref) * c);
+    z[i].z = row_ex2((z[i].z - ref) * c);
+    z[i].w = row_ex2((z[i].w - ref) * c);
+    s += (z[i].x + z[i].y) + (z[i].z + z[i].w);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (lane == 0) part[1][warp] = s;
+  __syncthreads();
+  s = 0.f;
+#pragma unroll
+  for (int i = 0; i < LR_THREADS / 32; ++i) s += part[1][i];
+  const float lp = in ? row_logp(zt, m, logf(s), a.scale) : 0.f;
+  const bool takes_part = in && w != 0.f && lp != ROW_NEG_INF;
+  if (threadIdx.x == 0) {
+    if (!in && t != -1) gram_device_fail(f.status, GRAM_ERR_ID_RANGE);
+    a.loss[n] = 0.f - lp;
+  }
+  if (f.clean && warp == 0) loss_clean(a, n, takes_part, f.clean);
+  const float factor = lp != lp ? lp : w * a.scale, each = takes_part ? factor / s : 0.f;
+#pragma unroll
+  for (int i = 0; i < LR_EACH / 4; ++i) {
+    const int v = 4 * (i * LR_THREADS + (int)threadIdx.x);
+    if (v >= a.V) break;
+    // of the target p - 1, in one rounding of the difference
+    float g[4] = {z[i].x, z[i].y, z[i].z, z[i].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) g[j] = !takes_part ? 0.f : v + j == t ? factor * (g[j] / s - 1.f) : g[j] * each;
+    bf16* to = f.at.g + n * f.at.ldg + v;
+#pragma unroll
+    for (int k = 0; k < PLANES; ++k) {
+      const uint2 h = make_uint2(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]));
+      *reinterpret_cast<uint2*>(to + k * f.at.plane) = h;
+      const float2 u = unpack_bf16x2(h.x), x = unpack_bf16x2(h.y);
+      g[0] -= u.x; g[1] -= u.y; g[2] -= x.x; g[3] -= x.y;
+    }
+  }
 }
 
 // ============================================================================================
@@ -468,6 +547,7 @@ __global__ void __launch_bounds__(ProdPipe<PLANES>::THREADS, 1)
   extern __shared__ uint8_t smem_raw[];
   Pipe pipe;
   const bool go = pipe.open(smem_raw);
+  chain_next();
   const ProdWalk walk(a);
   bool failed = false;
   if (pipe.warp == 0 && go) {
@@ -814,9 +894,10 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
   bf16* clean = a.ditems ? (bf16*)(base + p.clean) : nullptr;
   const int64_t ldz = ((int64_t)a.V + 7) / 8 * 8;
   const bool few = grads && loss_few(a.N, a.V);
+  const bool by_rows = few && !a.dbias && a.V <= LR_THREADS * LR_EACH && p.step >= (p.cut_users ? a.N : (int64_t)a.V);
   if (few) {
     GRAM_TRY(score_logits_launch(ctx, a.users, a.ld_users, a.items, a.ld_items, a.bias, a.N, a.V, a.d, (float*)score_ws, ldz, st));
-    GRAM_TRY(logprobs_launch(ctx, score_ws, GRAM_F32, ldz, a.N, a.V, a.scale, ask, st));
+    if (!by_rows) GRAM_TRY(logprobs_launch(ctx, score_ws, GRAM_F32, ldz, a.N, a.V, a.scale, ask, st));
   } else {
     GRAM_TRY(score_logprobs_launch(ctx, a.users, a.ld_users, a.items, a.ld_items, a.bias, a.N, a.V, a.d, a.scale, ask, score_ws, score_ws_bytes, st));
     ProfScope prof(ctx, GRAM_K_OTHER, (double)a.N * (32 + (clean ? 4.0 * a.d : 0.0)), 1, st, "loss_rows");
@@ -852,7 +933,10 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
     if (few) {
       const FewArgs f{e, (const float*)score_ws, ldz, logp, stats, clean, gram_status_word(ctx)};
       ProfScope prof(ctx, GRAM_K_OTHER, (4.0 + 2 * planes) * e.rows * e.cols, 1, st, "loss_few");
-      launch_chain(planes == 3 ? loss_few_kernel<3> : planes == 2 ? loss_few_kernel<2> : loss_few_kernel<1>, dim3((unsigned)ceil_div(e.cols, 128)), 256, 0, st, a, f);
+      if (by_rows)
+        launch_chain(planes == 3 ? loss_row_kernel<3> : planes == 2 ? loss_row_kernel<2> : loss_row_kernel<1>, dim3((unsigned)a.N), LR_THREADS, 0, st, a, f);
+      else
+        launch_chain(planes == 3 ? loss_few_kernel<3> : planes == 2 ? loss_few_kernel<2> : loss_few_kernel<1>, dim3((unsigned)ceil_div(e.cols, 128)), 256, 0, st, a, f);
       GRAM_LAUNCH_CHECK(ctx);
     } else {
       GradArgs f = {};
