@@ -212,6 +212,31 @@ template <typename Pipe> __device__ __forceinline__ bool i8_products(const Pipe&
   return true;
 }
 
+// 32 sums of a token with its scale and the channels' scales and biases, to its row of a box (128-byte swizzle): 32 fp32, or 32 of 64 bf16
+template <typename CT> __device__ __forceinline__ void i8_put(uint32_t (&v)[32], float sa, const float* scale, const float* bias, uint32_t row_at, int half) {
+  const uint32_t turn = threadIdx.x & 7;
+#pragma unroll
+  for (int j = 0; j < 32; j += 4) {
+    const float4 s = *reinterpret_cast<const float4*>(scale + j), b = *reinterpret_cast<const float4*>(bias + j);
+    v[j] = __float_as_uint(fmaf((float)(int32_t)v[j] * sa, s.x, b.x));
+    v[j + 1] = __float_as_uint(fmaf((float)(int32_t)v[j + 1] * sa, s.y, b.y));
+    v[j + 2] = __float_as_uint(fmaf((float)(int32_t)v[j + 2] * sa, s.z, b.z));
+    v[j + 3] = __float_as_uint(fmaf((float)(int32_t)v[j + 3] * sa, s.w, b.w));
+  }
+  if constexpr (sizeof(CT) == 4) {
+#pragma unroll
+    for (uint32_t j = 0; j < 8; ++j) sts128(row_at + ((j ^ turn) << 4), v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+  } else {
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) {
+      uint32_t h[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[i] = pack_bf16x2(__uint_as_float(v[8 * j + 2 * i]), __uint_as_float(v[8 * j + 2 * i + 1]));
+      sts128(row_at + (((half * 4 + j) ^ turn) << 4), h[0], h[1], h[2], h[3]);
+    }
+  }
+}
+
 template <typename CT>
 __global__ void __launch_bounds__(I8Rows::THREADS, 1) gemm_i8_rows_kernel(const __grid_constant__ CUtensorMap tokens, const __grid_constant__ CUtensorMap channels,
                                                                           const __grid_constant__ CUtensorMap result, const __grid_constant__ I8Args a) {
@@ -259,26 +284,7 @@ __global__ void __launch_bounds__(I8Rows::THREADS, 1) gemm_i8_rows_kernel(const 
             if (lane == 0) bulk_wait_read_all();
             __syncwarp();
           }
-#pragma unroll
-          for (int j = 0; j < 32; j += 4) {
-            const float4 sb = *reinterpret_cast<const float4*>(of + b * 32 + j), bias = *reinterpret_cast<const float4*>(of + 64 + b * 32 + j);
-            v[j] = __float_as_uint(fmaf((float)(int32_t)v[j] * sa, sb.x, bias.x));
-            v[j + 1] = __float_as_uint(fmaf((float)(int32_t)v[j + 1] * sa, sb.y, bias.y));
-            v[j + 2] = __float_as_uint(fmaf((float)(int32_t)v[j + 2] * sa, sb.z, bias.z));
-            v[j + 3] = __float_as_uint(fmaf((float)(int32_t)v[j + 3] * sa, sb.w, bias.w));
-          }
-          if constexpr (sizeof(CT) == 4) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sts128(row_at + ((uint32_t)(j ^ (lane & 7)) << 4), v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              uint32_t h[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) h[i] = pack_bf16x2(__uint_as_float(v[8 * j + 2 * i]), __uint_as_float(v[8 * j + 2 * i + 1]));
-              sts128(row_at + ((uint32_t)((b * 4 + j) ^ (lane & 7)) << 4), h[0], h[1], h[2], h[3]);
-            }
-          }
+          i8_put<CT>(v, sa, of + b * 32, of + 64 + b * 32, row_at, b);
           if (b == 1 || sizeof(CT) == 4) {
             fence_proxy_async_smem();
             __syncwarp();
@@ -293,6 +299,179 @@ __global__ void __launch_bounds__(I8Rows::THREADS, 1) gemm_i8_rows_kernel(const 
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_remote(pipe.lead_tempty(buf));
+    }
+    if (lane == 0) bulk_wait_all();                     // its stores are complete before the block may exit
+  }
+  pipe.close(failed, a.status);
+}
+
+// ROWS where a tile's channels fit beside the stages (K of up to 768): they stay in shared memory while tile after tile of tokens passes, so that
+// what comes from L2 for a tile is half (4096 x 100 000 x 768, bf16 out, a call by itself: 290 us with both operands of each tile fetched, 244 so; 25 600 x 2304 x 768:
+// 46 and 43.5).  What bounds it now is shared memory, which operands, results and scales all pass through: the tensor cores are busy 67 % of the
+// time, and neither more warps nor a cheaper conversion of the sums changed it.  A pair takes whole columns of tiles, neighbouring pairs neighbouring ones; what is left after the last full round is cut evenly
+// over all pairs.
+constexpr int I8_HELD = 6, I8_HELD_WARPS = 8;           // k-blocks of channels that are held
+constexpr int I8_HELD_BYTES = I8_HELD * PAIR_OPERAND;
+using I8Resident = PairPipe<5, I8_HELD_WARPS, I8_HELD_BYTES + I8_HELD_WARPS * 4096 + 2 * 2 * PAIR_COLS * 4 + 2 * I8_HELD * 8, 0>;
+
+// A segment: tiles of tokens [from, to) against one tile of channels.
+struct I8Segments {
+  int channel, from, to;
+  int pair, pairs, tokens, full, at, end, round;
+  __device__ __forceinline__ explicit I8Segments(const I8Args& a) : pair(blockIdx.x >> 1), pairs(gridDim.x >> 1), tokens(a.fast), round(0) {
+    const int channels = a.total / a.fast;
+    full = channels / pairs;
+    const int64_t rest = (int64_t)(channels - full * pairs) * tokens;
+    at = (int)(rest * pair / pairs);
+    end = (int)(rest * (pair + 1) / pairs);
+  }
+  __device__ __forceinline__ bool next() {
+    if (round < full) {
+      channel = round++ * pairs + pair;
+      from = 0;
+      to = tokens;
+      return true;
+    }
+    if (at >= end) return false;
+    channel = full * pairs + at / tokens;
+    from = at % tokens;
+    to = min(tokens, from + end - at);
+    at += to - from;
+    return true;
+  }
+};
+
+template <typename CT>
+__global__ void __launch_bounds__(I8Resident::THREADS, 1) gemm_i8_resident_kernel(const __grid_constant__ CUtensorMap tokens, const __grid_constant__ CUtensorMap channels,
+                                                                                  const __grid_constant__ CUtensorMap result, const __grid_constant__ I8Args a) {
+  extern __shared__ uint8_t smem_raw[];
+  I8Resident pipe;
+  const bool go = pipe.open(smem_raw, [&]() {
+    const uint32_t bars = smem_u32(pipe.extra) + I8_HELD_BYTES + I8_HELD_WARPS * 4096 + 2 * 2 * PAIR_COLS * 4;
+    for (int kb = 0; kb < I8_HELD; ++kb) {
+      mbar_init(bars + 8 * kb, 2);                      // the two blocks' copies of a k-block of channels; used in the leader
+      mbar_init(bars + 8 * (I8_HELD + kb), 1);          // its place is free; one per block
+    }
+  });
+  const uint32_t held = smem_u32(pipe.extra), boxes = held + I8_HELD_BYTES, bars = boxes + I8_HELD_WARPS * 4096 + 2 * 2 * PAIR_COLS * 4;
+  auto held_full = [&](int kb) { return bars + 8u * kb; };
+  auto held_empty = [&](int kb) { return bars + 8u * (I8_HELD + kb); };
+  bool failed = false;
+  I8Segments seg(a);
+  if (pipe.warp == 0 && go) {
+    // ------------------------------ copies (both blocks) ------------------------------
+    const uint32_t lead_bars = map_to_cta(bars, 0);
+    int s = 0, tile = 0;
+    uint32_t ph = 0;
+    for (uint32_t n = 0; !failed && seg.next(); ++n) {
+      const int c0 = seg.channel * PAIR_COLS + (int)pipe.rank * PAIR_ROWS;
+      for (int m = seg.from; m < seg.to && !failed; ++m, ++tile) {
+        if (tile == a.give_up) { failed = true; break; }
+        const int r0 = m * 2 * PAIR_ROWS + (int)pipe.rank * PAIR_ROWS;
+        for (int kb = 0; kb < a.num_kb; ++kb) {
+          if (m == seg.from && !mbar_wait_warp(held_empty(kb), (n & 1u) ^ 1u, pipe.abort_flag)) { failed = true; break; }
+          if (!mbar_wait_warp(pipe.empty(s), ph ^ 1u, pipe.abort_flag)) { failed = true; break; }
+          if (elect_one()) {
+            if (m == seg.from) {
+              mbar_arrive_expect_tx_remote(lead_bars + 8u * kb, PAIR_OPERAND);
+              tma_load_2d_pair(held + kb * PAIR_OPERAND, &channels, kb * I8_BK, c0, lead_bars + 8u * kb);
+            }
+            mbar_arrive_expect_tx_remote(pipe.lead_full(s), PAIR_OPERAND);
+            tma_load_2d_pair(pipe.a_of(s), &tokens, kb * I8_BK, r0, pipe.lead_full(s));
+          }
+          __syncwarp();
+          if (++s == I8Resident::STAGES) { s = 0; ph ^= 1u; }
+        }
+      }
+    }
+  } else if (pipe.warp == 1 && go) {
+    // ------------------------------ products (leader) ------------------------------
+    if (pipe.rank == 0) {
+      constexpr uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(PAIR_COLS >> 3) << 17) | ((uint32_t)(2 * PAIR_ROWS >> 4) << 24);
+      const uint64_t da0 = make_desc(pipe.a_of(0), 16, 1024), db0 = make_desc(held, 16, 1024);
+      int s = 0;
+      uint32_t ph = 0, it = 0;
+      for (uint32_t n = 0; !failed && seg.next(); ++n) {
+        for (int m = seg.from; m < seg.to && !failed; ++m, ++it) {
+          const int buf = (int)(it & 1);
+          if (!mbar_wait_warp(pipe.tempty(buf), ((it >> 1) & 1) ^ 1u, pipe.abort_flag)) { failed = true; break; }
+          tc_fence_after();
+          const uint32_t tmem_d = pipe.tmem + (uint32_t)(buf * PAIR_COLS);
+          for (int kb = 0; kb < a.num_kb; ++kb) {
+            if (m == seg.from && !mbar_wait_warp(held_full(kb), n & 1u, pipe.abort_flag)) { failed = true; break; }
+            if (!mbar_wait_warp(pipe.full(s), ph, pipe.abort_flag)) { failed = true; break; }
+            tc_fence_after();
+            const uint64_t da = da0 + (uint32_t)(s * (I8Resident::STAGE >> 4)), db = db0 + (uint32_t)(kb * (PAIR_OPERAND >> 4));
+            if (elect_one()) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) i8_mma_pair(tmem_d, da + (uint64_t)(k * 2), db + (uint64_t)(k * 2), idesc, (kb > 0 || k > 0) ? 1u : 0u);
+              tc_commit_pair(pipe.empty(s));
+              if (m == seg.to - 1) tc_commit_pair(held_empty(kb));
+              if (kb == a.num_kb - 1) tc_commit_pair(pipe.tfull(buf));
+            }
+            __syncwarp();
+            if (++s == I8Resident::STAGES) { s = 0; ph ^= 1u; }
+          }
+        }
+      }
+    }
+  } else if (go) {
+    // ------------------------------ results (both blocks): a token and 128 channels a thread ------------------------------
+    const int lane = pipe.lane, q = pipe.warp & 3, half = (pipe.warp - 2) >> 2;
+    const uint32_t box = boxes + (uint32_t)(pipe.warp - 2) * 4096u, row_at = box + (uint32_t)lane * 128u;
+    uint32_t it = 0;
+    for (uint32_t n = 0; !failed && seg.next(); ++n) {
+      // The segment's scales and biases, in two places in turn: a warp that is ahead has seen all others leave the segment before the last.
+      float* of = reinterpret_cast<float*>(pipe.extra + I8_HELD_BYTES + I8_HELD_WARPS * 4096) + (n & 1) * 2 * PAIR_COLS + half * 128;
+      const int col0 = seg.channel * PAIR_COLS + half * 128;
+      float scale[4], bias[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int c = col0 + k * 32 + lane;
+        scale[k] = c < a.N ? __ldg(a.scale_b + c) : 0.f;
+        bias[k] = c < a.N && a.bias ? __ldg(a.bias + c) : 0.f;
+      }
+      for (int m = seg.from; m < seg.to; ++m, ++it) {
+        const int buf = (int)(it & 1), row0 = m * 2 * PAIR_ROWS + (int)pipe.rank * PAIR_ROWS + q * 32;
+        const bool active = row0 < a.M && col0 < a.N;   // of the warp
+        const float sa = row0 + lane < a.M ? __ldg(a.scale_a + row0 + lane) : 0.f;
+        if (!mbar_wait_warp(pipe.tfull(buf), (it >> 1) & 1, pipe.abort_flag)) { failed = true; break; }
+        tc_fence_after();
+        if (m == seg.from) {                            // (the four warps of these columns write the same)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            of[k * 32 + lane] = scale[k];
+            of[PAIR_COLS + k * 32 + lane] = bias[k];
+          }
+          __syncwarp();
+        }
+        if (active) {
+          const uint32_t taddr = pipe.tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * PAIR_COLS + half * 128);
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            uint32_t v[32];
+            tc_ld32_issue(taddr + b * 32, v);
+            tc_ld32_wait(v);
+            if (b % 2 == 0 || sizeof(CT) == 4) {        // the box's last store has read it
+              if (lane == 0) bulk_wait_read_all();
+              __syncwarp();
+            }
+            i8_put<CT>(v, sa, of + b * 32, of + PAIR_COLS + b * 32, row_at, b % 2);
+            if (b % 2 == 1 || sizeof(CT) == 4) {
+              fence_proxy_async_smem();
+              __syncwarp();
+              const int c = col0 + (sizeof(CT) == 4 ? b : b - 1) * 32;
+              if (lane == 0 && c < a.N) {
+                tma_store_2d(&result, box, c, row0);
+                bulk_commit();
+              }
+            }
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_remote(pipe.lead_tempty(buf));
+      }
     }
     if (lane == 0) bulk_wait_all();                     // its stores are complete before the block may exit
   }
@@ -402,7 +581,8 @@ gram_status gemm_i8_launch(gram_ctx* ctx, const int8_t* A, int64_t lda, const fl
   const int64_t tiles_r = ceil_div64(rows ? M : N, 2 * PAIR_ROWS), tiles_c = ceil_div64(rows ? N : M, a.width);
   if (tiles_r * tiles_c > INT32_MAX - kPairs) return gram_set_error(ctx, "gram_gemm_i8: %lld x %d are too many results", (long long)M, N), GRAM_ERR_UNSUPPORTED;
   a.total = (int32_t)(tiles_r * tiles_c);
-  a.rows_fast = tiles_r < tiles_c;
+  const bool resident = rows && a.num_kb <= I8_HELD;
+  a.rows_fast = resident || tiles_r < tiles_c;
   a.fast = (int32_t)(a.rows_fast ? tiles_r : tiles_c);
   a.give_up = gram_ring_rows(ctx);
   a.status = gram_status_word(ctx);
@@ -414,7 +594,10 @@ gram_status gemm_i8_launch(gram_ctx* ctx, const int8_t* A, int64_t lda, const fl
     return gram_set_error(ctx, "gram_gemm_i8: cannot describe the matrices"), GRAM_ERR_UNSUPPORTED;
   ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * M * N * K, 1, st, "gemm_i8");
   const int pairs = a.total < kPairs ? a.total : kPairs;
-  if (rows) {
+  if (resident) {
+    if (c_dtype == GRAM_F32) GRAM_CUDA(ctx, launch_pairs<gemm_i8_resident_kernel<float>>(pairs, I8Resident::THREADS, I8Resident::SMEM, st, tokens, channels, result, a));
+    else GRAM_CUDA(ctx, launch_pairs<gemm_i8_resident_kernel<bf16>>(pairs, I8Resident::THREADS, I8Resident::SMEM, st, tokens, channels, result, a));
+  } else if (rows) {
     if (c_dtype == GRAM_F32) GRAM_CUDA(ctx, launch_pairs<gemm_i8_rows_kernel<float>>(pairs, I8Rows::THREADS, I8Rows::SMEM, st, tokens, channels, result, a));
     else GRAM_CUDA(ctx, launch_pairs<gemm_i8_rows_kernel<bf16>>(pairs, I8Rows::THREADS, I8Rows::SMEM, st, tokens, channels, result, a));
   } else {

@@ -14,7 +14,7 @@ constexpr int PAIR_COLS = 256;                          // columns of the widest
 constexpr int PAIR_OPERAND = PAIR_ROWS * 128;           // bytes of 128 rows of 128, the swizzle's width
 constexpr int PAIR_BOX = 64 * 128;                      // bytes of a copy's box: 64 rows of 128
 
-// A stage holds `A` operands of the MMA's rows and one of its columns.  EXTRA: bytes of the kernel's own, behind the stages.
+// A stage holds `A` operands of the MMA's rows and one of its columns (none of its rows: a single operand, whichever it is).  EXTRA: bytes of the kernel's own, behind the stages.
 template <int STAGES_, int EPI_WARPS_, int EXTRA = 0, int A = 1> struct PairPipe {
   static constexpr int STAGES = STAGES_, EPI_WARPS = EPI_WARPS_, THREADS = 64 + 32 * EPI_WARPS_, STAGE = (A + 1) * PAIR_OPERAND;
   static constexpr int SMEM = STAGES * STAGE + EXTRA + 1024 + 256;
@@ -34,8 +34,11 @@ template <int STAGES_, int EPI_WARPS_, int EXTRA = 0, int A = 1> struct PairPipe
   __device__ __forceinline__ uint32_t a_of(int s, int i = 0) const { return tiles + s * STAGE + i * PAIR_OPERAND; }
   __device__ __forceinline__ uint32_t b_of(int s) const { return tiles + s * STAGE + A * PAIR_OPERAND; }
 
-  // All threads; memory of the kernels before may be touched after it.
-  __device__ __forceinline__ bool open(uint8_t* smem_raw) {
+  // All threads; memory of the kernels before may be touched after it.  more(): further barriers, initialised by one thread.
+  struct NoMore {
+    __device__ void operator()() const {}
+  };
+  template <typename F = NoMore> __device__ __forceinline__ bool open(uint8_t* smem_raw, F more = F()) {
     const uint32_t raw = smem_u32(smem_raw);
     tiles = (raw + 1023u) & ~1023u;                     // the same offset in both blocks of the pair
     extra = smem_raw + (tiles - raw) + STAGES * STAGE;
@@ -54,6 +57,7 @@ template <int STAGES_, int EPI_WARPS_, int EXTRA = 0, int A = 1> struct PairPipe
         mbar_init(tfull(b), 1);
         mbar_init(tempty(b), 2 * EPI_WARPS);
       }
+      more();
       *abort_flag = 0;
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
