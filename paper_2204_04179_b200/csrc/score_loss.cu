@@ -446,12 +446,14 @@ __global__ void __launch_bounds__(256) loss_bias_kernel(const float* part, int64
 // ============================================================================================
 // both products of a piece's g
 // ============================================================================================
-// PLANES: bf16 that g is the sum of; a stage holds all of them beside one piece of the vectors.  With one, sixteen warps take the results, 64 columns
-// each; else eight with 128, which can add up several accumulators in registers.  A warp has a box of 32 rows x 128 bytes for its results.
-template <int PLANES> using ProdPipe = PairPipe<6 - PLANES, PLANES == 1 ? 16 : 8, (PLANES == 1 ? 16 : 8) * 4096, PLANES>;
+// PLANES: bf16 that g is the sum of; a stage holds all of them beside one piece of the vectors.  CHAINED: eight warps take the results, 128 columns
+// each, which can add up several accumulators in registers; else sixteen with 64.  A warp has a box of 32 rows x 128 bytes for its results.
+template <int PLANES, bool CHAINED> using ProdPipe = PairPipe<6 - PLANES, CHAINED ? 8 : 16, (CHAINED ? 8 : 16) * 4096, PLANES>;
 
-// Blocks of 64 whose products (of both planes) are added up in one accumulator for fp32 gradients.  bf16 results hide the error of any length.
-constexpr int LP_CHAIN = 24;
+// Blocks of 64 (of all planes) that are added up in one accumulator.  The tensor cores cut off, four times a block and plane, where other sums are
+// rounded: up to 2^-23 of the sum each time, half of that on average.  fp32 gradients: 24 blocks, 1e-5 at most.  bf16: 1024 blocks, 2.4e-4 on average,
+// hidden by the result's rounding of 2^-8.
+constexpr int LP_CHAIN = 24, LP_CHAIN_BF16 = 1024;
 
 // One gradient's share in a piece.
 struct ProdSide {
@@ -537,13 +539,12 @@ __device__ __forceinline__ void box_row(uint32_t box, const float (&x)[32], uint
            pack_bf16x2(x[8 * j + 4], x[8 * j + 5]), pack_bf16x2(x[8 * j + 6], x[8 * j + 7]));
 }
 
-template <typename GT, int PLANES>
-__global__ void __launch_bounds__(ProdPipe<PLANES>::THREADS, 1)
+template <typename GT, int PLANES, bool CHAINED>
+__global__ void __launch_bounds__(ProdPipe<PLANES, CHAINED>::THREADS, 1)
     loss_products_kernel(const __grid_constant__ CUtensorMap g0, const __grid_constant__ CUtensorMap g1, const __grid_constant__ CUtensorMap g2,
                          const __grid_constant__ CUtensorMap users, const __grid_constant__ CUtensorMap items, const __grid_constant__ CUtensorMap out_u,
                          const __grid_constant__ CUtensorMap out_i, const __grid_constant__ ProdArgs a) {
-  constexpr bool CHAINED = sizeof(GT) == 4;
-  using Pipe = ProdPipe<PLANES>;
+  using Pipe = ProdPipe<PLANES, CHAINED>;
   extern __shared__ uint8_t smem_raw[];
   Pipe pipe;
   const bool go = pipe.open(smem_raw);
@@ -624,7 +625,7 @@ __global__ void __launch_bounds__(ProdPipe<PLANES>::THREADS, 1)
     }
   } else if (go) {
     // ------------------------------ results (both blocks): a row and 64 or 128 columns a thread ------------------------------
-    constexpr int BLOCKS = PLANES == 1 ? 2 : 4;         // of 32 columns
+    constexpr int BLOCKS = CHAINED ? 4 : 2;             // of 32 columns
     const int lane = pipe.lane, q = pipe.warp & 3, part = (pipe.warp - 2) >> 2;
     const uint32_t lane_addr = pipe.tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(part * BLOCKS * 32);
     const uint32_t box = pipe.tiles + Pipe::STAGES * Pipe::STAGE + (uint32_t)(pipe.warp - 2) * 4096u;
@@ -661,7 +662,6 @@ __global__ void __launch_bounds__(ProdPipe<PLANES>::THREADS, 1)
         }
       };
       if constexpr (CHAINED) {
-        // The tensor cores cut off where this adds with rounding: a chain's length sets the sum's precision.
         float acc[4][32];
 #pragma unroll
         for (int b = 0; b < 4; ++b)
@@ -1005,17 +1005,19 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
     w.extra = span.extra;
     w.halves = span.halves;
     w.total = w.of[0].units + w.of[1].units;
-    w.chain = LP_CHAIN;
+    w.chain = f32 ? LP_CHAIN : LP_CHAIN_BF16;
     w.give_up = gram_ring_rows(ctx);
     w.status = gram_status_word(ctx);
     ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * planes * e.rows * e.cols * a.d * ((a.dusers != nullptr) + (a.ditems != nullptr)), 1, st, "loss_products");
     const int pairs = w.total < kPairs ? w.total : kPairs;
-#define LOSS_PRODUCTS(GT, PLANES)                                                                                                                   \
-  launch_pairs<loss_products_kernel<GT, PLANES>>(pairs, ProdPipe<PLANES>::THREADS, ProdPipe<PLANES>::SMEM, st, map_g[0], map_g[1], map_g[2], map_clean, map_i, \
-                                                 map_out[0], map_out[1], w)
-    if (planes == 1) GRAM_CUDA(ctx, LOSS_PRODUCTS(bf16, 1));
-    else if (planes == 2) GRAM_CUDA(ctx, LOSS_PRODUCTS(float, 2));
-    else GRAM_CUDA(ctx, LOSS_PRODUCTS(float, 3));
+#define LOSS_PRODUCTS(GT, PLANES, CHAINED)                                                                                                            \
+  launch_pairs<loss_products_kernel<GT, PLANES, CHAINED>>(pairs, ProdPipe<PLANES, CHAINED>::THREADS, ProdPipe<PLANES, CHAINED>::SMEM, st, map_g[0], map_g[1], \
+                                                          map_g[2], map_clean, map_i, map_out[0], map_out[1], w)
+    const bool chained = (w.of[0].units && w.of[0].kb_split > LP_CHAIN_BF16) || (w.of[1].units && w.of[1].kb_split > LP_CHAIN_BF16);
+    if (planes == 1 && !chained) GRAM_CUDA(ctx, LOSS_PRODUCTS(bf16, 1, false));
+    else if (planes == 1) GRAM_CUDA(ctx, LOSS_PRODUCTS(bf16, 1, true));
+    else if (planes == 2) GRAM_CUDA(ctx, LOSS_PRODUCTS(float, 2, true));
+    else GRAM_CUDA(ctx, LOSS_PRODUCTS(float, 3, true));
 #undef LOSS_PRODUCTS
   }
   if (joined) {

@@ -49,6 +49,18 @@ class Encoder:
         self.gram.gather(self.H, histories, E)
         return E.view(*histories.shape, -1).mean(1).to(torch.bfloat16)
 
+    def of_histories(self, G: torch.Tensor, dU: torch.Tensor, histories: torch.Tensor):
+        """Adds to the items' gradients G [n_items, d] what the users' gradients dU [N, d] leave in their histories' items."""
+        g, (N, L), (V, d), dev = self.gram, histories.shape, self.H.shape, self.H.device
+        P = N * L
+        index = lambda n: torch.empty(n, dtype=torch.int32, device=dev)  # noqa: E731
+        unique, inverse, perm, seg_off, count = index(P), index(P), index(P), index(P + 1), index(1)
+        g.dedup(histories, V, unique, inverse, perm, seg_off, count)
+        U = int(count)
+        sums = torch.empty(U, d, device=dev)
+        g.accumulate((dU / L).repeat_interleave(L, 0), perm, seg_off, U, sums)
+        G[unique[:U].long()] += sums
+
     def answer(self, histories: torch.Tensor, clicks: torch.Tensor, k: int, scale: float):
         """(Answers, log probabilities of the best k items)."""
         N, f = len(histories), dict(device=self.H.device, dtype=torch.float32)
@@ -82,14 +94,7 @@ class Student(Encoder):
         G, dU = new(V, d), new(N, d)
         g.gemm_bf16(dz, False, users, False, G, None, False, V, d, N)
         g.gemm_bf16(dz, True, items, False, dU, None, False, N, d, V)
-        P = N * L
-        index = lambda n: torch.empty(n, dtype=torch.int32, device=dev)  # noqa: E731
-        unique, inverse, perm, seg_off, count = index(P), index(P), index(P), index(P + 1), index(1)
-        g.dedup(histories, V, unique, inverse, perm, seg_off, count)
-        U = int(count)
-        sums = new(U, d)
-        g.accumulate((dU / L).repeat_interleave(L, 0), perm, seg_off, U, sums)
-        G[unique[:U].long()] += sums
+        self.of_histories(G, dU, histories)
         g.zero_grads(binding.GRAM_MODULE_CE)
         g.encoder_backward(G, self.pool, V)
         return loss, logp[:, 0], entropy
