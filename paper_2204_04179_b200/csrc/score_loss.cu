@@ -98,21 +98,25 @@ template <int PLANES> __global__ void __launch_bounds__(256) loss_few_kernel(con
   chain_next();
   if (!chain_begin()) return;
   __shared__ float4 sums[8][32];
+  __shared__ RowConst row[LOSS_FEW];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 128 + 4 * lane;
   const Piece& at = f.at;
+  const int rows = (int)at.rows;                        // LOSS_FEW at most
+  if (threadIdx.x < rows) row[threadIdx.x] = loss_row(a, f.logp, f.stats, at.n0 + threadIdx.x);
+  __syncthreads();
   if (at.first == 0)
-    for (int64_t i = blockIdx.x + (int64_t)warp * gridDim.x; i < at.rows; i += 8 * (int64_t)gridDim.x) {
-      const int64_t n = at.n0 + i;
-      if (lane == 0) a.loss[n] = loss_of(a, f.logp, n, f.status);
-      if (f.clean) loss_clean(a, n, loss_row(a, f.logp, f.stats, n).t >= 0, f.clean);
+    for (int i = blockIdx.x + warp * (int)gridDim.x; i < rows; i += 8 * (int)gridDim.x) {
+      if (lane == 0) a.loss[at.n0 + i] = loss_of(a, f.logp, at.n0 + i, f.status);
+      if (f.clean) loss_clean(a, at.n0 + i, row[i].t >= 0, f.clean);
     }
   const float c = a.scale * kLog2e;
   float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
   if (col < at.cols) {
-#pragma unroll 4
-    for (int64_t i = warp; i < at.rows; i += 8) {
-      const float4 z = *reinterpret_cast<const float4*>(f.z + (at.n0 + i) * f.ldz + at.first + col);
-      const RowConst r = loss_row(a, f.logp, f.stats, at.n0 + i);
+    const float* z_at = f.z + at.n0 * f.ldz + at.first + col;
+#pragma unroll 8
+    for (int i = warp; i < rows; i += 8) {
+      const float4 z = *reinterpret_cast<const float4*>(z_at + i * f.ldz);
+      const RowConst r = row[i];
       float g[4] = {loss_p(r, z.x, c), loss_p(r, z.y, c), loss_p(r, z.z, c), loss_p(r, z.w, c)};
       const int hot = r.t - at.first - col;
 #pragma unroll
