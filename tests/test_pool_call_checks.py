@@ -54,7 +54,7 @@ def test_workspaces(N, V, d, dtype):
     least, best = binding.Gram.score_loss_workspace(N, V, d, dtype)
     n, planes = max(N, 1), (4, 6) if dtype == torch.float32 else (2, 2)
     short = min(n, V)
-    fixed = 28 * n + 2 * n * d + 4 * ((short + 255) // 256 * 256) * d
+    fixed = 36 * n + 2 * n * d + 4 * ((short + 255) // 256 * 256) * d
     assert fixed + planes[0] * 256 * short <= least <= fixed + 6 * 256 * (short + 256) + 8 * 32 * (short + 256) + 4096
     assert least <= best <= max(2 * least, fixed * 33 + (257 << 20) * 17 // 16 + (planes[1] + 1) * 256 * (short + 256))
 
