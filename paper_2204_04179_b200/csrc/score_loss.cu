@@ -254,12 +254,33 @@ struct GradArgs {
   RowRest* rest;                 // [N] or null
   const float* bias;             // [V] or null
   int32_t V;
-  int32_t num_kb, tiles_m, total, width;
+  int32_t num_kb, tiles_m, width;
+  int32_t whole, total;          // tiles before those at the end that are dealt as two of half the width; of all, halves counted twice
   int32_t box_rows;              // users of a copy
   float c;
   float* bias_part;              // [32-row blocks of the piece, ldg] or null
   int32_t give_up;
   int32_t* status;
+};
+
+// first user and item of the piece, and width, of the t-th tile
+struct GradTile {
+  int m0, n0, width;
+  __device__ __forceinline__ GradTile(const GradArgs& a, int t) {
+    int half = -1;
+    if (t >= a.whole) {
+      half = (t - a.whole) & 1;
+      t = a.whole + ((t - a.whole) >> 1);
+    }
+    const int n = t / a.tiles_m;
+    m0 = (t - n * a.tiles_m) * 2 * PAIR_ROWS;
+    n0 = n * a.width;
+    width = a.width;
+    if (half >= 0) {
+      width = PAIR_COLS / 2;
+      n0 += half * width;
+    }
+  }
 };
 
 // the sum of column l of a 32 x 32 block whose rows the lanes hold, in lane l: halves of the columns are exchanged in turn
@@ -296,10 +317,10 @@ __global__ void __launch_bounds__(GradPipe::THREADS, 1) loss_grad_kernel(const _
     uint32_t ph = 0;
     for (int t = pair; t < a.total && !failed; t += pairs, ++tile) {
       if (tile == a.give_up) { failed = true; break; }
-      const int m0 = (t % a.tiles_m) * 2 * PAIR_ROWS + (int)pipe.rank * PAIR_ROWS;
-      const int n0 = a.at.first + (t / a.tiles_m) * a.width + (int)pipe.rank * (a.width / 2);
+      const GradTile u(a, t);
+      const int m0 = u.m0 + (int)pipe.rank * PAIR_ROWS, n0 = a.at.first + u.n0 + (int)pipe.rank * (u.width / 2);
       const bool some = m0 < a.at.rows;                 // what the rows of users past the last hold is not looked at
-      const uint32_t bytes = (some ? (uint32_t)a.box_rows * 128u : 0u) + (uint32_t)a.width * 64u;
+      const uint32_t bytes = (some ? (uint32_t)a.box_rows * 128u : 0u) + (uint32_t)u.width * 64u;
       for (int kb = 0; kb < a.num_kb; ++kb) {
         if (!mbar_wait_warp(pipe.empty(s), ph ^ 1u, pipe.abort_flag)) { failed = true; break; }
         const uint32_t bar = pipe.lead_full(s);
@@ -307,7 +328,7 @@ __global__ void __launch_bounds__(GradPipe::THREADS, 1) loss_grad_kernel(const _
           mbar_arrive_expect_tx_remote(bar, bytes);
           if (some) tma_load_2d_pair(pipe.a_of(s), &users, kb * 64, (int)a.at.n0 + m0, bar);
           tma_load_2d_pair(pipe.b_of(s), &items, kb * 64, n0, bar);
-          if (a.width == PAIR_COLS) tma_load_2d_pair(pipe.b_of(s) + PAIR_BOX, &items, kb * 64, n0 + 64, bar);
+          if (u.width == PAIR_COLS) tma_load_2d_pair(pipe.b_of(s) + PAIR_BOX, &items, kb * 64, n0 + 64, bar);
         }
         __syncwarp();
         if (++s == LG_STAGES) { s = 0; ph ^= 1u; }
@@ -316,11 +337,12 @@ __global__ void __launch_bounds__(GradPipe::THREADS, 1) loss_grad_kernel(const _
   } else if (pipe.warp == 1 && go) {
     // ------------------------------ products (leader) ------------------------------
     if (pipe.rank == 0) {
-      const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(a.width >> 3) << 17) | ((uint32_t)(2 * PAIR_ROWS >> 4) << 24);
+      constexpr uint32_t idesc0 = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(2 * PAIR_ROWS >> 4) << 24);
       const uint64_t da0 = make_desc(pipe.a_of(0), 16, 1024), db0 = make_desc(pipe.b_of(0), 16, 1024);
       int s = 0;
       uint32_t ph = 0, it = 0;
       for (int t = pair; t < a.total && !failed; t += pairs, ++it) {
+        const uint32_t idesc = idesc0 | ((uint32_t)(GradTile(a, t).width >> 3) << 17);
         const int buf = (int)(it & 1);
         if (!mbar_wait_warp(pipe.tempty(buf), ((it >> 1) & 1) ^ 1u, pipe.abort_flag)) { failed = true; break; }
         tc_fence_after();
@@ -345,13 +367,14 @@ __global__ void __launch_bounds__(GradPipe::THREADS, 1) loss_grad_kernel(const _
     // ------------------------------ g (both blocks) ------------------------------
     const int lane = pipe.lane, q = pipe.warp & 3, part = (pipe.warp - 2) >> 2;
     float* bias_w = reinterpret_cast<float*>(pipe.extra) + (pipe.warp - 2) * 64;
-    const int blocks = a.width / PAIR_ROWS;             // of 32 columns of this warp
     const f32x2 cc = x2_pack(a.c, a.c);
     uint32_t it = 0;
     for (int t = pair; t < a.total && !failed; t += pairs, ++it) {
       const int buf = (int)(it & 1);
-      const int col_t = part * blocks * 32, col0 = (t / a.tiles_m) * a.width + col_t;      // of the tile, of the piece
-      const int64_t n = (int64_t)(t % a.tiles_m) * 2 * PAIR_ROWS + (int)pipe.rank * PAIR_ROWS + q * 32 + lane;      // of the piece
+      const GradTile u(a, t);
+      const int blocks = u.width / PAIR_ROWS;           // of 32 columns of this warp
+      const int col_t = part * blocks * 32, col0 = u.n0 + col_t;                // of the tile, of the piece
+      const int64_t n = (int64_t)u.m0 + (int)pipe.rank * PAIR_ROWS + q * 32 + lane;        // of the piece
       const bool active = n - lane < a.at.rows;         // of the warp
       RowConst r{0.f, 0.f, 0.f, -1};
       const float* bias = nullptr;
@@ -992,7 +1015,9 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
       f.num_kb = ceil_div(a.d, 64);
       f.tiles_m = (int32_t)ceil_div64(e.rows, 2 * PAIR_ROWS);
       f.width = (int64_t)f.tiles_m * ceil_div(e.cols, PAIR_COLS) < kPairs ? PAIR_COLS / 2 : PAIR_COLS;    // tiles of half the width where they leave pairs idle
-      f.total = f.tiles_m * ceil_div(e.cols, f.width);
+      const int32_t tiles = f.tiles_m * ceil_div(e.cols, f.width), last = tiles % kPairs;
+      f.whole = f.width == PAIR_COLS && last > 0 && 2 * last <= kPairs ? tiles - last : tiles;
+      f.total = f.whole + 2 * (tiles - f.whole);
       f.box_rows = box_rows;
       f.c = a.scale * kLog2e;
       f.bias_part = a.dbias ? (float*)(base + p.bias) : nullptr;
