@@ -369,9 +369,10 @@ gram_status gram_score_logprobs(gram_ctx* ctx, const void* d_users, int64_t ld_u
  * it holds, reaches nothing else.  A row that holds NaN or +inf has loss NaN, and so have the gradients it takes part in.
  * d_dusers and d_ditems are `grad_dtype`, rows a multiple of 16 bytes apart, 16-byte aligned, d a multiple of 8 (GRAM_ERR_UNSUPPORTED
  * else); they must not overlap the inputs or each other.  For GRAM_BF16 g is rounded to bf16 before the two products, as a gradient that passes through
- * bf16 is; for GRAM_F32 it enters them as the sum of two bf16 (to 2^-16 of itself), at half again the cost.
- * g is formed for a piece of the items at a time in d_workspace, 256-byte aligned device memory of the caller's: as large a piece as
- * workspace_bytes allow.  Its content means nothing before and after; calls that may run at the same time need one each.  The call also uses the
+ * bf16 is; for GRAM_F32 it enters them as the sum of two bf16 (to 2^-16 of itself; of three for short products of few users), at half again the cost.
+ * d_dbias is summed in fp32 from g itself.
+ * g is formed for a piece of the items (of the users where they are more) at a time in d_workspace, 256-byte aligned device memory of the caller's: as
+ * large a piece as workspace_bytes allow.  Its content means nothing before and after; calls that may run at the same time need one each.  The call also uses the
  * context's workspace for matrix products.  Results depend, within rounding, on the size of the workspace, and repeat bit for bit. */
 gram_status gram_score_loss(gram_ctx* ctx, const void* d_users, int64_t ld_users, const void* d_items, int64_t ld_items, const float* d_bias,
                             int64_t N, int32_t V, int32_t d, float scale, const int32_t* d_targets, const float* d_weight, float* d_loss,

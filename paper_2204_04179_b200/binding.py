@@ -419,7 +419,7 @@ class Gram:
         p, ld, q, ld_items, N, d, V = _vectors(users, items)
         gu, ld_gu, type_u = _vector_gradient(dusers, N, d, "dusers")
         gi, ld_gi, type_i = _vector_gradient(ditems, V, d, "ditems")
-        room = workspace.numel()
+        room = 0 if workspace is None else workspace.numel()
         if type_u is not None and type_i is not None and type_u != type_i:
             raise GramError(1, f"dusers and ditems: one type is needed, not {dusers.dtype} and {ditems.dtype}")
         self._ck(lib().gram_score_loss(self._h, p, ld, q, ld_items, _array(bias, "f", V, "bias"), N, V, d, scale, _array(targets, "i", N, "targets"),

@@ -620,9 +620,11 @@ gram_status gram_quantize_rows(gram_ctx* ctx, const void* d_x, int dtype, int64_
   const char* name = "gram_quantize_rows";
   ROWS_ARG(rows >= 0 && rows <= INT32_MAX, "rows must be in [0, 2^31)");
   ROWS_ARG(cols >= 1, "cols must be positive");
-  GRAM_TRY(check_logits(ctx, name, d_x, dtype, ld, rows, cols));
+  ROWS_ARG(dtype == GRAM_F32 || dtype == GRAM_BF16, "unknown dtype");
+  ROWS_ARG(ld >= cols && ld <= INT64_MAX / 8 / (rows > 0 ? rows : 1), "rows must be at least cols elements apart");
+  ROWS_ARG(reinterpret_cast<uintptr_t>(d_x) % (dtype == GRAM_F32 ? 4 : 2) == 0, "an address that the type does not allow");
   ROWS_ARG(ld_codes >= cols && ld_codes <= INT64_MAX / 8 / (rows > 0 ? rows : 1), "rows of codes must be at least cols apart");
-  ROWS_ARG(rows == 0 || (d_codes && d_scale), "null codes or scales");
+  ROWS_ARG(rows == 0 || (d_x && d_codes && d_scale), "null rows, codes or scales");
   if (rows == 0) return GRAM_OK;
   return quantize_rows_launch(ctx, d_x, dtype, ld, rows, cols, d_codes, ld_codes, d_scale, S(stream));
 }

@@ -23,8 +23,10 @@ namespace {
 using namespace tc;
 
 constexpr int kPairs = kNumSMs / 2;
-constexpr int LOSS_FEW = 256;                           // users whose logits are kept where 32 MB hold them
-constexpr int LOSS_SHORT = 8 * kPairs;                  // blocks of 64 items x 256 columns that an SM pair takes a plane of in 2 us
+// Users whose logits are kept where 32 MB hold them.  us so and with a second product: 64 users, 100 000 items of 768 128 and 160, 260 and 30 000
+// 89 and 94, 512 and 15 000 60 and 69, but 1000 and 8000 68 and 61 (rows are too many for a block's eight warps).
+constexpr int LOSS_FEW = 512;
+constexpr int LOSS_SHORT = 8 * kPairs;                  // blocks of 64 items x 256 columns whose products take the pairs 2 us for each plane
 
 // ============================================================================================
 // rows: loss, and the constants of g
@@ -113,7 +115,7 @@ template <int PLANES> __global__ void __launch_bounds__(256) loss_few_kernel(con
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 128 + 4 * lane;
   const Piece& at = f.at;
   const int rows = (int)at.rows;                        // LOSS_FEW at most
-  if (threadIdx.x < rows) row[threadIdx.x] = loss_row(a, f.logp, f.stats, at.n0 + threadIdx.x);
+  for (int i = threadIdx.x; i < rows; i += 256) row[i] = loss_row(a, f.logp, f.stats, at.n0 + i);
   __syncthreads();
   if (at.first == 0)
     for (int i = blockIdx.x + warp * (int)gridDim.x; i < rows; i += 8 * (int)gridDim.x) {
@@ -943,7 +945,7 @@ void score_loss_workspace(int64_t N, int32_t V, int32_t d, int grad_dtype, size_
 gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_t ws_bytes, void* score_ws, size_t score_ws_bytes, cudaStream_t st) {
   const bool grads = a.dusers || a.ditems || a.dbias;
   const bool f32 = a.grad_dtype == GRAM_F32;
-  const int planes = loss_planes(a.N, a.V, a.d, a.grad_dtype);
+  const int planes = a.dusers || a.ditems ? loss_planes(a.N, a.V, a.d, a.grad_dtype) : 1;
   const LossPlan p = loss_plan(a.N, a.V, a.d, planes, f32, a.dusers != nullptr, a.ditems != nullptr, a.dbias != nullptr, 0, ws_bytes ? ws_bytes : 1);
   const size_t need = grads ? p.bytes : p.rows;
   if (need > ws_bytes)
