@@ -366,7 +366,7 @@ gram_status gram_score_logprobs(gram_ctx* ctx, const void* d_users, int64_t ld_u
  *   d_dusers[n, :] = sum_v g[n, v] items[v, :]     d_ditems[v, :] = sum_n g[n, v] users[n, :]     d_dbias[v] = sum_n g[n, v]
  * d_targets int32 [N], d_weight fp32 [N] or NULL (all 1), d_loss fp32 [N], d_dbias fp32 [V] (asked without d_bias too: that of zeros).  A row
  * takes no part in the gradients if its target is "none" or taken out or its weight 0: its row of d_dusers is 0, and its vector, whatever
- * it holds, reaches nothing else.  A row that holds NaN or +inf has loss NaN, and so have the gradients it takes part in.
+ * it holds, reaches nothing else (an item that d_bias takes out must be finite all the same).  A row that holds NaN or +inf has loss NaN, and so have the gradients it takes part in.
  * d_dusers and d_ditems are `grad_dtype`, rows a multiple of 16 bytes apart, 16-byte aligned, d a multiple of 8 (GRAM_ERR_UNSUPPORTED
  * else); they must not overlap the inputs or each other.  For GRAM_BF16 g is rounded to bf16 before the two products, as a gradient that passes through
  * bf16 is; for GRAM_F32 it enters them as the sum of two bf16 (to 2^-16 of itself; of three for short products of few users), at half again the cost.
