@@ -11,8 +11,12 @@
 //      gradients as the sum of two bf16: 2^-16 of each entry); loss_products_kernel takes both products of it, g I and g^T U, in one launch of tiles
 //      of either kind.  Where pieces are of items, those of g^T U are done with the piece and g I is summed over all; else the other way round.
 //   4. loss_finish_kernel: the summed gradient from its parts.
+// Where users are few and their logits fit 32 MB they are kept in L2 after all, and a kernel of elementwise work takes the place of the second product.
 // Bounded by the tensor cores where users are many: 8 N V d flops (12 with fp32 gradients), of which the products that cannot be done
-// without are 6; by the table's bytes, read three times and written once, where they are few.
+// without are 6; by the table's bytes, read twice and written once, where they are few.  Measured, vectors of 768: 4096 users against 100 000 items
+// 1700 us in a call by itself (1480 TFLOP/s of the 8 N V d) and 2070 in a loop of calls under the power cap (1220); against 30 522 with bias 548 and 675;
+// 25 600 users against 10 000 items, fp32 gradients, 1750 and 2070 (12 N V d: 1350 TFLOP/s by itself); 64 users against 100 000 120 in a graph of calls
+// (three passes over the table's 154 MB at 3.8 TB/s), one user against 10 000 27.
 #include "score_loss.h"
 
 #include "logits.h"
@@ -505,9 +509,10 @@ __global__ void __launch_bounds__(256) loss_bias_kernel(const float* part, int64
 template <int PLANES, bool CHAINED> using ProdPipe = PairPipe<6 - PLANES, CHAINED ? 8 : 16, (CHAINED ? 8 : 16) * 4096, PLANES>;
 
 // Blocks of 64 (of all planes) that are added up in one accumulator.  The tensor cores cut off, four times a block and plane, where other sums are
-// rounded: up to 2^-23 of the sum each time, half of that on average.  fp32 gradients: 24 blocks, 1e-5 at most.  bf16: 1024 blocks, 2.4e-4 on average,
-// hidden by the result's rounding of 2^-8.
-constexpr int LP_CHAIN = 24, LP_CHAIN_BF16 = 1024;
+// rounded: up to 2^-23 of the sum each time, half of that on average.  fp32 gradients of 25 600 users and 10 000 items of 768 against 64 bits: 4.2e-6 from
+// chains of 24 blocks, 2.65e-6 from 8 (of which g's rounding is 2.3e-6), 2.4e-6 from 4; 1767, 1770 and 1778 us.  bf16: 1024 blocks, 2.4e-4 on average, hidden by
+// the result's rounding of 2^-8.
+constexpr int LP_CHAIN = 8, LP_CHAIN_BF16 = 1024;
 
 // One gradient's share in a piece.
 struct ProdSide {
