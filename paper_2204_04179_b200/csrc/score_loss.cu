@@ -247,6 +247,146 @@ template <int PLANES> __global__ void __launch_bounds__(LR_THREADS) loss_row_ker
   }
 }
 
+// Up to four users: both products by lanes.  What they cost is the table's bytes, read and written once; a tile of the tensor cores would be 256 users, with
+// bf16 entries.  A block takes `chunk` items and 256 columns: g of its items in 32 bits from logits in L2, then a warp an item at a time, a lane eight columns of
+// it: dI leaves, dU and db are summed on the way.  us of a call in a graph, by tensor cores and so: 1 x 10 000 x 768 25.6 and 20.6, 1 x 148 184 x 728
+// with fp32 gradients 226 and 187, 4 x 2000 x 768 fp32 21.6 and 16.2, 4 x 100 000 x 768 111 and 113.  Eight items ahead for four took 22.4 for 20.6.
+constexpr int LO_USERS = 4, LO_CHUNK = 512;             // most items of a block
+constexpr int LO_AHEAD = 4;                             // items of a warp whose loads are on their way together
+struct OneArgs {
+  const float* z;                // [N, ldz]
+  int64_t ldz;
+  const float* logp;
+  const float2* stats;
+  int32_t chunk, wide;           // wide: rows of dI begin on 32 bytes
+  float* parts;                  // [chunks, N, d]: dU
+  int32_t* status;
+};
+__device__ __forceinline__ void st32(void* p, const uint32_t* v) {        // 32 bytes, 32-byte aligned
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]),
+               "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+template <typename GT> __device__ __forceinline__ void put8(GT* to, const f32x2 (&x)[4], bool wide) {        // wide: 32-byte aligned (fp32: whole sectors)
+  uint32_t h[8];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 f = x2_unpack(x[j]);
+    if constexpr (sizeof(GT) == 4) {
+      h[2 * j] = __float_as_uint(f.x);
+      h[2 * j + 1] = __float_as_uint(f.y);
+    } else {
+      h[j] = pack_bf16x2(f.x, f.y);
+    }
+  }
+  uint4* q = reinterpret_cast<uint4*>(to);
+  if (sizeof(GT) == 4 && wide) {
+    st32(to, h);
+  } else {
+    q[0] = make_uint4(h[0], h[1], h[2], h[3]);
+    if constexpr (sizeof(GT) == 4) q[1] = make_uint4(h[4], h[5], h[6], h[7]);
+  }
+}
+__device__ __forceinline__ void get8(uint4 w, f32x2 (&x)[4]) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = x2_pack(__uint_as_float(u[j] << 16), __uint_as_float(u[j] & 0xffff0000u));
+}
+template <typename GT, int USERS> __global__ void __launch_bounds__(256) loss_one_kernel(const ScoreLoss a, const OneArgs f) {
+  chain_next();
+  if (!chain_begin()) return;
+  __shared__ float g[USERS][LO_CHUNK];
+  __shared__ __align__(16) float sums[8][USERS][256];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, N = (int)a.N;
+  const int v0 = blockIdx.x * f.chunk, rows = min(f.chunk, a.V - v0), col = blockIdx.y * 256 + 8 * lane;
+  const float c = a.scale * kLog2e;
+  RowConst r[USERS];
+#pragma unroll
+  for (int n = 0; n < USERS; ++n) r[n] = n < N ? loss_row(a, f.logp, f.stats, n) : RowConst{0.f, 0.f, 0.f, -1};
+  if (blockIdx.x == 0 && blockIdx.y == 0 && (int)threadIdx.x < N) a.loss[threadIdx.x] = loss_of(a, f.logp, threadIdx.x, f.status);
+  for (int i = threadIdx.x; i < rows; i += 256) {
+    float sum = 0.f;
+#pragma unroll
+    for (int n = 0; n < USERS; ++n) {
+      float x = 0.f;
+      if (r[n].t >= 0) {
+        const float p = loss_p(r[n], f.z[n * f.ldz + v0 + i], c);
+        x = r[n].f * (v0 + i == r[n].t ? p - 1.f : p);
+      }
+      g[n][i] = x;
+      sum += x;
+    }
+    if (a.dbias && blockIdx.y == 0) a.dbias[v0 + i] = sum;
+  }
+  __syncthreads();
+  f32x2 u[USERS][4], acc[USERS][4];
+#pragma unroll
+  for (int n = 0; n < USERS; ++n) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) u[n][j] = acc[n][j] = x2_pack(0.f, 0.f);
+    if (r[n].t >= 0 && col < a.d) get8(__ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(a.users) + n * a.ld_users + col)), u[n]);
+  }
+  if (col < a.d) {
+    const bf16* items = reinterpret_cast<const bf16*>(a.items) + (int64_t)v0 * a.ld_items + col;
+    GT* out = reinterpret_cast<GT*>(a.ditems) + (int64_t)v0 * a.ld_ditems + col;
+    for (int i0 = warp; i0 < rows; i0 += 8 * LO_AHEAD) {
+      uint4 raw[LO_AHEAD];                              // all loads on their way before the first store
+#pragma unroll
+      for (int k = 0; k < LO_AHEAD; ++k)
+        if (a.dusers && i0 + 8 * k < rows) raw[k] = __ldg(reinterpret_cast<const uint4*>(items + (i0 + 8 * k) * a.ld_items));
+#pragma unroll
+      for (int k = 0; k < LO_AHEAD; ++k) {
+        const int i = i0 + 8 * k;
+        if (i >= rows) break;
+        f32x2 x[4], w[4];
+        get8(raw[k], w);
+#pragma unroll
+        for (int n = 0; n < USERS; ++n) {
+          const f32x2 gn = x2_pack(g[n][i], g[n][i]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            x[j] = n == 0 ? x2_mul(gn, u[n][j]) : x2_fma(gn, u[n][j], x[j]);
+            acc[n][j] = x2_fma(gn, w[j], acc[n][j]);    // not looked at where dU is not asked
+          }
+        }
+        if (a.ditems) put8(out + i * a.ld_ditems, x, f.wide);
+      }
+    }
+  }
+  if (!a.dusers) return;
+#pragma unroll
+  for (int n = 0; n < USERS; ++n)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) *reinterpret_cast<float2*>(&sums[warp][n][8 * lane + 2 * j]) = x2_unpack(acc[n][j]);
+  __syncthreads();
+  const int at = blockIdx.y * 256 + (int)threadIdx.x;
+  if (at >= a.d) return;
+#pragma unroll
+  for (int n = 0; n < USERS; ++n) {
+    float x = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) x += sums[w][n][threadIdx.x];
+    if (n < N) f.parts[((int64_t)blockIdx.x * N + n) * a.d + at] = x;
+  }
+}
+// their dU: a block takes 32 columns of a user, its warps the parts in turn
+template <typename GT> __global__ void __launch_bounds__(1024) loss_one_finish_kernel(const float* parts, int32_t chunks, int32_t d, int64_t stride, GT* dU, int64_t ld) {
+  if (!chain_begin()) return;
+  __shared__ float sums[32][33];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
+  float s = 0.f;
+  if (col < d) {
+#pragma unroll 8
+    for (int k = warp; k < chunks; k += 32) s += parts[k * stride + (int64_t)blockIdx.y * d + col];
+  }
+  sums[warp][lane] = s;
+  __syncthreads();
+  s = sums[lane][warp];                                 // of column `warp` now, a part a lane
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (lane == 0 && blockIdx.x * 32 + warp < d) dU[blockIdx.y * ld + blockIdx.x * 32 + warp] = row_round<GT>(s);
+}
+
 // ============================================================================================
 // g of a piece
 // ============================================================================================
@@ -302,11 +442,6 @@ __device__ __forceinline__ float column_sums(float (&v)[32]) {
     }
   }
   return v[0];
-}
-__device__ __forceinline__ void st32(void* p, const uint32_t* v) {        // 32 bytes, 32-byte aligned
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]),
-               "r"(v[5]), "r"(v[6]), "r"(v[7])
-               : "memory");
 }
 
 template <int PLANES>
@@ -505,8 +640,9 @@ __global__ void __launch_bounds__(256) loss_bias_kernel(const float* part, int64
 // both products of a piece's g
 // ============================================================================================
 // PLANES: bf16 that g is the sum of; a stage holds all of them beside one piece of the vectors.  CHAINED: eight warps take the results, 128 columns
-// each, which can add up several accumulators in registers; else sixteen with 64.  A warp has a box of 32 rows x 128 bytes for its results.
-template <int PLANES, bool CHAINED> using ProdPipe = PairPipe<6 - PLANES, CHAINED ? 8 : 16, (CHAINED ? 8 : 16) * 4096, PLANES>;
+// each, which can add up several accumulators in registers; else sixteen with 64.  A warp has a box of 32 rows x 128 bytes for its results,
+// two in turn where there are eight (46 users, 5545 items of 440, fp32 gradients 26.9 -> 24.3 us; sums of many users the same with a stage less).
+template <int PLANES, bool CHAINED> using ProdPipe = PairPipe<PLANES == 1 ? 5 : 5 - PLANES, CHAINED ? 8 : 16, 16 * 4096, PLANES>;
 
 // Blocks of 64 (of all planes) that are added up in one accumulator.  The tensor cores cut off, four times a block and plane, where other sums are
 // rounded: up to 2^-23 of the sum each time, half of that on average.  fp32 gradients of 25 600 users and 10 000 items of 768 against 64 bits: 4.2e-6 from
@@ -687,8 +823,9 @@ __global__ void __launch_bounds__(ProdPipe<PLANES, CHAINED>::THREADS, 1)
     constexpr int BLOCKS = CHAINED ? 4 : 2;             // of 32 columns
     const int lane = pipe.lane, q = pipe.warp & 3, part = (pipe.warp - 2) >> 2;
     const uint32_t lane_addr = pipe.tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(part * BLOCKS * 32);
-    const uint32_t box = pipe.tiles + Pipe::STAGES * Pipe::STAGE + (uint32_t)(pipe.warp - 2) * 4096u;
-    uint32_t it = 0;
+    constexpr bool TWO = CHAINED;                       // boxes, in turn
+    const uint32_t box0 = pipe.tiles + Pipe::STAGES * Pipe::STAGE + (uint32_t)(pipe.warp - 2) * (TWO ? 8192u : 4096u);
+    uint32_t it = 0, box = box0;
     for (int tile = 0, t; (t = walk(tile)) < walk.total && !failed; ++tile) {
       const ProdUnit u(a, t);
       const ProdSide& o = a.of[u.side];
@@ -697,17 +834,23 @@ __global__ void __launch_bounds__(ProdPipe<PLANES, CHAINED>::THREADS, 1)
       const bool there = m < o.rows && n < a.d && part * BLOCKS * 32 < u.width;
       const int row = m + u.split * o.part;
       auto free_box = [&]() {                           // its last store has read it
-        if (lane == 0) bulk_wait_read_all();
+        if (lane == 0) {
+          if (TWO) bulk_wait_read_but_one();
+          else bulk_wait_read_all();
+        }
         __syncwarp();
       };
       auto send = [&](int col, bool add) {
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0 && col < a.d) {
-          if (add) tma_reduce_add_2d(out, box, col, row);
-          else tma_store_2d(out, box, col, row);
+        if (lane == 0) {
+          if (col < a.d) {
+            if (add) tma_reduce_add_2d(out, box, col, row);
+            else tma_store_2d(out, box, col, row);
+          }
           bulk_commit();
         }
+        if (TWO) box = box == box0 ? box0 + 4096u : box0;
       };
       auto put = [&](int b, const float (&x)[32]) {     // block b of the warp's columns
         if (sizeof(GT) == 4 || o.partial) {
@@ -968,7 +1111,8 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
   bf16* clean = a.ditems ? (bf16*)(base + p.clean) : nullptr;
   const int64_t ldz = ((int64_t)a.V + 7) / 8 * 8;
   const bool few = grads && loss_few(a.N, a.V);
-  const bool by_rows = few && !a.dbias && a.V <= LR_THREADS * LR_EACH && p.step >= (p.cut_users ? a.N : (int64_t)a.V);
+  const bool by_lanes = few && (a.dusers || a.ditems) && a.N <= LO_USERS;
+  const bool by_rows = few && !by_lanes && !a.dbias && a.V <= LR_THREADS * LR_EACH && p.step >= (p.cut_users ? a.N : (int64_t)a.V);
   if (few) {
     GRAM_TRY(score_logits_launch(ctx, a.users, a.ld_users, a.items, a.ld_items, a.bias, a.N, a.V, a.d, (float*)score_ws, ldz, st));
     if (!by_rows) GRAM_TRY(logprobs_launch(ctx, score_ws, GRAM_F32, ldz, a.N, a.V, a.scale, ask, st));
@@ -980,6 +1124,37 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
     GRAM_LAUNCH_CHECK(ctx);
   }
   if (!grads) return GRAM_OK;
+  if (by_lanes) {
+    // chunks of items: eight blocks an SM or more, no more parts of dU than have room
+    const int32_t columns = ceil_div(a.d, 256);
+    const int64_t most = a.dusers ? (int64_t)((p.bias - p.parts) / ((size_t)a.N * a.d * 4)) : INT32_MAX;
+    int64_t chunks = ceil_div64(8 * kNumSMs, columns);
+    if (chunks < ceil_div64(a.V, LO_CHUNK)) chunks = ceil_div64(a.V, LO_CHUNK);
+    if (chunks > ceil_div64(a.V, 32)) chunks = ceil_div64(a.V, 32);
+    if (chunks > most) chunks = most;
+    if (chunks >= ceil_div64(a.V, LO_CHUNK)) {
+      const int32_t chunk = (int32_t)ceil_div64(a.V, chunks);
+      chunks = ceil_div64(a.V, chunk);
+      const int32_t wide = (uintptr_t)a.ditems % 32 == 0 && a.ld_ditems % 8 == 0;
+      const OneArgs f{(const float*)score_ws, ldz, logp, stats, chunk, wide, (float*)(base + p.parts), gram_status_word(ctx)};
+      const dim3 grid((unsigned)chunks, (unsigned)columns);
+      {
+        ProfScope prof(ctx, GRAM_K_OTHER, (double)a.V * a.d * (2 + (f32 ? 4 : 2)), 1, st, "loss_one");
+        auto kern = f32 ? (a.N == 1 ? loss_one_kernel<float, 1> : a.N == 2 ? loss_one_kernel<float, 2> : loss_one_kernel<float, 4>)
+                        : (a.N == 1 ? loss_one_kernel<bf16, 1> : a.N == 2 ? loss_one_kernel<bf16, 2> : loss_one_kernel<bf16, 4>);
+        launch_chain(kern, grid, 256, 0, st, a, f);
+        GRAM_LAUNCH_CHECK(ctx);
+      }
+      if (a.dusers) {
+        ProfScope prof(ctx, GRAM_K_OTHER, (double)chunks * a.N * a.d * 4, 1, st, "loss_finish");
+        const dim3 all((unsigned)ceil_div(a.d, 32), (unsigned)a.N);
+        if (f32) launch_chain(loss_one_finish_kernel<float>, all, 1024, 0, st, (const float*)f.parts, (int32_t)chunks, a.d, a.N * a.d, (float*)a.dusers, a.ld_dusers);
+        else launch_chain(loss_one_finish_kernel<bf16>, all, 1024, 0, st, (const float*)f.parts, (int32_t)chunks, a.d, a.N * a.d, (bf16*)a.dusers, a.ld_dusers);
+        GRAM_LAUNCH_CHECK(ctx);
+      }
+      return GRAM_OK;
+    }
+  }
 
   const char* what = "gram_score_loss: cannot describe the vectors";
   CUtensorMap map_u, map_i, map_clean, map_g[3], map_out[2];
