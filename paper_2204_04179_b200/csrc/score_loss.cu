@@ -11,12 +11,13 @@
 //      gradients as the sum of two bf16: 2^-16 of each entry); loss_products_kernel takes both products of it, g I and g^T U, in one launch of tiles
 //      of either kind.  Where pieces are of items, those of g^T U are done with the piece and g I is summed over all; else the other way round.
 //   4. loss_finish_kernel: the summed gradient from its parts.
-// Where users are few and their logits fit 32 MB they are kept in L2 after all, and a kernel of elementwise work takes the place of the second product.
+// Where users are few and their logits fit 32 MB they are kept in L2 after all, and a kernel of elementwise work takes the place of the second product; up to
+// four users' products are taken by lanes, with g in 32 bits.
 // Bounded by the tensor cores where users are many: 8 N V d flops (12 with fp32 gradients), of which the products that cannot be done
 // without are 6; by the table's bytes, read twice and written once, where they are few.  Measured, vectors of 768: 4096 users against 100 000 items
 // 1700 us in a call by itself (1480 TFLOP/s of the 8 N V d) and 2070 in a loop of calls under the power cap (1220); against 30 522 with bias 548 and 675;
 // 25 600 users against 10 000 items, fp32 gradients, 1750 and 2070 (12 N V d: 1350 TFLOP/s by itself); 64 users against 100 000 120 in a graph of calls
-// (three passes over the table's 154 MB at 3.8 TB/s), one user against 10 000 27.
+// (three passes over the table's 154 MB at 3.8 TB/s), one user against 10 000 21.
 #include "score_loss.h"
 
 #include "logits.h"

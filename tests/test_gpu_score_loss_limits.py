@@ -22,7 +22,8 @@ def outputs(N, V, d, dtype, ask):
 
 @pytest.mark.parametrize("ask", [[], ["dusers"], ["ditems"], ["dbias"], ["dusers", "ditems"], ["dusers", "dbias"], ["ditems", "dbias"]])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("N,V,d", [(1, 3000, 256), (7, 20_000, 64), (60, 257, 72), (300, 1500, 64), (700, 300, 128), (1, 16_384, 8), (3, 16_385, 8)])
+@pytest.mark.parametrize("N,V,d", [(1, 3000, 256), (7, 20_000, 64), (60, 257, 72), (300, 1500, 64), (700, 300, 128), (1, 16_384, 8), (3, 16_385, 8),
+                                   (4, 100, 1032), (2, 700_001, 8), (9, 16_384, 16), (513, 1000, 64)])
 def test_each_part_alone(N, V, d, dtype, ask):
     rng = np.random.default_rng(N + V)
     users, items, u, w, b, targets, weight, more, t = inputs(rng, N, V, d, 0, bias=V % 2 == 1, none=0.1)
@@ -70,7 +71,7 @@ def test_no_users():
     g.close()
 
 
-@pytest.mark.parametrize("N,V", [(40, 500), (40, 20_000), (300, 9000), (1500, 400)])
+@pytest.mark.parametrize("N,V", [(4, 500), (40, 500), (40, 20_000), (300, 9000), (600, 9000), (1500, 400)])
 def test_rows_that_take_no_part(N, V):
     """Rows of a padded batch hold NaN and infinities; targets of -1, weights of 0 and targets that the bias takes out."""
     d, rng = 64, np.random.default_rng(N)
@@ -91,7 +92,7 @@ def test_rows_that_take_no_part(N, V):
         none, real = torch.from_numpy(targets < 0).to(DEV), torch.from_numpy(~idle).to(DEV)
         assert bool((loss[none] == 0).all())
         near(loss[real], want.loss[~idle], want.d_loss[~idle], "loss")
-        assert np.isposinf(want.loss[~idle]).any()
+        assert N == 4 or np.isposinf(want.loss[~idle]).any()
         near(out["dusers"], want.dU, want.d_dU, "dusers")
         near(out["ditems"], want.dI, want.d_dI, "ditems")
         near(out["dbias"], want.db, want.d_db, "dbias")
@@ -100,7 +101,7 @@ def test_rows_that_take_no_part(N, V):
         g.close()
 
 
-@pytest.mark.parametrize("N,V", [(5, 300), (5, 40_000), (300, 2000)])
+@pytest.mark.parametrize("N,V", [(2, 300), (5, 300), (5, 40_000), (600, 2000)])
 def test_nothing_left(N, V):
     """A bias that takes all items out: every target is taken out, nothing has a gradient."""
     g = context()
@@ -117,7 +118,7 @@ def test_nothing_left(N, V):
 
 
 @pytest.mark.parametrize("value", [float("nan"), INF])
-@pytest.mark.parametrize("N,V", [(5, 300), (5, 40_000), (300, 2000)])
+@pytest.mark.parametrize("N,V", [(4, 300), (5, 300), (5, 40_000), (600, 2000)])
 def test_a_row_that_holds_nan_or_infinity(N, V, value):
     g = context()
     users, items = torch.randn(N, 32, device=DEV).to(torch.bfloat16), torch.rand(V, 32, device=DEV).to(torch.bfloat16)
@@ -135,7 +136,8 @@ def test_a_row_that_holds_nan_or_infinity(N, V, value):
 
 
 @pytest.mark.parametrize("ask", [PARTS, PARTS[:2]])
-@pytest.mark.parametrize("N,V,scale", [(4, 500, 1e-30), (4, 500, 1e30), (4, 500, 3e4), (300, 2000, 1e-30), (300, 2000, 1e30), (300, 2000, 3e4), (4, 30_000, 1e30)])
+@pytest.mark.parametrize("N,V,scale", [(4, 500, 1e-30), (4, 500, 1e30), (4, 500, 3e4), (9, 500, 1e-30), (9, 500, 1e30), (9, 500, 3e4), (600, 2000, 1e-30), (600, 2000, 1e30), (600, 2000, 3e4), (4, 30_000, 1e30),
+                                       (9, 30_000, 1e30)])
 def test_far_scales(N, V, scale, ask):
     """Whole numbers of a few bits, so that logits are exact and rows have either one largest entry or several equal ones."""
     rng = np.random.default_rng(V)
@@ -200,7 +202,7 @@ def test_a_target_out_of_range():
     g.close()
 
 
-@pytest.mark.parametrize("N,V", [(20, 4000), (500, 4000), (3000, 700)])
+@pytest.mark.parametrize("N,V", [(2, 4000), (20, 4000), (600, 4000), (3000, 700)])
 def test_another_stream_and_a_captured_call(N, V):
     """The same bits from another stream, and from a captured call whose inputs have changed since."""
     d = 64
