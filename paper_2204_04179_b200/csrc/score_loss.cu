@@ -30,7 +30,7 @@ using namespace tc;
 constexpr int kPairs = kNumSMs / 2;
 // Users whose logits are kept where 32 MB hold them.  us so and with a second product: 64 users, 100 000 items of 768 128 and 160, 260 and 30 000
 // 89 and 94, 512 and 15 000 60 and 69, but 1000 and 8000 68 and 61 (rows are too many for a block's eight warps).
-constexpr int LOSS_FEW = 512;
+constexpr int LOSS_FEW = 512, LOSS_FEW_ROWS = 64;
 constexpr int LOSS_SHORT = 8 * kPairs;                  // blocks of 64 items x 256 columns whose products take the pairs 2 us for each plane
 
 // ============================================================================================
@@ -77,6 +77,7 @@ __device__ __forceinline__ void loss_clean(const ScoreLoss& a, int64_t n, bool p
 // A warp a user.  rows, rest, clean: null where they are not needed.
 __global__ void __launch_bounds__(256) loss_rows_kernel(const ScoreLoss a, const float* logp, const float2* stats, RowConst* rows, RowRest* rest, bf16* clean,
                                                         int32_t* status) {
+  chain_next();
   if (!chain_begin()) return;
   const int64_t n = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (n >= a.N) return;
@@ -101,7 +102,7 @@ struct Piece {
 };
 
 // Few users: g from logits that lie in L2, with the loss, the users' vectors and db, in one launch.  A block takes 128 columns, four a lane,
-// its warps the rows in turn; where the piece is the row's first, the block also takes the rows of its own number's residue.
+// and 64 rows, its warps in turn; where the piece is the rows' first, the block also takes those of its own number's residue.
 struct FewArgs {
   Piece at;
   const float* z;                // [N, ldz]
@@ -110,32 +111,33 @@ struct FewArgs {
   const float2* stats;
   bf16* clean;                   // or null
   RowRest* rest;                 // or null
+  float* bias_part;              // [groups of rows, ldg]
   int32_t* status;
 };
 template <int PLANES> __global__ void __launch_bounds__(256) loss_few_kernel(const ScoreLoss a, const FewArgs f) {
   chain_next();
   if (!chain_begin()) return;
   __shared__ float4 sums[8][32];
-  __shared__ RowConst row[LOSS_FEW];
+  __shared__ RowConst row[LOSS_FEW_ROWS];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 128 + 4 * lane;
   const Piece& at = f.at;
-  const int rows = (int)at.rows;                        // LOSS_FEW at most
-  for (int i = threadIdx.x; i < rows; i += 256) row[i] = loss_row(a, f.logp, f.stats, at.n0 + i);
+  const int i0 = (int)blockIdx.y * LOSS_FEW_ROWS, rows = min((int)at.rows, i0 + LOSS_FEW_ROWS);       // of this block
+  if (i0 + (int)threadIdx.x < rows) row[threadIdx.x] = loss_row(a, f.logp, f.stats, at.n0 + i0 + threadIdx.x);
   __syncthreads();
   if (at.first == 0)
-    for (int i = blockIdx.x + warp * (int)gridDim.x; i < rows; i += 8 * (int)gridDim.x) {
+    for (int i = i0 + blockIdx.x + warp * (int)gridDim.x; i < rows; i += 8 * (int)gridDim.x) {
       if (lane == 0) a.loss[at.n0 + i] = loss_of(a, f.logp, at.n0 + i, f.status);
-      if (f.clean) loss_clean(a, at.n0 + i, row[i].t >= 0, f.clean);
-      if (f.rest && lane == 0 && row[i].t < 0) f.rest[at.n0 + i] = RowRest{0.f, -1};
+      if (f.clean) loss_clean(a, at.n0 + i, row[i - i0].t >= 0, f.clean);
+      if (f.rest && lane == 0 && row[i - i0].t < 0) f.rest[at.n0 + i] = RowRest{0.f, -1};
     }
   const float c = a.scale * kLog2e;
   float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
   if (col < at.cols) {
     const float* z_at = f.z + at.n0 * f.ldz + at.first + col;
 #pragma unroll 8
-    for (int i = warp; i < rows; i += 8) {
+    for (int i = i0 + warp; i < rows; i += 8) {
       const float4 z = *reinterpret_cast<const float4*>(z_at + i * f.ldz);
-      const RowConst r = row[i];
+      const RowConst r = row[i - i0];
       float g[4] = {loss_p(r, z.x, c), loss_p(r, z.y, c), loss_p(r, z.z, c), loss_p(r, z.w, c)};
       const int hot = r.t - at.first - col;
 #pragma unroll
@@ -161,11 +163,12 @@ template <int PLANES> __global__ void __launch_bounds__(256) loss_few_kernel(con
     const float4 x = sums[i][lane];
     sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
   }
-  float* to = a.dbias + at.first + col;
+  const bool part = gridDim.y > 1;                      // joined by loss_bias_kernel
+  float* to = part ? f.bias_part + blockIdx.y * at.ldg + col : a.dbias + at.first + col;
   const float all[4] = {sum.x, sum.y, sum.z, sum.w};
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    if (col + j < at.cols) to[j] = at.n0 > 0 ? to[j] + all[j] : all[j];
+    if (col + j < at.cols) to[j] = !part && at.n0 > 0 ? to[j] + all[j] : all[j];
 }
 
 // Few users and few items, all of g in one piece and db not asked: a block takes a row of logits into registers, with its statistics, the loss,
@@ -621,8 +624,9 @@ __global__ void __launch_bounds__(GradPipe::THREADS, 1) loss_grad_kernel(const _
   pipe.close(failed, a.status);
 }
 
-// db of a piece: the sum of its 32-row blocks, eight groups of them side by side
+// db of a piece: the sum of its blocks of rows, eight groups of them side by side
 __global__ void __launch_bounds__(256) loss_bias_kernel(const float* part, int64_t ldg, int64_t blocks, int32_t cols, int32_t add, float* dbias) {
+  chain_next();
   if (!chain_begin()) return;
   __shared__ float sums[8][32];
   const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, v = blockIdx.x * 32 + lane;
@@ -1170,6 +1174,13 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
   const int64_t axis = p.cut_users ? a.N : a.V, pieces = ceil_div64(axis, p.step);
   const int own = p.cut_users ? 0 : 1;                   // whose gradient is done with the piece
   const bool joined = p.splits > 0 && (p.splits > 1 || pieces > 1 || own == 1);      // the users' always: what is left of their targets is added there
+  auto join_bias = [&](const Piece& e, int64_t blocks) -> gram_status {
+    ProfScope prof(ctx, GRAM_K_COLSUM, 4.0 * blocks * e.cols, 1, st, "loss_bias");
+    launch_chain(loss_bias_kernel, dim3((unsigned)ceil_div(e.cols, 32)), 256, 0, st, (const float*)(base + p.bias), p.ldg, blocks, e.cols, (int32_t)(e.n0 > 0),
+                 a.dbias + e.first);
+    GRAM_LAUNCH_CHECK(ctx);
+    return GRAM_OK;
+  };
   for (int64_t i = 0; i < pieces; ++i) {
     const int64_t at = i * p.step, now = axis - at < p.step ? axis - at : p.step;
     Piece e;
@@ -1181,13 +1192,14 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
     e.ldg = p.ldg;
     e.plane = e.rows * p.ldg;
     if (few) {
-      const FewArgs f{e, (const float*)score_ws, ldz, logp, stats, clean, rest, gram_status_word(ctx)};
+      const FewArgs f{e, (const float*)score_ws, ldz, logp, stats, clean, rest, (float*)(base + p.bias), gram_status_word(ctx)};
       ProfScope prof(ctx, GRAM_K_OTHER, (4.0 + 2 * planes) * e.rows * e.cols, 1, st, "loss_few");
       if (by_rows)
         launch_chain(planes == 3 ? loss_row_kernel<3> : planes == 2 ? loss_row_kernel<2> : loss_row_kernel<1>, dim3((unsigned)a.N), LR_THREADS, 0, st, a, f);
       else
-        launch_chain(planes == 3 ? loss_few_kernel<3> : planes == 2 ? loss_few_kernel<2> : loss_few_kernel<1>, dim3((unsigned)ceil_div(e.cols, 128)), 256, 0, st, a, f);
+        launch_chain(planes == 3 ? loss_few_kernel<3> : planes == 2 ? loss_few_kernel<2> : loss_few_kernel<1>, dim3((unsigned)ceil_div(e.cols, 128), (unsigned)ceil_div64(e.rows, LOSS_FEW_ROWS)), 256, 0, st, a, f);
       GRAM_LAUNCH_CHECK(ctx);
+      if (a.dbias && e.rows > LOSS_FEW_ROWS) GRAM_TRY(join_bias(e, ceil_div64(e.rows, LOSS_FEW_ROWS)));
     } else {
       GradArgs f = {};
       f.at = e;
@@ -1212,12 +1224,7 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
         if (planes == 2) GRAM_CUDA(ctx, launch_pairs<loss_grad_kernel<2>>(pairs, GradPipe::THREADS, GradPipe::SMEM, st, map_u, map_i, f));
         else GRAM_CUDA(ctx, launch_pairs<loss_grad_kernel<1>>(pairs, GradPipe::THREADS, GradPipe::SMEM, st, map_u, map_i, f));
       }
-      if (a.dbias) {
-        ProfScope prof(ctx, GRAM_K_COLSUM, (double)e.rows / 8 * e.cols, 1, st, "loss_bias");
-        launch_chain(loss_bias_kernel, dim3((unsigned)ceil_div(e.cols, 32)), 256, 0, st, (const float*)f.bias_part, p.ldg, ceil_div64(e.rows, 32), e.cols,
-                     (int32_t)(e.n0 > 0), a.dbias + e.first);
-        GRAM_LAUNCH_CHECK(ctx);
-      }
+      if (a.dbias) GRAM_TRY(join_bias(e, ceil_div64(e.rows, 32)));
     }
     if (!a.dusers && !a.ditems) continue;
     for (int k = 0; k < planes; ++k)
