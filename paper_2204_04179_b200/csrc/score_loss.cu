@@ -29,7 +29,8 @@ using namespace tc;
 
 constexpr int kPairs = kNumSMs / 2;
 // Users whose logits are kept where 32 MB hold them.  us so and with a second product: 64 users, 100 000 items of 768 128 and 160, 260 and 30 000
-// 89 and 94, 512 and 15 000 60 and 69, but 1000 and 8000 68 and 61 (rows are too many for a block's eight warps).
+// 89 and 94, 512 and 15 000 60 and 69, 600 and 13 000 65 and 67, but 1000 and 8000 68 and 61, 2000 and 4000 of 128 62 and 37: the logits' way out
+// and back costs more there than their product.
 constexpr int LOSS_FEW = 512, LOSS_FEW_ROWS = 64;
 constexpr int LOSS_SHORT = 8 * kPairs;                  // blocks of 64 items x 256 columns whose products take the pairs 2 us for each plane
 
