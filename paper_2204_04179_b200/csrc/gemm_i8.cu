@@ -59,15 +59,15 @@ __global__ void __launch_bounds__(32 * QR_ROWS) quantize_rows_kernel(const T* x,
                                                                      float* scale) {
   if (!chain_begin()) return;
   constexpr int W = VEC ? QuantVec<T>::N : 1, HELD = QR_HELD / W;          // elements of a piece; pieces that a lane holds
-  const int lane = threadIdx.x & 31;
+  const uint32_t lane = threadIdx.x & 31, n = (uint32_t)cols;              // a step past the longest row leaves 31 bits, not 32
   const int64_t r = (int64_t)blockIdx.x * QR_ROWS + (threadIdx.x >> 5);
   if (r >= rows) return;
   const T* row = x + r * ld;
   int8_t* out = codes + r * ld_codes;
-  const int pieces = cols / W;                          // VEC: the rest is taken one by one
+  const uint32_t pieces = n / W;                        // VEC: the rest is taken one by one
   float v[HELD][W];
   uint32_t top = 0u;
-  auto load = [&](int i, float* to) {
+  auto load = [&](uint32_t i, float* to) {
     if constexpr (VEC) QuantVec<T>::load(row + i * W, to);
     else to[0] = quant_value(row + i);
   };
@@ -80,17 +80,17 @@ __global__ void __launch_bounds__(32 * QR_ROWS) quantize_rows_kernel(const T* x,
 #pragma unroll
       for (int j = 0; j < W; ++j) top = max(top, quant_size(v[h][j]));
     }
-  for (int i = HELD * 32 + lane; i < pieces; i += 32) {
+  for (uint32_t i = HELD * 32 + lane; i < pieces; i += 32) {
     float y[W];
     load(i, y);
 #pragma unroll
     for (int j = 0; j < W; ++j) top = max(top, quant_size(y[j]));
   }
-  for (int i = pieces * W + lane; i < cols; i += 32) top = max(top, quant_size(quant_value(row + i)));
+  for (uint32_t i = pieces * W + lane; i < n; i += 32) top = max(top, quant_size(quant_value(row + i)));
   const QuantScale s = quant_scale(__reduce_max_sync(0xffffffffu, top));
   // a row of infinities or NaN has codes 0 (0 times them would be NaN)
   const bool none = s.inv == 0.f;
-  auto store = [&](int i, const float* y) {
+  auto store = [&](uint32_t i, const float* y) {
     if constexpr (VEC) {
       uint32_t c[W / 4];
 #pragma unroll
@@ -106,12 +106,12 @@ __global__ void __launch_bounds__(32 * QR_ROWS) quantize_rows_kernel(const T* x,
 #pragma unroll
   for (int h = 0; h < HELD; ++h)
     if (h * 32 + lane < pieces) store(h * 32 + lane, v[h]);
-  for (int i = HELD * 32 + lane; i < pieces; i += 32) {
+  for (uint32_t i = HELD * 32 + lane; i < pieces; i += 32) {
     float y[W];
     load(i, y);
     store(i, y);
   }
-  for (int i = pieces * W + lane; i < cols; i += 32) out[i] = none ? (int8_t)0 : (int8_t)quant_code(quant_value(row + i), s.inv);
+  for (uint32_t i = pieces * W + lane; i < n; i += 32) out[i] = none ? (int8_t)0 : (int8_t)quant_code(quant_value(row + i), s.inv);
   if (lane == 0) scale[r] = s.scale;
 }
 
