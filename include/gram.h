@@ -361,7 +361,7 @@ gram_status gram_score_logprobs(gram_ctx* ctx, const void* d_users, int64_t ld_u
                                 int32_t* d_top_ids, int32_t k, gram_stream stream);
 /* Softmax cross entropy of users against the item table, and its gradients, without an [N, V] array: with z as in gram_score_logprobs and
  * p the softmax of scale z,
- *   d_loss[n]      = -log p[n, d_targets[n]];  0 for a target of -1 ("none"), +inf for one that d_bias takes out
+ *   d_loss[n]      = -log p[n, d_targets[n]];  0 for a target of -1 ("none"), +inf for one that d_bias takes out (and where it leaves 32 bits)
  * and, each where its array is given, the gradients of sum_n weight[n] loss[n], with g[n, v] = weight[n] scale (p[n, v] - [v = d_targets[n]]):
  *   d_dusers[n, :] = sum_v g[n, v] items[v, :]     d_ditems[v, :] = sum_n g[n, v] users[n, :]     d_dbias[v] = sum_n g[n, v]
  * d_targets int32 [N], d_weight fp32 [N] or NULL (all 1), d_loss fp32 [N], d_dbias fp32 [V] (asked without d_bias too: that of zeros).  A row

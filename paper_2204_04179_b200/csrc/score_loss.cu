@@ -54,12 +54,17 @@ struct RowRest {
   int32_t t;                     // -1: none
 };
 
+// Whether a row's target takes part: not where the bias takes it out, or nothing is left.  Its log p alone does not tell: one that leaves 32 bits (a mask of
+// the type's lowest value at a scale above 1) is -inf too.
+__device__ __forceinline__ bool loss_target(const ScoreLoss& a, int32_t t, float lp, float m) {
+  return lp != ROW_NEG_INF || (m != ROW_NEG_INF && !(a.bias && a.bias[t] == ROW_NEG_INF));
+}
 // A row's statistics, log p of its target and weight.
 __device__ __forceinline__ RowConst loss_row(const ScoreLoss& a, const float* logp, const float2* stats, int64_t n) {
   const int32_t t = a.targets[n];
   const float lp = logp[n], w = a.weight ? a.weight[n] : 1.f;
   const float2 s = stats[n];
-  const bool part = t >= 0 && t < a.V && w != 0.f && lp != ROW_NEG_INF;
+  const bool part = t >= 0 && t < a.V && w != 0.f && loss_target(a, t, lp, s.x);
   return RowConst{s.x, s.y * kLog2e, lp != lp ? lp : w * a.scale, part ? t : -1};
 }
 __device__ __forceinline__ float loss_of(const ScoreLoss& a, const float* logp, int64_t n, int32_t* status) {
@@ -224,7 +229,7 @@ template <int PLANES> __global__ void __launch_bounds__(LR_THREADS) loss_row_ker
 #pragma unroll
   for (int i = 0; i < LR_THREADS / 32; ++i) s += part[1][i];
   const float lp = in ? row_logp(zt, m, logf(s), a.scale) : 0.f;
-  const bool takes_part = in && w != 0.f && lp != ROW_NEG_INF;
+  const bool takes_part = in && w != 0.f && loss_target(a, t, lp, m);
   if (threadIdx.x == 0) {
     if (!in && t != -1) gram_device_fail(f.status, GRAM_ERR_ID_RANGE);
     a.loss[n] = 0.f - lp;
