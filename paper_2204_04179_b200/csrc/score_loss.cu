@@ -1122,7 +1122,7 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
   bf16* clean = a.ditems ? (bf16*)(base + p.clean) : nullptr;
   const int64_t ldz = ((int64_t)a.V + 7) / 8 * 8;
   const bool few = grads && loss_few(a.N, a.V);
-  const bool by_lanes = few && (a.dusers || a.ditems) && a.N <= LO_USERS;
+  const bool by_lanes = few && (a.dusers || a.ditems) && a.N <= LO_USERS && a.d <= 65535 * 256;      // columns that a grid's second dimension counts
   const bool by_rows = few && !by_lanes && !a.dbias && a.V <= LR_THREADS * LR_EACH && p.step >= (p.cut_users ? a.N : (int64_t)a.V);
   if (few) {
     GRAM_TRY(score_logits_launch(ctx, a.users, a.ld_users, a.items, a.ld_items, a.bias, a.N, a.V, a.d, (float*)score_ws, ldz, st));
