@@ -349,7 +349,7 @@ gram_status gram_distill(gram_ctx* ctx, const void* d_logits, int dtype, int64_t
                          const float* d_weight, void* d_dlogits, int64_t ld_out, gram_stream stream);
 /* gram_logprobs of z[n, v] = users[n, :] . items[v, :] + bias[v] without an [N, V] array: d_users bf16 [N, d] and d_items
  * bf16 [V, d] with rows ld_users and ld_items elements apart (multiples of 8, addresses 16-byte aligned: else
- * GRAM_ERR_UNSUPPORTED), d_bias fp32 [V] or NULL (-inf takes an item out), products summed in fp32.  Lists of candidates, and the
+ * GRAM_ERR_UNSUPPORTED; so are d above 2^31 - 256), d_bias fp32 [V] or NULL (-inf takes an item out), products summed in fp32.  Lists of candidates, and the
  * logits where they are few, lie in the context's workspace for matrix products (32 MB at least), as the partial sums of a product
  * do: calls of one context are ordered on one stream or by events.  Where candidates are listed, alternatives and sums take the tensor
  * cores' products and given tokens are summed by themselves: of one item the two may differ as two orders of an fp32 sum do (but a row
@@ -379,7 +379,7 @@ gram_status gram_score_loss(gram_ctx* ctx, const void* d_users, int64_t ld_users
                             int grad_dtype, void* d_dusers, int64_t ld_dusers, void* d_ditems, int64_t ld_ditems, float* d_dbias,
                             void* d_workspace, int64_t workspace_bytes, gram_stream stream);
 /* Bytes of workspace for a call of these sizes with all gradients (host only): the least that serves, and the size beyond which nothing
- * is gained.  Either pointer may be NULL. */
+ * is gained.  Either pointer may be NULL.  GRAM_ERR_UNSUPPORTED where users or items alone would be more than 2^50 elements. */
 gram_status gram_score_loss_workspace(int64_t N, int32_t V, int32_t d, int grad_dtype, int64_t* h_least, int64_t* h_best);
 
 /* --- tables in 8 bits --------------------------------------------------------

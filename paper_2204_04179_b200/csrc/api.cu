@@ -486,10 +486,13 @@ static gram_status check_answers(gram_ctx* ctx, const char* name, const RowAnswe
   ROWS_ARG(N == 0 || ask.k == 0 || (ask.top_ids && ask.top_logp), "alternatives need both arrays");
   return GRAM_OK;
 }
+// blocks of columns, up to 256 wide, are counted in 32 bits
+constexpr int32_t kLongestVector = INT32_MAX - 255;
 // users and items of bf16, as bulk copies read them
 static gram_status check_vectors(gram_ctx* ctx, const char* name, const void* users, int64_t* ld_users, const void* items, int64_t* ld_items,
                                  int64_t N, int32_t V, int32_t d) {
   ROWS_ARG(d >= 1 && *ld_users >= d && *ld_items >= d, "rows must be at least d elements apart, d positive");
+  if (d > kLongestVector) return gram_set_error(ctx, "%s: vectors of %d elements, of at most %d", name, d, kLongestVector), GRAM_ERR_UNSUPPORTED;
   ROWS_ARG(*ld_items <= INT64_MAX / 8 / V && *ld_users <= INT64_MAX / 8 / (N > 0 ? N : 1), "rows too far apart");
   ROWS_ARG(N == 0 || (users && items), "null vectors");
   if (N == 1) *ld_users = (*ld_users + 7) / 8 * 8;      // of a single row the distance means nothing
@@ -581,6 +584,7 @@ gram_status gram_score_logprobs(gram_ctx* ctx, const void* d_users, int64_t ld_u
 }
 gram_status gram_score_loss_workspace(int64_t N, int32_t V, int32_t d, int grad_dtype, int64_t* h_least, int64_t* h_best) {
   if (N < 0 || N > INT32_MAX || V < 1 || d < 1 || (grad_dtype != GRAM_F32 && grad_dtype != GRAM_BF16)) return GRAM_ERR_ARG;
+  if (d > kLongestVector || (double)(N > V ? N : V) * d > 0x1p50) return GRAM_ERR_UNSUPPORTED;       // petabytes of vectors: the sizes leave 64 bits
   size_t least, best;
   score_loss_workspace(N, V, d, grad_dtype, &least, &best);
   if (h_least) *h_least = (int64_t)least;
