@@ -153,6 +153,13 @@ def _row_setup():
     _current_stream = lambda: raw(device())  # noqa: E731
 
 
+_MOST = 2 ** 31 - 1                                       # rows and columns: the library counts them in 32 bits
+
+
+def _too_many(t, what: str):
+    raise GramError(1, f"{what}: at most 2^31 - 1 rows and columns, not shape {tuple(t.shape)}")
+
+
 def _no_matrix(t, what: str):
     raise GramError(1, f"{what}: a matrix is needed, not shape {tuple(t.shape)}")
 
@@ -166,6 +173,8 @@ def _rows(t, what: str):
         N, V = t.shape
     except ValueError:
         _no_matrix(t, what)
+    if N > _MOST or V > _MOST:
+        _too_many(t, what)
     ld, step = t.stride()
     if dtype is None or (step != 1 and V > 1) or not (t.is_cuda or t.is_pinned()):
         raise GramError(1, f"{what}: float32 or bfloat16 is needed, not {t.dtype}" if dtype is None else
@@ -210,6 +219,8 @@ def _codes(t, what: str):
         N, K = t.shape
     except ValueError:
         _no_matrix(t, what)
+    if N > _MOST or K > _MOST:
+        _too_many(t, what)
     ld, step = t.stride()
     if t.dtype is not _ROW_TYPES["c"] or (step != 1 and K > 1) or not (t.is_cuda or t.is_pinned()):
         raise GramError(1, f"{what}: int8 rows of contiguous elements in device or pinned host memory are needed, not {t.dtype} with strides {t.stride()} on {t.device}")
@@ -433,7 +444,8 @@ class Gram:
         if not _ROW_TYPES:
             _row_setup()
         least, best = C.c_int64(0), C.c_int64(0)
-        st = lib().gram_score_loss_workspace(C.c_int64(N), C.c_int32(V), C.c_int32(d), C.c_int(_ROW_TYPES.get(grad_dtype, -1)), C.byref(least), C.byref(best))
+        st = lib().gram_score_loss_workspace(C.c_int64(N), C.c_int32(V), C.c_int32(d), C.c_int(_ROW_TYPES.get(grad_dtype, -1)), C.byref(least),
+                                             C.byref(best)) if V <= _MOST and d <= _MOST else 1
         if st != 0:
             raise GramError(st, f"score_loss_workspace: N = {N}, V = {V}, d = {d}, {grad_dtype}")
         return least.value, best.value

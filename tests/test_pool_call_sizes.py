@@ -40,3 +40,37 @@ def test_vectors_too_long_to_count(d):
     assert L.gram_score_logprobs(h, p(x), d, p(x), d, None, 1, 1, d, 1.0, p(t), 1, p(f), None, None, None, None, 0, 0) == 4
     assert g.launch_count() == launches
     g.close()
+
+
+def _far(rows, cols, dtype):
+    from tests.test_row_call_checks import OnDevice
+    return torch.empty(rows, cols, dtype=dtype, device="meta").as_subclass(OnDevice)
+
+
+PAST = 2 ** 32 + 16                                       # 16 in 32 bits
+B, F, I8 = torch.bfloat16, torch.float32, torch.int8
+CALLS = {
+    "items": lambda g: g.score_loss(_far(4, 8, B), _far(PAST, 8, B), None, None, None),
+    "users": lambda g: g.score_logprobs(_far(PAST, 8, B), _far(9, 8, B)),
+    "longer vectors": lambda g: g.score_loss(_far(4, PAST, B), _far(9, PAST, B), None, None, None),
+    "rows": lambda g: g.quantize_rows(_far(4, PAST, F), _far(4, PAST, I8), None),
+    "codes' channels": lambda g: g.gemm_i8(_far(4, 16, I8), None, _far(PAST, 16, I8), None, _far(4, PAST, F)),
+    "codes of longer rows": lambda g: g.gemm_i8(_far(4, PAST, I8), None, _far(9, PAST, I8), None, _far(4, 9, F)),
+    "logits": lambda g: g.logprobs(_far(4, PAST, F)),
+}
+
+
+@pytest.mark.parametrize("name", sorted(CALLS))
+def test_sizes_that_leave_32_bits_are_refused(name):
+    """The library takes these sizes in 32 bits, where they would be other, smaller ones."""
+    from tests.test_row_call_checks import _NoContext
+    with pytest.raises(binding.GramError) as e:
+        CALLS[name](object.__new__(_NoContext))
+    assert e.value.status == 1 and "2^31 - 1" in str(e.value)
+
+
+@pytest.mark.parametrize("N,V,d", [(4, PAST, 8), (4, 9, PAST), (PAST, 9, 8)])
+def test_workspaces_of_sizes_that_leave_32_bits_are_refused(N, V, d):
+    with pytest.raises(binding.GramError) as e:
+        binding.Gram.score_loss_workspace(N, V, d, B)
+    assert e.value.status == 1
