@@ -103,10 +103,11 @@ __device__ __forceinline__ float loss_p(const RowConst& r, float z, float c) { r
 struct Piece {
   int64_t n0, rows;
   int32_t first, cols;
-  bf16* g;                       // [planes, rows, ldg]
+  bf16* g;                       // [planes, rows, ldg]; none where db alone is asked
   int64_t ldg, plane;            // elements between rows (a multiple of 256) and between planes
 };
 
+// PLANES of the kernels that form g: bf16 that it leaves as the sum of; 0: only db's sums leave.
 // Few users: g from logits that lie in L2, with the loss, the users' vectors and db, in one launch.  A block takes 128 columns, four a lane,
 // and 64 rows, its warps in turn; where the piece is the rows' first, the block also takes those of its own number's residue.
 struct FewArgs {
@@ -149,6 +150,7 @@ template <int PLANES> __global__ void __launch_bounds__(256) loss_few_kernel(con
 #pragma unroll
       for (int j = 0; j < 4; ++j) g[j] = r.t < 0 ? 0.f : r.f * (j == hot ? g[j] - 1.f : g[j]);
       sum.x += g[0]; sum.y += g[1]; sum.z += g[2]; sum.w += g[3];
+      if constexpr (PLANES == 0) continue;
       bf16* to = at.g + i * at.ldg + col;
 #pragma unroll
       for (int k = 0; k < PLANES; ++k) {
@@ -593,7 +595,7 @@ __global__ void __launch_bounds__(GradPipe::THREADS, 1) loss_grad_kernel(const _
 #pragma unroll
             for (int j = 0; j < 32; ++j) g[j] = r.t < 0 ? 0.f : g[j];
           }
-          if (n < a.at.rows) {
+          if (PLANES > 0 && n < a.at.rows) {
             bf16* to = a.at.g + n * a.at.ldg + col0 + b * 32;
             uint32_t h[16];
 #pragma unroll
@@ -1022,7 +1024,7 @@ LossSplits loss_splits(int64_t step, int64_t all, int32_t d, int planes, bool f3
   return best;
 }
 
-// Lays out a workspace of `room` bytes, or the one of pieces of `step`.
+// Lays out a workspace of `room` bytes, or the one of pieces of `step`.  planes 0: no product takes g, which is not kept.
 LossPlan loss_plan(int64_t N, int32_t V, int32_t d, int planes, bool f32, bool users, bool items, bool bias, int64_t step, size_t room) {
   LossPlan p = {};
   p.cut_users = N > V;
@@ -1059,7 +1061,7 @@ LossPlan loss_plan(int64_t N, int32_t V, int32_t d, int planes, bool f32, bool u
   }
   place(0, summed ? 1 : 0);
   const size_t per = (size_t)planes * (p.cut_users ? all_up : N) * 2 * 256 + (bias ? (p.cut_users ? (size_t)all_up * 32 : (size_t)ceil_div64(N, 32) * 1024) : 0);
-  int64_t c = room > p.bytes ? (int64_t)((room - p.bytes) / per) * 256 : 0;
+  int64_t c = room > p.bytes && per ? (int64_t)((room - p.bytes) / per) * 256 : 0;      // per 0: the loss alone
   if (c > most) c = most;
   if (c < 256) c = 256;
   // Pieces of about equal size: as few as fit or up to half as many again, whichever count deals their units out most evenly (a piece costs
@@ -1104,7 +1106,7 @@ void score_loss_workspace(int64_t N, int32_t V, int32_t d, int grad_dtype, size_
 gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_t ws_bytes, void* score_ws, size_t score_ws_bytes, cudaStream_t st) {
   const bool grads = a.dusers || a.ditems || a.dbias;
   const bool f32 = a.grad_dtype == GRAM_F32;
-  const int planes = a.dusers || a.ditems ? loss_planes(a.N, a.V, a.d, a.grad_dtype) : 1;
+  const int planes = a.dusers || a.ditems ? loss_planes(a.N, a.V, a.d, a.grad_dtype) : 0;
   const LossPlan p = loss_plan(a.N, a.V, a.d, planes, f32, a.dusers != nullptr, a.ditems != nullptr, a.dbias != nullptr, 0, ws_bytes ? ws_bytes : 1);
   const size_t need = grads ? p.bytes : p.rows;
   if (need > ws_bytes)
@@ -1203,7 +1205,7 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
       if (by_rows)
         launch_chain(planes == 3 ? loss_row_kernel<3> : planes == 2 ? loss_row_kernel<2> : loss_row_kernel<1>, dim3((unsigned)a.N), LR_THREADS, 0, st, a, f);
       else
-        launch_chain(planes == 3 ? loss_few_kernel<3> : planes == 2 ? loss_few_kernel<2> : loss_few_kernel<1>, dim3((unsigned)ceil_div(e.cols, 128), (unsigned)ceil_div64(e.rows, LOSS_FEW_ROWS)), 256, 0, st, a, f);
+        launch_chain(planes == 3 ? loss_few_kernel<3> : planes == 2 ? loss_few_kernel<2> : planes == 1 ? loss_few_kernel<1> : loss_few_kernel<0>, dim3((unsigned)ceil_div(e.cols, 128), (unsigned)ceil_div64(e.rows, LOSS_FEW_ROWS)), 256, 0, st, a, f);
       GRAM_LAUNCH_CHECK(ctx);
       if (a.dbias && e.rows > LOSS_FEW_ROWS) GRAM_TRY(join_bias(e, ceil_div64(e.rows, LOSS_FEW_ROWS)));
     } else {
@@ -1228,6 +1230,7 @@ gram_status score_loss_launch(gram_ctx* ctx, const ScoreLoss& a, void* ws, size_
         ProfScope prof(ctx, GRAM_K_GEMM, 2.0 * e.rows * e.cols * a.d, 1, st, "loss_grad");
         const int pairs = f.total < kPairs ? f.total : kPairs;
         if (planes == 2) GRAM_CUDA(ctx, launch_pairs<loss_grad_kernel<2>>(pairs, GradPipe::THREADS, GradPipe::SMEM, st, map_u, map_i, f));
+        else if (planes == 0) GRAM_CUDA(ctx, launch_pairs<loss_grad_kernel<0>>(pairs, GradPipe::THREADS, GradPipe::SMEM, st, map_u, map_i, f));
         else GRAM_CUDA(ctx, launch_pairs<loss_grad_kernel<1>>(pairs, GradPipe::THREADS, GradPipe::SMEM, st, map_u, map_i, f));
       }
       if (a.dbias) GRAM_TRY(join_bias(e, ceil_div64(e.rows, 32)));
