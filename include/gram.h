@@ -359,8 +359,8 @@ gram_status gram_score_logprobs(gram_ctx* ctx, const void* d_users, int64_t ld_u
                                 const float* d_bias, int64_t N, int32_t V, int32_t d, float scale, const int32_t* d_targets,
                                 int32_t C, float* d_logp, float* d_stats, float* d_entropy, float* d_top_logp,
                                 int32_t* d_top_ids, int32_t k, gram_stream stream);
-/* Softmax cross entropy of users against the item table, and its gradients, without an [N, V] array: with z as in gram_score_logprobs and
- * p the softmax of scale z,
+/* Softmax cross entropy of users against the item table, and its gradients, without an [N, V] array of logits (but for up to 512 users
+ * whose logits fit 32 MB: those lie in the context's workspace): with z as in gram_score_logprobs and p the softmax of scale z,
  *   d_loss[n]      = -log p[n, d_targets[n]];  0 for a target of -1 ("none"), +inf for one that d_bias takes out (and where it leaves 32 bits)
  * and, each where its array is given, the gradients of sum_n weight[n] loss[n], with g[n, v] = weight[n] scale (p[n, v] - [v = d_targets[n]]):
  *   d_dusers[n, :] = sum_v g[n, v] items[v, :]     d_ditems[v, :] = sum_n g[n, v] users[n, :]     d_dbias[v] = sum_n g[n, v]
@@ -369,7 +369,10 @@ gram_status gram_score_logprobs(gram_ctx* ctx, const void* d_users, int64_t ld_u
  * it holds, reaches nothing else (an item that d_bias takes out must be finite all the same).  A row that holds NaN or +inf has loss NaN, and so have the gradients it takes part in.
  * d_dusers and d_ditems are `grad_dtype`, rows a multiple of 16 bytes apart, 16-byte aligned, d a multiple of 8 (GRAM_ERR_UNSUPPORTED
  * else); they must not overlap the inputs or each other.  For GRAM_BF16 g is rounded to bf16 before the two products, as a gradient that passes through
- * bf16 is; for GRAM_F32 it enters them as the sum of two bf16 (to 2^-16 of itself; of three for short products of few users), at half again the cost.
+ * bf16 is (up to four users: in 32 bits); where N <= V what that rounding leaves of a target's entry is added to its row of d_dusers in 32 bits, else a row may be
+ * off by 2^-8 of that entry too.  For GRAM_F32 it enters them as the sum of two bf16 (to 2^-16 of itself; of three for short products of few users), at half again
+ * the cost.  The products' sums are held in 32 bits, to which the tensor cores add 16 products at a time, cutting off (by up to 2^-23 of the sum each time; for GRAM_F32 512
+ * products at most, for GRAM_BF16 65 536, before they are added with rounding).
  * d_dbias is summed in fp32 from g itself.
  * g is formed for a piece of the items (of the users where they are more) at a time in d_workspace, 256-byte aligned device memory of the caller's: as
  * large a piece as workspace_bytes allow.  Its content means nothing before and after; calls that may run at the same time need one each.  The call also uses the
@@ -394,7 +397,7 @@ enum { GRAM_I8_K_MAX = 131071 };         /* longest rows whose sums of products 
 gram_status gram_quantize_rows(gram_ctx* ctx, const void* d_x, int dtype, int64_t ld, int64_t rows, int32_t cols, int8_t* d_codes,
                                int64_t ld_codes, float* d_scale, gram_stream stream);
 /* C[m, n] = d_scale_a[m] d_scale_b[n] sum_k A[m, k] B[n, k] + d_bias[n]: A int8 [M, K], B int8 [N, K], the sum a whole number of 32 bits (exact),
- * the rest in fp32, C fp32 or bf16 (c_dtype) [M, N] with rows ldc apart at any address and stride that its type allows; d_bias fp32 [N] or
+ * the rest in fp32 (first the sum and d_scale_a, whose product has to be finite), C fp32 or bf16 (c_dtype) [M, N] with rows ldc apart at any address and stride that its type allows (what lies between is left alone); d_bias fp32 [N] or
  * NULL.  A and B 16-byte aligned, rows a multiple of 16 apart (GRAM_ERR_UNSUPPORTED else); K at most GRAM_I8_K_MAX, any M, N and K. */
 gram_status gram_gemm_i8(gram_ctx* ctx, const int8_t* d_A, int64_t lda, const float* d_scale_a, const int8_t* d_B, int64_t ldb,
                          const float* d_scale_b, const float* d_bias, void* d_C, int c_dtype, int64_t ldc, int64_t M, int32_t N, int32_t K,

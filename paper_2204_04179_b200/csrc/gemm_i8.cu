@@ -12,7 +12,7 @@ constexpr int kPairs = kNumSMs / 2;
 // codes = x (127 / max |x|) to the nearest whole number, scale = max |x| / 127
 // ============================================================================================
 // A warp a row.  Rows of up to QR_HELD elements a lane are read once, longer ones twice (the second time out of L1 or L2).
-// Bounded by HBM: 100 000 rows of 768 fp32 63 to 65 us (5.9 to 6.1 TB/s); 64 rows of bf16 2.3 us in a graph of calls.
+// Bounded by HBM: 100 000 rows of 768 fp32 59 us in a loop of calls (6.5 TB/s), bf16 51; 64 rows of bf16 2.3 us in a graph of calls.
 constexpr int QR_HELD = 32, QR_ROWS = 8;
 
 template <typename T> struct QuantVec;                  // 16 bytes of a row, and their codes
@@ -131,6 +131,9 @@ void launch_quantize(const void* x, int64_t ld, int64_t rows, int32_t cols, int8
 //             leave by bulk stores.  Many tokens, C aligned to 16 bytes, rows of 16 bytes or more.
 //   CHANNELS  256 channels x `width` tokens, channels are the MMA's rows: a warp's lanes run along C's rows, whatever its address and stride,
 //             and a few tokens are a narrow tile.
+// us of ROWS and of CHANNELS, K = 768, fp32 results, 2304, 16 384 and 100 000 channels: 96 tokens 8.2 and 5.8, 9.0 and 6.4, 25.7 and 22.9; 129 tokens 8.3 and 7.6,
+// 9.4 and 8.8, 28.5 and 28.7; 512 tokens 8.6 and 8.3, 12.2 and 12.6, 56 and 58.5; bf16 results, 129 tokens 7.2 and 7.7, 8.5 and 9.0, 26.0 and 27.4; 512 7.6 and
+// 8.4, 10.3 and 12.9, 43 and 53.
 // The tiles of the operand with fewer rows vary fastest: it stays in L2 while the other is read once.
 // Measured with K = 768: one token against 100 000 channels 16.9 us and 64 tokens 21.7 (the table's 77 MB at 4.6 TB/s, on tables in turn); many tokens with
 // both operands of each tile fetched 2.5 to 3.0 POP/s at K = 2048.  Results that leave by single stores in place of bulk stores: 4096 x 16 384 x 768 65 us
@@ -336,7 +339,7 @@ __global__ void __launch_bounds__(I8Rows::THREADS, 1) gemm_i8_rows_kernel(const 
 
 // ROWS where a tile's channels fit beside the stages (K of up to 768): they stay in shared memory while tile after tile of tokens passes, so that
 // what comes from L2 for a tile is half (4096 x 100 000 x 768, bf16 out, a call by itself: 290 us with both operands of each tile fetched, 244 so; 25 600 x 2304 x 768:
-// 46 and 43.5).  What bounds it now is shared memory, which operands, results and scales all pass through: the tensor cores are busy 67 % of the
+// 46 and 43.5; 4096 x 16 384 at K = 128 33.0 and 30.1, 512 39.9 and 34.8, 768 51.5 and 42; 25 600 x 2304 at K = 256 28.7 and 30.5, 512 34.3 and 34.1).  What bounds it now is shared memory, which operands, results and scales all pass through: the tensor cores are busy 67 % of the
 // time, and neither more warps nor a cheaper conversion of the sums changed it.  A pair takes whole columns of tiles, neighbouring pairs neighbouring ones; what is left after the last full round is cut evenly
 // over all pairs.
 constexpr int I8_HELD = 6, I8_HELD_WARPS = 8;           // k-blocks of channels that are held

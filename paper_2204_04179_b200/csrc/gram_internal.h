@@ -36,12 +36,14 @@ void gram_set_error(gram_ctx* ctx, const char* fmt, ...);
 // ---------------------------------------------------------------------------
 // Launches.  A step is a chain of some hundred short kernels on one stream; with ordinary launches each waits for the one
 // before it to drain, flush and retire and then pays its own start.  Every kernel here is launched with programmatic stream
-// serialisation instead: its blocks are placed as soon as all blocks of the kernel before have ended, they set up what needs
-// no memory of others, and chain_begin() then waits until that kernel's writes are visible.  (Ordinary launches -> this ->
+// serialisation instead: its blocks are placed as soon as all blocks of the kernel before have ended or called chain_next(), they set
+// up what needs no memory of others, and chain_begin() then waits until that kernel's writes are visible.  (Ordinary launches -> this ->
 // with an early trigger that lets blocks in while the kernel before still runs: the check's step 686 -> 532 -> 554 us, the
 // task module at 25 600 rows 3.49 -> 3.40 -> 3.39 ms, encodings of 2048 ragged texts 2.86 -> 2.85 -> 2.92 ms: the blocks that
-// wait on the SMs cost the large kernels more than they save, so there is no early trigger.)
-// A kernel launched with launch_chain (or chain_attribute) must call chain_begin() before it touches global memory.
+// wait on the SMs cost the large kernels more than they save, so the step's kernels have no early trigger; those of the loss over a
+// pool, which are short, have one, chain_next().)
+// A kernel launched with launch_chain (or chain_attribute) must call chain_begin() in all its threads before it touches global
+// memory: whatever kernel of the library came before it may still be running and writing.
 // It returns true; that the compiler cannot know it keeps loads that it takes to be of constant memory behind the wait.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ bool chain_begin() {

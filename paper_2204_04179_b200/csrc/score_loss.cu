@@ -3,7 +3,7 @@
 // With z = U I^T + b, p the softmax of scale z and t the rows' targets, loss_n = log sum_v exp(scale z_nv) - scale z_n,t, and the
 // gradient of sum_n w_n loss_n with respect to z is g_nv = w_n scale (p_nv - [v = t_n]); then dU = g I, dI = g^T U, db_v = sum_n g_nv.
 //
-// g has as many entries as the logits, which are never kept: it is formed for a piece at a time, some of the items and all users, or some of
+// g has as many entries as the logits, which are not kept but for few users: it is formed for a piece at a time, some of the items and all users, or some of
 // the users and all items where users are more.
 //   1. The statistics of the rows (m and log s) come from the kernels of gram_score_logprobs: one product.
 //   2. loss_rows_kernel: the loss, and what a row's g needs, in one float4.

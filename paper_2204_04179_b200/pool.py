@@ -2,7 +2,7 @@
 
 A user is the mean of the encodings of the items in a history, and the answer over the pool is the softmax of user . item.  A
 step encodes the pool, takes the loss of the clicked items over all items with the gradients of users and items
-(`score_loss`, the logits never kept), sums the gradient of each item's encoding over its places in the histories, and runs the
+(`score_loss`, from the vectors themselves), sums the gradient of each item's encoding over its places in the histories, and runs the
 encoder's backward pass and update.  Then the table is held as codes of 8 bits with a scale for each item (`quantize_rows`), and
 users are answered from it (`gemm_i8`, `logprobs`).  Inputs and weights are random, of the sizes given.
 """
