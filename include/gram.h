@@ -368,7 +368,7 @@ gram_status gram_score_logprobs(gram_ctx* ctx, const void* d_users, int64_t ld_u
  * takes no part in the gradients if its target is "none" or taken out or its weight 0: its row of d_dusers is 0, and its vector, whatever
  * it holds, reaches nothing else (an item that d_bias takes out must be finite all the same).  A row that holds NaN or +inf has loss NaN, and so have the gradients it takes part in.
  * d_dusers and d_ditems are `grad_dtype`, rows a multiple of 16 bytes apart, 16-byte aligned, d a multiple of 8 (GRAM_ERR_UNSUPPORTED
- * else); they must not overlap the inputs or each other.  For GRAM_BF16 g is rounded to bf16 before the two products, as a gradient that passes through
+ * else).  No array that is written may overlap another one of the call (GRAM_ERR_ARG; rows beside others' in one buffer do not).  For GRAM_BF16 g is rounded to bf16 before the two products, as a gradient that passes through
  * bf16 is (up to four users: in 32 bits); where N <= V what that rounding leaves of a target's entry is added to its row of d_dusers in 32 bits, else a row may be
  * off by 2^-8 of that entry too.  For GRAM_F32 it enters them as the sum of two bf16 (to 2^-16 of itself; of three for short products of few users), at half again
  * the cost.  The products' sums are held in 32 bits, to which the tensor cores add 16 products at a time, cutting off (by up to 2^-23 of the sum each time; for GRAM_F32 512
@@ -393,12 +393,14 @@ enum { GRAM_I8_K_MAX = 131071 };         /* longest rows whose sums of products 
 /* Rows x [rows, cols] of `dtype` (GRAM_F32 or GRAM_BF16), `ld` elements between them, at any address and stride that the type allows:
  *   d_scale[r] = max |x[r, :]| / 127 (fp32 [rows])      d_codes[r, c] = x[r, c] (127 / max |x[r, :]|), rounded to the nearest whole number, ties to even
  * quotients and product rounded to fp32, codes int8 in [-127, 127], rows ld_codes apart (what lies between is left alone).  A row whose
- * largest size is below 1e-30 has scale 0 and codes 0; one that holds NaN or an infinity scale NaN and codes 0. */
+ * largest size is below 1e-30 has scale 0 and codes 0; one that holds NaN or an infinity scale NaN and codes 0.
+ * Neither array may overlap x or the other. */
 gram_status gram_quantize_rows(gram_ctx* ctx, const void* d_x, int dtype, int64_t ld, int64_t rows, int32_t cols, int8_t* d_codes,
                                int64_t ld_codes, float* d_scale, gram_stream stream);
 /* C[m, n] = d_scale_a[m] d_scale_b[n] sum_k A[m, k] B[n, k] + d_bias[n]: A int8 [M, K], B int8 [N, K], the sum a whole number of 32 bits (exact),
  * the rest in fp32 (first the sum and d_scale_a, whose product has to be finite), C fp32 or bf16 (c_dtype) [M, N] with rows ldc apart at any address and stride that its type allows (what lies between is left alone); d_bias fp32 [N] or
- * NULL.  A and B 16-byte aligned, rows a multiple of 16 apart (GRAM_ERR_UNSUPPORTED else); K at most GRAM_I8_K_MAX, any M, N and K. */
+ * NULL.  A and B 16-byte aligned, rows a multiple of 16 apart (GRAM_ERR_UNSUPPORTED else); K at most GRAM_I8_K_MAX, any M, N and K.
+ * C must not overlap the others. */
 gram_status gram_gemm_i8(gram_ctx* ctx, const int8_t* d_A, int64_t lda, const float* d_scale_a, const int8_t* d_B, int64_t ldb,
                          const float* d_scale_b, const float* d_bias, void* d_C, int c_dtype, int64_t ldc, int64_t M, int32_t N, int32_t K,
                          gram_stream stream);
