@@ -530,17 +530,27 @@ struct Extent {
   const void* p;
   int64_t rows, row, pitch;
 };
-// Whether two arrays share bytes.  Of rows with different distances, whose first to last bytes cross, nothing is said.
+// Whether two arrays whose first to last bytes cross share some.  Of rows with different distances nothing is said.
 static bool extents_overlap(const Extent& x, const Extent& y) {
-  if (!x.p || !y.p || x.row == 0 || y.row == 0) return false;
-  const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), b = reinterpret_cast<uintptr_t>(y.p);
-  if (a + (uintptr_t)((x.rows - 1) * x.pitch + x.row) <= b || b + (uintptr_t)((y.rows - 1) * y.pitch + y.row) <= a) return false;
   if (x.rows > 1 && y.rows > 1 && x.pitch != y.pitch) return false;
   if (x.rows == 1 && y.rows == 1) return true;
   const Extent &m = x.rows > 1 ? x : y, &n = x.rows > 1 ? y : x;                 // n's rows begin at one place of m's distance
   const uintptr_t from = reinterpret_cast<uintptr_t>(m.p), to = reinterpret_cast<uintptr_t>(n.p), pitch = (uintptr_t)m.pitch;
   const int64_t at = (int64_t)(to >= from ? (to - from) % pitch : (pitch - (from - to) % pitch) % pitch);
   return !(at >= m.row && at + n.row <= m.pitch);
+}
+// The first `written` of `count` arrays (ten at most) must not overlap each other or the rest.
+static gram_status check_extents(gram_ctx* ctx, const char* name, const Extent* all, int written, int count) {
+  uintptr_t begin[10], end[10];
+  for (int i = 0; i < count; ++i) {
+    begin[i] = reinterpret_cast<uintptr_t>(all[i].p);
+    end[i] = all[i].p ? begin[i] + (uintptr_t)((all[i].rows - 1) * all[i].pitch + all[i].row) : 0;
+  }
+  for (int i = 0; i < written; ++i)
+    for (int j = i + 1; j < count; ++j)
+      if (begin[i] < end[j] && begin[j] < end[i] && extents_overlap(all[i], all[j]))
+        return gram_set_error(ctx, "%s: %s overlaps %s", name, all[i].what, all[j].what), GRAM_ERR_ARG;
+  return GRAM_OK;
 }
 
 gram_status gram_logprobs(gram_ctx* ctx, const void* d_logits, int dtype, int64_t ld, int64_t N, int32_t V, float scale,
@@ -634,7 +644,6 @@ gram_status gram_score_loss(gram_ctx* ctx, const void* d_users, int64_t ld_users
     return GRAM_OK;
   }
   const int64_t size = grad_dtype == GRAM_F32 ? 4 : 2;
-  // the first five are written
   const Extent all[] = {{"d_loss", d_loss, 1, N * 4, 0},
                         {"d_dusers", d_dusers, N, d * size, ld_dusers * size},
                         {"d_ditems", d_ditems, V, d * size, ld_ditems * size},
@@ -645,9 +654,7 @@ gram_status gram_score_loss(gram_ctx* ctx, const void* d_users, int64_t ld_users
                         {"d_bias", d_bias, 1, (int64_t)V * 4, 0},
                         {"d_targets", d_targets, 1, N * 4, 0},
                         {"d_weight", d_weight, 1, N * 4, 0}};
-  for (int i = 0; i < 5; ++i)
-    for (int j = i + 1; j < 10; ++j)
-      if (extents_overlap(all[i], all[j])) return gram_set_error(ctx, "%s: %s overlaps %s", name, all[i].what, all[j].what), GRAM_ERR_ARG;
+  GRAM_TRY(check_extents(ctx, name, all, 5, 10));
   const ScoreLoss a{d_users, d_items, ld_users, ld_items, d_bias, N, V, d, scale, d_targets, d_weight, d_loss, grad_dtype, d_dusers, d_ditems,
                     ld_dusers, ld_ditems, d_dbias};
   return score_loss_launch(ctx, a, d_workspace, (size_t)workspace_bytes, ctx->gws.splitk, ctx->gws.splitk_bytes, S(stream));
