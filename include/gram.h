@@ -368,7 +368,8 @@ gram_status gram_score_logprobs(gram_ctx* ctx, const void* d_users, int64_t ld_u
  * takes no part in the gradients if its target is "none" or taken out or its weight 0: its row of d_dusers is 0, and its vector, whatever
  * it holds, reaches nothing else (an item that d_bias takes out must be finite all the same).  A row that holds NaN or +inf has loss NaN, and so have the gradients it takes part in.
  * d_dusers and d_ditems are `grad_dtype`, rows a multiple of 16 bytes apart, 16-byte aligned, d a multiple of 8 (GRAM_ERR_UNSUPPORTED
- * else).  No array that is written may overlap another one of the call (GRAM_ERR_ARG; rows beside others' in one buffer do not).  For GRAM_BF16 g is rounded to bf16 before the two products, as a gradient that passes through
+ * else).  No array that is written may overlap another one of the call (GRAM_ERR_ARG; matrices whose rows lie at two distances are not looked
+ * through; rows beside others' in one buffer do not overlap).  For GRAM_BF16 g is rounded to bf16 before the two products, as a gradient that passes through
  * bf16 is (up to four users: in 32 bits); where N <= V what that rounding leaves of a target's entry is added to its row of d_dusers in 32 bits, else a row may be
  * off by 2^-8 of that entry too.  For GRAM_F32 it enters them as the sum of two bf16 (to 2^-16 of itself; of three for short products of few users), at half again
  * the cost.  The products' sums are held in 32 bits, to which the tensor cores add 16 products at a time, cutting off (by up to 2^-23 of the sum each time; for GRAM_F32 512
